@@ -194,8 +194,7 @@ def prepare(case, seed):
         if c["op"] == "route":
             s["ws"] = emu.workspace(emu.emu_route_workspace_bytes(c["tokens"], c["experts"], c["k"]))
         elif c["op"] == "grouped":
-            X, W = s["X"], s["W"]
-            s["ws"] = emu.grouped_workspace(X, W, s["ends"], emu.OP_T if c["trans"] else emu.OP_N, s["src"],
+            s["ws"] = emu.grouped_workspace(s["X"], s["W"], s["ends"], emu.OP_T if c["trans"] else emu.OP_N, s["src"],
                                             train=c["train"])
     return s
 
@@ -303,15 +302,19 @@ def _own_route(s, emu):
 
 
 def _own_grouped(s, emu):
-    c, X, W, ends = s["case"], s["X"], s["W"], s["ends"]
+    c, X, W, dY, ends, src, ws = s["case"], s["X"], s["W"], s["dY"], s["ends"], s["src"], s["ws"]
     op, back = (emu.OP_T, emu.OP_N) if c["trans"] else (emu.OP_N, emu.OP_T)
-    out = {"Y": emu.grouped_gemm(X, W, ends, opW=op, src=s["src"], ws=s["ws"])[0]}
-    if c["train"]:
-        out["dX"] = emu.grouped_gemm(s["dY"], W, ends, opW=back, ws=s["ws"])[0]
-        if c["trans"]:
-            out["dW"] = emu.grouped_wgrad(s["dY"], X, ends, srcB=s["src"], ws=s["ws"])[0]
-        else:
-            out["dW"] = emu.grouped_wgrad(X, s["dY"], ends, srcA=s["src"], ws=s["ws"])[0]
+    if not c["train"]:
+        return {"Y": emu.grouped_gemm(X, W, ends, opW=op, src=src, ws=ws)[0]}
+    if c["dtype"] == "f32":      # each operand of a training step is in two products: split it once
+        X, dY = emu.grouped_split(X, ends, src=src, ws=ws), emu.grouped_split(dY, ends, ws=ws)
+        W, src = emu.grouped_split(W, ws=ws), None
+    out = {"Y": emu.grouped_gemm(X, W, ends, opW=op, src=src, ws=ws)[0],
+           "dX": emu.grouped_gemm(dY, W, ends, opW=back, ws=ws)[0]}
+    if c["trans"]:
+        out["dW"] = emu.grouped_wgrad(dY, X, ends, srcB=src, ws=ws)[0]
+    else:
+        out["dW"] = emu.grouped_wgrad(X, dY, ends, srcA=src, ws=ws)[0]
     return out
 
 
