@@ -22,8 +22,9 @@ _lib = None
 EMU_OK = 0
 STATUS = {0: "ok", 1: "invalid argument", 2: "misaligned", 3: "workspace too small", 4: "CUDA error",
           5: "unsupported size"}
-FLAG_NONFINITE, FLAG_RANGE, FLAG_SLICE, FLAG_TIMEOUT = 0x1, 0x2, 0x4, 0x8
+FLAG_NONFINITE, FLAG_RANGE, FLAG_SLICE, FLAG_TIMEOUT, FLAG_INDEX = 0x1, 0x2, 0x4, 0x8, 0x10
 OP_N, OP_T = 0, 1
+F32, BF16 = 0, 1
 ZERO_LEVEL = -(2 ** 31)
 
 _SIGS = {
@@ -60,6 +61,16 @@ _SIGS = {
     "emu_gemm_ex_f64": ("i", ["i", "i", "l", "l", "l", "d", "p", "l", "p", "l", "d", "p", "l", "i", "p", "size", "p"]),
     "emu_gemm_f32_host": ("i", ["l", "l", "l", "p", "l", "p", "l", "p", "l", "p", "size", "p"]),
     "emu_gemm_f64_host": ("i", ["l", "l", "l", "p", "l", "p", "l", "p", "l", "i", "p", "size", "p"]),
+    "emu_grouped_plane_rows": ("l", ["l", "l"]),
+    "emu_grouped_split": ("i", ["i", "l", "l", "l", "p", "l", "l", "p", "l", "p", "size", "p"]),
+    "emu_grouped_split_rows": ("i", ["i", "l", "l", "p", "l", "l", "p", "p", "l", "p", "l", "p", "size", "p"]),
+    "emu_grouped_prodsum": ("i", ["i", "i", "l", "l", "l", "l", "p", "l", "i", "p", "l", "l", "p", "p", "i", "l", "p",
+                                  "size", "p"]),
+    "emu_grouped_gemm_workspace_bytes": ("size", ["i", "l", "l", "l", "l"]),
+    "emu_grouped_gemm_f32": ("i", ["i", "l", "l", "l", "l", "p", "l", "l", "p", "p", "l", "l", "p", "p", "l", "p",
+                                   "size", "p"]),
+    "emu_grouped_prodsum_wgrad": ("i", ["i", "l", "l", "l", "l", "p", "l", "p", "l", "p", "p", "i", "l", "l", "p",
+                                        "size", "p"]),
     "emu_read_flags": ("i", ["p", "p", "p"]),
     "emu_selftest_timeout": ("i", ["p", "size", "u32", "p"]),
     "emu_status_string": ("str", ["i"]),
@@ -134,6 +145,13 @@ emu_gemm_ex_f32 = _mk("emu_gemm_ex_f32")
 emu_gemm_ex_f64 = _mk("emu_gemm_ex_f64")
 emu_gemm_f32_host = _mk("emu_gemm_f32_host")
 emu_gemm_f64_host = _mk("emu_gemm_f64_host")
+emu_grouped_plane_rows = _mk("emu_grouped_plane_rows")
+emu_grouped_split = _mk("emu_grouped_split")
+emu_grouped_split_rows = _mk("emu_grouped_split_rows")
+emu_grouped_prodsum = _mk("emu_grouped_prodsum")
+emu_grouped_gemm_workspace_bytes = _mk("emu_grouped_gemm_workspace_bytes")
+emu_grouped_gemm_f32 = _mk("emu_grouped_gemm_f32")
+emu_grouped_prodsum_wgrad = _mk("emu_grouped_prodsum_wgrad")
 emu_read_flags = _mk("emu_read_flags")
 emu_selftest_timeout = _mk("emu_selftest_timeout")
 emu_status_string = _mk("emu_status_string")
@@ -350,3 +368,174 @@ def prodsum_f64(Ap, Bp, M: int, N: int, K: int, nprod: int, vA=None, vB=None, C=
                            int(nprod), C.data_ptr(), C.stride(0), ws.data_ptr(), ws.numel(), _stream(stream)),
            "emu_prodsum_f64")
     return C, ws
+
+
+# ------------------------------------------------------------- expert layers
+def _need(ok, what):
+    if not ok:
+        raise ValueError(what)
+
+
+def _empty(shape, dtype, device, stream):
+    """torch.empty whose memory belongs to the stream that the kernels use."""
+    torch = _torch()
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    s = stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=device)
+    with torch.cuda.stream(s):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _dtype(t, where):
+    torch = _torch()
+    _need(t.dtype in (torch.float32, torch.bfloat16), f"{where}: float32 or bfloat16 is needed, got {t.dtype}")
+    return F32 if t.dtype == torch.float32 else BF16
+
+
+def _ints(t, numel, device, where):
+    torch = _torch()
+    _need(t.dtype == torch.int32 and t.is_contiguous() and t.device == device,
+          f"{where}: a contiguous int32 tensor on {device} is needed")
+    _need(numel is None or t.numel() == numel, f"{where}: {numel} entries are needed, got {t.numel()}")
+    return t.data_ptr()
+
+
+def _rows_of(t, where):
+    """Row pitch of a 2-D (or last two dimensions of a 3-D) tensor with contiguous rows."""
+    _need(t.is_cuda, f"{where}: a CUDA tensor is needed")
+    _need(t.shape[-1] <= 1 or t.stride(-1) == 1, f"{where}: rows have to be contiguous")
+    pitch = t.stride(-2) if t.shape[-2] > 1 else t.shape[-1]
+    _need(pitch >= t.shape[-1], f"{where}: rows overlap")
+    return max(pitch, 1)
+
+
+class GroupedPlanes:
+    """BF16 planes of an operand of the products grouped by expert, from
+    grouped_split: planes int16 [S, plane rows, ld]; `shape` is the operand's
+    (rows, cols) for token rows in group order, (G, rows, cols) for weights."""
+
+    def __init__(self, planes, shape, padded):
+        self.planes, self.shape, self.padded = planes, tuple(shape), padded
+        self.device, self.nslices, self.ld = planes.device, planes.shape[0], planes.shape[2]
+
+
+def grouped_split(X, ends=None, src=None, planes=None, ws=None, stream=None):
+    """emu_grouped_split / emu_grouped_split_rows: the planes of weights X
+    [G, rows, cols] (ends None), or of token rows X[src] (src None: X) grouped
+    by ends; three for FP32 (Eq. (fp32split)), one for BF16.  A plane set can
+    stand for its operand in grouped_gemm and grouped_wgrad, in all directions."""
+    torch = _torch()
+    dt, ldx = _dtype(X, "grouped_split"), _rows_of(X, "grouped_split")
+    cols = X.shape[-1]
+    S, ld = (3 if dt == F32 else 1), gemm_ldk(cols)
+    ws = ws if ws is not None else _empty(emu_split_workspace_bytes(32), torch.uint8, X.device, stream)
+    if ends is None:
+        _need(X.dim() == 3 and src is None, "grouped_split: weights are [G, rows, cols]; token rows need ends")
+        G, rows = X.shape[0], X.shape[1]
+        shape, prows = (G, rows, cols), G * rows
+    else:
+        _need(X.dim() == 2, "grouped_split: token rows are [rows, cols]")
+        G, rows = ends.numel(), (src.numel() if src is not None else X.shape[0])
+        shape, prows = (rows, cols), emu_grouped_plane_rows(rows, G)
+    if planes is None:
+        planes = _empty((S, prows, ld), torch.int16, X.device, stream)
+    _need(tuple(planes.shape) == (S, prows, ld) and planes.dtype == torch.int16 and planes.is_contiguous(),
+          f"grouped_split: planes have to be contiguous int16 {(S, prows, ld)}")
+    if ends is None:
+        r = emu_grouped_split(dt, G, rows, cols, X.data_ptr(), ldx, X.stride(0) if G > 1 else 0, planes.data_ptr(),
+                              ld, ws.data_ptr(), ws.numel(), _stream(stream))
+    else:
+        r = emu_grouped_split_rows(dt, rows, cols, X.data_ptr(), X.shape[0], ldx,
+                                   _ints(src, None, X.device, "grouped_split: src") if src is not None else None,
+                                   _ints(ends, G, X.device, "grouped_split: ends"), G, planes.data_ptr(), ld,
+                                   ws.data_ptr(), ws.numel(), _stream(stream))
+    _check(r, "emu_grouped_split")
+    return GroupedPlanes(planes, shape, ends is not None)
+
+
+def _tma_ok(t):
+    """Whether a BF16 tensor can be read by the tensor memory accelerator as it stands."""
+    return (t.data_ptr() % 16 == 0 and _rows_of(t, "operand") % 8 == 0 and
+            (t.dim() < 3 or t.shape[0] <= 1 or (t.stride(0) % 8 == 0 and t.stride(0) >= 0)))
+
+
+def grouped_workspace(X, W, ends, opW: int = OP_N, src=None, train: bool = False):
+    """A workspace for grouped_gemm(X, W, ends, opW, src) and, with train, for
+    the splits and gradients of the same operands."""
+    rows = src.numel() if src is not None else X.shape[0]
+    G = ends.numel()
+    K, N = (W.shape[2], W.shape[1]) if opW == OP_T else (W.shape[1], W.shape[2])
+    f32 = not isinstance(X, GroupedPlanes) and X.dtype == _torch().float32 and not train
+    return workspace(emu_grouped_gemm_workspace_bytes(F32 if f32 else BF16, G, rows, N, K), X.device)
+
+
+def grouped_gemm(X, W, ends, opW: int = OP_N, src=None, Y=None, ws=None, stream=None):
+    """Y[r] = X[src[r]] op(W_g) for the rows r of group g (src None: X[r]);
+    W [G, K, N] (OP_N) or [G, N, K] (OP_T).  FP32 operands multiply by six BF16
+    products (Algorithm 1), BF16 ones by one; X and W may each be a plane set
+    of grouped_split.  Y: FP32, or BF16 / FP32 for BF16 operands (given Y
+    decides; BF16 otherwise).  Returns (Y, ws).  The gradient of X is
+    grouped_gemm(dY, W, ends, the other op)."""
+    torch = _torch()
+    G, dev = ends.numel(), X.device
+    xp, wp = isinstance(X, GroupedPlanes), isinstance(W, GroupedPlanes)
+    _need(len(W.shape) == 3 and W.shape[0] == G, f"grouped_gemm: W has to be [{G}, ., .], got {tuple(W.shape)}")
+    _need(len(X.shape) == 2 and (not xp or (X.padded and src is None)), "grouped_gemm: X has to be token rows")
+    K, N = (W.shape[2], W.shape[1]) if opW == OP_T else (W.shape[1], W.shape[2])
+    _need(X.shape[1] == K, f"grouped_gemm: X has {X.shape[1]} columns, op(W) {K} rows")
+    S = X.nslices if xp else (3 if _dtype(X, "grouped_gemm: X") == F32 else 1)
+    _need(S == (W.nslices if wp else (3 if _dtype(W, "grouped_gemm: W") == F32 else 1)),
+          "grouped_gemm: X and W have to be of one type")
+    rows = src.numel() if src is not None else X.shape[0]
+    if Y is None:
+        Y = _empty((rows, N), torch.float32 if S == 3 else torch.bfloat16, dev, stream)
+    yt, ldy = _dtype(Y, "grouped_gemm: Y"), _rows_of(Y, "grouped_gemm: Y")
+    _need(tuple(Y.shape) == (rows, N) and (S == 1 or yt == F32), "grouped_gemm: Y has another shape or type")
+    pe = _ints(ends, G, dev, "grouped_gemm: ends")
+    ps = _ints(src, None, dev, "grouped_gemm: src") if src is not None else None
+    if S == 3 and not xp and not wp:
+        ws = ws if ws is not None else _empty(emu_grouped_gemm_workspace_bytes(F32, G, rows, N, K), torch.uint8, dev,
+                                              stream)
+        _check(emu_grouped_gemm_f32(opW, G, rows, N, K, X.data_ptr(), X.shape[0], _rows_of(X, "X"), ps, W.data_ptr(),
+                                    _rows_of(W, "W"), W.stride(0) if G > 1 else 0, pe, Y.data_ptr(), ldy,
+                                    ws.data_ptr(), ws.numel(), _stream(stream)), "emu_grouped_gemm_f32")
+        return Y, ws
+    ws = ws if ws is not None else _empty(emu_split_workspace_bytes(32), torch.uint8, dev, stream)
+    if not xp and (S == 3 or src is not None or not _tma_ok(X)):
+        X, xp = grouped_split(X, ends, src, ws=ws, stream=stream), True
+    if not wp and (S == 3 or not _tma_ok(W)):
+        W, wp = grouped_split(W, ws=ws, stream=stream), True
+    xptr, ldx = (X.planes.data_ptr(), X.ld) if xp else (X.data_ptr(), _rows_of(X, "X"))
+    wptr, ldw = (W.planes.data_ptr(), W.ld) if wp else (W.data_ptr(), _rows_of(W, "W"))
+    stride = W.shape[1] * ldw if wp or G <= 1 else W.stride(0)
+    _check(emu_grouped_prodsum(S, opW, G, rows, N, K, xptr, ldx, int(xp), wptr, ldw, stride, pe, Y.data_ptr(), yt, ldy,
+                               ws.data_ptr(), ws.numel(), _stream(stream)), "emu_grouped_prodsum")
+    return Y, ws
+
+
+def grouped_wgrad(A, B, ends, srcA=None, srcB=None, D=None, ws=None, stream=None):
+    """D_g = A[srcA]^T B[srcB] over the rows of group g: D [G, M, N].  The
+    gradient of W is grouped_wgrad(X, dY) for OP_N and grouped_wgrad(dY, X)
+    for OP_T.  A and B: token rows of one type, or plane sets of
+    grouped_split.  D as Y in grouped_gemm.  Returns (D, ws)."""
+    torch = _torch()
+    G, dev = ends.numel(), A.device
+    ws = ws if ws is not None else _empty(emu_split_workspace_bytes(32), torch.uint8, dev, stream)
+    ops = []
+    for t, src, name in ((A, srcA, "A"), (B, srcB, "B")):
+        if not isinstance(t, GroupedPlanes):
+            t = grouped_split(t, ends, src, ws=ws, stream=stream)
+        _need(t.padded, f"grouped_wgrad: {name} has to be token rows")
+        ops.append(t)
+    A, B = ops
+    _need(A.shape[0] == B.shape[0] and A.nslices == B.nslices, "grouped_wgrad: A and B differ in rows or type")
+    (rows, M), N, S = A.shape, B.shape[1], A.nslices
+    if D is None:
+        D = _empty((G, M, N), torch.float32 if S == 3 else torch.bfloat16, dev, stream)
+    dt, ldd = _dtype(D, "grouped_wgrad: D"), _rows_of(D, "grouped_wgrad: D")
+    _need(tuple(D.shape) == (G, M, N) and (S == 1 or dt == F32), "grouped_wgrad: D has another shape or type")
+    _check(emu_grouped_prodsum_wgrad(S, G, rows, M, N, A.planes.data_ptr(), A.ld, B.planes.data_ptr(), B.ld,
+                                     _ints(ends, G, dev, "grouped_wgrad: ends"), D.data_ptr(), dt, ldd,
+                                     D.stride(0) if G > 1 else M * ldd, ws.data_ptr(), ws.numel(), _stream(stream)),
+           "emu_grouped_prodsum_wgrad")
+    return D, ws

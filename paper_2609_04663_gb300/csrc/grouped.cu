@@ -1,0 +1,614 @@
+// Matrix products grouped by expert, on tcgen05 BF16 MMAs with FP32
+// accumulators in tensor memory.
+//
+//   product:   Y[r, n]    = sum_k X[r, k] W_g[k, n]   for the rows r of group g
+//   gradient:  D_g[m, n]  = sum over the rows r of group g of A[r, m] B[r, n]
+//
+// Operands are sets of S BF16 planes: S = 3 for FP32 operands (Eq.
+// (fp32split); the six products of Eq. (fp32six) are issued from one stage,
+// in the order of Eq. (fp32reuseorder), into one accumulator), S = 1 for BF16
+// operands, whose plane is the operand itself.
+//
+// Both forms compute tiles of the TRANSPOSED result: the contiguous output
+// dimension n (the weights' features) lies on the 128 MMA rows = TMEM lanes,
+// and the other dimension (a group's rows, or m) on the up to 256 MMA columns.
+// A group's ragged row count then only changes the MMA's N, which goes in
+// steps of 16 (32 on CTA pairs), so a group of 300 rows costs 320 columns and
+// not 384 or 512 rows; a few rows for each expert cost little more than reading
+// the weights; and an accumulator column is 32 consecutive output elements
+// per warp, stored without staging and with any row pitch.
+//
+// The grid is persistent: one CTA (or CTA pair) per SM (pair) walks the tiles
+// of all groups, which every CTA derives from `ends` on the device.  Warp 0
+// issues TMA loads, warp 1 the MMAs, warps 2-9 read TMEM and store.  Every
+// wait is bounded (EMU_FLAG_TIMEOUT).
+//
+// BF16 operands: two accumulators alternate in TMEM, so the stores of one tile
+// overlap the MMAs of the next.
+//
+// FP32 operands: the tensor cores truncate when they add to an FP32
+// accumulator, a bias of about 1.8e-8 of the result per 16-wide step; six
+// products over K = 256 in one accumulator came out at 1.7e-6 (2-norm).  So
+// the leading product A0B0 has an accumulator of its own that is read every
+// 256 elements of K (the K-chunk of Section 6.1) and added, correctly rounded,
+// to a running FP32 sum in registers; the five products with i + j > 0, 2^-8
+// of it and less, share a second accumulator over all of K.  While the
+// epilogue warps read a chunk's leading sum, the MMAs of the five others of
+// the next K-block run.
+#include "gemm_common.cuh"
+#include "grouped_common.cuh"
+#include "launchers.cuh"
+#include "pair_common.cuh"
+
+namespace emu {
+
+namespace {
+
+constexpr int kLRows = 128;           // MMA rows (output features) per CTA
+constexpr int kKB = 64;               // K-block: one 128-byte swizzle row of BF16
+constexpr int kSmemMax = 232448;      // shared memory per CTA
+
+// The products of Eq. (fp32six) below the leading one.
+__constant__ int8_t kGroupChain[5][2] = {{1, 1}, {1, 0}, {2, 0}, {0, 2}, {0, 1}};
+constexpr int kChunkBlocks = kKChunk / kKB;   // K-blocks of one chunk of the leading product
+constexpr int kEpiWarps = 8;
+
+struct GroupedArgs {
+    const int32_t *ends;
+    int G, rows;
+    int L;                 // output features (the lane dimension)
+    int C;                 // gradient: output rows m
+    int K;                 // product: contraction length
+    int padded;            // product: X's rows are at padded positions
+    void *out;
+    int64_t ldo, strideo;  // row pitch; gradient: distance between the groups' results
+    int out_f32;
+    uint32_t *flags;
+};
+
+// S slices, BC MMA columns at most, PAIR: a tile's 256 features on two CTAs.
+template <int S, int BC, bool PAIR>
+struct GroupedCfg {
+    static constexpr int CTAS = PAIR ? 2 : 1;
+    static constexpr int CROWS = BC / CTAS;                       // column-operand rows staged per CTA
+    static constexpr int STEP = PAIR ? 32 : 16;                   // granularity of the MMA's N
+    static constexpr int L_TILE = kLRows * kKB * 2;
+    static constexpr int C_TILE = CROWS * kKB * 2;
+    static constexpr int STAGE = S * (L_TILE + C_TILE);
+    static constexpr int FIXED = 1024 + 512 + 2 * (kMaxGroups + 1) * 4;   // alignment, barriers, group tables
+    static constexpr int FIT = (kSmemMax - FIXED) / STAGE;
+    static constexpr int STAGES = FIT > 8 ? 8 : FIT;
+    static constexpr int BAR_OFF = STAGES * STAGE;
+    static constexpr int TAB_OFF = BAR_OFF + 512;
+    static constexpr int SMEM = STAGES * STAGE + FIXED;
+    static constexpr int THREADS = 64 + 32 * kEpiWarps;
+    static constexpr int HALF = BC >= 64 ? BC / 2 : 32;           // accumulator columns of one epilogue warp
+    static_assert(STAGES >= 2, "stages");
+    static_assert(BC <= 256 && CROWS % 64 == 0 || BC < 128, "column tile");
+};
+
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap *map, uint32_t bar, int32_t c0, int32_t c1,
+                                            int32_t c2, int32_t c3)
+{
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+                 " [%0], [%1, {%3, %4, %5, %6}], [%2];"
+                 ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
+                 : "memory");
+}
+__device__ __forceinline__ void tma_load_4d_pair(uint32_t dst, const CUtensorMap *map, uint32_t bar, int32_t c0,
+                                                 int32_t c1, int32_t c2, int32_t c3)
+{
+    asm volatile("cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+                 " [%0], [%1, {%3, %4, %5, %6}], [%2];"
+                 ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
+                 : "memory");
+}
+
+// 16 FP32 accumulator columns of the warp's lanes.
+__device__ __forceinline__ void tmem_load16(uint32_t taddr, uint32_t (&r)[16])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr)
+        : "memory");
+}
+
+// Shared-memory descriptor of a 128-byte-swizzled tile.  K-major: rows of 64
+// K elements, 8-row groups 1024 bytes apart; the next 16 K elements start 32
+// bytes on.  MN-major: boxes of 64 MN elements (one 128-byte row) by kKB rows
+// of K, the boxes `lbo` bytes apart, 8-row groups of K 1024 bytes apart; the
+// next 16 K rows start 2048 bytes on.
+__device__ __forceinline__ uint64_t group_desc(uint32_t saddr, uint32_t lbo)
+{
+    uint64_t d = (uint64_t)((saddr & 0x3FFFFu) >> 4);
+    d |= (uint64_t)(lbo >> 4) << 16;
+    d |= (uint64_t)(1024u >> 4) << 32;
+    d |= (uint64_t)1u << 46;
+    d |= (uint64_t)2u << 61;
+    return d;
+}
+
+// One output tile: features l0 .. (this CTA's 128), columns c0 .. c0 + cols
+// of group g (rows of the group, or m), contraction of nk elements from k0.
+struct Tile {
+    int g, l0, c0, cols, csz, k0, nk;
+};
+
+template <int S, int BC, bool PAIR, bool LMN, bool CMN>
+__device__ __forceinline__ Tile tile_at(int t, const GroupedArgs &a, const int *starts, const int *tpre, int rank)
+{
+    using Cfg = GroupedCfg<S, BC, PAIR>;
+    constexpr int LT = kLRows * Cfg::CTAS;
+    const int nlt = (a.L + LT - 1) / LT;
+    Tile x;
+    int local, n;
+    if constexpr (CMN) {
+        const int per = nlt * ((a.C + BC - 1) / BC);
+        x.g = t / per;
+        local = t - x.g * per;
+        n = a.C;
+    } else {
+        x.g = find_group(tpre, a.G, t);
+        local = t - tpre[x.g];
+        n = starts[x.g + 1] - starts[x.g];
+    }
+    // column tiles of equal size; 8 of them walk the feature tiles together
+    const int nct = (n + BC - 1) / BC;
+    int ct, lt;
+    tile_coords(local, nct, nlt, ct, lt);
+    const int each = ((n + nct - 1) / nct + Cfg::STEP - 1) / Cfg::STEP * Cfg::STEP;
+    x.c0 = ct * each;
+    x.cols = min(each, n - x.c0);
+    x.csz = (x.cols + Cfg::STEP - 1) / Cfg::STEP * Cfg::STEP;
+    x.l0 = lt * LT + rank * kLRows;
+    if constexpr (CMN) {
+        x.k0 = (int)padded_start(starts[x.g], x.g);
+        x.nk = starts[x.g + 1] - starts[x.g];
+    } else {
+        x.k0 = 0;
+        x.nk = a.K;
+    }
+    return x;
+}
+
+// 32 accumulator columns of this warp's lanes -> rows 0 .. cols - 1 of out:
+// column j is output row j, lane i feature l + i.  BF16: two columns at a
+// time, neighbouring lanes exchange values so that each stores two features
+// of one row.
+__device__ __forceinline__ void store_columns(const float (&v)[32], int cols, void *out, int64_t ldo, int l, int L,
+                                              bool out_f32, bool pairs_ok)
+{
+    const int lane = (int)lane_id();
+    if (out_f32) {
+        float *o = static_cast<float *>(out) + l + lane;
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+            if (l + lane < L && j < cols) o[(int64_t)j * ldo] = v[j];
+    } else {
+        const bool odd = lane & 1;
+        const int i = lane & ~1;
+        uint16_t *o = static_cast<uint16_t *>(out) + (odd ? ldo : 0) + l + i;
+#pragma unroll
+        for (int j = 0; j < 32; j += 2) {
+            const float keep = odd ? v[j + 1] : v[j];
+            const float got = __shfl_xor_sync(0xFFFFFFFFu, odd ? v[j] : v[j + 1], 1);
+            uint32_t w;                               // features i (low half) and i + 1 of row j + odd
+            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(odd ? keep : got), "f"(odd ? got : keep));
+            if (j + (odd ? 1 : 0) < cols) {
+                uint16_t *p = o + (int64_t)j * ldo;
+                if (pairs_ok && l + i + 1 < L) {
+                    *reinterpret_cast<uint32_t *>(p) = w;
+                } else {
+                    if (l + i < L) p[0] = (uint16_t)w;
+                    if (l + i + 1 < L) p[1] = (uint16_t)(w >> 16);
+                }
+            }
+        }
+    }
+}
+
+// LMN / CMN: the feature / column operand is stored with its MN dimension
+// contiguous (else with the contraction contiguous).  CMN is the gradient.
+template <int S, int BC, bool PAIR, bool LMN, bool CMN>
+__global__ void __launch_bounds__(64 + 32 * kEpiWarps, 1)
+grouped_kernel(const __grid_constant__ CUtensorMap tmL, const __grid_constant__ CUtensorMap tmC, const GroupedArgs a)
+{
+    using Cfg = GroupedCfg<S, BC, PAIR>;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw = smem_u32(smem_raw);
+    const uint32_t base = (raw + 1023u) & ~1023u;
+    uint8_t *base_ptr = smem_raw + (base - raw);
+    const uint32_t full0 = base + Cfg::BAR_OFF, empty0 = full0 + 8u * Cfg::STAGES;
+    // BF16: tfull / tempty of the two accumulators; FP32: [0] of the leading
+    // accumulator (per chunk), tempty[1] of the other one (per tile)
+    const uint32_t tfull0 = empty0 + 8u * Cfg::STAGES, tempty0 = tfull0 + 16u, done_bar = tempty0 + 16u;
+    volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(base_ptr + Cfg::BAR_OFF + 16 * Cfg::STAGES + 48);
+    int *starts = reinterpret_cast<int *>(base_ptr + Cfg::TAB_OFF), *tpre = starts + a.G + 1;
+
+    const int warp = threadIdx.x >> 5, lane = (int)lane_id();
+    const int rank = PAIR ? (int)cluster_rank() : 0;
+    uint32_t *flags = a.flags;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < Cfg::STAGES; ++s) { mbar_init(full0 + 8u * s, 1); mbar_init(empty0 + 8u * s, 1); }
+        for (int b = 0; b < 2; ++b) { mbar_init(tfull0 + 8u * b, 1); mbar_init(tempty0 + 8u * b, kEpiWarps * Cfg::CTAS); }
+        mbar_init(done_bar, 1);
+        fence_mbar_init();
+        tma_prefetch_desc(&tmL);
+        tma_prefetch_desc(&tmC);
+    }
+    if constexpr (PAIR) {
+        __syncthreads();
+        cluster_sync();                                   // both CTAs' barriers initialised
+        if (warp == 1) tmem_alloc_pair(smem_u32((const void *)tmem_slot), 512);
+    } else {
+        if (warp == 1) { tmem_alloc(smem_u32((const void *)tmem_slot), 512); tmem_relinquish(); }
+    }
+    // the set-up above overlaps the end of the kernel before this one when it
+    // is launched as its programmatic dependent
+    griddep_wait();
+    if (load_groups(a.ends, a.G, a.rows, starts) && blockIdx.x == 0 && threadIdx.x == 0)
+        atomicOr(flags, (uint32_t)EMU_FLAG_INDEX);
+    constexpr int LT = kLRows * Cfg::CTAS;
+    const int nlt = (a.L + LT - 1) / LT;
+    int total;
+    if constexpr (CMN) {
+        total = a.G * nlt * ((a.C + BC - 1) / BC);
+    } else {
+        // tile prefix over the groups (one warp, 32 groups a step)
+        if (warp == 2) {
+            int carry = 0;
+            for (int g0 = 0; g0 < a.G; g0 += 32) {
+                const int g = g0 + lane;
+                int v = g < a.G ? (starts[g + 1] - starts[g] + BC - 1) / BC * nlt : 0;
+#pragma unroll
+                for (int d = 1; d < 32; d <<= 1) {
+                    const int u = __shfl_up_sync(0xFFFFFFFFu, v, d);
+                    if (lane >= d) v += u;
+                }
+                if (g < a.G) tpre[g + 1] = carry + v;
+                carry += __shfl_sync(0xFFFFFFFFu, v, 31);
+            }
+            if (lane == 0) tpre[0] = 0;
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if constexpr (!CMN) total = tpre[a.G];
+    const uint32_t tmem = *tmem_slot;
+    const int first = (int)blockIdx.x / Cfg::CTAS, step = (int)gridDim.x / Cfg::CTAS;
+
+    if (warp == 0 && lane == 0) {
+        // ---------------- TMA producer
+        long issued = 0;
+        int s = 0;
+        uint32_t ph = 0;
+        bool ok = true;
+        for (int t = first; t < total && ok; t += step) {
+            const Tile x = tile_at<S, BC, PAIR, LMN, CMN>(t, a, starts, tpre, rank);
+            const int nkb = (x.nk + kKB - 1) / kKB, crows = x.csz / Cfg::CTAS, cfirst = rank * crows;
+            const int cboxes = CMN ? (crows + 63) / 64 : crows / 16;
+            const uint32_t bytes = (uint32_t)(S * (Cfg::L_TILE + cboxes * (CMN ? 64 * kKB * 2 : 16 * kKB * 2)));
+            const int crow0 = CMN ? 0 : (a.padded ? (int)padded_start(starts[x.g], x.g) : starts[x.g]) + x.c0 + cfirst;
+            for (int kb = 0; kb < nkb; ++kb) {
+                if (!(ok = mbar_wait(empty0 + 8u * s, ph ^ 1u, flags))) break;
+                const uint32_t st = base + (uint32_t)(s * Cfg::STAGE), fb = full0 + 8u * s;
+                const uint32_t bar = PAIR ? peer_addr(fb, 0) : fb;
+                if (rank == 0) mbar_arrive_expect_tx(fb, bytes * Cfg::CTAS);
+                const int k = x.k0 + kb * kKB;
+                auto load = [&](uint32_t dst, const CUtensorMap *m, int c0, int c1, int c2, int c3) {
+                    if constexpr (PAIR) tma_load_4d_pair(dst, m, bar, c0, c1, c2, c3);
+                    else tma_load_4d(dst, m, bar, c0, c1, c2, c3);
+                };
+#pragma unroll
+                for (int r = 0; r < S; ++r) {
+                    const uint32_t dl = st + (uint32_t)(r * Cfg::L_TILE);
+                    if constexpr (LMN) {
+                        // boxes of 64 features x 64 contraction rows (a weight matrix's rows, or token rows)
+                        load(dl, &tmL, x.l0, k, CMN ? 0 : x.g, r);
+                        load(dl + Cfg::L_TILE / 2, &tmL, x.l0 + 64, k, CMN ? 0 : x.g, r);
+                    } else {
+                        load(dl, &tmL, k, x.l0, x.g, r);
+                    }
+                    const uint32_t dc = st + (uint32_t)(S * Cfg::L_TILE + r * Cfg::C_TILE);
+                    if constexpr (CMN) {
+                        for (int b = 0; b < cboxes; ++b)
+                            load(dc + (uint32_t)(b * 64 * kKB * 2), &tmC, x.c0 + cfirst + 64 * b, k, 0, r);
+                    } else {
+                        for (int b = 0; b < cboxes; ++b)
+                            load(dc + (uint32_t)(b * 16 * kKB * 2), &tmC, k, crow0 + 16 * b, 0, r);
+                    }
+                }
+                ++issued;
+                if (++s == Cfg::STAGES) { s = 0; ph ^= 1u; }
+            }
+        }
+        if (!ok) {
+            if (rank == 0) {
+                drain_inflight(full0, Cfg::STAGES, issued, flags);
+            } else {
+                // the peer's copies complete on the leader's barriers, which it
+                // cannot observe: give them 200 us before the CTA winds down
+                const unsigned long long t0 = globaltimer_ns();
+                while (globaltimer_ns() - t0 < 200000ull) {}
+            }
+        }
+    } else if (warp == 1 && lane == 0 && rank == 0) {
+        // ---------------- MMA issuer (a pair's leader)
+        int s = 0, it = 0;
+        uint32_t ph = 0, cph = 0;                     // cph: chunks issued (FP32)
+        bool ok = true;
+        constexpr uint32_t kstepL = LMN ? 2048u : 32u, kstepC = CMN ? 2048u : 32u, lbo = 64u * kKB * 2u;
+        auto commit = [&](uint32_t bar) {
+            if constexpr (PAIR) mma_commit_pair(bar);
+            else mma_commit(bar);
+        };
+        for (int t = first; t < total && ok; t += step, ++it) {
+            const Tile x = tile_at<S, BC, PAIR, LMN, CMN>(t, a, starts, tpre, rank);
+            const int nkb = (x.nk + kKB - 1) / kKB, b = it & 1;
+            if (nkb == 0) { --it; continue; }         // an empty group: the epilogue writes zeros by itself
+            const uint32_t idesc = make_idesc_bf16(kLRows * Cfg::CTAS, x.csz) | (LMN ? 1u << 15 : 0u) |
+                                   (CMN ? 1u << 16 : 0u);
+            const uint32_t d = tmem + (S == 1 ? (uint32_t)(b * 256) : 0u), d2 = tmem + 256u;
+            if (S == 1) ok = mbar_wait(tempty0 + 8u * b, (((uint32_t)it >> 1) & 1u) ^ 1u, flags);
+            else ok = mbar_wait(tempty0 + 8u, ((uint32_t)it & 1u) ^ 1u, flags);
+            if (!ok) break;
+            tc_fence_after();
+            for (int kb = 0; kb < nkb; ++kb) {
+                if (!(ok = mbar_wait(full0 + 8u * s, ph, flags))) break;
+                tc_fence_after();
+                const uint32_t st = base + (uint32_t)(s * Cfg::STAGE);
+                // 16-wide steps that hold contraction elements (the rest of the stage may hold anything)
+                const int steps = min(kKB / 16, (x.nk - kb * kKB + 15) / 16);
+                auto mma = [&](uint32_t acc, int il, int ic, int kk, bool add) {
+                    const uint64_t ld = group_desc(st + (uint32_t)(il * Cfg::L_TILE) + kk * kstepL, LMN ? lbo : 16u);
+                    const uint64_t cd = group_desc(st + (uint32_t)(S * Cfg::L_TILE + ic * Cfg::C_TILE) + kk * kstepC,
+                                                   CMN ? lbo : 16u);
+                    if constexpr (PAIR) mma_bf16_pair(acc, ld, cd, idesc, add);
+                    else mma_bf16(acc, ld, cd, idesc, add);
+                };
+                if constexpr (S == 3) {
+                    const int kc = kb % kChunkBlocks;
+                    for (int kk = 0; kk < steps; ++kk)
+#pragma unroll
+                        for (int q = 0; q < 5; ++q)
+                            mma(d2, kGroupChain[q][0], kGroupChain[q][1], kk, (kb | kk | q) != 0);
+                    if (kc == 0) {                    // the last chunk's leading sum has been read
+                        if (!(ok = mbar_wait(tempty0, (cph & 1u) ^ 1u, flags))) break;
+                        tc_fence_after();
+                    }
+                    for (int kk = 0; kk < steps; ++kk) mma(d, 0, 0, kk, (kc | kk) != 0);
+                    commit(empty0 + 8u * s);
+                    if (kc == kChunkBlocks - 1 || kb == nkb - 1) { commit(tfull0); ++cph; }
+                } else {
+                    for (int kk = 0; kk < steps; ++kk) mma(d, 0, 0, kk, (kb | kk) != 0);
+                    commit(empty0 + 8u * s);
+                }
+                if (++s == Cfg::STAGES) { s = 0; ph ^= 1u; }
+            }
+            if (ok && S == 1) commit(tfull0 + 8u * b);
+        }
+        commit(done_bar);
+        (void)mbar_wait(done_bar, 0, flags);
+    } else if (warp >= 2) {
+        // ---------------- epilogue: this CTA's 128 features of each tile; a warp
+        // has a quarter of the lanes and half of the columns
+        const int quarter = warp & 3, h0 = ((warp - 2) >> 2) * Cfg::HALF;
+        const int esize = a.out_f32 ? 4 : 2;
+        const bool pairs_ok = (a.ldo & 1) == 0 && (a.strideo & 1) == 0 && (reinterpret_cast<uintptr_t>(a.out) & 3u) == 0;
+        const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)h0;
+        if constexpr (!CMN) {
+            // rows of no group are zero
+            const int tid = (int)threadIdx.x - 64;
+            for (int64_t r = (int64_t)starts[a.G] + blockIdx.x; r < a.rows; r += gridDim.x)
+                for (int n = tid; n < a.L; n += 32 * kEpiWarps) {
+                    if (a.out_f32) static_cast<float *>(a.out)[r * a.ldo + n] = 0.0f;
+                    else static_cast<uint16_t *>(a.out)[r * a.ldo + n] = 0;
+                }
+        }
+        auto release = [&](uint32_t bar) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                if constexpr (PAIR) mbar_arrive_peer(peer_addr(bar, 0));
+                else mbar_arrive(bar);
+            }
+        };
+        int it = 0;
+        uint32_t cph = 0;
+        bool ok = true;
+        for (int t = first; t < total && ok; t += step, ++it) {
+            const Tile x = tile_at<S, BC, PAIR, LMN, CMN>(t, a, starts, tpre, rank);
+            const int l = x.l0 + quarter * 32, b = it & 1;
+            const int cols = x.cols - h0;             // columns from this warp's first on
+            const int64_t row0 = (CMN ? 0 : (int64_t)starts[x.g]) + x.c0 + h0;
+            char *o = static_cast<char *>(a.out) + (row0 * a.ldo + (CMN ? x.g * a.strideo : 0)) * esize;
+            auto store32 = [&](const float (&v)[32], int c) {
+                if (l < a.L && c < cols)
+                    store_columns(v, cols - c, o + (int64_t)c * a.ldo * esize, a.ldo, l, a.L, a.out_f32 != 0, pairs_ok);
+            };
+            if (x.nk == 0) {
+                --it;
+                const float z[32] = {};
+                for (int c = 0; c < Cfg::HALF; c += 32) store32(z, c);
+                continue;
+            }
+            // tcgen05.ld needs the whole warp, so a timeout in any lane ends the warp's work
+            if constexpr (S == 3) {
+                float acc[Cfg::HALF];
+#pragma unroll
+                for (int j = 0; j < Cfg::HALF; ++j) acc[j] = 0.0f;
+                const int nch = (x.nk + kKChunk - 1) / kKChunk;
+                for (int c = 0; c <= nch; ++c) {      // the chunks' leading sums, then the other products
+                    if (c < nch) {
+                        ok = __all_sync(0xFFFFFFFFu, mbar_wait(tfull0, cph & 1u, flags));
+                        if (!ok) break;
+                        ++cph;
+                        tc_fence_after();
+                    }
+#pragma unroll
+                    for (int h = 0; h < Cfg::HALF; h += 16) {
+                        if (h < cols) {
+                            uint32_t v[16];
+                            tmem_load16(lanes + (uint32_t)(c < nch ? h : 256 + h), v);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) acc[h + j] = __fadd_rn(acc[h + j], __uint_as_float(v[j]));
+                        }
+                    }
+                    release(c < nch ? tempty0 : tempty0 + 8u);
+                }
+                if (ok) {
+#pragma unroll
+                    for (int h = 0; h < Cfg::HALF; h += 32) {
+                        float v[32];
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] = acc[h + j];
+                        store32(v, h);
+                    }
+                }
+            } else {
+                ok = __all_sync(0xFFFFFFFFu, mbar_wait(tfull0 + 8u * b, ((uint32_t)it >> 1) & 1u, flags));
+                if (!ok) break;
+                tc_fence_after();
+#pragma unroll 1
+                for (int h = 0; h < Cfg::HALF; h += 32) {
+                    if (h < cols) {
+                        uint32_t u[32];
+                        float v[32];
+                        tmem_ld32(lanes + (uint32_t)(b * 256 + h), u);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(u[j]);
+                        store32(v, h);
+                    }
+                }
+                release(tempty0 + 8u * b);
+            }
+        }
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if constexpr (PAIR) cluster_sync();               // the leader's MMAs are done with both CTAs
+    if (warp == 1) {
+        __syncwarp();
+        tc_fence_after();
+        if constexpr (PAIR) tmem_dealloc_pair(tmem, 512);
+        else tmem_dealloc(tmem, 512);
+    }
+}
+
+// Tensor map over a plane set: dims (inner, rows, batch, S), box (64, box_rows).
+bool make_group_map(CUtensorMap *map, const uint16_t *p, int64_t inner, int64_t rows, int64_t batch, int S, int64_t ld,
+                    int64_t stride, int64_t plane, int box_rows)
+{
+    EncodeTiledFn enc = encode_fn();
+    if (!enc) return false;
+    if (batch <= 1) stride = rows * ld;
+    if (S <= 1) plane = batch * stride;
+    cuuint64_t dims[4] = {(cuuint64_t)inner, (cuuint64_t)rows, (cuuint64_t)batch, (cuuint64_t)S};
+    cuuint64_t strides[3] = {(cuuint64_t)ld * 2, (cuuint64_t)stride * 2, (cuuint64_t)plane * 2};
+    cuuint32_t box[4] = {64, (cuuint32_t)box_rows, 1, 1};
+    cuuint32_t estr[4] = {1, 1, 1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<uint16_t *>(p), dims, strides, box, estr,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+int sm_count()
+{
+    int dev = 0, sms = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess ||
+        cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sms < 2)
+        sms = 152;
+    return sms;
+}
+
+template <int S, int BC, bool PAIR, bool LMN, bool CMN>
+cudaError_t run_grouped(const CUtensorMap &tl, const CUtensorMap &tc, const GroupedArgs &a, int64_t tiles, cudaStream_t st)
+{
+    using Cfg = GroupedCfg<S, BC, PAIR>;
+    auto kern = grouped_kernel<S, BC, PAIR, LMN, CMN>;
+    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::SMEM);
+    if (e != cudaSuccess) return e;
+    int64_t units = sm_count() / Cfg::CTAS;
+    if (units > tiles) units = tiles < 1 ? 1 : tiles;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(units * Cfg::CTAS));
+    cfg.blockDim = dim3(Cfg::THREADS);
+    cfg.dynamicSmemBytes = Cfg::SMEM;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = Cfg::CTAS;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = PAIR ? 2 : 1;
+    e = cudaLaunchKernelEx(&cfg, kern, tl, tc, a);
+    if (e != cudaSuccess) return e;
+    return cudaGetLastError();
+}
+
+// Tiles at most (the host does not know the groups' sizes): every group may
+// end in a partial column tile.
+int64_t max_tiles(int64_t rows, int64_t G, int64_t L, int bc, int ctas)
+{
+    const int64_t groups = G < rows ? G : rows, lt = kLRows * ctas;
+    return (rows / bc + groups) * ((L + lt - 1) / lt);
+}
+
+template <int S, bool LMN>
+cudaError_t product(const GroupedOperand &X, const GroupedOperand &W, const GroupedArgs &a, cudaStream_t st)
+{
+    CUtensorMap tl, tc;
+    const bool ok = LMN ? make_group_map(&tl, W.planes, a.L, a.K, a.G, S, W.ld, W.stride, W.plane, 64)
+                        : make_group_map(&tl, W.planes, a.K, a.L, a.G, S, W.ld, W.stride, W.plane, kLRows);
+    if (!ok || !make_group_map(&tc, X.planes, a.K, X.rows, 1, S, X.ld, 0, X.plane, 16)) return cudaErrorInvalidValue;
+    const int64_t each = a.rows / a.G;            // rows of a group on average
+    if (each >= 128)
+        return run_grouped<S, 256, true, LMN, false>(tl, tc, a, max_tiles(a.rows, a.G, a.L, 256, 2), st);
+    return run_grouped<S, 64, false, LMN, false>(tl, tc, a, max_tiles(a.rows, a.G, a.L, 64, 1), st);
+}
+
+template <int S>
+cudaError_t gradient(const GroupedOperand &A, const GroupedOperand &B, const GroupedArgs &a, cudaStream_t st)
+{
+    CUtensorMap tl, tc;
+    if (!make_group_map(&tl, B.planes, a.L, B.rows, 1, S, B.ld, 0, B.plane, 64) ||
+        !make_group_map(&tc, A.planes, a.C, A.rows, 1, S, A.ld, 0, A.plane, 64))
+        return cudaErrorInvalidValue;
+    return run_grouped<S, 256, true, true, true>(tl, tc, a, (int64_t)a.G * ((a.L + 255) / 256) * ((a.C + 255) / 256), st);
+}
+
+}  // namespace
+
+cudaError_t launch_grouped_product(int S, bool trans, int64_t G, int64_t rows, int64_t N, int64_t K,
+                                   const GroupedOperand &X, const GroupedOperand &W, const int32_t *ends, void *Y,
+                                   bool y_f32, int64_t ldy, uint32_t *flags, cudaStream_t st)
+{
+    GroupedArgs a = {};
+    a.ends = ends; a.G = (int)G; a.rows = (int)rows; a.L = (int)N; a.K = (int)K; a.padded = X.padded ? 1 : 0;
+    a.out = Y; a.ldo = ldy; a.out_f32 = y_f32 ? 1 : 0; a.flags = flags;
+    if (S == 3) return trans ? product<3, false>(X, W, a, st) : product<3, true>(X, W, a, st);
+    return trans ? product<1, false>(X, W, a, st) : product<1, true>(X, W, a, st);
+}
+
+cudaError_t launch_grouped_gradient(int S, int64_t G, int64_t rows, int64_t M, int64_t N, const GroupedOperand &A,
+                                    const GroupedOperand &B, const int32_t *ends, void *D, bool d_f32, int64_t ldd,
+                                    int64_t strided, uint32_t *flags, cudaStream_t st)
+{
+    GroupedArgs a = {};
+    a.ends = ends; a.G = (int)G; a.rows = (int)rows; a.L = (int)N; a.C = (int)M;
+    a.out = D; a.ldo = ldd; a.strideo = strided; a.out_f32 = d_f32 ? 1 : 0; a.flags = flags;
+    return S == 3 ? gradient<3>(A, B, a, st) : gradient<1>(A, B, a, st);
+}
+
+}  // namespace emu

@@ -1,0 +1,232 @@
+// C-ABI of the products grouped by expert (declared in include/emu.h):
+// argument checks, workspace layout and launch sequences.
+#include "grouped_common.cuh"
+#include "launchers.cuh"
+
+using namespace emu;
+
+namespace {
+
+constexpr int64_t kMaxDim = (int64_t)1 << 31;      // kernels index with 32-bit coordinates
+
+int64_t round_up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
+bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+emu_status cuda_status(cudaError_t e) { return e == cudaSuccess ? EMU_OK : EMU_ERR_CUDA; }
+int64_t plane_ld(int64_t cols) { return round_up(cols < 1 ? 1 : cols, 8); }
+int slices(int dtype) { return dtype == EMU_F32 ? 3 : 1; }
+bool known(int dtype) { return dtype == EMU_F32 || dtype == EMU_BF16; }
+
+emu_status check_ws(void *ws, size_t ws_bytes, size_t need)
+{
+    if (!ws) return EMU_ERR_INVALID_ARG;
+    if (ws_bytes < need) return EMU_ERR_WORKSPACE_TOO_SMALL;
+    return aligned16(ws) ? EMU_OK : EMU_ERR_MISALIGNED;
+}
+
+cudaError_t clear_flags(void *ws, cudaStream_t st)
+{
+    return cudaMemsetAsync(&static_cast<WsHeader *>(ws)->flags, 0, sizeof(uint32_t), st);
+}
+
+// Sizes of a grouped call: G groups over `rows` rows, a and b the two matrix
+// dimensions; also keeps the tile counts within 32 bits.
+emu_status check_sizes(int64_t G, int64_t rows, int64_t a, int64_t b)
+{
+    if (G < 1 || rows < 0 || a < 0 || b < 0) return EMU_ERR_INVALID_ARG;
+    if (G > kMaxGroups || rows >= kMaxDim - 65536 || a >= kMaxDim || b >= kMaxDim || G * a >= kMaxDim || G * b >= kMaxDim)
+        return EMU_ERR_UNSUPPORTED;
+    const int64_t ta = a / 128 + 1, tb = b / 128 + 1;
+    if ((rows / 64 + G + 1) * ta >= kMaxDim || (rows / 64 + G + 1) * tb >= kMaxDim || G * ta >= kMaxDim / tb)
+        return EMU_ERR_UNSUPPORTED;
+    return EMU_OK;
+}
+
+// A matrix operand as the tensor memory accelerator reads it.
+emu_status check_planes(const void *p, int64_t ld, int64_t cols, int64_t stride)
+{
+    if (!p || ld < cols) return EMU_ERR_INVALID_ARG;
+    if (!aligned16(p) || ld % 8 != 0 || stride % 8 != 0) return EMU_ERR_MISALIGNED;
+    return EMU_OK;
+}
+
+cudaError_t zero_rows(void *p, int64_t rows, int64_t cols, int64_t ld, int esize, cudaStream_t st)
+{
+    if (rows <= 0 || cols <= 0) return cudaSuccess;
+    return cudaMemset2DAsync(p, (size_t)ld * esize, 0, (size_t)cols * esize, (size_t)rows, st);
+}
+
+emu_status product(int S, int opW, int64_t G, int64_t rows, int64_t N, int64_t K, const GroupedOperand &X,
+                   const GroupedOperand &W, const int32_t *ends, void *Y, int ytype, int64_t ldy, uint32_t *flags,
+                   cudaStream_t st)
+{
+    const int esize = ytype == EMU_F32 ? 4 : 2;
+    if (rows == 0 || N == 0) return EMU_OK;
+    if (K == 0) return cuda_status(zero_rows(Y, rows, N, ldy, esize, st));
+    return cuda_status(launch_grouped_product(S, opW == EMU_OP_T, G, rows, N, K, X, W, ends, Y, ytype == EMU_F32, ldy,
+                                              flags, st));
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t emu_grouped_plane_rows(int64_t rows, int64_t G)
+{
+    return rows < 0 || G < 1 ? 0 : padded_rows(rows, G);
+}
+
+emu_status emu_grouped_split(int dtype, int64_t G, int64_t rows, int64_t cols, const void *X, int64_t ldx,
+                             int64_t stridex, uint16_t *comps, int64_t ldcomp, void *ws, size_t ws_bytes,
+                             emu_stream_t stream)
+{
+    if (!known(dtype) || ldx < cols || (G > 1 && stridex < 0)) return EMU_ERR_INVALID_ARG;
+    emu_status s = check_sizes(G, 0, rows, cols);
+    if (s != EMU_OK) return s;
+    if (G * rows > 0 && cols > 0) {
+        if (!X) return EMU_ERR_INVALID_ARG;
+        s = check_planes(comps, ldcomp, cols, 0);
+        if (s != EMU_OK) return s;
+    }
+    s = check_ws(ws, ws_bytes, kWsHeaderBytes);
+    if (s != EMU_OK) return s;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    cudaError_t e = clear_flags(ws, st);
+    if (e == cudaSuccess)
+        e = launch_grouped_split(dtype == EMU_F32, G, rows, cols, X, ldx, stridex, comps, ldcomp,
+                                 &static_cast<WsHeader *>(ws)->flags, st);
+    return cuda_status(e);
+}
+
+emu_status emu_grouped_split_rows(int dtype, int64_t rows, int64_t cols, const void *X, int64_t xrows, int64_t ldx,
+                                  const int32_t *src, const int32_t *ends, int64_t G, uint16_t *comps,
+                                  int64_t ldcomp, void *ws, size_t ws_bytes, emu_stream_t stream)
+{
+    if (!known(dtype) || xrows < 0 || ldx < cols || (!src && xrows < rows)) return EMU_ERR_INVALID_ARG;
+    emu_status s = check_sizes(G, rows, cols, 0);
+    if (s != EMU_OK) return s;
+    if (rows > 0 && cols > 0) {
+        if (!ends || (xrows > 0 && !X)) return EMU_ERR_INVALID_ARG;
+        s = check_planes(comps, ldcomp, cols, 0);
+        if (s != EMU_OK) return s;
+    }
+    s = check_ws(ws, ws_bytes, kWsHeaderBytes);
+    if (s != EMU_OK) return s;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    cudaError_t e = clear_flags(ws, st);
+    if (e == cudaSuccess && rows > 0 && cols > 0)
+        e = launch_grouped_split_rows(dtype == EMU_F32, rows, cols, X, xrows, ldx, src, ends, G, comps, ldcomp,
+                                      &static_cast<WsHeader *>(ws)->flags, st);
+    return cuda_status(e);
+}
+
+emu_status emu_grouped_prodsum(int nslices, int opW, int64_t G, int64_t rows, int64_t N, int64_t K,
+                               const uint16_t *Xcomps, int64_t ldx, int padded, const uint16_t *Wcomps, int64_t ldw,
+                               int64_t stridew, const int32_t *ends, void *Y, int ytype, int64_t ldy, void *ws,
+                               size_t ws_bytes, emu_stream_t stream)
+{
+    if ((nslices != 1 && nslices != 3) || (opW != EMU_OP_N && opW != EMU_OP_T) || !known(ytype) || ldy < N)
+        return EMU_ERR_INVALID_ARG;
+    emu_status s = check_sizes(G, rows, N, K);
+    if (s != EMU_OK) return s;
+    const int64_t wrows = opW == EMU_OP_T ? N : K, wcols = opW == EMU_OP_T ? K : N;
+    if (rows > 0 && N > 0) {
+        if (!ends || !Y) return EMU_ERR_INVALID_ARG;
+        if (K > 0) {
+            // slices of the weights are planes of G dense matrices
+            if (nslices == 3 && G > 1 && stridew != wrows * ldw) return EMU_ERR_INVALID_ARG;
+            if (G > 1 && stridew < 0) return EMU_ERR_INVALID_ARG;
+            s = check_planes(Xcomps, ldx, K, 0);
+            if (s == EMU_OK) s = check_planes(Wcomps, ldw, wcols, G > 1 ? stridew : 0);
+            if (s != EMU_OK) return s;
+        }
+    }
+    s = check_ws(ws, ws_bytes, kWsHeaderBytes);
+    if (s != EMU_OK) return s;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    if (clear_flags(ws, st) != cudaSuccess) return EMU_ERR_CUDA;
+    GroupedOperand X, W;
+    X.planes = Xcomps; X.rows = padded ? padded_rows(rows, G) : rows; X.ld = ldx; X.plane = X.rows * ldx;
+    X.padded = padded != 0;
+    W.planes = Wcomps; W.ld = ldw; W.stride = stridew; W.plane = G * wrows * ldw;
+    return product(nslices, opW, G, rows, N, K, X, W, ends, Y, ytype, ldy, &static_cast<WsHeader *>(ws)->flags, st);
+}
+
+size_t emu_grouped_gemm_workspace_bytes(int dtype, int64_t G, int64_t rows, int64_t N, int64_t K)
+{
+    if (G < 1 || rows < 0 || N < 0 || K < 0) return 0;
+    if (dtype != EMU_F32) return kWsHeaderBytes;
+    // planes of the weights in the larger of their two orientations
+    const int64_t w = N * plane_ld(K) > K * plane_ld(N) ? N * plane_ld(K) : K * plane_ld(N);
+    return kWsHeaderBytes + (size_t)round_up(3 * padded_rows(rows, G) * plane_ld(K) * 2, 256) +
+           (size_t)round_up(3 * G * w * 2, 256);
+}
+
+emu_status emu_grouped_gemm_f32(int opW, int64_t G, int64_t rows, int64_t N, int64_t K, const float *X, int64_t xrows,
+                                int64_t ldx, const int32_t *src, const float *W, int64_t ldw, int64_t stridew,
+                                const int32_t *ends, float *Y, int64_t ldy, void *ws, size_t ws_bytes,
+                                emu_stream_t stream)
+{
+    if ((opW != EMU_OP_N && opW != EMU_OP_T) || ldy < N || ldx < K || xrows < 0 || (!src && xrows < rows))
+        return EMU_ERR_INVALID_ARG;
+    emu_status s = check_sizes(G, rows, N, K);
+    if (s != EMU_OK) return s;
+    const int64_t wrows = opW == EMU_OP_T ? N : K, wcols = opW == EMU_OP_T ? K : N;
+    if (ldw < wcols || (G > 1 && stridew < 0)) return EMU_ERR_INVALID_ARG;
+    if (rows > 0 && N > 0 && (!ends || !Y || (K > 0 && (!W || (xrows > 0 && !X))))) return EMU_ERR_INVALID_ARG;
+    s = check_ws(ws, ws_bytes, emu_grouped_gemm_workspace_bytes(EMU_F32, G, rows, N, K));
+    if (s != EMU_OK) return s;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    uint32_t *flags = &static_cast<WsHeader *>(ws)->flags;
+    if (clear_flags(ws, st) != cudaSuccess) return EMU_ERR_CUDA;
+    GroupedOperand xo, wo;
+    if (rows > 0 && N > 0 && K > 0) {
+        uint16_t *xp = reinterpret_cast<uint16_t *>(static_cast<char *>(ws) + kWsHeaderBytes);
+        xo.rows = padded_rows(rows, G); xo.ld = plane_ld(K); xo.plane = xo.rows * xo.ld; xo.padded = true; xo.planes = xp;
+        uint16_t *wp = reinterpret_cast<uint16_t *>(reinterpret_cast<char *>(xp) + round_up(3 * xo.plane * 2, 256));
+        wo.ld = plane_ld(wcols); wo.stride = wrows * wo.ld; wo.plane = G * wo.stride; wo.planes = wp;
+        cudaError_t e = launch_grouped_split_rows(true, rows, K, X, xrows, ldx, src, ends, G, xp, xo.ld, flags, st);
+        if (e == cudaSuccess) e = launch_grouped_split(true, G, wrows, wcols, W, ldw, stridew, wp, wo.ld, flags, st);
+        if (e != cudaSuccess) return EMU_ERR_CUDA;
+    }
+    return product(3, opW, G, rows, N, K, xo, wo, ends, Y, EMU_F32, ldy, flags, st);
+}
+
+emu_status emu_grouped_prodsum_wgrad(int nslices, int64_t G, int64_t rows, int64_t M, int64_t N,
+                                     const uint16_t *Acomps, int64_t lda, const uint16_t *Bcomps, int64_t ldb,
+                                     const int32_t *ends, void *D, int dtype, int64_t ldd, int64_t strided, void *ws,
+                                     size_t ws_bytes, emu_stream_t stream)
+{
+    if ((nslices != 1 && nslices != 3) || !known(dtype) || ldd < N || (G > 1 && strided < M * ldd))
+        return EMU_ERR_INVALID_ARG;
+    emu_status s = check_sizes(G, rows, M, N);
+    if (s != EMU_OK) return s;
+    if (M > 0 && N > 0) {
+        if (!D) return EMU_ERR_INVALID_ARG;
+        if (rows > 0) {
+            if (!ends) return EMU_ERR_INVALID_ARG;
+            s = check_planes(Acomps, lda, M, 0);
+            if (s == EMU_OK) s = check_planes(Bcomps, ldb, N, 0);
+            if (s != EMU_OK) return s;
+        }
+    }
+    s = check_ws(ws, ws_bytes, kWsHeaderBytes);
+    if (s != EMU_OK) return s;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    if (clear_flags(ws, st) != cudaSuccess) return EMU_ERR_CUDA;
+    if (M == 0 || N == 0) return EMU_OK;
+    if (rows == 0) {
+        for (int64_t g = 0; g < G; ++g) {
+            const int esize = dtype == EMU_F32 ? 4 : 2;
+            if (zero_rows(static_cast<char *>(D) + g * strided * esize, M, N, ldd, esize, st) != cudaSuccess)
+                return EMU_ERR_CUDA;
+        }
+        return EMU_OK;
+    }
+    GroupedOperand A, B;
+    A.planes = Acomps; A.rows = padded_rows(rows, G); A.ld = lda; A.plane = A.rows * lda; A.padded = true;
+    B.planes = Bcomps; B.rows = A.rows; B.ld = ldb; B.plane = B.rows * ldb; B.padded = true;
+    return cuda_status(launch_grouped_gradient(nslices, G, rows, M, N, A, B, ends, D, dtype == EMU_F32, ldd, strided,
+                                               &static_cast<WsHeader *>(ws)->flags, st));
+}
+
+}  // extern "C"

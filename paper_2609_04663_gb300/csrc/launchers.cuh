@@ -132,4 +132,25 @@ cudaError_t launch_axpby_f32(const float *P, int64_t ldp, float *C, int64_t ldc,
 cudaError_t launch_axpby_f64(const double *P, int64_t ldp, double *C, int64_t ldc, int64_t M, int64_t N,
                              double alpha, double beta, cudaStream_t st);
 
+// Products grouped by expert (grouped.cu).  One operand as planes: S planes
+// `plane` elements apart, row pitch ld; weights: matrices `stride` elements
+// apart; token rows: `rows` plane rows, `padded` when each group starts at
+// padded_start (grouped_common.cuh) and ends in zero rows.
+struct GroupedOperand {
+    const uint16_t *planes = nullptr;
+    int64_t rows = 0, ld = 0, stride = 0, plane = 0;
+    bool padded = false;
+};
+cudaError_t launch_grouped_split(bool f32, int64_t G, int64_t rows, int64_t cols, const void *X, int64_t ldx,
+                                 int64_t stride, uint16_t *comps, int64_t ldcomp, uint32_t *flags, cudaStream_t st);
+cudaError_t launch_grouped_split_rows(bool f32, int64_t rows, int64_t cols, const void *X, int64_t xrows,
+                                      int64_t ldx, const int32_t *src, const int32_t *ends, int64_t G,
+                                      uint16_t *comps, int64_t ldcomp, uint32_t *flags, cudaStream_t st);
+cudaError_t launch_grouped_product(int S, bool trans, int64_t G, int64_t rows, int64_t N, int64_t K,
+                                   const GroupedOperand &X, const GroupedOperand &W, const int32_t *ends, void *Y,
+                                   bool y_f32, int64_t ldy, uint32_t *flags, cudaStream_t st);
+cudaError_t launch_grouped_gradient(int S, int64_t G, int64_t rows, int64_t M, int64_t N, const GroupedOperand &A,
+                                    const GroupedOperand &B, const int32_t *ends, void *D, bool d_f32, int64_t ldd,
+                                    int64_t strided, uint32_t *flags, cudaStream_t st);
+
 }  // namespace emu
