@@ -462,6 +462,62 @@ emu_status emu_grouped_prodsum_wgrad(int nslices, int64_t G, int64_t rows, int64
                                      const int32_t *ends, void *D, int dtype, int64_t ldd, int64_t strided, void *ws,
                                      size_t ws_bytes, emu_stream_t stream);
 
+/* Matrix-vector products with 4-bit weights and group scales, for one row or a
+ * few rows (of each expert):
+ *   Y[r, n] = sum_k X[r, k] (q[g, n, k] - z[g, n, k/group]) s[g, n, k/group]
+ * for every row r of group g.  q: unsigned 4-bit codes, uint8 [G][N][K/2], the
+ * even k in the low half of a byte; s: stype [G][N][K/group]; z: uint8
+ * [G][N][K/group] with values 0 .. 15 (the low half counts), or NULL for 8
+ * throughout.  group: a multiple of 32 that divides K.  X: rows x K and Y:
+ * rows x N of dtype (EMU_F32: FP32 rows as their three BF16 slices, exact
+ * products; EMU_BF16), any alignment; sums in FP32.  ends as above, or NULL
+ * with G = 1: one matrix for all rows.  Values in ends outside 0 .. rows or
+ * decreasing are clamped.  Rows of no group are zero.  Any number of rows is
+ * computed; the weights are read again for every 24 (BF16) or 8 (FP32) of an
+ * expert.  q 16-byte aligned.  No workspace. */
+emu_status emu_w4_matvec(int dtype, int64_t G, int64_t rows, int64_t N, int64_t K, int64_t group, const void *X,
+                         int64_t ldx, const uint8_t *q, const void *s, int stype, const uint8_t *z,
+                         const int32_t *ends, void *Y, int64_t ldy, emu_stream_t stream);
+
+/* Routing of T tokens to the k of E experts with the largest logits (dtype,
+ * T x E, row pitch ldl; ties: the lower index; NaN counts as minus infinity):
+ *   experts [T][k] by falling logit; weights [T][k] FP32, the softmax over the
+ *   chosen (renorm = 1) or over all experts (renorm = 0), 0 where the logit is
+ *   minus infinity (all of a token's where all its logits are);
+ * and the order of the T k assignments by expert, then token, then rank:
+ *   slots [T][k] the place of each in that order, rows [T k] the token at each
+ *   place, ends [E] the places' ends by expert, as the grouped calls take them.
+ * 1 <= k <= 32, k <= E <= 1024, T k < 2^31.  Deterministic.  ws: at least
+ * emu_route_workspace_bytes.  Flags: EMU_FLAG_NONFINITE (a logit is NaN or plus
+ * infinity), EMU_FLAG_TIMEOUT. */
+size_t emu_route_workspace_bytes(int64_t T, int64_t E, int64_t k);
+emu_status emu_route(int dtype, int64_t T, int64_t E, int64_t k, int renorm, const void *logits, int64_t ldl,
+                     float *weights, int32_t *experts, int32_t *slots, int32_t *rows, int32_t *ends, void *ws,
+                     size_t ws_bytes, emu_stream_t stream);
+
+/* Gradient of the weights' softmax: dlogits (T x E of dtype, row pitch lddl,
+ * all entries written) from the weights' gradients dweights [T][k] and the
+ * experts that emu_route chose for the same logits and renorm. */
+emu_status emu_route_backward(int dtype, int64_t T, int64_t E, int64_t k, int renorm, const void *logits, int64_t ldl,
+                              const int32_t *experts, const float *dweights, void *dlogits, int64_t lddl,
+                              emu_stream_t stream);
+
+/* Weighted sum of the answers: O[t] = sum_j weights[t, j] Y[slots[t, j]], j
+ * ascending in FP32, one rounding to dtype.  Y: yrows x cols, O: T x cols of
+ * dtype; weights [T][k] FP32, or NULL for 1 throughout (the gradient of a
+ * gather of token rows).  A slot outside 0 .. yrows-1 contributes nothing. */
+emu_status emu_rows_combine(int dtype, int64_t T, int64_t k, int64_t cols, const void *Y, int64_t yrows, int64_t ldy,
+                            const int32_t *slots, const float *weights, void *O, int64_t ldo, emu_stream_t stream);
+
+/* Its gradients: dY[slots[t, j]] = weights[t, j] dO[t] (dY: yrows x cols; rows
+ * that no slot names are not written; no two slots may name the same row) and
+ * dweights[t, j] = Y[slots[t, j]] . dO[t] in FP32 (0 for a slot outside), or
+ * dweights NULL when they are not wanted (Y is then not read). */
+emu_status emu_rows_combine_backward(int dtype, int64_t T, int64_t k, int64_t cols, const void *dO, int64_t lddo,
+                                     const void *Y, int64_t yrows, int64_t ldy, const int32_t *slots,
+                                     const float *weights, void *dY, int64_t lddy, float *dweights,
+                                     emu_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

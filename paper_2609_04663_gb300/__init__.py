@@ -12,6 +12,7 @@ library raises.
 """
 from __future__ import annotations
 
+import collections
 import ctypes
 import os
 
@@ -71,6 +72,12 @@ _SIGS = {
                                    "size", "p"]),
     "emu_grouped_prodsum_wgrad": ("i", ["i", "l", "l", "l", "l", "p", "l", "p", "l", "p", "p", "i", "l", "l", "p",
                                         "size", "p"]),
+    "emu_w4_matvec": ("i", ["i", "l", "l", "l", "l", "l", "p", "l", "p", "p", "i", "p", "p", "p", "l", "p"]),
+    "emu_route_workspace_bytes": ("size", ["l", "l", "l"]),
+    "emu_route": ("i", ["i", "l", "l", "l", "i", "p", "l", "p", "p", "p", "p", "p", "p", "size", "p"]),
+    "emu_route_backward": ("i", ["i", "l", "l", "l", "i", "p", "l", "p", "p", "p", "l", "p"]),
+    "emu_rows_combine": ("i", ["i", "l", "l", "l", "p", "l", "l", "p", "p", "p", "l", "p"]),
+    "emu_rows_combine_backward": ("i", ["i", "l", "l", "l", "p", "l", "p", "l", "l", "p", "p", "p", "l", "p", "p"]),
     "emu_read_flags": ("i", ["p", "p", "p"]),
     "emu_selftest_timeout": ("i", ["p", "size", "u32", "p"]),
     "emu_status_string": ("str", ["i"]),
@@ -152,6 +159,12 @@ emu_grouped_prodsum = _mk("emu_grouped_prodsum")
 emu_grouped_gemm_workspace_bytes = _mk("emu_grouped_gemm_workspace_bytes")
 emu_grouped_gemm_f32 = _mk("emu_grouped_gemm_f32")
 emu_grouped_prodsum_wgrad = _mk("emu_grouped_prodsum_wgrad")
+emu_w4_matvec = _mk("emu_w4_matvec")
+emu_route_workspace_bytes = _mk("emu_route_workspace_bytes")
+emu_route = _mk("emu_route")
+emu_route_backward = _mk("emu_route_backward")
+emu_rows_combine = _mk("emu_rows_combine")
+emu_rows_combine_backward = _mk("emu_rows_combine_backward")
 emu_read_flags = _mk("emu_read_flags")
 emu_selftest_timeout = _mk("emu_selftest_timeout")
 emu_status_string = _mk("emu_status_string")
@@ -376,13 +389,19 @@ def _need(ok, what):
         raise ValueError(what)
 
 
+def _torch_stream(stream, device):
+    torch = _torch()
+    if stream is None:
+        return torch.cuda.current_stream(device)
+    return stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=device)
+
+
 def _empty(shape, dtype, device, stream):
     """torch.empty whose memory belongs to the stream that the kernels use."""
     torch = _torch()
     if stream is None:
         return torch.empty(shape, dtype=dtype, device=device)
-    s = stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=device)
-    with torch.cuda.stream(s):
+    with torch.cuda.stream(_torch_stream(stream, device)):
         return torch.empty(shape, dtype=dtype, device=device)
 
 
@@ -539,3 +558,117 @@ def grouped_wgrad(A, B, ends, srcA=None, srcB=None, D=None, ws=None, stream=None
                                      D.stride(0) if G > 1 else M * ldd, ws.data_ptr(), ws.numel(), _stream(stream)),
            "emu_grouped_prodsum_wgrad")
     return D, ws
+
+
+def w4_matvec(X, Wq, scales, zeros=None, ends=None, Y=None, stream=None):
+    """emu_w4_matvec: Y[r] = W_g X[r] for the rows r of group g (ends None: one
+    matrix Wq [N, K/2] for all rows), W = (codes - zeros) * scales.  Wq uint8
+    [G, N, K/2], the even k in the low half of a byte; scales FP32 or BF16 and
+    zeros uint8 (None: 8) [G, N, K/group].  X and Y: FP32 or BF16.  For a few
+    rows per expert.  Returns Y."""
+    torch = _torch()
+    dev = X.device
+    dt, ldx = _dtype(X, "w4_matvec: X"), _rows_of(X, "w4_matvec: X")
+    lead, (N, half), (rows, K) = tuple(Wq.shape[:-2]), Wq.shape[-2:], X.shape
+    G = ends.numel() if ends is not None else 1
+    _need(K == 2 * half, f"w4_matvec: X has {K} columns, the weights {2 * half}")
+    _need(lead == ((G,) if ends is not None else ()), f"w4_matvec: weights of {lead} matrices for {G} groups")
+    ng = scales.shape[-1]
+    group = K // ng if ng else 32
+    _need(group * ng == K and tuple(scales.shape) == lead + (N, ng), "w4_matvec: scales have another shape")
+    for t, want, name in ((Wq, torch.uint8, "Wq"), (scales, scales.dtype, "scales"), (zeros, torch.uint8, "zeros")):
+        _need(t is None or (t.dtype == want and t.is_contiguous() and t.device == dev),
+              f"w4_matvec: {name} has to be contiguous {want} on {dev}")
+    _need(zeros is None or zeros.shape == scales.shape, "w4_matvec: zeros have another shape")
+    if Y is None:
+        Y = _empty((rows, N), X.dtype, dev, stream)
+    _need(tuple(Y.shape) == (rows, N) and Y.dtype == X.dtype, "w4_matvec: Y has another shape or type")
+    _check(emu_w4_matvec(dt, G, rows, N, K, group, X.data_ptr(), ldx, Wq.data_ptr(), scales.data_ptr(),
+                         _dtype(scales, "w4_matvec: scales"), zeros.data_ptr() if zeros is not None else None,
+                         _ints(ends, G, dev, "w4_matvec: ends") if ends is not None else None, Y.data_ptr(),
+                         _rows_of(Y, "w4_matvec: Y"), _stream(stream)), "emu_w4_matvec")
+    return Y
+
+
+Route = collections.namedtuple("Route", "weights experts slots rows ends")
+
+
+def route(logits, k: int, renorm: bool = True, ws=None, stream=None):
+    """emu_route: the k experts of each token (ties: the lower index), their
+    softmax weights over the chosen (renorm) or all experts, and the order of
+    the assignments by expert.  Returns (Route(weights, experts, slots [T, k],
+    rows [T k], ends [E]), ws): rows and ends are src and ends of grouped_gemm,
+    slots and weights those of rows_combine."""
+    torch = _torch()
+    dt, ldl = _dtype(logits, "route"), _rows_of(logits, "route")
+    (T, E), dev = logits.shape, logits.device
+    ws = ws if ws is not None else _empty(emu_route_workspace_bytes(T, E, k), torch.uint8, dev, stream)
+    weights = _empty((T, k), torch.float32, dev, stream)
+    experts, slots = (_empty((T, k), torch.int32, dev, stream) for _ in range(2))
+    rows, ends = _empty(T * k, torch.int32, dev, stream), _empty(E, torch.int32, dev, stream)
+    _check(emu_route(dt, T, E, k, int(renorm), logits.data_ptr(), ldl, weights.data_ptr(), experts.data_ptr(),
+                     slots.data_ptr(), rows.data_ptr(), ends.data_ptr(), ws.data_ptr(), ws.numel(), _stream(stream)),
+           "emu_route")
+    return Route(weights, experts, slots, rows, ends), ws
+
+
+def route_backward(logits, experts, dweights, renorm: bool = True, dlogits=None, stream=None):
+    """emu_route_backward: the logits' gradients from those of route's weights."""
+    torch = _torch()
+    dt, (T, E), k = _dtype(logits, "route_backward"), logits.shape, experts.shape[1]
+    if dlogits is None:
+        dlogits = _empty((T, E), logits.dtype, logits.device, stream)
+    _need(tuple(dlogits.shape) == (T, E) and dlogits.dtype == logits.dtype, "route_backward: dlogits differ from logits")
+    _need(tuple(dweights.shape) == (T, k) and dweights.dtype == torch.float32 and dweights.is_contiguous(),
+          "route_backward: dweights have to be contiguous float32 [T, k]")
+    _check(emu_route_backward(dt, T, E, k, int(renorm), logits.data_ptr(), _rows_of(logits, "route_backward"),
+                              _ints(experts, T * k, logits.device, "route_backward: experts"), dweights.data_ptr(),
+                              dlogits.data_ptr(), _rows_of(dlogits, "route_backward"), _stream(stream)),
+           "emu_route_backward")
+    return dlogits
+
+
+def _weights(weights, shape, where):
+    torch = _torch()
+    if weights is None:
+        return None
+    _need(tuple(weights.shape) == tuple(shape) and weights.dtype == torch.float32 and weights.is_contiguous(),
+          f"{where}: weights have to be contiguous float32 {tuple(shape)}")
+    return weights.data_ptr()
+
+
+def rows_combine(Y, slots, weights=None, O=None, stream=None):
+    """emu_rows_combine: O[t] = sum_j weights[t, j] Y[slots[t, j]] (weights None: 1)."""
+    dt, ldy, (T, k), cols = _dtype(Y, "rows_combine"), _rows_of(Y, "rows_combine"), slots.shape, Y.shape[1]
+    if O is None:
+        O = _empty((T, cols), Y.dtype, Y.device, stream)
+    _need(tuple(O.shape) == (T, cols) and O.dtype == Y.dtype, "rows_combine: O has another shape or type")
+    _check(emu_rows_combine(dt, T, k, cols, Y.data_ptr(), Y.shape[0], ldy,
+                            _ints(slots, T * k, Y.device, "rows_combine: slots"),
+                            _weights(weights, (T, k), "rows_combine"), O.data_ptr(), _rows_of(O, "rows_combine: O"),
+                            _stream(stream)), "emu_rows_combine")
+    return O
+
+
+def rows_combine_backward(dO, Y, slots, weights=None, dY=None, stream=None):
+    """emu_rows_combine_backward: (dY, dweights) of rows_combine(Y, slots,
+    weights); dweights is None without weights.  No two slots may name the
+    same row; rows of a dY made here that no slot names are zero."""
+    torch = _torch()
+    dt, (T, k), cols = _dtype(Y, "rows_combine_backward"), slots.shape, Y.shape[1]
+    _need(tuple(dO.shape) == (T, cols) and dO.dtype == Y.dtype, "rows_combine_backward: dO has another shape or type")
+    if dY is None:
+        dY = _empty(tuple(Y.shape), Y.dtype, Y.device, stream)
+        if Y.shape[0] != T * k:
+            with torch.cuda.stream(_torch_stream(stream, Y.device)):
+                dY.zero_()
+    _need(tuple(dY.shape) == tuple(Y.shape) and dY.dtype == Y.dtype, "rows_combine_backward: dY differs from Y")
+    dw = _empty((T, k), torch.float32, Y.device, stream) if weights is not None else None
+    _check(emu_rows_combine_backward(dt, T, k, cols, dO.data_ptr(), _rows_of(dO, "rows_combine_backward: dO"),
+                                     Y.data_ptr(), Y.shape[0], _rows_of(Y, "rows_combine_backward: Y"),
+                                     _ints(slots, T * k, Y.device, "rows_combine_backward: slots"),
+                                     _weights(weights, (T, k), "rows_combine_backward"), dY.data_ptr(),
+                                     _rows_of(dY, "rows_combine_backward: dY"),
+                                     dw.data_ptr() if dw is not None else None, _stream(stream)),
+           "emu_rows_combine_backward")
+    return dY, dw

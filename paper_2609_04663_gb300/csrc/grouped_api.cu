@@ -229,4 +229,88 @@ emu_status emu_grouped_prodsum_wgrad(int nslices, int64_t G, int64_t rows, int64
                                                &static_cast<WsHeader *>(ws)->flags, st));
 }
 
+emu_status emu_w4_matvec(int dtype, int64_t G, int64_t rows, int64_t N, int64_t K, int64_t group, const void *X,
+                         int64_t ldx, const uint8_t *q, const void *scales, int stype, const uint8_t *zeros,
+                         const int32_t *ends, void *Y, int64_t ldy, emu_stream_t stream)
+{
+    if (!known(dtype) || !known(stype) || ldx < K || ldy < N || group < 32 || group % 32 != 0 || K < 0 || K % group != 0 ||
+        (!ends && G != 1))
+        return EMU_ERR_INVALID_ARG;
+    emu_status s = check_sizes(G, rows, N, K);
+    if (s != EMU_OK) return s;
+    if (rows == 0 || N == 0) return EMU_OK;
+    if (!Y) return EMU_ERR_INVALID_ARG;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    const int esize = dtype == EMU_F32 ? 4 : 2;
+    if (K == 0) return cuda_status(zero_rows(Y, rows, N, ldy, esize, st));
+    if (!X || !q || !scales) return EMU_ERR_INVALID_ARG;
+    if (!aligned16(q)) return EMU_ERR_MISALIGNED;
+    if (rows > 65535 * 2) return EMU_ERR_UNSUPPORTED;           // items of two rows and more on the grid's y dimension
+    return cuda_status(launch_w4_matvec(dtype == EMU_F32, G, rows, N, K, (int)group, X, ldx, q, scales,
+                                        stype == EMU_F32, zeros, ends, Y, ldy, st));
+}
+
+size_t emu_route_workspace_bytes(int64_t T, int64_t E, int64_t k)
+{
+    (void)T;
+    (void)k;
+    return E < 1 ? 0 : kWsHeaderBytes + route_scratch_bytes(E);
+}
+
+emu_status emu_route(int dtype, int64_t T, int64_t E, int64_t k, int renorm, const void *logits, int64_t ldl,
+                     float *weights, int32_t *experts, int32_t *slots, int32_t *rows, int32_t *ends, void *ws,
+                     size_t ws_bytes, emu_stream_t stream)
+{
+    if (!known(dtype) || T < 0 || E < 1 || k < 1 || k > E || ldl < E || !ends) return EMU_ERR_INVALID_ARG;
+    if (E > kMaxGroups || k > 32 || T >= kMaxDim / k) return EMU_ERR_UNSUPPORTED;
+    if (T > 0 && (!logits || !weights || !experts || !slots || !rows)) return EMU_ERR_INVALID_ARG;
+    emu_status s = check_ws(ws, ws_bytes, emu_route_workspace_bytes(T, E, k));
+    if (s != EMU_OK) return s;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    WsHeader *h = static_cast<WsHeader *>(ws);
+    cudaError_t e = cudaMemsetAsync(h, 0, 2 * sizeof(uint32_t), st);       // the flag word and the barrier's count
+    if (e == cudaSuccess)
+        e = launch_route(T, E, (int)k, renorm != 0, logits, dtype == EMU_F32, ldl, weights, experts, slots, rows, ends,
+                         reinterpret_cast<int32_t *>(static_cast<char *>(ws) + kWsHeaderBytes), h, st);
+    return cuda_status(e);
+}
+
+emu_status emu_route_backward(int dtype, int64_t T, int64_t E, int64_t k, int renorm, const void *logits, int64_t ldl,
+                              const int32_t *experts, const float *dweights, void *dlogits, int64_t lddl,
+                              emu_stream_t stream)
+{
+    if (!known(dtype) || T < 0 || E < 1 || k < 1 || k > E || ldl < E || lddl < E) return EMU_ERR_INVALID_ARG;
+    if (E > kMaxGroups || k > 32 || T >= kMaxDim / k) return EMU_ERR_UNSUPPORTED;
+    if (T == 0) return EMU_OK;
+    if (!logits || !experts || !dweights || !dlogits) return EMU_ERR_INVALID_ARG;
+    return cuda_status(launch_route_backward(T, E, (int)k, renorm != 0, logits, dtype == EMU_F32, ldl, experts,
+                                             dweights, dlogits, lddl, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+emu_status emu_rows_combine(int dtype, int64_t T, int64_t k, int64_t cols, const void *Y, int64_t yrows, int64_t ldy,
+                            const int32_t *slots, const float *weights, void *O, int64_t ldo, emu_stream_t stream)
+{
+    if (!known(dtype) || T < 0 || k < 1 || cols < 0 || yrows < 0 || ldy < cols || ldo < cols) return EMU_ERR_INVALID_ARG;
+    if (k >= 65536 || T >= kMaxDim / k || cols >= kMaxDim - 8 || yrows >= kMaxDim) return EMU_ERR_UNSUPPORTED;
+    if (T == 0 || cols == 0) return EMU_OK;
+    if (!slots || !O || (yrows > 0 && !Y)) return EMU_ERR_INVALID_ARG;
+    return cuda_status(launch_combine(dtype == EMU_F32, T, (int)k, cols, Y, yrows, ldy, slots, weights, O, ldo,
+                                      reinterpret_cast<cudaStream_t>(stream)));
+}
+
+emu_status emu_rows_combine_backward(int dtype, int64_t T, int64_t k, int64_t cols, const void *dO, int64_t lddo,
+                                     const void *Y, int64_t yrows, int64_t ldy, const int32_t *slots,
+                                     const float *weights, void *dY, int64_t lddy, float *dweights,
+                                     emu_stream_t stream)
+{
+    if (!known(dtype) || T < 0 || k < 1 || cols < 0 || yrows < 0 || lddo < cols || lddy < cols ||
+        (dweights && ldy < cols))
+        return EMU_ERR_INVALID_ARG;
+    if (k >= 65536 || T >= kMaxDim / k || cols >= kMaxDim - 8 || yrows >= kMaxDim) return EMU_ERR_UNSUPPORTED;
+    if (T == 0) return EMU_OK;
+    if (!slots || (cols > 0 && (!dO || (yrows > 0 && (!dY || (dweights && !Y)))))) return EMU_ERR_INVALID_ARG;
+    return cuda_status(launch_combine_backward(dtype == EMU_F32, T, (int)k, cols, dO, lddo, Y, yrows, ldy, slots,
+                                               weights, dY, lddy, dweights, reinterpret_cast<cudaStream_t>(stream)));
+}
+
 }  // extern "C"

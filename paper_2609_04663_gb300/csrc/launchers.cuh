@@ -153,4 +153,21 @@ cudaError_t launch_grouped_gradient(int S, int64_t G, int64_t rows, int64_t M, i
                                     const GroupedOperand &B, const int32_t *ends, void *D, bool d_f32, int64_t ldd,
                                     int64_t strided, uint32_t *flags, cudaStream_t st);
 
+// Matrix-vector products with 4-bit weights (w4.cu), routing and the weighted
+// sum of answers (route.cu).
+cudaError_t launch_w4_matvec(bool x_f32, int64_t G, int64_t rows, int64_t N, int64_t K, int group, const void *X,
+                             int64_t ldx, const uint8_t *q, const void *scales, bool s_f32, const uint8_t *zeros,
+                             const int32_t *ends, void *Y, int64_t ldy, cudaStream_t st);
+size_t route_scratch_bytes(int64_t E);
+cudaError_t launch_route(int64_t T, int64_t E, int k, bool renorm, const void *logits, bool f32, int64_t ldl,
+                         float *weights, int32_t *experts, int32_t *slots, int32_t *rows, int32_t *ends,
+                         int32_t *counts, WsHeader *ws, cudaStream_t st);
+cudaError_t launch_route_backward(int64_t T, int64_t E, int k, bool renorm, const void *logits, bool f32, int64_t ldl,
+                                  const int32_t *experts, const float *dw, void *dl, int64_t lddl, cudaStream_t st);
+cudaError_t launch_combine(bool f32, int64_t T, int k, int64_t cols, const void *Y, int64_t yrows, int64_t ldy,
+                           const int32_t *slots, const float *weights, void *O, int64_t ldo, cudaStream_t st);
+cudaError_t launch_combine_backward(bool f32, int64_t T, int k, int64_t cols, const void *dO, int64_t lddo,
+                                    const void *Y, int64_t yrows, int64_t ldy, const int32_t *slots,
+                                    const float *weights, void *dY, int64_t lddy, float *dw, cudaStream_t st);
+
 }  // namespace emu

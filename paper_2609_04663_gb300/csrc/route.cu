@@ -1,0 +1,533 @@
+// Routing of tokens to experts, its gradient, and the weighted sum of the
+// experts' answers with its gradients.
+//
+// route: for each token the k largest logits (ties: the lower index), their
+// softmax weights, and the stable order of all T k assignments by expert: a
+// counting sort.  One launch: every block ranks a contiguous range of tokens
+// (a warp per token: the largest key by a warp maximum, its lowest index by a
+// warp minimum, k times), counts its assignments per expert, and after one
+// grid barrier places them behind those of the blocks before it.  A single
+// block needs no barrier.  Bound by latency (two reads of `experts`, the
+// barrier) up to some ten thousand tokens, then by reading the logits.
+//
+// combine: bound by HBM; every answer row is read once, rows in 16-byte pieces.
+#include "grouped_common.cuh"
+#include "launchers.cuh"
+#include "split_f32_pair.cuh"
+
+namespace emu {
+
+namespace {
+
+constexpr int kRouteThreads = 1024, kRouteWarps = kRouteThreads / 32, kRouteBlocks = 152;
+
+__device__ __forceinline__ float bf16_f32(uint32_t b) { return __uint_as_float(b << 16); }
+__device__ __forceinline__ uint16_t f32_bf16(float x) { return (uint16_t)bf16x2_rn(x, 0.0f); }
+
+// A logit as the softmax sees it: NaN counts as minus infinity.
+__device__ __forceinline__ float load_logit(const void *row, int e, bool f32)
+{
+    const float x = f32 ? __ldg(static_cast<const float *>(row) + e)
+                        : bf16_f32(__ldg(static_cast<const uint16_t *>(row) + e));
+    return x;
+}
+
+// Order-preserving key of a logit, never 0: negative zero like zero, NaN like
+// minus infinity.
+__device__ __forceinline__ uint32_t logit_key(float x)
+{
+    if (!(x == x)) x = -INFINITY;
+    const uint32_t b = __float_as_uint(x + 0.0f);
+    return (b & 0x80000000u) ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float key_logit(uint32_t k)
+{
+    return __uint_as_float((k & 0x80000000u) ? k & 0x7FFFFFFFu : ~k);
+}
+
+__device__ __forceinline__ float warp_sum(float x)
+{
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, d);
+    return x;
+}
+
+struct RouteArgs {
+    const void *logits;
+    int64_t ldl;
+    int T, E, k, f32, renorm;
+    float *weights;
+    int32_t *experts, *slots, *rows, *ends;
+    int32_t *counts;                      // [blocks][E]
+    uint32_t *flags, *bar;
+};
+
+// Bounded barrier over the blocks of a cooperative launch (one use per launch;
+// *bar starts at zero).
+__device__ __forceinline__ void route_barrier(uint32_t *bar, uint32_t *flags)
+{
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        __threadfence();
+        atomicAdd(bar, 1u);
+        volatile uint32_t *seen = bar;
+        const unsigned long long t0 = globaltimer_ns();
+        for (uint32_t it = 0; *seen < gridDim.x; ++it) {
+            if ((it & 63u) == 63u && globaltimer_ns() - t0 > kWaitLimitNs) {
+                atomicOr(flags, (uint32_t)EMU_FLAG_TIMEOUT);
+                break;
+            }
+        }
+        __threadfence();
+    }
+    __syncthreads();
+}
+
+// V: logits per lane (E <= 32 V).
+template <int V>
+__global__ void __launch_bounds__(kRouteThreads) route_kernel(const RouteArgs a)
+{
+    extern __shared__ int32_t sm[];
+    int32_t *hist = sm;                                   // [kRouteWarps][E]
+    int32_t *base = sm + kRouteWarps * a.E;               // [E] first slot of this block's assignments
+    int32_t *all = base + a.E;                            // [E] assignments of all blocks
+    const int warp = threadIdx.x >> 5, lane = (int)lane_id();
+    const int per = (a.T + (int)gridDim.x - 1) / (int)gridDim.x;
+    const int t0 = min(a.T, (int)blockIdx.x * per), t1 = min(a.T, t0 + per);
+
+    // ---- the k largest of each token
+    bool odd = false;
+    for (int t = t0 + warp; t < t1; t += kRouteWarps) {
+        const char *row = static_cast<const char *>(a.logits) + (int64_t)t * a.ldl * (a.f32 ? 4 : 2);
+        uint32_t key[V];
+        float x[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const int e = i * 32 + lane;
+            x[i] = e < a.E ? load_logit(row, e, a.f32 != 0) : -INFINITY;
+            odd |= !(x[i] < INFINITY);                    // NaN or plus infinity
+            key[i] = e < a.E ? logit_key(x[i]) : 0u;
+        }
+        float mine = -INFINITY, top = -INFINITY;          // lane j: the j-th logit
+        int chosen = 0;
+        for (int j = 0; j < a.k; ++j) {
+            uint32_t best = 0;
+            int at = 0x7FFFFFFF;
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if (key[i] > best) { best = key[i]; at = i * 32 + lane; }
+            const uint32_t most = __reduce_max_sync(0xFFFFFFFFu, best);
+            const int e = (int)__reduce_min_sync(0xFFFFFFFFu, best == most ? (uint32_t)at : 0x7FFFFFFFu);
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if (i * 32 + lane == e) key[i] = 0u;
+            if (j == 0) top = key_logit(most);
+            if (lane == j) { mine = key_logit(most); chosen = e; }
+        }
+        const bool some = top > -INFINITY;                // else no expert is allowed: weights 0
+        const float p = some && lane < a.k ? expf(mine - top) : 0.0f;
+        float total;
+        if (a.renorm) {
+            total = warp_sum(p);
+        } else {
+            total = 0.0f;
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if (some && i * 32 + lane < a.E) total += x[i] == x[i] ? expf(x[i] - top) : 0.0f;
+            total = warp_sum(total);
+        }
+        if (lane < a.k) {
+            a.weights[(int64_t)t * a.k + lane] = some ? p / total : 0.0f;
+            a.experts[(int64_t)t * a.k + lane] = chosen;
+        }
+    }
+    if (__any_sync(0xFFFFFFFFu, odd) && lane == 0) atomicOr(a.flags, (uint32_t)EMU_FLAG_NONFINITE);
+
+    // ---- assignments per warp (a contiguous range each) and expert
+    for (int i = threadIdx.x; i < kRouteWarps * a.E; i += kRouteThreads) hist[i] = 0;
+    __syncthreads();
+    const int n = (t1 - t0) * a.k, wper = (n + kRouteThreads - 1) / kRouteThreads * 32;
+    const int w0 = min(n, warp * wper), w1 = min(n, w0 + wper);
+    const int32_t *ex = a.experts + (int64_t)t0 * a.k;
+    int32_t *h = hist + warp * a.E;
+    for (int i = w0; i < w1; i += 32) {
+        const int e = i + lane < w1 ? ex[i + lane] : -1;
+        const uint32_t same = __match_any_sync(0xFFFFFFFFu, e);
+        if (e >= 0 && lane == __ffs(same) - 1) h[e] += __popc(same);
+        __syncwarp();
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < a.E; e += kRouteThreads) {
+        int sum = 0;
+#pragma unroll 8
+        for (int w = 0; w < kRouteWarps; ++w) {
+            const int c = hist[w * a.E + e];
+            hist[w * a.E + e] = sum;
+            sum += c;
+        }
+        all[e] = sum;
+        base[e] = 0;
+        if (gridDim.x > 1) a.counts[(int64_t)blockIdx.x * a.E + e] = sum;
+    }
+    if (gridDim.x > 1) {
+        route_barrier(a.bar, a.flags);
+        for (int e = threadIdx.x; e < a.E; e += kRouteThreads) all[e] = 0;
+        __syncthreads();
+        // groups of threads sum up a share of the blocks for every expert
+        const int width = (a.E + 31) / 32 * 32, parts = max(1, kRouteThreads / width);
+        const int share = ((int)gridDim.x + parts - 1) / parts;
+        for (int i = threadIdx.x; i < width * parts; i += kRouteThreads) {
+            const int e = i % width, b0 = (i / width) * share, b1 = min((int)gridDim.x, b0 + share);
+            if (e < a.E) {
+                int before = 0, sum = 0;
+#pragma unroll 8
+                for (int b = b0; b < b1; ++b) {
+                    const int c = __ldcg(a.counts + (int64_t)b * a.E + e);
+                    sum += c;
+                    if (b < (int)blockIdx.x) before += c;
+                }
+                atomicAdd(all + e, sum);                  // integers: the order does not matter
+                atomicAdd(base + e, before);
+            }
+        }
+    }
+    __syncthreads();
+    if (warp == 0) {                                      // experts' first slots
+        int carry = 0;
+        for (int e0 = 0; e0 < a.E; e0 += 32) {
+            const int e = e0 + lane, c = e < a.E ? all[e] : 0;
+            int v = c;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int u = __shfl_up_sync(0xFFFFFFFFu, v, d);
+                if (lane >= d) v += u;
+            }
+            if (e < a.E) {
+                base[e] += carry + v - c;
+                if (blockIdx.x == 0) a.ends[e] = carry + v;
+            }
+            carry += __shfl_sync(0xFFFFFFFFu, v, 31);
+        }
+    }
+    __syncthreads();
+
+    // ---- slots: behind the same expert's assignments of earlier blocks, warps and lanes
+    for (int i = w0; i < w1; i += 32) {
+        const int e = i + lane < w1 ? ex[i + lane] : -1;
+        const uint32_t same = __match_any_sync(0xFFFFFFFFu, e);
+        if (e >= 0) {
+            const int slot = base[e] + h[e] + __popc(same & ((1u << lane) - 1u));
+            const int64_t at = (int64_t)t0 * a.k + i + lane;
+            a.slots[at] = slot;
+            a.rows[slot] = (int32_t)(at / a.k);
+        }
+        __syncwarp();
+        if (e >= 0 && lane == __ffs(same) - 1) h[e] += __popc(same);
+        __syncwarp();
+    }
+}
+
+struct RouteBackArgs {
+    const void *logits;
+    int64_t ldl;
+    const int32_t *experts;
+    const float *dw;
+    void *dl;
+    int64_t lddl;
+    int T, E, k, f32, renorm;
+};
+
+// One warp per token.  With p the probabilities that the weights came from
+// (over the chosen experts, or over all) and g the weights' gradients:
+// dl_e = p_e ([e chosen] g_e - sum over the chosen of p g).
+template <int V>
+__global__ void __launch_bounds__(256) route_backward_kernel(const RouteBackArgs a)
+{
+    const int lane = (int)lane_id();
+    for (int64_t t = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); t < a.T; t += (int64_t)gridDim.x * 8) {
+        const char *row = static_cast<const char *>(a.logits) + t * a.ldl * (a.f32 ? 4 : 2);
+        float x[V], g[V];
+        uint32_t sel = 0;
+        float top = -INFINITY;
+        const int mine = lane < a.k ? __ldg(a.experts + t * a.k + lane) : -1;
+        const float gm = lane < a.k ? __ldg(a.dw + t * a.k + lane) : 0.0f;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const int e = i * 32 + lane;
+            x[i] = e < a.E ? load_logit(row, e, a.f32 != 0) : -INFINITY;
+            if (!(x[i] == x[i])) x[i] = -INFINITY;
+            g[i] = 0.0f;
+        }
+        for (int j = 0; j < a.k; ++j) {
+            const int e = __shfl_sync(0xFFFFFFFFu, mine, j);
+            const float ge = __shfl_sync(0xFFFFFFFFu, gm, j);
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if (i * 32 + lane == e) { g[i] = ge; sel |= 1u << i; }
+        }
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (!a.renorm || (sel >> i & 1u)) top = fmaxf(top, x[i]);
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+        const bool some = top > -INFINITY;
+        float total = 0.0f;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const bool in = some && i * 32 + lane < a.E && (!a.renorm || (sel >> i & 1u));
+            x[i] = in ? expf(x[i] - top) : 0.0f;
+            total += x[i];
+        }
+        total = warp_sum(total);
+        float inner = 0.0f;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            x[i] = some ? x[i] / total : 0.0f;
+            if (sel >> i & 1u) inner += x[i] * g[i];
+        }
+        inner = warp_sum(inner);
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const int e = i * 32 + lane;
+            const float d = x[i] * ((sel >> i & 1u ? g[i] : 0.0f) - inner);
+            if (e < a.E) {
+                if (a.f32) static_cast<float *>(a.dl)[t * a.lddl + e] = d;
+                else static_cast<uint16_t *>(a.dl)[t * a.lddl + e] = f32_bf16(d);
+            }
+        }
+    }
+}
+
+// ------------------------------------------------------------------ combine
+struct CombineArgs {
+    const void *Y, *dO;
+    int64_t yrows, ldy, ldo, lddy;
+    const int32_t *slots;
+    const float *weights;
+    void *O, *dY;
+    float *dw;
+    int64_t T;
+    int k, cols, vec;
+};
+
+// A 16-byte piece of a row as floats: 4 FP32 or 8 BF16.
+template <bool F32>
+struct Piece {
+    static constexpr int N = F32 ? 4 : 8;
+    float x[N];
+    __device__ __forceinline__ void load(const void *row, int64_t c, int cols, bool vec)
+    {
+        if constexpr (F32) {
+            const float *p = static_cast<const float *>(row) + c;
+            if (vec) {
+                const float4 v = __ldg(reinterpret_cast<const float4 *>(p));
+                x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+            } else {
+#pragma unroll
+                for (int i = 0; i < N; ++i) x[i] = c + i < cols ? __ldg(p + i) : 0.0f;
+            }
+        } else {
+            const uint16_t *p = static_cast<const uint16_t *>(row) + c;
+            if (vec) {
+                const uint4 v = __ldg(reinterpret_cast<const uint4 *>(p));
+                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    x[2 * i] = __uint_as_float(w[i] << 16);
+                    x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < N; ++i) x[i] = c + i < cols ? bf16_f32(__ldg(p + i)) : 0.0f;
+            }
+        }
+    }
+    __device__ __forceinline__ void store(void *row, int64_t c, int cols, bool vec) const
+    {
+        if constexpr (F32) {
+            float *p = static_cast<float *>(row) + c;
+            if (vec) {
+                *reinterpret_cast<float4 *>(p) = make_float4(x[0], x[1], x[2], x[3]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    if (c + i < cols) p[i] = x[i];
+            }
+        } else {
+            uint16_t *p = static_cast<uint16_t *>(row) + c;
+            if (vec) {
+                *reinterpret_cast<uint4 *>(p) = make_uint4(bf16x2_rn(x[0], x[1]), bf16x2_rn(x[2], x[3]),
+                                                           bf16x2_rn(x[4], x[5]), bf16x2_rn(x[6], x[7]));
+            } else {
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    if (c + i < cols) p[i] = f32_bf16(x[i]);
+            }
+        }
+    }
+};
+
+// O[t] = sum_j w[t, j] Y[slots[t, j]], j ascending, in FP32; a thread has one
+// 16-byte piece of one token, its k loads independent.
+template <bool F32>
+__global__ void __launch_bounds__(256) combine_kernel(const CombineArgs a)
+{
+    constexpr int N = Piece<F32>::N, ES = F32 ? 4 : 2;
+    const int pieces = (a.cols + N - 1) / N;
+    const int64_t total = a.T * pieces;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+        const int64_t t = i / pieces, c = (i - t * pieces) * N;
+        const bool vec = a.vec && c + N <= a.cols;
+        Piece<F32> acc;
+#pragma unroll
+        for (int e = 0; e < N; ++e) acc.x[e] = 0.0f;
+#pragma unroll 4
+        for (int j = 0; j < a.k; ++j) {
+            const int64_t s = __ldg(a.slots + t * a.k + j);
+            if (s < 0 || s >= a.yrows) continue;
+            const float w = a.weights ? __ldg(a.weights + t * a.k + j) : 1.0f;
+            Piece<F32> y;
+            y.load(static_cast<const char *>(a.Y) + s * a.ldy * ES, c, a.cols, vec);
+#pragma unroll
+            for (int e = 0; e < N; ++e) acc.x[e] = fmaf(w, y.x[e], acc.x[e]);
+        }
+        acc.store(static_cast<char *>(a.O) + t * a.ldo * ES, c, a.cols, vec);
+    }
+}
+
+// dY[slots[t, j]] = w[t, j] dO[t], dw[t, j] = Y[slots[t, j]] . dO[t]; a warp
+// per (t, j), so that a token's k warps share its dO row in the caches.
+template <bool F32>
+__global__ void __launch_bounds__(256) combine_backward_kernel(const CombineArgs a)
+{
+    constexpr int N = Piece<F32>::N, ES = F32 ? 4 : 2;
+    const int lane = (int)lane_id();
+    for (int64_t i = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); i < a.T * a.k; i += (int64_t)gridDim.x * 8) {
+        const int64_t t = i / a.k, s = __ldg(a.slots + i);
+        const bool ok = s >= 0 && s < a.yrows;
+        const float w = a.weights ? __ldg(a.weights + i) : 1.0f;
+        const char *dO = static_cast<const char *>(a.dO) + t * a.ldo * ES;
+        const char *y = static_cast<const char *>(a.Y) + s * a.ldy * ES;
+        char *dY = static_cast<char *>(a.dY) + s * a.lddy * ES;
+        float dot = 0.0f;
+        if (ok) {
+#pragma unroll 4
+            for (int64_t c = (int64_t)lane * N; c < a.cols; c += 32 * N) {
+                const bool vec = a.vec && c + N <= a.cols;
+                Piece<F32> d, v;
+                d.load(dO, c, a.cols, vec);
+                if (a.dw) {
+                    v.load(y, c, a.cols, vec);
+#pragma unroll
+                    for (int e = 0; e < N; ++e) dot = fmaf(v.x[e], d.x[e], dot);
+                }
+#pragma unroll
+                for (int e = 0; e < N; ++e) d.x[e] *= w;
+                d.store(dY, c, a.cols, vec);
+            }
+        }
+        if (a.dw) {
+            dot = warp_sum(dot);
+            if (lane == 0) a.dw[i] = ok ? dot : 0.0f;
+        }
+    }
+}
+
+bool can_vec(const void *p, int64_t ld, int esize)
+{
+    return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && ld * esize % 16 == 0;
+}
+
+template <int V>
+cudaError_t run_route(const RouteArgs &a, int blocks, cudaStream_t st)
+{
+    const size_t sm = (size_t)(kRouteWarps + 2) * a.E * sizeof(int32_t);
+    auto kern = route_kernel<V>;
+    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sm);
+    if (e != cudaSuccess) return e;
+    if (blocks == 1) {
+        kern<<<1, kRouteThreads, sm, st>>>(a);
+        return cudaGetLastError();
+    }
+    void *args[] = {(void *)&a};
+    return cudaLaunchCooperativeKernel((const void *)kern, dim3((unsigned)blocks), dim3(kRouteThreads), args, sm, st);
+}
+
+template <int V>
+cudaError_t run_route_back(const RouteBackArgs &a, cudaStream_t st)
+{
+    const int64_t blocks = ((int64_t)a.T + 7) / 8;
+    route_backward_kernel<V><<<(unsigned)(blocks > 152 * 16 ? 152 * 16 : blocks), 256, 0, st>>>(a);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+size_t route_scratch_bytes(int64_t E) { return (size_t)kRouteBlocks * (size_t)E * sizeof(int32_t); }
+
+cudaError_t launch_route(int64_t T, int64_t E, int k, bool renorm, const void *logits, bool f32, int64_t ldl,
+                         float *weights, int32_t *experts, int32_t *slots, int32_t *rows, int32_t *ends,
+                         int32_t *counts, WsHeader *ws, cudaStream_t st)
+{
+    RouteArgs a = {};
+    a.logits = logits; a.ldl = ldl; a.T = (int)T; a.E = (int)E; a.k = k; a.f32 = f32; a.renorm = renorm;
+    a.weights = weights; a.experts = experts; a.slots = slots; a.rows = rows; a.ends = ends; a.counts = counts;
+    a.flags = &ws->flags; a.bar = &ws->fix_any;
+    // a warp per token while there are SMs left
+    int64_t blocks = (T + kRouteWarps - 1) / kRouteWarps;
+    int dev = 0, sms = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess ||
+        cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sms < 1)
+        return cudaErrorInvalidDevice;
+    const int64_t most = sms < kRouteBlocks ? sms : kRouteBlocks;     // one block per SM: all of them run at once
+    if (blocks > most) blocks = most;
+    if (blocks < 1) blocks = 1;
+    const int v = (int)((E + 31) / 32);
+    return v <= 1 ? run_route<1>(a, (int)blocks, st) : v <= 2 ? run_route<2>(a, (int)blocks, st)
+           : v <= 4 ? run_route<4>(a, (int)blocks, st) : v <= 8 ? run_route<8>(a, (int)blocks, st)
+           : v <= 16 ? run_route<16>(a, (int)blocks, st) : run_route<32>(a, (int)blocks, st);
+}
+
+cudaError_t launch_route_backward(int64_t T, int64_t E, int k, bool renorm, const void *logits, bool f32, int64_t ldl,
+                                  const int32_t *experts, const float *dw, void *dl, int64_t lddl, cudaStream_t st)
+{
+    RouteBackArgs a = {};
+    a.logits = logits; a.ldl = ldl; a.experts = experts; a.dw = dw; a.dl = dl; a.lddl = lddl;
+    a.T = (int)T; a.E = (int)E; a.k = k; a.f32 = f32; a.renorm = renorm;
+    const int v = (int)((E + 31) / 32);
+    return v <= 1 ? run_route_back<1>(a, st) : v <= 2 ? run_route_back<2>(a, st) : v <= 4 ? run_route_back<4>(a, st)
+           : v <= 8 ? run_route_back<8>(a, st) : v <= 16 ? run_route_back<16>(a, st) : run_route_back<32>(a, st);
+}
+
+cudaError_t launch_combine(bool f32, int64_t T, int k, int64_t cols, const void *Y, int64_t yrows, int64_t ldy,
+                           const int32_t *slots, const float *weights, void *O, int64_t ldo, cudaStream_t st)
+{
+    CombineArgs a = {};
+    a.Y = Y; a.yrows = yrows; a.ldy = ldy; a.slots = slots; a.weights = weights; a.O = O; a.ldo = ldo;
+    a.T = T; a.k = k; a.cols = (int)cols;
+    const int es = f32 ? 4 : 2;
+    a.vec = can_vec(Y, ldy, es) && can_vec(O, ldo, es);
+    const int64_t total = T * ((cols + (f32 ? 3 : 7)) / (f32 ? 4 : 8)), blocks = (total + 255) / 256;
+    const unsigned grid = (unsigned)(blocks > 152 * 64 ? 152 * 64 : blocks);
+    if (f32) combine_kernel<true><<<grid, 256, 0, st>>>(a);
+    else combine_kernel<false><<<grid, 256, 0, st>>>(a);
+    return cudaGetLastError();
+}
+
+cudaError_t launch_combine_backward(bool f32, int64_t T, int k, int64_t cols, const void *dO, int64_t lddo,
+                                    const void *Y, int64_t yrows, int64_t ldy, const int32_t *slots,
+                                    const float *weights, void *dY, int64_t lddy, float *dw, cudaStream_t st)
+{
+    CombineArgs a = {};
+    a.Y = Y; a.dO = dO; a.yrows = yrows; a.ldy = ldy; a.ldo = lddo; a.lddy = lddy; a.slots = slots;
+    a.weights = weights; a.dY = dY; a.dw = dw; a.T = T; a.k = k; a.cols = (int)cols;
+    const int es = f32 ? 4 : 2;
+    a.vec = (!dw || can_vec(Y, ldy, es)) && can_vec(dO, lddo, es) && can_vec(dY, lddy, es);
+    const int64_t blocks = (T * k + 7) / 8;
+    const unsigned grid = (unsigned)(blocks > 152 * 64 ? 152 * 64 : blocks);
+    if (f32) combine_backward_kernel<true><<<grid, 256, 0, st>>>(a);
+    else combine_backward_kernel<false><<<grid, 256, 0, st>>>(a);
+    return cudaGetLastError();
+}
+
+}  // namespace emu
