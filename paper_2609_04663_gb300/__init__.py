@@ -384,9 +384,17 @@ def prodsum_f64(Ap, Bp, M: int, N: int, K: int, nprod: int, vA=None, vB=None, C=
 
 
 # ------------------------------------------------------------- expert layers
-def _need(ok, what):
-    if not ok:
-        raise ValueError(what)
+# Small calls take a few microseconds on the GPU, so these helpers keep the
+# host's share small: plain comparisons, messages only made when one fails.
+def _bad(where, what):
+    raise ValueError(f"{where}: {what}")
+
+
+def _raw_stream(stream, device):
+    """The CUDA stream handle to launch on (None: PyTorch's current one)."""
+    if stream is None:
+        return _torch()._C._cuda_getCurrentRawStream(device.index)
+    return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
 def _torch_stream(stream, device):
@@ -407,25 +415,34 @@ def _empty(shape, dtype, device, stream):
 
 def _dtype(t, where):
     torch = _torch()
-    _need(t.dtype in (torch.float32, torch.bfloat16), f"{where}: float32 or bfloat16 is needed, got {t.dtype}")
-    return F32 if t.dtype == torch.float32 else BF16
+    if t.dtype is torch.float32:
+        return F32
+    if t.dtype is torch.bfloat16:
+        return BF16
+    _bad(where, f"float32 or bfloat16 is needed, got {t.dtype}")
 
 
 def _ints(t, numel, device, where):
-    torch = _torch()
-    _need(t.dtype == torch.int32 and t.is_contiguous() and t.device == device,
-          f"{where}: a contiguous int32 tensor on {device} is needed")
-    _need(numel is None or t.numel() == numel, f"{where}: {numel} entries are needed, got {t.numel()}")
+    """Address of an int32 tensor of `numel` entries (None: any number)."""
+    if t.dtype is not _torch().int32 or t.device != device or not t.is_contiguous():
+        _bad(where, f"a contiguous int32 tensor on {device} is needed")
+    if numel is not None and t.numel() != numel:
+        _bad(where, f"{numel} entries are needed, got {t.numel()}")
     return t.data_ptr()
 
 
-def _rows_of(t, where):
-    """Row pitch of a 2-D (or last two dimensions of a 3-D) tensor with contiguous rows."""
-    _need(t.is_cuda, f"{where}: a CUDA tensor is needed")
-    _need(t.shape[-1] <= 1 or t.stride(-1) == 1, f"{where}: rows have to be contiguous")
-    pitch = t.stride(-2) if t.shape[-2] > 1 else t.shape[-1]
-    _need(pitch >= t.shape[-1], f"{where}: rows overlap")
-    return max(pitch, 1)
+def _pitch(t, where, device=None):
+    """Row pitch of a CUDA tensor whose rows are contiguous (on `device`, if given)."""
+    if not t.is_cuda or (device is not None and t.device != device):
+        _bad(where, f"a tensor on {device or 'a GPU'} is needed, got one on {t.device}")
+    rows, cols = t.shape[-2:]
+    st = t.stride()
+    if cols > 1 and st[-1] != 1:
+        _bad(where, "rows have to be contiguous")
+    pitch = st[-2] if rows > 1 else cols
+    if pitch < cols:
+        _bad(where, "rows overlap")
+    return pitch or 1
 
 
 class GroupedPlanes:
@@ -438,43 +455,50 @@ class GroupedPlanes:
         self.device, self.nslices, self.ld = planes.device, planes.shape[0], planes.shape[2]
 
 
+def _slices(t, where):
+    return t.nslices if isinstance(t, GroupedPlanes) else (3 if _dtype(t, where) == F32 else 1)
+
+
 def grouped_split(X, ends=None, src=None, planes=None, ws=None, stream=None):
     """emu_grouped_split / emu_grouped_split_rows: the planes of weights X
     [G, rows, cols] (ends None), or of token rows X[src] (src None: X) grouped
     by ends; three for FP32 (Eq. (fp32split)), one for BF16.  A plane set can
     stand for its operand in grouped_gemm and grouped_wgrad, in all directions."""
-    torch = _torch()
-    dt, ldx = _dtype(X, "grouped_split"), _rows_of(X, "grouped_split")
+    torch, where = _torch(), "grouped_split"
+    dt, ldx, dev = _dtype(X, where), _pitch(X, where), X.device
     cols = X.shape[-1]
     S, ld = (3 if dt == F32 else 1), gemm_ldk(cols)
-    ws = ws if ws is not None else _empty(emu_split_workspace_bytes(32), torch.uint8, X.device, stream)
+    if ws is None:
+        ws = _empty(emu_split_workspace_bytes(32), torch.uint8, dev, stream)
     if ends is None:
-        _need(X.dim() == 3 and src is None, "grouped_split: weights are [G, rows, cols]; token rows need ends")
+        if X.dim() != 3 or src is not None:
+            _bad(where, "weights are [G, rows, cols]; token rows need ends")
         G, rows = X.shape[0], X.shape[1]
         shape, prows = (G, rows, cols), G * rows
     else:
-        _need(X.dim() == 2, "grouped_split: token rows are [rows, cols]")
+        if X.dim() != 2:
+            _bad(where, "token rows are [rows, cols]")
         G, rows = ends.numel(), (src.numel() if src is not None else X.shape[0])
         shape, prows = (rows, cols), emu_grouped_plane_rows(rows, G)
     if planes is None:
-        planes = _empty((S, prows, ld), torch.int16, X.device, stream)
-    _need(tuple(planes.shape) == (S, prows, ld) and planes.dtype == torch.int16 and planes.is_contiguous(),
-          f"grouped_split: planes have to be contiguous int16 {(S, prows, ld)}")
+        planes = _empty((S, prows, ld), torch.int16, dev, stream)
+    elif planes.shape != (S, prows, ld) or planes.dtype is not torch.int16 or not planes.is_contiguous():
+        _bad(where, f"planes have to be contiguous int16 {(S, prows, ld)}")
     if ends is None:
-        r = emu_grouped_split(dt, G, rows, cols, X.data_ptr(), ldx, X.stride(0) if G > 1 else 0, planes.data_ptr(),
-                              ld, ws.data_ptr(), ws.numel(), _stream(stream))
+        r = load().emu_grouped_split(dt, G, rows, cols, X.data_ptr(), ldx, X.stride(0) if G > 1 else 0,
+                                     planes.data_ptr(), ld, ws.data_ptr(), ws.numel(), _raw_stream(stream, dev))
     else:
-        r = emu_grouped_split_rows(dt, rows, cols, X.data_ptr(), X.shape[0], ldx,
-                                   _ints(src, None, X.device, "grouped_split: src") if src is not None else None,
-                                   _ints(ends, G, X.device, "grouped_split: ends"), G, planes.data_ptr(), ld,
-                                   ws.data_ptr(), ws.numel(), _stream(stream))
+        r = load().emu_grouped_split_rows(dt, rows, cols, X.data_ptr(), X.shape[0], ldx,
+                                          _ints(src, None, dev, "grouped_split: src") if src is not None else None,
+                                          _ints(ends, G, dev, "grouped_split: ends"), G, planes.data_ptr(), ld,
+                                          ws.data_ptr(), ws.numel(), _raw_stream(stream, dev))
     _check(r, "emu_grouped_split")
     return GroupedPlanes(planes, shape, ends is not None)
 
 
-def _tma_ok(t):
+def _tma_ok(t, pitch):
     """Whether a BF16 tensor can be read by the tensor memory accelerator as it stands."""
-    return (t.data_ptr() % 16 == 0 and _rows_of(t, "operand") % 8 == 0 and
+    return (t.data_ptr() % 16 == 0 and pitch % 8 == 0 and
             (t.dim() < 3 or t.shape[0] <= 1 or (t.stride(0) % 8 == 0 and t.stride(0) >= 0)))
 
 
@@ -495,40 +519,55 @@ def grouped_gemm(X, W, ends, opW: int = OP_N, src=None, Y=None, ws=None, stream=
     of grouped_split.  Y: FP32, or BF16 / FP32 for BF16 operands (given Y
     decides; BF16 otherwise).  Returns (Y, ws).  The gradient of X is
     grouped_gemm(dY, W, ends, the other op)."""
-    torch = _torch()
+    torch, where = _torch(), "grouped_gemm"
     G, dev = ends.numel(), X.device
     xp, wp = isinstance(X, GroupedPlanes), isinstance(W, GroupedPlanes)
-    _need(len(W.shape) == 3 and W.shape[0] == G, f"grouped_gemm: W has to be [{G}, ., .], got {tuple(W.shape)}")
-    _need(len(X.shape) == 2 and (not xp or (X.padded and src is None)), "grouped_gemm: X has to be token rows")
+    if len(W.shape) != 3 or W.shape[0] != G:
+        _bad(where, f"W has to be [{G}, ., .], got {tuple(W.shape)}")
+    if len(X.shape) != 2 or (xp and (not X.padded or src is not None)):
+        _bad(where, "X has to be token rows")
     K, N = (W.shape[2], W.shape[1]) if opW == OP_T else (W.shape[1], W.shape[2])
-    _need(X.shape[1] == K, f"grouped_gemm: X has {X.shape[1]} columns, op(W) {K} rows")
-    S = X.nslices if xp else (3 if _dtype(X, "grouped_gemm: X") == F32 else 1)
-    _need(S == (W.nslices if wp else (3 if _dtype(W, "grouped_gemm: W") == F32 else 1)),
-          "grouped_gemm: X and W have to be of one type")
+    if X.shape[1] != K:
+        _bad(where, f"X has {X.shape[1]} columns, op(W) {K} rows")
+    S = _slices(X, where)
+    if S != _slices(W, where) or W.device != dev:
+        _bad(where, "X and W have to be of one type, on one device")
     rows = src.numel() if src is not None else X.shape[0]
     if Y is None:
-        Y = _empty((rows, N), torch.float32 if S == 3 else torch.bfloat16, dev, stream)
-    yt, ldy = _dtype(Y, "grouped_gemm: Y"), _rows_of(Y, "grouped_gemm: Y")
-    _need(tuple(Y.shape) == (rows, N) and (S == 1 or yt == F32), "grouped_gemm: Y has another shape or type")
+        Y, yt = _empty((rows, N), torch.float32 if S == 3 else torch.bfloat16, dev, stream), (F32 if S == 3 else BF16)
+    else:
+        yt = _dtype(Y, where)
+    ldy = _pitch(Y, "grouped_gemm: Y", dev)
+    if Y.shape != (rows, N) or (S == 3 and yt != F32):
+        _bad(where, "Y has another shape or type")
     pe = _ints(ends, G, dev, "grouped_gemm: ends")
-    ps = _ints(src, None, dev, "grouped_gemm: src") if src is not None else None
+    ldx = X.ld if xp else _pitch(X, "grouped_gemm: X")
+    ldw = W.ld if wp else _pitch(W, "grouped_gemm: W")
+    raw = _raw_stream(stream, dev)
     if S == 3 and not xp and not wp:
-        ws = ws if ws is not None else _empty(emu_grouped_gemm_workspace_bytes(F32, G, rows, N, K), torch.uint8, dev,
-                                              stream)
-        _check(emu_grouped_gemm_f32(opW, G, rows, N, K, X.data_ptr(), X.shape[0], _rows_of(X, "X"), ps, W.data_ptr(),
-                                    _rows_of(W, "W"), W.stride(0) if G > 1 else 0, pe, Y.data_ptr(), ldy,
-                                    ws.data_ptr(), ws.numel(), _stream(stream)), "emu_grouped_gemm_f32")
+        ps = _ints(src, None, dev, "grouped_gemm: src") if src is not None else None
+        if ws is None:
+            ws = _empty(emu_grouped_gemm_workspace_bytes(F32, G, rows, N, K), torch.uint8, dev, stream)
+        r = load().emu_grouped_gemm_f32(opW, G, rows, N, K, X.data_ptr(), X.shape[0], ldx, ps, W.data_ptr(), ldw,
+                                        W.stride(0) if G > 1 else 0, pe, Y.data_ptr(), ldy, ws.data_ptr(), ws.numel(),
+                                        raw)
+        if r:
+            _check(r, "emu_grouped_gemm_f32")
         return Y, ws
-    ws = ws if ws is not None else _empty(emu_split_workspace_bytes(32), torch.uint8, dev, stream)
-    if not xp and (S == 3 or src is not None or not _tma_ok(X)):
+    if ws is None:
+        ws = _empty(emu_split_workspace_bytes(32), torch.uint8, dev, stream)
+    if not xp and (S == 3 or src is not None or not _tma_ok(X, ldx)):
         X, xp = grouped_split(X, ends, src, ws=ws, stream=stream), True
-    if not wp and (S == 3 or not _tma_ok(W)):
+        ldx = X.ld
+    if not wp and (S == 3 or not _tma_ok(W, ldw)):
         W, wp = grouped_split(W, ws=ws, stream=stream), True
-    xptr, ldx = (X.planes.data_ptr(), X.ld) if xp else (X.data_ptr(), _rows_of(X, "X"))
-    wptr, ldw = (W.planes.data_ptr(), W.ld) if wp else (W.data_ptr(), _rows_of(W, "W"))
-    stride = W.shape[1] * ldw if wp or G <= 1 else W.stride(0)
-    _check(emu_grouped_prodsum(S, opW, G, rows, N, K, xptr, ldx, int(xp), wptr, ldw, stride, pe, Y.data_ptr(), yt, ldy,
-                               ws.data_ptr(), ws.numel(), _stream(stream)), "emu_grouped_prodsum")
+        ldw = W.ld
+    r = load().emu_grouped_prodsum(S, opW, G, rows, N, K, X.planes.data_ptr() if xp else X.data_ptr(), ldx, int(xp),
+                                   W.planes.data_ptr() if wp else W.data_ptr(), ldw,
+                                   W.shape[1] * ldw if wp or G <= 1 else W.stride(0), pe, Y.data_ptr(), yt, ldy,
+                                   ws.data_ptr(), ws.numel(), raw)
+    if r:
+        _check(r, "emu_grouped_prodsum")
     return Y, ws
 
 
@@ -537,26 +576,28 @@ def grouped_wgrad(A, B, ends, srcA=None, srcB=None, D=None, ws=None, stream=None
     gradient of W is grouped_wgrad(X, dY) for OP_N and grouped_wgrad(dY, X)
     for OP_T.  A and B: token rows of one type, or plane sets of
     grouped_split.  D as Y in grouped_gemm.  Returns (D, ws)."""
-    torch = _torch()
+    torch, where = _torch(), "grouped_wgrad"
     G, dev = ends.numel(), A.device
-    ws = ws if ws is not None else _empty(emu_split_workspace_bytes(32), torch.uint8, dev, stream)
-    ops = []
-    for t, src, name in ((A, srcA, "A"), (B, srcB, "B")):
-        if not isinstance(t, GroupedPlanes):
-            t = grouped_split(t, ends, src, ws=ws, stream=stream)
-        _need(t.padded, f"grouped_wgrad: {name} has to be token rows")
-        ops.append(t)
-    A, B = ops
-    _need(A.shape[0] == B.shape[0] and A.nslices == B.nslices, "grouped_wgrad: A and B differ in rows or type")
+    if ws is None:
+        ws = _empty(emu_split_workspace_bytes(32), torch.uint8, dev, stream)
+    if not isinstance(A, GroupedPlanes):
+        A = grouped_split(A, ends, srcA, ws=ws, stream=stream)
+    if not isinstance(B, GroupedPlanes):
+        B = grouped_split(B, ends, srcB, ws=ws, stream=stream)
+    if not A.padded or not B.padded or A.shape[0] != B.shape[0] or A.nslices != B.nslices or B.device != dev:
+        _bad(where, "A and B have to be token rows, as many and of one type, on one device")
     (rows, M), N, S = A.shape, B.shape[1], A.nslices
     if D is None:
         D = _empty((G, M, N), torch.float32 if S == 3 else torch.bfloat16, dev, stream)
-    dt, ldd = _dtype(D, "grouped_wgrad: D"), _rows_of(D, "grouped_wgrad: D")
-    _need(tuple(D.shape) == (G, M, N) and (S == 1 or dt == F32), "grouped_wgrad: D has another shape or type")
-    _check(emu_grouped_prodsum_wgrad(S, G, rows, M, N, A.planes.data_ptr(), A.ld, B.planes.data_ptr(), B.ld,
-                                     _ints(ends, G, dev, "grouped_wgrad: ends"), D.data_ptr(), dt, ldd,
-                                     D.stride(0) if G > 1 else M * ldd, ws.data_ptr(), ws.numel(), _stream(stream)),
-           "emu_grouped_prodsum_wgrad")
+    dt, ldd = _dtype(D, "grouped_wgrad: D"), _pitch(D, "grouped_wgrad: D", dev)
+    if D.shape != (G, M, N) or (S == 3 and dt != F32):
+        _bad(where, "D has another shape or type")
+    r = load().emu_grouped_prodsum_wgrad(S, G, rows, M, N, A.planes.data_ptr(), A.ld, B.planes.data_ptr(), B.ld,
+                                         _ints(ends, G, dev, "grouped_wgrad: ends"), D.data_ptr(), dt, ldd,
+                                         D.stride(0) if G > 1 else M * ldd, ws.data_ptr(), ws.numel(),
+                                         _raw_stream(stream, dev))
+    if r:
+        _check(r, "emu_grouped_prodsum_wgrad")
     return D, ws
 
 
@@ -566,27 +607,33 @@ def w4_matvec(X, Wq, scales, zeros=None, ends=None, Y=None, stream=None):
     [G, N, K/2], the even k in the low half of a byte; scales FP32 or BF16 and
     zeros uint8 (None: 8) [G, N, K/group].  X and Y: FP32 or BF16.  For a few
     rows per expert.  Returns Y."""
-    torch = _torch()
-    dev = X.device
-    dt, ldx = _dtype(X, "w4_matvec: X"), _rows_of(X, "w4_matvec: X")
-    lead, (N, half), (rows, K) = tuple(Wq.shape[:-2]), Wq.shape[-2:], X.shape
-    G = ends.numel() if ends is not None else 1
-    _need(K == 2 * half, f"w4_matvec: X has {K} columns, the weights {2 * half}")
-    _need(lead == ((G,) if ends is not None else ()), f"w4_matvec: weights of {lead} matrices for {G} groups")
-    ng = scales.shape[-1]
+    torch, where = _torch(), "w4_matvec"
+    dev, u8 = X.device, torch.uint8
+    dt, ldx, (rows, K) = _dtype(X, "w4_matvec: X"), _pitch(X, "w4_matvec: X"), X.shape
+    shape, sshape = Wq.shape, scales.shape
+    G = 1 if ends is None else ends.numel()
+    N, ng = shape[-2], sshape[-1]
+    if 2 * shape[-1] != K:
+        _bad(where, f"X has {K} columns, the weights {2 * shape[-1]}")
+    if len(shape) != (2 if ends is None else 3) or (ends is not None and shape[0] != G):
+        _bad(where, f"weights {tuple(shape)} for {G} group(s)")
     group = K // ng if ng else 32
-    _need(group * ng == K and tuple(scales.shape) == lead + (N, ng), "w4_matvec: scales have another shape")
-    for t, want, name in ((Wq, torch.uint8, "Wq"), (scales, scales.dtype, "scales"), (zeros, torch.uint8, "zeros")):
-        _need(t is None or (t.dtype == want and t.is_contiguous() and t.device == dev),
-              f"w4_matvec: {name} has to be contiguous {want} on {dev}")
-    _need(zeros is None or zeros.shape == scales.shape, "w4_matvec: zeros have another shape")
+    if group * ng != K or sshape[:-1] != shape[:-1] or (zeros is not None and zeros.shape != sshape):
+        _bad(where, "scales or zeros have another shape")
+    if Wq.dtype is not u8 or Wq.device != dev or not Wq.is_contiguous() or scales.device != dev or \
+            not scales.is_contiguous() or \
+            (zeros is not None and (zeros.dtype is not u8 or zeros.device != dev or not zeros.is_contiguous())):
+        _bad(where, f"Wq and zeros have to be uint8, all weights contiguous on {dev}")
     if Y is None:
         Y = _empty((rows, N), X.dtype, dev, stream)
-    _need(tuple(Y.shape) == (rows, N) and Y.dtype == X.dtype, "w4_matvec: Y has another shape or type")
-    _check(emu_w4_matvec(dt, G, rows, N, K, group, X.data_ptr(), ldx, Wq.data_ptr(), scales.data_ptr(),
-                         _dtype(scales, "w4_matvec: scales"), zeros.data_ptr() if zeros is not None else None,
-                         _ints(ends, G, dev, "w4_matvec: ends") if ends is not None else None, Y.data_ptr(),
-                         _rows_of(Y, "w4_matvec: Y"), _stream(stream)), "emu_w4_matvec")
+    elif Y.shape != (rows, N) or Y.dtype is not X.dtype:
+        _bad(where, "Y has another shape or type")
+    r = load().emu_w4_matvec(dt, G, rows, N, K, group, X.data_ptr(), ldx, Wq.data_ptr(), scales.data_ptr(),
+                             _dtype(scales, "w4_matvec: scales"), zeros.data_ptr() if zeros is not None else None,
+                             _ints(ends, G, dev, "w4_matvec: ends") if ends is not None else None, Y.data_ptr(),
+                             _pitch(Y, "w4_matvec: Y", dev), _raw_stream(stream, dev))
+    if r:
+        _check(r, "emu_w4_matvec")
     return Y
 
 
@@ -600,53 +647,60 @@ def route(logits, k: int, renorm: bool = True, ws=None, stream=None):
     rows [T k], ends [E]), ws): rows and ends are src and ends of grouped_gemm,
     slots and weights those of rows_combine."""
     torch = _torch()
-    dt, ldl = _dtype(logits, "route"), _rows_of(logits, "route")
-    (T, E), dev = logits.shape, logits.device
-    ws = ws if ws is not None else _empty(emu_route_workspace_bytes(T, E, k), torch.uint8, dev, stream)
-    weights = _empty((T, k), torch.float32, dev, stream)
-    experts, slots = (_empty((T, k), torch.int32, dev, stream) for _ in range(2))
-    rows, ends = _empty(T * k, torch.int32, dev, stream), _empty(E, torch.int32, dev, stream)
-    _check(emu_route(dt, T, E, k, int(renorm), logits.data_ptr(), ldl, weights.data_ptr(), experts.data_ptr(),
-                     slots.data_ptr(), rows.data_ptr(), ends.data_ptr(), ws.data_ptr(), ws.numel(), _stream(stream)),
-           "emu_route")
-    return Route(weights, experts, slots, rows, ends), ws
+    dt, ldl = _dtype(logits, "route"), _pitch(logits, "route")
+    (T, E), dev, i32 = logits.shape, logits.device, torch.int32
+    if ws is None:
+        ws = _empty(emu_route_workspace_bytes(T, E, k), torch.uint8, dev, stream)
+    out = Route(_empty((T, k), torch.float32, dev, stream), _empty((T, k), i32, dev, stream),
+                _empty((T, k), i32, dev, stream), _empty(T * k, i32, dev, stream), _empty(E, i32, dev, stream))
+    r = load().emu_route(dt, T, E, k, int(renorm), logits.data_ptr(), ldl, out[0].data_ptr(), out[1].data_ptr(),
+                         out[2].data_ptr(), out[3].data_ptr(), out[4].data_ptr(), ws.data_ptr(), ws.numel(),
+                         _raw_stream(stream, dev))
+    if r:
+        _check(r, "emu_route")
+    return out, ws
+
+
+def _float_pairs(t, shape, device, where):
+    """Address of a contiguous float32 tensor of this shape (None: none)."""
+    if t is None:
+        return None
+    if t.shape != shape or t.dtype is not _torch().float32 or t.device != device or not t.is_contiguous():
+        _bad(where, f"a contiguous float32 tensor {tuple(shape)} on {device} is needed")
+    return t.data_ptr()
 
 
 def route_backward(logits, experts, dweights, renorm: bool = True, dlogits=None, stream=None):
     """emu_route_backward: the logits' gradients from those of route's weights."""
-    torch = _torch()
-    dt, (T, E), k = _dtype(logits, "route_backward"), logits.shape, experts.shape[1]
+    where = "route_backward"
+    dt, (T, E), k, dev = _dtype(logits, where), logits.shape, experts.shape[1], logits.device
     if dlogits is None:
-        dlogits = _empty((T, E), logits.dtype, logits.device, stream)
-    _need(tuple(dlogits.shape) == (T, E) and dlogits.dtype == logits.dtype, "route_backward: dlogits differ from logits")
-    _need(tuple(dweights.shape) == (T, k) and dweights.dtype == torch.float32 and dweights.is_contiguous(),
-          "route_backward: dweights have to be contiguous float32 [T, k]")
-    _check(emu_route_backward(dt, T, E, k, int(renorm), logits.data_ptr(), _rows_of(logits, "route_backward"),
-                              _ints(experts, T * k, logits.device, "route_backward: experts"), dweights.data_ptr(),
-                              dlogits.data_ptr(), _rows_of(dlogits, "route_backward"), _stream(stream)),
-           "emu_route_backward")
+        dlogits = _empty((T, E), logits.dtype, dev, stream)
+    elif dlogits.shape != logits.shape or dlogits.dtype is not logits.dtype:
+        _bad(where, "dlogits differ from logits")
+    r = load().emu_route_backward(dt, T, E, k, int(renorm), logits.data_ptr(), _pitch(logits, where),
+                                  _ints(experts, T * k, dev, "route_backward: experts"),
+                                  _float_pairs(dweights, experts.shape, dev, "route_backward: dweights"),
+                                  dlogits.data_ptr(), _pitch(dlogits, where, dev), _raw_stream(stream, dev))
+    if r:
+        _check(r, "emu_route_backward")
     return dlogits
-
-
-def _weights(weights, shape, where):
-    torch = _torch()
-    if weights is None:
-        return None
-    _need(tuple(weights.shape) == tuple(shape) and weights.dtype == torch.float32 and weights.is_contiguous(),
-          f"{where}: weights have to be contiguous float32 {tuple(shape)}")
-    return weights.data_ptr()
 
 
 def rows_combine(Y, slots, weights=None, O=None, stream=None):
     """emu_rows_combine: O[t] = sum_j weights[t, j] Y[slots[t, j]] (weights None: 1)."""
-    dt, ldy, (T, k), cols = _dtype(Y, "rows_combine"), _rows_of(Y, "rows_combine"), slots.shape, Y.shape[1]
+    where = "rows_combine"
+    dt, ldy, shape, (yrows, cols), dev = _dtype(Y, where), _pitch(Y, where), slots.shape, Y.shape, Y.device
+    T, k = shape
     if O is None:
-        O = _empty((T, cols), Y.dtype, Y.device, stream)
-    _need(tuple(O.shape) == (T, cols) and O.dtype == Y.dtype, "rows_combine: O has another shape or type")
-    _check(emu_rows_combine(dt, T, k, cols, Y.data_ptr(), Y.shape[0], ldy,
-                            _ints(slots, T * k, Y.device, "rows_combine: slots"),
-                            _weights(weights, (T, k), "rows_combine"), O.data_ptr(), _rows_of(O, "rows_combine: O"),
-                            _stream(stream)), "emu_rows_combine")
+        O = _empty((T, cols), Y.dtype, dev, stream)
+    elif O.shape != (T, cols) or O.dtype is not Y.dtype:
+        _bad(where, "O has another shape or type")
+    r = load().emu_rows_combine(dt, T, k, cols, Y.data_ptr(), yrows, ldy, _ints(slots, T * k, dev, "rows_combine: slots"),
+                                _float_pairs(weights, shape, dev, "rows_combine: weights"), O.data_ptr(),
+                                _pitch(O, "rows_combine: O", dev), _raw_stream(stream, dev))
+    if r:
+        _check(r, "emu_rows_combine")
     return O
 
 
@@ -654,21 +708,25 @@ def rows_combine_backward(dO, Y, slots, weights=None, dY=None, stream=None):
     """emu_rows_combine_backward: (dY, dweights) of rows_combine(Y, slots,
     weights); dweights is None without weights.  No two slots may name the
     same row; rows of a dY made here that no slot names are zero."""
-    torch = _torch()
-    dt, (T, k), cols = _dtype(Y, "rows_combine_backward"), slots.shape, Y.shape[1]
-    _need(tuple(dO.shape) == (T, cols) and dO.dtype == Y.dtype, "rows_combine_backward: dO has another shape or type")
+    torch, where = _torch(), "rows_combine_backward"
+    dt, shape, (yrows, cols), dev = _dtype(Y, where), slots.shape, Y.shape, Y.device
+    T, k = shape
+    if dO.shape != (T, cols) or dO.dtype is not Y.dtype:
+        _bad(where, "dO has another shape or type")
     if dY is None:
-        dY = _empty(tuple(Y.shape), Y.dtype, Y.device, stream)
-        if Y.shape[0] != T * k:
-            with torch.cuda.stream(_torch_stream(stream, Y.device)):
+        dY = _empty((yrows, cols), Y.dtype, dev, stream)
+        if yrows != T * k:
+            with torch.cuda.stream(_torch_stream(stream, dev)):
                 dY.zero_()
-    _need(tuple(dY.shape) == tuple(Y.shape) and dY.dtype == Y.dtype, "rows_combine_backward: dY differs from Y")
-    dw = _empty((T, k), torch.float32, Y.device, stream) if weights is not None else None
-    _check(emu_rows_combine_backward(dt, T, k, cols, dO.data_ptr(), _rows_of(dO, "rows_combine_backward: dO"),
-                                     Y.data_ptr(), Y.shape[0], _rows_of(Y, "rows_combine_backward: Y"),
-                                     _ints(slots, T * k, Y.device, "rows_combine_backward: slots"),
-                                     _weights(weights, (T, k), "rows_combine_backward"), dY.data_ptr(),
-                                     _rows_of(dY, "rows_combine_backward: dY"),
-                                     dw.data_ptr() if dw is not None else None, _stream(stream)),
-           "emu_rows_combine_backward")
+    elif dY.shape != Y.shape or dY.dtype is not Y.dtype:
+        _bad(where, "dY differs from Y")
+    dw = _empty((T, k), torch.float32, dev, stream) if weights is not None else None
+    r = load().emu_rows_combine_backward(dt, T, k, cols, dO.data_ptr(), _pitch(dO, "rows_combine_backward: dO", dev),
+                                         Y.data_ptr(), yrows, _pitch(Y, where),
+                                         _ints(slots, T * k, dev, "rows_combine_backward: slots"),
+                                         _float_pairs(weights, shape, dev, "rows_combine_backward: weights"),
+                                         dY.data_ptr(), _pitch(dY, "rows_combine_backward: dY", dev),
+                                         dw.data_ptr() if dw is not None else None, _raw_stream(stream, dev))
+    if r:
+        _check(r, "emu_rows_combine_backward")
     return dY, dw

@@ -214,7 +214,8 @@ __device__ __forceinline__ void store_columns(const float (&v)[32], int cols, vo
 // contiguous (else with the contraction contiguous).  CMN is the gradient.
 template <int S, int BC, bool PAIR, bool LMN, bool CMN>
 __global__ void __launch_bounds__(64 + 32 * kEpiWarps, 1)
-grouped_kernel(const __grid_constant__ CUtensorMap tmL, const __grid_constant__ CUtensorMap tmC, const GroupedArgs a)
+grouped_kernel(const __grid_constant__ CUtensorMap tmL, const __grid_constant__ CUtensorMap tmC,
+               const __grid_constant__ CUtensorMap tmS, const GroupedArgs a)
 {
     using Cfg = GroupedCfg<S, BC, PAIR>;
     extern __shared__ uint8_t smem_raw[];
@@ -291,8 +292,9 @@ grouped_kernel(const __grid_constant__ CUtensorMap tmL, const __grid_constant__ 
         for (int t = first; t < total && ok; t += step) {
             const Tile x = tile_at<S, BC, PAIR, LMN, CMN>(t, a, starts, tpre, rank);
             const int nkb = (x.nk + kKB - 1) / kKB, crows = x.csz / Cfg::CTAS, cfirst = rank * crows;
-            const int cboxes = CMN ? (crows + 63) / 64 : crows / 16;
-            const uint32_t bytes = (uint32_t)(S * (Cfg::L_TILE + cboxes * (CMN ? 64 * kKB * 2 : 16 * kKB * 2)));
+            // 64-row (or 64-column) boxes; a short rest in boxes of 16 rows
+            const int rest = crows % 64, cbig = crows / 64 + (CMN ? rest > 0 : rest > 32), csmall = CMN || rest > 32 ? 0 : rest / 16;
+            const uint32_t bytes = (uint32_t)(S * (Cfg::L_TILE + (cbig * 64 + csmall * 16) * kKB * 2));
             const int crow0 = CMN ? 0 : (a.padded ? (int)padded_start(starts[x.g], x.g) : starts[x.g]) + x.c0 + cfirst;
             for (int kb = 0; kb < nkb; ++kb) {
                 if (!(ok = mbar_wait(empty0 + 8u * s, ph ^ 1u, flags))) break;
@@ -316,11 +318,13 @@ grouped_kernel(const __grid_constant__ CUtensorMap tmL, const __grid_constant__ 
                     }
                     const uint32_t dc = st + (uint32_t)(S * Cfg::L_TILE + r * Cfg::C_TILE);
                     if constexpr (CMN) {
-                        for (int b = 0; b < cboxes; ++b)
+                        for (int b = 0; b < cbig; ++b)
                             load(dc + (uint32_t)(b * 64 * kKB * 2), &tmC, x.c0 + cfirst + 64 * b, k, 0, r);
                     } else {
-                        for (int b = 0; b < cboxes; ++b)
-                            load(dc + (uint32_t)(b * 16 * kKB * 2), &tmC, k, crow0 + 16 * b, 0, r);
+                        for (int b = 0; b < cbig; ++b)
+                            load(dc + (uint32_t)(b * 64 * kKB * 2), &tmC, k, crow0 + 64 * b, 0, r);
+                        for (int b = 0; b < csmall; ++b)
+                            load(dc + (uint32_t)((cbig * 64 + b * 16) * kKB * 2), &tmS, k, crow0 + 64 * cbig + 16 * b, 0, r);
                     }
                 }
                 ++issued;
@@ -530,7 +534,8 @@ int sm_count()
 }
 
 template <int S, int BC, bool PAIR, bool LMN, bool CMN>
-cudaError_t run_grouped(const CUtensorMap &tl, const CUtensorMap &tc, const GroupedArgs &a, int64_t tiles, cudaStream_t st)
+cudaError_t run_grouped(const CUtensorMap &tl, const CUtensorMap &tc, const CUtensorMap &ts, const GroupedArgs &a,
+                        int64_t tiles, cudaStream_t st)
 {
     using Cfg = GroupedCfg<S, BC, PAIR>;
     auto kern = grouped_kernel<S, BC, PAIR, LMN, CMN>;
@@ -552,7 +557,7 @@ cudaError_t run_grouped(const CUtensorMap &tl, const CUtensorMap &tc, const Grou
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = PAIR ? 2 : 1;
-    e = cudaLaunchKernelEx(&cfg, kern, tl, tc, a);
+    e = cudaLaunchKernelEx(&cfg, kern, tl, tc, ts, a);
     if (e != cudaSuccess) return e;
     return cudaGetLastError();
 }
@@ -568,14 +573,16 @@ int64_t max_tiles(int64_t rows, int64_t G, int64_t L, int bc, int ctas)
 template <int S, bool LMN>
 cudaError_t product(const GroupedOperand &X, const GroupedOperand &W, const GroupedArgs &a, cudaStream_t st)
 {
-    CUtensorMap tl, tc;
+    CUtensorMap tl, tc, ts;
     const bool ok = LMN ? make_group_map(&tl, W.planes, a.L, a.K, a.G, S, W.ld, W.stride, W.plane, 64)
                         : make_group_map(&tl, W.planes, a.K, a.L, a.G, S, W.ld, W.stride, W.plane, kLRows);
-    if (!ok || !make_group_map(&tc, X.planes, a.K, X.rows, 1, S, X.ld, 0, X.plane, 16)) return cudaErrorInvalidValue;
+    if (!ok || !make_group_map(&tc, X.planes, a.K, X.rows, 1, S, X.ld, 0, X.plane, 64) ||
+        !make_group_map(&ts, X.planes, a.K, X.rows, 1, S, X.ld, 0, X.plane, 16))
+        return cudaErrorInvalidValue;
     const int64_t each = a.rows / a.G;            // rows of a group on average
     if (each >= 128)
-        return run_grouped<S, 256, true, LMN, false>(tl, tc, a, max_tiles(a.rows, a.G, a.L, 256, 2), st);
-    return run_grouped<S, 64, false, LMN, false>(tl, tc, a, max_tiles(a.rows, a.G, a.L, 64, 1), st);
+        return run_grouped<S, 256, true, LMN, false>(tl, tc, ts, a, max_tiles(a.rows, a.G, a.L, 256, 2), st);
+    return run_grouped<S, 64, false, LMN, false>(tl, tc, ts, a, max_tiles(a.rows, a.G, a.L, 64, 1), st);
 }
 
 template <int S>
@@ -585,7 +592,7 @@ cudaError_t gradient(const GroupedOperand &A, const GroupedOperand &B, const Gro
     if (!make_group_map(&tl, B.planes, a.L, B.rows, 1, S, B.ld, 0, B.plane, 64) ||
         !make_group_map(&tc, A.planes, a.C, A.rows, 1, S, A.ld, 0, A.plane, 64))
         return cudaErrorInvalidValue;
-    return run_grouped<S, 256, true, true, true>(tl, tc, a, (int64_t)a.G * ((a.L + 255) / 256) * ((a.C + 255) / 256), st);
+    return run_grouped<S, 256, true, true, true>(tl, tc, tc, a, (int64_t)a.G * ((a.L + 255) / 256) * ((a.C + 255) / 256), st);
 }
 
 }  // namespace

@@ -11,6 +11,8 @@ constexpr int64_t kMaxDim = (int64_t)1 << 31;      // kernels index with 32-bit 
 
 int64_t round_up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+// Whether p is aligned to its elements.
+bool fits(const void *p, int type) { return (reinterpret_cast<uintptr_t>(p) & (type == EMU_F32 ? 3u : 1u)) == 0; }
 emu_status cuda_status(cudaError_t e) { return e == cudaSuccess ? EMU_OK : EMU_ERR_CUDA; }
 int64_t plane_ld(int64_t cols) { return round_up(cols < 1 ? 1 : cols, 8); }
 int slices(int dtype) { return dtype == EMU_F32 ? 3 : 1; }
@@ -84,6 +86,7 @@ emu_status emu_grouped_split(int dtype, int64_t G, int64_t rows, int64_t cols, c
     if (s != EMU_OK) return s;
     if (G * rows > 0 && cols > 0) {
         if (!X) return EMU_ERR_INVALID_ARG;
+        if (!fits(X, dtype)) return EMU_ERR_MISALIGNED;
         s = check_planes(comps, ldcomp, cols, 0);
         if (s != EMU_OK) return s;
     }
@@ -106,6 +109,7 @@ emu_status emu_grouped_split_rows(int dtype, int64_t rows, int64_t cols, const v
     if (s != EMU_OK) return s;
     if (rows > 0 && cols > 0) {
         if (!ends || (xrows > 0 && !X)) return EMU_ERR_INVALID_ARG;
+        if (!fits(X, dtype) || !fits(src, EMU_F32) || !fits(ends, EMU_F32)) return EMU_ERR_MISALIGNED;
         s = check_planes(comps, ldcomp, cols, 0);
         if (s != EMU_OK) return s;
     }
@@ -131,6 +135,7 @@ emu_status emu_grouped_prodsum(int nslices, int opW, int64_t G, int64_t rows, in
     const int64_t wrows = opW == EMU_OP_T ? N : K, wcols = opW == EMU_OP_T ? K : N;
     if (rows > 0 && N > 0) {
         if (!ends || !Y) return EMU_ERR_INVALID_ARG;
+        if (!fits(ends, EMU_F32) || !fits(Y, ytype)) return EMU_ERR_MISALIGNED;
         if (K > 0) {
             // slices of the weights are planes of G dense matrices
             if (nslices == 3 && G > 1 && stridew != wrows * ldw) return EMU_ERR_INVALID_ARG;
@@ -173,6 +178,8 @@ emu_status emu_grouped_gemm_f32(int opW, int64_t G, int64_t rows, int64_t N, int
     const int64_t wrows = opW == EMU_OP_T ? N : K, wcols = opW == EMU_OP_T ? K : N;
     if (ldw < wcols || (G > 1 && stridew < 0)) return EMU_ERR_INVALID_ARG;
     if (rows > 0 && N > 0 && (!ends || !Y || (K > 0 && (!W || (xrows > 0 && !X))))) return EMU_ERR_INVALID_ARG;
+    if (!fits(X, EMU_F32) || !fits(W, EMU_F32) || !fits(Y, EMU_F32) || !fits(src, EMU_F32) || !fits(ends, EMU_F32))
+        return EMU_ERR_MISALIGNED;
     s = check_ws(ws, ws_bytes, emu_grouped_gemm_workspace_bytes(EMU_F32, G, rows, N, K));
     if (s != EMU_OK) return s;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
@@ -202,6 +209,7 @@ emu_status emu_grouped_prodsum_wgrad(int nslices, int64_t G, int64_t rows, int64
     if (s != EMU_OK) return s;
     if (M > 0 && N > 0) {
         if (!D) return EMU_ERR_INVALID_ARG;
+        if (!fits(D, dtype) || !fits(ends, EMU_F32)) return EMU_ERR_MISALIGNED;
         if (rows > 0) {
             if (!ends) return EMU_ERR_INVALID_ARG;
             s = check_planes(Acomps, lda, M, 0);
@@ -244,7 +252,7 @@ emu_status emu_w4_matvec(int dtype, int64_t G, int64_t rows, int64_t N, int64_t 
     const int esize = dtype == EMU_F32 ? 4 : 2;
     if (K == 0) return cuda_status(zero_rows(Y, rows, N, ldy, esize, st));
     if (!X || !q || !scales) return EMU_ERR_INVALID_ARG;
-    if (!aligned16(q)) return EMU_ERR_MISALIGNED;
+    if (!aligned16(q) || !fits(X, dtype) || !fits(Y, dtype) || !fits(scales, stype)) return EMU_ERR_MISALIGNED;
     if (rows > 65535 * 2) return EMU_ERR_UNSUPPORTED;           // items of two rows and more on the grid's y dimension
     return cuda_status(launch_w4_matvec(dtype == EMU_F32, G, rows, N, K, (int)group, X, ldx, q, scales,
                                         stype == EMU_F32, zeros, ends, Y, ldy, st));
@@ -264,6 +272,9 @@ emu_status emu_route(int dtype, int64_t T, int64_t E, int64_t k, int renorm, con
     if (!known(dtype) || T < 0 || E < 1 || k < 1 || k > E || ldl < E || !ends) return EMU_ERR_INVALID_ARG;
     if (E > kMaxGroups || k > 32 || T >= kMaxDim / k) return EMU_ERR_UNSUPPORTED;
     if (T > 0 && (!logits || !weights || !experts || !slots || !rows)) return EMU_ERR_INVALID_ARG;
+    if (!fits(logits, dtype) || !fits(weights, EMU_F32) || !fits(experts, EMU_F32) || !fits(slots, EMU_F32) ||
+        !fits(rows, EMU_F32) || !fits(ends, EMU_F32))
+        return EMU_ERR_MISALIGNED;
     emu_status s = check_ws(ws, ws_bytes, emu_route_workspace_bytes(T, E, k));
     if (s != EMU_OK) return s;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
@@ -283,6 +294,8 @@ emu_status emu_route_backward(int dtype, int64_t T, int64_t E, int64_t k, int re
     if (E > kMaxGroups || k > 32 || T >= kMaxDim / k) return EMU_ERR_UNSUPPORTED;
     if (T == 0) return EMU_OK;
     if (!logits || !experts || !dweights || !dlogits) return EMU_ERR_INVALID_ARG;
+    if (!fits(logits, dtype) || !fits(dlogits, dtype) || !fits(experts, EMU_F32) || !fits(dweights, EMU_F32))
+        return EMU_ERR_MISALIGNED;
     return cuda_status(launch_route_backward(T, E, (int)k, renorm != 0, logits, dtype == EMU_F32, ldl, experts,
                                              dweights, dlogits, lddl, reinterpret_cast<cudaStream_t>(stream)));
 }
@@ -294,6 +307,7 @@ emu_status emu_rows_combine(int dtype, int64_t T, int64_t k, int64_t cols, const
     if (k >= 65536 || T >= kMaxDim / k || cols >= kMaxDim - 8 || yrows >= kMaxDim) return EMU_ERR_UNSUPPORTED;
     if (T == 0 || cols == 0) return EMU_OK;
     if (!slots || !O || (yrows > 0 && !Y)) return EMU_ERR_INVALID_ARG;
+    if (!fits(Y, dtype) || !fits(O, dtype) || !fits(weights, EMU_F32) || !fits(slots, EMU_F32)) return EMU_ERR_MISALIGNED;
     return cuda_status(launch_combine(dtype == EMU_F32, T, (int)k, cols, Y, yrows, ldy, slots, weights, O, ldo,
                                       reinterpret_cast<cudaStream_t>(stream)));
 }
@@ -309,6 +323,9 @@ emu_status emu_rows_combine_backward(int dtype, int64_t T, int64_t k, int64_t co
     if (k >= 65536 || T >= kMaxDim / k || cols >= kMaxDim - 8 || yrows >= kMaxDim) return EMU_ERR_UNSUPPORTED;
     if (T == 0) return EMU_OK;
     if (!slots || (cols > 0 && (!dO || (yrows > 0 && (!dY || (dweights && !Y)))))) return EMU_ERR_INVALID_ARG;
+    if (!fits(dO, dtype) || !fits(Y, dtype) || !fits(dY, dtype) || !fits(weights, EMU_F32) || !fits(dweights, EMU_F32) ||
+        !fits(slots, EMU_F32))
+        return EMU_ERR_MISALIGNED;
     return cuda_status(launch_combine_backward(dtype == EMU_F32, T, (int)k, cols, dO, lddo, Y, yrows, ldy, slots,
                                                weights, dY, lddy, dweights, reinterpret_cast<cudaStream_t>(stream)));
 }

@@ -108,19 +108,52 @@ __global__ void __launch_bounds__(kRouteThreads) route_kernel(const RouteArgs a)
             odd |= !(x[i] < INFINITY);                    // NaN or plus infinity
             key[i] = e < a.E ? logit_key(x[i]) : 0u;
         }
+        // up to 8 logits a lane: its candidates by falling key (equal keys: rising
+        // index), the best of all lanes' firsts taken off k times; more: each lane
+        // looks for its best again every time
+        constexpr bool SORT = V <= 8;
+        int at[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) at[i] = i * 32 + lane;
+        if constexpr (SORT) {
+#pragma unroll
+            for (int i = 1; i < V; ++i)
+#pragma unroll
+                for (int q = V - 1; q >= i; --q)
+                    if (key[q] > key[q - 1]) {
+                        const uint32_t u = key[q];
+                        const int v = at[q];
+                        key[q] = key[q - 1]; at[q] = at[q - 1];
+                        key[q - 1] = u; at[q - 1] = v;
+                    }
+        }
         float mine = -INFINITY, top = -INFINITY;          // lane j: the j-th logit
         int chosen = 0;
         for (int j = 0; j < a.k; ++j) {
-            uint32_t best = 0;
-            int at = 0x7FFFFFFF;
+            uint32_t best = key[0];
+            int first = at[0];
+            if constexpr (!SORT) {
 #pragma unroll
-            for (int i = 0; i < V; ++i)
-                if (key[i] > best) { best = key[i]; at = i * 32 + lane; }
+                for (int i = 1; i < V; ++i)
+                    if (key[i] > best) { best = key[i]; first = i * 32 + lane; }
+            }
             const uint32_t most = __reduce_max_sync(0xFFFFFFFFu, best);
-            const int e = (int)__reduce_min_sync(0xFFFFFFFFu, best == most ? (uint32_t)at : 0x7FFFFFFFu);
+            const uint32_t hit = __ballot_sync(0xFFFFFFFFu, best == most);
+            int e;
+            if ((hit & (hit - 1)) == 0) e = __shfl_sync(0xFFFFFFFFu, first, __ffs(hit) - 1);
+            else e = (int)__reduce_min_sync(0xFFFFFFFFu, best == most ? (uint32_t)first : 0x7FFFFFFFu);
+            if constexpr (SORT) {
+                if (first == e) {
 #pragma unroll
-            for (int i = 0; i < V; ++i)
-                if (i * 32 + lane == e) key[i] = 0u;
+                    for (int i = 1; i < V; ++i) { key[i - 1] = key[i]; at[i - 1] = at[i]; }
+                    key[V - 1] = 0u;
+                    at[V - 1] = -1;
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+                    if (i * 32 + lane == e) key[i] = 0u;
+            }
             if (j == 0) top = key_logit(most);
             if (lane == j) { mine = key_logit(most); chosen = e; }
         }
@@ -239,61 +272,64 @@ struct RouteBackArgs {
 
 // One warp per token.  With p the probabilities that the weights came from
 // (over the chosen experts, or over all) and g the weights' gradients:
-// dl_e = p_e ([e chosen] g_e - sum over the chosen of p g).
+// dl_e = p_e ([e chosen] g_e - sum over the chosen of p g).  Lane j has the
+// j-th chosen expert and writes its entry over the row's other formula, which
+// the lanes have stored before.
 template <int V>
 __global__ void __launch_bounds__(256) route_backward_kernel(const RouteBackArgs a)
 {
     const int lane = (int)lane_id();
+    const int es = a.f32 ? 4 : 2;
     for (int64_t t = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); t < a.T; t += (int64_t)gridDim.x * 8) {
-        const char *row = static_cast<const char *>(a.logits) + t * a.ldl * (a.f32 ? 4 : 2);
-        float x[V], g[V];
-        uint32_t sel = 0;
-        float top = -INFINITY;
-        const int mine = lane < a.k ? __ldg(a.experts + t * a.k + lane) : -1;
-        const float gm = lane < a.k ? __ldg(a.dw + t * a.k + lane) : 0.0f;
+        const char *row = static_cast<const char *>(a.logits) + t * a.ldl * es;
+        char *out = static_cast<char *>(a.dl) + t * a.lddl * es;
+        int e = lane < a.k ? __ldg(a.experts + t * a.k + lane) : -1;
+        if (e >= a.E) e = -1;
+        const float g = e >= 0 ? __ldg(a.dw + t * a.k + lane) : 0.0f;
+        float x[V];
+        if (!a.renorm) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const int e = i * 32 + lane;
-            x[i] = e < a.E ? load_logit(row, e, a.f32 != 0) : -INFINITY;
-            if (!(x[i] == x[i])) x[i] = -INFINITY;
-            g[i] = 0.0f;
-        }
-        for (int j = 0; j < a.k; ++j) {
-            const int e = __shfl_sync(0xFFFFFFFFu, mine, j);
-            const float ge = __shfl_sync(0xFFFFFFFFu, gm, j);
-#pragma unroll
-            for (int i = 0; i < V; ++i)
-                if (i * 32 + lane == e) { g[i] = ge; sel |= 1u << i; }
-        }
-#pragma unroll
-        for (int i = 0; i < V; ++i)
-            if (!a.renorm || (sel >> i & 1u)) top = fmaxf(top, x[i]);
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
-        const bool some = top > -INFINITY;
-        float total = 0.0f;
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const bool in = some && i * 32 + lane < a.E && (!a.renorm || (sel >> i & 1u));
-            x[i] = in ? expf(x[i] - top) : 0.0f;
-            total += x[i];
-        }
-        total = warp_sum(total);
-        float inner = 0.0f;
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            x[i] = some ? x[i] / total : 0.0f;
-            if (sel >> i & 1u) inner += x[i] * g[i];
-        }
-        inner = warp_sum(inner);
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const int e = i * 32 + lane;
-            const float d = x[i] * ((sel >> i & 1u ? g[i] : 0.0f) - inner);
-            if (e < a.E) {
-                if (a.f32) static_cast<float *>(a.dl)[t * a.lddl + e] = d;
-                else static_cast<uint16_t *>(a.dl)[t * a.lddl + e] = f32_bf16(d);
+            for (int i = 0; i < V; ++i) {
+                const int c = i * 32 + lane;
+                x[i] = c < a.E ? load_logit(row, c, a.f32 != 0) : -INFINITY;
+                if (!(x[i] == x[i])) x[i] = -INFINITY;
             }
+        }
+        float mine = e >= 0 ? load_logit(row, e, a.f32 != 0) : -INFINITY;
+        if (!(mine == mine)) mine = -INFINITY;
+        uint32_t best = logit_key(mine);
+        if (!a.renorm) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) best = max(best, logit_key(x[i]));
+        }
+        const float top = key_logit(__reduce_max_sync(0xFFFFFFFFu, best));
+        const bool some = top > -INFINITY;
+        float p = some && e >= 0 ? expf(mine - top) : 0.0f, total = p;
+        if (!a.renorm) {
+            total = 0.0f;
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                x[i] = some && i * 32 + lane < a.E ? expf(x[i] - top) : 0.0f;
+                total += x[i];
+            }
+        }
+        const float inv_of = warp_sum(total);
+        p = some ? p / inv_of : 0.0f;
+        const float inner = warp_sum(p * g);
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const int c = i * 32 + lane;
+            const float d = a.renorm || !some ? 0.0f : -(x[i] / inv_of) * inner;
+            if (c < a.E) {
+                if (a.f32) reinterpret_cast<float *>(out)[c] = d;
+                else reinterpret_cast<uint16_t *>(out)[c] = f32_bf16(d);
+            }
+        }
+        __syncwarp();
+        if (e >= 0) {
+            const float d = p * (g - inner);
+            if (a.f32) reinterpret_cast<float *>(out)[e] = d;
+            else reinterpret_cast<uint16_t *>(out)[e] = f32_bf16(d);
         }
     }
 }
@@ -307,123 +343,140 @@ struct CombineArgs {
     void *O, *dY;
     float *dw;
     int64_t T;
-    int k, cols, vec;
+    int k, cols;
 };
 
-// A 16-byte piece of a row as floats: 4 FP32 or 8 BF16.
+// 16 bytes of a row (4 FP32 or 8 BF16) from column c on; columns past the last
+// read as zero and are not stored.  VEC: rows are 16-byte aligned and whole
+// pieces.
+template <bool F32, bool VEC>
+__device__ __forceinline__ uint4 load_piece(const char *row, int64_t c, int cols)
+{
+    if constexpr (VEC) {
+        return __ldg(reinterpret_cast<const uint4 *>(row + c * (F32 ? 4 : 2)));
+    } else if constexpr (F32) {
+        const uint32_t *p = reinterpret_cast<const uint32_t *>(row) + c;
+        return make_uint4(__ldg(p), c + 1 < cols ? __ldg(p + 1) : 0u, c + 2 < cols ? __ldg(p + 2) : 0u,
+                          c + 3 < cols ? __ldg(p + 3) : 0u);
+    } else {
+        const uint16_t *p = reinterpret_cast<const uint16_t *>(row) + c;
+        uint32_t h[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) h[i] = c + i < cols ? (uint32_t)__ldg(p + i) : 0u;
+        return make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
+    }
+}
+
 template <bool F32>
-struct Piece {
-    static constexpr int N = F32 ? 4 : 8;
-    float x[N];
-    __device__ __forceinline__ void load(const void *row, int64_t c, int cols, bool vec)
-    {
+__device__ __forceinline__ void to_floats(uint4 v, float (&x)[F32 ? 4 : 8])
+{
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
         if constexpr (F32) {
-            const float *p = static_cast<const float *>(row) + c;
-            if (vec) {
-                const float4 v = __ldg(reinterpret_cast<const float4 *>(p));
-                x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
-            } else {
-#pragma unroll
-                for (int i = 0; i < N; ++i) x[i] = c + i < cols ? __ldg(p + i) : 0.0f;
-            }
+            x[i] = __uint_as_float(w[i]);
         } else {
-            const uint16_t *p = static_cast<const uint16_t *>(row) + c;
-            if (vec) {
-                const uint4 v = __ldg(reinterpret_cast<const uint4 *>(p));
-                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    x[2 * i] = __uint_as_float(w[i] << 16);
-                    x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < N; ++i) x[i] = c + i < cols ? bf16_f32(__ldg(p + i)) : 0.0f;
-            }
+            x[2 * i] = __uint_as_float(w[i] << 16);
+            x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
         }
     }
-    __device__ __forceinline__ void store(void *row, int64_t c, int cols, bool vec) const
-    {
-        if constexpr (F32) {
-            float *p = static_cast<float *>(row) + c;
-            if (vec) {
-                *reinterpret_cast<float4 *>(p) = make_float4(x[0], x[1], x[2], x[3]);
-            } else {
+}
+
+template <bool F32, bool VEC>
+__device__ __forceinline__ void store_piece(char *row, int64_t c, int cols, const float (&x)[F32 ? 4 : 8])
+{
+    if constexpr (VEC) {
+        uint4 v;
+        if constexpr (F32) v = make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+        else v = make_uint4(bf16x2_rn(x[0], x[1]), bf16x2_rn(x[2], x[3]), bf16x2_rn(x[4], x[5]), bf16x2_rn(x[6], x[7]));
+        *reinterpret_cast<uint4 *>(row + c * (F32 ? 4 : 2)) = v;
+    } else {
 #pragma unroll
-                for (int i = 0; i < N; ++i)
-                    if (c + i < cols) p[i] = x[i];
+        for (int i = 0; i < (F32 ? 4 : 8); ++i)
+            if (c + i < cols) {
+                if constexpr (F32) reinterpret_cast<float *>(row)[c + i] = x[i];
+                else reinterpret_cast<uint16_t *>(row)[c + i] = f32_bf16(x[i]);
             }
-        } else {
-            uint16_t *p = static_cast<uint16_t *>(row) + c;
-            if (vec) {
-                *reinterpret_cast<uint4 *>(p) = make_uint4(bf16x2_rn(x[0], x[1]), bf16x2_rn(x[2], x[3]),
-                                                           bf16x2_rn(x[4], x[5]), bf16x2_rn(x[6], x[7]));
-            } else {
-#pragma unroll
-                for (int i = 0; i < N; ++i)
-                    if (c + i < cols) p[i] = f32_bf16(x[i]);
-            }
-        }
     }
-};
+}
+
+constexpr int kBatch = 4;             // rows or pieces that a thread loads before it uses the first
 
 // O[t] = sum_j w[t, j] Y[slots[t, j]], j ascending, in FP32; a thread has one
-// 16-byte piece of one token, its k loads independent.
-template <bool F32>
+// 16-byte piece of one token.
+template <bool F32, bool VEC>
 __global__ void __launch_bounds__(256) combine_kernel(const CombineArgs a)
 {
-    constexpr int N = Piece<F32>::N, ES = F32 ? 4 : 2;
+    constexpr int N = F32 ? 4 : 8, ES = F32 ? 4 : 2;
     const int pieces = (a.cols + N - 1) / N;
     const int64_t total = a.T * pieces;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-        const int64_t t = i / pieces, c = (i - t * pieces) * N;
-        const bool vec = a.vec && c + N <= a.cols;
-        Piece<F32> acc;
+        const int64_t t = total < 0x7FFFFFFF ? (int64_t)((uint32_t)i / (uint32_t)pieces) : i / pieces;
+        const int64_t c = (i - t * pieces) * N;
+        float acc[N] = {};
+        for (int j0 = 0; j0 < a.k; j0 += kBatch) {
+            uint4 v[kBatch];
+            float w[kBatch];
 #pragma unroll
-        for (int e = 0; e < N; ++e) acc.x[e] = 0.0f;
-#pragma unroll 4
-        for (int j = 0; j < a.k; ++j) {
-            const int64_t s = __ldg(a.slots + t * a.k + j);
-            if (s < 0 || s >= a.yrows) continue;
-            const float w = a.weights ? __ldg(a.weights + t * a.k + j) : 1.0f;
-            Piece<F32> y;
-            y.load(static_cast<const char *>(a.Y) + s * a.ldy * ES, c, a.cols, vec);
+            for (int j = 0; j < kBatch; ++j) {
+                const int64_t s = j0 + j < a.k ? __ldg(a.slots + t * a.k + j0 + j) : -1;
+                w[j] = j0 + j < a.k && a.weights ? __ldg(a.weights + t * a.k + j0 + j) : 1.0f;
+                v[j] = make_uint4(0u, 0u, 0u, 0u);
+                const bool ok = s >= 0 && s < a.yrows;
+                if (!ok) w[j] = 0.0f;
+                else v[j] = load_piece<F32, VEC>(static_cast<const char *>(a.Y) + s * a.ldy * ES, c, a.cols);
+            }
 #pragma unroll
-            for (int e = 0; e < N; ++e) acc.x[e] = fmaf(w, y.x[e], acc.x[e]);
+            for (int j = 0; j < kBatch; ++j) {
+                float x[N];
+                to_floats<F32>(v[j], x);
+#pragma unroll
+                for (int e = 0; e < N; ++e) acc[e] = fmaf(w[j], x[e], acc[e]);
+            }
         }
-        acc.store(static_cast<char *>(a.O) + t * a.ldo * ES, c, a.cols, vec);
+        store_piece<F32, VEC>(static_cast<char *>(a.O) + t * a.ldo * ES, c, a.cols, acc);
     }
 }
 
 // dY[slots[t, j]] = w[t, j] dO[t], dw[t, j] = Y[slots[t, j]] . dO[t]; a warp
 // per (t, j), so that a token's k warps share its dO row in the caches.
-template <bool F32>
+template <bool F32, bool VEC>
 __global__ void __launch_bounds__(256) combine_backward_kernel(const CombineArgs a)
 {
-    constexpr int N = Piece<F32>::N, ES = F32 ? 4 : 2;
+    constexpr int N = F32 ? 4 : 8, ES = F32 ? 4 : 2;
     const int lane = (int)lane_id();
     for (int64_t i = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); i < a.T * a.k; i += (int64_t)gridDim.x * 8) {
-        const int64_t t = i / a.k, s = __ldg(a.slots + i);
+        const int64_t t = (int64_t)((uint32_t)i / (uint32_t)a.k), s = __ldg(a.slots + i);
         const bool ok = s >= 0 && s < a.yrows;
         const float w = a.weights ? __ldg(a.weights + i) : 1.0f;
         const char *dO = static_cast<const char *>(a.dO) + t * a.ldo * ES;
-        const char *y = static_cast<const char *>(a.Y) + s * a.ldy * ES;
-        char *dY = static_cast<char *>(a.dY) + s * a.lddy * ES;
+        const char *y = static_cast<const char *>(a.Y) + (ok ? s : 0) * a.ldy * ES;
+        char *dY = static_cast<char *>(a.dY) + (ok ? s : 0) * a.lddy * ES;
+        const int cols = ok ? a.cols : 0;
         float dot = 0.0f;
-        if (ok) {
-#pragma unroll 4
-            for (int64_t c = (int64_t)lane * N; c < a.cols; c += 32 * N) {
-                const bool vec = a.vec && c + N <= a.cols;
-                Piece<F32> d, v;
-                d.load(dO, c, a.cols, vec);
-                if (a.dw) {
-                    v.load(y, c, a.cols, vec);
+        for (int64_t c0 = (int64_t)lane * N; c0 < cols; c0 += 32 * N * kBatch) {
+            uint4 d[kBatch], v[kBatch];
 #pragma unroll
-                    for (int e = 0; e < N; ++e) dot = fmaf(v.x[e], d.x[e], dot);
+            for (int b = 0; b < kBatch; ++b) {
+                const int64_t c = c0 + 32 * N * b;
+                d[b] = v[b] = make_uint4(0u, 0u, 0u, 0u);
+                if (c < cols) {
+                    d[b] = load_piece<F32, VEC>(dO, c, cols);
+                    if (a.dw) v[b] = load_piece<F32, VEC>(y, c, cols);
                 }
+            }
 #pragma unroll
-                for (int e = 0; e < N; ++e) d.x[e] *= w;
-                d.store(dY, c, a.cols, vec);
+            for (int b = 0; b < kBatch; ++b) {
+                const int64_t c = c0 + 32 * N * b;
+                float x[N], u[N];
+                to_floats<F32>(d[b], x);
+                to_floats<F32>(v[b], u);
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    dot = fmaf(u[e], x[e], dot);
+                    x[e] *= w;
+                }
+                if (c < cols) store_piece<F32, VEC>(dY, c, cols, x);
             }
         }
         if (a.dw) {
@@ -506,11 +559,13 @@ cudaError_t launch_combine(bool f32, int64_t T, int k, int64_t cols, const void 
     a.Y = Y; a.yrows = yrows; a.ldy = ldy; a.slots = slots; a.weights = weights; a.O = O; a.ldo = ldo;
     a.T = T; a.k = k; a.cols = (int)cols;
     const int es = f32 ? 4 : 2;
-    a.vec = can_vec(Y, ldy, es) && can_vec(O, ldo, es);
+    const bool vec = can_vec(Y, ldy, es) && can_vec(O, ldo, es) && cols * es % 16 == 0;
     const int64_t total = T * ((cols + (f32 ? 3 : 7)) / (f32 ? 4 : 8)), blocks = (total + 255) / 256;
     const unsigned grid = (unsigned)(blocks > 152 * 64 ? 152 * 64 : blocks);
-    if (f32) combine_kernel<true><<<grid, 256, 0, st>>>(a);
-    else combine_kernel<false><<<grid, 256, 0, st>>>(a);
+    if (f32 && vec) combine_kernel<true, true><<<grid, 256, 0, st>>>(a);
+    else if (f32) combine_kernel<true, false><<<grid, 256, 0, st>>>(a);
+    else if (vec) combine_kernel<false, true><<<grid, 256, 0, st>>>(a);
+    else combine_kernel<false, false><<<grid, 256, 0, st>>>(a);
     return cudaGetLastError();
 }
 
@@ -522,11 +577,13 @@ cudaError_t launch_combine_backward(bool f32, int64_t T, int k, int64_t cols, co
     a.Y = Y; a.dO = dO; a.yrows = yrows; a.ldy = ldy; a.ldo = lddo; a.lddy = lddy; a.slots = slots;
     a.weights = weights; a.dY = dY; a.dw = dw; a.T = T; a.k = k; a.cols = (int)cols;
     const int es = f32 ? 4 : 2;
-    a.vec = (!dw || can_vec(Y, ldy, es)) && can_vec(dO, lddo, es) && can_vec(dY, lddy, es);
+    const bool vec = (!dw || can_vec(Y, ldy, es)) && can_vec(dO, lddo, es) && can_vec(dY, lddy, es) && cols * es % 16 == 0;
     const int64_t blocks = (T * k + 7) / 8;
     const unsigned grid = (unsigned)(blocks > 152 * 64 ? 152 * 64 : blocks);
-    if (f32) combine_backward_kernel<true><<<grid, 256, 0, st>>>(a);
-    else combine_backward_kernel<false><<<grid, 256, 0, st>>>(a);
+    if (f32 && vec) combine_backward_kernel<true, true><<<grid, 256, 0, st>>>(a);
+    else if (f32) combine_backward_kernel<true, false><<<grid, 256, 0, st>>>(a);
+    else if (vec) combine_backward_kernel<false, true><<<grid, 256, 0, st>>>(a);
+    else combine_backward_kernel<false, false><<<grid, 256, 0, st>>>(a);
     return cudaGetLastError();
 }
 

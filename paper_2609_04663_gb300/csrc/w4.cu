@@ -32,8 +32,8 @@ namespace {
 
 constexpr int kWarps = 4, kRows = 32 * kWarps;        // features per CTA
 constexpr int kStageK = 256;                          // k of one ring stage: 128 bytes of codes per row
-constexpr int kStages = 4;
-constexpr int kPassK = 512;                           // k for which X and the scales are staged at once
+constexpr int kStages = 3;
+constexpr int kPassK = 1024;                          // k for which X and the scales are staged at once
 
 struct W4Args {
     const void *X;
@@ -61,12 +61,6 @@ __device__ __forceinline__ uint32_t lds32(uint32_t a)
 {
     uint32_t v;
     asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(a));
-    return v;
-}
-__device__ __forceinline__ uint2 lds64(uint32_t a)
-{
-    uint2 v;
-    asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
     return v;
 }
 __device__ __forceinline__ uint4 lds128(uint32_t a)
@@ -103,17 +97,26 @@ __device__ __forceinline__ uint4 pair_order(uint32_t w01, uint32_t w23, uint32_t
 
 __device__ __forceinline__ void sts128(uint32_t a, uint4 v) { st_shared_v4(a, v.x, v.y, v.z, v.w); }
 
+// Row pitch of the staged scales or zero points of one pass: an odd number of
+// 16-byte pieces, so that the 8 rows that a warp reads at once lie in
+// different banks.
+__host__ __device__ __forceinline__ int meta_pitch(int group, int size)
+{
+    const int pieces = ((kPassK / group + 2) * size + 15) / 16;
+    return (pieces | 1) * 16;
+}
+
 // Shared memory of a CTA, in bytes: the codes' rings, X's columns for one
 // pass (64 bytes per 32 k and column), the pass's scales and zero points.
-int w4_smem(int cols, int group)
+int w4_smem(int cols, int group, int ssize, bool zeros)
 {
-    return kWarps * kStages * 32 * 128 + (kPassK / 32) * cols * 64 + (kPassK / group + 2) * kRows * 8 +
-           (kMaxGroups + 4) * 4;
+    return kWarps * kStages * 32 * 128 + (kPassK / 32) * cols * 64 + kRows * meta_pitch(group, ssize) +
+           (zeros ? kRows * meta_pitch(group, 1) : 0);
 }
 
 // NT: tiles of 8 columns; F32X: FP32 rows, three columns each.
 template <int NT, bool F32X>
-__global__ void __launch_bounds__(32 * kWarps) w4_kernel(const W4Args a)
+__global__ void __launch_bounds__(32 * kWarps, 2) w4_kernel(const W4Args a)
 {
     constexpr int S = F32X ? 3 : 1;
     extern __shared__ __align__(128) uint8_t smem[];
@@ -175,8 +178,9 @@ __global__ void __launch_bounds__(32 * kWarps) w4_kernel(const W4Args a)
         m = min(a.tokens, a.rows - row0);
     }
     const int cols = m * S, gb = a.group / 32, ngroups = a.K / a.group;
+    const int ssize = a.s_f32 ? 4 : 2, sp = meta_pitch(a.group, ssize), zp = meta_pitch(a.group, 1);
     const uint32_t xs = codes + kWarps * kStages * 32 * 128;
-    const uint32_t sc = xs + (uint32_t)((kPassK / 32) * a.tokens * S * 64);
+    const uint32_t sc = xs + (uint32_t)((kPassK / 32) * a.tokens * S * 64), zs = sc + (uint32_t)(kRows * sp);
     const int k0 = (int)rank * a.slice, k1 = min(a.K, k0 + a.slice);
     const int nst = k1 > k0 ? (k1 - k0 + kStageK - 1) / kStageK : 0;
 
@@ -197,8 +201,38 @@ __global__ void __launch_bounds__(32 * kWarps) w4_kernel(const W4Args a)
         }
         cp_async_commit();
     };
-#pragma unroll
-    for (int st = 0; st < kStages - 1; ++st) fetch(st);
+    // n scales or zero points of each feature from group g0 on -> rows of pitch
+    // dpitch at dst, by 16-byte copies where the source rows allow it
+    auto meta = [&](uint32_t dst, int dpitch, const void *src, int size, int g0, int n) {
+        const uint8_t *from = static_cast<const uint8_t *>(src) + (((int64_t)g * a.N + n0) * ngroups + g0) * size;
+        const int64_t rowb = (int64_t)ngroups * size;
+        const int pieces = (n * size + 15) / 16;
+        // whole pieces only: a row's last piece may not run into what follows the array
+        const bool wide = ((reinterpret_cast<uintptr_t>(from) | (uintptr_t)rowb) & 15u) == 0;
+        for (int i = threadIdx.x; i < kRows * pieces; i += 32 * kWarps) {
+            const int r = i / pieces, o = (i % pieces) * 16;
+            const bool ok = n0 + r < a.N;
+            const uint32_t to = dst + (uint32_t)(r * dpitch + o);
+            if (wide) {
+                cp_async16(to, ok ? from + r * rowb + o : a.q, ok);
+            } else {
+                const int len = ok ? min(16, n * size - o) : 0;
+                for (int b = 0; b < 16; b += size) {
+                    const uint8_t *p = from + r * rowb + o + b;
+                    if (size == 4) {
+                        const uint32_t v = b < len ? __ldg(reinterpret_cast<const uint32_t *>(p)) : 0u;
+                        asm volatile("st.shared.b32 [%0], %1;" ::"r"(to + b), "r"(v) : "memory");
+                    } else if (size == 2) {
+                        const uint16_t v = b < len ? __ldg(reinterpret_cast<const uint16_t *>(p)) : (uint16_t)0;
+                        asm volatile("st.shared.b16 [%0], %1;" ::"r"(to + b), "h"(v) : "memory");
+                    } else {
+                        const uint16_t v = b < len ? __ldg(p) : (uint16_t)0;
+                        asm volatile("st.shared.b8 [%0], %1;" ::"r"(to + b), "h"(v) : "memory");
+                    }
+                }
+            }
+        }
+    };
 
     float total[2][NT][4], part[2][NT][4];
 #pragma unroll
@@ -209,9 +243,17 @@ __global__ void __launch_bounds__(32 * kWarps) w4_kernel(const W4Args a)
             for (int e = 0; e < 4; ++e) total[i][t][e] = part[i][t][e] = 0.0f;
 
     for (int st0 = 0; st0 < nst; st0 += kPassK / kStageK) {
-        // ---- X and the scales of this pass
+        // ---- X, scales and zero points of this pass
         const int p0 = k0 + st0 * kStageK, p1 = min(k1, p0 + kPassK), g0 = p0 / a.group;
+        const int ng = (p1 - 1) / a.group - g0 + 1;
         __syncthreads();                              // the pass before has been read
+        meta(sc, sp, a.scales, ssize, g0, ng);
+        if (a.zeros) meta(zs, zp, a.zeros, 1, g0, ng);
+        cp_async_commit();
+        if (st0 == 0) {
+#pragma unroll
+            for (int st = 0; st < kStages - 1; ++st) fetch(st);
+        }
         for (int i = threadIdx.x; i < m * (kPassK / 8); i += 32 * kWarps) {
             const int t = i / (kPassK / 8), o = i % (kPassK / 8), k = p0 + o * 8;
             const uint32_t dst = xs + (uint32_t)(((o >> 2) * cols + t * S) * 64 + (o & 3) * 16);
@@ -237,20 +279,10 @@ __global__ void __launch_bounds__(32 * kWarps) w4_kernel(const W4Args a)
                 sts128(dst, pair_order(w.x, w.y, w.z, w.w));
             }
         }
-        const int ng = (p1 - 1) / a.group - g0 + 1;
-        for (int i = threadIdx.x; i < ng * kRows; i += 32 * kWarps) {
-            const int r = i / ng, e = i % ng;         // a row's groups are neighbours in memory
-            float s = 0.0f;
-            uint32_t z = 8;
-            if (n0 + r < a.N) {
-                const int64_t at = ((int64_t)g * a.N + n0 + r) * ngroups + g0 + e;
-                s = a.s_f32 ? __ldg(static_cast<const float *>(a.scales) + at)
-                            : __uint_as_float((uint32_t)__ldg(static_cast<const uint16_t *>(a.scales) + at) << 16);
-                if (a.zeros) z = __ldg(a.zeros + at);
-            }
-            // 128 + z as a BF16 pair (z <= 15)
-            st_shared_v2(sc + (uint32_t)((e * kRows + r) * 8), __float_as_uint(s), 0x43004300u + (z & 15u) * 0x00010001u);
-        }
+        // the scales have arrived: with the first pass the codes' first stages
+        // may still be on their way, later ones were asked for before the scales
+        if (st0 == 0) cp_async_wait<kStages - 1>();
+        else cp_async_wait<0>();
         __syncthreads();
 
         for (int st = st0; st < min(nst, st0 + kPassK / kStageK); ++st) {
@@ -260,58 +292,67 @@ __global__ void __launch_bounds__(32 * kWarps) w4_kernel(const W4Args a)
             const uint32_t stage = ring + (uint32_t)((st % kStages) * 32 * 128) + (uint32_t)(lr * 128 + lc * 4);
             const int kb0 = (k0 + st * kStageK) / 32, kb1 = min(kb0 + 8, k1 / 32);
             int gi = kb0 / gb, left = gb - kb0 % gb;  // scale group, its 32-k blocks left
-            float s[4];
-            uint32_t z[4];
-            auto scales = [&] {
+            for (int kb = kb0; kb < kb1;) {
+                // the part of a scale group that this stage holds
+                const int end = min(kb1, kb + left);
+                float s[4];
+                uint32_t z[4];
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const uint2 v = lds64(sc + (uint32_t)(((gi - g0) * kRows + warp * 32 + r * 8 + lr) * 8));
-                    s[r] = __uint_as_float(v.x);
-                    z[r] = v.y;
+                    const int row = warp * 32 + r * 8 + lr;
+                    const uint32_t at = sc + (uint32_t)(row * sp + (gi - g0) * ssize);
+                    if (a.s_f32) {
+                        s[r] = __uint_as_float(lds32(at));
+                    } else {
+                        uint16_t h;
+                        asm volatile("ld.shared.b16 %0, [%1];" : "=h"(h) : "r"(at));
+                        s[r] = __uint_as_float((uint32_t)h << 16);
+                    }
+                    z[r] = 0x43084308u;               // 128 + z as a BF16 pair (z <= 15)
+                    if (a.zeros) {
+                        uint32_t v;
+                        asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(zs + (uint32_t)(row * zp + gi - g0)));
+                        z[r] = (v & 15u) * 0x00010001u + 0x43004300u;
+                    }
                 }
-            };
-            scales();
 #pragma unroll 2
-            for (int kb = kb0; kb < kb1; ++kb) {
-                const uint32_t at = stage + (uint32_t)((((kb - kb0) ^ lr) & 7) << 4);
-                uint32_t w[4];
+                for (; kb < end; ++kb) {
+                    const uint32_t at = stage + (uint32_t)((((kb - kb0) ^ lr) & 7) << 4);
+                    uint32_t w[4];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) w[r] = lds32(at + r * 1024);      // rows lr + 8 r
-                uint4 b[NT];
-                const uint32_t xa = xs + (uint32_t)((kb - p0 / 32) * cols * 64 + lc * 16);
-#pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    const int n = t * 8 + lr;
-                    b[t] = n < cols ? lds128(xa + (uint32_t)(n * 64)) : make_uint4(0, 0, 0, 0);
-                }
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const uint32_t u = w[2 * i], v = w[2 * i + 1], zu = z[2 * i], zv = z[2 * i + 1];
-                    const uint32_t u0 = decode(u, 0, zu), u1 = decode(u, 4, zu), u2 = decode(u, 8, zu), u3 = decode(u, 12, zu);
-                    const uint32_t v0 = decode(v, 0, zv), v1 = decode(v, 4, zv), v2 = decode(v, 8, zv), v3 = decode(v, 12, zv);
+                    for (int r = 0; r < 4; ++r) w[r] = lds32(at + r * 1024);      // rows lr + 8 r
+                    uint4 b[NT];
+                    const uint32_t xa = xs + (uint32_t)((kb - p0 / 32) * cols * 64 + lc * 16);
 #pragma unroll
                     for (int t = 0; t < NT; ++t) {
-                        mma16816(part[i][t], u0, v0, u1, v1, b[t].x, b[t].y);
-                        mma16816(part[i][t], u2, v2, u3, v3, b[t].z, b[t].w);
+                        const int n = t * 8 + lr;
+                        b[t] = n < cols ? lds128(xa + (uint32_t)(n * 64)) : make_uint4(0, 0, 0, 0);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const uint32_t u = w[2 * i], v = w[2 * i + 1], zu = z[2 * i], zv = z[2 * i + 1];
+                        const uint32_t u0 = decode(u, 0, zu), u1 = decode(u, 4, zu), u2 = decode(u, 8, zu),
+                                       u3 = decode(u, 12, zu);
+                        const uint32_t v0 = decode(v, 0, zv), v1 = decode(v, 4, zv), v2 = decode(v, 8, zv),
+                                       v3 = decode(v, 12, zv);
+#pragma unroll
+                        for (int t = 0; t < NT; ++t) {
+                            mma16816(part[i][t], u0, v0, u1, v1, b[t].x, b[t].y);
+                            mma16816(part[i][t], u2, v2, u3, v3, b[t].z, b[t].w);
+                        }
                     }
                 }
-                if (--left == 0 || kb + 1 == kb1) {
-                    // a scale group's sums (or what the stage holds of them)
 #pragma unroll
-                    for (int i = 0; i < 2; ++i)
+                for (int i = 0; i < 2; ++i)
 #pragma unroll
-                        for (int t = 0; t < NT; ++t)
+                    for (int t = 0; t < NT; ++t)
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                total[i][t][e] = fmaf(part[i][t][e], s[2 * i + (e >> 1)], total[i][t][e]);
-                                part[i][t][e] = 0.0f;
-                            }
-                    if (left == 0 && kb + 1 < kb1) {
-                        ++gi;
-                        left = gb;
-                        scales();
-                    }
-                }
+                        for (int e = 0; e < 4; ++e) {
+                            total[i][t][e] = fmaf(part[i][t][e], s[2 * i + (e >> 1)], total[i][t][e]);
+                            part[i][t][e] = 0.0f;
+                        }
+                ++gi;
+                left = gb;
             }
         }
     }
@@ -362,7 +403,7 @@ template <int NT, bool F32X>
 cudaError_t run_w4(const W4Args &a, int64_t blocks, int64_t items, int ks, cudaStream_t st)
 {
     auto kern = w4_kernel<NT, F32X>;
-    const int sm = w4_smem(a.tokens * (F32X ? 3 : 1), a.group);
+    const int sm = w4_smem(a.tokens * (F32X ? 3 : 1), a.group, a.s_f32 ? 4 : 2, a.zeros != nullptr);
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, sm);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
@@ -405,9 +446,10 @@ cudaError_t launch_w4_matvec(bool x_f32, int64_t G, int64_t rows, int64_t N, int
     const int64_t blocks = (N + kRows - 1) / kRows;
     const int64_t items = ends ? active + rows / a.tokens + 1 : (rows + a.tokens - 1) / a.tokens;
     if (items > 65535) return cudaErrorInvalidValue;
-    // slices of K: as many CTAs as twice the SMs want, each with one ring stage at least
+    // slices of K: at most one pass each where 8 of them allow it, and as many
+    // CTAs as twice the SMs want while each still has one ring stage
     int ks = 1;
-    while (ks < 8 && blocks * active * ks < 2 * 152 && ks * 2 * kStageK <= K) ks *= 2;
+    while (ks < 8 && (ks * kPassK < K || (blocks * active * ks < 2 * 152 && ks * 2 * kStageK <= K))) ks *= 2;
     a.slice = (int)((K + (int64_t)ks * kStageK - 1) / ((int64_t)ks * kStageK) * kStageK);
 #define EMU_W4(NT) (x_f32 ? run_w4<NT, true>(a, blocks, items, ks, st) : run_w4<NT, false>(a, blocks, items, ks, st))
     return nt == 1 ? EMU_W4(1) : nt == 2 ? EMU_W4(2) : EMU_W4(3);
