@@ -171,9 +171,15 @@ emu_status_string = _mk("emu_status_string")
 
 
 # ------------------------------------------------------------ tensor helpers
+_torch_module = None
+
+
 def _torch():
-    import torch
-    return torch
+    global _torch_module
+    if _torch_module is None:
+        import torch
+        _torch_module = torch
+    return _torch_module
 
 
 def _stream(stream):
@@ -393,7 +399,7 @@ def _bad(where, what):
 def _raw_stream(stream, device):
     """The CUDA stream handle to launch on (None: PyTorch's current one)."""
     if stream is None:
-        return _torch()._C._cuda_getCurrentRawStream(device.index)
+        return _torch_module._C._cuda_getCurrentRawStream(device.index)
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
@@ -406,25 +412,31 @@ def _torch_stream(stream, device):
 
 def _empty(shape, dtype, device, stream):
     """torch.empty whose memory belongs to the stream that the kernels use."""
-    torch = _torch()
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    with torch.cuda.stream(_torch_stream(stream, device)):
-        return torch.empty(shape, dtype=dtype, device=device)
+        return _torch_module.empty(shape, dtype=dtype, device=device)
+    with _torch().cuda.stream(_torch_stream(stream, device)):
+        return _torch_module.empty(shape, dtype=dtype, device=device)
+
+
+_codes = {}
 
 
 def _dtype(t, where):
-    torch = _torch()
-    if t.dtype is torch.float32:
-        return F32
-    if t.dtype is torch.bfloat16:
-        return BF16
-    _bad(where, f"float32 or bfloat16 is needed, got {t.dtype}")
+    """The EMU_* code of a tensor's type (every call asks for one first: loads the library)."""
+    code = _codes.get(t.dtype)
+    if code is None:
+        torch = _torch()
+        load()
+        _codes.update({torch.float32: F32, torch.bfloat16: BF16})
+        code = _codes.get(t.dtype)
+        if code is None:
+            _bad(where, f"float32 or bfloat16 is needed, got {t.dtype}")
+    return code
 
 
 def _ints(t, numel, device, where):
     """Address of an int32 tensor of `numel` entries (None: any number)."""
-    if t.dtype is not _torch().int32 or t.device != device or not t.is_contiguous():
+    if t.dtype is not _torch_module.int32 or t.device != device or not t.is_contiguous():
         _bad(where, f"a contiguous int32 tensor on {device} is needed")
     if numel is not None and t.numel() != numel:
         _bad(where, f"{numel} entries are needed, got {t.numel()}")
@@ -435,6 +447,8 @@ def _pitch(t, where, device=None):
     """Row pitch of a CUDA tensor whose rows are contiguous (on `device`, if given)."""
     if not t.is_cuda or (device is not None and t.device != device):
         _bad(where, f"a tensor on {device or 'a GPU'} is needed, got one on {t.device}")
+    if t.is_contiguous():
+        return t.shape[-1] or 1
     rows, cols = t.shape[-2:]
     st = t.stride()
     if cols > 1 and st[-1] != 1:
@@ -485,10 +499,10 @@ def grouped_split(X, ends=None, src=None, planes=None, ws=None, stream=None):
     elif planes.shape != (S, prows, ld) or planes.dtype is not torch.int16 or not planes.is_contiguous():
         _bad(where, f"planes have to be contiguous int16 {(S, prows, ld)}")
     if ends is None:
-        r = load().emu_grouped_split(dt, G, rows, cols, X.data_ptr(), ldx, X.stride(0) if G > 1 else 0,
+        r = _lib.emu_grouped_split(dt, G, rows, cols, X.data_ptr(), ldx, X.stride(0) if G > 1 else 0,
                                      planes.data_ptr(), ld, ws.data_ptr(), ws.numel(), _raw_stream(stream, dev))
     else:
-        r = load().emu_grouped_split_rows(dt, rows, cols, X.data_ptr(), X.shape[0], ldx,
+        r = _lib.emu_grouped_split_rows(dt, rows, cols, X.data_ptr(), X.shape[0], ldx,
                                           _ints(src, None, dev, "grouped_split: src") if src is not None else None,
                                           _ints(ends, G, dev, "grouped_split: ends"), G, planes.data_ptr(), ld,
                                           ws.data_ptr(), ws.numel(), _raw_stream(stream, dev))
@@ -548,7 +562,7 @@ def grouped_gemm(X, W, ends, opW: int = OP_N, src=None, Y=None, ws=None, stream=
         ps = _ints(src, None, dev, "grouped_gemm: src") if src is not None else None
         if ws is None:
             ws = _empty(emu_grouped_gemm_workspace_bytes(F32, G, rows, N, K), torch.uint8, dev, stream)
-        r = load().emu_grouped_gemm_f32(opW, G, rows, N, K, X.data_ptr(), X.shape[0], ldx, ps, W.data_ptr(), ldw,
+        r = _lib.emu_grouped_gemm_f32(opW, G, rows, N, K, X.data_ptr(), X.shape[0], ldx, ps, W.data_ptr(), ldw,
                                         W.stride(0) if G > 1 else 0, pe, Y.data_ptr(), ldy, ws.data_ptr(), ws.numel(),
                                         raw)
         if r:
@@ -562,7 +576,7 @@ def grouped_gemm(X, W, ends, opW: int = OP_N, src=None, Y=None, ws=None, stream=
     if not wp and (S == 3 or not _tma_ok(W, ldw)):
         W, wp = grouped_split(W, ws=ws, stream=stream), True
         ldw = W.ld
-    r = load().emu_grouped_prodsum(S, opW, G, rows, N, K, X.planes.data_ptr() if xp else X.data_ptr(), ldx, int(xp),
+    r = _lib.emu_grouped_prodsum(S, opW, G, rows, N, K, X.planes.data_ptr() if xp else X.data_ptr(), ldx, int(xp),
                                    W.planes.data_ptr() if wp else W.data_ptr(), ldw,
                                    W.shape[1] * ldw if wp or G <= 1 else W.stride(0), pe, Y.data_ptr(), yt, ldy,
                                    ws.data_ptr(), ws.numel(), raw)
@@ -592,7 +606,7 @@ def grouped_wgrad(A, B, ends, srcA=None, srcB=None, D=None, ws=None, stream=None
     dt, ldd = _dtype(D, "grouped_wgrad: D"), _pitch(D, "grouped_wgrad: D", dev)
     if D.shape != (G, M, N) or (S == 3 and dt != F32):
         _bad(where, "D has another shape or type")
-    r = load().emu_grouped_prodsum_wgrad(S, G, rows, M, N, A.planes.data_ptr(), A.ld, B.planes.data_ptr(), B.ld,
+    r = _lib.emu_grouped_prodsum_wgrad(S, G, rows, M, N, A.planes.data_ptr(), A.ld, B.planes.data_ptr(), B.ld,
                                          _ints(ends, G, dev, "grouped_wgrad: ends"), D.data_ptr(), dt, ldd,
                                          D.stride(0) if G > 1 else M * ldd, ws.data_ptr(), ws.numel(),
                                          _raw_stream(stream, dev))
@@ -628,7 +642,7 @@ def w4_matvec(X, Wq, scales, zeros=None, ends=None, Y=None, stream=None):
         Y = _empty((rows, N), X.dtype, dev, stream)
     elif Y.shape != (rows, N) or Y.dtype is not X.dtype:
         _bad(where, "Y has another shape or type")
-    r = load().emu_w4_matvec(dt, G, rows, N, K, group, X.data_ptr(), ldx, Wq.data_ptr(), scales.data_ptr(),
+    r = _lib.emu_w4_matvec(dt, G, rows, N, K, group, X.data_ptr(), ldx, Wq.data_ptr(), scales.data_ptr(),
                              _dtype(scales, "w4_matvec: scales"), zeros.data_ptr() if zeros is not None else None,
                              _ints(ends, G, dev, "w4_matvec: ends") if ends is not None else None, Y.data_ptr(),
                              _pitch(Y, "w4_matvec: Y", dev), _raw_stream(stream, dev))
@@ -653,7 +667,7 @@ def route(logits, k: int, renorm: bool = True, ws=None, stream=None):
         ws = _empty(emu_route_workspace_bytes(T, E, k), torch.uint8, dev, stream)
     out = Route(_empty((T, k), torch.float32, dev, stream), _empty((T, k), i32, dev, stream),
                 _empty((T, k), i32, dev, stream), _empty(T * k, i32, dev, stream), _empty(E, i32, dev, stream))
-    r = load().emu_route(dt, T, E, k, int(renorm), logits.data_ptr(), ldl, out[0].data_ptr(), out[1].data_ptr(),
+    r = _lib.emu_route(dt, T, E, k, int(renorm), logits.data_ptr(), ldl, out[0].data_ptr(), out[1].data_ptr(),
                          out[2].data_ptr(), out[3].data_ptr(), out[4].data_ptr(), ws.data_ptr(), ws.numel(),
                          _raw_stream(stream, dev))
     if r:
@@ -678,7 +692,7 @@ def route_backward(logits, experts, dweights, renorm: bool = True, dlogits=None,
         dlogits = _empty((T, E), logits.dtype, dev, stream)
     elif dlogits.shape != logits.shape or dlogits.dtype is not logits.dtype:
         _bad(where, "dlogits differ from logits")
-    r = load().emu_route_backward(dt, T, E, k, int(renorm), logits.data_ptr(), _pitch(logits, where),
+    r = _lib.emu_route_backward(dt, T, E, k, int(renorm), logits.data_ptr(), _pitch(logits, where),
                                   _ints(experts, T * k, dev, "route_backward: experts"),
                                   _float_pairs(dweights, experts.shape, dev, "route_backward: dweights"),
                                   dlogits.data_ptr(), _pitch(dlogits, where, dev), _raw_stream(stream, dev))
@@ -696,7 +710,7 @@ def rows_combine(Y, slots, weights=None, O=None, stream=None):
         O = _empty((T, cols), Y.dtype, dev, stream)
     elif O.shape != (T, cols) or O.dtype is not Y.dtype:
         _bad(where, "O has another shape or type")
-    r = load().emu_rows_combine(dt, T, k, cols, Y.data_ptr(), yrows, ldy, _ints(slots, T * k, dev, "rows_combine: slots"),
+    r = _lib.emu_rows_combine(dt, T, k, cols, Y.data_ptr(), yrows, ldy, _ints(slots, T * k, dev, "rows_combine: slots"),
                                 _float_pairs(weights, shape, dev, "rows_combine: weights"), O.data_ptr(),
                                 _pitch(O, "rows_combine: O", dev), _raw_stream(stream, dev))
     if r:
@@ -721,7 +735,7 @@ def rows_combine_backward(dO, Y, slots, weights=None, dY=None, stream=None):
     elif dY.shape != Y.shape or dY.dtype is not Y.dtype:
         _bad(where, "dY differs from Y")
     dw = _empty((T, k), torch.float32, dev, stream) if weights is not None else None
-    r = load().emu_rows_combine_backward(dt, T, k, cols, dO.data_ptr(), _pitch(dO, "rows_combine_backward: dO", dev),
+    r = _lib.emu_rows_combine_backward(dt, T, k, cols, dO.data_ptr(), _pitch(dO, "rows_combine_backward: dO", dev),
                                          Y.data_ptr(), yrows, _pitch(Y, where),
                                          _ints(slots, T * k, dev, "rows_combine_backward: slots"),
                                          _float_pairs(weights, shape, dev, "rows_combine_backward: weights"),

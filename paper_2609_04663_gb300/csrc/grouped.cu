@@ -48,8 +48,6 @@ constexpr int kLRows = 128;           // MMA rows (output features) per CTA
 constexpr int kKB = 64;               // K-block: one 128-byte swizzle row of BF16
 constexpr int kSmemMax = 232448;      // shared memory per CTA
 
-// The products of Eq. (fp32six) below the leading one.
-__constant__ int8_t kGroupChain[5][2] = {{1, 1}, {1, 0}, {2, 0}, {0, 2}, {0, 1}};
 constexpr int kChunkBlocks = kKChunk / kKB;   // K-blocks of one chunk of the leading product
 constexpr int kEpiWarps = 8;
 
@@ -63,6 +61,7 @@ struct GroupedArgs {
     void *out;
     int64_t ldo, strideo;  // row pitch; gradient: distance between the groups' results
     int out_f32;
+    int lwide, cwide;      // the MN-major operand's tensor map loads two blocks of 64 at once
     uint32_t *flags;
 };
 
@@ -87,21 +86,38 @@ struct GroupedCfg {
     static_assert(BC <= 256 && CROWS % 64 == 0 || BC < 128, "column tile");
 };
 
+// Tile loads, counted on this CTA's barrier or (PAIR) on one of either CTA.
+// 4-D: K-major operands (K, MN, group, slice).  5-D: MN-major operands with
+// the MN dimension in blocks of 64 (MN % 64, K, MN / 64, group, slice).
+template <bool PAIR>
 __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap *map, uint32_t bar, int32_t c0, int32_t c1,
                                             int32_t c2, int32_t c3)
 {
-    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
-                 " [%0], [%1, {%3, %4, %5, %6}], [%2];"
-                 ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
-                 : "memory");
+    if constexpr (PAIR)
+        asm volatile("cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+                     " [%0], [%1, {%3, %4, %5, %6}], [%2];"
+                     ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
+                     : "memory");
+    else
+        asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+                     " [%0], [%1, {%3, %4, %5, %6}], [%2];"
+                     ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
+                     : "memory");
 }
-__device__ __forceinline__ void tma_load_4d_pair(uint32_t dst, const CUtensorMap *map, uint32_t bar, int32_t c0,
-                                                 int32_t c1, int32_t c2, int32_t c3)
+template <bool PAIR>
+__device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap *map, uint32_t bar, int32_t c0, int32_t c1,
+                                            int32_t c2, int32_t c3, int32_t c4)
 {
-    asm volatile("cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
-                 " [%0], [%1, {%3, %4, %5, %6}], [%2];"
-                 ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
-                 : "memory");
+    if constexpr (PAIR)
+        asm volatile("cp.async.bulk.tensor.5d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+                     " [%0], [%1, {%3, %4, %5, %6, %7}], [%2];"
+                     ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4)
+                     : "memory");
+    else
+        asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+                     " [%0], [%1, {%3, %4, %5, %6, %7}], [%2];"
+                     ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4)
+                     : "memory");
 }
 
 // 16 FP32 accumulator columns of the warp's lanes.
@@ -116,19 +132,15 @@ __device__ __forceinline__ void tmem_load16(uint32_t taddr, uint32_t (&r)[16])
         : "memory");
 }
 
-// Shared-memory descriptor of a 128-byte-swizzled tile.  K-major: rows of 64
-// K elements, 8-row groups 1024 bytes apart; the next 16 K elements start 32
-// bytes on.  MN-major: boxes of 64 MN elements (one 128-byte row) by kKB rows
-// of K, the boxes `lbo` bytes apart, 8-row groups of K 1024 bytes apart; the
-// next 16 K rows start 2048 bytes on.
-__device__ __forceinline__ uint64_t group_desc(uint32_t saddr, uint32_t lbo)
+// Shared-memory descriptor of a 128-byte-swizzled tile at shared address 0:
+// the address is added in units of 16 bytes.  K-major: rows of 64 K elements,
+// 8-row groups 1024 bytes apart; the next 16 K elements start 32 bytes on.
+// MN-major: blocks of 64 MN elements (one 128-byte row) by kKB rows of K, the
+// blocks `lbo` bytes apart, 8-row groups of K 1024 bytes apart; the next 16 K
+// rows start 2048 bytes on.
+__host__ __device__ constexpr uint64_t group_desc(uint32_t lbo)
 {
-    uint64_t d = (uint64_t)((saddr & 0x3FFFFu) >> 4);
-    d |= (uint64_t)(lbo >> 4) << 16;
-    d |= (uint64_t)(1024u >> 4) << 32;
-    d |= (uint64_t)1u << 46;
-    d |= (uint64_t)2u << 61;
-    return d;
+    return (uint64_t)(lbo >> 4) << 16 | (uint64_t)(1024u >> 4) << 32 | (uint64_t)1u << 46 | (uint64_t)2u << 61;
 }
 
 // One output tile: features l0 .. (this CTA's 128), columns c0 .. c0 + cols
@@ -177,34 +189,47 @@ __device__ __forceinline__ Tile tile_at(int t, const GroupedArgs &a, const int *
 // 32 accumulator columns of this warp's lanes -> rows 0 .. cols - 1 of out:
 // column j is output row j, lane i feature l + i.  BF16: two columns at a
 // time, neighbouring lanes exchange values so that each stores two features
-// of one row.
+// of one row.  The usual case (32 whole columns, 32 features, pairs that can be
+// stored as words) has no test per element: these instructions, not the
+// stores' bandwidth, are what the epilogue takes.
 __device__ __forceinline__ void store_columns(const float (&v)[32], int cols, void *out, int64_t ldo, int l, int L,
                                               bool out_f32, bool pairs_ok)
 {
     const int lane = (int)lane_id();
+    const bool whole = cols >= 32 && l + 32 <= L;
     if (out_f32) {
         float *o = static_cast<float *>(out) + l + lane;
+        if (whole) {
 #pragma unroll
-        for (int j = 0; j < 32; ++j)
-            if (l + lane < L && j < cols) o[(int64_t)j * ldo] = v[j];
+            for (int j = 0; j < 32; ++j, o += ldo) *o = v[j];
+        } else {
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+                if (l + lane < L && j < cols) o[(int64_t)j * ldo] = v[j];
+        }
     } else {
         const bool odd = lane & 1;
         const int i = lane & ~1;
         uint16_t *o = static_cast<uint16_t *>(out) + (odd ? ldo : 0) + l + i;
+        uint32_t w[16];                               // features i (low half) and i + 1 of row 2 j + odd
 #pragma unroll
-        for (int j = 0; j < 32; j += 2) {
-            const float keep = odd ? v[j + 1] : v[j];
-            const float got = __shfl_xor_sync(0xFFFFFFFFu, odd ? v[j] : v[j + 1], 1);
-            uint32_t w;                               // features i (low half) and i + 1 of row j + odd
-            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(odd ? keep : got), "f"(odd ? got : keep));
-            if (j + (odd ? 1 : 0) < cols) {
-                uint16_t *p = o + (int64_t)j * ldo;
-                if (pairs_ok && l + i + 1 < L) {
-                    *reinterpret_cast<uint32_t *>(p) = w;
-                } else {
-                    if (l + i < L) p[0] = (uint16_t)w;
-                    if (l + i + 1 < L) p[1] = (uint16_t)(w >> 16);
-                }
+        for (int j = 0; j < 16; ++j) {
+            const float keep = odd ? v[2 * j + 1] : v[2 * j];
+            const float got = __shfl_xor_sync(0xFFFFFFFFu, odd ? v[2 * j] : v[2 * j + 1], 1);
+            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[j]) : "f"(odd ? keep : got), "f"(odd ? got : keep));
+        }
+        if (whole && pairs_ok) {
+            char *p = reinterpret_cast<char *>(o);
+            const int64_t two = 4 * ldo;
+#pragma unroll
+            for (int j = 0; j < 16; ++j, p += two) *reinterpret_cast<uint32_t *>(p) = w[j];
+        } else {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                if (2 * j + (odd ? 1 : 0) >= cols) continue;
+                uint16_t *p = o + (int64_t)(2 * j) * ldo;
+                if (l + i < L) p[0] = (uint16_t)w[j];
+                if (l + i + 1 < L) p[1] = (uint16_t)(w[j] >> 16);
             }
         }
     }
@@ -294,37 +319,46 @@ grouped_kernel(const __grid_constant__ CUtensorMap tmL, const __grid_constant__ 
             const int nkb = (x.nk + kKB - 1) / kKB, crows = x.csz / Cfg::CTAS, cfirst = rank * crows;
             // 64-row (or 64-column) boxes; a short rest in boxes of 16 rows
             const int rest = crows % 64, cbig = crows / 64 + (CMN ? rest > 0 : rest > 32), csmall = CMN || rest > 32 ? 0 : rest / 16;
-            const uint32_t bytes = (uint32_t)(S * (Cfg::L_TILE + (cbig * 64 + csmall * 16) * kKB * 2));
-            const int crow0 = CMN ? 0 : (a.padded ? (int)padded_start(starts[x.g], x.g) : starts[x.g]) + x.c0 + cfirst;
-            for (int kb = 0; kb < nkb; ++kb) {
+            // two blocks of 64 columns in one copy, also where the second is not needed
+            const bool ctwo = CMN && a.cwide != 0;
+            const uint32_t bytes = (uint32_t)(S * (Cfg::L_TILE + ((ctwo ? 2 : cbig) * 64 + csmall * 16) * kKB * 2)) * Cfg::CTAS;
+            const int crow0 = CMN ? x.c0 + cfirst
+                                  : (a.padded ? (int)padded_start(starts[x.g], x.g) : starts[x.g]) + x.c0 + cfirst;
+            int k = x.k0;
+            for (int kb = 0; kb < nkb; ++kb, k += kKB) {
                 if (!(ok = mbar_wait(empty0 + 8u * s, ph ^ 1u, flags))) break;
                 const uint32_t st = base + (uint32_t)(s * Cfg::STAGE), fb = full0 + 8u * s;
                 const uint32_t bar = PAIR ? peer_addr(fb, 0) : fb;
-                if (rank == 0) mbar_arrive_expect_tx(fb, bytes * Cfg::CTAS);
-                const int k = x.k0 + kb * kKB;
-                auto load = [&](uint32_t dst, const CUtensorMap *m, int c0, int c1, int c2, int c3) {
-                    if constexpr (PAIR) tma_load_4d_pair(dst, m, bar, c0, c1, c2, c3);
-                    else tma_load_4d(dst, m, bar, c0, c1, c2, c3);
-                };
+                if (rank == 0) mbar_arrive_expect_tx(fb, bytes);
 #pragma unroll
                 for (int r = 0; r < S; ++r) {
                     const uint32_t dl = st + (uint32_t)(r * Cfg::L_TILE);
                     if constexpr (LMN) {
-                        // boxes of 64 features x 64 contraction rows (a weight matrix's rows, or token rows)
-                        load(dl, &tmL, x.l0, k, CMN ? 0 : x.g, r);
-                        load(dl + Cfg::L_TILE / 2, &tmL, x.l0 + 64, k, CMN ? 0 : x.g, r);
+                        // 128 features x 64 contraction rows (a weight matrix's rows, or token rows)
+                        const int g = CMN ? 0 : x.g;
+                        if (a.lwide) {
+                            tma_load_5d<PAIR>(dl, &tmL, bar, 0, k, x.l0 >> 6, g, r);
+                        } else {
+                            tma_load_5d<PAIR>(dl, &tmL, bar, x.l0, k, 0, g, r);
+                            tma_load_5d<PAIR>(dl + Cfg::L_TILE / 2, &tmL, bar, x.l0 + 64, k, 0, g, r);
+                        }
                     } else {
-                        load(dl, &tmL, k, x.l0, x.g, r);
+                        tma_load_4d<PAIR>(dl, &tmL, bar, k, x.l0, x.g, r);
                     }
                     const uint32_t dc = st + (uint32_t)(S * Cfg::L_TILE + r * Cfg::C_TILE);
                     if constexpr (CMN) {
-                        for (int b = 0; b < cbig; ++b)
-                            load(dc + (uint32_t)(b * 64 * kKB * 2), &tmC, x.c0 + cfirst + 64 * b, k, 0, r);
+                        if (ctwo) {
+                            tma_load_5d<PAIR>(dc, &tmC, bar, 0, k, crow0 >> 6, 0, r);
+                        } else {
+                            for (int b = 0; b < cbig; ++b)
+                                tma_load_5d<PAIR>(dc + (uint32_t)(b * 64 * kKB * 2), &tmC, bar, crow0 + 64 * b, k, 0, 0, r);
+                        }
                     } else {
                         for (int b = 0; b < cbig; ++b)
-                            load(dc + (uint32_t)(b * 64 * kKB * 2), &tmC, k, crow0 + 64 * b, 0, r);
+                            tma_load_4d<PAIR>(dc + (uint32_t)(b * 64 * kKB * 2), &tmC, bar, k, crow0 + 64 * b, 0, r);
                         for (int b = 0; b < csmall; ++b)
-                            load(dc + (uint32_t)((cbig * 64 + b * 16) * kKB * 2), &tmS, k, crow0 + 64 * cbig + 16 * b, 0, r);
+                            tma_load_4d<PAIR>(dc + (uint32_t)((cbig * 64 + b * 16) * kKB * 2), &tmS, bar, k,
+                                              crow0 + 64 * cbig + 16 * b, 0, r);
                     }
                 }
                 ++issued;
@@ -346,7 +380,8 @@ grouped_kernel(const __grid_constant__ CUtensorMap tmL, const __grid_constant__ 
         int s = 0, it = 0;
         uint32_t ph = 0, cph = 0;                     // cph: chunks issued (FP32)
         bool ok = true;
-        constexpr uint32_t kstepL = LMN ? 2048u : 32u, kstepC = CMN ? 2048u : 32u, lbo = 64u * kKB * 2u;
+        constexpr int kstepL = LMN ? 2048 : 32, kstepC = CMN ? 2048 : 32;
+        constexpr uint64_t descL = group_desc(LMN ? 64u * kKB * 2u : 16u), descC = group_desc(CMN ? 64u * kKB * 2u : 16u);
         auto commit = [&](uint32_t bar) {
             if constexpr (PAIR) mma_commit_pair(bar);
             else mma_commit(bar);
@@ -365,31 +400,39 @@ grouped_kernel(const __grid_constant__ CUtensorMap tmL, const __grid_constant__ 
             for (int kb = 0; kb < nkb; ++kb) {
                 if (!(ok = mbar_wait(full0 + 8u * s, ph, flags))) break;
                 tc_fence_after();
-                const uint32_t st = base + (uint32_t)(s * Cfg::STAGE);
+                const uint32_t st = (base + (uint32_t)(s * Cfg::STAGE)) >> 4;
                 // 16-wide steps that hold contraction elements (the rest of the stage may hold anything)
-                const int steps = min(kKB / 16, (x.nk - kb * kKB + 15) / 16);
+                const int left = x.nk - kb * kKB;
                 auto mma = [&](uint32_t acc, int il, int ic, int kk, bool add) {
-                    const uint64_t ld = group_desc(st + (uint32_t)(il * Cfg::L_TILE) + kk * kstepL, LMN ? lbo : 16u);
-                    const uint64_t cd = group_desc(st + (uint32_t)(S * Cfg::L_TILE + ic * Cfg::C_TILE) + kk * kstepC,
-                                                   CMN ? lbo : 16u);
+                    const uint64_t ld = descL + (st + (uint32_t)((il * Cfg::L_TILE + kk * kstepL) >> 4));
+                    const uint64_t cd = descC + (st + (uint32_t)((S * Cfg::L_TILE + ic * Cfg::C_TILE + kk * kstepC) >> 4));
                     if constexpr (PAIR) mma_bf16_pair(acc, ld, cd, idesc, add);
                     else mma_bf16(acc, ld, cd, idesc, add);
                 };
                 if constexpr (S == 3) {
                     const int kc = kb % kChunkBlocks;
-                    for (int kk = 0; kk < steps; ++kk)
 #pragma unroll
-                        for (int q = 0; q < 5; ++q)
-                            mma(d2, kGroupChain[q][0], kGroupChain[q][1], kk, (kb | kk | q) != 0);
+                    for (int kk = 0; kk < kKB / 16; ++kk) {
+                        if (16 * kk >= left) break;
+                        mma(d2, 1, 1, kk, (kb | kk) != 0);
+                        mma(d2, 1, 0, kk, true);
+                        mma(d2, 2, 0, kk, true);
+                        mma(d2, 0, 2, kk, true);
+                        mma(d2, 0, 1, kk, true);
+                    }
                     if (kc == 0) {                    // the last chunk's leading sum has been read
                         if (!(ok = mbar_wait(tempty0, (cph & 1u) ^ 1u, flags))) break;
                         tc_fence_after();
                     }
-                    for (int kk = 0; kk < steps; ++kk) mma(d, 0, 0, kk, (kc | kk) != 0);
+#pragma unroll
+                    for (int kk = 0; kk < kKB / 16; ++kk)
+                        if (16 * kk < left) mma(d, 0, 0, kk, (kc | kk) != 0);
                     commit(empty0 + 8u * s);
                     if (kc == kChunkBlocks - 1 || kb == nkb - 1) { commit(tfull0); ++cph; }
                 } else {
-                    for (int kk = 0; kk < steps; ++kk) mma(d, 0, 0, kk, (kb | kk) != 0);
+#pragma unroll
+                    for (int kk = 0; kk < kKB / 16; ++kk)
+                        if (16 * kk < left) mma(d, 0, 0, kk, (kb | kk) != 0);
                     commit(empty0 + 8u * s);
                 }
                 if (++s == Cfg::STAGES) { s = 0; ph ^= 1u; }
@@ -507,19 +550,35 @@ grouped_kernel(const __grid_constant__ CUtensorMap tmL, const __grid_constant__ 
     }
 }
 
-// Tensor map over a plane set: dims (inner, rows, batch, S), box (64, box_rows).
+// Tensor maps over a plane set [S][batch][rows][ld].  K-major: dims (inner,
+// rows, batch, S), box (64, box_rows).  MN-major: dims (64, rows, inner / 64,
+// batch, S) and two blocks per box where inner is a multiple of `tile`, so that
+// tiles start on whole blocks (*wide), else (inner, rows, 1, batch, S) and one.
 bool make_group_map(CUtensorMap *map, const uint16_t *p, int64_t inner, int64_t rows, int64_t batch, int S, int64_t ld,
-                    int64_t stride, int64_t plane, int box_rows)
+                    int64_t stride, int64_t plane, int box_rows, int *wide = nullptr, int tile = 64)
 {
     EncodeTiledFn enc = encode_fn();
     if (!enc) return false;
     if (batch <= 1) stride = rows * ld;
     if (S <= 1) plane = batch * stride;
-    cuuint64_t dims[4] = {(cuuint64_t)inner, (cuuint64_t)rows, (cuuint64_t)batch, (cuuint64_t)S};
-    cuuint64_t strides[3] = {(cuuint64_t)ld * 2, (cuuint64_t)stride * 2, (cuuint64_t)plane * 2};
-    cuuint32_t box[4] = {64, (cuuint32_t)box_rows, 1, 1};
-    cuuint32_t estr[4] = {1, 1, 1, 1};
-    return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<uint16_t *>(p), dims, strides, box, estr,
+    const bool mn = wide != nullptr, two = mn && inner % tile == 0;
+    if (mn) *wide = two ? 1 : 0;
+    cuuint64_t dims[5] = {(cuuint64_t)(two ? 64 : inner), (cuuint64_t)rows}, strides[4] = {(cuuint64_t)ld * 2};
+    cuuint32_t box[5] = {64, (cuuint32_t)box_rows, 1, 1, 1}, estr[5] = {1, 1, 1, 1, 1};
+    int n = 2;
+    if (mn) {
+        dims[n] = (cuuint64_t)(two ? inner / 64 : 1);
+        box[n] = two ? 2 : 1;
+        strides[n - 1] = 128;
+        ++n;
+    }
+    dims[n] = (cuuint64_t)batch;
+    strides[n - 1] = (cuuint64_t)stride * 2;
+    ++n;
+    dims[n] = (cuuint64_t)S;
+    strides[n - 1] = (cuuint64_t)plane * 2;
+    ++n;
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)n, const_cast<uint16_t *>(p), dims, strides, box, estr,
                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -571,10 +630,10 @@ int64_t max_tiles(int64_t rows, int64_t G, int64_t L, int bc, int ctas)
 }
 
 template <int S, bool LMN>
-cudaError_t product(const GroupedOperand &X, const GroupedOperand &W, const GroupedArgs &a, cudaStream_t st)
+cudaError_t product(const GroupedOperand &X, const GroupedOperand &W, GroupedArgs a, cudaStream_t st)
 {
     CUtensorMap tl, tc, ts;
-    const bool ok = LMN ? make_group_map(&tl, W.planes, a.L, a.K, a.G, S, W.ld, W.stride, W.plane, 64)
+    const bool ok = LMN ? make_group_map(&tl, W.planes, a.L, a.K, a.G, S, W.ld, W.stride, W.plane, kKB, &a.lwide)
                         : make_group_map(&tl, W.planes, a.K, a.L, a.G, S, W.ld, W.stride, W.plane, kLRows);
     if (!ok || !make_group_map(&tc, X.planes, a.K, X.rows, 1, S, X.ld, 0, X.plane, 64) ||
         !make_group_map(&ts, X.planes, a.K, X.rows, 1, S, X.ld, 0, X.plane, 16))
@@ -586,11 +645,11 @@ cudaError_t product(const GroupedOperand &X, const GroupedOperand &W, const Grou
 }
 
 template <int S>
-cudaError_t gradient(const GroupedOperand &A, const GroupedOperand &B, const GroupedArgs &a, cudaStream_t st)
+cudaError_t gradient(const GroupedOperand &A, const GroupedOperand &B, GroupedArgs a, cudaStream_t st)
 {
     CUtensorMap tl, tc;
-    if (!make_group_map(&tl, B.planes, a.L, B.rows, 1, S, B.ld, 0, B.plane, 64) ||
-        !make_group_map(&tc, A.planes, a.C, A.rows, 1, S, A.ld, 0, A.plane, 64))
+    if (!make_group_map(&tl, B.planes, a.L, B.rows, 1, S, B.ld, 0, B.plane, kKB, &a.lwide) ||
+        !make_group_map(&tc, A.planes, a.C, A.rows, 1, S, A.ld, 0, A.plane, kKB, &a.cwide, 256))
         return cudaErrorInvalidValue;
     return run_grouped<S, 256, true, true, true>(tl, tc, tc, a, (int64_t)a.G * ((a.L + 255) / 256) * ((a.C + 255) / 256), st);
 }

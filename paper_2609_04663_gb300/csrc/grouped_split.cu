@@ -120,12 +120,19 @@ __global__ void __launch_bounds__(kThreads) grouped_split_kernel(const SplitArgs
             row = static_cast<const char *>(a.X) + ((p / a.per) * a.stride + (p % a.per) * a.ldx) * esize;
         }
         uint16_t *dst = a.comps + p * a.ldcomp;
-#pragma unroll 4
-        for (int64_t j0 = lane * 8; j0 < a.ldcomp; j0 += 256) {
-            uint4 w[S];
-            amax = load8<S>(row, j0, a.cols, vec, w, amax);
+        constexpr int B = 4;                      // pieces loaded before the first is stored
+        for (int64_t j0 = lane * 8; j0 < a.ldcomp; j0 += 256 * B) {
+            uint4 w[B][S];
 #pragma unroll
-            for (int r = 0; r < S; ++r) *reinterpret_cast<uint4 *>(dst + r * a.plane + j0) = w[r];
+            for (int b = 0; b < B; ++b)
+                if (j0 + 256 * b < a.ldcomp) amax = load8<S>(row, j0 + 256 * b, a.cols, vec, w[b], amax);
+#pragma unroll
+            for (int b = 0; b < B; ++b)
+                if (j0 + 256 * b < a.ldcomp) {
+#pragma unroll
+                    for (int r = 0; r < S; ++r)
+                        *reinterpret_cast<uint4 *>(dst + r * a.plane + j0 + 256 * b) = w[b][r];
+                }
         }
     }
     if constexpr (S == 3) publish_f32_flags(amax, a.flags);

@@ -30,10 +30,11 @@ namespace emu {
 
 namespace {
 
-constexpr int kWarps = 4, kRows = 32 * kWarps;        // features per CTA
-constexpr int kStageK = 256;                          // k of one ring stage: 128 bytes of codes per row
+constexpr int kWarps = 8, kRows = 32 * kWarps;        // features per CTA
+constexpr int kStageK = 128;                          // k of one ring stage: 64 bytes of codes per row
 constexpr int kStages = 3;
-constexpr int kPassK = 1024;                          // k for which X and the scales are staged at once
+constexpr int kStageBytes = 32 * kStageK / 2;         // of one warp
+constexpr int kPassK = 512;                           // k for which X and the scales are staged at once
 
 struct W4Args {
     const void *X;
@@ -48,9 +49,9 @@ struct W4Args {
     int x_f32, s_f32, x_vec;                          // x_vec: X's rows can be read 16 bytes at a time
 };
 
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, bool valid)
+// The first n of 16 bytes from src (16-byte aligned), the rest zeros.
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, int n)
 {
-    const int n = valid ? 16 : 0;                     // 0: the 16 bytes are filled with zeros
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
 }
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
@@ -61,6 +62,24 @@ __device__ __forceinline__ uint32_t lds32(uint32_t a)
 {
     uint32_t v;
     asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(a));
+    return v;
+}
+__device__ __forceinline__ uint32_t lds16(uint32_t a)
+{
+    uint16_t v;
+    asm volatile("ld.shared.b16 %0, [%1];" : "=h"(v) : "r"(a));
+    return v;
+}
+__device__ __forceinline__ uint32_t lds8(uint32_t a)
+{
+    uint32_t v;
+    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(a));
+    return v;
+}
+__device__ __forceinline__ uint2 lds64(uint32_t a)
+{
+    uint2 v;
+    asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
     return v;
 }
 __device__ __forceinline__ uint4 lds128(uint32_t a)
@@ -88,6 +107,16 @@ __device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
+// The same with a zero accumulator.
+__device__ __forceinline__ void mma16816_first(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                               uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+                 "{%10, %10, %10, %10};"
+                 : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.0f));
+}
+
 // 8 consecutive BF16 as pairs (0,4) (1,5) (2,6) (3,7).
 __device__ __forceinline__ uint4 pair_order(uint32_t w01, uint32_t w23, uint32_t w45, uint32_t w67)
 {
@@ -110,12 +139,14 @@ __host__ __device__ __forceinline__ int meta_pitch(int group, int size)
 // pass (64 bytes per 32 k and column), the pass's scales and zero points.
 int w4_smem(int cols, int group, int ssize, bool zeros)
 {
-    return kWarps * kStages * 32 * 128 + (kPassK / 32) * cols * 64 + kRows * meta_pitch(group, ssize) +
+    return kWarps * kStages * kStageBytes + (kPassK / 32) * cols * 64 + kRows * meta_pitch(group, ssize) +
            (zeros ? kRows * meta_pitch(group, 1) : 0);
 }
 
-// NT: tiles of 8 columns; F32X: FP32 rows, three columns each.
-template <int NT, bool F32X>
+// NT: tiles of 8 columns; F32X: FP32 rows, three columns each.  GB: 32-k blocks
+// of a scale group within a stage of 4: 1 or 2 (groups of 32 or 64), 4
+// (multiples of 128); 0: any other group, with its bounds looked for.
+template <int NT, bool F32X, int GB>
 __global__ void __launch_bounds__(32 * kWarps, 2) w4_kernel(const W4Args a)
 {
     constexpr int S = F32X ? 3 : 1;
@@ -179,24 +210,24 @@ __global__ void __launch_bounds__(32 * kWarps, 2) w4_kernel(const W4Args a)
     }
     const int cols = m * S, gb = a.group / 32, ngroups = a.K / a.group;
     const int ssize = a.s_f32 ? 4 : 2, sp = meta_pitch(a.group, ssize), zp = meta_pitch(a.group, 1);
-    const uint32_t xs = codes + kWarps * kStages * 32 * 128;
+    const uint32_t xs = codes + kWarps * kStages * kStageBytes;
     const uint32_t sc = xs + (uint32_t)((kPassK / 32) * a.tokens * S * 64), zs = sc + (uint32_t)(kRows * sp);
     const int k0 = (int)rank * a.slice, k1 = min(a.K, k0 + a.slice);
     const int nst = k1 > k0 ? (k1 - k0 + kStageK - 1) / kStageK : 0;
 
-    // ---- this warp's ring: rows n0 + 32 warp .. + 31, 16-byte piece j of a row at piece j ^ (row % 8)
-    const uint32_t ring = codes + (uint32_t)(warp * kStages * 32 * 128);
+    // ---- this warp's ring: rows n0 + 32 warp .. + 31, 16-byte piece j of a row at piece j ^ (row / 2 % 4)
+    const uint32_t ring = codes + (uint32_t)(warp * kStages * kStageBytes);
     const int64_t pitch = a.K / 2;
     const uint8_t *qbase = a.q + ((int64_t)g * a.N + n0 + warp * 32) * pitch;
     auto fetch = [&](int st) {
         if (st < nst) {
-            const uint32_t dst = ring + (uint32_t)((st % kStages) * 32 * 128);
-            const int piece = lane & 7, byte = (k0 + st * kStageK) / 2 + piece * 16;
+            const uint32_t dst = ring + (uint32_t)((st % kStages) * kStageBytes);
+            const int piece = lane & 3, byte = (k0 + st * kStageK) / 2 + piece * 16;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int r = i * 4 + (lane >> 3);
+            for (int i = 0; i < 4; ++i) {
+                const int r = i * 8 + (lane >> 2);
                 const bool ok = n0 + warp * 32 + r < a.N && byte < k1 / 2;
-                cp_async16(dst + (uint32_t)(r * 128 + ((piece ^ (r & 7)) << 4)), ok ? qbase + r * pitch + byte : a.q, ok);
+                cp_async16(dst + (uint32_t)(r * 64 + ((piece ^ (r >> 1 & 3)) << 4)), ok ? qbase + r * pitch + byte : a.q, ok ? 16 : 0);
             }
         }
         cp_async_commit();
@@ -206,7 +237,7 @@ __global__ void __launch_bounds__(32 * kWarps, 2) w4_kernel(const W4Args a)
     auto meta = [&](uint32_t dst, int dpitch, const void *src, int size, int g0, int n) {
         const uint8_t *from = static_cast<const uint8_t *>(src) + (((int64_t)g * a.N + n0) * ngroups + g0) * size;
         const int64_t rowb = (int64_t)ngroups * size;
-        const int pieces = (n * size + 15) / 16;
+        const int pieces = dpitch / 16;               // past the n values: zeros
         // whole pieces only: a row's last piece may not run into what follows the array
         const bool wide = ((reinterpret_cast<uintptr_t>(from) | (uintptr_t)rowb) & 15u) == 0;
         for (int i = threadIdx.x; i < kRows * pieces; i += 32 * kWarps) {
@@ -214,9 +245,10 @@ __global__ void __launch_bounds__(32 * kWarps, 2) w4_kernel(const W4Args a)
             const bool ok = n0 + r < a.N;
             const uint32_t to = dst + (uint32_t)(r * dpitch + o);
             if (wide) {
-                cp_async16(to, ok ? from + r * rowb + o : a.q, ok);
+                const int len = ok ? min(max(n * size - o, 0), 16) : 0;
+                cp_async16(to, len ? from + r * rowb + o : a.q, len);
             } else {
-                const int len = ok ? min(16, n * size - o) : 0;
+                const int len = ok ? n * size - o : 0;
                 for (int b = 0; b < 16; b += size) {
                     const uint8_t *p = from + r * rowb + o + b;
                     if (size == 4) {
@@ -254,29 +286,48 @@ __global__ void __launch_bounds__(32 * kWarps, 2) w4_kernel(const W4Args a)
 #pragma unroll
             for (int st = 0; st < kStages - 1; ++st) fetch(st);
         }
-        for (int i = threadIdx.x; i < m * (kPassK / 8); i += 32 * kWarps) {
-            const int t = i / (kPassK / 8), o = i % (kPassK / 8), k = p0 + o * 8;
-            const uint32_t dst = xs + (uint32_t)(((o >> 2) * cols + t * S) * 64 + (o & 3) * 16);
-            if constexpr (F32X) {
-                const float *x = static_cast<const float *>(a.X) + (int64_t)(row0 + t) * a.ldx + k;
-                uint32_t w[3][4];
+        // eight k of one row at a time, the loads of several in flight
+        constexpr int XB = 4;
+        for (int i0 = threadIdx.x; i0 < m * (kPassK / 8); i0 += 32 * kWarps * XB) {
+            uint4 v[XB][S == 3 ? 2 : 1];
 #pragma unroll
-                for (int e = 0; e < 4; e += 2) {
-                    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                    if (k < p1 && a.x_vec) v = __ldg(reinterpret_cast<const float4 *>(x) + (e >> 1));
-                    else if (k < p1) v = make_float4(__ldg(x + 2 * e), __ldg(x + 2 * e + 1), __ldg(x + 2 * e + 2), __ldg(x + 2 * e + 3));
-                    split_pair(v.x, v.y, w[0][e], w[1][e], w[2][e]);
-                    split_pair(v.z, v.w, w[0][e + 1], w[1][e + 1], w[2][e + 1]);
+            for (int b = 0; b < XB; ++b) {
+                const int i = i0 + b * 32 * kWarps, k = p0 + i % (kPassK / 8) * 8;
+                const bool in = i < m * (kPassK / 8) && k < p1;
+                const char *x = static_cast<const char *>(a.X) + ((int64_t)(row0 + i / (kPassK / 8)) * a.ldx + k) * (F32X ? 4 : 2);
+#pragma unroll
+                for (int h = 0; h < (F32X ? 2 : 1); ++h) {
+                    v[b][h] = make_uint4(0u, 0u, 0u, 0u);
+                    if (in && a.x_vec) {
+                        v[b][h] = __ldg(reinterpret_cast<const uint4 *>(x) + h);
+                    } else if (in && F32X) {
+                        const uint32_t *u = reinterpret_cast<const uint32_t *>(x) + 4 * h;
+                        v[b][h] = make_uint4(__ldg(u), __ldg(u + 1), __ldg(u + 2), __ldg(u + 3));
+                    } else if (in) {
+                        const uint16_t *u = reinterpret_cast<const uint16_t *>(x);
+                        auto two = [&](int e) { return (uint32_t)__ldg(u + e) | (uint32_t)__ldg(u + e + 1) << 16; };
+                        v[b][h] = make_uint4(two(0), two(2), two(4), two(6));
+                    }
                 }
+            }
 #pragma unroll
-                for (int s = 0; s < 3; ++s) sts128(dst + s * 64, pair_order(w[s][0], w[s][1], w[s][2], w[s][3]));
-            } else {
-                const uint16_t *x = static_cast<const uint16_t *>(a.X) + (int64_t)(row0 + t) * a.ldx + k;
-                uint4 w = make_uint4(0u, 0u, 0u, 0u);
-                auto two = [&](int e) { return (uint32_t)__ldg(x + e) | (uint32_t)__ldg(x + e + 1) << 16; };
-                if (k < p1 && a.x_vec) w = __ldg(reinterpret_cast<const uint4 *>(x));
-                else if (k < p1) w = make_uint4(two(0), two(2), two(4), two(6));
-                sts128(dst, pair_order(w.x, w.y, w.z, w.w));
+            for (int b = 0; b < XB; ++b) {
+                const int i = i0 + b * 32 * kWarps, o = i % (kPassK / 8);
+                if (i >= m * (kPassK / 8)) break;
+                const uint32_t dst = xs + (uint32_t)(((o >> 2) * cols + i / (kPassK / 8) * S) * 64 + (o & 3) * 16);
+                if constexpr (F32X) {
+                    uint32_t w[3][4];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        split_pair(__uint_as_float(v[b][h].x), __uint_as_float(v[b][h].y), w[0][2 * h], w[1][2 * h], w[2][2 * h]);
+                        split_pair(__uint_as_float(v[b][h].z), __uint_as_float(v[b][h].w), w[0][2 * h + 1], w[1][2 * h + 1],
+                                   w[2][2 * h + 1]);
+                    }
+#pragma unroll
+                    for (int s = 0; s < 3; ++s) sts128(dst + s * 64, pair_order(w[s][0], w[s][1], w[s][2], w[s][3]));
+                } else {
+                    sts128(dst, pair_order(v[b][0].x, v[b][0].y, v[b][0].z, v[b][0].w));
+                }
             }
         }
         // the scales have arrived: with the first pass the codes' first stages
@@ -289,70 +340,103 @@ __global__ void __launch_bounds__(32 * kWarps, 2) w4_kernel(const W4Args a)
             cp_async_wait<kStages - 2>();
             __syncwarp();
             fetch(st + kStages - 1);                  // into the stage read in the step before
-            const uint32_t stage = ring + (uint32_t)((st % kStages) * 32 * 128) + (uint32_t)(lr * 128 + lc * 4);
-            const int kb0 = (k0 + st * kStageK) / 32, kb1 = min(kb0 + 8, k1 / 32);
-            int gi = kb0 / gb, left = gb - kb0 % gb;  // scale group, its 32-k blocks left
-            for (int kb = kb0; kb < kb1;) {
-                // the part of a scale group that this stage holds
-                const int end = min(kb1, kb + left);
-                float s[4];
-                uint32_t z[4];
+            const uint32_t stage = ring + (uint32_t)((st % kStages) * kStageBytes) + (uint32_t)(lr * 64 + lc * 4);
+            const uint32_t xst = xs + (uint32_t)((st - st0) * (kStageK / 32) * cols * 64 + lr * 64 + lc * 16);
+            const uint32_t srow = sc + (uint32_t)((warp * 32 + lr) * sp), zrow = zs + (uint32_t)((warp * 32 + lr) * zp);
+            // block b of the stage: codes of rows lr + 8 r, X's columns
+            auto block = [&](int b, bool first, const uint32_t (&z)[4]) {
+                uint32_t w[4];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int row = warp * 32 + r * 8 + lr;
-                    const uint32_t at = sc + (uint32_t)(row * sp + (gi - g0) * ssize);
-                    if (a.s_f32) {
-                        s[r] = __uint_as_float(lds32(at));
-                    } else {
-                        uint16_t h;
-                        asm volatile("ld.shared.b16 %0, [%1];" : "=h"(h) : "r"(at));
-                        s[r] = __uint_as_float((uint32_t)h << 16);
-                    }
-                    z[r] = 0x43084308u;               // 128 + z as a BF16 pair (z <= 15)
-                    if (a.zeros) {
-                        uint32_t v;
-                        asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(zs + (uint32_t)(row * zp + gi - g0)));
-                        z[r] = (v & 15u) * 0x00010001u + 0x43004300u;
-                    }
-                }
-#pragma unroll 2
-                for (; kb < end; ++kb) {
-                    const uint32_t at = stage + (uint32_t)((((kb - kb0) ^ lr) & 7) << 4);
-                    uint32_t w[4];
+                for (int r = 0; r < 4; ++r) w[r] = lds32(stage + (uint32_t)(((b ^ (lr >> 1)) << 4) + r * 512));
+                uint4 x[NT];
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) w[r] = lds32(at + r * 1024);      // rows lr + 8 r
-                    uint4 b[NT];
-                    const uint32_t xa = xs + (uint32_t)((kb - p0 / 32) * cols * 64 + lc * 16);
+                for (int t = 0; t < NT; ++t)
+                    x[t] = t * 8 + lr < cols ? lds128(xst + (uint32_t)((b * cols + t * 8) * 64)) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const uint32_t u = w[2 * i], v = w[2 * i + 1], zu = z[2 * i], zv = z[2 * i + 1];
+                    const uint32_t u0 = decode(u, 0, zu), u1 = decode(u, 4, zu), u2 = decode(u, 8, zu), u3 = decode(u, 12, zu);
+                    const uint32_t v0 = decode(v, 0, zv), v1 = decode(v, 4, zv), v2 = decode(v, 8, zv), v3 = decode(v, 12, zv);
 #pragma unroll
                     for (int t = 0; t < NT; ++t) {
-                        const int n = t * 8 + lr;
-                        b[t] = n < cols ? lds128(xa + (uint32_t)(n * 64)) : make_uint4(0, 0, 0, 0);
-                    }
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const uint32_t u = w[2 * i], v = w[2 * i + 1], zu = z[2 * i], zv = z[2 * i + 1];
-                        const uint32_t u0 = decode(u, 0, zu), u1 = decode(u, 4, zu), u2 = decode(u, 8, zu),
-                                       u3 = decode(u, 12, zu);
-                        const uint32_t v0 = decode(v, 0, zv), v1 = decode(v, 4, zv), v2 = decode(v, 8, zv),
-                                       v3 = decode(v, 12, zv);
-#pragma unroll
-                        for (int t = 0; t < NT; ++t) {
-                            mma16816(part[i][t], u0, v0, u1, v1, b[t].x, b[t].y);
-                            mma16816(part[i][t], u2, v2, u3, v3, b[t].z, b[t].w);
-                        }
+                        if (first) mma16816_first(part[i][t], u0, v0, u1, v1, x[t].x, x[t].y);
+                        else mma16816(part[i][t], u0, v0, u1, v1, x[t].x, x[t].y);
+                        mma16816(part[i][t], u2, v2, u3, v3, x[t].z, x[t].w);
                     }
                 }
+            };
+            auto scale_up = [&](const float (&s)[4]) {
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
 #pragma unroll
                     for (int t = 0; t < NT; ++t)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
+                        for (int e = 0; e < 4; ++e)
                             total[i][t][e] = fmaf(part[i][t][e], s[2 * i + (e >> 1)], total[i][t][e]);
-                            part[i][t][e] = 0.0f;
-                        }
-                ++gi;
-                left = gb;
+            };
+            if constexpr (GB > 0) {
+                // what lies past the slice is zero codes, zero X and zero scales
+                constexpr int NG = 4 / GB;            // scale groups of the stage
+                const int go = GB == 4 ? (k0 + st * kStageK) / a.group - g0 : (st - st0) * NG;
+                float s[NG][4];
+                uint32_t z[NG][4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const uint32_t at = srow + (uint32_t)(r * 8 * sp + go * ssize);
+                    uint32_t f[4];
+                    if (a.s_f32) {
+                        if constexpr (NG == 4) { const uint4 v = lds128(at); f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w; }
+                        else if constexpr (NG == 2) { const uint2 v = lds64(at); f[0] = v.x; f[1] = v.y; }
+                        else f[0] = lds32(at);
+                    } else {
+                        uint2 v;
+                        if constexpr (NG == 4) v = lds64(at);
+                        else if constexpr (NG == 2) v.x = lds32(at);
+                        else v.x = lds16(at);
+                        f[0] = v.x << 16;
+                        f[1] = v.x & 0xFFFF0000u;
+                        f[2] = v.y << 16;
+                        f[3] = v.y & 0xFFFF0000u;
+                    }
+                    uint32_t q = 0x08080808u;
+                    if (a.zeros) {
+                        const uint32_t az = zrow + (uint32_t)(r * 8 * zp + go);
+                        q = (NG == 4 ? lds32(az) : NG == 2 ? lds16(az) : lds8(az)) & 0x0F0F0F0Fu;
+                    }
+#pragma unroll
+                    for (int n = 0; n < NG; ++n) {
+                        s[n][r] = __uint_as_float(f[n]);
+                        z[n][r] = __byte_perm(q, 0x43434343u, 0x4040u + 0x0101u * n);      // 128 + z as a BF16 pair
+                    }
+                }
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    block(b, b % GB == 0, z[b / GB]);
+                    if (b % GB == GB - 1) scale_up(s[b / GB]);
+                }
+            } else {
+                const int kb0 = (k0 + st * kStageK) / 32, kb1 = min(kb0 + kStageK / 32, k1 / 32);
+                for (int kb = kb0; kb < kb1;) {
+                    // the part of a scale group that this stage holds
+                    const int gi = kb / gb, end = min(kb1, (gi + 1) * gb);
+                    float s[4];
+                    uint32_t z[4];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const uint32_t at = srow + (uint32_t)(r * 8 * sp + (gi - g0) * ssize);
+                        s[r] = __uint_as_float(a.s_f32 ? lds32(at) : lds16(at) << 16);
+                        const uint32_t q = a.zeros ? lds8(zrow + (uint32_t)(r * 8 * zp + gi - g0)) & 15u : 8u;
+                        z[r] = __byte_perm(q, 0x43434343u, 0x4040u);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int t = 0; t < NT; ++t)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) part[i][t][e] = 0.0f;
+                    for (; kb < end; ++kb) block(kb - kb0, false, z);
+                    scale_up(s);
+                }
             }
         }
     }
@@ -377,18 +461,22 @@ __global__ void __launch_bounds__(32 * kWarps, 2) w4_kernel(const W4Args a)
     const int per = kRows / (int)ks;
     for (int i = threadIdx.x; i < m * per; i += 32 * kWarps) {
         const int t = i / per, r = (int)rank * per + i % per, n = n0 + r;
-        float y = 0.0f;
-        for (uint32_t c = 0; c < ks; ++c) {
+        float v[8][S], y = 0.0f;
 #pragma unroll
-            for (int s = S - 1; s >= 0; --s) {
+        for (uint32_t c = 0; c < 8; ++c) {
+#pragma unroll
+            for (int s = 0; s < S; ++s) {
                 uint32_t at;
                 asm volatile("mapa.shared::cluster.u32 %0, %1, %2;"
-                             : "=r"(at) : "r"(codes + (uint32_t)(((t * S + s) * kRows + r) * 4)), "r"(c));
-                float v;
-                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
-                y = __fadd_rn(y, v);
+                             : "=r"(at) : "r"(codes + (uint32_t)(((t * S + s) * kRows + r) * 4)), "r"(c < ks ? c : 0u));
+                v[c][s] = 0.0f;
+                if (c < ks) asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[c][s]) : "r"(at) : "memory");
             }
         }
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+#pragma unroll
+            for (int s = S - 1; s >= 0; --s) y = __fadd_rn(y, v[c][s]);
         if (n < a.N) {
             const int64_t o = (int64_t)(row0 + t) * a.ldy + n;
             if (a.x_f32) static_cast<float *>(a.Y)[o] = y;
@@ -399,10 +487,10 @@ __global__ void __launch_bounds__(32 * kWarps, 2) w4_kernel(const W4Args a)
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-template <int NT, bool F32X>
+template <int NT, bool F32X, int GB>
 cudaError_t run_w4(const W4Args &a, int64_t blocks, int64_t items, int ks, cudaStream_t st)
 {
-    auto kern = w4_kernel<NT, F32X>;
+    auto kern = w4_kernel<NT, F32X, GB>;
     const int sm = w4_smem(a.tokens * (F32X ? 3 : 1), a.group, a.s_f32 ? 4 : 2, a.zeros != nullptr);
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, sm);
     if (e != cudaSuccess) return e;
@@ -441,18 +529,20 @@ cudaError_t launch_w4_matvec(bool x_f32, int64_t G, int64_t rows, int64_t N, int
     int64_t want = ends ? 2 * ((rows + active - 1) / active) : rows;
     if (want > rows) want = rows;
     int nt = (int)((want * S + 7) / 8);
-    if (nt > 3) nt = 3;
+    nt = nt > 1 ? 3 : 1;
     a.tokens = 8 * nt / S;
     const int64_t blocks = (N + kRows - 1) / kRows;
     const int64_t items = ends ? active + rows / a.tokens + 1 : (rows + a.tokens - 1) / a.tokens;
     if (items > 65535) return cudaErrorInvalidValue;
-    // slices of K: at most one pass each where 8 of them allow it, and as many
-    // CTAs as twice the SMs want while each still has one ring stage
+    // slices of K, each of one pass at least: as many CTAs as one and a half
+    // times what runs at once
     int ks = 1;
-    while (ks < 8 && (ks * kPassK < K || (blocks * active * ks < 2 * 152 && ks * 2 * kStageK <= K))) ks *= 2;
-    a.slice = (int)((K + (int64_t)ks * kStageK - 1) / ((int64_t)ks * kStageK) * kStageK);
-#define EMU_W4(NT) (x_f32 ? run_w4<NT, true>(a, blocks, items, ks, st) : run_w4<NT, false>(a, blocks, items, ks, st))
-    return nt == 1 ? EMU_W4(1) : nt == 2 ? EMU_W4(2) : EMU_W4(3);
+    while (ks < 8 && blocks * active * ks < 3 * 152 && ks * 2 * kPassK <= K) ks *= 2;
+    a.slice = (int)((K + (int64_t)ks * kPassK - 1) / ((int64_t)ks * kPassK) * kPassK);
+#define EMU_W4(GB)                                                                                              \
+    (x_f32 ? (nt == 1 ? run_w4<1, true, GB>(a, blocks, items, ks, st) : run_w4<3, true, GB>(a, blocks, items, ks, st)) \
+           : (nt == 1 ? run_w4<1, false, GB>(a, blocks, items, ks, st) : run_w4<3, false, GB>(a, blocks, items, ks, st)))
+    return group == 32 ? EMU_W4(1) : group == 64 ? EMU_W4(2) : group % 128 == 0 ? EMU_W4(4) : EMU_W4(0);
 #undef EMU_W4
 }
 
