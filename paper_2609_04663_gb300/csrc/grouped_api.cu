@@ -192,6 +192,8 @@ emu_status emu_grouped_gemm_f32(int opW, int64_t G, int64_t rows, int64_t N, int
         uint16_t *wp = reinterpret_cast<uint16_t *>(reinterpret_cast<char *>(xp) + round_up(3 * xo.plane * 2, 256));
         wo.ld = plane_ld(wcols); wo.stride = wrows * wo.ld; wo.plane = G * wo.stride; wo.planes = wp;
         cudaError_t e = launch_grouped_split_rows(true, rows, K, X, xrows, ldx, src, ends, G, xp, xo.ld, flags, st);
+        if (e == cudaSuccess && rows <= kFusedRows * G && fused_takes(W, G, ldw, stridew))
+            return cuda_status(launch_grouped_fused(opW == EMU_OP_T, G, rows, N, K, xo, W, ldw, stridew, ends, Y, ldy, flags, st));
         if (e == cudaSuccess) e = launch_grouped_split(true, G, wrows, wcols, W, ldw, stridew, wp, wo.ld, flags, st);
         if (e != cudaSuccess) return EMU_ERR_CUDA;
     }

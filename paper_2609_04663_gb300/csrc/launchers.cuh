@@ -149,6 +149,14 @@ cudaError_t launch_grouped_split_rows(bool f32, int64_t rows, int64_t cols, cons
 cudaError_t launch_grouped_product(int S, bool trans, int64_t G, int64_t rows, int64_t N, int64_t K,
                                    const GroupedOperand &X, const GroupedOperand &W, const int32_t *ends, void *Y,
                                    bool y_f32, int64_t ldy, uint32_t *flags, cudaStream_t st);
+// FP32 weights that meet few rows each, split inside the product
+// (grouped_fused.cu); fused_takes: whether their rows can be read by TMA;
+// kFusedRows: up to so many rows for each group on average that is the faster way.
+bool fused_takes(const float *W, int64_t G, int64_t ldw, int64_t stridew);
+cudaError_t launch_grouped_fused(bool trans, int64_t G, int64_t rows, int64_t N, int64_t K, const GroupedOperand &X,
+                                 const float *W, int64_t ldw, int64_t stridew, const int32_t *ends, float *Y,
+                                 int64_t ldy, uint32_t *flags, cudaStream_t st);
+constexpr int64_t kFusedRows = 127;
 cudaError_t launch_grouped_gradient(int S, int64_t G, int64_t rows, int64_t M, int64_t N, const GroupedOperand &A,
                                     const GroupedOperand &B, const int32_t *ends, void *D, bool d_f32, int64_t ldd,
                                     int64_t strided, uint32_t *flags, cudaStream_t st);

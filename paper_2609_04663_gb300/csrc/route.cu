@@ -84,7 +84,7 @@ __device__ __forceinline__ void route_barrier(uint32_t *bar, uint32_t *flags)
 }
 
 // V: logits per lane (E <= 32 V).
-template <int V>
+template <int V, bool F32>
 __global__ void __launch_bounds__(kRouteThreads) route_kernel(const RouteArgs a)
 {
     extern __shared__ int32_t sm[];
@@ -98,15 +98,22 @@ __global__ void __launch_bounds__(kRouteThreads) route_kernel(const RouteArgs a)
     // ---- the k largest of each token
     bool odd = false;
     for (int t = t0 + warp; t < t1; t += kRouteWarps) {
-        const char *row = static_cast<const char *>(a.logits) + (int64_t)t * a.ldl * (a.f32 ? 4 : 2);
+        const char *row = static_cast<const char *>(a.logits) + (int64_t)t * a.ldl * (F32 ? 4 : 2);
         uint32_t key[V];
         float x[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             const int e = i * 32 + lane;
-            x[i] = e < a.E ? load_logit(row, e, a.f32 != 0) : -INFINITY;
+            x[i] = e < a.E ? load_logit(row, e, F32) : -INFINITY;
+        }
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const int e = i * 32 + lane;
             odd |= !(x[i] < INFINITY);                    // NaN or plus infinity
             key[i] = e < a.E ? logit_key(x[i]) : 0u;
+            // a BF16 logit's key fills the upper half: with the inverted index below
+            // it the largest word is the largest logit of the lowest index
+            if (!F32 && e < a.E) key[i] = (key[i] & 0xFFFF0000u) | (0xFFFFu - (uint32_t)e);
         }
         // up to 8 logits a lane: its candidates by falling key (equal keys: rising
         // index), the best of all lanes' firsts taken off k times; more: each lane
@@ -119,15 +126,15 @@ __global__ void __launch_bounds__(kRouteThreads) route_kernel(const RouteArgs a)
 #pragma unroll
             for (int i = 1; i < V; ++i)
 #pragma unroll
-                for (int q = V - 1; q >= i; --q)
-                    if (key[q] > key[q - 1]) {
-                        const uint32_t u = key[q];
-                        const int v = at[q];
-                        key[q] = key[q - 1]; at[q] = at[q - 1];
-                        key[q - 1] = u; at[q - 1] = v;
-                    }
+                for (int q = V - 1; q >= i; --q) {
+                    const bool swap = key[q] > key[q - 1];
+                    const uint32_t hi = max(key[q], key[q - 1]), lo = min(key[q], key[q - 1]);
+                    const int u = at[q], v = at[q - 1];
+                    key[q - 1] = hi; key[q] = lo;
+                    if (F32) { at[q - 1] = swap ? u : v; at[q] = swap ? v : u; }
+                }
         }
-        float mine = -INFINITY, top = -INFINITY;          // lane j: the j-th logit
+        uint32_t mine = 0u, top_key = 0u;                 // lane j: the j-th key
         int chosen = 0;
         for (int j = 0; j < a.k; ++j) {
             uint32_t best = key[0];
@@ -138,12 +145,19 @@ __global__ void __launch_bounds__(kRouteThreads) route_kernel(const RouteArgs a)
                     if (key[i] > best) { best = key[i]; first = i * 32 + lane; }
             }
             const uint32_t most = __reduce_max_sync(0xFFFFFFFFu, best);
-            const uint32_t hit = __ballot_sync(0xFFFFFFFFu, best == most);
             int e;
-            if ((hit & (hit - 1)) == 0) e = __shfl_sync(0xFFFFFFFFu, first, __ffs(hit) - 1);
-            else e = (int)__reduce_min_sync(0xFFFFFFFFu, best == most ? (uint32_t)first : 0x7FFFFFFFu);
+            bool own;
+            if constexpr (F32) {
+                const uint32_t hit = __ballot_sync(0xFFFFFFFFu, best == most);
+                if ((hit & (hit - 1)) == 0) e = __shfl_sync(0xFFFFFFFFu, first, __ffs(hit) - 1);
+                else e = (int)__reduce_min_sync(0xFFFFFFFFu, best == most ? (uint32_t)first : 0x7FFFFFFFu);
+                own = first == e;
+            } else {
+                e = 0xFFFF - (int)(most & 0xFFFFu);
+                own = best == most;
+            }
             if constexpr (SORT) {
-                if (first == e) {
+                if (own) {
 #pragma unroll
                     for (int i = 1; i < V; ++i) { key[i - 1] = key[i]; at[i - 1] = at[i]; }
                     key[V - 1] = 0u;
@@ -154,11 +168,14 @@ __global__ void __launch_bounds__(kRouteThreads) route_kernel(const RouteArgs a)
                 for (int i = 0; i < V; ++i)
                     if (i * 32 + lane == e) key[i] = 0u;
             }
-            if (j == 0) top = key_logit(most);
-            if (lane == j) { mine = key_logit(most); chosen = e; }
+            if (j == 0) top_key = most;
+            if (lane == j) { mine = most; chosen = e; }
         }
+        // the padding below a BF16 key is its logit's lower half: zeros, or ones where negative
+        auto logit = [&](uint32_t k) { return key_logit(F32 ? k : (k & 0x80000000u) ? k & 0xFFFF0000u : k | 0xFFFFu); };
+        const float top = logit(top_key);
         const bool some = top > -INFINITY;                // else no expert is allowed: weights 0
-        const float p = some && lane < a.k ? expf(mine - top) : 0.0f;
+        const float p = some && lane < a.k ? expf(logit(mine) - top) : 0.0f;
         float total;
         if (a.renorm) {
             total = warp_sum(p);
@@ -495,7 +512,7 @@ template <int V>
 cudaError_t run_route(const RouteArgs &a, int blocks, cudaStream_t st)
 {
     const size_t sm = (size_t)(kRouteWarps + 2) * a.E * sizeof(int32_t);
-    auto kern = route_kernel<V>;
+    auto kern = a.f32 ? route_kernel<V, true> : route_kernel<V, false>;
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sm);
     if (e != cudaSuccess) return e;
     if (blocks == 1) {
