@@ -59,7 +59,7 @@ grouped_kernel(const __grid_constant__ CUtensorMap tmL, const __grid_constant__ 
     volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(base_ptr + Cfg::BAR_OFF + 16 * Cfg::STAGES + 48);
     int *starts = reinterpret_cast<int *>(base_ptr + Cfg::TAB_OFF), *tpre = starts + a.G + 1;
 
-    const int warp = threadIdx.x >> 5, lane = (int)lane_id();
+    const int warp = uniform((int)threadIdx.x >> 5), lane = (int)lane_id();
     const int rank = PAIR ? (int)cluster_rank() : 0;
     uint32_t *flags = a.flags;
 
@@ -94,8 +94,8 @@ grouped_kernel(const __grid_constant__ CUtensorMap tmL, const __grid_constant__ 
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if constexpr (!CMN) total = tpre[a.G];
-    const uint32_t tmem = *tmem_slot;
+    if constexpr (!CMN) total = uniform(tpre[a.G]);
+    const uint32_t tmem = (uint32_t)uniform((int)*tmem_slot);
     const int first = (int)blockIdx.x / Cfg::CTAS, step = (int)gridDim.x / Cfg::CTAS;
 
     if (warp == 0 && lane == 0) {
@@ -165,71 +165,69 @@ grouped_kernel(const __grid_constant__ CUtensorMap tmL, const __grid_constant__ 
                 while (globaltimer_ns() - t0 < 200000ull) {}
             }
         }
-    } else if (warp == 1 && lane == 0 && rank == 0) {
+    } else if (warp == 1 && rank == 0) {
         // ---------------- MMA issuer (a pair's leader)
-        int s = 0, it = 0;
-        uint32_t ph = 0, cph = 0;                     // cph: chunks issued (FP32)
+        const uint32_t elected = elect_lane();
+        uint32_t s = 0, ph = 0, it = 0, cph = 0;      // it: tiles with a contraction, cph: chunks issued (FP32)
         bool ok = true;
         constexpr int kstepL = LMN ? 2048 : 32, kstepC = CMN ? 2048 : 32;
         constexpr uint64_t descL = group_desc(LMN ? 64u * kKB * 2u : 16u), descC = group_desc(CMN ? 64u * kKB * 2u : 16u);
-        auto commit = [&](uint32_t bar) {
-            if constexpr (PAIR) mma_commit_pair(bar);
-            else mma_commit(bar);
-        };
-        for (int t = first; t < total && ok; t += step, ++it) {
+        for (int t = first; t < total && ok; t += step) {
             const Tile x = tile_at<S, BC, PAIR, LMN, CMN>(t, a, starts, tpre, rank);
-            const int nkb = (x.nk + kKB - 1) / kKB, b = it & 1;
-            if (nkb == 0) { --it; continue; }         // an empty group: the epilogue writes zeros by itself
-            const uint32_t idesc = make_idesc_bf16(kLRows * Cfg::CTAS, x.csz) | (LMN ? 1u << 15 : 0u) |
+            const int nk = uniform(x.nk), nkb = (nk + kKB - 1) / kKB;
+            if (nkb == 0) continue;                   // an empty group: the epilogue writes zeros by itself
+            const uint32_t b = it & 1u, csz = (uint32_t)uniform(x.csz);
+            const uint32_t idesc = make_idesc_bf16(kLRows * Cfg::CTAS, 0) | csz >> 3 << 17 | (LMN ? 1u << 15 : 0u) |
                                    (CMN ? 1u << 16 : 0u);
-            const uint32_t d = tmem + (S == 1 ? (uint32_t)(b * 256) : 0u), d2 = tmem + 256u;
-            if (S == 1) ok = mbar_wait(tempty0 + 8u * b, (((uint32_t)it >> 1) & 1u) ^ 1u, flags);
-            else ok = mbar_wait(tempty0 + 8u, ((uint32_t)it & 1u) ^ 1u, flags);
+            const uint32_t d = tmem + (S == 1 ? b * 256u : 0u), d2 = tmem + 256u;
+            if (S == 1) ok = warp_wait(tempty0 + 8u * b, ((it >> 1) & 1u) ^ 1u, flags);
+            else ok = warp_wait(tempty0 + 8u, (it & 1u) ^ 1u, flags);
             if (!ok) break;
+            ++it;
             tc_fence_after();
             for (int kb = 0; kb < nkb; ++kb) {
-                if (!(ok = mbar_wait(full0 + 8u * s, ph, flags))) break;
+                if (!(ok = warp_wait(full0 + 8u * s, ph, flags))) break;
                 tc_fence_after();
-                const uint32_t st = (base + (uint32_t)(s * Cfg::STAGE)) >> 4;
+                const uint32_t st = (base + s * (uint32_t)Cfg::STAGE) >> 4;
                 // 16-wide steps that hold contraction elements (the rest of the stage may hold anything)
-                const int left = x.nk - kb * kKB;
+                const int left = nk - kb * kKB;
                 auto mma = [&](uint32_t acc, int il, int ic, int kk, bool add) {
-                    const uint64_t ld = descL + (st + (uint32_t)((il * Cfg::L_TILE + kk * kstepL) >> 4));
-                    const uint64_t cd = descC + (st + (uint32_t)((S * Cfg::L_TILE + ic * Cfg::C_TILE + kk * kstepC) >> 4));
-                    if constexpr (PAIR) mma_bf16_pair(acc, ld, cd, idesc, add);
-                    else mma_bf16(acc, ld, cd, idesc, add);
+                    mma_elected<PAIR>(elected, acc, descL + (st + (uint32_t)((il * Cfg::L_TILE + kk * kstepL) >> 4)),
+                                      descC + (st + (uint32_t)((S * Cfg::L_TILE + ic * Cfg::C_TILE + kk * kstepC) >> 4)), idesc,
+                                      add);
                 };
                 if constexpr (S == 3) {
                     const int kc = kb % kChunkBlocks;
 #pragma unroll
                     for (int kk = 0; kk < kKB / 16; ++kk) {
-                        if (16 * kk >= left) break;
-                        mma(d2, 1, 1, kk, (kb | kk) != 0);
-                        mma(d2, 1, 0, kk, true);
-                        mma(d2, 2, 0, kk, true);
-                        mma(d2, 0, 2, kk, true);
-                        mma(d2, 0, 1, kk, true);
+                        if (16 * kk < left) {
+                            mma(d2, 1, 1, kk, (kb | kk) != 0);
+                            mma(d2, 1, 0, kk, true);
+                            mma(d2, 2, 0, kk, true);
+                            mma(d2, 0, 2, kk, true);
+                            mma(d2, 0, 1, kk, true);
+                        }
                     }
                     if (kc == 0) {                    // the last chunk's leading sum has been read
-                        if (!(ok = mbar_wait(tempty0, (cph & 1u) ^ 1u, flags))) break;
+                        if (!(ok = warp_wait(tempty0, (cph & 1u) ^ 1u, flags))) break;
                         tc_fence_after();
                     }
 #pragma unroll
                     for (int kk = 0; kk < kKB / 16; ++kk)
                         if (16 * kk < left) mma(d, 0, 0, kk, (kc | kk) != 0);
-                    commit(empty0 + 8u * s);
-                    if (kc == kChunkBlocks - 1 || kb == nkb - 1) { commit(tfull0); ++cph; }
+                    commit_elected<PAIR>(elected, empty0 + 8u * s);
+                    if (kc == kChunkBlocks - 1 || kb == nkb - 1) { commit_elected<PAIR>(elected, tfull0); ++cph; }
                 } else {
 #pragma unroll
                     for (int kk = 0; kk < kKB / 16; ++kk)
                         if (16 * kk < left) mma(d, 0, 0, kk, (kb | kk) != 0);
-                    commit(empty0 + 8u * s);
+                    commit_elected<PAIR>(elected, empty0 + 8u * s);
                 }
                 if (++s == Cfg::STAGES) { s = 0; ph ^= 1u; }
             }
-            if (ok && S == 1) commit(tfull0 + 8u * b);
+            if (ok && S == 1) commit_elected<PAIR>(elected, tfull0 + 8u * b);
         }
-        commit(done_bar);
+        commit_elected<PAIR>(elected, done_bar);
         (void)mbar_wait(done_bar, 0, flags);
     } else if (warp >= 2) {
         // ---------------- epilogue: this CTA's 128 features of each tile; a warp

@@ -63,7 +63,7 @@ grouped_fused_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_const
     const uint32_t wfull0 = cempty + 8u, wempty0 = wfull0 + 24u, done_bar = wempty0 + 24u;
     volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(base_ptr + Cfg::BAR_OFF + 16 * Cfg::STAGES + 16 * kLead + 64);
     int *starts = reinterpret_cast<int *>(base_ptr + Cfg::TAB_OFF), *tpre = starts + a.G + 1;
-    const int warp = threadIdx.x >> 5, lane = (int)lane_id();
+    const int warp = uniform((int)threadIdx.x >> 5), lane = (int)lane_id();
     uint32_t *flags = a.flags;
 
     if (threadIdx.x == 0) {
@@ -86,8 +86,8 @@ grouped_fused_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_const
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const int total = tpre[a.G], nkb = (a.K + kKB - 1) / kKB;
-    const uint32_t tmem = *tmem_slot;
+    const int total = uniform(tpre[a.G]), nkb = (a.K + kKB - 1) / kKB;
+    const uint32_t tmem = (uint32_t)uniform((int)*tmem_slot);
     auto tile = [&](int t) { return tile_at<3, COLS, false, LMN, false>(t, a, starts, tpre, 0); };
 
     if (warp < kSplitWarps) {
@@ -185,51 +185,53 @@ grouped_fused_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_const
         }
         // copies that no MMA has waited for may still be on their way
         if (!ok) drain_inflight(full0, Cfg::STAGES, issued, flags);
-    } else if (warp == kSplitWarps + 1 && lane == 0) {
+    } else if (warp == kSplitWarps + 1) {
         // ---------------- MMA issuer
-        int s = 0, it = 0;
-        uint32_t ph = 0, cph = 0;
+        const uint32_t elected = elect_lane();
+        uint32_t s = 0, ph = 0, cph = 0, it = 0;
         bool ok = true;
         constexpr int kstepL = LMN ? 2048 : 32, kstepC = 32;
         constexpr uint64_t descL = group_desc(LMN ? 64u * kKB * 2u : 16u), descC = group_desc(16u);
         const uint32_t rest = tmem;
         for (int t = (int)blockIdx.x; t < total && ok; t += (int)gridDim.x, ++it) {
-            const Tile x = tile(t);
-            const uint32_t idesc = make_idesc_bf16(kLRows, x.csz) | (LMN ? 1u << 15 : 0u);
-            if (!(ok = mbar_wait(cempty, ((uint32_t)it & 1u) ^ 1u, flags))) break;
+            const uint32_t csz = (uint32_t)uniform(tile(t).csz);
+            const uint32_t idesc = make_idesc_bf16(kLRows, 0) | csz >> 3 << 17 | (LMN ? 1u << 15 : 0u);
+            if (!(ok = warp_wait(cempty, (it & 1u) ^ 1u, flags))) break;
             tc_fence_after();
             for (int kb = 0; kb < nkb; ++kb) {
-                if (!(ok = mbar_wait(full0 + 8u * s, ph, flags))) break;
+                if (!(ok = warp_wait(full0 + 8u * s, ph, flags))) break;
                 tc_fence_after();
-                const uint32_t st = (base + (uint32_t)(s * Cfg::STAGE)) >> 4;
-                const int left = x.nk - kb * kKB, kc = kb % kChunkBlocks;
+                const uint32_t st = (base + s * (uint32_t)Cfg::STAGE) >> 4;
+                const int left = a.K - kb * kKB, kc = kb % kChunkBlocks;
                 auto mma = [&](uint32_t acc, int il, int ic, int kk, bool add) {
-                    mma_bf16(acc, descL + (st + (uint32_t)((il * Cfg::L_TILE + kk * kstepL) >> 4)),
-                             descC + (st + (uint32_t)((3 * Cfg::L_TILE + ic * Cfg::C_TILE + kk * kstepC) >> 4)), idesc, add);
+                    mma_elected<false>(elected, acc, descL + (st + (uint32_t)((il * Cfg::L_TILE + kk * kstepL) >> 4)),
+                                       descC + (st + (uint32_t)((3 * Cfg::L_TILE + ic * Cfg::C_TILE + kk * kstepC) >> 4)), idesc,
+                                       add);
                 };
 #pragma unroll
                 for (int kk = 0; kk < kKB / 16; ++kk) {
-                    if (16 * kk >= left) break;
-                    mma(rest, 1, 1, kk, (kb | kk) != 0);
-                    mma(rest, 1, 0, kk, true);
-                    mma(rest, 2, 0, kk, true);
-                    mma(rest, 0, 2, kk, true);
-                    mma(rest, 0, 1, kk, true);
+                    if (16 * kk < left) {
+                        mma(rest, 1, 1, kk, (kb | kk) != 0);
+                        mma(rest, 1, 0, kk, true);
+                        mma(rest, 2, 0, kk, true);
+                        mma(rest, 0, 2, kk, true);
+                        mma(rest, 0, 1, kk, true);
+                    }
                 }
                 const uint32_t b = cph % kLead, lead = tmem + (b + 1u) * COLS;
                 if (kc == 0) {                        // this accumulator's last sum has been read
-                    if (!(ok = mbar_wait(tempty0 + 8u * b, ((cph / kLead) & 1u) ^ 1u, flags))) break;
+                    if (!(ok = warp_wait(tempty0 + 8u * b, ((cph / kLead) & 1u) ^ 1u, flags))) break;
                     tc_fence_after();
                 }
 #pragma unroll
                 for (int kk = 0; kk < kKB / 16; ++kk)
                     if (16 * kk < left) mma(lead, 0, 0, kk, (kc | kk) != 0);
-                mma_commit(empty0 + 8u * s);
-                if (kc == kChunkBlocks - 1 || kb == nkb - 1) { mma_commit(tfull0 + 8u * b); ++cph; }
+                commit_elected<false>(elected, empty0 + 8u * s);
+                if (kc == kChunkBlocks - 1 || kb == nkb - 1) { commit_elected<false>(elected, tfull0 + 8u * b); ++cph; }
                 if (++s == Cfg::STAGES) { s = 0; ph ^= 1u; }
             }
         }
-        mma_commit(done_bar);
+        commit_elected<false>(elected, done_bar);
         (void)mbar_wait(done_bar, 0, flags);
     } else if (warp >= kSplitWarps + 3) {
         // ---------------- epilogue: a quarter of the lanes, 32 columns

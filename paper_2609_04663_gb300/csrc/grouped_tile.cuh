@@ -113,6 +113,47 @@ __host__ __device__ constexpr uint64_t group_desc(uint32_t lbo)
     return (uint64_t)(lbo >> 4) << 16 | (uint64_t)(1024u >> 4) << 32 | (uint64_t)1u << 46 | (uint64_t)2u << 61;
 }
 
+// The MMA warp runs converged, with every operand the same in all lanes, so
+// that the compiler can keep descriptors in uniform registers (one thread in a
+// branch of its own took 92 clocks per MMA, moving them there one by one); one
+// elected lane issues.
+__device__ __forceinline__ uint32_t elect_lane()
+{
+    uint32_t q;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(q));
+    return q;
+}
+template <bool PAIR>
+__device__ __forceinline__ void mma_elected(uint32_t elected, uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc,
+                                            uint32_t accumulate)
+{
+    if constexpr (PAIR)
+        asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+                     "@q tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                     ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(elected) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+                     "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                     ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(elected) : "memory");
+}
+template <bool PAIR>
+__device__ __forceinline__ void commit_elected(uint32_t elected, uint32_t bar)
+{
+    if (elected) {
+        if constexpr (PAIR) mma_commit_pair(bar);
+        else mma_commit(bar);
+    }
+    __syncwarp();
+}
+// A wait of a whole warp: true when every lane saw the phase complete.
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, uint32_t *flags)
+{
+    return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, flags));
+}
+// The warp's index as a value the compiler knows to be uniform, and any other
+// value that is the same in all lanes.
+__device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xFFFFFFFFu, x, 0); }
+
 // One output tile: features l0 .. (this CTA's 128), columns c0 .. c0 + cols
 // of group g (rows of the group, or m), contraction of nk elements from k0.
 struct Tile {
