@@ -101,6 +101,8 @@ grouped_fused_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_const
         // the second one first
         const bool swap = (lane >> 2) & 1;
         const uint32_t from = base + Cfg::W_OFF + (uint32_t)(LMN ? row0 * 512 + (tid & 15) * 32 : row0 * 256 + c * 32);
+        // rows of all runs are the same modulo 8
+        const uint32_t to = (uint32_t)((LMN ? ((tid >> 3) & 1) * (Cfg::L_TILE / 2) : 0) + row0 * 128 + ((c ^ (row0 & 7)) << 4));
         uint32_t amax = 0, s = 0, ph = 0, ws = 0, wph = 0;
         bool ok = true;
         const int mine = total > (int)blockIdx.x ? (total - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x : 0;
@@ -119,25 +121,26 @@ grouped_fused_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_const
             __syncwarp();
             if (lane == 0) mbar_arrive(wempty0 + 8u * ws);
             if (++ws == Cfg::W_STAGES) { ws = 0; wph ^= 1u; }
-            ok = __all_sync(0xFFFFFFFFu, mbar_wait(empty0 + 8u * s, ph ^ 1u, flags));
-            if (!ok) break;
-            const uint32_t st = base + s * (uint32_t)Cfg::STAGE;
+            // split before the stage is waited for: between its release and the
+            // next MMAs only the stores are left
+            uint4 p[kRuns][3];
 #pragma unroll
             for (int r = 0; r < kRuns; ++r) {
                 const float4 u = w[r][0], v = w[r][1];
-                uint4 p[3];
                 amax = abs_bits_max(abs_bits_max(abs_bits_max(abs_bits_max(amax, u.x, u.y), u.z, u.w), v.x, v.y), v.z, v.w);
-                split_pair(u.x, u.y, p[0].x, p[1].x, p[2].x);
-                split_pair(u.z, u.w, p[0].y, p[1].y, p[2].y);
-                split_pair(v.x, v.y, p[0].z, p[1].z, p[2].z);
-                split_pair(v.z, v.w, p[0].w, p[1].w, p[2].w);
-                const int row = row0 + r * RSTEP;
-                const uint32_t at = st + (uint32_t)((LMN ? ((tid >> 3) & 1) * (Cfg::L_TILE / 2) : 0) + row * 128 +
-                                                    ((c ^ (row & 7)) << 4));
+                split_pair(u.x, u.y, p[r][0].x, p[r][1].x, p[r][2].x);
+                split_pair(u.z, u.w, p[r][0].y, p[r][1].y, p[r][2].y);
+                split_pair(v.x, v.y, p[r][0].z, p[r][1].z, p[r][2].z);
+                split_pair(v.z, v.w, p[r][0].w, p[r][1].w, p[r][2].w);
+            }
+            ok = __all_sync(0xFFFFFFFFu, mbar_wait(empty0 + 8u * s, ph ^ 1u, flags));
+            if (!ok) break;
+            const uint32_t st = base + s * (uint32_t)Cfg::STAGE + to;
+#pragma unroll
+            for (int r = 0; r < kRuns; ++r)
 #pragma unroll
                 for (int q = 0; q < 3; ++q)
-                    st_shared_v4(at + (uint32_t)(q * Cfg::L_TILE), p[q].x, p[q].y, p[q].z, p[q].w);
-            }
+                    st_shared_v4(st + (uint32_t)(r * RSTEP * 128 + q * Cfg::L_TILE), p[r][q].x, p[r][q].y, p[r][q].z, p[r][q].w);
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(full0 + 8u * s);
