@@ -452,15 +452,15 @@ emu_status emu_grouped_gemm_f32(int opW, int64_t G, int64_t rows, int64_t N, int
                                 const int32_t *ends, float *Y, int64_t ldy, void *ws, size_t ws_bytes,
                                 emu_stream_t stream);
 
-/* Weight gradient: D_g = A_g^T B_g over the rows of group g, from padded
- * planes (emu_grouped_split_rows) of A (rows x M) and B (rows x N).  D:
- * G matrices M x N of dtype, row pitch ldd, strided elements apart; empty
- * groups write zeros.  With A = X, B = dY this is the gradient of W for
+/* Weight gradient: D_g = A_g^T B_g over the rows of group g, from planes of A
+ * (rows x M) and B (rows x N): apadded / bpadded as in emu_grouped_prodsum, 1
+ * for both when nslices = 3.  D: G matrices M x N of dtype, row pitch ldd,
+ * strided elements apart; empty groups write zeros.  With A = X, B = dY this is the gradient of W for
  * EMU_OP_N, with A = dY, B = X for EMU_OP_T. */
 emu_status emu_grouped_prodsum_wgrad(int nslices, int64_t G, int64_t rows, int64_t M, int64_t N,
-                                     const uint16_t *Acomps, int64_t lda, const uint16_t *Bcomps, int64_t ldb,
-                                     const int32_t *ends, void *D, int dtype, int64_t ldd, int64_t strided, void *ws,
-                                     size_t ws_bytes, emu_stream_t stream);
+                                     const uint16_t *Acomps, int64_t lda, int apadded, const uint16_t *Bcomps,
+                                     int64_t ldb, int bpadded, const int32_t *ends, void *D, int dtype, int64_t ldd,
+                                     int64_t strided, void *ws, size_t ws_bytes, emu_stream_t stream);
 
 /* Matrix-vector products with 4-bit weights and group scales, for one row or a
  * few rows (of each expert):

@@ -70,8 +70,8 @@ _SIGS = {
     "emu_grouped_gemm_workspace_bytes": ("size", ["i", "l", "l", "l", "l"]),
     "emu_grouped_gemm_f32": ("i", ["i", "l", "l", "l", "l", "p", "l", "l", "p", "p", "l", "l", "p", "p", "l", "p",
                                    "size", "p"]),
-    "emu_grouped_prodsum_wgrad": ("i", ["i", "l", "l", "l", "l", "p", "l", "p", "l", "p", "p", "i", "l", "l", "p",
-                                        "size", "p"]),
+    "emu_grouped_prodsum_wgrad": ("i", ["i", "l", "l", "l", "l", "p", "l", "i", "p", "l", "i", "p", "p", "i", "l", "l",
+                                        "p", "size", "p"]),
     "emu_w4_matvec": ("i", ["i", "l", "l", "l", "l", "l", "p", "l", "p", "p", "i", "p", "p", "p", "l", "p"]),
     "emu_route_workspace_bytes": ("size", ["l", "l", "l"]),
     "emu_route": ("i", ["i", "l", "l", "l", "i", "p", "l", "p", "p", "p", "p", "p", "p", "size", "p"]),
@@ -585,6 +585,19 @@ def grouped_gemm(X, W, ends, opW: int = OP_N, src=None, Y=None, ws=None, stream=
     return Y, ws
 
 
+def _token_operand(t, ends, src, ws, stream, where):
+    """(operand, address, row pitch, padded, slices) of token rows: BF16 rows as
+    they stand where the tensor memory accelerator can read them, else planes."""
+    if not isinstance(t, GroupedPlanes):
+        ld = _pitch(t, where)
+        if len(t.shape) == 2 and _dtype(t, where) == BF16 and src is None and _tma_ok(t, ld):
+            return t, t.data_ptr(), ld, 0, 1
+        t = grouped_split(t, ends, src, ws=ws, stream=stream)
+    elif src is not None or not t.padded:
+        _bad(where, "a plane set of token rows, already gathered, is needed")
+    return t, t.planes.data_ptr(), t.ld, 1, t.nslices
+
+
 def grouped_wgrad(A, B, ends, srcA=None, srcB=None, D=None, ws=None, stream=None):
     """D_g = A[srcA]^T B[srcB] over the rows of group g: D [G, M, N].  The
     gradient of W is grouped_wgrad(X, dY) for OP_N and grouped_wgrad(dY, X)
@@ -594,22 +607,20 @@ def grouped_wgrad(A, B, ends, srcA=None, srcB=None, D=None, ws=None, stream=None
     G, dev = ends.numel(), A.device
     if ws is None:
         ws = _empty(emu_split_workspace_bytes(32), torch.uint8, dev, stream)
-    if not isinstance(A, GroupedPlanes):
-        A = grouped_split(A, ends, srcA, ws=ws, stream=stream)
-    if not isinstance(B, GroupedPlanes):
-        B = grouped_split(B, ends, srcB, ws=ws, stream=stream)
-    if not A.padded or not B.padded or A.shape[0] != B.shape[0] or A.nslices != B.nslices or B.device != dev:
+    A, pa, lda, apad, Sa = _token_operand(A, ends, srcA, ws, stream, "grouped_wgrad: A")
+    B, pb, ldb, bpad, Sb = _token_operand(B, ends, srcB, ws, stream, "grouped_wgrad: B")
+    if A.shape[0] != B.shape[0] or Sa != Sb or B.device != dev:
         _bad(where, "A and B have to be token rows, as many and of one type, on one device")
-    (rows, M), N, S = A.shape, B.shape[1], A.nslices
+    (rows, M), N, S = A.shape, B.shape[1], Sa
     if D is None:
         D = _empty((G, M, N), torch.float32 if S == 3 else torch.bfloat16, dev, stream)
     dt, ldd = _dtype(D, "grouped_wgrad: D"), _pitch(D, "grouped_wgrad: D", dev)
     if D.shape != (G, M, N) or (S == 3 and dt != F32):
         _bad(where, "D has another shape or type")
-    r = _lib.emu_grouped_prodsum_wgrad(S, G, rows, M, N, A.planes.data_ptr(), A.ld, B.planes.data_ptr(), B.ld,
-                                         _ints(ends, G, dev, "grouped_wgrad: ends"), D.data_ptr(), dt, ldd,
-                                         D.stride(0) if G > 1 else M * ldd, ws.data_ptr(), ws.numel(),
-                                         _raw_stream(stream, dev))
+    r = _lib.emu_grouped_prodsum_wgrad(S, G, rows, M, N, pa, lda, apad, pb, ldb, bpad,
+                                       _ints(ends, G, dev, "grouped_wgrad: ends"), D.data_ptr(), dt, ldd,
+                                       D.stride(0) if G > 1 else M * ldd, ws.data_ptr(), ws.numel(),
+                                       _raw_stream(stream, dev))
     if r:
         _check(r, "emu_grouped_prodsum_wgrad")
     return D, ws

@@ -1,12 +1,12 @@
-// Matrix products grouped by expert, on tcgen05 BF16 MMAs with FP32
-// accumulators in tensor memory.
+// FP32 matrix products grouped by expert and their weight gradients, on tcgen05
+// BF16 MMAs with FP32 accumulators in tensor memory (BF16 operands:
+// grouped_bf16.cu; few rows for each group: grouped_fused.cu).
 //
 //   product:   Y[r, n]    = sum_k X[r, k] W_g[k, n]   for the rows r of group g
 //   gradient:  D_g[m, n]  = sum over the rows r of group g of A[r, m] B[r, n]
 //
-// Operands are sets of S BF16 planes: S = 3 for FP32 operands (Eq.
-// (fp32split); the six products of Eq. (fp32six) are issued from one stage),
-// S = 1 for BF16 operands, whose plane is the operand itself.
+// Operands are sets of three BF16 planes (Eq. (fp32split)); the six products of
+// Eq. (fp32six) are issued from one stage.
 //
 // Both forms compute tiles of the TRANSPOSED result: the contiguous output
 // dimension n (the weights' features) lies on the 128 MMA rows = TMEM lanes,
@@ -22,10 +22,7 @@
 // issues TMA loads, warp 1 the MMAs, warps 2-9 read TMEM and store.  Every
 // wait is bounded (EMU_FLAG_TIMEOUT).
 //
-// BF16 operands: two accumulators alternate in TMEM, so the stores of one tile
-// overlap the MMAs of the next.
-//
-// FP32 operands: the tensor cores truncate when they add to an FP32
+// The tensor cores truncate when they add to an FP32
 // accumulator, a bias of about 1.8e-8 of the result per 16-wide step; six
 // products over K = 256 in one accumulator came out at 1.7e-6 (2-norm).  So
 // the leading product A0B0 has an accumulator of its own that is read every
@@ -40,9 +37,11 @@ namespace emu {
 
 namespace {
 
+constexpr int S = 3;
+
 // LMN / CMN: the feature / column operand is stored with its MN dimension
 // contiguous (else with the contraction contiguous).  CMN is the gradient.
-template <int S, int BC, bool PAIR, bool LMN, bool CMN>
+template <int BC, bool PAIR, bool LMN, bool CMN>
 __global__ void __launch_bounds__(64 + 32 * kEpiWarps, 1)
 grouped_kernel(const __grid_constant__ CUtensorMap tmL, const __grid_constant__ CUtensorMap tmC,
                const __grid_constant__ CUtensorMap tmS, const GroupedArgs a)
@@ -53,8 +52,8 @@ grouped_kernel(const __grid_constant__ CUtensorMap tmL, const __grid_constant__ 
     const uint32_t base = (raw + 1023u) & ~1023u;
     uint8_t *base_ptr = smem_raw + (base - raw);
     const uint32_t full0 = base + Cfg::BAR_OFF, empty0 = full0 + 8u * Cfg::STAGES;
-    // BF16: tfull / tempty of the two accumulators; FP32: [0] of the leading
-    // accumulator (per chunk), tempty[1] of the other one (per tile)
+    // tfull[0], tempty[0]: the leading accumulator (per chunk); tempty[1]: the
+    // other one (per tile)
     const uint32_t tfull0 = empty0 + 8u * Cfg::STAGES, tempty0 = tfull0 + 16u, done_bar = tempty0 + 16u;
     volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(base_ptr + Cfg::BAR_OFF + 16 * Cfg::STAGES + 48);
     int *starts = reinterpret_cast<int *>(base_ptr + Cfg::TAB_OFF), *tpre = starts + a.G + 1;
@@ -168,7 +167,7 @@ grouped_kernel(const __grid_constant__ CUtensorMap tmL, const __grid_constant__ 
     } else if (warp == 1 && rank == 0) {
         // ---------------- MMA issuer (a pair's leader)
         const uint32_t elected = elect_lane();
-        uint32_t s = 0, ph = 0, it = 0, cph = 0;      // it: tiles with a contraction, cph: chunks issued (FP32)
+        uint32_t s = 0, ph = 0, it = 0, cph = 0;      // it: tiles with a contraction, cph: chunks issued
         bool ok = true;
         constexpr int kstepL = LMN ? 2048 : 32, kstepC = CMN ? 2048 : 32;
         constexpr uint64_t descL = group_desc(LMN ? 64u * kKB * 2u : 16u), descC = group_desc(CMN ? 64u * kKB * 2u : 16u);
@@ -176,13 +175,11 @@ grouped_kernel(const __grid_constant__ CUtensorMap tmL, const __grid_constant__ 
             const Tile x = tile_at<S, BC, PAIR, LMN, CMN>(t, a, starts, tpre, rank);
             const int nk = uniform(x.nk), nkb = (nk + kKB - 1) / kKB;
             if (nkb == 0) continue;                   // an empty group: the epilogue writes zeros by itself
-            const uint32_t b = it & 1u, csz = (uint32_t)uniform(x.csz);
+            const uint32_t csz = (uint32_t)uniform(x.csz);
             const uint32_t idesc = make_idesc_bf16(kLRows * Cfg::CTAS, 0) | csz >> 3 << 17 | (LMN ? 1u << 15 : 0u) |
                                    (CMN ? 1u << 16 : 0u);
-            const uint32_t d = tmem + (S == 1 ? b * 256u : 0u), d2 = tmem + 256u;
-            if (S == 1) ok = warp_wait(tempty0 + 8u * b, ((it >> 1) & 1u) ^ 1u, flags);
-            else ok = warp_wait(tempty0 + 8u, (it & 1u) ^ 1u, flags);
-            if (!ok) break;
+            const uint32_t d = tmem, d2 = tmem + 256u;
+            if (!(ok = warp_wait(tempty0 + 8u, (it & 1u) ^ 1u, flags))) break;
             ++it;
             tc_fence_after();
             for (int kb = 0; kb < nkb; ++kb) {
@@ -196,36 +193,28 @@ grouped_kernel(const __grid_constant__ CUtensorMap tmL, const __grid_constant__ 
                                       descC + (st + (uint32_t)((S * Cfg::L_TILE + ic * Cfg::C_TILE + kk * kstepC) >> 4)), idesc,
                                       add);
                 };
-                if constexpr (S == 3) {
-                    const int kc = kb % kChunkBlocks;
+                const int kc = kb % kChunkBlocks;
 #pragma unroll
-                    for (int kk = 0; kk < kKB / 16; ++kk) {
-                        if (16 * kk < left) {
-                            mma(d2, 1, 1, kk, (kb | kk) != 0);
-                            mma(d2, 1, 0, kk, true);
-                            mma(d2, 2, 0, kk, true);
-                            mma(d2, 0, 2, kk, true);
-                            mma(d2, 0, 1, kk, true);
-                        }
+                for (int kk = 0; kk < kKB / 16; ++kk) {
+                    if (16 * kk < left) {
+                        mma(d2, 1, 1, kk, (kb | kk) != 0);
+                        mma(d2, 1, 0, kk, true);
+                        mma(d2, 2, 0, kk, true);
+                        mma(d2, 0, 2, kk, true);
+                        mma(d2, 0, 1, kk, true);
                     }
-                    if (kc == 0) {                    // the last chunk's leading sum has been read
-                        if (!(ok = warp_wait(tempty0, (cph & 1u) ^ 1u, flags))) break;
-                        tc_fence_after();
-                    }
-#pragma unroll
-                    for (int kk = 0; kk < kKB / 16; ++kk)
-                        if (16 * kk < left) mma(d, 0, 0, kk, (kc | kk) != 0);
-                    commit_elected<PAIR>(elected, empty0 + 8u * s);
-                    if (kc == kChunkBlocks - 1 || kb == nkb - 1) { commit_elected<PAIR>(elected, tfull0); ++cph; }
-                } else {
-#pragma unroll
-                    for (int kk = 0; kk < kKB / 16; ++kk)
-                        if (16 * kk < left) mma(d, 0, 0, kk, (kb | kk) != 0);
-                    commit_elected<PAIR>(elected, empty0 + 8u * s);
                 }
+                if (kc == 0) {                    // the last chunk's leading sum has been read
+                    if (!(ok = warp_wait(tempty0, (cph & 1u) ^ 1u, flags))) break;
+                    tc_fence_after();
+                }
+#pragma unroll
+                for (int kk = 0; kk < kKB / 16; ++kk)
+                    if (16 * kk < left) mma(d, 0, 0, kk, (kc | kk) != 0);
+                commit_elected<PAIR>(elected, empty0 + 8u * s);
+                if (kc == kChunkBlocks - 1 || kb == nkb - 1) { commit_elected<PAIR>(elected, tfull0); ++cph; }
                 if (++s == Cfg::STAGES) { s = 0; ph ^= 1u; }
             }
-            if (ok && S == 1) commit_elected<PAIR>(elected, tfull0 + 8u * b);
         }
         commit_elected<PAIR>(elected, done_bar);
         (void)mbar_wait(done_bar, 0, flags);
@@ -252,7 +241,7 @@ grouped_kernel(const __grid_constant__ CUtensorMap tmL, const __grid_constant__ 
         bool ok = true;
         for (int t = first; t < total && ok; t += step, ++it) {
             const Tile x = tile_at<S, BC, PAIR, LMN, CMN>(t, a, starts, tpre, rank);
-            const int l = x.l0 + quarter * 32, b = it & 1;
+            const int l = x.l0 + quarter * 32;
             const int cols = x.cols - h0;             // columns from this warp's first on
             const int64_t row0 = (CMN ? 0 : (int64_t)starts[x.g]) + x.c0 + h0;
             char *o = static_cast<char *>(a.out) + (row0 * a.ldo + (CMN ? x.g * a.strideo : 0)) * esize;
@@ -267,56 +256,37 @@ grouped_kernel(const __grid_constant__ CUtensorMap tmL, const __grid_constant__ 
                 continue;
             }
             // tcgen05.ld needs the whole warp, so a timeout in any lane ends the warp's work
-            if constexpr (S == 3) {
-                float acc[Cfg::HALF];
+            float acc[Cfg::HALF];
 #pragma unroll
-                for (int j = 0; j < Cfg::HALF; ++j) acc[j] = 0.0f;
-                const int nch = (x.nk + kKChunk - 1) / kKChunk;
-                for (int c = 0; c <= nch; ++c) {      // the chunks' leading sums, then the other products
-                    if (c < nch) {
-                        ok = __all_sync(0xFFFFFFFFu, mbar_wait(tfull0, cph & 1u, flags));
-                        if (!ok) break;
-                        ++cph;
-                        tc_fence_after();
-                    }
-#pragma unroll
-                    for (int h = 0; h < Cfg::HALF; h += 16) {
-                        if (h < cols) {
-                            uint32_t v[16];
-                            tmem_load16(lanes + (uint32_t)(c < nch ? h : 256 + h), v);
-                            tmem_ld_wait();
-#pragma unroll
-                            for (int j = 0; j < 16; ++j) acc[h + j] = __fadd_rn(acc[h + j], __uint_as_float(v[j]));
-                        }
-                    }
-                    release(c < nch ? tempty0 : tempty0 + 8u);
+            for (int j = 0; j < Cfg::HALF; ++j) acc[j] = 0.0f;
+            const int nch = (x.nk + kKChunk - 1) / kKChunk;
+            for (int c = 0; c <= nch; ++c) {      // the chunks' leading sums, then the other products
+                if (c < nch) {
+                    ok = __all_sync(0xFFFFFFFFu, mbar_wait(tfull0, cph & 1u, flags));
+                    if (!ok) break;
+                    ++cph;
+                    tc_fence_after();
                 }
-                if (ok) {
 #pragma unroll
-                    for (int h = 0; h < Cfg::HALF; h += 32) {
-                        float v[32];
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] = acc[h + j];
-                        store32(v, h);
-                    }
-                }
-            } else {
-                ok = __all_sync(0xFFFFFFFFu, mbar_wait(tfull0 + 8u * b, ((uint32_t)it >> 1) & 1u, flags));
-                if (!ok) break;
-                tc_fence_after();
-#pragma unroll 1
-                for (int h = 0; h < Cfg::HALF; h += 32) {
+                for (int h = 0; h < Cfg::HALF; h += 16) {
                     if (h < cols) {
-                        uint32_t u[32];
-                        float v[32];
-                        tmem_ld32(lanes + (uint32_t)(b * 256 + h), u);
+                        uint32_t v[16];
+                        tmem_load16(lanes + (uint32_t)(c < nch ? h : 256 + h), v);
                         tmem_ld_wait();
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(u[j]);
-                        store32(v, h);
+                        for (int j = 0; j < 16; ++j) acc[h + j] = __fadd_rn(acc[h + j], __uint_as_float(v[j]));
                     }
                 }
-                release(tempty0 + 8u * b);
+                release(c < nch ? tempty0 : tempty0 + 8u);
+            }
+            if (ok) {
+#pragma unroll
+                for (int h = 0; h < Cfg::HALF; h += 32) {
+                    float v[32];
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) v[j] = acc[h + j];
+                    store32(v, h);
+                }
             }
         }
     }
@@ -332,36 +302,15 @@ grouped_kernel(const __grid_constant__ CUtensorMap tmL, const __grid_constant__ 
     }
 }
 
-template <int S, int BC, bool PAIR, bool LMN, bool CMN>
+template <int BC, bool PAIR, bool LMN, bool CMN>
 cudaError_t run_grouped(const CUtensorMap &tl, const CUtensorMap &tc, const CUtensorMap &ts, const GroupedArgs &a,
                         int64_t tiles, cudaStream_t st)
 {
     using Cfg = GroupedCfg<S, BC, PAIR>;
-    auto kern = grouped_kernel<S, BC, PAIR, LMN, CMN>;
-    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::SMEM);
-    if (e != cudaSuccess) return e;
-    int64_t units = sm_count() / Cfg::CTAS;
-    if (units > tiles) units = tiles < 1 ? 1 : tiles;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(units * Cfg::CTAS));
-    cfg.blockDim = dim3(Cfg::THREADS);
-    cfg.dynamicSmemBytes = Cfg::SMEM;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = Cfg::CTAS;
-    attr[1].val.clusterDim.y = 1;
-    attr[1].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = PAIR ? 2 : 1;
-    e = cudaLaunchKernelEx(&cfg, kern, tl, tc, ts, a);
-    if (e != cudaSuccess) return e;
-    return cudaGetLastError();
+    return launch_persistent(grouped_kernel<BC, PAIR, LMN, CMN>, Cfg::SMEM, Cfg::THREADS, Cfg::CTAS, tiles, st, tl, tc, ts, a);
 }
 
-template <int S, bool LMN>
+template <bool LMN>
 cudaError_t product(const GroupedOperand &X, const GroupedOperand &W, GroupedArgs a, cudaStream_t st)
 {
     CUtensorMap tl, tc, ts;
@@ -372,41 +321,40 @@ cudaError_t product(const GroupedOperand &X, const GroupedOperand &W, GroupedArg
         return cudaErrorInvalidValue;
     const int64_t each = a.rows / a.G;            // rows of a group on average
     if (each >= 128)
-        return run_grouped<S, 256, true, LMN, false>(tl, tc, ts, a, max_tiles(a.rows, a.G, a.L, 256, 2), st);
-    return run_grouped<S, 64, false, LMN, false>(tl, tc, ts, a, max_tiles(a.rows, a.G, a.L, 64, 1), st);
+        return run_grouped<256, true, LMN, false>(tl, tc, ts, a, max_tiles(a.rows, a.G, a.L, 256, 2), st);
+    return run_grouped<64, false, LMN, false>(tl, tc, ts, a, max_tiles(a.rows, a.G, a.L, 64, 1), st);
 }
 
-template <int S>
 cudaError_t gradient(const GroupedOperand &A, const GroupedOperand &B, GroupedArgs a, cudaStream_t st)
 {
     CUtensorMap tl, tc;
     if (!make_group_map(&tl, B.planes, a.L, B.rows, 1, S, B.ld, 0, B.plane, kKB, &a.lwide) ||
-        !make_group_map(&tc, A.planes, a.C, A.rows, 1, S, A.ld, 0, A.plane, kKB, &a.cwide, 256))
+        !make_group_map(&tc, A.planes, a.C, A.rows, 1, S, A.ld, 0, A.plane, kKB, &a.cwide, a.C <= 128 ? 128 : 256))
         return cudaErrorInvalidValue;
-    return run_grouped<S, 256, true, true, true>(tl, tc, tc, a, (int64_t)a.G * ((a.L + 255) / 256) * ((a.C + 255) / 256), st);
+    return run_grouped<256, true, true, true>(tl, tc, tc, a, (int64_t)a.G * ((a.L + 255) / 256) * ((a.C + 255) / 256), st);
 }
 
 }  // namespace
 
-cudaError_t launch_grouped_product(int S, bool trans, int64_t G, int64_t rows, int64_t N, int64_t K,
+cudaError_t launch_grouped_product(int nslices, bool trans, int64_t G, int64_t rows, int64_t N, int64_t K,
                                    const GroupedOperand &X, const GroupedOperand &W, const int32_t *ends, void *Y,
                                    bool y_f32, int64_t ldy, uint32_t *flags, cudaStream_t st)
 {
     GroupedArgs a = {};
     a.ends = ends; a.G = (int)G; a.rows = (int)rows; a.L = (int)N; a.K = (int)K; a.padded = X.padded ? 1 : 0;
     a.out = Y; a.ldo = ldy; a.out_f32 = y_f32 ? 1 : 0; a.flags = flags;
-    if (S == 3) return trans ? product<3, false>(X, W, a, st) : product<3, true>(X, W, a, st);
-    return trans ? product<1, false>(X, W, a, st) : product<1, true>(X, W, a, st);
+    if (nslices == 1) return launch_bf16_product(trans, X, W, a, st);
+    return trans ? product<false>(X, W, a, st) : product<true>(X, W, a, st);
 }
 
-cudaError_t launch_grouped_gradient(int S, int64_t G, int64_t rows, int64_t M, int64_t N, const GroupedOperand &A,
+cudaError_t launch_grouped_gradient(int nslices, int64_t G, int64_t rows, int64_t M, int64_t N, const GroupedOperand &A,
                                     const GroupedOperand &B, const int32_t *ends, void *D, bool d_f32, int64_t ldd,
                                     int64_t strided, uint32_t *flags, cudaStream_t st)
 {
     GroupedArgs a = {};
     a.ends = ends; a.G = (int)G; a.rows = (int)rows; a.L = (int)N; a.C = (int)M;
     a.out = D; a.ldo = ldd; a.strideo = strided; a.out_f32 = d_f32 ? 1 : 0; a.flags = flags;
-    return S == 3 ? gradient<3>(A, B, a, st) : gradient<1>(A, B, a, st);
+    return nslices == 1 ? launch_bf16_gradient(A, B, a, st) : gradient(A, B, a, st);
 }
 
 }  // namespace emu

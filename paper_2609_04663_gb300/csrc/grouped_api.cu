@@ -201,11 +201,11 @@ emu_status emu_grouped_gemm_f32(int opW, int64_t G, int64_t rows, int64_t N, int
 }
 
 emu_status emu_grouped_prodsum_wgrad(int nslices, int64_t G, int64_t rows, int64_t M, int64_t N,
-                                     const uint16_t *Acomps, int64_t lda, const uint16_t *Bcomps, int64_t ldb,
-                                     const int32_t *ends, void *D, int dtype, int64_t ldd, int64_t strided, void *ws,
-                                     size_t ws_bytes, emu_stream_t stream)
+                                     const uint16_t *Acomps, int64_t lda, int apadded, const uint16_t *Bcomps,
+                                     int64_t ldb, int bpadded, const int32_t *ends, void *D, int dtype, int64_t ldd,
+                                     int64_t strided, void *ws, size_t ws_bytes, emu_stream_t stream)
 {
-    if ((nslices != 1 && nslices != 3) || !known(dtype) || ldd < N || (G > 1 && strided < M * ldd))
+    if ((nslices != 1 && nslices != 3) || (nslices == 3 && (!apadded || !bpadded)) || !known(dtype) || ldd < N || (G > 1 && strided < M * ldd))
         return EMU_ERR_INVALID_ARG;
     emu_status s = check_sizes(G, rows, M, N);
     if (s != EMU_OK) return s;
@@ -233,8 +233,10 @@ emu_status emu_grouped_prodsum_wgrad(int nslices, int64_t G, int64_t rows, int64
         return EMU_OK;
     }
     GroupedOperand A, B;
-    A.planes = Acomps; A.rows = padded_rows(rows, G); A.ld = lda; A.plane = A.rows * lda; A.padded = true;
-    B.planes = Bcomps; B.rows = A.rows; B.ld = ldb; B.plane = B.rows * ldb; B.padded = true;
+    A.planes = Acomps; A.padded = apadded != 0; A.rows = apadded ? padded_rows(rows, G) : rows; A.ld = lda;
+    A.plane = A.rows * lda;
+    B.planes = Bcomps; B.padded = bpadded != 0; B.rows = bpadded ? padded_rows(rows, G) : rows; B.ld = ldb;
+    B.plane = B.rows * ldb;
     return cuda_status(launch_grouped_gradient(nslices, G, rows, M, N, A, B, ends, D, dtype == EMU_F32, ldd, strided,
                                                &static_cast<WsHeader *>(ws)->flags, st));
 }

@@ -293,24 +293,7 @@ cudaError_t run_fused(const CUtensorMap &tw, const CUtensorMap &tc, const CUtens
                       int64_t tiles, cudaStream_t st)
 {
     using Cfg = FusedCfg<COLS>;
-    auto kern = grouped_fused_kernel<COLS, LMN>;
-    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::SMEM);
-    if (e != cudaSuccess) return e;
-    int64_t units = sm_count();
-    if (units > tiles) units = tiles < 1 ? 1 : tiles;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)units);
-    cfg.blockDim = dim3(Cfg::THREADS);
-    cfg.dynamicSmemBytes = Cfg::SMEM;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    e = cudaLaunchKernelEx(&cfg, kern, tw, tc, ts, a);
-    if (e != cudaSuccess) return e;
-    return cudaGetLastError();
+    return launch_persistent(grouped_fused_kernel<COLS, LMN>, Cfg::SMEM, Cfg::THREADS, 1, tiles, st, tw, tc, ts, a);
 }
 
 // Tensor map over G FP32 matrices of rows x inner, box box_inner x box_rows.

@@ -12,6 +12,24 @@
 
 namespace emu {
 
+struct GroupedArgs {
+    const int32_t *ends;
+    int G, rows;
+    int L;                 // output features (the lane dimension)
+    int C;                 // gradient: output rows m
+    int K;                 // product: contraction length
+    int padded, lpadded;   // rows at padded positions: X or the gradient's A, the gradient's B
+    void *out;
+    int64_t ldo, strideo;  // row pitch; gradient: distance between the groups' results
+    int out_f32;
+    int lwide, cwide;      // the MN-major operand's tensor map loads two blocks of 64 at once
+    uint32_t *flags;
+};
+
+// BF16 operands (grouped_bf16.cu).
+cudaError_t launch_bf16_product(bool trans, const GroupedOperand &X, const GroupedOperand &W, const GroupedArgs &a, cudaStream_t st);
+cudaError_t launch_bf16_gradient(const GroupedOperand &A, const GroupedOperand &B, GroupedArgs a, cudaStream_t st);
+
 namespace {
 
 constexpr int kLRows = 128;           // MMA rows (output features) per CTA
@@ -20,20 +38,6 @@ constexpr int kSmemMax = 232448;      // shared memory per CTA
 
 constexpr int kChunkBlocks = kKChunk / kKB;   // K-blocks of one chunk of the leading product
 constexpr int kEpiWarps = 8;
-
-struct GroupedArgs {
-    const int32_t *ends;
-    int G, rows;
-    int L;                 // output features (the lane dimension)
-    int C;                 // gradient: output rows m
-    int K;                 // product: contraction length
-    int padded;            // product: X's rows are at padded positions
-    void *out;
-    int64_t ldo, strideo;  // row pitch; gradient: distance between the groups' results
-    int out_f32;
-    int lwide, cwide;      // the MN-major operand's tensor map loads two blocks of 64 at once
-    uint32_t *flags;
-};
 
 // S slices, BC MMA columns at most, PAIR: a tile's 256 features on two CTAs.
 template <int S, int BC, bool PAIR>
@@ -197,13 +201,17 @@ __device__ __forceinline__ Tile tile_at(int t, const GroupedArgs &a, const int *
     return x;
 }
 
+__device__ __forceinline__ float as_float(float x) { return x; }
+__device__ __forceinline__ float as_float(uint32_t x) { return __uint_as_float(x); }
+
 // 32 accumulator columns of this warp's lanes -> rows 0 .. cols - 1 of out:
 // column j is output row j, lane i feature l + i.  BF16: two columns at a
 // time, neighbouring lanes exchange values so that each stores two features
 // of one row.  The usual case (32 whole columns, 32 features, pairs that can be
 // stored as words) has no test per element: these instructions, not the
 // stores' bandwidth, are what the epilogue takes.
-__device__ __forceinline__ void store_columns(const float (&v)[32], int cols, void *out, int64_t ldo, int l, int L,
+template <typename T>
+__device__ __forceinline__ void store_columns(const T (&v)[32], int cols, void *out, int64_t ldo, int l, int L,
                                               bool out_f32, bool pairs_ok)
 {
     const int lane = (int)lane_id();
@@ -212,11 +220,11 @@ __device__ __forceinline__ void store_columns(const float (&v)[32], int cols, vo
         float *o = static_cast<float *>(out) + l + lane;
         if (whole) {
 #pragma unroll
-            for (int j = 0; j < 32; ++j, o += ldo) *o = v[j];
+            for (int j = 0; j < 32; ++j, o += ldo) *o = as_float(v[j]);
         } else {
 #pragma unroll
             for (int j = 0; j < 32; ++j)
-                if (l + lane < L && j < cols) o[(int64_t)j * ldo] = v[j];
+                if (l + lane < L && j < cols) o[(int64_t)j * ldo] = as_float(v[j]);
         }
     } else {
         const bool odd = lane & 1;
@@ -225,8 +233,8 @@ __device__ __forceinline__ void store_columns(const float (&v)[32], int cols, vo
         uint32_t w[16];                               // features i (low half) and i + 1 of row 2 j + odd
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
-            const float keep = odd ? v[2 * j + 1] : v[2 * j];
-            const float got = __shfl_xor_sync(0xFFFFFFFFu, odd ? v[2 * j] : v[2 * j + 1], 1);
+            const float keep = as_float(odd ? v[2 * j + 1] : v[2 * j]);
+            const float got = __shfl_xor_sync(0xFFFFFFFFu, as_float(odd ? v[2 * j] : v[2 * j + 1]), 1);
             asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[j]) : "f"(odd ? keep : got), "f"(odd ? got : keep));
         }
         if (whole && pairs_ok) {
@@ -317,6 +325,34 @@ int sm_count()
         cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sms < 2)
         sms = 152;
     return sms;
+}
+
+// A persistent launch: one CTA (or cluster of `ctas`) per SM (pair), no more
+// than there are tiles, as a programmatic dependent of the kernel before it.
+template <typename Kernel, typename... Args>
+cudaError_t launch_persistent(Kernel kern, int smem, int threads, int ctas, int64_t tiles, cudaStream_t st, const Args &...args)
+{
+    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+    int64_t units = sm_count() / ctas;
+    if (units > tiles) units = tiles < 1 ? 1 : tiles;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(units * ctas));
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = (size_t)smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)ctas;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = ctas > 1 ? 2 : 1;
+    e = cudaLaunchKernelEx(&cfg, kern, args...);
+    if (e != cudaSuccess) return e;
+    return cudaGetLastError();
 }
 
 // Tiles at most (the host does not know the groups' sizes): every group may

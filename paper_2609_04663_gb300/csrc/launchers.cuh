@@ -139,14 +139,14 @@ cudaError_t launch_axpby_f64(const double *P, int64_t ldp, double *C, int64_t ld
 struct GroupedOperand {
     const uint16_t *planes = nullptr;
     int64_t rows = 0, ld = 0, stride = 0, plane = 0;
-    bool padded = false;
+    bool padded = false;       // (three planes of a gradient's operands: always)
 };
 cudaError_t launch_grouped_split(bool f32, int64_t G, int64_t rows, int64_t cols, const void *X, int64_t ldx,
                                  int64_t stride, uint16_t *comps, int64_t ldcomp, uint32_t *flags, cudaStream_t st);
 cudaError_t launch_grouped_split_rows(bool f32, int64_t rows, int64_t cols, const void *X, int64_t xrows,
                                       int64_t ldx, const int32_t *src, const int32_t *ends, int64_t G,
                                       uint16_t *comps, int64_t ldcomp, uint32_t *flags, cudaStream_t st);
-cudaError_t launch_grouped_product(int S, bool trans, int64_t G, int64_t rows, int64_t N, int64_t K,
+cudaError_t launch_grouped_product(int nslices, bool trans, int64_t G, int64_t rows, int64_t N, int64_t K,
                                    const GroupedOperand &X, const GroupedOperand &W, const int32_t *ends, void *Y,
                                    bool y_f32, int64_t ldy, uint32_t *flags, cudaStream_t st);
 // FP32 weights that meet few rows each, split inside the product
@@ -157,7 +157,7 @@ cudaError_t launch_grouped_fused(bool trans, int64_t G, int64_t rows, int64_t N,
                                  const float *W, int64_t ldw, int64_t stridew, const int32_t *ends, float *Y,
                                  int64_t ldy, uint32_t *flags, cudaStream_t st);
 constexpr int64_t kFusedRows = 127;
-cudaError_t launch_grouped_gradient(int S, int64_t G, int64_t rows, int64_t M, int64_t N, const GroupedOperand &A,
+cudaError_t launch_grouped_gradient(int nslices, int64_t G, int64_t rows, int64_t M, int64_t N, const GroupedOperand &A,
                                     const GroupedOperand &B, const int32_t *ends, void *D, bool d_f32, int64_t ldd,
                                     int64_t strided, uint32_t *flags, cudaStream_t st);
 

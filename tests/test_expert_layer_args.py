@@ -30,8 +30,9 @@ def test_argument_checks_need_no_gpu(lib):
     assert g(1, 0, 1025, 8, 8, 8, P, 8, 0, P, 8, 64, P, P, 0, 8, P, 512, None) == 5   # groups
     assert emu.emu_grouped_gemm_f32(0, 2, 8, 8, 8, P, 4, 8, None, P, 8, 64, P, P, 8, P, big, None) == 1   # xrows < rows
     assert emu.emu_grouped_gemm_f32(0, 2, 8, 8, 8, P, 8, 8, None, P, 8, 64, P, P, 8, P, 512, None) == 3
-    assert emu.emu_grouped_prodsum_wgrad(1, 2, 8, 8, 8, P, 8, P, 8, P, P, 0, 8, 63, P, 512, None) == 1    # matrices overlap
-    assert emu.emu_grouped_prodsum_wgrad(1, 2, 8, 8, 8, P, 12, P, 8, P, P, 0, 8, 64, P, 512, None) == 2
+    assert emu.emu_grouped_prodsum_wgrad(1, 2, 8, 8, 8, P, 8, 0, P, 8, 0, P, P, 0, 8, 63, P, 512, None) == 1    # matrices overlap
+    assert emu.emu_grouped_prodsum_wgrad(1, 2, 8, 8, 8, P, 12, 0, P, 8, 0, P, P, 0, 8, 64, P, 512, None) == 2
+    assert emu.emu_grouped_prodsum_wgrad(3, 2, 8, 8, 8, P, 8, 1, P, 8, 0, P, P, 0, 8, 64, P, 512, None) == 1    # slices at padded rows only
     assert emu.emu_grouped_split(2, 2, 8, 8, P, 8, 64, P, 8, P, 512, None) == 1                          # type
     assert emu.emu_grouped_split(0, 2, 8, 9, P, 9, 72, P, 12, P, 512, None) == 2                         # plane pitch
     assert emu.emu_grouped_split_rows(0, 8, 8, P, 7, 8, None, P, 2, P, 8, P, 512, None) == 1
