@@ -310,6 +310,21 @@ cudaError_t run_grouped(const CUtensorMap &tl, const CUtensorMap &tc, const CUte
     return launch_persistent(grouped_kernel<BC, PAIR, LMN, CMN>, Cfg::SMEM, Cfg::THREADS, Cfg::CTAS, tiles, st, tl, tc, ts, a);
 }
 
+// Whether 256 x 256 tiles on CTA pairs are estimated faster than 128 x 64 tiles
+// for G results of n columns x L features.  A K-block takes a pair 12 clocks
+// per MMA column (the products' time) and a single CTA about 1000 (a 128-row
+// MMA no less than 41 clocks, whatever its columns): the pair is a quarter
+// faster per SM where the tiles fill the GPU, and 4 times longer where one
+// wave holds them all (7 groups of 219 rows, 333 x 517: product 23 us on pairs).
+bool pairs_win(int64_t n, int64_t L, int64_t G)
+{
+    auto waves = [](int64_t tiles, int64_t units) { return (tiles + units - 1) / units; };
+    const int64_t nct = (n + 255) / 256, cols = (n + nct - 1) / nct, sms = sm_count();
+    const int64_t pair = waves(G * nct * ((L + 255) / 256), sms / 2) * 12 * (cols < 128 ? 128 : cols);
+    const int64_t one = waves(G * ((n + 63) / 64) * ((L + 127) / 128), sms) * 1000;
+    return pair <= one;
+}
+
 template <bool LMN>
 cudaError_t product(const GroupedOperand &X, const GroupedOperand &W, GroupedArgs a, cudaStream_t st)
 {
@@ -319,8 +334,8 @@ cudaError_t product(const GroupedOperand &X, const GroupedOperand &W, GroupedArg
     if (!ok || !make_group_map(&tc, X.planes, a.K, X.rows, 1, S, X.ld, 0, X.plane, 64) ||
         !make_group_map(&ts, X.planes, a.K, X.rows, 1, S, X.ld, 0, X.plane, 16))
         return cudaErrorInvalidValue;
-    const int64_t each = a.rows / a.G;            // rows of a group on average
-    if (each >= 128)
+    const int64_t each = (a.rows + a.G - 1) / a.G;    // rows of a group on average
+    if (pairs_win(each, a.L, a.G))
         return run_grouped<256, true, LMN, false>(tl, tc, ts, a, max_tiles(a.rows, a.G, a.L, 256, 2), st);
     return run_grouped<64, false, LMN, false>(tl, tc, ts, a, max_tiles(a.rows, a.G, a.L, 64, 1), st);
 }
@@ -331,7 +346,11 @@ cudaError_t gradient(const GroupedOperand &A, const GroupedOperand &B, GroupedAr
     if (!make_group_map(&tl, B.planes, a.L, B.rows, 1, S, B.ld, 0, B.plane, kKB, &a.lwide) ||
         !make_group_map(&tc, A.planes, a.C, A.rows, 1, S, A.ld, 0, A.plane, kKB, &a.cwide, a.C <= 128 ? 128 : 256))
         return cudaErrorInvalidValue;
-    return run_grouped<256, true, true, true>(tl, tc, tc, a, (int64_t)a.G * ((a.L + 255) / 256) * ((a.C + 255) / 256), st);
+    if (pairs_win(a.C, a.L, a.G))
+        return run_grouped<256, true, true, true>(tl, tc, tc, a, (int64_t)a.G * ((a.L + 255) / 256) * ((a.C + 255) / 256), st);
+    // (a 64-column tile is one block: the map must not load two)
+    if (!make_group_map(&tc, A.planes, a.C, A.rows, 1, S, A.ld, 0, A.plane, kKB, &a.cwide, 1 << 30)) return cudaErrorInvalidValue;
+    return run_grouped<64, false, true, true>(tl, tc, tc, a, (int64_t)a.G * ((a.L + 127) / 128) * ((a.C + 63) / 64), st);
 }
 
 }  // namespace

@@ -283,11 +283,9 @@ emu_status emu_route(int dtype, int64_t T, int64_t E, int64_t k, int renorm, con
     if (s != EMU_OK) return s;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     WsHeader *h = static_cast<WsHeader *>(ws);
-    cudaError_t e = cudaMemsetAsync(h, 0, 2 * sizeof(uint32_t), st);       // the flag word and the barrier's count
-    if (e == cudaSuccess)
-        e = launch_route(T, E, (int)k, renorm != 0, logits, dtype == EMU_F32, ldl, weights, experts, slots, rows, ends,
-                         reinterpret_cast<int32_t *>(static_cast<char *>(ws) + kWsHeaderBytes), h, st);
-    return cuda_status(e);
+    return cuda_status(launch_route(T, E, (int)k, renorm != 0, logits, dtype == EMU_F32, ldl, weights, experts, slots,
+                                    rows, ends, reinterpret_cast<int32_t *>(static_cast<char *>(ws) + kWsHeaderBytes),
+                                    h, st));
 }
 
 emu_status emu_route_backward(int dtype, int64_t T, int64_t E, int64_t k, int renorm, const void *logits, int64_t ldl,

@@ -403,6 +403,21 @@ cudaError_t run_bf16(const CUtensorMap &tl, const CUtensorMap &tc, const CUtenso
                              Cfg::CTAS, tiles, st, tl, tc, ts, a);
 }
 
+// Columns of the tiles for G results of n columns x L features on average: pairs
+// with 512 or 256, or single CTAs with 64, by waves times the clocks of a
+// K-block (measured about 1050, 750 and 530).  64 uneven groups of 512 rows, 2048
+// x 4096: 423 us with 512, 497 with 256; 32 groups of 256 rows: 120 and 109; of
+// 64: 91 with 64.
+int columns_for(int64_t n, int64_t L, int64_t G)
+{
+    auto waves = [](int64_t tiles, int64_t units) { return (tiles + units - 1) / units; };
+    const int64_t sms = sm_count(), lp = (L + 255) / 256;
+    const int64_t t512 = waves(G * ((n + 511) / 512) * lp, sms / 2) * (n > 256 ? 1050 : 820);
+    const int64_t t256 = waves(G * ((n + 255) / 256) * lp, sms / 2) * 750;
+    const int64_t t64 = waves(G * ((n + 63) / 64) * ((L + 127) / 128), sms) * 530;
+    return t64 <= t256 && t64 <= t512 ? 64 : t256 <= t512 ? 256 : 512;
+}
+
 template <bool LMN>
 cudaError_t product(const GroupedOperand &X, const GroupedOperand &W, GroupedArgs a, cudaStream_t st)
 {
@@ -412,14 +427,10 @@ cudaError_t product(const GroupedOperand &X, const GroupedOperand &W, GroupedArg
     if (!ok || !make_group_map(&tc, X.planes, a.K, X.rows, 1, 1, X.ld, 0, X.plane, 64) ||
         !make_group_map(&ts, X.planes, a.K, X.rows, 1, 1, X.ld, 0, X.plane, 16))
         return cudaErrorInvalidValue;
-    const int64_t each = a.rows / a.G;            // rows of a group on average
-    // 512 columns where groups fill them (64 uneven groups of 512 rows, 2048 x
-    // 4096: 423 us against 497 with 256), 256 with a longer ring below (32 groups
-    // of 256 rows: 109 us against 120), one CTA per tile for few rows (of 128: 99
-    // us against 109; of 64: 91 us)
-    if (each > 256)
+    const int bc = columns_for((a.rows + a.G - 1) / a.G, a.L, a.G);
+    if (bc == 512)
         return run_bf16<512, true, LMN, false>(tl, tc, ts, a, max_tiles(a.rows, a.G, a.L, 512, 2), st);
-    if (each >= 128)
+    if (bc == 256)
         return run_bf16<256, true, LMN, false>(tl, tc, ts, a, max_tiles(a.rows, a.G, a.L, 256, 2), st);
     return run_bf16<64, false, LMN, false>(tl, tc, ts, a, max_tiles(a.rows, a.G, a.L, 64, 1), st);
 }
@@ -439,6 +450,8 @@ cudaError_t launch_bf16_gradient(const GroupedOperand &A, const GroupedOperand &
         return cudaErrorInvalidValue;
     a.lpadded = B.padded;
     a.padded = A.padded;
+    // (512 columns: 547 us for 64 groups of 512 rows, 2048 x 4096, against 495; a
+    // short contraction does not hide the reading of two halves)
     return run_bf16<256, true, true, true>(tl, tc, tc, a, (int64_t)a.G * ((a.L + 255) / 256) * ((a.C + 255) / 256), st);
 }
 

@@ -191,7 +191,15 @@ __global__ void __launch_bounds__(kRouteThreads) route_kernel(const RouteArgs a)
             a.experts[(int64_t)t * a.k + lane] = chosen;
         }
     }
-    if (__any_sync(0xFFFFFFFFu, odd) && lane == 0) atomicOr(a.flags, (uint32_t)EMU_FLAG_NONFINITE);
+    if (gridDim.x == 1) {                                 // the only block: it sets the flag word
+        if (__syncthreads_or(odd ? 1 : 0)) {
+            if (threadIdx.x == 0) *a.flags = (uint32_t)EMU_FLAG_NONFINITE;
+        } else if (threadIdx.x == 0) {
+            *a.flags = 0u;
+        }
+    } else if (__any_sync(0xFFFFFFFFu, odd) && lane == 0) {
+        atomicOr(a.flags, (uint32_t)EMU_FLAG_NONFINITE);
+    }
 
     // ---- assignments per warp (a contiguous range each) and expert
     for (int i = threadIdx.x; i < kRouteWarps * a.E; i += kRouteThreads) hist[i] = 0;
@@ -287,12 +295,40 @@ struct RouteBackArgs {
     int T, E, k, f32, renorm;
 };
 
+// V consecutive values of a row from V * lane on, as floats; NaN as minus
+// infinity, past the end too.  VEC: rows allow one load per lane.
+template <int V, bool VEC>
+__device__ __forceinline__ void load_row(const char *row, int lane, int E, bool f32, float (&x)[V])
+{
+    if (VEC && lane * V < E) {
+        if (f32) {
+#pragma unroll
+            for (int i = 0; i < V; i += 4) {
+                const float4 v = __ldg(reinterpret_cast<const float4 *>(row) + (lane * V + i) / 4);
+                x[i] = v.x; x[i + 1] = v.y; x[i + 2] = v.z; x[i + 3] = v.w;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; i += 4) {
+                const uint2 v = __ldg(reinterpret_cast<const uint2 *>(row) + (lane * V + i) / 4);
+                x[i] = __uint_as_float(v.x << 16); x[i + 1] = __uint_as_float(v.x & 0xFFFF0000u);
+                x[i + 2] = __uint_as_float(v.y << 16); x[i + 3] = __uint_as_float(v.y & 0xFFFF0000u);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) x[i] = !VEC && lane * V + i < E ? load_logit(row, lane * V + i, f32) : -INFINITY;
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) x[i] = x[i] == x[i] ? x[i] : -INFINITY;
+}
+
 // One warp per token.  With p the probabilities that the weights came from
 // (over the chosen experts, or over all) and g the weights' gradients:
 // dl_e = p_e ([e chosen] g_e - sum over the chosen of p g).  Lane j has the
 // j-th chosen expert and writes its entry over the row's other formula, which
 // the lanes have stored before.
-template <int V>
+template <int V, bool VEC>
 __global__ void __launch_bounds__(256) route_backward_kernel(const RouteBackArgs a)
 {
     const int lane = (int)lane_id();
@@ -301,52 +337,60 @@ __global__ void __launch_bounds__(256) route_backward_kernel(const RouteBackArgs
         const char *row = static_cast<const char *>(a.logits) + t * a.ldl * es;
         char *out = static_cast<char *>(a.dl) + t * a.lddl * es;
         int e = lane < a.k ? __ldg(a.experts + t * a.k + lane) : -1;
-        if (e >= a.E) e = -1;
-        const float g = e >= 0 ? __ldg(a.dw + t * a.k + lane) : 0.0f;
+        const float gw = lane < a.k ? __ldg(a.dw + t * a.k + lane) : 0.0f;
         float x[V];
-        if (!a.renorm) {
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const int c = i * 32 + lane;
-                x[i] = c < a.E ? load_logit(row, c, a.f32 != 0) : -INFINITY;
-                if (!(x[i] == x[i])) x[i] = -INFINITY;
-            }
-        }
+        if (!a.renorm) load_row<V, VEC>(row, lane, a.E, a.f32 != 0, x);
+        if (e >= a.E) e = -1;
+        const float g = e >= 0 ? gw : 0.0f;
         float mine = e >= 0 ? load_logit(row, e, a.f32 != 0) : -INFINITY;
-        if (!(mine == mine)) mine = -INFINITY;
-        uint32_t best = logit_key(mine);
+        mine = mine == mine ? mine : -INFINITY;
+        float top = mine;
         if (!a.renorm) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) best = max(best, logit_key(x[i]));
+            for (int i = 0; i < V; ++i) top = fmaxf(top, x[i]);
         }
-        const float top = key_logit(__reduce_max_sync(0xFFFFFFFFu, best));
-        const bool some = top > -INFINITY;
-        float p = some && e >= 0 ? expf(mine - top) : 0.0f, total = p;
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+        const bool some = top > -INFINITY;            // else no expert is allowed: gradients 0
+        float p = some ? expf(mine - top) : 0.0f, total = p;
         if (!a.renorm) {
             total = 0.0f;
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                x[i] = some && i * 32 + lane < a.E ? expf(x[i] - top) : 0.0f;
+                x[i] = some ? expf(x[i] - top) : 0.0f;
                 total += x[i];
             }
         }
-        const float inv_of = warp_sum(total);
-        p = some ? p / inv_of : 0.0f;
-        const float inner = warp_sum(p * g);
+        total = warp_sum(total);
+        const float inv = some ? 1.0f / total : 0.0f;
+        p *= inv;
+        const float inner = warp_sum(p * g), scale = a.renorm ? 0.0f : -inner * inv;
+        float d[V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const int c = i * 32 + lane;
-            const float d = a.renorm || !some ? 0.0f : -(x[i] / inv_of) * inner;
-            if (c < a.E) {
-                if (a.f32) reinterpret_cast<float *>(out)[c] = d;
-                else reinterpret_cast<uint16_t *>(out)[c] = f32_bf16(d);
+        for (int i = 0; i < V; ++i) d[i] = a.renorm ? 0.0f : x[i] * scale;
+        if (VEC) {
+            if (lane * V < a.E) {
+#pragma unroll
+                for (int i = 0; i < V; i += 4) {
+                    if (a.f32)
+                        reinterpret_cast<float4 *>(out)[(lane * V + i) / 4] = make_float4(d[i], d[i + 1], d[i + 2], d[i + 3]);
+                    else
+                        reinterpret_cast<uint2 *>(out)[(lane * V + i) / 4] = make_uint2(bf16x2_rn(d[i], d[i + 1]), bf16x2_rn(d[i + 2], d[i + 3]));
+                }
             }
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if (lane * V + i < a.E) {
+                    if (a.f32) reinterpret_cast<float *>(out)[lane * V + i] = d[i];
+                    else reinterpret_cast<uint16_t *>(out)[lane * V + i] = f32_bf16(d[i]);
+                }
         }
         __syncwarp();
         if (e >= 0) {
-            const float d = p * (g - inner);
-            if (a.f32) reinterpret_cast<float *>(out)[e] = d;
-            else reinterpret_cast<uint16_t *>(out)[e] = f32_bf16(d);
+            const float s = p * (g - inner);
+            if (a.f32) reinterpret_cast<float *>(out)[e] = s;
+            else reinterpret_cast<uint16_t *>(out)[e] = f32_bf16(s);
         }
     }
 }
@@ -513,7 +557,8 @@ cudaError_t run_route(const RouteArgs &a, int blocks, cudaStream_t st)
 {
     const size_t sm = (size_t)(kRouteWarps + 2) * a.E * sizeof(int32_t);
     auto kern = a.f32 ? route_kernel<V, true> : route_kernel<V, false>;
-    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sm);
+    cudaError_t e = cudaSuccess;
+    if (sm > 48 * 1024) e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sm);
     if (e != cudaSuccess) return e;
     if (blocks == 1) {
         kern<<<1, kRouteThreads, sm, st>>>(a);
@@ -527,7 +572,19 @@ template <int V>
 cudaError_t run_route_back(const RouteBackArgs &a, cudaStream_t st)
 {
     const int64_t blocks = ((int64_t)a.T + 7) / 8;
-    route_backward_kernel<V><<<(unsigned)(blocks > 152 * 16 ? 152 * 16 : blocks), 256, 0, st>>>(a);
+    const unsigned grid = (unsigned)(blocks > 152 * 16 ? 152 * 16 : blocks);
+    // whole lanes of 4 values, rows that start on them
+    const int es = a.f32 ? 4 : 2;
+    bool vec = false;
+    if constexpr (V >= 4)
+        vec = a.E % V == 0 && can_vec(a.logits, a.ldl, es) && can_vec(a.dl, a.lddl, es);
+    if constexpr (V >= 4) {
+        if (vec) {
+            route_backward_kernel<V, true><<<grid, 256, 0, st>>>(a);
+            return cudaGetLastError();
+        }
+    }
+    route_backward_kernel<V, false><<<grid, 256, 0, st>>>(a);
     return cudaGetLastError();
 }
 
@@ -545,12 +602,17 @@ cudaError_t launch_route(int64_t T, int64_t E, int k, bool renorm, const void *l
     a.flags = &ws->flags; a.bar = &ws->fix_any;
     // a warp per token while there are SMs left
     int64_t blocks = (T + kRouteWarps - 1) / kRouteWarps;
-    int dev = 0, sms = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess ||
-        cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sms < 1)
-        return cudaErrorInvalidDevice;
-    const int64_t most = sms < kRouteBlocks ? sms : kRouteBlocks;     // one block per SM: all of them run at once
-    if (blocks > most) blocks = most;
+    if (blocks > 1) {
+        int dev = 0, sms = 0;
+        if (cudaGetDevice(&dev) != cudaSuccess ||
+            cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sms < 1)
+            return cudaErrorInvalidDevice;
+        const int64_t most = sms < kRouteBlocks ? sms : kRouteBlocks;     // one block per SM: all of them run at once
+        if (blocks > most) blocks = most;
+        // the flag word and the barrier's count (a single block sets the one and needs no other)
+        const cudaError_t e = cudaMemsetAsync(ws, 0, 2 * sizeof(uint32_t), st);
+        if (e != cudaSuccess) return e;
+    }
     if (blocks < 1) blocks = 1;
     const int v = (int)((E + 31) / 32);
     return v <= 1 ? run_route<1>(a, (int)blocks, st) : v <= 2 ? run_route<2>(a, (int)blocks, st)

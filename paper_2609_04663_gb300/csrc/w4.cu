@@ -32,9 +32,11 @@ namespace {
 
 constexpr int kWarps = 8, kRows = 32 * kWarps;        // features per CTA
 constexpr int kStageK = 128;                          // k of one ring stage: 64 bytes of codes per row
-constexpr int kStages = 3;
 constexpr int kStageBytes = 32 * kStageK / 2;         // of one warp
-constexpr int kPassK = 512;                           // k for which X and the scales are staged at once
+// Ring stages, and k for which X and the scales are staged at once, by the
+// tiles of 8 columns (two CTAs' shared memory fits an SM).
+__host__ __device__ constexpr int ring_stages(int nt) { return nt == 1 ? 4 : 3; }
+__host__ __device__ constexpr int pass_k(int nt) { return nt == 1 ? 1024 : 512; }
 
 struct W4Args {
     const void *X;
@@ -46,6 +48,7 @@ struct W4Args {
     void *Y;
     int64_t ldy;
     int G, rows, N, K, group, slice, tokens;          // slice: k per CTA; tokens: rows of X per item at most
+    int sp, zp;                                       // row pitches of the staged scales and zero points
     int x_f32, s_f32, x_vec;                          // x_vec: X's rows can be read 16 bytes at a time
 };
 
@@ -128,19 +131,13 @@ __device__ __forceinline__ void sts128(uint32_t a, uint4 v) { st_shared_v4(a, v.
 
 // Row pitch of the staged scales or zero points of one pass: an odd number of
 // 16-byte pieces, so that the 8 rows that a warp reads at once lie in
-// different banks.
-__host__ __device__ __forceinline__ int meta_pitch(int group, int size)
+// different banks.  A pass holds pass / group groups where slices and passes
+// start on whole ones, part of one where slices divide groups, and may begin
+// and end within groups otherwise.
+int meta_pitch(int pass, int group, int slice, int size)
 {
-    const int pieces = ((kPassK / group + 2) * size + 15) / 16;
-    return (pieces | 1) * 16;
-}
-
-// Shared memory of a CTA, in bytes: the codes' rings, X's columns for one
-// pass (64 bytes per 32 k and column), the pass's scales and zero points.
-int w4_smem(int cols, int group, int ssize, bool zeros)
-{
-    return kWarps * kStages * kStageBytes + (kPassK / 32) * cols * 64 + kRows * meta_pitch(group, ssize) +
-           (zeros ? kRows * meta_pitch(group, 1) : 0);
+    const int n = slice % group == 0 && pass % group == 0 ? pass / group : group % slice == 0 ? 1 : pass / group + 2;
+    return ((n * size + 15) / 16 | 1) * 16;
 }
 
 // NT: tiles of 8 columns; F32X: FP32 rows, three columns each.  GB: 32-k blocks
@@ -149,7 +146,7 @@ int w4_smem(int cols, int group, int ssize, bool zeros)
 template <int NT, bool F32X, int GB>
 __global__ void __launch_bounds__(32 * kWarps, 2) w4_kernel(const W4Args a)
 {
-    constexpr int S = F32X ? 3 : 1;
+    constexpr int S = F32X ? 3 : 1, kStages = ring_stages(NT), kPassK = pass_k(NT);
     extern __shared__ __align__(128) uint8_t smem[];
     const uint32_t codes = smem_u32(smem);
     const int warp = threadIdx.x >> 5, lane = (int)lane_id(), lr = lane >> 2, lc = lane & 3;
@@ -209,7 +206,7 @@ __global__ void __launch_bounds__(32 * kWarps, 2) w4_kernel(const W4Args a)
         m = min(a.tokens, a.rows - row0);
     }
     const int cols = m * S, gb = a.group / 32, ngroups = a.K / a.group;
-    const int ssize = a.s_f32 ? 4 : 2, sp = meta_pitch(a.group, ssize), zp = meta_pitch(a.group, 1);
+    const int ssize = a.s_f32 ? 4 : 2, sp = a.sp, zp = a.zp;
     const uint32_t xs = codes + kWarps * kStages * kStageBytes;
     const uint32_t sc = xs + (uint32_t)((kPassK / 32) * a.tokens * S * 64), zs = sc + (uint32_t)(kRows * sp);
     const int k0 = (int)rank * a.slice, k1 = min(a.K, k0 + a.slice);
@@ -238,10 +235,11 @@ __global__ void __launch_bounds__(32 * kWarps, 2) w4_kernel(const W4Args a)
         const uint8_t *from = static_cast<const uint8_t *>(src) + (((int64_t)g * a.N + n0) * ngroups + g0) * size;
         const int64_t rowb = (int64_t)ngroups * size;
         const int pieces = dpitch / 16;               // past the n values: zeros
+        const uint32_t inv = 65536u / (uint32_t)pieces + 1u;       // i / pieces for i < 4096, pieces < 16
         // whole pieces only: a row's last piece may not run into what follows the array
         const bool wide = ((reinterpret_cast<uintptr_t>(from) | (uintptr_t)rowb) & 15u) == 0;
         for (int i = threadIdx.x; i < kRows * pieces; i += 32 * kWarps) {
-            const int r = i / pieces, o = (i % pieces) * 16;
+            const int r = pieces < 16 ? (int)((uint32_t)i * inv >> 16) : i / pieces, o = (i - r * pieces) * 16;
             const bool ok = n0 + r < a.N;
             const uint32_t to = dst + (uint32_t)(r * dpitch + o);
             if (wide) {
@@ -284,7 +282,7 @@ __global__ void __launch_bounds__(32 * kWarps, 2) w4_kernel(const W4Args a)
         cp_async_commit();
         if (st0 == 0) {
 #pragma unroll
-            for (int st = 0; st < kStages - 1; ++st) fetch(st);
+            for (int st = 0; st < kStages; ++st) fetch(st);
         }
         // eight k of one row at a time, the loads of several in flight
         constexpr int XB = 4;
@@ -332,14 +330,13 @@ __global__ void __launch_bounds__(32 * kWarps, 2) w4_kernel(const W4Args a)
         }
         // the scales have arrived: with the first pass the codes' first stages
         // may still be on their way, later ones were asked for before the scales
-        if (st0 == 0) cp_async_wait<kStages - 1>();
+        if (st0 == 0) cp_async_wait<kStages>();
         else cp_async_wait<0>();
         __syncthreads();
 
         for (int st = st0; st < min(nst, st0 + kPassK / kStageK); ++st) {
-            cp_async_wait<kStages - 2>();
+            cp_async_wait<kStages - 1>();
             __syncwarp();
-            fetch(st + kStages - 1);                  // into the stage read in the step before
             const uint32_t stage = ring + (uint32_t)((st % kStages) * kStageBytes) + (uint32_t)(lr * 64 + lc * 4);
             const uint32_t xst = xs + (uint32_t)((st - st0) * (kStageK / 32) * cols * 64 + lr * 64 + lc * 16);
             const uint32_t srow = sc + (uint32_t)((warp * 32 + lr) * sp), zrow = zs + (uint32_t)((warp * 32 + lr) * zp);
@@ -438,6 +435,8 @@ __global__ void __launch_bounds__(32 * kWarps, 2) w4_kernel(const W4Args a)
                     scale_up(s);
                 }
             }
+            __syncwarp();
+            fetch(st + kStages);                      // into the stage just read
         }
     }
     cp_async_wait<0>();
@@ -491,7 +490,10 @@ template <int NT, bool F32X, int GB>
 cudaError_t run_w4(const W4Args &a, int64_t blocks, int64_t items, int ks, cudaStream_t st)
 {
     auto kern = w4_kernel<NT, F32X, GB>;
-    const int sm = w4_smem(a.tokens * (F32X ? 3 : 1), a.group, a.s_f32 ? 4 : 2, a.zeros != nullptr);
+    // the codes' rings, X's columns for one pass (64 bytes per 32 k and column),
+    // the pass's scales and zero points
+    const int sm = kWarps * ring_stages(NT) * kStageBytes + pass_k(NT) / 32 * a.tokens * (F32X ? 3 : 1) * 64 +
+                   kRows * (a.sp + (a.zeros ? a.zp : 0));
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, sm);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
@@ -531,14 +533,19 @@ cudaError_t launch_w4_matvec(bool x_f32, int64_t G, int64_t rows, int64_t N, int
     int nt = (int)((want * S + 7) / 8);
     nt = nt > 1 ? 3 : 1;
     a.tokens = 8 * nt / S;
+    if (a.tokens > rows) a.tokens = (int)rows;
+    const int pass = pass_k(nt);
     const int64_t blocks = (N + kRows - 1) / kRows;
     const int64_t items = ends ? active + rows / a.tokens + 1 : (rows + a.tokens - 1) / a.tokens;
     if (items > 65535) return cudaErrorInvalidValue;
-    // slices of K, each of one pass at least: as many CTAs as one and a half
-    // times what runs at once
+    // slices of K: one pass each where 8 of them allow it, and more while there
+    // are fewer CTAs than SMs and each has 512 k
     int ks = 1;
-    while (ks < 8 && blocks * active * ks < 3 * 152 && ks * 2 * kPassK <= K) ks *= 2;
-    a.slice = (int)((K + (int64_t)ks * kPassK - 1) / ((int64_t)ks * kPassK) * kPassK);
+    while (ks < 8 && (ks * pass < K || (blocks * active * ks < 152 && ks * 2 * 512 <= K))) ks *= 2;
+    const int64_t unit = K < (int64_t)ks * pass ? kStageK : pass;
+    a.slice = (int)((K + ks * unit - 1) / (ks * unit) * unit);
+    a.sp = meta_pitch(pass, group, a.slice, s_f32 ? 4 : 2);
+    a.zp = meta_pitch(pass, group, a.slice, 1);
 #define EMU_W4(GB)                                                                                              \
     (x_f32 ? (nt == 1 ? run_w4<1, true, GB>(a, blocks, items, ks, st) : run_w4<3, true, GB>(a, blocks, items, ks, st)) \
            : (nt == 1 ? run_w4<1, false, GB>(a, blocks, items, ks, st) : run_w4<3, false, GB>(a, blocks, items, ks, st)))
