@@ -474,10 +474,12 @@ emu_status emu_grouped_prodsum_wgrad(int nslices, int64_t G, int64_t rows, int64
  * with G = 1: one matrix for all rows.  Values in ends outside 0 .. rows or
  * decreasing are clamped.  Rows of no group are zero.  Any number of rows is
  * computed; the weights are read again for every 24 (BF16) or 8 (FP32) of an
- * expert.  q 16-byte aligned.  No workspace. */
+ * expert.  q 16-byte aligned.  ws: emu_w4_workspace_bytes, 16-byte aligned, for
+ * X's slices; NULL will do for BF16 rows of 16-byte aligned base and pitch. */
+size_t emu_w4_workspace_bytes(int dtype, int64_t rows, int64_t K);
 emu_status emu_w4_matvec(int dtype, int64_t G, int64_t rows, int64_t N, int64_t K, int64_t group, const void *X,
                          int64_t ldx, const uint8_t *q, const void *s, int stype, const uint8_t *z,
-                         const int32_t *ends, void *Y, int64_t ldy, emu_stream_t stream);
+                         const int32_t *ends, void *Y, int64_t ldy, void *ws, size_t ws_bytes, emu_stream_t stream);
 
 /* Routing of T tokens to the k of E experts with the largest logits (dtype,
  * T x E, row pitch ldl; ties: the lower index; NaN counts as minus infinity):

@@ -72,7 +72,9 @@ _SIGS = {
                                    "size", "p"]),
     "emu_grouped_prodsum_wgrad": ("i", ["i", "l", "l", "l", "l", "p", "l", "i", "p", "l", "i", "p", "p", "i", "l", "l",
                                         "p", "size", "p"]),
-    "emu_w4_matvec": ("i", ["i", "l", "l", "l", "l", "l", "p", "l", "p", "p", "i", "p", "p", "p", "l", "p"]),
+    "emu_w4_workspace_bytes": ("size", ["i", "l", "l"]),
+    "emu_w4_matvec": ("i", ["i", "l", "l", "l", "l", "l", "p", "l", "p", "p", "i", "p", "p", "p", "l", "p", "size",
+                            "p"]),
     "emu_route_workspace_bytes": ("size", ["l", "l", "l"]),
     "emu_route": ("i", ["i", "l", "l", "l", "i", "p", "l", "p", "p", "p", "p", "p", "p", "size", "p"]),
     "emu_route_backward": ("i", ["i", "l", "l", "l", "i", "p", "l", "p", "p", "p", "l", "p"]),
@@ -159,6 +161,7 @@ emu_grouped_prodsum = _mk("emu_grouped_prodsum")
 emu_grouped_gemm_workspace_bytes = _mk("emu_grouped_gemm_workspace_bytes")
 emu_grouped_gemm_f32 = _mk("emu_grouped_gemm_f32")
 emu_grouped_prodsum_wgrad = _mk("emu_grouped_prodsum_wgrad")
+emu_w4_workspace_bytes = _mk("emu_w4_workspace_bytes")
 emu_w4_matvec = _mk("emu_w4_matvec")
 emu_route_workspace_bytes = _mk("emu_route_workspace_bytes")
 emu_route = _mk("emu_route")
@@ -626,12 +629,13 @@ def grouped_wgrad(A, B, ends, srcA=None, srcB=None, D=None, ws=None, stream=None
     return D, ws
 
 
-def w4_matvec(X, Wq, scales, zeros=None, ends=None, Y=None, stream=None):
+def w4_matvec(X, Wq, scales, zeros=None, ends=None, Y=None, ws=None, stream=None):
     """emu_w4_matvec: Y[r] = W_g X[r] for the rows r of group g (ends None: one
     matrix Wq [N, K/2] for all rows), W = (codes - zeros) * scales.  Wq uint8
     [G, N, K/2], the even k in the low half of a byte; scales FP32 or BF16 and
     zeros uint8 (None: 8) [G, N, K/group].  X and Y: FP32 or BF16.  For a few
-    rows per expert.  Returns Y."""
+    rows per expert.  ws: emu_w4_workspace_bytes bytes that a caller may keep
+    (made here where they are needed).  Returns Y."""
     torch, where = _torch(), "w4_matvec"
     dev, u8 = X.device, torch.uint8
     dt, ldx, (rows, K) = _dtype(X, "w4_matvec: X"), _pitch(X, "w4_matvec: X"), X.shape
@@ -653,10 +657,14 @@ def w4_matvec(X, Wq, scales, zeros=None, ends=None, Y=None, stream=None):
         Y = _empty((rows, N), X.dtype, dev, stream)
     elif Y.shape != (rows, N) or Y.dtype is not X.dtype:
         _bad(where, "Y has another shape or type")
-    r = _lib.emu_w4_matvec(dt, G, rows, N, K, group, X.data_ptr(), ldx, Wq.data_ptr(), scales.data_ptr(),
-                             _dtype(scales, "w4_matvec: scales"), zeros.data_ptr() if zeros is not None else None,
-                             _ints(ends, G, dev, "w4_matvec: ends") if ends is not None else None, Y.data_ptr(),
-                             _pitch(Y, "w4_matvec: Y", dev), _raw_stream(stream, dev))
+    x = X.data_ptr()
+    if ws is None and (dt == F32 or x % 16 or ldx % 8):
+        ws = _empty(rows * K * (6 if dt == F32 else 2), u8, dev, stream)
+    r = _lib.emu_w4_matvec(dt, G, rows, N, K, group, x, ldx, Wq.data_ptr(), scales.data_ptr(),
+                           _dtype(scales, "w4_matvec: scales"), zeros.data_ptr() if zeros is not None else None,
+                           _ints(ends, G, dev, "w4_matvec: ends") if ends is not None else None, Y.data_ptr(),
+                           _pitch(Y, "w4_matvec: Y", dev), ws.data_ptr() if ws is not None else None,
+                           ws.numel() if ws is not None else 0, _raw_stream(stream, dev))
     if r:
         _check(r, "emu_w4_matvec")
     return Y

@@ -241,9 +241,14 @@ emu_status emu_grouped_prodsum_wgrad(int nslices, int64_t G, int64_t rows, int64
                                                &static_cast<WsHeader *>(ws)->flags, st));
 }
 
+size_t emu_w4_workspace_bytes(int dtype, int64_t rows, int64_t K)
+{
+    return rows < 0 || K < 0 ? 0 : (size_t)rows * (size_t)K * (dtype == EMU_F32 ? 6 : 2);
+}
+
 emu_status emu_w4_matvec(int dtype, int64_t G, int64_t rows, int64_t N, int64_t K, int64_t group, const void *X,
                          int64_t ldx, const uint8_t *q, const void *scales, int stype, const uint8_t *zeros,
-                         const int32_t *ends, void *Y, int64_t ldy, emu_stream_t stream)
+                         const int32_t *ends, void *Y, int64_t ldy, void *ws, size_t ws_bytes, emu_stream_t stream)
 {
     if (!known(dtype) || !known(stype) || ldx < K || ldy < N || group < 32 || group % 32 != 0 || K < 0 || K % group != 0 ||
         (!ends && G != 1))
@@ -258,8 +263,12 @@ emu_status emu_w4_matvec(int dtype, int64_t G, int64_t rows, int64_t N, int64_t 
     if (!X || !q || !scales) return EMU_ERR_INVALID_ARG;
     if (!aligned16(q) || !fits(X, dtype) || !fits(Y, dtype) || !fits(scales, stype)) return EMU_ERR_MISALIGNED;
     if (rows > 65535 * 2) return EMU_ERR_UNSUPPORTED;           // items of two rows and more on the grid's y dimension
+    if (!w4_direct(dtype == EMU_F32, X, ldx)) {
+        s = check_ws(ws, ws_bytes, emu_w4_workspace_bytes(dtype, rows, K));
+        if (s != EMU_OK) return s;
+    }
     return cuda_status(launch_w4_matvec(dtype == EMU_F32, G, rows, N, K, (int)group, X, ldx, q, scales,
-                                        stype == EMU_F32, zeros, ends, Y, ldy, st));
+                                        stype == EMU_F32, zeros, ends, Y, ldy, static_cast<uint16_t *>(ws), st));
 }
 
 size_t emu_route_workspace_bytes(int64_t T, int64_t E, int64_t k)

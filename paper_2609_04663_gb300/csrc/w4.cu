@@ -13,15 +13,20 @@
 // BF16, 16 features are its rows, and its 8 columns are BF16 rows of X, or the
 // three BF16 slices (Eq. (fp32split)) of FP32 rows, whose products are exact as
 // well.  tcgen05 would need the decoded weights back in shared memory.  A code
-// pair becomes BF16 by one or-with-mask (128 + q) and one subtraction of
-// 128 + z; since a dot product may take its k in any order, the pairs are the
+// pair becomes BF16 by one or-with-mask (128 + q) and one multiply-add that
+// takes 128 + z off; since a dot product may take its k in any order, the pairs are the
 // nibbles i and i + 4 of a word, and X is staged in that order.  Sums of one
 // scale group are scaled and added in FP32.
 //
-// A CTA takes 128 features and one of KS slices of K; the KS CTAs of a cluster
-// add their sums through distributed shared memory in a fixed order.  Each warp
-// streams its own 32 rows of codes through a ring in shared memory with
-// 16-byte asynchronous copies, so no wait is a spin.
+// A CTA takes 32 features; its 4 or 8 warps take a part of K each, on their own
+// until their sums are added through shared memory in a fixed order.  A warp
+// streams its codes, scales and zero points with 16-byte asynchronous copies
+// into a ring and tables of its own, so no wait is a spin, and reads X's columns
+// from L1 and L2: BF16 rows as they are, FP32 rows (or such that allow no 16-byte
+// reads) as slices that a small kernel has split and put in pair order before.
+// (K split over a cluster, with X staged for 256 features at a time, kept most
+// warps waiting for each other's staging: 16 rows over 12 experts of 2048 x 4096
+// took 28 us, 7 FP32 rows times 16384 x 8192 53 us.)
 #include "grouped_common.cuh"
 #include "launchers.cuh"
 #include "split_f32_pair.cuh"
@@ -30,16 +35,14 @@ namespace emu {
 
 namespace {
 
-constexpr int kWarps = 8, kRows = 32 * kWarps;        // features per CTA
+constexpr int kRows = 32;                             // features per CTA
 constexpr int kStageK = 128;                          // k of one ring stage: 64 bytes of codes per row
-constexpr int kStageBytes = 32 * kStageK / 2;         // of one warp
-// Ring stages, and k for which X and the scales are staged at once, by the
-// tiles of 8 columns (two CTAs' shared memory fits an SM).
-__host__ __device__ constexpr int ring_stages(int nt) { return nt == 1 ? 4 : 3; }
-__host__ __device__ constexpr int pass_k(int nt) { return nt == 1 ? 1024 : 512; }
+constexpr int kStages = 4;
+constexpr int kStageBytes = kRows * kStageK / 2;
+constexpr int kPassK = 1024;                          // k of a warp for which scales are held at once
 
 struct W4Args {
-    const void *X;
+    const void *X;            // rows of X, or planes: column c (row c / S, slice c % S) at c * K
     int64_t ldx;
     const uint8_t *q;
     const void *scales;
@@ -47,9 +50,10 @@ struct W4Args {
     const int32_t *ends;      // NULL: one matrix, all rows
     void *Y;
     int64_t ldy;
-    int G, rows, N, K, group, slice, tokens;          // slice: k per CTA; tokens: rows of X per item at most
-    int sp, zp;                                       // row pitches of the staged scales and zero points
-    int x_f32, s_f32, x_vec;                          // x_vec: X's rows can be read 16 bytes at a time
+    int G, rows, N, K, group, slice, tokens;          // slice: k per warp; tokens: rows of X per item at most
+    int S;                                            // slices of a row: columns per row
+    int sp, zp;                                       // row pitches of the held scales and zero points
+    int y_f32, s_f32;
 };
 
 // The first n of 16 bytes from src (16-byte aligned), the rest zeros.
@@ -61,50 +65,26 @@ __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commi
 template <int N>
 __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-__device__ __forceinline__ uint32_t lds32(uint32_t a)
-{
-    uint32_t v;
-    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(a));
-    return v;
-}
-__device__ __forceinline__ uint32_t lds16(uint32_t a)
-{
-    uint16_t v;
-    asm volatile("ld.shared.b16 %0, [%1];" : "=h"(v) : "r"(a));
-    return v;
-}
-__device__ __forceinline__ uint32_t lds8(uint32_t a)
-{
-    uint32_t v;
-    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(a));
-    return v;
-}
-__device__ __forceinline__ uint2 lds64(uint32_t a)
-{
-    uint2 v;
-    asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
-    return v;
-}
-__device__ __forceinline__ uint4 lds128(uint32_t a)
-{
-    uint4 v;
-    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
-    return v;
-}
+// A value at byte `at` of shared memory, by an ordinary load: unlike volatile
+// assembly it may move between the products of earlier blocks.
+template <typename T>
+__device__ __forceinline__ T shared_at(const uint8_t *smem, uint32_t at) { return *reinterpret_cast<const T *>(smem + at); }
 
-// Codes of nibbles s / 4 and s / 4 + 4 of w, minus the zero point, as a BF16 pair.
+// Codes of nibbles s / 4 and s / 4 + 4 of w, minus the zero point (as the pair
+// -(128 + z)), as a BF16 pair.  One three-input logic operation with both masks
+// in registers (written with operators it becomes two), one multiply-add by one.
 __device__ __forceinline__ uint32_t decode(uint32_t w, int s, uint32_t zero)
 {
-    const uint32_t p = ((w >> s) & 0x000F000Fu) | 0x43004300u;      // BF16 128 + q
-    uint32_t d;
-    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(p), "r"(zero));
+    uint32_t p, d;                                                  // BF16 128 + q: (w & mask) | magic
+    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(p) : "r"(w >> s), "r"(0x000F000Fu), "r"(0x43004300u));
+    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(p), "r"(0x3F803F80u), "r"(zero));
     return d;
 }
 
 __device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
                                          uint32_t b0, uint32_t b1)
 {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
                  "{%0, %1, %2, %3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
@@ -114,7 +94,7 @@ __device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1
 __device__ __forceinline__ void mma16816_first(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
                                                uint32_t b0, uint32_t b1)
 {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
                  "{%10, %10, %10, %10};"
                  : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.0f));
@@ -127,9 +107,7 @@ __device__ __forceinline__ uint4 pair_order(uint32_t w01, uint32_t w23, uint32_t
                       __byte_perm(w23, w67, 0x7632));
 }
 
-__device__ __forceinline__ void sts128(uint32_t a, uint4 v) { st_shared_v4(a, v.x, v.y, v.z, v.w); }
-
-// Row pitch of the staged scales or zero points of one pass: an odd number of
+// Row pitch of the held scales or zero points of one pass: an odd number of
 // 16-byte pieces, so that the 8 rows that a warp reads at once lie in
 // different banks.  A pass holds pass / group groups where slices and passes
 // start on whole ones, part of one where slices divide groups, and may begin
@@ -140,20 +118,42 @@ int meta_pitch(int pass, int group, int slice, int size)
     return ((n * size + 15) / 16 | 1) * 16;
 }
 
-// NT: tiles of 8 columns; F32X: FP32 rows, three columns each.  GB: 32-k blocks
-// of a scale group within a stage of 4: 1 or 2 (groups of 32 or 64), 4
-// (multiples of 128); 0: any other group, with its bounds looked for.
-template <int NT, bool F32X, int GB>
-__global__ void __launch_bounds__(32 * kWarps, 2) w4_kernel(const W4Args a)
+// FP32 rows (or BF16 rows of any alignment) -> planes in pair order, 8 k a thread.
+template <bool F32X>
+__global__ void __launch_bounds__(256) w4_planes_kernel(const void *__restrict__ X, int64_t ldx, int rows, int K,
+                                                        uint16_t *__restrict__ planes)
 {
-    constexpr int S = F32X ? 3 : 1, kStages = ring_stages(NT), kPassK = pass_k(NT);
+    griddep_launch_dependents();
+    const int octets = K / 8;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= (int64_t)rows * octets) return;
+    const int64_t r = i / octets, k = (i - r * octets) * 8;
+    constexpr int S = F32X ? 3 : 1;
+    uint32_t w[3][4];
+    if constexpr (F32X) {
+        const float *x = static_cast<const float *>(X) + r * ldx + k;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) split_pair(__ldg(x + 2 * e), __ldg(x + 2 * e + 1), w[0][e], w[1][e], w[2][e]);
+    } else {
+        const uint16_t *x = static_cast<const uint16_t *>(X) + r * ldx + k;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[0][e] = (uint32_t)__ldg(x + 2 * e) | (uint32_t)__ldg(x + 2 * e + 1) << 16;
+    }
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+        *reinterpret_cast<uint4 *>(planes + (r * S + s) * K + k) = pair_order(w[s][0], w[s][1], w[s][2], w[s][3]);
+}
+
+// NT: tiles of 8 columns; DIRECT: X as rows, not planes.  GB: 32-k blocks of a
+// scale group within a stage of 4: 1 or 2 (groups of 32 or 64), 4 (multiples of
+// 128); 0: any other group, with its bounds looked for.
+template <int NT, bool DIRECT, int GB, int kWarps>
+__global__ void __launch_bounds__(32 * kWarps, 16 / kWarps) w4_kernel(const W4Args a)
+{
     extern __shared__ __align__(128) uint8_t smem[];
-    const uint32_t codes = smem_u32(smem);
-    const int warp = threadIdx.x >> 5, lane = (int)lane_id(), lr = lane >> 2, lc = lane & 3;
-    uint32_t ks, rank;
-    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(ks));
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
-    const int n0 = (int)(blockIdx.x / ks) * kRows;
+    const uint32_t rings = 0, sbase = smem_u32(smem);     // shared addresses are offsets from smem
+    const int warp = __shfl_sync(0xFFFFFFFFu, (int)threadIdx.x >> 5, 0), lane = (int)lane_id(), lr = lane >> 2, lc = lane & 3;
+    const int n0 = (int)blockIdx.x * kRows;
 
     // ---- the item: rows [row0, row0 + m) of X, all of one expert
     int g = 0, row0 = 0, m = a.rows;
@@ -190,45 +190,52 @@ __global__ void __launch_bounds__(32 * kWarps, 2) w4_kernel(const W4Args a)
             m = min(a.tokens, starts[g + 1] - row0);
         } else {
             // no item left: the first CTA without one clears the rows of no group
-            if (chunk == 0 && rank == 0) {
-                const int n = n0 + (int)threadIdx.x;
-                for (int64_t r = starts[a.G]; r < a.rows; ++r)
+            if (chunk == 0) {
+                const int n = n0 + lane;
+                for (int64_t r = starts[a.G] + warp; r < a.rows; r += kWarps)
                     if (n < a.N) {
-                        if (a.x_f32) static_cast<float *>(a.Y)[r * a.ldy + n] = 0.0f;
+                        if (a.y_f32) static_cast<float *>(a.Y)[r * a.ldy + n] = 0.0f;
                         else static_cast<uint16_t *>(a.Y)[r * a.ldy + n] = 0;
                     }
             }
-            return;                                   // all CTAs of the cluster take this way
+            return;
         }
         __syncthreads();                              // the tables are read, the rings may be filled
     } else {
         row0 = (int)blockIdx.y * a.tokens;
         m = min(a.tokens, a.rows - row0);
     }
-    const int cols = m * S, gb = a.group / 32, ngroups = a.K / a.group;
+    const int cols = m * a.S, gb = a.group / 32, ngroups = a.K / a.group;
     const int ssize = a.s_f32 ? 4 : 2, sp = a.sp, zp = a.zp;
-    const uint32_t xs = codes + kWarps * kStages * kStageBytes;
-    const uint32_t sc = xs + (uint32_t)((kPassK / 32) * a.tokens * S * 64), zs = sc + (uint32_t)(kRows * sp);
-    const int k0 = (int)rank * a.slice, k1 = min(a.K, k0 + a.slice);
+    const uint32_t ring = rings + (uint32_t)(warp * kStages * kStageBytes);
+    const uint32_t sc = rings + (uint32_t)(kWarps * kStages * kStageBytes + warp * kRows * (sp + (a.zeros ? zp : 0)));
+    const uint32_t zs = sc + (uint32_t)(kRows * sp);
+    const int k0 = warp * a.slice, k1 = min(a.K, k0 + a.slice);
     const int nst = k1 > k0 ? (k1 - k0 + kStageK - 1) / kStageK : 0;
 
-    // ---- this warp's ring: rows n0 + 32 warp .. + 31, 16-byte piece j of a row at piece j ^ (row / 2 % 4)
-    const uint32_t ring = codes + (uint32_t)(warp * kStages * kStageBytes);
-    const int64_t pitch = a.K / 2;
-    const uint8_t *qbase = a.q + ((int64_t)g * a.N + n0 + warp * 32) * pitch;
-    auto fetch = [&](int st) {
-        if (st < nst) {
-            const uint32_t dst = ring + (uint32_t)((st % kStages) * kStageBytes);
-            const int piece = lane & 3, byte = (k0 + st * kStageK) / 2 + piece * 16;
+    // ---- this warp's ring: rows n0 .. n0 + 31, 16-byte piece j of a row at piece j ^ (row / 2 % 4);
+    // a lane copies piece lane % 4 of rows lane / 4 + 8 i.  Rows past the last
+    // feature read that one again (their sums go nowhere), pieces past the slice
+    // are not copied (nor read).
+    const int pitch = a.K / 2, tail = (k1 - k0) % kStageK / 32;       // blocks of a last stage that is not whole
+    const uint8_t *qp[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int r = i * 8 + (lane >> 2);
-                const bool ok = n0 + warp * 32 + r < a.N && byte < k1 / 2;
-                cp_async16(dst + (uint32_t)(r * 64 + ((piece ^ (r >> 1 & 3)) << 4)), ok ? qbase + r * pitch + byte : a.q, ok ? 16 : 0);
-            }
+    for (int i = 0; i < 4; ++i)
+        qp[i] = a.q + ((int64_t)g * a.N + min(n0 + lr + 8 * i, a.N - 1)) * pitch + k0 / 2 + lc * 16;
+    uint32_t qdst = sbase + ring + (uint32_t)(lr * 64 + ((lc ^ (lr >> 1 & 3)) << 4));
+    int asked = 0;                                    // stages asked for
+    auto fetch = [&]() {                              // the next one, if there is one
+        if (asked < nst && (tail == 0 || asked < nst - 1 || lc < tail)) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(qdst + (uint32_t)(i * 512)), "l"(qp[i]) : "memory");
         }
         cp_async_commit();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) qp[i] += kStageK / 2;
+        qdst = (++asked & (kStages - 1)) == 0 ? qdst - (kStages - 1) * kStageBytes : qdst + kStageBytes;
     };
+    static_assert((kStages & (kStages - 1)) == 0, "ring stages");
     // n scales or zero points of each feature from group g0 on -> rows of pitch
     // dpitch at dst, by 16-byte copies where the source rows allow it
     auto meta = [&](uint32_t dst, int dpitch, const void *src, int size, int g0, int n) {
@@ -238,10 +245,10 @@ __global__ void __launch_bounds__(32 * kWarps, 2) w4_kernel(const W4Args a)
         const uint32_t inv = 65536u / (uint32_t)pieces + 1u;       // i / pieces for i < 4096, pieces < 16
         // whole pieces only: a row's last piece may not run into what follows the array
         const bool wide = ((reinterpret_cast<uintptr_t>(from) | (uintptr_t)rowb) & 15u) == 0;
-        for (int i = threadIdx.x; i < kRows * pieces; i += 32 * kWarps) {
+        for (int i = lane; i < kRows * pieces; i += 32) {
             const int r = pieces < 16 ? (int)((uint32_t)i * inv >> 16) : i / pieces, o = (i - r * pieces) * 16;
             const bool ok = n0 + r < a.N;
-            const uint32_t to = dst + (uint32_t)(r * dpitch + o);
+            const uint32_t to = sbase + dst + (uint32_t)(r * dpitch + o);
             if (wide) {
                 const int len = ok ? min(max(n * size - o, 0), 16) : 0;
                 cp_async16(to, len ? from + r * rowb + o : a.q, len);
@@ -263,6 +270,26 @@ __global__ void __launch_bounds__(32 * kWarps, 2) w4_kernel(const W4Args a)
             }
         }
     };
+    // ---- X's columns of this lane: 8 k of column 8 t + lr per block of 32 (columns
+    // that are not there read the first one: no other column sees them)
+    const uint8_t *xp[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const int c = t * 8 + lr < cols ? t * 8 + lr : 0;
+        xp[t] = static_cast<const uint8_t *>(a.X) +
+                ((DIRECT ? (row0 + c) * a.ldx : ((int64_t)row0 * a.S + c) * a.K) + k0) * 2 + lc * 16;
+    }
+    int ahead = (k1 - k0) / 32;                       // blocks of X still to be loaded
+    uint4 xn[NT];                                     // the next block's
+    auto load_x = [&]() {
+        if (--ahead >= 0) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                xn[t] = __ldg(reinterpret_cast<const uint4 *>(xp[t]));
+                xp[t] += 64;
+            }
+        }
+    };
 
     float total[2][NT][4], part[2][NT][4];
 #pragma unroll
@@ -273,82 +300,36 @@ __global__ void __launch_bounds__(32 * kWarps, 2) w4_kernel(const W4Args a)
             for (int e = 0; e < 4; ++e) total[i][t][e] = part[i][t][e] = 0.0f;
 
     for (int st0 = 0; st0 < nst; st0 += kPassK / kStageK) {
-        // ---- X, scales and zero points of this pass
+        // ---- scales and zero points of this pass
         const int p0 = k0 + st0 * kStageK, p1 = min(k1, p0 + kPassK), g0 = p0 / a.group;
         const int ng = (p1 - 1) / a.group - g0 + 1;
-        __syncthreads();                              // the pass before has been read
+        __syncwarp();                                 // the pass before has been read
         meta(sc, sp, a.scales, ssize, g0, ng);
         if (a.zeros) meta(zs, zp, a.zeros, 1, g0, ng);
         cp_async_commit();
         if (st0 == 0) {
 #pragma unroll
-            for (int st = 0; st < kStages; ++st) fetch(st);
+            for (int st = 0; st < kStages; ++st) fetch();
+            if (!DIRECT) griddep_wait();              // the planes: all else was there before their kernel
+            load_x();
+        } else {
+            cp_async_wait<0>();                       // these came last
         }
-        // eight k of one row at a time, the loads of several in flight
-        constexpr int XB = 4;
-        for (int i0 = threadIdx.x; i0 < m * (kPassK / 8); i0 += 32 * kWarps * XB) {
-            uint4 v[XB][S == 3 ? 2 : 1];
-#pragma unroll
-            for (int b = 0; b < XB; ++b) {
-                const int i = i0 + b * 32 * kWarps, k = p0 + i % (kPassK / 8) * 8;
-                const bool in = i < m * (kPassK / 8) && k < p1;
-                const char *x = static_cast<const char *>(a.X) + ((int64_t)(row0 + i / (kPassK / 8)) * a.ldx + k) * (F32X ? 4 : 2);
-#pragma unroll
-                for (int h = 0; h < (F32X ? 2 : 1); ++h) {
-                    v[b][h] = make_uint4(0u, 0u, 0u, 0u);
-                    if (in && a.x_vec) {
-                        v[b][h] = __ldg(reinterpret_cast<const uint4 *>(x) + h);
-                    } else if (in && F32X) {
-                        const uint32_t *u = reinterpret_cast<const uint32_t *>(x) + 4 * h;
-                        v[b][h] = make_uint4(__ldg(u), __ldg(u + 1), __ldg(u + 2), __ldg(u + 3));
-                    } else if (in) {
-                        const uint16_t *u = reinterpret_cast<const uint16_t *>(x);
-                        auto two = [&](int e) { return (uint32_t)__ldg(u + e) | (uint32_t)__ldg(u + e + 1) << 16; };
-                        v[b][h] = make_uint4(two(0), two(2), two(4), two(6));
-                    }
-                }
-            }
-#pragma unroll
-            for (int b = 0; b < XB; ++b) {
-                const int i = i0 + b * 32 * kWarps, o = i % (kPassK / 8);
-                if (i >= m * (kPassK / 8)) break;
-                const uint32_t dst = xs + (uint32_t)(((o >> 2) * cols + i / (kPassK / 8) * S) * 64 + (o & 3) * 16);
-                if constexpr (F32X) {
-                    uint32_t w[3][4];
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        split_pair(__uint_as_float(v[b][h].x), __uint_as_float(v[b][h].y), w[0][2 * h], w[1][2 * h], w[2][2 * h]);
-                        split_pair(__uint_as_float(v[b][h].z), __uint_as_float(v[b][h].w), w[0][2 * h + 1], w[1][2 * h + 1],
-                                   w[2][2 * h + 1]);
-                    }
-#pragma unroll
-                    for (int s = 0; s < 3; ++s) sts128(dst + s * 64, pair_order(w[s][0], w[s][1], w[s][2], w[s][3]));
-                } else {
-                    sts128(dst, pair_order(v[b][0].x, v[b][0].y, v[b][0].z, v[b][0].w));
-                }
-            }
-        }
-        // the scales have arrived: with the first pass the codes' first stages
-        // may still be on their way, later ones were asked for before the scales
-        if (st0 == 0) cp_async_wait<kStages>();
-        else cp_async_wait<0>();
-        __syncthreads();
-
         for (int st = st0; st < min(nst, st0 + kPassK / kStageK); ++st) {
-            cp_async_wait<kStages - 1>();
+            cp_async_wait<kStages - 1>();             // this stage, and the first pass's scales before it
             __syncwarp();
-            const uint32_t stage = ring + (uint32_t)((st % kStages) * kStageBytes) + (uint32_t)(lr * 64 + lc * 4);
-            const uint32_t xst = xs + (uint32_t)((st - st0) * (kStageK / 32) * cols * 64 + lr * 64 + lc * 16);
-            const uint32_t srow = sc + (uint32_t)((warp * 32 + lr) * sp), zrow = zs + (uint32_t)((warp * 32 + lr) * zp);
+            const uint32_t stage = ring + (uint32_t)((st % kStages) * kStageBytes) + (uint32_t)(lr * 64 + ((lr >> 1) << 4) + lc * 4);
+            const int blocks = st == nst - 1 && tail ? tail : 4;  // 32-k blocks of this stage
+            const uint32_t srow = sc + (uint32_t)(lr * sp), zrow = zs + (uint32_t)(lr * zp);
             // block b of the stage: codes of rows lr + 8 r, X's columns
             auto block = [&](int b, bool first, const uint32_t (&z)[4]) {
                 uint32_t w[4];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) w[r] = lds32(stage + (uint32_t)(((b ^ (lr >> 1)) << 4) + r * 512));
+                for (int r = 0; r < 4; ++r) w[r] = shared_at<uint32_t>(smem, (stage ^ (uint32_t)(b << 4)) + (uint32_t)(r * 512));
                 uint4 x[NT];
 #pragma unroll
-                for (int t = 0; t < NT; ++t)
-                    x[t] = t * 8 + lr < cols ? lds128(xst + (uint32_t)((b * cols + t * 8) * 64)) : make_uint4(0, 0, 0, 0);
+                for (int t = 0; t < NT; ++t) x[t] = DIRECT ? pair_order(xn[t].x, xn[t].y, xn[t].z, xn[t].w) : xn[t];
+                load_x();
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     const uint32_t u = w[2 * i], v = w[2 * i + 1], zu = z[2 * i], zv = z[2 * i + 1];
@@ -372,7 +353,6 @@ __global__ void __launch_bounds__(32 * kWarps, 2) w4_kernel(const W4Args a)
                             total[i][t][e] = fmaf(part[i][t][e], s[2 * i + (e >> 1)], total[i][t][e]);
             };
             if constexpr (GB > 0) {
-                // what lies past the slice is zero codes, zero X and zero scales
                 constexpr int NG = 4 / GB;            // scale groups of the stage
                 const int go = GB == 4 ? (k0 + st * kStageK) / a.group - g0 : (st - st0) * NG;
                 float s[NG][4];
@@ -382,14 +362,14 @@ __global__ void __launch_bounds__(32 * kWarps, 2) w4_kernel(const W4Args a)
                     const uint32_t at = srow + (uint32_t)(r * 8 * sp + go * ssize);
                     uint32_t f[4];
                     if (a.s_f32) {
-                        if constexpr (NG == 4) { const uint4 v = lds128(at); f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w; }
-                        else if constexpr (NG == 2) { const uint2 v = lds64(at); f[0] = v.x; f[1] = v.y; }
-                        else f[0] = lds32(at);
+                        if constexpr (NG == 4) { const uint4 v = shared_at<uint4>(smem, at); f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w; }
+                        else if constexpr (NG == 2) { const uint2 v = shared_at<uint2>(smem, at); f[0] = v.x; f[1] = v.y; }
+                        else f[0] = shared_at<uint32_t>(smem, at);
                     } else {
                         uint2 v;
-                        if constexpr (NG == 4) v = lds64(at);
-                        else if constexpr (NG == 2) v.x = lds32(at);
-                        else v.x = lds16(at);
+                        if constexpr (NG == 4) v = shared_at<uint2>(smem, at);
+                        else if constexpr (NG == 2) v.x = shared_at<uint32_t>(smem, at);
+                        else v.x = shared_at<uint16_t>(smem, at);
                         f[0] = v.x << 16;
                         f[1] = v.x & 0xFFFF0000u;
                         f[2] = v.y << 16;
@@ -398,21 +378,30 @@ __global__ void __launch_bounds__(32 * kWarps, 2) w4_kernel(const W4Args a)
                     uint32_t q = 0x08080808u;
                     if (a.zeros) {
                         const uint32_t az = zrow + (uint32_t)(r * 8 * zp + go);
-                        q = (NG == 4 ? lds32(az) : NG == 2 ? lds16(az) : lds8(az)) & 0x0F0F0F0Fu;
+                        q = (NG == 4 ? shared_at<uint32_t>(smem, az) : NG == 2 ? (uint32_t)shared_at<uint16_t>(smem, az) : (uint32_t)smem[az]) & 0x0F0F0F0Fu;
                     }
 #pragma unroll
                     for (int n = 0; n < NG; ++n) {
                         s[n][r] = __uint_as_float(f[n]);
-                        z[n][r] = __byte_perm(q, 0x43434343u, 0x4040u + 0x0101u * n);      // 128 + z as a BF16 pair
+                        z[n][r] = __byte_perm(q, 0xC3C3C3C3u, 0x4040u + 0x0101u * n);      // -(128 + z) as a BF16 pair
                     }
                 }
+                if (blocks == 4) {
 #pragma unroll
-                for (int b = 0; b < 4; ++b) {
-                    block(b, b % GB == 0, z[b / GB]);
-                    if (b % GB == GB - 1) scale_up(s[b / GB]);
+                    for (int b = 0; b < 4; ++b) {
+                        block(b, b % GB == 0, z[b / GB]);
+                        if (b % GB == GB - 1) scale_up(s[b / GB]);
+                    }
+                } else {                              // (K may end within a stage, but not within a group)
+#pragma unroll
+                    for (int b = 0; b < 3; ++b) {
+                        if (b >= blocks) break;
+                        block(b, b % GB == 0, z[b / GB]);
+                        if (b % GB == GB - 1) scale_up(s[b / GB]);
+                    }
                 }
             } else {
-                const int kb0 = (k0 + st * kStageK) / 32, kb1 = min(kb0 + kStageK / 32, k1 / 32);
+                const int kb0 = (k0 + st * kStageK) / 32, kb1 = kb0 + blocks;
                 for (int kb = kb0; kb < kb1;) {
                     // the part of a scale group that this stage holds
                     const int gi = kb / gb, end = min(kb1, (gi + 1) * gb);
@@ -421,9 +410,9 @@ __global__ void __launch_bounds__(32 * kWarps, 2) w4_kernel(const W4Args a)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         const uint32_t at = srow + (uint32_t)(r * 8 * sp + (gi - g0) * ssize);
-                        s[r] = __uint_as_float(a.s_f32 ? lds32(at) : lds16(at) << 16);
-                        const uint32_t q = a.zeros ? lds8(zrow + (uint32_t)(r * 8 * zp + gi - g0)) & 15u : 8u;
-                        z[r] = __byte_perm(q, 0x43434343u, 0x4040u);
+                        s[r] = __uint_as_float(a.s_f32 ? shared_at<uint32_t>(smem, at) : (uint32_t)shared_at<uint16_t>(smem, at) << 16);
+                        const uint32_t q = a.zeros ? smem[zrow + (uint32_t)(r * 8 * zp + gi - g0)] & 15u : 8u;
+                        z[r] = __byte_perm(q, 0xC3C3C3C3u, 0x4040u);
                     }
 #pragma unroll
                     for (int i = 0; i < 2; ++i)
@@ -436,14 +425,14 @@ __global__ void __launch_bounds__(32 * kWarps, 2) w4_kernel(const W4Args a)
                 }
             }
             __syncwarp();
-            fetch(st + kStages);                      // into the stage just read
+            fetch();                                  // into the stage just read
         }
     }
     cp_async_wait<0>();
-    __syncwarp();
     __syncthreads();                                  // the rings are free: their memory takes the sums
 
-    // ---- sums of this CTA: [column][feature]
+    // ---- the warps' sums, [warp][column][feature]; added in warp order, slices of a
+    // row smallest first
     float *sums = reinterpret_cast<float *>(smem);
 #pragma unroll
     for (int i = 0; i < 2; ++i)
@@ -451,63 +440,41 @@ __global__ void __launch_bounds__(32 * kWarps, 2) w4_kernel(const W4Args a)
         for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const int c = t * 8 + lc * 2 + (e & 1), r = warp * 32 + i * 16 + lr + (e >> 1) * 8;
-                if (c < cols) sums[c * kRows + r] = total[i][t][e];
+                const int c = t * 8 + lc * 2 + (e & 1), r = i * 16 + lr + (e >> 1) * 8;
+                if (c < cols) sums[(warp * cols + c) * kRows + r] = total[i][t][e];
             }
-    __syncwarp();
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-    // ---- the cluster's sums in rank order, slices of a row smallest first
-    const int per = kRows / (int)ks;
-    for (int i = threadIdx.x; i < m * per; i += 32 * kWarps) {
-        const int t = i / per, r = (int)rank * per + i % per, n = n0 + r;
-        float v[8][S], y = 0.0f;
+    __syncthreads();
+    const int n = n0 + lane;
+    for (int t = warp; t < m; t += kWarps) {
+        float y = 0.0f;
+        for (int s = a.S - 1; s >= 0; --s)
 #pragma unroll
-        for (uint32_t c = 0; c < 8; ++c) {
-#pragma unroll
-            for (int s = 0; s < S; ++s) {
-                uint32_t at;
-                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;"
-                             : "=r"(at) : "r"(codes + (uint32_t)(((t * S + s) * kRows + r) * 4)), "r"(c < ks ? c : 0u));
-                v[c][s] = 0.0f;
-                if (c < ks) asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[c][s]) : "r"(at) : "memory");
-            }
-        }
-#pragma unroll
-        for (int c = 0; c < 8; ++c)
-#pragma unroll
-            for (int s = S - 1; s >= 0; --s) y = __fadd_rn(y, v[c][s]);
+            for (int w = 0; w < kWarps; ++w) y = __fadd_rn(y, sums[(w * cols + t * a.S + s) * kRows + lane]);
         if (n < a.N) {
             const int64_t o = (int64_t)(row0 + t) * a.ldy + n;
-            if (a.x_f32) static_cast<float *>(a.Y)[o] = y;
+            if (a.y_f32) static_cast<float *>(a.Y)[o] = y;
             else static_cast<uint16_t *>(a.Y)[o] = (uint16_t)bf16x2_rn(y, 0.0f);
         }
     }
-    __syncwarp();                                     // the others may still read this CTA's sums
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-template <int NT, bool F32X, int GB>
-cudaError_t run_w4(const W4Args &a, int64_t blocks, int64_t items, int ks, cudaStream_t st)
+template <int NT, bool DIRECT, int GB, int kWarps>
+cudaError_t run_w4(const W4Args &a, int64_t blocks, int64_t items, cudaStream_t st)
 {
-    auto kern = w4_kernel<NT, F32X, GB>;
-    // the codes' rings, X's columns for one pass (64 bytes per 32 k and column),
-    // the pass's scales and zero points
-    const int sm = kWarps * ring_stages(NT) * kStageBytes + pass_k(NT) / 32 * a.tokens * (F32X ? 3 : 1) * 64 +
-                   kRows * (a.sp + (a.zeros ? a.zp : 0));
+    auto kern = w4_kernel<NT, DIRECT, GB, kWarps>;
+    const int sm = kWarps * (kStages * kStageBytes + kRows * (a.sp + (a.zeros ? a.zp : 0)));
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, sm);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(blocks * ks), (unsigned)items);
+    cfg.gridDim = dim3((unsigned)blocks, (unsigned)items);
     cfg.blockDim = dim3(32 * kWarps);
     cfg.dynamicSmemBytes = (size_t)sm;
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)ks;
-    attr[0].val.clusterDim.y = 1;
-    attr[0].val.clusterDim.z = 1;
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = DIRECT ? 0 : 1;
     e = cudaLaunchKernelEx(&cfg, kern, a);
     if (e != cudaSuccess) return e;
     return cudaGetLastError();
@@ -515,42 +482,53 @@ cudaError_t run_w4(const W4Args &a, int64_t blocks, int64_t items, int ks, cudaS
 
 }  // namespace
 
+bool w4_direct(bool x_f32, const void *X, int64_t ldx)
+{
+    return !x_f32 && (reinterpret_cast<uintptr_t>(X) & 15u) == 0 && ldx % 8 == 0;
+}
+
+// planes: rows * K values of S = 3 (FP32) or 1 slices, unless w4_direct.
 cudaError_t launch_w4_matvec(bool x_f32, int64_t G, int64_t rows, int64_t N, int64_t K, int group, const void *X,
                              int64_t ldx, const uint8_t *q, const void *scales, bool s_f32, const uint8_t *zeros,
-                             const int32_t *ends, void *Y, int64_t ldy, cudaStream_t st)
+                             const int32_t *ends, void *Y, int64_t ldy, uint16_t *planes, cudaStream_t st)
 {
+    const bool direct = w4_direct(x_f32, X, ldx);
     W4Args a = {};
-    a.X = X; a.ldx = ldx; a.q = q; a.scales = scales; a.zeros = zeros; a.ends = ends; a.Y = Y; a.ldy = ldy;
+    a.X = direct ? X : planes; a.ldx = ldx; a.q = q; a.scales = scales; a.zeros = zeros; a.ends = ends; a.Y = Y; a.ldy = ldy;
     a.G = (int)G; a.rows = (int)rows; a.N = (int)N; a.K = (int)K; a.group = group;
-    a.x_f32 = x_f32 ? 1 : 0; a.s_f32 = s_f32 ? 1 : 0;
-    a.x_vec = (reinterpret_cast<uintptr_t>(X) & 15u) == 0 && ldx * (x_f32 ? 4 : 2) % 16 == 0;
+    a.S = x_f32 ? 3 : 1; a.y_f32 = x_f32 ? 1 : 0; a.s_f32 = s_f32 ? 1 : 0;
     // rows of X per item: up to 24 columns; an expert is expected to get up to
     // twice its share of the rows (one that gets more is read again)
-    const int S = x_f32 ? 3 : 1;
     const int64_t active = !ends ? 1 : (G < rows ? G : rows);
     int64_t want = ends ? 2 * ((rows + active - 1) / active) : rows;
     if (want > rows) want = rows;
-    int nt = (int)((want * S + 7) / 8);
-    nt = nt > 1 ? 3 : 1;
-    a.tokens = 8 * nt / S;
+    const int nt = want * a.S <= 8 ? 1 : 3;
+    a.tokens = 8 * nt / a.S;
     if (a.tokens > rows) a.tokens = (int)rows;
-    const int pass = pass_k(nt);
+    // where the CTAs fill the GPU, four small ones per SM overlap one's start with
+    // the others' products; few take more warps each
     const int64_t blocks = (N + kRows - 1) / kRows;
-    const int64_t items = ends ? active + rows / a.tokens + 1 : (rows + a.tokens - 1) / a.tokens;
-    if (items > 65535) return cudaErrorInvalidValue;
-    // slices of K: one pass each where 8 of them allow it, and more while there
-    // are fewer CTAs than SMs and each has 512 k
-    int ks = 1;
-    while (ks < 8 && (ks * pass < K || (blocks * active * ks < 152 && ks * 2 * 512 <= K))) ks *= 2;
-    const int64_t unit = K < (int64_t)ks * pass ? kStageK : pass;
-    a.slice = (int)((K + ks * unit - 1) / (ks * unit) * unit);
+    const int warps = blocks * active >= 2 * 152 ? 4 : 8;
+    a.slice = (int)((K + warps * kStageK - 1) / (warps * kStageK) * kStageK);
+    const int pass = a.slice < kPassK ? a.slice : kPassK;
     a.sp = meta_pitch(pass, group, a.slice, s_f32 ? 4 : 2);
     a.zp = meta_pitch(pass, group, a.slice, 1);
-#define EMU_W4(GB)                                                                                              \
-    (x_f32 ? (nt == 1 ? run_w4<1, true, GB>(a, blocks, items, ks, st) : run_w4<3, true, GB>(a, blocks, items, ks, st)) \
-           : (nt == 1 ? run_w4<1, false, GB>(a, blocks, items, ks, st) : run_w4<3, false, GB>(a, blocks, items, ks, st)))
+    const int64_t items = ends ? active + rows / a.tokens + 1 : (rows + a.tokens - 1) / a.tokens;
+    if (items > 65535) return cudaErrorInvalidValue;
+    if (!direct) {
+        const unsigned grid = (unsigned)((rows * (K / 8) + 255) / 256);
+        if (x_f32) w4_planes_kernel<true><<<grid, 256, 0, st>>>(X, ldx, (int)rows, (int)K, planes);
+        else w4_planes_kernel<false><<<grid, 256, 0, st>>>(X, ldx, (int)rows, (int)K, planes);
+        const cudaError_t e = cudaGetLastError();
+        if (e != cudaSuccess) return e;
+    }
+#define EMU_W4W(GB, W)                                                                                                  \
+    (direct ? (nt == 1 ? run_w4<1, true, GB, W>(a, blocks, items, st) : run_w4<3, true, GB, W>(a, blocks, items, st))   \
+            : (nt == 1 ? run_w4<1, false, GB, W>(a, blocks, items, st) : run_w4<3, false, GB, W>(a, blocks, items, st)))
+#define EMU_W4(GB) (warps == 4 ? EMU_W4W(GB, 4) : EMU_W4W(GB, 8))
     return group == 32 ? EMU_W4(1) : group == 64 ? EMU_W4(2) : group % 128 == 0 ? EMU_W4(4) : EMU_W4(0);
 #undef EMU_W4
+#undef EMU_W4W
 }
 
 }  // namespace emu

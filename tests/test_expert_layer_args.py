@@ -38,11 +38,13 @@ def test_argument_checks_need_no_gpu(lib):
     assert emu.emu_grouped_split_rows(0, 8, 8, P, 7, 8, None, P, 2, P, 8, P, 512, None) == 1
     # 4-bit weights
     w = emu.emu_w4_matvec
-    assert w(0, 1, 1, 8, 64, 48, P, 64, P, P, 0, None, None, P, 8, None) == 1         # group does not divide K
-    assert w(0, 1, 1, 8, 64, 16, P, 64, P, P, 0, None, None, P, 8, None) == 1         # group not a multiple of 32
-    assert w(0, 2, 1, 8, 64, 32, P, 64, P, P, 0, None, None, P, 8, None) == 1         # groups without ends
-    assert w(0, 1, 1, 8, 64, 32, P, 64, P + 4, P, 0, None, None, P, 8, None) == 2
-    assert w(0, 1, 1, 8, 64, 32, P, 63, P, P, 0, None, None, P, 8, None) == 1
+    assert w(0, 1, 1, 8, 64, 48, P, 64, P, P, 0, None, None, P, 8, P, 1 << 20, None) == 1         # group does not divide K
+    assert w(0, 1, 1, 8, 64, 16, P, 64, P, P, 0, None, None, P, 8, P, 1 << 20, None) == 1         # group not a multiple of 32
+    assert w(0, 2, 1, 8, 64, 32, P, 64, P, P, 0, None, None, P, 8, P, 1 << 20, None) == 1         # groups without ends
+    assert w(0, 1, 1, 8, 64, 32, P, 64, P + 4, P, 0, None, None, P, 8, P, 1 << 20, None) == 2
+    assert w(0, 1, 1, 8, 64, 32, P, 63, P, P, 0, None, None, P, 8, P, 1 << 20, None) == 1
+    assert w(0, 1, 2, 8, 64, 32, P, 64, P, P, 0, None, None, P, 8, P, 767, None) == 3          # room for two rows' slices
+    assert w(0, 1, 2, 8, 64, 32, P, 64, P, P, 0, None, None, P, 8, None, 0, None) == 1
     # routing
     assert emu.emu_route(0, 4, 8, 9, 1, P, 8, P, P, P, P, P, P, big, None) == 1       # k > E
     assert emu.emu_route(0, 4, 2000, 2, 1, P, 2000, P, P, P, P, P, P, big, None) == 5
