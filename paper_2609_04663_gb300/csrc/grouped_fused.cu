@@ -78,7 +78,9 @@ grouped_fused_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_const
         tma_prefetch_desc(&tmS);
     }
     if (warp == kSplitWarps + 1) { tmem_alloc(smem_u32((const void *)tmem_slot), 512); tmem_relinquish(); }
-    griddep_wait();
+    // launched as the programmatic dependent of the kernel that splits the rows,
+    // which itself started after everything before it: only the rows' planes have
+    // to be waited for (below)
     if (load_groups(a.ends, a.G, a.rows, starts) && blockIdx.x == 0 && threadIdx.x == 0)
         atomicOr(flags, (uint32_t)EMU_FLAG_INDEX);
     const int nlt = (a.L + kLRows - 1) / kLRows;
@@ -165,6 +167,7 @@ grouped_fused_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_const
         if (!ok) drain_inflight(wfull0, Cfg::W_STAGES, i, flags);
     } else if (warp == kSplitWarps && lane == 0) {
         // ---------------- TMA: the rows' planes
+        griddep_wait();
         long issued = 0;
         int s = 0;
         uint32_t ph = 0;

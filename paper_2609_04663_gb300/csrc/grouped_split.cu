@@ -83,6 +83,7 @@ template <int S, bool TOKENS>
 __global__ void __launch_bounds__(kThreads) grouped_split_kernel(const SplitArgs a)
 {
     extern __shared__ int starts[];
+    griddep_launch_dependents();              // a product launched as this kernel's dependent sets itself up meanwhile
     const int esize = S == 3 ? 4 : 2;
     int64_t nrows = a.rows;
     int total = 0;
