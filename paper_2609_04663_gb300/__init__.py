@@ -496,7 +496,7 @@ def grouped_split(X, ends=None, src=None, planes=None, ws=None, stream=None):
         if X.dim() != 2:
             _bad(where, "token rows are [rows, cols]")
         G, rows = ends.numel(), (src.numel() if src is not None else X.shape[0])
-        shape, prows = (rows, cols), emu_grouped_plane_rows(rows, G)
+        shape, prows = (rows, cols), _lib.emu_grouped_plane_rows(rows, G)
     if planes is None:
         planes = _empty((S, prows, ld), torch.int16, dev, stream)
     elif planes.shape != (S, prows, ld) or planes.dtype is not torch.int16 or not planes.is_contiguous():

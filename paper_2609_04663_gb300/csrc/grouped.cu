@@ -80,8 +80,7 @@ grouped_kernel(const __grid_constant__ CUtensorMap tmL, const __grid_constant__ 
     // the set-up above overlaps the end of the kernel before this one when it
     // is launched as its programmatic dependent
     griddep_wait();
-    if (load_groups(a.ends, a.G, a.rows, starts) && blockIdx.x == 0 && threadIdx.x == 0)
-        atomicOr(flags, (uint32_t)EMU_FLAG_INDEX);
+    groups_and_flags(a, starts);
     constexpr int LT = kLRows * Cfg::CTAS;
     const int nlt = (a.L + LT - 1) / LT;
     int total;
@@ -307,7 +306,7 @@ cudaError_t run_grouped(const CUtensorMap &tl, const CUtensorMap &tc, const CUte
                         int64_t tiles, cudaStream_t st)
 {
     using Cfg = GroupedCfg<S, BC, PAIR>;
-    return launch_persistent(grouped_kernel<BC, PAIR, LMN, CMN>, Cfg::SMEM, Cfg::THREADS, Cfg::CTAS, tiles, st, tl, tc, ts, a);
+    return launch_persistent<grouped_kernel<BC, PAIR, LMN, CMN>>(Cfg::SMEM, Cfg::THREADS, Cfg::CTAS, tiles, st, tl, tc, ts, a);
 }
 
 // Whether 256 x 256 tiles on CTA pairs are estimated faster than 128 x 64 tiles
@@ -357,22 +356,23 @@ cudaError_t gradient(const GroupedOperand &A, const GroupedOperand &B, GroupedAr
 
 cudaError_t launch_grouped_product(int nslices, bool trans, int64_t G, int64_t rows, int64_t N, int64_t K,
                                    const GroupedOperand &X, const GroupedOperand &W, const int32_t *ends, void *Y,
-                                   bool y_f32, int64_t ldy, uint32_t *flags, cudaStream_t st)
+                                   bool y_f32, int64_t ldy, uint32_t *flags, bool own_flags, cudaStream_t st)
 {
     GroupedArgs a = {};
     a.ends = ends; a.G = (int)G; a.rows = (int)rows; a.L = (int)N; a.K = (int)K; a.padded = X.padded ? 1 : 0;
-    a.out = Y; a.ldo = ldy; a.out_f32 = y_f32 ? 1 : 0; a.flags = flags;
+    a.out = Y; a.ldo = ldy; a.out_f32 = y_f32 ? 1 : 0; a.flags = flags; a.own_flags = own_flags ? 1 : 0;
     if (nslices == 1) return launch_bf16_product(trans, X, W, a, st);
     return trans ? product<false>(X, W, a, st) : product<true>(X, W, a, st);
 }
 
 cudaError_t launch_grouped_gradient(int nslices, int64_t G, int64_t rows, int64_t M, int64_t N, const GroupedOperand &A,
                                     const GroupedOperand &B, const int32_t *ends, void *D, bool d_f32, int64_t ldd,
-                                    int64_t strided, uint32_t *flags, cudaStream_t st)
+                                    int64_t strided, uint32_t *flags, bool own_flags, cudaStream_t st)
 {
     GroupedArgs a = {};
     a.ends = ends; a.G = (int)G; a.rows = (int)rows; a.L = (int)N; a.C = (int)M;
     a.out = D; a.ldo = ldd; a.strideo = strided; a.out_f32 = d_f32 ? 1 : 0; a.flags = flags;
+    a.own_flags = own_flags ? 1 : 0;
     return nslices == 1 ? launch_bf16_gradient(A, B, a, st) : gradient(A, B, a, st);
 }
 

@@ -15,7 +15,6 @@ bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) ==
 bool fits(const void *p, int type) { return (reinterpret_cast<uintptr_t>(p) & (type == EMU_F32 ? 3u : 1u)) == 0; }
 emu_status cuda_status(cudaError_t e) { return e == cudaSuccess ? EMU_OK : EMU_ERR_CUDA; }
 int64_t plane_ld(int64_t cols) { return round_up(cols < 1 ? 1 : cols, 8); }
-int slices(int dtype) { return dtype == EMU_F32 ? 3 : 1; }
 bool known(int dtype) { return dtype == EMU_F32 || dtype == EMU_BF16; }
 
 emu_status check_ws(void *ws, size_t ws_bytes, size_t need)
@@ -59,13 +58,13 @@ cudaError_t zero_rows(void *p, int64_t rows, int64_t cols, int64_t ld, int esize
 
 emu_status product(int S, int opW, int64_t G, int64_t rows, int64_t N, int64_t K, const GroupedOperand &X,
                    const GroupedOperand &W, const int32_t *ends, void *Y, int ytype, int64_t ldy, uint32_t *flags,
-                   cudaStream_t st)
+                   bool own_flags, cudaStream_t st)
 {
     const int esize = ytype == EMU_F32 ? 4 : 2;
     if (rows == 0 || N == 0) return EMU_OK;
     if (K == 0) return cuda_status(zero_rows(Y, rows, N, ldy, esize, st));
     return cuda_status(launch_grouped_product(S, opW == EMU_OP_T, G, rows, N, K, X, W, ends, Y, ytype == EMU_F32, ldy,
-                                              flags, st));
+                                              flags, own_flags, st));
 }
 
 }  // namespace
@@ -148,12 +147,13 @@ emu_status emu_grouped_prodsum(int nslices, int opW, int64_t G, int64_t rows, in
     s = check_ws(ws, ws_bytes, kWsHeaderBytes);
     if (s != EMU_OK) return s;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-    if (clear_flags(ws, st) != cudaSuccess) return EMU_ERR_CUDA;
+    const bool runs = rows > 0 && N > 0 && K > 0;     // the kernel then sets the flag word itself
+    if (!runs && clear_flags(ws, st) != cudaSuccess) return EMU_ERR_CUDA;
     GroupedOperand X, W;
     X.planes = Xcomps; X.rows = padded ? padded_rows(rows, G) : rows; X.ld = ldx; X.plane = X.rows * ldx;
     X.padded = padded != 0;
     W.planes = Wcomps; W.ld = ldw; W.stride = stridew; W.plane = G * wrows * ldw;
-    return product(nslices, opW, G, rows, N, K, X, W, ends, Y, ytype, ldy, &static_cast<WsHeader *>(ws)->flags, st);
+    return product(nslices, opW, G, rows, N, K, X, W, ends, Y, ytype, ldy, &static_cast<WsHeader *>(ws)->flags, true, st);
 }
 
 size_t emu_grouped_gemm_workspace_bytes(int dtype, int64_t G, int64_t rows, int64_t N, int64_t K)
@@ -197,7 +197,7 @@ emu_status emu_grouped_gemm_f32(int opW, int64_t G, int64_t rows, int64_t N, int
         if (e == cudaSuccess) e = launch_grouped_split(true, G, wrows, wcols, W, ldw, stridew, wp, wo.ld, flags, st);
         if (e != cudaSuccess) return EMU_ERR_CUDA;
     }
-    return product(3, opW, G, rows, N, K, xo, wo, ends, Y, EMU_F32, ldy, flags, st);
+    return product(3, opW, G, rows, N, K, xo, wo, ends, Y, EMU_F32, ldy, flags, false, st);
 }
 
 emu_status emu_grouped_prodsum_wgrad(int nslices, int64_t G, int64_t rows, int64_t M, int64_t N,
@@ -222,7 +222,7 @@ emu_status emu_grouped_prodsum_wgrad(int nslices, int64_t G, int64_t rows, int64
     s = check_ws(ws, ws_bytes, kWsHeaderBytes);
     if (s != EMU_OK) return s;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-    if (clear_flags(ws, st) != cudaSuccess) return EMU_ERR_CUDA;
+    if ((M == 0 || N == 0 || rows == 0) && clear_flags(ws, st) != cudaSuccess) return EMU_ERR_CUDA;
     if (M == 0 || N == 0) return EMU_OK;
     if (rows == 0) {
         for (int64_t g = 0; g < G; ++g) {
@@ -238,7 +238,7 @@ emu_status emu_grouped_prodsum_wgrad(int nslices, int64_t G, int64_t rows, int64
     B.planes = Bcomps; B.padded = bpadded != 0; B.rows = bpadded ? padded_rows(rows, G) : rows; B.ld = ldb;
     B.plane = B.rows * ldb;
     return cuda_status(launch_grouped_gradient(nslices, G, rows, M, N, A, B, ends, D, dtype == EMU_F32, ldd, strided,
-                                               &static_cast<WsHeader *>(ws)->flags, st));
+                                               &static_cast<WsHeader *>(ws)->flags, true, st));
 }
 
 size_t emu_w4_workspace_bytes(int dtype, int64_t rows, int64_t K)

@@ -141,8 +141,7 @@ grouped_bf16_kernel(const __grid_constant__ CUtensorMap tmL, const __grid_consta
     // the set-up above overlaps the end of the kernel before this one when it
     // is launched as its programmatic dependent
     griddep_wait();
-    if (load_groups(a.ends, a.G, a.rows, starts) && blockIdx.x == 0 && threadIdx.x == 0)
-        atomicOr(flags, (uint32_t)EMU_FLAG_INDEX);
+    groups_and_flags(a, starts);
     constexpr int LT = kLRows * Cfg::CTAS;
     const int nlt = (a.L + LT - 1) / LT;
     int total;
@@ -399,8 +398,8 @@ cudaError_t run_bf16(const CUtensorMap &tl, const CUtensorMap &tc, const CUtenso
                      cudaStream_t st)
 {
     using Cfg = Bf16Cfg<BC, PAIR>;
-    return launch_persistent(grouped_bf16_kernel<BC, PAIR, LMN, CMN>, Cfg::SMEM, Cfg::THREADS + (CMN ? 32 : 0),
-                             Cfg::CTAS, tiles, st, tl, tc, ts, a);
+    return launch_persistent<grouped_bf16_kernel<BC, PAIR, LMN, CMN>>(Cfg::SMEM, Cfg::THREADS + (CMN ? 32 : 0), Cfg::CTAS,
+                                                                      tiles, st, tl, tc, ts, a);
 }
 
 // Columns of the tiles for G results of n columns x L features on average: pairs

@@ -81,8 +81,7 @@ grouped_fused_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_const
     // launched as the programmatic dependent of the kernel that splits the rows,
     // which itself started after everything before it: only the rows' planes have
     // to be waited for (below)
-    if (load_groups(a.ends, a.G, a.rows, starts) && blockIdx.x == 0 && threadIdx.x == 0)
-        atomicOr(flags, (uint32_t)EMU_FLAG_INDEX);
+    groups_and_flags(a, starts);
     const int nlt = (a.L + kLRows - 1) / kLRows;
     if (warp == kSplitWarps) tile_prefix(starts, a.G, COLS, nlt, tpre);
     tc_fence_before();
@@ -296,7 +295,7 @@ cudaError_t run_fused(const CUtensorMap &tw, const CUtensorMap &tc, const CUtens
                       int64_t tiles, cudaStream_t st)
 {
     using Cfg = FusedCfg<COLS>;
-    return launch_persistent(grouped_fused_kernel<COLS, LMN>, Cfg::SMEM, Cfg::THREADS, 1, tiles, st, tw, tc, ts, a);
+    return launch_persistent<grouped_fused_kernel<COLS, LMN>>(Cfg::SMEM, Cfg::THREADS, 1, tiles, st, tw, tc, ts, a);
 }
 
 // Tensor map over G FP32 matrices of rows x inner, box box_inner x box_rows.

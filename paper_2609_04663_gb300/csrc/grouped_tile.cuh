@@ -3,6 +3,8 @@
 // the stores of an epilogue warp.  Each translation unit gets its own copies
 // (unnamed namespace).
 #pragma once
+#include <atomic>
+
 #include "gemm_common.cuh"
 #include "grouped_common.cuh"
 #include "launchers.cuh"
@@ -24,6 +26,7 @@ struct GroupedArgs {
     int out_f32;
     int lwide, cwide;      // the MN-major operand's tensor map loads two blocks of 64 at once
     uint32_t *flags;
+    int own_flags;         // the flag word is this kernel's alone: it is set, not added to
 };
 
 // BF16 operands (grouped_bf16.cu).
@@ -254,6 +257,18 @@ __device__ __forceinline__ void store_columns(const T (&v)[32], int cols, void *
     }
 }
 
+// The groups' bounds, and what their check says in the flag word.  All CTAs see
+// the same bounds; one reports.  A kernel that owns the word clears it this way
+// too: the only other flag, a wait that gave up, comes seconds later.
+__device__ __forceinline__ void groups_and_flags(const GroupedArgs &a, int *starts)
+{
+    const bool bad = load_groups(a.ends, a.G, a.rows, starts);
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        if (a.own_flags) *a.flags = bad ? (uint32_t)EMU_FLAG_INDEX : 0u;
+        else if (bad) atomicOr(a.flags, (uint32_t)EMU_FLAG_INDEX);
+    }
+}
+
 // First tile of every group (tpre[G]: all tiles), for groups of n rows in
 // column tiles of bc rows and nlt feature tiles; one warp.
 __device__ __forceinline__ void tile_prefix(const int *starts, int G, int bc, int nlt, int *tpre)
@@ -318,21 +333,39 @@ bool make_group_map(CUtensorMap *map, const uint16_t *p, int64_t inner, int64_t 
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// SMs of the current device (asked for once per device).
 int sm_count()
 {
+    static std::atomic<int> known[64];
     int dev = 0, sms = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess ||
-        cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sms < 2)
-        sms = 152;
+    if (cudaGetDevice(&dev) != cudaSuccess) return 152;
+    if (dev >= 0 && dev < 64 && (sms = known[dev].load(std::memory_order_relaxed)) > 0) return sms;
+    if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sms < 2) return 152;
+    if (dev >= 0 && dev < 64) known[dev].store(sms, std::memory_order_relaxed);
     return sms;
+}
+
+// Lets a kernel take `smem` bytes of dynamic shared memory (set once per device).
+template <auto KERN>
+cudaError_t allow_smem(int smem)
+{
+    static std::atomic<uint64_t> done{0};
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const uint64_t bit = dev >= 0 && dev < 64 ? 1ull << dev : 0ull;
+    if (done.load(std::memory_order_relaxed) & bit) return cudaSuccess;
+    e = cudaFuncSetAttribute(KERN, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+    return e;
 }
 
 // A persistent launch: one CTA (or cluster of `ctas`) per SM (pair), no more
 // than there are tiles, as a programmatic dependent of the kernel before it.
-template <typename Kernel, typename... Args>
-cudaError_t launch_persistent(Kernel kern, int smem, int threads, int ctas, int64_t tiles, cudaStream_t st, const Args &...args)
+template <auto KERN, typename... Args>
+cudaError_t launch_persistent(int smem, int threads, int ctas, int64_t tiles, cudaStream_t st, const Args &...args)
 {
-    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    cudaError_t e = allow_smem<KERN>(smem);
     if (e != cudaSuccess) return e;
     int64_t units = sm_count() / ctas;
     if (units > tiles) units = tiles < 1 ? 1 : tiles;
@@ -350,7 +383,7 @@ cudaError_t launch_persistent(Kernel kern, int smem, int threads, int ctas, int6
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = ctas > 1 ? 2 : 1;
-    e = cudaLaunchKernelEx(&cfg, kern, args...);
+    e = cudaLaunchKernelEx(&cfg, KERN, args...);
     if (e != cudaSuccess) return e;
     return cudaGetLastError();
 }

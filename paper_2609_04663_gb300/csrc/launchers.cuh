@@ -146,9 +146,10 @@ cudaError_t launch_grouped_split(bool f32, int64_t G, int64_t rows, int64_t cols
 cudaError_t launch_grouped_split_rows(bool f32, int64_t rows, int64_t cols, const void *X, int64_t xrows,
                                       int64_t ldx, const int32_t *src, const int32_t *ends, int64_t G,
                                       uint16_t *comps, int64_t ldcomp, uint32_t *flags, cudaStream_t st);
+// own_flags: nothing else sets the flag word (the kernel clears it).
 cudaError_t launch_grouped_product(int nslices, bool trans, int64_t G, int64_t rows, int64_t N, int64_t K,
                                    const GroupedOperand &X, const GroupedOperand &W, const int32_t *ends, void *Y,
-                                   bool y_f32, int64_t ldy, uint32_t *flags, cudaStream_t st);
+                                   bool y_f32, int64_t ldy, uint32_t *flags, bool own_flags, cudaStream_t st);
 // FP32 weights that meet few rows each, split inside the product
 // (grouped_fused.cu); fused_takes: whether their rows can be read by TMA;
 // kFusedRows: up to so many rows for each group on average that is the faster way.
@@ -159,7 +160,7 @@ cudaError_t launch_grouped_fused(bool trans, int64_t G, int64_t rows, int64_t N,
 constexpr int64_t kFusedRows = 127;
 cudaError_t launch_grouped_gradient(int nslices, int64_t G, int64_t rows, int64_t M, int64_t N, const GroupedOperand &A,
                                     const GroupedOperand &B, const int32_t *ends, void *D, bool d_f32, int64_t ldd,
-                                    int64_t strided, uint32_t *flags, cudaStream_t st);
+                                    int64_t strided, uint32_t *flags, bool own_flags, cudaStream_t st);
 
 // Matrix-vector products with 4-bit weights (w4.cu), routing and the weighted
 // sum of answers (route.cu).

@@ -461,9 +461,9 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps) w4_kernel(const W4Ar
 template <int NT, bool DIRECT, int GB, int kWarps>
 cudaError_t run_w4(const W4Args &a, int64_t blocks, int64_t items, cudaStream_t st)
 {
-    auto kern = w4_kernel<NT, DIRECT, GB, kWarps>;
+    constexpr auto kern = w4_kernel<NT, DIRECT, GB, kWarps>;
     const int sm = kWarps * (kStages * kStageBytes + kRows * (a.sp + (a.zeros ? a.zp : 0)));
-    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, sm);
+    cudaError_t e = sm > 48 * 1024 ? cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, sm) : cudaSuccess;
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)blocks, (unsigned)items);
