@@ -516,7 +516,7 @@ def grouped_split(X, ends=None, src=None, planes=None, ws=None, stream=None):
 def _tma_ok(t, pitch):
     """Whether a BF16 tensor can be read by the tensor memory accelerator as it stands."""
     return (t.data_ptr() % 16 == 0 and pitch % 8 == 0 and
-            (t.dim() < 3 or t.shape[0] <= 1 or (t.stride(0) % 8 == 0 and t.stride(0) >= 0)))
+            (t.dim() < 3 or t.shape[0] <= 1 or (t.stride(0) % 8 == 0 and t.stride(0) >= t.shape[1] * pitch)))
 
 
 def grouped_workspace(X, W, ends, opW: int = OP_N, src=None, train: bool = False):

@@ -138,7 +138,7 @@ emu_status emu_grouped_prodsum(int nslices, int opW, int64_t G, int64_t rows, in
         if (K > 0) {
             // slices of the weights are planes of G dense matrices
             if (nslices == 3 && G > 1 && stridew != wrows * ldw) return EMU_ERR_INVALID_ARG;
-            if (G > 1 && stridew < 0) return EMU_ERR_INVALID_ARG;
+            if (G > 1 && stridew < (wrows - 1) * ldw + wcols) return EMU_ERR_INVALID_ARG;      // matrices overlap
             s = check_planes(Xcomps, ldx, K, 0);
             if (s == EMU_OK) s = check_planes(Wcomps, ldw, wcols, G > 1 ? stridew : 0);
             if (s != EMU_OK) return s;

@@ -24,12 +24,9 @@ constexpr int kRouteThreads = 1024, kRouteWarps = kRouteThreads / 32, kRouteBloc
 __device__ __forceinline__ float bf16_f32(uint32_t b) { return __uint_as_float(b << 16); }
 __device__ __forceinline__ uint16_t f32_bf16(float x) { return (uint16_t)bf16x2_rn(x, 0.0f); }
 
-// A logit as the softmax sees it: NaN counts as minus infinity.
 __device__ __forceinline__ float load_logit(const void *row, int e, bool f32)
 {
-    const float x = f32 ? __ldg(static_cast<const float *>(row) + e)
-                        : bf16_f32(__ldg(static_cast<const uint16_t *>(row) + e));
-    return x;
+    return f32 ? __ldg(static_cast<const float *>(row) + e) : bf16_f32(__ldg(static_cast<const uint16_t *>(row) + e));
 }
 
 // Order-preserving key of a logit, never 0: negative zero like zero, NaN like

@@ -225,3 +225,60 @@ def test_another_stream(dev):
     got = emu.grouped_gemm(X, W, ends, src=src, stream=s)[0]
     s.synchronize()
     assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("rows_each", [3, 40, 200])
+def test_shared_weights_of_all_groups(dev, dtype, rows_each):
+    """One matrix expanded over the groups (distance 0) is the plain product."""
+    import torch
+    dt = getattr(torch, dtype)
+    sizes = [rows_each, 0, rows_each + 1]
+    X, W, dY, ends, _ = make(dev, sizes, 64, 80, dt, 10)
+    Ws = W[:1].expand(3, 64, 80)
+    (Y, dX, _), (aY, aX, _) = reference(X, Ws, dY, sizes, False)
+    y, _ = emu.grouped_gemm(X, Ws, ends)
+    dx, _ = emu.grouped_gemm(dY, Ws, ends, opW=emu.OP_T)
+    assert within(y, Y, aY, 64, dtype == "float32") and within(dx, dX, aX, 80, dtype == "float32")
+
+
+@pytest.mark.parametrize("rows", [8, 5120])
+def test_weights_past_4_gib(dev, rows):
+    """The last group's matrix lies past 2^32 bytes."""
+    import torch
+    G, K, N = 40, 8192, 8192
+    W = torch.zeros(G, K, N, dtype=torch.bfloat16, device=dev)
+    W[-1].normal_(generator=torch.Generator(device=dev).manual_seed(11))
+    X = torch.randn(rows, K, device=dev, generator=torch.Generator(device=dev).manual_seed(12)).bfloat16()
+    ends = torch.zeros(G, dtype=torch.int32, device=dev)
+    ends[-1] = rows
+    y, ws = emu.grouped_gemm(X, W, ends)
+    one, _ = emu.grouped_gemm(X, W[-1:], ends[-1:])
+    assert emu.read_flags(ws) == 0
+    assert float((y.float() - one.float()).abs().max()) <= 2.0 ** -8 * float(one.float().abs().max())
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("seed", range(6))
+def test_random_shapes(dev, dtype, seed):
+    """Sizes, orders and paths at random: few and many rows, odd widths, gathers."""
+    import torch
+    rng = np.random.default_rng(100 + seed)
+    G = int(rng.integers(1, 12))
+    sizes = [int(v) for v in rng.integers(0, [4, 70, 600][seed % 3], G)]
+    K, N = (int(v) for v in rng.integers(1, 700, 2))
+    if seed % 2:
+        K, N = K // 8 * 8 + 8, N // 64 * 64 + 64
+    trans = bool(rng.integers(0, 2))
+    dt = getattr(torch, dtype)
+    X, W, dY, ends, src = make(dev, sizes, K, N, dt, seed, tail=int(rng.integers(0, 3)), trans=trans, gather=seed % 2 == 0)
+    Xg = X[src.long()] if src is not None else X
+    (Y, dX, dW), (aY, aX, aW) = reference(Xg, W, dY, sizes, trans)
+    op, back = (emu.OP_T, emu.OP_N) if trans else (emu.OP_N, emu.OP_T)
+    f32 = dtype == "float32"
+    if dY.shape[0] == 0:
+        return
+    assert within(emu.grouped_gemm(X, W, ends, opW=op, src=src)[0], Y, aY, K, f32)
+    assert within(emu.grouped_gemm(dY, W, ends, opW=back)[0], dX, aX, N, f32)
+    dw = emu.grouped_wgrad(dY, X, ends, srcB=src)[0] if trans else emu.grouped_wgrad(X, dY, ends, srcA=src)[0]
+    assert within(dw, dW, aW, max(sizes + [1]), f32)

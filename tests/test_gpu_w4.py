@@ -133,3 +133,46 @@ def test_empty(dev):
     import torch
     X, q, s, z = make(dev, 0, 16, 32, 32, torch.float32, False)
     assert emu.w4_matvec(X, q, s).shape == (0, 16)
+
+
+def test_weights_past_4_gib(dev):
+    import torch
+    G, N, K = 80, 8192, 16384
+    q = torch.zeros(G, N, K // 2, dtype=torch.uint8, device=dev)
+    q[-1].random_(0, 256, generator=torch.Generator(device=dev).manual_seed(7))
+    s = torch.ones(G, N, K // 128, device=dev)
+    X = torch.randn(2, K, device=dev, generator=torch.Generator(device=dev).manual_seed(8))
+    ends = torch.zeros(G, dtype=torch.int32, device=dev)
+    ends[-1] = 2
+    # the file's bound: the number of experts changes how K is cut, so last bits may differ from one matrix's
+    assert check(emu.w4_matvec(X, q, s, ends=ends), X, weights(q[-1], s[-1], None, 128))
+
+
+@pytest.mark.parametrize("seed", range(8))
+def test_random_shapes(dev, seed):
+    import torch
+    rng = __import__("random").Random(seed)
+    group = rng.choice((32, 64, 96, 128, 160, 256, 512))
+    K, N, G = group * rng.randint(1, max(1, 5000 // group)), rng.randint(1, 700), rng.choice((0, 0, 7))
+    rows = rng.randint(1, 30)
+    dt = rng.choice((torch.float32, torch.bfloat16))
+    X, q, s, z = make(dev, rows, N, K, group, dt, rng.random() < 0.5, G=G, seed=seed)
+    if not G:
+        assert check(emu.w4_matvec(X, q, s, zeros=z), X, weights(q, s, z, group))
+        return
+    cuts = sorted(rng.randint(0, rows) for _ in range(G - 1)) + [rows]
+    Y = emu.w4_matvec(X, q, s, zeros=z, ends=torch.tensor(cuts, dtype=torch.int32, device=dev))
+    for g, (a, b) in enumerate(zip([0] + cuts, cuts)):
+        if b > a:
+            assert check(Y[a:b], X[a:b], weights(q[g], s[g], z[g] if z is not None else None, group))
+
+
+def test_another_stream(dev):
+    import torch
+    X, q, s, z = make(dev, 3, 200, 512, 64, torch.float32, True, seed=9)
+    want = emu.w4_matvec(X, q, s, zeros=z)
+    st = torch.cuda.Stream()
+    st.wait_stream(torch.cuda.current_stream())
+    got = emu.w4_matvec(X, q, s, zeros=z, stream=st)
+    st.synchronize()
+    assert torch.equal(got, want)
