@@ -1,9 +1,10 @@
 """GB300-native BF16 component-product GEMM emulation (arXiv 2609.04663).
 
-Thin ctypes binding over the C-ABI of ``include/emu.h`` (library
-``_emu.so`` built in-tree by ``_build.py``).  The functions named ``emu_*``
-take plain integers (device pointers, sizes, the raw CUDA stream handle) and
-return the ``emu_status`` code, exactly as the C entry points do.  The
+Thin ctypes binding over the C-ABI of ``include/emu.h`` and
+``include/emu_experts.h`` (library ``_emu.so`` built in-tree by
+``_build.py``).  The functions named ``emu_*`` take plain integers (device
+pointers, sizes, the raw CUDA stream handle) and return the ``emu_status``
+code, exactly as the C entry points do.  The
 tensor-level helpers below them only allocate device memory with PyTorch and
 marshal pointers: every step of the method runs in the CUDA kernels.
 
@@ -118,7 +119,7 @@ def _mk(name):
     def f(*args):
         return getattr(load(), name)(*args)
     f.__name__ = name
-    f.__doc__ = f"C-ABI ``{name}`` (include/emu.h); returns its result unchanged."
+    f.__doc__ = f"C-ABI ``{name}`` (declared under include/); returns its result unchanged."
     return f
 
 

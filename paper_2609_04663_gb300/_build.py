@@ -32,7 +32,7 @@ def _nvcc() -> str:
 
 def _deps():
     files = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".cu", ".cuh"))]
-    files.append(os.path.join(INCLUDE, "emu.h"))
+    files += [os.path.join(INCLUDE, f) for f in ("emu.h", "emu_experts.h")]
     return files
 
 

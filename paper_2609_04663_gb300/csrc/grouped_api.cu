@@ -1,7 +1,7 @@
 // C-ABI of the products grouped by expert (declared in include/emu.h):
 // argument checks, workspace layout and launch sequences.
 #include "grouped_common.cuh"
-#include "launchers.cuh"
+#include "expert_launchers.cuh"
 
 using namespace emu;
 

@@ -3,6 +3,7 @@
 // limits.
 #pragma once
 
+#include "../../include/emu_experts.h"
 #include "common.cuh"
 
 namespace emu {

@@ -12,7 +12,7 @@
 // element.  One warp takes a row, a lane 8 consecutive elements per step
 // (two 16-byte loads, one 16-byte store per plane).
 #include "grouped_common.cuh"
-#include "launchers.cuh"
+#include "expert_launchers.cuh"
 #include "split_f32_pair.cuh"
 
 namespace emu {

@@ -7,7 +7,7 @@
 
 #include "gemm_common.cuh"
 #include "grouped_common.cuh"
-#include "launchers.cuh"
+#include "expert_launchers.cuh"
 #include "pair_common.cuh"
 
 #pragma nv_diag_suppress 177      // helpers a translation unit does not use

@@ -132,52 +132,4 @@ cudaError_t launch_axpby_f32(const float *P, int64_t ldp, float *C, int64_t ldc,
 cudaError_t launch_axpby_f64(const double *P, int64_t ldp, double *C, int64_t ldc, int64_t M, int64_t N,
                              double alpha, double beta, cudaStream_t st);
 
-// Products grouped by expert (grouped.cu).  One operand as planes: S planes
-// `plane` elements apart, row pitch ld; weights: matrices `stride` elements
-// apart; token rows: `rows` plane rows, `padded` when each group starts at
-// padded_start (grouped_common.cuh) and ends in zero rows.
-struct GroupedOperand {
-    const uint16_t *planes = nullptr;
-    int64_t rows = 0, ld = 0, stride = 0, plane = 0;
-    bool padded = false;       // (three planes of a gradient's operands: always)
-};
-cudaError_t launch_grouped_split(bool f32, int64_t G, int64_t rows, int64_t cols, const void *X, int64_t ldx,
-                                 int64_t stride, uint16_t *comps, int64_t ldcomp, uint32_t *flags, cudaStream_t st);
-cudaError_t launch_grouped_split_rows(bool f32, int64_t rows, int64_t cols, const void *X, int64_t xrows,
-                                      int64_t ldx, const int32_t *src, const int32_t *ends, int64_t G,
-                                      uint16_t *comps, int64_t ldcomp, uint32_t *flags, cudaStream_t st);
-// own_flags: nothing else sets the flag word (the kernel clears it).
-cudaError_t launch_grouped_product(int nslices, bool trans, int64_t G, int64_t rows, int64_t N, int64_t K,
-                                   const GroupedOperand &X, const GroupedOperand &W, const int32_t *ends, void *Y,
-                                   bool y_f32, int64_t ldy, uint32_t *flags, bool own_flags, cudaStream_t st);
-// FP32 weights that meet few rows each, split inside the product
-// (grouped_fused.cu); fused_takes: whether their rows can be read by TMA;
-// kFusedRows: up to so many rows for each group on average that is the faster way.
-bool fused_takes(const float *W, int64_t G, int64_t ldw, int64_t stridew);
-cudaError_t launch_grouped_fused(bool trans, int64_t G, int64_t rows, int64_t N, int64_t K, const GroupedOperand &X,
-                                 const float *W, int64_t ldw, int64_t stridew, const int32_t *ends, float *Y,
-                                 int64_t ldy, uint32_t *flags, cudaStream_t st);
-constexpr int64_t kFusedRows = 127;
-cudaError_t launch_grouped_gradient(int nslices, int64_t G, int64_t rows, int64_t M, int64_t N, const GroupedOperand &A,
-                                    const GroupedOperand &B, const int32_t *ends, void *D, bool d_f32, int64_t ldd,
-                                    int64_t strided, uint32_t *flags, bool own_flags, cudaStream_t st);
-
-// Matrix-vector products with 4-bit weights (w4.cu), routing and the weighted
-// sum of answers (route.cu).
-cudaError_t launch_w4_matvec(bool x_f32, int64_t G, int64_t rows, int64_t N, int64_t K, int group, const void *X,
-                             int64_t ldx, const uint8_t *q, const void *scales, bool s_f32, const uint8_t *zeros,
-                             const int32_t *ends, void *Y, int64_t ldy, uint16_t *planes, cudaStream_t st);
-bool w4_direct(bool x_f32, const void *X, int64_t ldx);     // X is read as it is, without planes
-size_t route_scratch_bytes(int64_t E);
-cudaError_t launch_route(int64_t T, int64_t E, int k, bool renorm, const void *logits, bool f32, int64_t ldl,
-                         float *weights, int32_t *experts, int32_t *slots, int32_t *rows, int32_t *ends,
-                         int32_t *counts, WsHeader *ws, cudaStream_t st);
-cudaError_t launch_route_backward(int64_t T, int64_t E, int k, bool renorm, const void *logits, bool f32, int64_t ldl,
-                                  const int32_t *experts, const float *dw, void *dl, int64_t lddl, cudaStream_t st);
-cudaError_t launch_combine(bool f32, int64_t T, int k, int64_t cols, const void *Y, int64_t yrows, int64_t ldy,
-                           const int32_t *slots, const float *weights, void *O, int64_t ldo, cudaStream_t st);
-cudaError_t launch_combine_backward(bool f32, int64_t T, int k, int64_t cols, const void *dO, int64_t lddo,
-                                    const void *Y, int64_t yrows, int64_t ldy, const int32_t *slots,
-                                    const float *weights, void *dY, int64_t lddy, float *dw, cudaStream_t st);
-
 }  // namespace emu

@@ -12,7 +12,7 @@
 //
 // combine: bound by HBM; every answer row is read once, rows in 16-byte pieces.
 #include "grouped_common.cuh"
-#include "launchers.cuh"
+#include "expert_launchers.cuh"
 #include "split_f32_pair.cuh"
 
 namespace emu {

@@ -28,7 +28,7 @@
 // warps waiting for each other's staging: 16 rows over 12 experts of 2048 x 4096
 // took 28 us, 7 FP32 rows times 16384 x 8192 53 us.)
 #include "grouped_common.cuh"
-#include "launchers.cuh"
+#include "expert_launchers.cuh"
 #include "split_f32_pair.cuh"
 
 namespace emu {

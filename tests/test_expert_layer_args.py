@@ -1,5 +1,8 @@
 """The expert-layer entry points reject bad arguments on the host, before any
 CUDA call: status codes of the C entry points, ValueError of the tensor calls."""
+import os
+import re
+
 import pytest
 
 import paper_2609_04663_gb300 as emu
@@ -10,6 +13,15 @@ from paper_2609_04663_gb300 import _build
 def lib():
     _build.build()
     return emu.load()
+
+
+def test_every_declared_symbol_is_exported_and_bound(lib):
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    text = re.sub(r"/\*.*?\*/", "", open(os.path.join(root, "include", "emu_experts.h")).read(), flags=re.S)
+    names = set(re.findall(r"\b(emu_[a-z0-9_]+)\s*\(", text))
+    assert len(names) >= 14
+    for name in names:
+        assert hasattr(lib, name) and name in emu._SIGS, name
 
 
 def test_argument_checks_need_no_gpu(lib):
