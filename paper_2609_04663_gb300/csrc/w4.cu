@@ -24,9 +24,16 @@
 // into a ring and tables of its own, so no wait is a spin, and reads X's columns
 // from L1 and L2: BF16 rows as they are, FP32 rows (or such that allow no 16-byte
 // reads) as slices that a small kernel has split and put in pair order before.
-// (K split over a cluster, with X staged for 256 features at a time, kept most
-// warps waiting for each other's staging: 16 rows over 12 experts of 2048 x 4096
-// took 28 us, 7 FP32 rows times 16384 x 8192 53 us.)
+// What holds it: shifts, masks and multiply-adds of the decoding take 2 clocks
+// per warp instruction, two pipes together about half of the 164 clocks that a
+// scheduler spends on 1024 weights; leaving any one part out (decoding, MMAs, X,
+// copies) saves 2-22 %, so the rest is latency at the 4 warps per scheduler that
+// registers allow (more warps spill and are slower; 16 features per CTA: 29 us
+// for the 16 rows; K split over a cluster with X staged for 256 features: 28 us
+// and 53 us for 7 FP32 rows).
+// Measured (GPU time, weights from HBM): 1 row x 4096 x 4096 5.8 us; 1 row x 16384 x
+// 16384 47 us (2.8 TB/s of weights); 16 rows over 12 experts of 2048 x 4096 25 us;
+// 7 FP32 rows x 16384 x 8192 41 us with the slices' kernel.
 #include "grouped_common.cuh"
 #include "expert_launchers.cuh"
 #include "split_f32_pair.cuh"
@@ -279,13 +286,17 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps) w4_kernel(const W4Ar
         xp[t] = static_cast<const uint8_t *>(a.X) +
                 ((DIRECT ? (row0 + c) * a.ldx : ((int64_t)row0 * a.S + c) * a.K) + k0) * 2 + lc * 16;
     }
+    // kAhead blocks of X are on their way: with one tile a whole stage's (16 rows
+    // over 12 experts 25 us against 30 with one block); with three tiles two
+    // already spill (7 FP32 rows 47 us against 41)
+    constexpr int kAhead = GB == 0 || NT == 3 ? 1 : 4;
     int ahead = (k1 - k0) / 32;                       // blocks of X still to be loaded
-    uint4 xn[NT];                                     // the next block's
-    auto load_x = [&]() {
+    uint4 xn[kAhead][NT];
+    auto load_x = [&](int slot) {
         if (--ahead >= 0) {
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
-                xn[t] = __ldg(reinterpret_cast<const uint4 *>(xp[t]));
+                xn[slot][t] = __ldg(reinterpret_cast<const uint4 *>(xp[t]));
                 xp[t] += 64;
             }
         }
@@ -311,7 +322,8 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps) w4_kernel(const W4Ar
 #pragma unroll
             for (int st = 0; st < kStages; ++st) fetch();
             if (!DIRECT) griddep_wait();              // the planes: all else was there before their kernel
-            load_x();
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) load_x(i);
         } else {
             cp_async_wait<0>();                       // these came last
         }
@@ -328,8 +340,11 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps) w4_kernel(const W4Ar
                 for (int r = 0; r < 4; ++r) w[r] = shared_at<uint32_t>(smem, (stage ^ (uint32_t)(b << 4)) + (uint32_t)(r * 512));
                 uint4 x[NT];
 #pragma unroll
-                for (int t = 0; t < NT; ++t) x[t] = DIRECT ? pair_order(xn[t].x, xn[t].y, xn[t].z, xn[t].w) : xn[t];
-                load_x();
+                for (int t = 0; t < NT; ++t) {
+                    const uint4 v = xn[b % kAhead][t];
+                    x[t] = DIRECT ? pair_order(v.x, v.y, v.z, v.w) : v;
+                }
+                load_x(b % kAhead);
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     const uint32_t u = w[2 * i], v = w[2 * i + 1], zu = z[2 * i], zv = z[2 * i + 1];
