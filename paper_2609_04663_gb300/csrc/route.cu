@@ -3,14 +3,19 @@
 //
 // route: for each token the k largest logits (ties: the lower index), their
 // softmax weights, and the stable order of all T k assignments by expert: a
-// counting sort.  One launch: every block ranks a contiguous range of tokens
-// (a warp per token: the largest key by a warp maximum, its lowest index by a
-// warp minimum, k times), counts its assignments per expert, and after one
-// grid barrier places them behind those of the blocks before it.  A single
-// block needs no barrier.  Bound by latency (two reads of `experts`, the
-// barrier) up to some ten thousand tokens, then by reading the logits.
+// counting sort.  One launch: every block ranks a contiguous range of tokens and
+// every warp one within it (a token at a time: the largest key by a warp maximum,
+// its lowest index, k times), each warp counts its own choices per expert, and
+// after one grid barrier it places them behind those of the blocks and warps
+// before it.  A single block needs no barrier.  Bound by instructions (sorting a
+// lane's keys, k warp maxima) and by the barrier's and counts' latency:
+// 32768 x 128 BF16, k = 8: 21 us, of which ranking 11, barrier and counts 4
+// (the logits' bytes alone: 1.2); 8 x 64: 3.7 us; the gradient at 32768 x 128:
+// 11 us.
 //
 // combine: bound by HBM; every answer row is read once, rows in 16-byte pieces.
+// 16384 tokens, k = 4, 2048 BF16 columns: 54 us (6.2 TB/s), gradients 86 us (7.0
+// TB/s with what L2 keeps).
 #include "grouped_common.cuh"
 #include "expert_launchers.cuh"
 #include "split_f32_pair.cuh"
@@ -29,13 +34,12 @@ __device__ __forceinline__ float load_logit(const void *row, int e, bool f32)
     return f32 ? __ldg(static_cast<const float *>(row) + e) : bf16_f32(__ldg(static_cast<const uint16_t *>(row) + e));
 }
 
-// Order-preserving key of a logit, never 0: negative zero like zero, NaN like
-// minus infinity.
+// Order-preserving key of a logit that is not NaN, never 0; negative zero like
+// zero.
 __device__ __forceinline__ uint32_t logit_key(float x)
 {
-    if (!(x == x)) x = -INFINITY;
     const uint32_t b = __float_as_uint(x + 0.0f);
-    return (b & 0x80000000u) ? ~b : b | 0x80000000u;
+    return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float key_logit(uint32_t k)
 {
@@ -55,9 +59,12 @@ struct RouteArgs {
     int T, E, k, f32, renorm;
     float *weights;
     int32_t *experts, *slots, *rows, *ends;
-    int32_t *counts;                      // [blocks][E]
+    int32_t *counts;                      // [blocks][count_pitch(E)]
     uint32_t *flags, *bar;
 };
+
+// Row pitch of the blocks' counts: whole 16-byte pieces.
+__host__ __device__ __forceinline__ int count_pitch(int E) { return (E + 3) & ~3; }
 
 // Bounded barrier over the blocks of a cooperative launch (one use per launch;
 // *bar starts at zero).
@@ -90,35 +97,45 @@ __global__ void __launch_bounds__(kRouteThreads) route_kernel(const RouteArgs a)
     int32_t *all = base + a.E;                            // [E] assignments of all blocks
     const int warp = threadIdx.x >> 5, lane = (int)lane_id();
     const int per = (a.T + (int)gridDim.x - 1) / (int)gridDim.x;
-    const int t0 = min(a.T, (int)blockIdx.x * per), t1 = min(a.T, t0 + per);
+    const int t0 = min(a.T, (int)blockIdx.x * per), n = min(a.T, t0 + per) - t0;
+    // this warp's tokens: a contiguous range, so that it can count and place its
+    // own choices, in order (a token's experts are distinct: lanes never collide)
+    const int wper = (n + kRouteWarps - 1) / kRouteWarps;
+    const int w0 = t0 + min(n, warp * wper), w1 = t0 + min(n, (warp + 1) * wper);
+    int32_t *h = hist + warp * a.E;
+    for (int e = lane; e < a.E; e += 32) h[e] = 0;
+    __syncwarp();
 
     // ---- the k largest of each token
     bool odd = false;
-    for (int t = t0 + warp; t < t1; t += kRouteWarps) {
-        const char *row = static_cast<const char *>(a.logits) + (int64_t)t * a.ldl * (F32 ? 4 : 2);
+    const int64_t pitch = a.ldl * (F32 ? 4 : 2);
+    const char *row = static_cast<const char *>(a.logits) + w0 * pitch;
+    int64_t out = (int64_t)w0 * a.k + lane;
+    for (int t = w0; t < w1; ++t, row += pitch, out += a.k) {
         uint32_t key[V];
         float x[V];
+        int at[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             const int e = i * 32 + lane;
             x[i] = e < a.E ? load_logit(row, e, F32) : -INFINITY;
         }
+        // lanes past the last expert hold minus infinity under higher indexes than
+        // every expert's: with k <= E they are never taken
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const int e = i * 32 + lane;
+            at[i] = i * 32 + lane;
             odd |= !(x[i] < INFINITY);                    // NaN or plus infinity
-            key[i] = e < a.E ? logit_key(x[i]) : 0u;
+            x[i] = fmaxf(x[i], -INFINITY);                // NaN counts as minus infinity
+            key[i] = logit_key(x[i]);
             // a BF16 logit's key fills the upper half: with the inverted index below
             // it the largest word is the largest logit of the lowest index
-            if (!F32 && e < a.E) key[i] = (key[i] & 0xFFFF0000u) | (0xFFFFu - (uint32_t)e);
+            if (!F32) key[i] = (key[i] & 0xFFFF0000u) | (0xFFFFu - (uint32_t)at[i]);
         }
         // up to 8 logits a lane: its candidates by falling key (equal keys: rising
         // index), the best of all lanes' firsts taken off k times; more: each lane
         // looks for its best again every time
         constexpr bool SORT = V <= 8;
-        int at[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) at[i] = i * 32 + lane;
         if constexpr (SORT) {
 #pragma unroll
             for (int i = 1; i < V; ++i)
@@ -131,8 +148,24 @@ __global__ void __launch_bounds__(kRouteThreads) route_kernel(const RouteArgs a)
                     if (F32) { at[q - 1] = swap ? u : v; at[q] = swap ? v : u; }
                 }
         }
-        uint32_t mine = 0u, top_key = 0u;                 // lane j: the j-th key
+        // the padding below a BF16 key is its logit's lower half: zeros, or ones where negative
+        auto logit = [&](uint32_t k) { return key_logit(F32 ? k : (k & 0x80000000u) ? k & 0xFFFF0000u : k | 0xFFFFu); };
+        float total = 0.0f;
+        if (!a.renorm) {                                  // the softmax over all, while the logits are at hand
+            uint32_t best = key[0];
+            if constexpr (!SORT) {
+#pragma unroll
+                for (int i = 1; i < V; ++i) best = max(best, key[i]);
+            }
+            const float top = logit(__reduce_max_sync(0xFFFFFFFFu, best));
+            if (top > -INFINITY) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) total += expf(x[i] - top);
+            }
+        }
+        uint32_t mine = 0u;                               // lane j: the j-th key
         int chosen = 0;
+#pragma unroll (SORT ? 4 : 1)                         // (E = 1024: 31 us against 33 unrolled)
         for (int j = 0; j < a.k; ++j) {
             uint32_t best = key[0];
             int first = at[0];
@@ -142,51 +175,41 @@ __global__ void __launch_bounds__(kRouteThreads) route_kernel(const RouteArgs a)
                     if (key[i] > best) { best = key[i]; first = i * 32 + lane; }
             }
             const uint32_t most = __reduce_max_sync(0xFFFFFFFFu, best);
-            int e;
-            bool own;
+            bool own = best == most;
+            int e = 0;
             if constexpr (F32) {
-                const uint32_t hit = __ballot_sync(0xFFFFFFFFu, best == most);
+                const uint32_t hit = __ballot_sync(0xFFFFFFFFu, own);
                 if ((hit & (hit - 1)) == 0) e = __shfl_sync(0xFFFFFFFFu, first, __ffs(hit) - 1);
-                else e = (int)__reduce_min_sync(0xFFFFFFFFu, best == most ? (uint32_t)first : 0x7FFFFFFFu);
-                own = first == e;
-            } else {
-                e = 0xFFFF - (int)(most & 0xFFFFu);
-                own = best == most;
+                else e = (int)__reduce_min_sync(0xFFFFFFFFu, own ? (uint32_t)first : 0x7FFFFFFFu);
+                own = own && first == e;
+                chosen = lane == j ? e : chosen;
             }
             if constexpr (SORT) {
-                if (own) {
 #pragma unroll
-                    for (int i = 1; i < V; ++i) { key[i - 1] = key[i]; at[i - 1] = at[i]; }
-                    key[V - 1] = 0u;
-                    at[V - 1] = -1;
+                for (int i = 1; i < V; ++i) {
+                    key[i - 1] = own ? key[i] : key[i - 1];
+                    if (F32) at[i - 1] = own ? at[i] : at[i - 1];
                 }
+                key[V - 1] = own ? 0u : key[V - 1];
             } else {
+                if (!F32) e = 0xFFFF - (int)(most & 0xFFFFu);
 #pragma unroll
                 for (int i = 0; i < V; ++i)
                     if (i * 32 + lane == e) key[i] = 0u;
             }
-            if (j == 0) top_key = most;
-            if (lane == j) { mine = most; chosen = e; }
+            mine = lane == j ? most : mine;
         }
-        // the padding below a BF16 key is its logit's lower half: zeros, or ones where negative
-        auto logit = [&](uint32_t k) { return key_logit(F32 ? k : (k & 0x80000000u) ? k & 0xFFFF0000u : k | 0xFFFFu); };
-        const float top = logit(top_key);
+        if (!F32) chosen = 0xFFFF - (int)(mine & 0xFFFFu);
+        const float own_logit = logit(mine), top = __shfl_sync(0xFFFFFFFFu, own_logit, 0);
         const bool some = top > -INFINITY;                // else no expert is allowed: weights 0
-        const float p = some && lane < a.k ? expf(logit(mine) - top) : 0.0f;
-        float total;
-        if (a.renorm) {
-            total = warp_sum(p);
-        } else {
-            total = 0.0f;
-#pragma unroll
-            for (int i = 0; i < V; ++i)
-                if (some && i * 32 + lane < a.E) total += x[i] == x[i] ? expf(x[i] - top) : 0.0f;
-            total = warp_sum(total);
-        }
+        const float p = some && lane < a.k ? expf(own_logit - top) : 0.0f;
+        total = warp_sum(a.renorm ? p : total);
         if (lane < a.k) {
-            a.weights[(int64_t)t * a.k + lane] = some ? p / total : 0.0f;
-            a.experts[(int64_t)t * a.k + lane] = chosen;
+            a.weights[out] = some ? p / total : 0.0f;
+            a.experts[out] = chosen;
+            ++h[chosen];
         }
+        __syncwarp();
     }
     if (gridDim.x == 1) {                                 // the only block: it sets the flag word
         if (__syncthreads_or(odd ? 1 : 0)) {
@@ -194,24 +217,12 @@ __global__ void __launch_bounds__(kRouteThreads) route_kernel(const RouteArgs a)
         } else if (threadIdx.x == 0) {
             *a.flags = 0u;
         }
-    } else if (__any_sync(0xFFFFFFFFu, odd) && lane == 0) {
-        atomicOr(a.flags, (uint32_t)EMU_FLAG_NONFINITE);
+    } else {
+        if (__any_sync(0xFFFFFFFFu, odd) && lane == 0) atomicOr(a.flags, (uint32_t)EMU_FLAG_NONFINITE);
+        __syncthreads();
     }
 
-    // ---- assignments per warp (a contiguous range each) and expert
-    for (int i = threadIdx.x; i < kRouteWarps * a.E; i += kRouteThreads) hist[i] = 0;
-    __syncthreads();
-    const int n = (t1 - t0) * a.k, wper = (n + kRouteThreads - 1) / kRouteThreads * 32;
-    const int w0 = min(n, warp * wper), w1 = min(n, w0 + wper);
-    const int32_t *ex = a.experts + (int64_t)t0 * a.k;
-    int32_t *h = hist + warp * a.E;
-    for (int i = w0; i < w1; i += 32) {
-        const int e = i + lane < w1 ? ex[i + lane] : -1;
-        const uint32_t same = __match_any_sync(0xFFFFFFFFu, e);
-        if (e >= 0 && lane == __ffs(same) - 1) h[e] += __popc(same);
-        __syncwarp();
-    }
-    __syncthreads();
+    // ---- each warp's count per expert -> the counts of the warps before it
     for (int e = threadIdx.x; e < a.E; e += kRouteThreads) {
         int sum = 0;
 #pragma unroll 8
@@ -220,65 +231,72 @@ __global__ void __launch_bounds__(kRouteThreads) route_kernel(const RouteArgs a)
             hist[w * a.E + e] = sum;
             sum += c;
         }
-        all[e] = sum;
+        all[e] = gridDim.x > 1 ? 0 : sum;
         base[e] = 0;
-        if (gridDim.x > 1) a.counts[(int64_t)blockIdx.x * a.E + e] = sum;
+        if (gridDim.x > 1) a.counts[(int64_t)blockIdx.x * count_pitch(a.E) + e] = sum;
     }
     if (gridDim.x > 1) {
         route_barrier(a.bar, a.flags);
-        for (int e = threadIdx.x; e < a.E; e += kRouteThreads) all[e] = 0;
-        __syncthreads();
-        // groups of threads sum up a share of the blocks for every expert
-        const int width = (a.E + 31) / 32 * 32, parts = max(1, kRouteThreads / width);
-        const int share = ((int)gridDim.x + parts - 1) / parts;
-        for (int i = threadIdx.x; i < width * parts; i += kRouteThreads) {
-            const int e = i % width, b0 = (i / width) * share, b1 = min((int)gridDim.x, b0 + share);
-            if (e < a.E) {
-                int before = 0, sum = 0;
+        // parts of the threads sum up every parts-th block's counts, four experts a thread
+        const int quads = (a.E + 3) / 4, parts = max(1, kRouteThreads / quads);
+        const int part = (int)threadIdx.x / quads, q = (int)threadIdx.x - part * quads;
+        if (part < parts) {
+            int4 before = make_int4(0, 0, 0, 0), sum = before;
+            const int4 *from = reinterpret_cast<const int4 *>(a.counts) + q;
 #pragma unroll 8
-                for (int b = b0; b < b1; ++b) {
-                    const int c = __ldcg(a.counts + (int64_t)b * a.E + e);
-                    sum += c;
-                    if (b < (int)blockIdx.x) before += c;
-                }
-                atomicAdd(all + e, sum);                  // integers: the order does not matter
-                atomicAdd(base + e, before);
+            for (int b = part; b < (int)gridDim.x; b += parts) {
+                const int4 c = __ldcg(from + (int64_t)b * quads);
+                sum.x += c.x; sum.y += c.y; sum.z += c.z; sum.w += c.w;
+                if (b < (int)blockIdx.x) { before.x += c.x; before.y += c.y; before.z += c.z; before.w += c.w; }
             }
+            const int s[4] = {sum.x, sum.y, sum.z, sum.w}, f[4] = {before.x, before.y, before.z, before.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i)                   // (integers: the order does not matter)
+                if (q * 4 + i < a.E) {
+                    atomicAdd(all + q * 4 + i, s[i]);
+                    atomicAdd(base + q * 4 + i, f[i]);
+                }
         }
     }
     __syncthreads();
-    if (warp == 0) {                                      // experts' first slots
-        int carry = 0;
-        for (int e0 = 0; e0 < a.E; e0 += 32) {
-            const int e = e0 + lane, c = e < a.E ? all[e] : 0;
-            int v = c;
+    // ---- experts' first slots: thread e has expert e
+    {
+        __shared__ int32_t warps[kRouteWarps];
+        const int e = (int)threadIdx.x, c = e < a.E ? all[e] : 0;
+        int v = c;
 #pragma unroll
-            for (int d = 1; d < 32; d <<= 1) {
-                const int u = __shfl_up_sync(0xFFFFFFFFu, v, d);
-                if (lane >= d) v += u;
-            }
-            if (e < a.E) {
-                base[e] += carry + v - c;
-                if (blockIdx.x == 0) a.ends[e] = carry + v;
-            }
-            carry += __shfl_sync(0xFFFFFFFFu, v, 31);
+        for (int d = 1; d < 32; d <<= 1) {
+            const int u = __shfl_up_sync(0xFFFFFFFFu, v, d);
+            if (lane >= d) v += u;
+        }
+        if (lane == 31) warps[warp] = v;
+        __syncthreads();
+        const int earlier = (int)__reduce_add_sync(0xFFFFFFFFu, lane < warp ? warps[lane] : 0);
+        if (e < a.E) {
+            base[e] += earlier + v - c;
+            if (blockIdx.x == 0) a.ends[e] = earlier + v;
         }
     }
     __syncthreads();
 
-    // ---- slots: behind the same expert's assignments of earlier blocks, warps and lanes
-    for (int i = w0; i < w1; i += 32) {
-        const int e = i + lane < w1 ? ex[i + lane] : -1;
-        const uint32_t same = __match_any_sync(0xFFFFFFFFu, e);
-        if (e >= 0) {
-            const int slot = base[e] + h[e] + __popc(same & ((1u << lane) - 1u));
-            const int64_t at = (int64_t)t0 * a.k + i + lane;
-            a.slots[at] = slot;
-            a.rows[slot] = (int32_t)(at / a.k);
+    // ---- slots: behind the same expert's assignments of earlier blocks, warps and
+    // tokens.  Every lane reads back what it wrote.
+    out = (int64_t)w0 * a.k + lane;
+    for (int t = w0; t < w1; t += 4) {
+        int e[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) e[i] = lane < a.k && t + i < w1 ? a.experts[out + i * a.k] : -1;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (e[i] >= 0) {
+                const int before = h[e[i]], slot = base[e[i]] + before;
+                h[e[i]] = before + 1;
+                a.slots[out + i * a.k] = slot;
+                a.rows[slot] = t + i;
+            }
+            __syncwarp();
         }
-        __syncwarp();
-        if (e >= 0 && lane == __ffs(same) - 1) h[e] += __popc(same);
-        __syncwarp();
+        out += 4 * a.k;
     }
 }
 
@@ -587,7 +605,7 @@ cudaError_t run_route_back(const RouteBackArgs &a, cudaStream_t st)
 
 }  // namespace
 
-size_t route_scratch_bytes(int64_t E) { return (size_t)kRouteBlocks * (size_t)E * sizeof(int32_t); }
+size_t route_scratch_bytes(int64_t E) { return (size_t)kRouteBlocks * (size_t)count_pitch((int)E) * sizeof(int32_t); }
 
 cudaError_t launch_route(int64_t T, int64_t E, int k, bool renorm, const void *logits, bool f32, int64_t ldl,
                          float *weights, int32_t *experts, int32_t *slots, int32_t *rows, int32_t *ends,
