@@ -26,12 +26,15 @@ cudaError_t launch_grouped_product(int nslices, bool trans, int64_t G, int64_t r
                                    bool y_f32, int64_t ldy, uint32_t *flags, bool own_flags, cudaStream_t st);
 // FP32 weights that meet few rows each, split inside the product
 // (grouped_fused.cu); fused_takes: whether their rows can be read by TMA;
-// kFusedRows: up to so many rows for each group on average that is the faster way.
+// kFusedRows: up to so many rows for each group on average that is the faster
+// way (16 groups of 1024 x 2048: 64 rows 44 us against 103 through planes, 256 115
+// and 141, 384 170 and 182, 512 216 and 205; 8 of 4096 x 4096: 384 603 and 658, 512
+// 778 and 723).
 bool fused_takes(const float *W, int64_t G, int64_t ldw, int64_t stridew);
 cudaError_t launch_grouped_fused(bool trans, int64_t G, int64_t rows, int64_t N, int64_t K, const GroupedOperand &X,
                                  const float *W, int64_t ldw, int64_t stridew, const int32_t *ends, float *Y,
                                  int64_t ldy, uint32_t *flags, cudaStream_t st);
-constexpr int64_t kFusedRows = 127;
+constexpr int64_t kFusedRows = 448;
 cudaError_t launch_grouped_gradient(int nslices, int64_t G, int64_t rows, int64_t M, int64_t N, const GroupedOperand &A,
                                     const GroupedOperand &B, const int32_t *ends, void *D, bool d_f32, int64_t ldd,
                                     int64_t strided, uint32_t *flags, bool own_flags, cudaStream_t st);

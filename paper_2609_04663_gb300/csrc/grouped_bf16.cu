@@ -15,6 +15,12 @@
 // groups; a warp of each CTA sets them to zero in shared memory, in both
 // operands, before it passes the stage on to the MMAs (a zero times an infinity
 // would not be zero).
+//
+// Bound by the copies from L2 into the SMs (41-45 bytes per clock and SM) where
+// groups have hundreds of rows: 64 uneven groups of 512 rows on average, 2048 x 4096:
+// 411 us (1.34 PFLOP/s), the rows' gradient 392, the weights' 455 (1.21; only 8
+// K-blocks between two epilogues); by reading the weights with few: 32 groups
+// of 4 to 64 rows 81-87 us (6.6-6.1 TB/s), one row of 4 groups 14 us.
 #include "grouped_tile.cuh"
 
 namespace emu {
@@ -169,8 +175,10 @@ grouped_bf16_kernel(const __grid_constant__ CUtensorMap tmL, const __grid_consta
         for (int t = first; t < total && ok; t += step) {
             const HalfTile x = tile(t);
             const int nkb = (x.nk + kKB - 1) / kKB;
-            // per half: this CTA's rows (columns), as 64-row boxes and a short rest in
-            // boxes of 16; a gradient's two 64-column blocks in one copy where they
+            // per half: this CTA's rows (columns), as 64-row boxes, the last one also for a
+            // part of them (rows past the tile's are not multiplied) unless that is 16
+            // (32 groups of 40 rows, 2048 x 4096: 86 us against 90 with boxes of 16
+            // for every rest; of 330: 140 and 148); a gradient's two 64-column blocks in one copy where they
             // start on whole blocks (also where the second is not needed)
             int row[2], big[2], small[2];
             uint32_t bytes = Cfg::L_TILE;
@@ -179,8 +187,8 @@ grouped_bf16_kernel(const __grid_constant__ CUtensorMap tmL, const __grid_consta
                 const int n = x.n[h] / Cfg::CTAS, rest = n % 64;
                 row[h] = x.c0 + (h ? x.n[0] : 0) + rank * n;
                 if (!CMN) row[h] += a.padded ? (int)padded_start(starts[x.g], x.g) : starts[x.g];
-                big[h] = n / 64 + (CMN && rest > 0);
-                small[h] = CMN ? 0 : rest / 16;
+                big[h] = n / 64 + (rest > (CMN ? 0 : 16));
+                small[h] = !CMN && rest == 16 ? 1 : 0;
                 if (CMN && a.cwide && n > 0) big[h] = 2;
                 bytes += (uint32_t)((big[h] * 64 + small[h] * 16) * kKB * 2);
             }
@@ -226,9 +234,8 @@ grouped_bf16_kernel(const __grid_constant__ CUtensorMap tmL, const __grid_consta
                     } else {
                         for (int b = 0; b < big[h]; ++b)
                             tma_load_4d<PAIR>(dc + (uint32_t)(b * 64 * kKB * 2), &tmC, bar, kc, row[h] + 64 * b, 0, 0);
-                        for (int b = 0; b < small[h]; ++b)
-                            tma_load_4d<PAIR>(dc + (uint32_t)((big[h] * 64 + b * 16) * kKB * 2), &tmS, bar, kc,
-                                              row[h] + 64 * big[h] + 16 * b, 0, 0);
+                        if (small[h])
+                            tma_load_4d<PAIR>(dc + (uint32_t)(big[h] * 64 * kKB * 2), &tmS, bar, kc, row[h] + 64 * big[h], 0, 0);
                     }
                 }
                 ++issued;

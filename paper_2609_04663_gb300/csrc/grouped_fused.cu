@@ -1,8 +1,11 @@
 // Products grouped by expert for FP32 weights that meet only a few rows each:
 // the weights are read once, as FP32, and split (Eq. (fp32split)) on their way
 // to the tensor cores, instead of being written and read again as planes (10
-// bytes of traffic per element more than the 4 that are needed).  Bound by
-// reading the weights from HBM.
+// bytes of traffic per element more than the 4 that are needed).  Bound by the
+// way of a K-block through the split (HBM latency, 16 warps' splitting, MMAs) and
+// by HBM's rate behind it.  16 matrices of 1024 x 2048 with the rows' split: 37 us
+// for one row each, 38 for 16, 44 for 64, 115 for 256; 8 of 4096 x 4096 with 8 rows
+// each: 125 us (4.3 TB/s).
 //
 // Tiles and products are those of grouped.cu with one CTA per tile (128
 // features x up to 64 rows).  The leading products A0B0 of every 256 elements
@@ -34,26 +37,24 @@ __device__ __forceinline__ float4 lds_f4(uint32_t a)
     return v;
 }
 
-// COLS: rows of X per tile at most.  With 32, a third K-block of FP32 weights
-// fits in shared memory: at two the ring (64 KB in flight per SM) does not
-// cover HBM's latency.
-template <int COLS>
+constexpr int kCols = 64;                             // rows of X per tile at most
+
 struct FusedCfg {
-    static constexpr int STORE_WARPS = COLS / 8, THREADS = 32 * (kSplitWarps + 3 + STORE_WARPS);
-    static constexpr int L_TILE = kLRows * kKB * 2, C_TILE = COLS * kKB * 2;
+    static constexpr int STORE_WARPS = kCols / 8, THREADS = 32 * (kSplitWarps + 3 + STORE_WARPS);
+    static constexpr int L_TILE = kLRows * kKB * 2, C_TILE = kCols * kKB * 2;
     static constexpr int STAGE = 3 * (L_TILE + C_TILE), STAGES = 2;
-    static constexpr int W_TILE = kLRows * kKB * 4, W_STAGES = COLS == 32 ? 3 : 2, W_OFF = STAGES * STAGE;
+    static constexpr int W_TILE = kLRows * kKB * 4, W_STAGES = 2, W_OFF = STAGES * STAGE;
     static constexpr int BAR_OFF = W_OFF + W_STAGES * W_TILE, TAB_OFF = BAR_OFF + 256;
     static constexpr int SMEM = TAB_OFF + 1024 + 2 * (kMaxGroups + 1) * 4;
     static_assert(SMEM <= kSmemMax, "shared memory per CTA");
 };
 
-template <int COLS, bool LMN>
-__global__ void __launch_bounds__(FusedCfg<COLS>::THREADS, 1)
+template <bool LMN>
+__global__ void __launch_bounds__(FusedCfg::THREADS, 1)
 grouped_fused_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmC,
                      const __grid_constant__ CUtensorMap tmS, const GroupedArgs a)
 {
-    using Cfg = FusedCfg<COLS>;
+    using Cfg = FusedCfg;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t base = (raw + 1023u) & ~1023u;
@@ -83,13 +84,13 @@ grouped_fused_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_const
     // to be waited for (below)
     groups_and_flags(a, starts);
     const int nlt = (a.L + kLRows - 1) / kLRows;
-    if (warp == kSplitWarps) tile_prefix(starts, a.G, COLS, nlt, tpre);
+    if (warp == kSplitWarps) tile_prefix(starts, a.G, kCols, nlt, tpre);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const int total = uniform(tpre[a.G]), nkb = (a.K + kKB - 1) / kKB;
     const uint32_t tmem = (uint32_t)uniform((int)*tmem_slot);
-    auto tile = [&](int t) { return tile_at<3, COLS, false, LMN, false>(t, a, starts, tpre, 0); };
+    auto tile = [&](int t) { return tile_at<3, kCols, false, LMN, false>(t, a, starts, tpre, 0); };
 
     if (warp < kSplitWarps) {
         // ---------------- split: weights -> three slices of the stage.  LMN (W_g
@@ -173,17 +174,16 @@ grouped_fused_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_const
         bool ok = true;
         for (int t = (int)blockIdx.x; t < total && ok; t += (int)gridDim.x) {
             const Tile x = tile(t);
-            const int big = x.csz == COLS, small = big ? 0 : x.csz / 16;
+            // one copy per plane, of 16 rows or a tile's (rows past the group's are not
+            // multiplied): several short ones take longer than the bytes
+            const bool big = x.csz > 16;
             const int row = (a.padded ? (int)padded_start(starts[x.g], x.g) : starts[x.g]) + x.c0;
             for (int kb = 0; kb < nkb; ++kb) {
                 if (!(ok = mbar_wait(empty0 + 8u * s, ph ^ 1u, flags))) break;
                 const uint32_t fb = full0 + 8u * s, dc = base + (uint32_t)(s * Cfg::STAGE + 3 * Cfg::L_TILE);
-                mbar_arrive_expect_tx(fb, (uint32_t)(3 * x.csz * kKB * 2));
-                for (int r = 0; r < 3; ++r) {
-                    if (big) tma_load_4d<false>(dc + (uint32_t)(r * Cfg::C_TILE), &tmC, fb, kb * kKB, row, 0, r);
-                    for (int b = 0; b < small; ++b)
-                        tma_load_4d<false>(dc + (uint32_t)(r * Cfg::C_TILE + b * 16 * kKB * 2), &tmS, fb, kb * kKB, row + 16 * b, 0, r);
-                }
+                mbar_arrive_expect_tx(fb, (uint32_t)(3 * (big ? kCols : 16) * kKB * 2));
+                for (int r = 0; r < 3; ++r)
+                    tma_load_4d<false>(dc + (uint32_t)(r * Cfg::C_TILE), big ? &tmC : &tmS, fb, kb * kKB, row, 0, r);
                 ++issued;
                 if (++s == Cfg::STAGES) { s = 0; ph ^= 1u; }
             }
@@ -223,7 +223,7 @@ grouped_fused_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_const
                         mma(rest, 0, 1, kk, true);
                     }
                 }
-                const uint32_t b = cph % kLead, lead = tmem + (b + 1u) * COLS;
+                const uint32_t b = cph % kLead, lead = tmem + (b + 1u) * kCols;
                 if (kc == 0) {                        // this accumulator's last sum has been read
                     if (!(ok = warp_wait(tempty0 + 8u * b, ((cph / kLead) & 1u) ^ 1u, flags))) break;
                     tc_fence_after();
@@ -265,7 +265,7 @@ grouped_fused_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_const
                 for (int h = 0; h < HALF; h += 16) {
                     if (h < cols) {
                         uint32_t v[16];
-                        tmem_load16(lanes + (c < nch ? (b + 1u) * COLS : 0u) + (uint32_t)h, v);
+                        tmem_load16(lanes + (c < nch ? (b + 1u) * kCols : 0u) + (uint32_t)h, v);
                         tmem_ld_wait();
 #pragma unroll
                         for (int j = 0; j < 16; ++j) acc[h + j] = __fadd_rn(acc[h + j], __uint_as_float(v[j]));
@@ -290,12 +290,12 @@ grouped_fused_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_const
     }
 }
 
-template <int COLS, bool LMN>
+template <bool LMN>
 cudaError_t run_fused(const CUtensorMap &tw, const CUtensorMap &tc, const CUtensorMap &ts, const GroupedArgs &a,
                       int64_t tiles, cudaStream_t st)
 {
-    using Cfg = FusedCfg<COLS>;
-    return launch_persistent<grouped_fused_kernel<COLS, LMN>>(Cfg::SMEM, Cfg::THREADS, 1, tiles, st, tw, tc, ts, a);
+    using Cfg = FusedCfg;
+    return launch_persistent<grouped_fused_kernel<LMN>>(Cfg::SMEM, Cfg::THREADS, 1, tiles, st, tw, tc, ts, a);
 }
 
 // Tensor map over G FP32 matrices of rows x inner, box box_inner x box_rows.
@@ -330,15 +330,11 @@ cudaError_t launch_grouped_fused(bool trans, int64_t G, int64_t rows, int64_t N,
     CUtensorMap tw, tc, ts;
     const bool ok = trans ? make_weight_map(&tw, W, K, N, G, ldw, stridew, kKB, kLRows)
                           : make_weight_map(&tw, W, N, K, G, ldw, stridew, kLRows, kKB);
-    // experts of up to 32 rows or so take 32-row tiles (one that has more reads
-    // its weights again, from L2)
-    const int cols = rows <= 24 * G ? 32 : 64;
-    if (!ok || !make_group_map(&tc, X.planes, K, X.rows, 1, 3, X.ld, 0, X.plane, cols) ||
+    if (!ok || !make_group_map(&tc, X.planes, K, X.rows, 1, 3, X.ld, 0, X.plane, kCols) ||
         !make_group_map(&ts, X.planes, K, X.rows, 1, 3, X.ld, 0, X.plane, 16))
         return cudaErrorInvalidValue;
-    const int64_t tiles = max_tiles(rows, G, N, cols, 1);
-    if (cols == 32) return trans ? run_fused<32, false>(tw, tc, ts, a, tiles, st) : run_fused<32, true>(tw, tc, ts, a, tiles, st);
-    return trans ? run_fused<64, false>(tw, tc, ts, a, tiles, st) : run_fused<64, true>(tw, tc, ts, a, tiles, st);
+    const int64_t tiles = max_tiles(rows, G, N, kCols, 1);
+    return trans ? run_fused<false>(tw, tc, ts, a, tiles, st) : run_fused<true>(tw, tc, ts, a, tiles, st);
 }
 
 }  // namespace emu

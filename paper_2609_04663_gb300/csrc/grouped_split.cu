@@ -10,7 +10,9 @@
 //
 // Bound by HBM: 10 bytes per FP32 element (4 read, 6 written), 4 per BF16
 // element.  One warp takes a row, a lane 8 consecutive elements per step
-// (two 16-byte loads, one 16-byte store per plane).
+// (two 16-byte loads, one 16-byte store per plane).  16384 x 2048 FP32 rows: 54
+// us (6.2 TB/s); 16 matrices of 2048 x 2048: 103 us (6.5 TB/s); 32768 BF16 rows of
+// 2048 gathered from 8192: 30 us.
 #include "grouped_common.cuh"
 #include "expert_launchers.cuh"
 #include "split_f32_pair.cuh"
