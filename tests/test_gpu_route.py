@@ -210,3 +210,21 @@ def test_route_feeds_the_products(dev):
     ref = (per * r.weights.double()[..., None]).sum(1)
     bound = 1e-5 * (mag * r.weights.double()[..., None]).sum(1)
     assert bool(((O - ref).abs() <= bound).all())
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("T,E,k,kind", [(20001, 36, 5, "masked"), (6000, 70, 32, "ties"), (40000, 3, 1, "one expert"), (33, 1021, 32, "plain")])
+def test_route_many_tokens_of_padded_rows(dev, dtype, T, E, k, kind):
+    """Several tokens for each warp of every block, logits as a part of wider rows; twice the same."""
+    import torch
+    x = logits(dev, T, E, getattr(torch, dtype), kind, 5)
+    ex, w, slots, rows, ends = reference(x, k, True)
+    wide = torch.full((T, E + 3), float("nan"), dtype=x.dtype, device=dev)
+    wide[:, :E] = x.to(dev)
+    r, ws = emu.route(wide[:, :E], k)
+    again, _ = emu.route(wide[:, :E], k)
+    assert emu.read_flags(ws) == (emu.FLAG_NONFINITE if bool(x.isnan().any()) else 0)
+    assert torch.equal(r.experts.cpu().long(), ex) and torch.equal(r.slots.cpu().long(), slots)
+    assert torch.equal(r.rows.cpu().long(), rows) and torch.equal(r.ends.cpu().long(), ends)
+    assert bool(((r.weights.cpu().double() - w).abs() <= (E + 16) * 2.0 ** -23 * w + 1e-37).all())
+    assert all(torch.equal(a, b) for a, b in zip(r, again))
