@@ -97,9 +97,9 @@ emu_status emu_grouped_prodsum_wgrad(int nslices, int64_t G, int64_t rows, int64
  * rows x N of dtype (EMU_F32: FP32 rows as their three BF16 slices, exact
  * products; EMU_BF16), any alignment; sums in FP32.  ends as above, or NULL
  * with G = 1: one matrix for all rows.  Values in ends outside 0 .. rows or
- * decreasing are clamped.  Rows of no group are zero.  Any number of rows is
- * computed; the weights are read again for every 24 (BF16) or 8 (FP32) of an
- * expert.  q 16-byte aligned.  ws: emu_w4_workspace_bytes, 16-byte aligned, for
+ * decreasing are clamped.  Rows of no group are zero.  Up to
+ * 131070 rows are computed; the weights are read again for every 24 (BF16) or 8
+ * (FP32) of an expert.  q 16-byte aligned.  ws: emu_w4_workspace_bytes, 16-byte aligned, for
  * X's slices; NULL will do for BF16 rows of 16-byte aligned base and pitch. */
 size_t emu_w4_workspace_bytes(int dtype, int64_t rows, int64_t K);
 emu_status emu_w4_matvec(int dtype, int64_t G, int64_t rows, int64_t N, int64_t K, int64_t group, const void *X,

@@ -261,7 +261,8 @@ emu_status emu_w4_matvec(int dtype, int64_t G, int64_t rows, int64_t N, int64_t 
     const int esize = dtype == EMU_F32 ? 4 : 2;
     if (K == 0) return cuda_status(zero_rows(Y, rows, N, ldy, esize, st));
     if (!X || !q || !scales) return EMU_ERR_INVALID_ARG;
-    if (!aligned16(q) || !fits(X, dtype) || !fits(Y, dtype) || !fits(scales, stype)) return EMU_ERR_MISALIGNED;
+    if (!aligned16(q) || !fits(X, dtype) || !fits(Y, dtype) || !fits(scales, stype) || !fits(ends, EMU_F32))
+        return EMU_ERR_MISALIGNED;
     if (rows > 65535 * 2) return EMU_ERR_UNSUPPORTED;           // items of two rows and more on the grid's y dimension
     if (!w4_direct(dtype == EMU_F32, X, ldx)) {
         s = check_ws(ws, ws_bytes, emu_w4_workspace_bytes(dtype, rows, K));

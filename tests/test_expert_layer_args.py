@@ -57,6 +57,8 @@ def test_argument_checks_need_no_gpu(lib):
     assert w(0, 1, 1, 8, 64, 32, P, 63, P, P, 0, None, None, P, 8, P, 1 << 20, None) == 1
     assert w(0, 1, 2, 8, 64, 32, P, 64, P, P, 0, None, None, P, 8, P, 767, None) == 3          # room for two rows' slices
     assert w(0, 1, 2, 8, 64, 32, P, 64, P, P, 0, None, None, P, 8, None, 0, None) == 1
+    assert w(0, 1, 2, 8, 64, 32, P, 64, P, P, 0, None, P + 2, P, 8, P, 1 << 20, None) == 2      # address of ends
+    assert w(1, 1, 131071, 8, 64, 32, P, 64, P, P, 1, None, None, P, 8, None, 0, None) == 5    # rows
     # routing
     assert emu.emu_route(0, 4, 8, 9, 1, P, 8, P, P, P, P, P, P, big, None) == 1       # k > E
     assert emu.emu_route(0, 4, 2000, 2, 1, P, 2000, P, P, P, P, P, P, big, None) == 5
