@@ -76,6 +76,30 @@ def test_quantized_experts(ex):
         assert rel(out, want) <= 1e-5
 
 
+@pytest.mark.parametrize("served", [False, True])
+def test_in_a_cuda_graph(ex, served):
+    """The layer captured once and replayed on other tokens: the call's own results, bit for bit."""
+    import torch
+    layer = ex.ExpertLayer(128, 256, 5, 2, torch.bfloat16)
+    if served:
+        layer = ex.QuantizedExperts(layer, group=64)
+    g = torch.Generator(device="cuda").manual_seed(5)
+    x = torch.randn(6, 128, generator=g, device="cuda").bfloat16()
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        layer.forward(x)
+    torch.cuda.current_stream().wait_stream(stream)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = layer.forward(x)
+    for _ in range(3):
+        x.normal_(generator=g)
+        graph.replay()
+        got = out.clone()
+        assert torch.equal(got, layer.forward(x)) and bool(got.any())
+
+
 def test_command(ex):
     losses, off = ex.main(["--tokens", "256", "--width", "128", "--hidden", "256", "--experts", "4", "--steps", "8"])
     assert losses[-1] < losses[0] and max(off) < 0.5

@@ -282,3 +282,44 @@ def test_random_shapes(dev, dtype, seed):
     assert within(emu.grouped_gemm(dY, W, ends, opW=back)[0], dX, aX, N, f32)
     dw = emu.grouped_wgrad(dY, X, ends, srcB=src)[0] if trans else emu.grouped_wgrad(X, dY, ends, srcA=src)[0]
     assert within(dw, dW, aW, max(sizes + [1]), f32)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_most_groups(dev, dtype):
+    """1024 groups, most of them empty or of one row: product, both gradients."""
+    import torch
+    rng = np.random.default_rng(13)
+    sizes = [int(v) for v in rng.choice((0, 0, 1, 1, 2, 19), 1024)]
+    X, W, dY, ends, src = make(dev, sizes, 40, 72, getattr(torch, dtype), 14, tail=3, gather=True)
+    (Y, dX, dW), (aY, aX, aW) = reference(X[src.long()], W, dY, sizes, False)
+    f32 = dtype == "float32"
+    assert within(emu.grouped_gemm(X, W, ends, src=src)[0], Y, aY, 40, f32)
+    assert within(emu.grouped_gemm(dY, W, ends, opW=emu.OP_T)[0], dX, aX, 72, f32)
+    assert within(emu.grouped_wgrad(X, dY, ends, srcA=src)[0], dW, aW, 19, f32)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_rows_past_2_31_elements(dev, dtype):
+    """Token rows and results of more than 2^31 elements: the first and last rows
+    of the product and of the rows' gradient, parts of the weights' gradient."""
+    import torch
+    dt, f32 = getattr(torch, dtype), dtype == "float32"
+    G, rows, K, N = 3, 66000, 16, 32776
+    g = torch.Generator(device=dev).manual_seed(15)
+    X, W = torch.randn(rows, K, generator=g, device=dev).to(dt), torch.randn(G, K, N, generator=g, device=dev).to(dt)
+    dY = torch.randn(rows, N, generator=g, device=dev).to(dt)
+    ends = torch.tensor([100, 100, rows], dtype=torch.int32, device=dev)
+    assert rows * N > 2 ** 31
+    y, _ = emu.grouped_gemm(X, W, ends)
+    dx, _ = emu.grouped_gemm(dY, W, ends, opW=emu.OP_T)
+    for at, w in ((slice(0, 100), W[0].double()), (slice(rows - 70, rows), W[2].double())):
+        x, d = X[at].double(), dY[at].double()
+        assert within(y[at], x @ w, x.abs() @ w.abs(), K, f32)
+        assert within(dx[at], d @ w.T, d.abs() @ w.abs().T, N, f32)
+    del y, dx
+    dw, _ = emu.grouped_wgrad(X, dY, ends)
+    x = X[100:].double()
+    for at in (slice(0, 65), slice(N - 65, N)):
+        d = dY[100:, at].double()
+        assert within(dw[2][:, at], x.T @ d, x.abs().T @ d.abs(), rows, f32)
+    assert not dw[1].any()

@@ -228,3 +228,29 @@ def test_route_many_tokens_of_padded_rows(dev, dtype, T, E, k, kind):
     assert torch.equal(r.rows.cpu().long(), rows) and torch.equal(r.ends.cpu().long(), ends)
     assert bool(((r.weights.cpu().double() - w).abs() <= (E + 16) * 2.0 ** -23 * w + 1e-37).all())
     assert all(torch.equal(a, b) for a, b in zip(r, again))
+
+
+def test_combine_past_2_31_elements(dev):
+    """Answers and their gradients of more than 2^31 elements, the last rows named first."""
+    import torch
+    T, k, cols = 270000, 2, 4096
+    assert T * k * cols > 2 ** 31
+    Y = torch.zeros((T * k, cols), dtype=torch.bfloat16, device=dev)
+    g = torch.Generator(device=dev).manual_seed(8)
+    Y[-8:].normal_(generator=g)
+    Y[:8].normal_(generator=g)
+    slots = torch.arange(T * k - 1, -1, -1, dtype=torch.int32, device=dev).view(T, k)
+    w = torch.rand((T, k), generator=g, device=dev)
+    O = emu.rows_combine(Y, slots, w)
+    ends = [t for at in (0, T - 4) for t in range(at, at + 4)]
+    per = w.double()[ends, :, None] * Y[slots[ends].long()].double()
+    bound = k * 2.0 ** -23 * per.abs().sum(1) + 2.0 ** -8 * per.sum(1).abs()
+    assert bool(((O[ends].double() - per.sum(1)).abs() <= bound).all())
+    dO = torch.zeros_like(O)
+    dO[ends] = torch.randn((8, cols), generator=g, device=dev).bfloat16()
+    dY, dw = emu.rows_combine_backward(dO, Y, slots, w)
+    dot = Y[slots[ends].long()].double() * dO[ends].double()[:, None]
+    assert bool(((dw[ends].double() - dot.sum(2)).abs() <= cols * 2.0 ** -23 * dot.abs().sum(2)).all())
+    want = w.double()[ends, :, None] * dO[ends].double()[:, None]
+    assert bool(((dY[slots[ends].long()].double() - want).abs() <= (2.0 ** -8 + 2.0 ** -23) * want.abs()).all())
+    assert not dw[4:T - 4].any() and not dY[8:-8].any()

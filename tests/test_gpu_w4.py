@@ -176,3 +176,22 @@ def test_another_stream(dev):
     got = emu.w4_matvec(X, q, s, zeros=z, stream=st)
     st.synchronize()
     assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_most_experts_and_many_rows(dev, dtype):
+    import torch
+    G, N, K, group = 1024, 33, 64, 32
+    sizes = [(i * 7) % 4 if i % 3 else 0 for i in range(G)]
+    sizes[5] = 150                                         # far more than its share
+    rows = sum(sizes) + 2
+    X, q, s, z = make(dev, rows, N, K, group, getattr(torch, dtype), True, G=G, seed=10)
+    W = weights(q, s, z, group)
+    of = torch.repeat_interleave(torch.arange(G, device=dev), torch.tensor(sizes, device=dev))
+    Y = emu.w4_matvec(X, q, s, zeros=z, ends=torch.tensor(sizes, device=dev).cumsum(0).to(torch.int32))
+    assert not Y[rows - 2:].any()
+    for g in (1, 2, 5, 1021, 1022):
+        assert check(Y[:rows - 2][of == g], X[:rows - 2][of == g], W[g])
+    assert all(check(Y[i:i + 1], X[i:i + 1], W[of[i]]) for i in range(0, rows - 2, 97))
+    X, q, s, z = make(dev, 3001, N, K, group, getattr(torch, dtype), True, seed=11)
+    assert check(emu.w4_matvec(X, q, s, zeros=z), X, weights(q, s, z, group))
