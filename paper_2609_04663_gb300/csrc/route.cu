@@ -422,23 +422,23 @@ struct CombineArgs {
     int k, cols;
 };
 
-// 16 bytes of a row (4 FP32 or 8 BF16) from column c on; columns past the last
-// read as zero and are not stored.  VEC: rows are 16-byte aligned and whole
-// pieces.
-template <bool F32, bool VEC>
+// 16 bytes of a row: 4 FP32 or 8 BF16.  VEC (rows are 16-byte aligned and whole
+// pieces): from column c on at once.  Else one by one, columns c, c + STEP, ..;
+// columns past the last read as zero and are not stored (c is in the row).
+template <bool F32, bool VEC, int STEP>
 __device__ __forceinline__ uint4 load_piece(const char *row, int64_t c, int cols)
 {
     if constexpr (VEC) {
         return __ldg(reinterpret_cast<const uint4 *>(row + c * (F32 ? 4 : 2)));
     } else if constexpr (F32) {
         const uint32_t *p = reinterpret_cast<const uint32_t *>(row) + c;
-        return make_uint4(__ldg(p), c + 1 < cols ? __ldg(p + 1) : 0u, c + 2 < cols ? __ldg(p + 2) : 0u,
-                          c + 3 < cols ? __ldg(p + 3) : 0u);
+        return make_uint4(__ldg(p), c + STEP < cols ? __ldg(p + STEP) : 0u, c + 2 * STEP < cols ? __ldg(p + 2 * STEP) : 0u,
+                          c + 3 * STEP < cols ? __ldg(p + 3 * STEP) : 0u);
     } else {
         const uint16_t *p = reinterpret_cast<const uint16_t *>(row) + c;
         uint32_t h[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) h[i] = c + i < cols ? (uint32_t)__ldg(p + i) : 0u;
+        for (int i = 0; i < 8; ++i) h[i] = i == 0 || c + STEP * i < cols ? (uint32_t)__ldg(p + STEP * i) : 0u;
         return make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
     }
 }
@@ -458,7 +458,7 @@ __device__ __forceinline__ void to_floats(uint4 v, float (&x)[F32 ? 4 : 8])
     }
 }
 
-template <bool F32, bool VEC>
+template <bool F32, bool VEC, int STEP>
 __device__ __forceinline__ void store_piece(char *row, int64_t c, int cols, const float (&x)[F32 ? 4 : 8])
 {
     if constexpr (VEC) {
@@ -469,9 +469,9 @@ __device__ __forceinline__ void store_piece(char *row, int64_t c, int cols, cons
     } else {
 #pragma unroll
         for (int i = 0; i < (F32 ? 4 : 8); ++i)
-            if (c + i < cols) {
-                if constexpr (F32) reinterpret_cast<float *>(row)[c + i] = x[i];
-                else reinterpret_cast<uint16_t *>(row)[c + i] = f32_bf16(x[i]);
+            if (c + STEP * i < cols) {
+                if constexpr (F32) reinterpret_cast<float *>(row)[c + STEP * i] = x[i];
+                else reinterpret_cast<uint16_t *>(row)[c + STEP * i] = f32_bf16(x[i]);
             }
     }
 }
@@ -479,7 +479,7 @@ __device__ __forceinline__ void store_piece(char *row, int64_t c, int cols, cons
 constexpr int kBatch = 4;             // rows or pieces that a thread loads before it uses the first
 
 // O[t] = sum_j w[t, j] Y[slots[t, j]], j ascending, in FP32; a thread has one
-// 16-byte piece of one token.
+// piece of one token.
 template <bool F32, bool VEC>
 __global__ void __launch_bounds__(256) combine_kernel(const CombineArgs a)
 {
@@ -500,7 +500,7 @@ __global__ void __launch_bounds__(256) combine_kernel(const CombineArgs a)
                 v[j] = make_uint4(0u, 0u, 0u, 0u);
                 const bool ok = s >= 0 && s < a.yrows;
                 if (!ok) w[j] = 0.0f;
-                else v[j] = load_piece<F32, VEC>(static_cast<const char *>(a.Y) + s * a.ldy * ES, c, a.cols);
+                else v[j] = load_piece<F32, VEC, 1>(static_cast<const char *>(a.Y) + s * a.ldy * ES, c, a.cols);
             }
 #pragma unroll
             for (int j = 0; j < kBatch; ++j) {
@@ -510,40 +510,50 @@ __global__ void __launch_bounds__(256) combine_kernel(const CombineArgs a)
                 for (int e = 0; e < N; ++e) acc[e] = fmaf(w[j], x[e], acc[e]);
             }
         }
-        store_piece<F32, VEC>(static_cast<char *>(a.O) + t * a.ldo * ES, c, a.cols, acc);
+        store_piece<F32, VEC, 1>(static_cast<char *>(a.O) + t * a.ldo * ES, c, a.cols, acc);
     }
 }
 
-// dY[slots[t, j]] = w[t, j] dO[t], dw[t, j] = Y[slots[t, j]] . dO[t]; a warp
-// per (t, j), so that a token's k warps share its dO row in the caches.
-template <bool F32, bool VEC>
+// dY[slots[t, j]] = w[t, j] dO[t], dw[t, j] = Y[slots[t, j]] . dO[t]; W lanes
+// for each (t, j), those of a token next to each other, so that they share its dO
+// row in the caches.  Fewer than a warp for short rows (32768 tokens, k = 2, 64 BF16
+// columns: 8 us with 8 lanes, 24 with 32).  Rows that allow no 16-byte pieces: lanes
+// have neighbouring columns, so that a load or store touches one line or two
+// (16384 tokens, k = 4, 2047 BF16 columns: 200 us, 304 with consecutive columns per
+// lane; the weighted sum itself keeps these: 113 us there against 108, but 23 against
+// 42 for 30000 tokens, k = 8, 97 columns, whose lanes would be idle).
+template <bool F32, bool VEC, int W>
 __global__ void __launch_bounds__(256) combine_backward_kernel(const CombineArgs a)
 {
-    constexpr int N = F32 ? 4 : 8, ES = F32 ? 4 : 2;
-    const int lane = (int)lane_id();
-    for (int64_t i = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); i < a.T * a.k; i += (int64_t)gridDim.x * 8) {
-        const int64_t t = (int64_t)((uint32_t)i / (uint32_t)a.k), s = __ldg(a.slots + i);
+    constexpr int N = F32 ? 4 : 8, ES = F32 ? 4 : 2, PER = 32 / W;
+    static_assert(VEC || W == 32, "lanes with neighbouring columns are a warp");
+    const int lane = (int)lane_id() % W;
+    const int64_t total = a.T * a.k;
+    for (int64_t i0 = ((int64_t)blockIdx.x * 8 + (threadIdx.x >> 5)) * PER; i0 < total; i0 += (int64_t)gridDim.x * 8 * PER) {
+        const int64_t i = i0 + (int64_t)lane_id() / W;
+        const bool here = i < total;
+        const int64_t t = (int64_t)((uint32_t)i / (uint32_t)a.k), s = here ? __ldg(a.slots + i) : -1;
         const bool ok = s >= 0 && s < a.yrows;
-        const float w = a.weights ? __ldg(a.weights + i) : 1.0f;
-        const char *dO = static_cast<const char *>(a.dO) + t * a.ldo * ES;
+        const float w = here && a.weights ? __ldg(a.weights + i) : 1.0f;
+        const char *dO = static_cast<const char *>(a.dO) + (ok ? t : 0) * a.ldo * ES;
         const char *y = static_cast<const char *>(a.Y) + (ok ? s : 0) * a.ldy * ES;
         char *dY = static_cast<char *>(a.dY) + (ok ? s : 0) * a.lddy * ES;
         const int cols = ok ? a.cols : 0;
         float dot = 0.0f;
-        for (int64_t c0 = (int64_t)lane * N; c0 < cols; c0 += 32 * N * kBatch) {
+        for (int64_t c0 = VEC ? lane * N : lane; c0 < cols; c0 += W * N * kBatch) {
             uint4 d[kBatch], v[kBatch];
 #pragma unroll
             for (int b = 0; b < kBatch; ++b) {
-                const int64_t c = c0 + 32 * N * b;
+                const int64_t c = c0 + W * N * b;
                 d[b] = v[b] = make_uint4(0u, 0u, 0u, 0u);
                 if (c < cols) {
-                    d[b] = load_piece<F32, VEC>(dO, c, cols);
-                    if (a.dw) v[b] = load_piece<F32, VEC>(y, c, cols);
+                    d[b] = load_piece<F32, VEC, 32>(dO, c, cols);
+                    if (a.dw) v[b] = load_piece<F32, VEC, 32>(y, c, cols);
                 }
             }
 #pragma unroll
             for (int b = 0; b < kBatch; ++b) {
-                const int64_t c = c0 + 32 * N * b;
+                const int64_t c = c0 + W * N * b;
                 float x[N], u[N];
                 to_floats<F32>(d[b], x);
                 to_floats<F32>(v[b], u);
@@ -552,14 +562,33 @@ __global__ void __launch_bounds__(256) combine_backward_kernel(const CombineArgs
                     dot = fmaf(u[e], x[e], dot);
                     x[e] *= w;
                 }
-                if (c < cols) store_piece<F32, VEC>(dY, c, cols, x);
+                if (c < cols) store_piece<F32, VEC, 32>(dY, c, cols, x);
             }
         }
         if (a.dw) {
-            dot = warp_sum(dot);
-            if (lane == 0) a.dw[i] = ok ? dot : 0.0f;
+            __syncwarp();
+#pragma unroll
+            for (int d = W / 2; d > 0; d >>= 1) dot += __shfl_xor_sync(0xFFFFFFFFu, dot, d);
+            if (here && lane == 0) a.dw[i] = ok ? dot : 0.0f;
         }
     }
+}
+
+template <bool F32, bool VEC, int W>
+cudaError_t run_combine_back(const CombineArgs &a, cudaStream_t st)
+{
+    const int64_t per = 8 * (32 / W), blocks = (a.T * a.k + per - 1) / per;
+    combine_backward_kernel<F32, VEC, W><<<(unsigned)(blocks > 152 * 64 ? 152 * 64 : blocks), 256, 0, st>>>(a);
+    return cudaGetLastError();
+}
+
+template <bool F32>
+cudaError_t combine_back(const CombineArgs &a, bool vec, cudaStream_t st)
+{
+    const int pieces = a.cols / (F32 ? 4 : 8);
+    if (!vec) return run_combine_back<F32, false, 32>(a, st);
+    return pieces <= 8 ? run_combine_back<F32, true, 8>(a, st) : pieces <= 16 ? run_combine_back<F32, true, 16>(a, st)
+                                                                             : run_combine_back<F32, true, 32>(a, st);
 }
 
 bool can_vec(const void *p, int64_t ld, int esize)
@@ -654,7 +683,7 @@ cudaError_t launch_combine(bool f32, int64_t T, int k, int64_t cols, const void 
     a.T = T; a.k = k; a.cols = (int)cols;
     const int es = f32 ? 4 : 2;
     const bool vec = can_vec(Y, ldy, es) && can_vec(O, ldo, es) && cols * es % 16 == 0;
-    const int64_t total = T * ((cols + (f32 ? 3 : 7)) / (f32 ? 4 : 8)), blocks = (total + 255) / 256;
+    const int64_t blocks = (T * ((cols + (f32 ? 3 : 7)) / (f32 ? 4 : 8)) + 255) / 256;
     const unsigned grid = (unsigned)(blocks > 152 * 64 ? 152 * 64 : blocks);
     if (f32 && vec) combine_kernel<true, true><<<grid, 256, 0, st>>>(a);
     else if (f32) combine_kernel<true, false><<<grid, 256, 0, st>>>(a);
@@ -672,13 +701,7 @@ cudaError_t launch_combine_backward(bool f32, int64_t T, int k, int64_t cols, co
     a.weights = weights; a.dY = dY; a.dw = dw; a.T = T; a.k = k; a.cols = (int)cols;
     const int es = f32 ? 4 : 2;
     const bool vec = (!dw || can_vec(Y, ldy, es)) && can_vec(dO, lddo, es) && can_vec(dY, lddy, es) && cols * es % 16 == 0;
-    const int64_t blocks = (T * k + 7) / 8;
-    const unsigned grid = (unsigned)(blocks > 152 * 64 ? 152 * 64 : blocks);
-    if (f32 && vec) combine_backward_kernel<true, true><<<grid, 256, 0, st>>>(a);
-    else if (f32) combine_backward_kernel<true, false><<<grid, 256, 0, st>>>(a);
-    else if (vec) combine_backward_kernel<false, true><<<grid, 256, 0, st>>>(a);
-    else combine_backward_kernel<false, false><<<grid, 256, 0, st>>>(a);
-    return cudaGetLastError();
+    return f32 ? combine_back<true>(a, vec, st) : combine_back<false>(a, vec, st);
 }
 
 }  // namespace emu

@@ -254,3 +254,28 @@ def test_combine_past_2_31_elements(dev):
     want = w.double()[ends, :, None] * dO[ends].double()[:, None]
     assert bool(((dY[slots[ends].long()].double() - want).abs() <= (2.0 ** -8 + 2.0 ** -23) * want.abs()).all())
     assert not dw[4:T - 4].any() and not dY[8:-8].any()
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("cols", [1, 4, 8, 31, 32, 33, 56, 64, 65, 120, 128, 129, 255, 257, 1023])
+def test_combine_gradients_of_short_and_odd_rows(dev, dtype, cols):
+    """Every share of a warp and both kinds of pieces, slots outside and a last part of a warp among them."""
+    import torch
+    T, k = 37, 3
+    g = torch.Generator(device=dev).manual_seed(9)
+    Y, dO = (torch.randn((r, cols), generator=g, device=dev).to(getattr(torch, dtype)) for r in (T * k, T))
+    slots = torch.randperm(T * k, generator=g, device=dev).to(torch.int32).view(T, k)
+    w = torch.rand((T, k), generator=g, device=dev)
+    slots[5, 1], slots[36, 2] = -1, T * k
+    dY, dw = emu.rows_combine_backward(dO, Y, slots, w, dY=torch.full_like(Y, 7.0))
+    ok = (slots >= 0) & (slots < T * k)
+    at = slots.clamp(0, T * k - 1).long()
+    dot = Y[at].double() * dO.double()[:, None]
+    assert bool(((dw.double() - dot.sum(2)).abs() <= cols * 2.0 ** -23 * dot.abs().sum(2))[ok].all())
+    assert not dw[~ok].any()
+    want = w.double()[..., None] * dO.double()[:, None]
+    tol = 2.0 ** -23 + (2.0 ** -8 if dtype == "bfloat16" else 0.0)
+    assert bool(((dY[at].double() - want).abs() <= tol * want.abs())[ok].all())
+    named = torch.zeros(T * k, dtype=torch.bool, device=dev)
+    named[at[ok]] = True
+    assert bool((dY[~named] == 7.0).all())
