@@ -481,7 +481,10 @@ def grouped_split(X, ends=None, src=None, planes=None, ws=None, stream=None):
     """emu_grouped_split / emu_grouped_split_rows: the planes of weights X
     [G, rows, cols] (ends None), or of token rows X[src] (src None: X) grouped
     by ends; three for FP32 (Eq. (fp32split)), one for BF16.  A plane set can
-    stand for its operand in grouped_gemm and grouped_wgrad, in all directions."""
+    stand for its operand in grouped_gemm and grouped_wgrad, in all directions.
+    Pays for FP32 weights that meet hundreds of rows each; with a few the
+    products are faster on the weights themselves (62 rows over 14 experts of
+    6528 x 3232, product and both gradients: 1.53 ms with planes, 0.82 without)."""
     torch, where = _torch(), "grouped_split"
     dt, ldx, dev = _dtype(X, where), _pitch(X, where), X.device
     cols = X.shape[-1]
