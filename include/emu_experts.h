@@ -145,6 +145,14 @@ emu_status emu_rows_combine_backward(int dtype, int64_t T, int64_t k, int64_t co
                                      const float *weights, void *dY, int64_t lddy, float *dweights,
                                      emu_stream_t stream);
 
+/* The same, and zeros in the rows of dY that no slot names: all of dY is
+ * written.  ws: at least emu_rows_combine_workspace_bytes, 16-byte aligned. */
+size_t emu_rows_combine_workspace_bytes(int64_t yrows);
+emu_status emu_rows_combine_backward_full(int dtype, int64_t T, int64_t k, int64_t cols, const void *dO, int64_t lddo,
+                                          const void *Y, int64_t yrows, int64_t ldy, const int32_t *slots,
+                                          const float *weights, void *dY, int64_t lddy, float *dweights, void *ws,
+                                          size_t ws_bytes, emu_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -81,6 +81,9 @@ _SIGS = {
     "emu_route_backward": ("i", ["i", "l", "l", "l", "i", "p", "l", "p", "p", "p", "l", "p"]),
     "emu_rows_combine": ("i", ["i", "l", "l", "l", "p", "l", "l", "p", "p", "p", "l", "p"]),
     "emu_rows_combine_backward": ("i", ["i", "l", "l", "l", "p", "l", "p", "l", "l", "p", "p", "p", "l", "p", "p"]),
+    "emu_rows_combine_workspace_bytes": ("size", ["l"]),
+    "emu_rows_combine_backward_full": ("i", ["i", "l", "l", "l", "p", "l", "p", "l", "l", "p", "p", "p", "l", "p", "p",
+                                             "size", "p"]),
     "emu_read_flags": ("i", ["p", "p", "p"]),
     "emu_selftest_timeout": ("i", ["p", "size", "u32", "p"]),
     "emu_status_string": ("str", ["i"]),
@@ -169,6 +172,8 @@ emu_route = _mk("emu_route")
 emu_route_backward = _mk("emu_route_backward")
 emu_rows_combine = _mk("emu_rows_combine")
 emu_rows_combine_backward = _mk("emu_rows_combine_backward")
+emu_rows_combine_workspace_bytes = _mk("emu_rows_combine_workspace_bytes")
+emu_rows_combine_backward_full = _mk("emu_rows_combine_backward_full")
 emu_read_flags = _mk("emu_read_flags")
 emu_selftest_timeout = _mk("emu_selftest_timeout")
 emu_status_string = _mk("emu_status_string")
@@ -744,26 +749,28 @@ def rows_combine(Y, slots, weights=None, O=None, stream=None):
 def rows_combine_backward(dO, Y, slots, weights=None, dY=None, stream=None):
     """emu_rows_combine_backward: (dY, dweights) of rows_combine(Y, slots,
     weights); dweights is None without weights.  No two slots may name the
-    same row; rows of a dY made here that no slot names are zero."""
-    torch, where = _torch(), "rows_combine_backward"
+    same row.  Rows that no slot names are zero in a dY made here, and left as
+    they are in a given one."""
+    where = "rows_combine_backward"
     dt, shape, (yrows, cols), dev = _dtype(Y, where), slots.shape, Y.shape, Y.device
     T, k = shape
     if dO.shape != (T, cols) or dO.dtype is not Y.dtype:
         _bad(where, "dO has another shape or type")
-    if dY is None:
+    full = dY is None
+    if full:
         dY = _empty((yrows, cols), Y.dtype, dev, stream)
-        if yrows != T * k:
-            with torch.cuda.stream(_torch_stream(stream, dev)):
-                dY.zero_()
+        ws = _empty(yrows, _torch_module.int32, dev, stream)
     elif dY.shape != Y.shape or dY.dtype is not Y.dtype:
         _bad(where, "dY differs from Y")
-    dw = _empty((T, k), torch.float32, dev, stream) if weights is not None else None
-    r = _lib.emu_rows_combine_backward(dt, T, k, cols, dO.data_ptr(), _pitch(dO, "rows_combine_backward: dO", dev),
-                                         Y.data_ptr(), yrows, _pitch(Y, where),
-                                         _ints(slots, T * k, dev, "rows_combine_backward: slots"),
-                                         _float_pairs(weights, shape, dev, "rows_combine_backward: weights"),
-                                         dY.data_ptr(), _pitch(dY, "rows_combine_backward: dY", dev),
-                                         dw.data_ptr() if dw is not None else None, _raw_stream(stream, dev))
+    dw = _empty((T, k), _torch_module.float32, dev, stream) if weights is not None else None
+    args = (dt, T, k, cols, dO.data_ptr(), _pitch(dO, "rows_combine_backward: dO", dev), Y.data_ptr(), yrows,
+            _pitch(Y, where), _ints(slots, T * k, dev, "rows_combine_backward: slots"),
+            _float_pairs(weights, shape, dev, "rows_combine_backward: weights"), dY.data_ptr(),
+            _pitch(dY, "rows_combine_backward: dY", dev), dw.data_ptr() if dw is not None else None)
+    if full:
+        r = _lib.emu_rows_combine_backward_full(*args, ws.data_ptr(), 4 * yrows, _raw_stream(stream, dev))
+    else:
+        r = _lib.emu_rows_combine_backward(*args, _raw_stream(stream, dev))
     if r:
         _check(r, "emu_rows_combine_backward")
     return dY, dw

@@ -55,6 +55,7 @@ cudaError_t launch_combine(bool f32, int64_t T, int k, int64_t cols, const void 
                            const int32_t *slots, const float *weights, void *O, int64_t ldo, cudaStream_t st);
 cudaError_t launch_combine_backward(bool f32, int64_t T, int k, int64_t cols, const void *dO, int64_t lddo,
                                     const void *Y, int64_t yrows, int64_t ldy, const int32_t *slots,
-                                    const float *weights, void *dY, int64_t lddy, float *dw, cudaStream_t st);
+                                    const float *weights, void *dY, int64_t lddy, float *dw, int32_t *owner,
+                                    cudaStream_t st);       // owner: [yrows], or NULL: unnamed rows of dY are left
 
 }  // namespace emu

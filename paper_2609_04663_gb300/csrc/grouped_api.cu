@@ -67,6 +67,21 @@ emu_status product(int S, int opW, int64_t G, int64_t rows, int64_t N, int64_t K
                                               flags, own_flags, st));
 }
 
+emu_status check_combine_backward(int dtype, int64_t T, int64_t k, int64_t cols, const void *dO, int64_t lddo,
+                                  const void *Y, int64_t yrows, int64_t ldy, const int32_t *slots,
+                                  const float *weights, const void *dY, int64_t lddy, const float *dweights)
+{
+    if (!known(dtype) || T < 0 || k < 1 || cols < 0 || yrows < 0 || lddo < cols || lddy < cols ||
+        (dweights && ldy < cols))
+        return EMU_ERR_INVALID_ARG;
+    if (k >= 65536 || T >= kMaxDim / k || cols >= kMaxDim - 8 || yrows >= kMaxDim) return EMU_ERR_UNSUPPORTED;
+    if (T > 0 && (!slots || (cols > 0 && (!dO || (yrows > 0 && (!dY || (dweights && !Y))))))) return EMU_ERR_INVALID_ARG;
+    if (T > 0 && (!fits(dO, dtype) || !fits(Y, dtype) || !fits(dY, dtype) || !fits(weights, EMU_F32) ||
+                  !fits(dweights, EMU_F32) || !fits(slots, EMU_F32)))
+        return EMU_ERR_MISALIGNED;
+    return EMU_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -329,17 +344,35 @@ emu_status emu_rows_combine_backward(int dtype, int64_t T, int64_t k, int64_t co
                                      const float *weights, void *dY, int64_t lddy, float *dweights,
                                      emu_stream_t stream)
 {
-    if (!known(dtype) || T < 0 || k < 1 || cols < 0 || yrows < 0 || lddo < cols || lddy < cols ||
-        (dweights && ldy < cols))
-        return EMU_ERR_INVALID_ARG;
-    if (k >= 65536 || T >= kMaxDim / k || cols >= kMaxDim - 8 || yrows >= kMaxDim) return EMU_ERR_UNSUPPORTED;
-    if (T == 0) return EMU_OK;
-    if (!slots || (cols > 0 && (!dO || (yrows > 0 && (!dY || (dweights && !Y)))))) return EMU_ERR_INVALID_ARG;
-    if (!fits(dO, dtype) || !fits(Y, dtype) || !fits(dY, dtype) || !fits(weights, EMU_F32) || !fits(dweights, EMU_F32) ||
-        !fits(slots, EMU_F32))
-        return EMU_ERR_MISALIGNED;
+    const emu_status s = check_combine_backward(dtype, T, k, cols, dO, lddo, Y, yrows, ldy, slots, weights, dY, lddy, dweights);
+    if (s != EMU_OK || T == 0) return s;
     return cuda_status(launch_combine_backward(dtype == EMU_F32, T, (int)k, cols, dO, lddo, Y, yrows, ldy, slots,
-                                               weights, dY, lddy, dweights, reinterpret_cast<cudaStream_t>(stream)));
+                                               weights, dY, lddy, dweights, nullptr,
+                                               reinterpret_cast<cudaStream_t>(stream)));
+}
+
+size_t emu_rows_combine_workspace_bytes(int64_t yrows)
+{
+    return yrows < 0 ? 0 : (size_t)yrows * sizeof(int32_t);
+}
+
+emu_status emu_rows_combine_backward_full(int dtype, int64_t T, int64_t k, int64_t cols, const void *dO, int64_t lddo,
+                                          const void *Y, int64_t yrows, int64_t ldy, const int32_t *slots,
+                                          const float *weights, void *dY, int64_t lddy, float *dweights, void *ws,
+                                          size_t ws_bytes, emu_stream_t stream)
+{
+    emu_status s = check_combine_backward(dtype, T, k, cols, dO, lddo, Y, yrows, ldy, slots, weights, dY, lddy, dweights);
+    if (s != EMU_OK) return s;
+    if (yrows > 0 && cols > 0) {
+        if (!dY) return EMU_ERR_INVALID_ARG;              // (every row is written, also without tokens)
+        if (!fits(dY, dtype)) return EMU_ERR_MISALIGNED;
+        s = check_ws(ws, ws_bytes, emu_rows_combine_workspace_bytes(yrows));
+        if (s != EMU_OK) return s;
+    }
+    return cuda_status(launch_combine_backward(dtype == EMU_F32, T, (int)k, cols, dO, lddo, Y, yrows, ldy, slots,
+                                               weights, dY, lddy, dweights,
+                                               yrows > 0 && cols > 0 ? static_cast<int32_t *>(ws) : nullptr,
+                                               reinterpret_cast<cudaStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -1,0 +1,25 @@
+"""Arguments that the expert-layer calls have to reject on the host, before any CUDA call."""
+import pytest
+
+import paper_2609_04663_gb300 as emu
+from paper_2609_04663_gb300 import _build
+
+
+@pytest.fixture(scope="module", autouse=True)
+def lib():
+    _build.build()
+    return emu.load()
+
+
+def test_gradients_of_all_answer_rows():
+    P, f = 16, emu.emu_rows_combine_backward_full
+    assert emu.emu_rows_combine_workspace_bytes(100) >= 400
+    #        type T k cols dO ldo Y yrows ldy slots w dY lddy dw ws bytes stream
+    assert f(3, 4, 2, 8, P, 8, P, 8, 8, P, P, P, 8, P, P, 32, None) == 1
+    assert f(0, 4, 2, 8, P, 7, P, 8, 8, P, P, P, 8, P, P, 32, None) == 1
+    assert f(0, 4, 2, 8, P, 8, P, 8, 8, P, P, P, 8, P, None, 32, None) == 1
+    assert f(0, 4, 2, 8, P, 8, P, 8, 8, P, P, P, 8, P, P, 31, None) == 3
+    assert f(0, 4, 2, 8, P, 8, P, 8, 8, P, P, P, 8, P, P + 4, 32, None) == 2
+    assert f(0, 0, 2, 8, None, 8, P, 8, 8, None, None, None, 8, None, P, 32, None) == 1     # rows to clear
+    assert f(0, 0, 2, 8, None, 8, P, 8, 8, None, None, P + 1, 8, None, P, 32, None) == 2
+    assert f(0, 0, 2, 8, None, 8, P, 0, 8, None, None, None, 8, None, None, 0, None) == 0
