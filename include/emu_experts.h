@@ -18,6 +18,12 @@ extern "C" {
 #define EMU_F32  0
 #define EMU_BF16 1
 
+/* Added to the first argument (type or slices) of emu_grouped_split,
+ * emu_grouped_split_rows, emu_grouped_prodsum and emu_grouped_prodsum_wgrad: the
+ * call adds its flags to those in the workspace instead of starting anew, so
+ * that one word reports a product and the splits of its operands. */
+#define EMU_KEEP_FLAGS 0x100
+
 /* ---------------------------------------------------------------------------
  * Expert layers: matrix products grouped by expert, of ragged sizes.
  *

@@ -27,6 +27,7 @@ STATUS = {0: "ok", 1: "invalid argument", 2: "misaligned", 3: "workspace too sma
 FLAG_NONFINITE, FLAG_RANGE, FLAG_SLICE, FLAG_TIMEOUT, FLAG_INDEX = 0x1, 0x2, 0x4, 0x8, 0x10
 OP_N, OP_T = 0, 1
 F32, BF16 = 0, 1
+KEEP_FLAGS = 0x100
 ZERO_LEVEL = -(2 ** 31)
 
 _SIGS = {
@@ -489,7 +490,13 @@ def grouped_split(X, ends=None, src=None, planes=None, ws=None, stream=None):
     stand for its operand in grouped_gemm and grouped_wgrad, in all directions.
     Pays for FP32 weights that meet hundreds of rows each; with a few the
     products are faster on the weights themselves (62 rows over 14 experts of
-    6528 x 3232, product and both gradients: 1.53 ms with planes, 0.82 without)."""
+    6528 x 3232, product and both gradients: 1.53 ms with planes, 0.82 without).
+    The flags of the call are in ws, where a caller gives one."""
+    return _split(X, ends, src, planes, ws, stream, 0)
+
+
+def _split(X, ends, src, planes, ws, stream, keep):
+    """grouped_split; keep: KEEP_FLAGS where ws holds the flags of another operand's split, else 0."""
     torch, where = _torch(), "grouped_split"
     dt, ldx, dev = _dtype(X, where), _pitch(X, where), X.device
     cols = X.shape[-1]
@@ -511,10 +518,10 @@ def grouped_split(X, ends=None, src=None, planes=None, ws=None, stream=None):
     elif planes.shape != (S, prows, ld) or planes.dtype is not torch.int16 or not planes.is_contiguous():
         _bad(where, f"planes have to be contiguous int16 {(S, prows, ld)}")
     if ends is None:
-        r = _lib.emu_grouped_split(dt, G, rows, cols, X.data_ptr(), ldx, X.stride(0) if G > 1 else 0,
+        r = _lib.emu_grouped_split(dt | keep, G, rows, cols, X.data_ptr(), ldx, X.stride(0) if G > 1 else 0,
                                      planes.data_ptr(), ld, ws.data_ptr(), ws.numel(), _raw_stream(stream, dev))
     else:
-        r = _lib.emu_grouped_split_rows(dt, rows, cols, X.data_ptr(), X.shape[0], ldx,
+        r = _lib.emu_grouped_split_rows(dt | keep, rows, cols, X.data_ptr(), X.shape[0], ldx,
                                           _ints(src, None, dev, "grouped_split: src") if src is not None else None,
                                           _ints(ends, G, dev, "grouped_split: ends"), G, planes.data_ptr(), ld,
                                           ws.data_ptr(), ws.numel(), _raw_stream(stream, dev))
@@ -582,13 +589,14 @@ def grouped_gemm(X, W, ends, opW: int = OP_N, src=None, Y=None, ws=None, stream=
         return Y, ws
     if ws is None:
         ws = _empty(emu_split_workspace_bytes(32), torch.uint8, dev, stream)
+    keep = 0                                          # the first launch clears the flag word, the others add to it
     if not xp and (S == 3 or src is not None or not _tma_ok(X, ldx)):
-        X, xp = grouped_split(X, ends, src, ws=ws, stream=stream), True
+        X, xp, keep = _split(X, ends, src, None, ws, stream, keep), True, KEEP_FLAGS
         ldx = X.ld
     if not wp and (S == 3 or not _tma_ok(W, ldw)):
-        W, wp = grouped_split(W, ws=ws, stream=stream), True
+        W, wp, keep = _split(W, None, None, None, ws, stream, keep), True, KEEP_FLAGS
         ldw = W.ld
-    r = _lib.emu_grouped_prodsum(S, opW, G, rows, N, K, X.planes.data_ptr() if xp else X.data_ptr(), ldx, int(xp),
+    r = _lib.emu_grouped_prodsum(S | keep, opW, G, rows, N, K, X.planes.data_ptr() if xp else X.data_ptr(), ldx, int(xp),
                                    W.planes.data_ptr() if wp else W.data_ptr(), ldw,
                                    W.shape[1] * ldw if wp or G <= 1 else W.stride(0), pe, Y.data_ptr(), yt, ldy,
                                    ws.data_ptr(), ws.numel(), raw)
@@ -597,17 +605,18 @@ def grouped_gemm(X, W, ends, opW: int = OP_N, src=None, Y=None, ws=None, stream=
     return Y, ws
 
 
-def _token_operand(t, ends, src, ws, stream, where):
-    """(operand, address, row pitch, padded, slices) of token rows: BF16 rows as
-    they stand where the tensor memory accelerator can read them, else planes."""
+def _token_operand(t, ends, src, ws, stream, keep, where):
+    """(operand, address, row pitch, padded, slices, keep) of token rows: BF16 rows as
+    they stand where the tensor memory accelerator can read them, else planes.  keep:
+    KEEP_FLAGS once a split has written its flags to ws."""
     if not isinstance(t, GroupedPlanes):
         ld = _pitch(t, where)
         if len(t.shape) == 2 and _dtype(t, where) == BF16 and src is None and _tma_ok(t, ld):
-            return t, t.data_ptr(), ld, 0, 1
-        t = grouped_split(t, ends, src, ws=ws, stream=stream)
+            return t, t.data_ptr(), ld, 0, 1, keep
+        t, keep = _split(t, ends, src, None, ws, stream, keep), KEEP_FLAGS
     elif src is not None or not t.padded:
         _bad(where, "a plane set of token rows, already gathered, is needed")
-    return t, t.planes.data_ptr(), t.ld, 1, t.nslices
+    return t, t.planes.data_ptr(), t.ld, 1, t.nslices, keep
 
 
 def grouped_wgrad(A, B, ends, srcA=None, srcB=None, D=None, ws=None, stream=None):
@@ -619,8 +628,8 @@ def grouped_wgrad(A, B, ends, srcA=None, srcB=None, D=None, ws=None, stream=None
     G, dev = ends.numel(), A.device
     if ws is None:
         ws = _empty(emu_split_workspace_bytes(32), torch.uint8, dev, stream)
-    A, pa, lda, apad, Sa = _token_operand(A, ends, srcA, ws, stream, "grouped_wgrad: A")
-    B, pb, ldb, bpad, Sb = _token_operand(B, ends, srcB, ws, stream, "grouped_wgrad: B")
+    A, pa, lda, apad, Sa, keep = _token_operand(A, ends, srcA, ws, stream, 0, "grouped_wgrad: A")
+    B, pb, ldb, bpad, Sb, keep = _token_operand(B, ends, srcB, ws, stream, keep, "grouped_wgrad: B")
     if A.shape[0] != B.shape[0] or Sa != Sb or B.device != dev:
         _bad(where, "A and B have to be token rows, as many and of one type, on one device")
     (rows, M), N, S = A.shape, B.shape[1], Sa
@@ -629,7 +638,7 @@ def grouped_wgrad(A, B, ends, srcA=None, srcB=None, D=None, ws=None, stream=None
     dt, ldd = _dtype(D, "grouped_wgrad: D"), _pitch(D, "grouped_wgrad: D", dev)
     if D.shape != (G, M, N) or (S == 3 and dt != F32):
         _bad(where, "D has another shape or type")
-    r = _lib.emu_grouped_prodsum_wgrad(S, G, rows, M, N, pa, lda, apad, pb, ldb, bpad,
+    r = _lib.emu_grouped_prodsum_wgrad(S | keep, G, rows, M, N, pa, lda, apad, pb, ldb, bpad,
                                        _ints(ends, G, dev, "grouped_wgrad: ends"), D.data_ptr(), dt, ldd,
                                        D.stride(0) if G > 1 else M * ldd, ws.data_ptr(), ws.numel(),
                                        _raw_stream(stream, dev))

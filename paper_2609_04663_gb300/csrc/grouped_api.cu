@@ -29,6 +29,14 @@ cudaError_t clear_flags(void *ws, cudaStream_t st)
     return cudaMemsetAsync(&static_cast<WsHeader *>(ws)->flags, 0, sizeof(uint32_t), st);
 }
 
+// Takes EMU_KEEP_FLAGS off a type or a number of slices.
+bool take_keep(int &arg)
+{
+    const bool keep = arg >= 0 && (arg & EMU_KEEP_FLAGS) != 0;
+    if (keep) arg &= ~EMU_KEEP_FLAGS;
+    return keep;
+}
+
 // Sizes of a grouped call: G groups over `rows` rows, a and b the two matrix
 // dimensions; also keeps the tile counts within 32 bits.
 emu_status check_sizes(int64_t G, int64_t rows, int64_t a, int64_t b)
@@ -95,6 +103,7 @@ emu_status emu_grouped_split(int dtype, int64_t G, int64_t rows, int64_t cols, c
                              int64_t stridex, uint16_t *comps, int64_t ldcomp, void *ws, size_t ws_bytes,
                              emu_stream_t stream)
 {
+    const bool keep = take_keep(dtype);
     if (!known(dtype) || ldx < cols || (G > 1 && stridex < 0)) return EMU_ERR_INVALID_ARG;
     emu_status s = check_sizes(G, 0, rows, cols);
     if (s != EMU_OK) return s;
@@ -107,7 +116,7 @@ emu_status emu_grouped_split(int dtype, int64_t G, int64_t rows, int64_t cols, c
     s = check_ws(ws, ws_bytes, kWsHeaderBytes);
     if (s != EMU_OK) return s;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-    cudaError_t e = clear_flags(ws, st);
+    cudaError_t e = keep ? cudaSuccess : clear_flags(ws, st);
     if (e == cudaSuccess)
         e = launch_grouped_split(dtype == EMU_F32, G, rows, cols, X, ldx, stridex, comps, ldcomp,
                                  &static_cast<WsHeader *>(ws)->flags, st);
@@ -118,6 +127,7 @@ emu_status emu_grouped_split_rows(int dtype, int64_t rows, int64_t cols, const v
                                   const int32_t *src, const int32_t *ends, int64_t G, uint16_t *comps,
                                   int64_t ldcomp, void *ws, size_t ws_bytes, emu_stream_t stream)
 {
+    const bool keep = take_keep(dtype);
     if (!known(dtype) || xrows < 0 || ldx < cols || (!src && xrows < rows)) return EMU_ERR_INVALID_ARG;
     emu_status s = check_sizes(G, rows, cols, 0);
     if (s != EMU_OK) return s;
@@ -130,7 +140,7 @@ emu_status emu_grouped_split_rows(int dtype, int64_t rows, int64_t cols, const v
     s = check_ws(ws, ws_bytes, kWsHeaderBytes);
     if (s != EMU_OK) return s;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-    cudaError_t e = clear_flags(ws, st);
+    cudaError_t e = keep ? cudaSuccess : clear_flags(ws, st);
     if (e == cudaSuccess && rows > 0 && cols > 0)
         e = launch_grouped_split_rows(dtype == EMU_F32, rows, cols, X, xrows, ldx, src, ends, G, comps, ldcomp,
                                       &static_cast<WsHeader *>(ws)->flags, st);
@@ -142,6 +152,7 @@ emu_status emu_grouped_prodsum(int nslices, int opW, int64_t G, int64_t rows, in
                                int64_t stridew, const int32_t *ends, void *Y, int ytype, int64_t ldy, void *ws,
                                size_t ws_bytes, emu_stream_t stream)
 {
+    const bool keep = take_keep(nslices);
     if ((nslices != 1 && nslices != 3) || (opW != EMU_OP_N && opW != EMU_OP_T) || !known(ytype) || ldy < N)
         return EMU_ERR_INVALID_ARG;
     emu_status s = check_sizes(G, rows, N, K);
@@ -163,12 +174,12 @@ emu_status emu_grouped_prodsum(int nslices, int opW, int64_t G, int64_t rows, in
     if (s != EMU_OK) return s;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     const bool runs = rows > 0 && N > 0 && K > 0;     // the kernel then sets the flag word itself
-    if (!runs && clear_flags(ws, st) != cudaSuccess) return EMU_ERR_CUDA;
+    if (!runs && !keep && clear_flags(ws, st) != cudaSuccess) return EMU_ERR_CUDA;
     GroupedOperand X, W;
     X.planes = Xcomps; X.rows = padded ? padded_rows(rows, G) : rows; X.ld = ldx; X.plane = X.rows * ldx;
     X.padded = padded != 0;
     W.planes = Wcomps; W.ld = ldw; W.stride = stridew; W.plane = G * wrows * ldw;
-    return product(nslices, opW, G, rows, N, K, X, W, ends, Y, ytype, ldy, &static_cast<WsHeader *>(ws)->flags, true, st);
+    return product(nslices, opW, G, rows, N, K, X, W, ends, Y, ytype, ldy, &static_cast<WsHeader *>(ws)->flags, !keep, st);
 }
 
 size_t emu_grouped_gemm_workspace_bytes(int dtype, int64_t G, int64_t rows, int64_t N, int64_t K)
@@ -220,6 +231,7 @@ emu_status emu_grouped_prodsum_wgrad(int nslices, int64_t G, int64_t rows, int64
                                      int64_t ldb, int bpadded, const int32_t *ends, void *D, int dtype, int64_t ldd,
                                      int64_t strided, void *ws, size_t ws_bytes, emu_stream_t stream)
 {
+    const bool keep = take_keep(nslices);
     if ((nslices != 1 && nslices != 3) || (nslices == 3 && (!apadded || !bpadded)) || !known(dtype) || ldd < N || (G > 1 && strided < M * ldd))
         return EMU_ERR_INVALID_ARG;
     emu_status s = check_sizes(G, rows, M, N);
@@ -237,7 +249,7 @@ emu_status emu_grouped_prodsum_wgrad(int nslices, int64_t G, int64_t rows, int64
     s = check_ws(ws, ws_bytes, kWsHeaderBytes);
     if (s != EMU_OK) return s;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-    if ((M == 0 || N == 0 || rows == 0) && clear_flags(ws, st) != cudaSuccess) return EMU_ERR_CUDA;
+    if ((M == 0 || N == 0 || rows == 0) && !keep && clear_flags(ws, st) != cudaSuccess) return EMU_ERR_CUDA;
     if (M == 0 || N == 0) return EMU_OK;
     if (rows == 0) {
         for (int64_t g = 0; g < G; ++g) {
@@ -253,7 +265,7 @@ emu_status emu_grouped_prodsum_wgrad(int nslices, int64_t G, int64_t rows, int64
     B.planes = Bcomps; B.padded = bpadded != 0; B.rows = bpadded ? padded_rows(rows, G) : rows; B.ld = ldb;
     B.plane = B.rows * ldb;
     return cuda_status(launch_grouped_gradient(nslices, G, rows, M, N, A, B, ends, D, dtype == EMU_F32, ldd, strided,
-                                               &static_cast<WsHeader *>(ws)->flags, true, st));
+                                               &static_cast<WsHeader *>(ws)->flags, !keep, st));
 }
 
 size_t emu_w4_workspace_bytes(int dtype, int64_t rows, int64_t K)

@@ -23,3 +23,16 @@ def test_gradients_of_all_answer_rows():
     assert f(0, 0, 2, 8, None, 8, P, 8, 8, None, None, None, 8, None, P, 32, None) == 1     # rows to clear
     assert f(0, 0, 2, 8, None, 8, P, 8, 8, None, None, P + 1, 8, None, P, 32, None) == 2
     assert f(0, 0, 2, 8, None, 8, P, 0, 8, None, None, None, 8, None, None, 0, None) == 0
+
+
+def test_keep_flags_changes_no_check():
+    P, K = 16, emu.KEEP_FLAGS
+    g = emu.emu_grouped_prodsum
+    for S in (2, 0, 4):
+        assert g(S | K, 0, 2, 8, 8, 8, P, 8, 0, P, 8, 64, P, P, 0, 8, P, 512, None) == 1
+    assert g(1 | K | 0x200, 0, 2, 8, 8, 8, P, 8, 0, P, 8, 64, P, P, 0, 8, P, 512, None) == 1
+    assert g(-1, 0, 2, 8, 8, 8, P, 8, 0, P, 8, 64, P, P, 0, 8, P, 512, None) == 1
+    assert g(1 | K, 0, 2, 8, 8, 8, P, 8, 0, P, 8, 64, P, P, 0, 8, P, 511, None) == 3
+    assert emu.emu_grouped_prodsum_wgrad(3 | K, 2, 8, 8, 8, P, 8, 1, P, 8, 0, P, P, 0, 8, 64, P, 512, None) == 1
+    assert emu.emu_grouped_split(2 | K, 2, 8, 8, P, 8, 64, P, 8, P, 512, None) == 1
+    assert emu.emu_grouped_split_rows(0 | K, 8, 8, P, 7, 8, None, P, 2, P, 8, P, 512, None) == 1
