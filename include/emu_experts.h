@@ -122,11 +122,18 @@ emu_status emu_w4_matvec(int dtype, int64_t G, int64_t rows, int64_t N, int64_t 
  *   place, ends [E] the places' ends by expert, as the grouped calls take them.
  * 1 <= k <= 32, k <= E <= 1024, T k < 2^31.  Deterministic.  ws: at least
  * emu_route_workspace_bytes.  Flags: EMU_FLAG_NONFINITE (a logit is NaN or plus
- * infinity), EMU_FLAG_TIMEOUT. */
+ * infinity), EMU_FLAG_TIMEOUT (slots, rows and ends are then not whole). */
 size_t emu_route_workspace_bytes(int64_t T, int64_t E, int64_t k);
 emu_status emu_route(int dtype, int64_t T, int64_t E, int64_t k, int renorm, const void *logits, int64_t ldl,
                      float *weights, int32_t *experts, int32_t *slots, int32_t *rows, int32_t *ends, void *ws,
                      size_t ws_bytes, emu_stream_t stream);
+
+/* Watchdog self-test of emu_route (FP32, renorm = 1, more than 32 tokens): its
+ * blocks wait, timeout_us microseconds at most (1 .. 10^6), for one more than there
+ * are, set EMU_FLAG_TIMEOUT and return; slots, rows and ends are not written. */
+emu_status emu_selftest_route_timeout(uint32_t timeout_us, int64_t T, int64_t E, int64_t k, const float *logits,
+                                      int64_t ldl, float *weights, int32_t *experts, int32_t *slots, int32_t *rows,
+                                      int32_t *ends, void *ws, size_t ws_bytes, emu_stream_t stream);
 
 /* Gradient of the weights' softmax: dlogits (T x E of dtype, row pitch lddl,
  * all entries written) from the weights' gradients dweights [T][k] and the

@@ -79,6 +79,7 @@ _SIGS = {
                             "p"]),
     "emu_route_workspace_bytes": ("size", ["l", "l", "l"]),
     "emu_route": ("i", ["i", "l", "l", "l", "i", "p", "l", "p", "p", "p", "p", "p", "p", "size", "p"]),
+    "emu_selftest_route_timeout": ("i", ["u32", "l", "l", "l", "p", "l", "p", "p", "p", "p", "p", "p", "size", "p"]),
     "emu_route_backward": ("i", ["i", "l", "l", "l", "i", "p", "l", "p", "p", "p", "l", "p"]),
     "emu_rows_combine": ("i", ["i", "l", "l", "l", "p", "l", "l", "p", "p", "p", "l", "p"]),
     "emu_rows_combine_backward": ("i", ["i", "l", "l", "l", "p", "l", "p", "l", "l", "p", "p", "p", "l", "p", "p"]),
@@ -170,6 +171,7 @@ emu_w4_workspace_bytes = _mk("emu_w4_workspace_bytes")
 emu_w4_matvec = _mk("emu_w4_matvec")
 emu_route_workspace_bytes = _mk("emu_route_workspace_bytes")
 emu_route = _mk("emu_route")
+emu_selftest_route_timeout = _mk("emu_selftest_route_timeout")
 emu_route_backward = _mk("emu_route_backward")
 emu_rows_combine = _mk("emu_rows_combine")
 emu_rows_combine_backward = _mk("emu_rows_combine_backward")

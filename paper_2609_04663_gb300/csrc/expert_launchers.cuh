@@ -2,6 +2,7 @@
 #pragma once
 
 #include "../../include/emu_experts.h"
+#include "common.cuh"
 #include "launchers.cuh"
 
 namespace emu {
@@ -48,7 +49,8 @@ bool w4_direct(bool x_f32, const void *X, int64_t ldx);     // X is read as it i
 size_t route_scratch_bytes(int64_t E);
 cudaError_t launch_route(int64_t T, int64_t E, int k, bool renorm, const void *logits, bool f32, int64_t ldl,
                          float *weights, int32_t *experts, int32_t *slots, int32_t *rows, int32_t *ends,
-                         int32_t *counts, WsHeader *ws, cudaStream_t st);
+                         int32_t *counts, WsHeader *ws, cudaStream_t st, uint32_t missing = 0,
+                         unsigned long long limit_ns = kWaitLimitNs);      // missing: arrivals that never come
 cudaError_t launch_route_backward(int64_t T, int64_t E, int k, bool renorm, const void *logits, bool f32, int64_t ldl,
                                   const int32_t *experts, const float *dw, void *dl, int64_t lddl, cudaStream_t st);
 cudaError_t launch_combine(bool f32, int64_t T, int k, int64_t cols, const void *Y, int64_t yrows, int64_t ldy,

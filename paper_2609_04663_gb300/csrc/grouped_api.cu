@@ -75,6 +75,21 @@ emu_status product(int S, int opW, int64_t G, int64_t rows, int64_t N, int64_t K
                                               flags, own_flags, st));
 }
 
+emu_status check_route(int dtype, int64_t T, int64_t E, int64_t k, const void *logits, int64_t ldl, const float *weights,
+                       const int32_t *experts, const int32_t *slots, const int32_t *rows, const int32_t *ends, void *ws,
+                       size_t ws_bytes)
+{
+    if (!known(dtype) || T < 0 || E < 1 || k < 1 || k > E || ldl < E || !ends) return EMU_ERR_INVALID_ARG;
+    if (E > kMaxGroups || k > 32 || T >= kMaxDim / k) return EMU_ERR_UNSUPPORTED;
+    if (T > 0 && (!logits || !weights || !experts || !slots || !rows)) return EMU_ERR_INVALID_ARG;
+    if (!fits(logits, dtype) || !fits(weights, EMU_F32) || !fits(experts, EMU_F32) || !fits(slots, EMU_F32) ||
+        !fits(rows, EMU_F32) || !fits(ends, EMU_F32))
+        return EMU_ERR_MISALIGNED;
+    return check_ws(ws, ws_bytes, kWsHeaderBytes + route_scratch_bytes(E));
+}
+
+int32_t *route_counts(void *ws) { return reinterpret_cast<int32_t *>(static_cast<char *>(ws) + kWsHeaderBytes); }
+
 emu_status check_combine_backward(int dtype, int64_t T, int64_t k, int64_t cols, const void *dO, int64_t lddo,
                                   const void *Y, int64_t yrows, int64_t ldy, const int32_t *slots,
                                   const float *weights, const void *dY, int64_t lddy, const float *dweights)
@@ -310,19 +325,23 @@ emu_status emu_route(int dtype, int64_t T, int64_t E, int64_t k, int renorm, con
                      float *weights, int32_t *experts, int32_t *slots, int32_t *rows, int32_t *ends, void *ws,
                      size_t ws_bytes, emu_stream_t stream)
 {
-    if (!known(dtype) || T < 0 || E < 1 || k < 1 || k > E || ldl < E || !ends) return EMU_ERR_INVALID_ARG;
-    if (E > kMaxGroups || k > 32 || T >= kMaxDim / k) return EMU_ERR_UNSUPPORTED;
-    if (T > 0 && (!logits || !weights || !experts || !slots || !rows)) return EMU_ERR_INVALID_ARG;
-    if (!fits(logits, dtype) || !fits(weights, EMU_F32) || !fits(experts, EMU_F32) || !fits(slots, EMU_F32) ||
-        !fits(rows, EMU_F32) || !fits(ends, EMU_F32))
-        return EMU_ERR_MISALIGNED;
-    emu_status s = check_ws(ws, ws_bytes, emu_route_workspace_bytes(T, E, k));
+    const emu_status s = check_route(dtype, T, E, k, logits, ldl, weights, experts, slots, rows, ends, ws, ws_bytes);
     if (s != EMU_OK) return s;
-    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-    WsHeader *h = static_cast<WsHeader *>(ws);
     return cuda_status(launch_route(T, E, (int)k, renorm != 0, logits, dtype == EMU_F32, ldl, weights, experts, slots,
-                                    rows, ends, reinterpret_cast<int32_t *>(static_cast<char *>(ws) + kWsHeaderBytes),
-                                    h, st));
+                                    rows, ends, route_counts(ws), static_cast<WsHeader *>(ws),
+                                    reinterpret_cast<cudaStream_t>(stream)));
+}
+
+emu_status emu_selftest_route_timeout(uint32_t timeout_us, int64_t T, int64_t E, int64_t k, const float *logits,
+                                      int64_t ldl, float *weights, int32_t *experts, int32_t *slots, int32_t *rows,
+                                      int32_t *ends, void *ws, size_t ws_bytes, emu_stream_t stream)
+{
+    if (timeout_us < 1 || timeout_us > 1000000 || T <= 32) return EMU_ERR_INVALID_ARG;      // (32 tokens: one block)
+    const emu_status s = check_route(EMU_F32, T, E, k, logits, ldl, weights, experts, slots, rows, ends, ws, ws_bytes);
+    if (s != EMU_OK) return s;
+    return cuda_status(launch_route(T, E, (int)k, true, logits, true, ldl, weights, experts, slots, rows, ends,
+                                    route_counts(ws), static_cast<WsHeader *>(ws),
+                                    reinterpret_cast<cudaStream_t>(stream), 1u, 1000ull * timeout_us));
 }
 
 emu_status emu_route_backward(int dtype, int64_t T, int64_t E, int64_t k, int renorm, const void *logits, int64_t ldl,

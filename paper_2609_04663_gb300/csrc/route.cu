@@ -61,30 +61,35 @@ struct RouteArgs {
     int32_t *experts, *slots, *rows, *ends;
     int32_t *counts;                      // [blocks][count_pitch(E)]
     uint32_t *flags, *bar;
+    uint32_t arrivals;                    // blocks that the barrier waits for
+    unsigned long long limit_ns;          // and how long at most
 };
 
 // Row pitch of the blocks' counts: whole 16-byte pieces.
 __host__ __device__ __forceinline__ int count_pitch(int E) { return (E + 3) & ~3; }
 
 // Bounded barrier over the blocks of a cooperative launch (one use per launch;
-// *bar starts at zero).
-__device__ __forceinline__ void route_barrier(uint32_t *bar, uint32_t *flags)
+// *bar starts at zero).  False, in every thread of the block, when the wait was
+// given up: other blocks' counts may be missing then, and the block has to end.
+__device__ __forceinline__ bool route_barrier(const RouteArgs &a)
 {
     __syncthreads();
+    bool late = false;
     if (threadIdx.x == 0) {
         __threadfence();
-        atomicAdd(bar, 1u);
-        volatile uint32_t *seen = bar;
+        atomicAdd(a.bar, 1u);
+        volatile uint32_t *seen = a.bar;
         const unsigned long long t0 = globaltimer_ns();
-        for (uint32_t it = 0; *seen < gridDim.x; ++it) {
-            if ((it & 63u) == 63u && globaltimer_ns() - t0 > kWaitLimitNs) {
-                atomicOr(flags, (uint32_t)EMU_FLAG_TIMEOUT);
+        for (uint32_t it = 0; *seen < a.arrivals; ++it) {
+            if (it >= (1u << 30) || ((it & 63u) == 63u && globaltimer_ns() - t0 > a.limit_ns)) {
+                atomicOr(a.flags, (uint32_t)EMU_FLAG_TIMEOUT);
+                late = true;
                 break;
             }
         }
         __threadfence();
     }
-    __syncthreads();
+    return __syncthreads_or(late ? 1 : 0) == 0;
 }
 
 // V: logits per lane (E <= 32 V).
@@ -236,7 +241,7 @@ __global__ void __launch_bounds__(kRouteThreads) route_kernel(const RouteArgs a)
         if (gridDim.x > 1) a.counts[(int64_t)blockIdx.x * count_pitch(a.E) + e] = sum;
     }
     if (gridDim.x > 1) {
-        route_barrier(a.bar, a.flags);
+        if (!route_barrier(a)) return;                    // slots, rows and ends stay as they were
         // parts of the threads sum up every parts-th block's counts, four experts a thread
         const int quads = (a.E + 3) / 4, parts = max(1, kRouteThreads / quads);
         const int part = (int)threadIdx.x / quads, q = (int)threadIdx.x - part * quads;
@@ -282,6 +287,7 @@ __global__ void __launch_bounds__(kRouteThreads) route_kernel(const RouteArgs a)
     // ---- slots: behind the same expert's assignments of earlier blocks, warps and
     // tokens.  Every lane reads back what it wrote.
     out = (int64_t)w0 * a.k + lane;
+    const uint32_t total = (uint32_t)a.T * (uint32_t)a.k;
     for (int t = w0; t < w1; t += 4) {
         int e[4];
 #pragma unroll
@@ -292,7 +298,8 @@ __global__ void __launch_bounds__(kRouteThreads) route_kernel(const RouteArgs a)
                 const int before = h[e[i]], slot = base[e[i]] + before;
                 h[e[i]] = before + 1;
                 a.slots[out + i * a.k] = slot;
-                a.rows[slot] = t + i;
+                // (a workspace that another call overwrites meanwhile must not lead out of rows)
+                if ((uint32_t)slot < total) a.rows[slot] = t + i;
             }
             __syncwarp();
         }
@@ -669,7 +676,7 @@ size_t route_scratch_bytes(int64_t E) { return (size_t)kRouteBlocks * (size_t)co
 
 cudaError_t launch_route(int64_t T, int64_t E, int k, bool renorm, const void *logits, bool f32, int64_t ldl,
                          float *weights, int32_t *experts, int32_t *slots, int32_t *rows, int32_t *ends,
-                         int32_t *counts, WsHeader *ws, cudaStream_t st)
+                         int32_t *counts, WsHeader *ws, cudaStream_t st, uint32_t missing, unsigned long long limit_ns)
 {
     RouteArgs a = {};
     a.logits = logits; a.ldl = ldl; a.T = (int)T; a.E = (int)E; a.k = k; a.f32 = f32; a.renorm = renorm;
@@ -689,6 +696,7 @@ cudaError_t launch_route(int64_t T, int64_t E, int k, bool renorm, const void *l
         if (e != cudaSuccess) return e;
     }
     if (blocks < 1) blocks = 1;
+    a.arrivals = (uint32_t)blocks + missing; a.limit_ns = limit_ns;
     const int v = (int)((E + 31) / 32);
     return v <= 1 ? run_route<1>(a, (int)blocks, st) : v <= 2 ? run_route<2>(a, (int)blocks, st)
            : v <= 4 ? run_route<4>(a, (int)blocks, st) : v <= 8 ? run_route<8>(a, (int)blocks, st)

@@ -36,3 +36,11 @@ def test_keep_flags_changes_no_check():
     assert emu.emu_grouped_prodsum_wgrad(3 | K, 2, 8, 8, 8, P, 8, 1, P, 8, 0, P, P, 0, 8, 64, P, 512, None) == 1
     assert emu.emu_grouped_split(2 | K, 2, 8, 8, P, 8, 64, P, 8, P, 512, None) == 1
     assert emu.emu_grouped_split_rows(0 | K, 8, 8, P, 7, 8, None, P, 2, P, 8, P, 512, None) == 1
+
+
+def test_routing_self_test_arguments():
+    P, f = 16, emu.emu_selftest_route_timeout
+    for us, T in ((0, 64), (1000001, 64), (1000, 32), (1000, -1)):
+        assert f(us, T, 8, 2, P, 8, P, P, P, P, P, P, 1 << 30, None) == 1
+    assert f(1000, 64, 8, 2, P, 8, P, P, P, P, P, P, 512, None) == 3
+    assert f(1000, 64, 8, 2, P, 8, P, P, P, P + 2, P, P, 1 << 30, None) == 2
