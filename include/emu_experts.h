@@ -63,7 +63,8 @@ emu_status emu_grouped_split_rows(int dtype, int64_t rows, int64_t cols, const v
                                   int64_t ldcomp, void *ws, size_t ws_bytes, emu_stream_t stream);
 
 /* Y[r] = X[r] op(W_g) for every row r of group g: X (rows x K) planes
- * (padded = 1: from emu_grouped_split_rows; 0: rows in their own order), W_g
+ * (padded = 1: from emu_grouped_split_rows with the same rows, G and ends, so of
+ * emu_grouped_plane_rows(rows, G) rows each; 0: rows in their own order), W_g
  * K x N (EMU_OP_N) or N x K (EMU_OP_T) planes, not overlapping, dense over the
  * groups when nslices = 3.  Y: rows x N of ytype, row pitch ldy, any alignment.  The
  * gradient with respect to X is the same call with dY for X and the other op.

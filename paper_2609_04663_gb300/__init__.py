@@ -474,11 +474,21 @@ def _pitch(t, where, device=None):
 class GroupedPlanes:
     """BF16 planes of an operand of the products grouped by expert, from
     grouped_split: planes int16 [S, plane rows, ld]; `shape` is the operand's
-    (rows, cols) for token rows in group order, (G, rows, cols) for weights."""
+    (rows, cols) for token rows in group order, (G, rows, cols) for weights.
+    Token rows are padded for the `ends` that they were split with: a call
+    with other ends needs other planes."""
 
     def __init__(self, planes, shape, padded):
         self.planes, self.shape, self.padded = planes, tuple(shape), padded
         self.device, self.nslices, self.ld = planes.device, planes.shape[0], planes.shape[2]
+
+
+def _whole_planes(t, G, where):
+    """Refuses a plane set that does not have the plane rows of its shape in G groups:
+    the kernels take them as given."""
+    rows = emu_grouped_plane_rows(t.shape[0], G) if t.padded else G * t.shape[1]
+    if t.planes.shape[1] != rows:
+        _bad(where, f"a plane set made for {G} groups is needed")
 
 
 def _slices(t, where):
@@ -564,6 +574,10 @@ def grouped_gemm(X, W, ends, opW: int = OP_N, src=None, Y=None, ws=None, stream=
     K, N = (W.shape[2], W.shape[1]) if opW == OP_T else (W.shape[1], W.shape[2])
     if X.shape[1] != K:
         _bad(where, f"X has {X.shape[1]} columns, op(W) {K} rows")
+    if xp:
+        _whole_planes(X, G, "grouped_gemm: X")
+    if wp:
+        _whole_planes(W, G, "grouped_gemm: W")
     S = _slices(X, where)
     if S != _slices(W, where) or W.device != dev:
         _bad(where, "X and W have to be of one type, on one device")
@@ -618,6 +632,8 @@ def _token_operand(t, ends, src, ws, stream, keep, where):
         t, keep = _split(t, ends, src, None, ws, stream, keep), KEEP_FLAGS
     elif src is not None or not t.padded:
         _bad(where, "a plane set of token rows, already gathered, is needed")
+    else:
+        _whole_planes(t, ends.numel(), where)
     return t, t.planes.data_ptr(), t.ld, 1, t.nslices, keep
 
 

@@ -44,3 +44,31 @@ def test_routing_self_test_arguments():
         assert f(us, T, 8, 2, P, 8, P, P, P, P, P, P, 1 << 30, None) == 1
     assert f(1000, 64, 8, 2, P, 8, P, P, P, P, P, P, 512, None) == 3
     assert f(1000, 64, 8, 2, P, 8, P, P, P, P + 2, P, P, 1 << 30, None) == 2
+
+
+def _planes(S, rows, cols, G, plane_rows=None):
+    import torch
+    n = emu.emu_grouped_plane_rows(rows, G) if plane_rows is None else plane_rows
+    return emu.GroupedPlanes(torch.zeros((S, n, emu.gemm_ldk(cols)), dtype=torch.int16), (rows, cols), True)
+
+
+@pytest.mark.parametrize("made,used", [(4, 512), (512, 4), (1, 2)])
+def test_planes_of_token_rows_belong_to_a_number_of_groups(made, used):
+    """Rows padded for other groups lie elsewhere, and a plane set made for fewer
+    of them ends before the rows that the kernels would read."""
+    import torch
+    ends = torch.zeros(used, dtype=torch.int32)
+    for S, dt in ((3, torch.float32), (1, torch.bfloat16)):
+        X, W, B = _planes(S, 40, 24, made), torch.zeros((used, 24, 16), dtype=dt), _planes(S, 40, 16, used)
+        for call in (lambda: emu.grouped_gemm(X, W, ends), lambda: emu.grouped_wgrad(X, B, ends),
+                     lambda: emu.grouped_wgrad(B, X, ends)):
+            with pytest.raises(ValueError, match=f"{used} groups"):
+                call()
+
+
+def test_planes_of_weights_are_whole():
+    import torch
+    ends = torch.zeros(3, dtype=torch.int32)
+    W = emu.GroupedPlanes(torch.zeros((3, 2 * 24, 16), dtype=torch.int16), (3, 24, 16), False)
+    with pytest.raises(ValueError, match="3 groups"):
+        emu.grouped_gemm(_planes(3, 40, 24, 3), W, ends)
