@@ -205,6 +205,7 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps) w4_kernel(const W4Ar
                         else static_cast<uint16_t *>(a.Y)[r * a.ldy + n] = 0;
                     }
             }
+            if (!DIRECT) griddep_wait();              // this launch may not end before the planes' kernel has
             return;
         }
         __syncthreads();                              // the tables are read, the rings may be filled
