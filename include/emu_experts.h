@@ -31,7 +31,8 @@ extern "C" {
  * ends[g-1] .. ends[g]-1 (ends[-1] = 0; device int32[G], non-decreasing, at
  * most rows).  Groups may be empty; rows from ends[G-1] on belong to no group:
  * they contribute nothing and their result rows are zero.  Group sizes are
- * read on the device, nothing synchronises with the host.  1 <= G <= 1024.
+ * read on the device, nothing synchronises with the host.  1 <= G <= 1024; rows,
+ * K and N (M and N) each below 2^31 - 65536.
  *
  * Operands are plane sets of nslices BF16 planes: 3 for FP32 operands (the
  * split of Eq. (fp32split); products are Eq. (fp32six), FP32 accumulation), 1
@@ -121,7 +122,7 @@ emu_status emu_w4_matvec(int dtype, int64_t G, int64_t rows, int64_t N, int64_t 
  * and the order of the T k assignments by expert, then token, then rank:
  *   slots [T][k] the place of each in that order, rows [T k] the token at each
  *   place, ends [E] the places' ends by expert, as the grouped calls take them.
- * 1 <= k <= 32, k <= E <= 1024, T k < 2^31.  Deterministic.  ws: at least
+ * 1 <= k <= 32, k <= E <= 1024, T k < 2^31 - 65536.  Deterministic.  ws: at least
  * emu_route_workspace_bytes.  Flags: EMU_FLAG_NONFINITE (a logit is NaN or plus
  * infinity), EMU_FLAG_TIMEOUT (slots, rows and ends are then not whole). */
 size_t emu_route_workspace_bytes(int64_t T, int64_t E, int64_t k);

@@ -7,7 +7,10 @@ using namespace emu;
 
 namespace {
 
-constexpr int64_t kMaxDim = (int64_t)1 << 31;      // kernels index with 32-bit coordinates
+// Kernels index with 32-bit coordinates, which they take up to a tile, a stage or
+// a block's share past the last element: sizes that they walk through stay
+// below kMaxWalk.
+constexpr int64_t kMaxDim = (int64_t)1 << 31, kMaxWalk = kMaxDim - 65536;
 
 int64_t round_up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -42,7 +45,7 @@ bool take_keep(int &arg)
 emu_status check_sizes(int64_t G, int64_t rows, int64_t a, int64_t b)
 {
     if (G < 1 || rows < 0 || a < 0 || b < 0) return EMU_ERR_INVALID_ARG;
-    if (G > kMaxGroups || rows >= kMaxDim - 65536 || a >= kMaxDim || b >= kMaxDim || G * a >= kMaxDim || G * b >= kMaxDim)
+    if (G > kMaxGroups || rows >= kMaxWalk || a >= kMaxWalk || b >= kMaxWalk || G * a >= kMaxDim || G * b >= kMaxDim)
         return EMU_ERR_UNSUPPORTED;
     const int64_t ta = a / 128 + 1, tb = b / 128 + 1;
     if ((rows / 64 + G + 1) * ta >= kMaxDim || (rows / 64 + G + 1) * tb >= kMaxDim || G * ta >= kMaxDim / tb)
@@ -80,7 +83,7 @@ emu_status check_route(int dtype, int64_t T, int64_t E, int64_t k, const void *l
                        size_t ws_bytes)
 {
     if (!known(dtype) || T < 0 || E < 1 || k < 1 || k > E || ldl < E || !ends) return EMU_ERR_INVALID_ARG;
-    if (E > kMaxGroups || k > 32 || T >= kMaxDim / k) return EMU_ERR_UNSUPPORTED;
+    if (E > kMaxGroups || k > 32 || T >= kMaxWalk / k) return EMU_ERR_UNSUPPORTED;
     if (T > 0 && (!logits || !weights || !experts || !slots || !rows)) return EMU_ERR_INVALID_ARG;
     if (!fits(logits, dtype) || !fits(weights, EMU_F32) || !fits(experts, EMU_F32) || !fits(slots, EMU_F32) ||
         !fits(rows, EMU_F32) || !fits(ends, EMU_F32))

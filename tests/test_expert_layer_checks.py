@@ -72,3 +72,19 @@ def test_planes_of_weights_are_whole():
     W = emu.GroupedPlanes(torch.zeros((3, 2 * 24, 16), dtype=torch.int16), (3, 24, 16), False)
     with pytest.raises(ValueError, match="3 groups"):
         emu.grouped_gemm(_planes(3, 40, 24, 3), W, ends)
+
+
+@pytest.mark.parametrize("near", [1, 60, 65535])
+def test_sizes_next_to_2_31_are_refused(near):
+    """Kernels step over tokens, rows and contractions with 32-bit numbers, by whole
+    tiles and shares of a block: a size closer to 2^31 than those would wrap."""
+    P, n = 16, 2 ** 31 - near
+    assert emu.emu_route(1, n, 1, 1, 1, P, 1, P, P, P, P, P, P, 1 << 40, None) == 5
+    assert emu.emu_route(0, n // 2 + 1, 2, 2, 1, P, 2, P, P, P, P, P, P, 1 << 40, None) == 5
+    assert emu.emu_selftest_route_timeout(1000, n, 1, 1, P, 1, P, P, P, P, P, P, 1 << 40, None) == 5
+    n8 = n // 32 * 32                       # a contraction of whole scale groups
+    assert emu.emu_w4_matvec(1, 1, 1, 1, n8, 32, P, n8, P, P, 1, None, None, P, 1, None, 0, None) == 5
+    for N, K in ((n, 8), (8, n)):
+        assert emu.emu_grouped_prodsum(1, 1, 1, 8, N, K, P, 1 << 32, 0, P, 1 << 32, 0, P, P, 1, N, P, 512, None) == 5
+        assert emu.emu_grouped_prodsum_wgrad(1, 1, 8, N, K, P, 1 << 32, 0, P, 1 << 32, 0, P, P, 1, K, 0, P, 512, None) == 5
+        assert emu.emu_grouped_gemm_f32(1, 1, 8, N, K, P, 8, K, None, P, K, 0, P, P, N, P, 1 << 62, None) == 5
