@@ -553,8 +553,11 @@ def grouped_workspace(X, W, ends, opW: int = OP_N, src=None, train: bool = False
     rows = src.numel() if src is not None else X.shape[0]
     G = ends.numel()
     K, N = (W.shape[2], W.shape[1]) if opW == OP_T else (W.shape[1], W.shape[2])
-    f32 = not isinstance(X, GroupedPlanes) and X.dtype == _torch().float32 and not train
-    return workspace(emu_grouped_gemm_workspace_bytes(F32 if f32 else BF16, G, rows, N, K), X.device)
+    dt = F32 if not isinstance(X, GroupedPlanes) and X.dtype == _torch().float32 else BF16
+    need = emu_grouped_gemm_workspace_bytes(dt, G, rows, N, K)
+    if train:                                         # the rows' gradient: the product with K and N exchanged
+        need = max(need, emu_grouped_gemm_workspace_bytes(dt, G, rows, K, N))
+    return workspace(need, X.device)
 
 
 def grouped_gemm(X, W, ends, opW: int = OP_N, src=None, Y=None, ws=None, stream=None):

@@ -88,3 +88,15 @@ def test_sizes_next_to_2_31_are_refused(near):
         assert emu.emu_grouped_prodsum(1, 1, 1, 8, N, K, P, 1 << 32, 0, P, 1 << 32, 0, P, P, 1, N, P, 512, None) == 5
         assert emu.emu_grouped_prodsum_wgrad(1, 1, 8, N, K, P, 1 << 32, 0, P, 1 << 32, 0, P, P, 1, K, 0, P, 512, None) == 5
         assert emu.emu_grouped_gemm_f32(1, 1, 8, N, K, P, 8, K, None, P, K, 0, P, P, N, P, 1 << 62, None) == 5
+
+
+def test_a_training_steps_workspace_is_enough_for_every_call():
+    import torch
+    ends = torch.zeros(3, dtype=torch.int32)
+    for dt, code in ((torch.float32, emu.F32), (torch.bfloat16, emu.BF16)):
+        for K, N in ((24, 200), (200, 24)):
+            need = max(emu.emu_grouped_gemm_workspace_bytes(code, 3, 60, *s) for s in ((N, K), (K, N)))
+            for W, op in ((torch.zeros(3, K, N, dtype=dt), emu.OP_N), (torch.zeros(3, N, K, dtype=dt), emu.OP_T)):
+                X = torch.zeros(60, K, dtype=dt)
+                assert emu.grouped_workspace(X, W, ends, op, train=True).numel() >= need
+                assert emu.grouped_workspace(X, W, ends, op).numel() >= emu.emu_grouped_gemm_workspace_bytes(code, 3, 60, N, K)
