@@ -108,7 +108,11 @@ emu_status emu_grouped_prodsum_wgrad(int nslices, int64_t G, int64_t rows, int64
  * decreasing are clamped.  Rows of no group are zero.  Up to
  * 131070 rows are computed; the weights are read again for every 24 (BF16) or 8
  * (FP32) of an expert.  q 16-byte aligned.  ws: emu_w4_workspace_bytes, 16-byte aligned, for
- * X's slices; NULL will do for BF16 rows of 16-byte aligned base and pitch. */
+ * X's slices; for BF16 rows of 16-byte aligned base and pitch
+ * emu_split_workspace_bytes(32) are enough (the flags), or NULL, which reports none.
+ * An FP32 value of 0x1.FFp+127 or more (in magnitude) has slices that are not
+ * finite, and a row with one comes out as NaN.  Flags: EMU_FLAG_INDEX,
+ * EMU_FLAG_NONFINITE and EMU_FLAG_SLICE (of all of X, FP32). */
 size_t emu_w4_workspace_bytes(int dtype, int64_t rows, int64_t K);
 emu_status emu_w4_matvec(int dtype, int64_t G, int64_t rows, int64_t N, int64_t K, int64_t group, const void *X,
                          int64_t ldx, const uint8_t *q, const void *s, int stype, const uint8_t *z,

@@ -674,7 +674,8 @@ def w4_matvec(X, Wq, scales, zeros=None, ends=None, Y=None, ws=None, stream=None
     [G, N, K/2], the even k in the low half of a byte; scales FP32 or BF16 and
     zeros uint8 (None: 8) [G, N, K/group].  X and Y: FP32 or BF16.  For a few
     rows per expert.  ws: emu_w4_workspace_bytes bytes that a caller may keep
-    (made here where they are needed).  Returns Y."""
+    (made here where they are needed); the call's flags are in a given one.
+    Returns Y."""
     torch, where = _torch(), "w4_matvec"
     dev, u8 = X.device, torch.uint8
     dt, ldx, (rows, K) = _dtype(X, "w4_matvec: X"), _pitch(X, "w4_matvec: X"), X.shape
@@ -698,7 +699,7 @@ def w4_matvec(X, Wq, scales, zeros=None, ends=None, Y=None, ws=None, stream=None
         _bad(where, "Y has another shape or type")
     x = X.data_ptr()
     if ws is None and (dt == F32 or x % 16 or ldx % 8):
-        ws = _empty(rows * K * (6 if dt == F32 else 2), u8, dev, stream)
+        ws = _empty(_lib.emu_w4_workspace_bytes(dt, rows, K), u8, dev, stream)
     r = _lib.emu_w4_matvec(dt, G, rows, N, K, group, x, ldx, Wq.data_ptr(), scales.data_ptr(),
                            _dtype(scales, "w4_matvec: scales"), zeros.data_ptr() if zeros is not None else None,
                            _ints(ends, G, dev, "w4_matvec: ends") if ends is not None else None, Y.data_ptr(),

@@ -44,7 +44,8 @@ cudaError_t launch_grouped_gradient(int nslices, int64_t G, int64_t rows, int64_
 // sum of answers (route.cu).
 cudaError_t launch_w4_matvec(bool x_f32, int64_t G, int64_t rows, int64_t N, int64_t K, int group, const void *X,
                              int64_t ldx, const uint8_t *q, const void *scales, bool s_f32, const uint8_t *zeros,
-                             const int32_t *ends, void *Y, int64_t ldy, uint16_t *planes, cudaStream_t st);
+                             const int32_t *ends, void *Y, int64_t ldy, uint16_t *planes, uint32_t *flags,
+                             cudaStream_t st);
 bool w4_direct(bool x_f32, const void *X, int64_t ldx);     // X is read as it is, without planes
 size_t route_scratch_bytes(int64_t E);
 cudaError_t launch_route(int64_t T, int64_t E, int k, bool renorm, const void *logits, bool f32, int64_t ldl,

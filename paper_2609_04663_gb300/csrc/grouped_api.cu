@@ -286,9 +286,10 @@ emu_status emu_grouped_prodsum_wgrad(int nslices, int64_t G, int64_t rows, int64
                                                &static_cast<WsHeader *>(ws)->flags, !keep, st));
 }
 
+// The flag word and the slices.
 size_t emu_w4_workspace_bytes(int dtype, int64_t rows, int64_t K)
 {
-    return rows < 0 || K < 0 ? 0 : (size_t)rows * (size_t)K * (dtype == EMU_F32 ? 6 : 2);
+    return rows < 0 || K < 0 ? 0 : kWsHeaderBytes + (size_t)rows * (size_t)K * (dtype == EMU_F32 ? 6 : 2);
 }
 
 emu_status emu_w4_matvec(int dtype, int64_t G, int64_t rows, int64_t N, int64_t K, int64_t group, const void *X,
@@ -300,21 +301,30 @@ emu_status emu_w4_matvec(int dtype, int64_t G, int64_t rows, int64_t N, int64_t 
         return EMU_ERR_INVALID_ARG;
     emu_status s = check_sizes(G, rows, N, K);
     if (s != EMU_OK) return s;
-    if (rows == 0 || N == 0) return EMU_OK;
-    if (!Y) return EMU_ERR_INVALID_ARG;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     const int esize = dtype == EMU_F32 ? 4 : 2;
-    if (K == 0) return cuda_status(zero_rows(Y, rows, N, ldy, esize, st));
-    if (!X || !q || !scales) return EMU_ERR_INVALID_ARG;
+    if (rows == 0 || N == 0 || K == 0) {                        // nothing to multiply
+        if (rows > 0 && N > 0 && !Y) return EMU_ERR_INVALID_ARG;
+        if (ws) {
+            s = check_ws(ws, ws_bytes, kWsHeaderBytes);
+            if (s != EMU_OK) return s;
+            if (clear_flags(ws, st) != cudaSuccess) return EMU_ERR_CUDA;
+        }
+        return cuda_status(zero_rows(Y, rows, N, ldy, esize, st));
+    }
+    if (!Y || !X || !q || !scales) return EMU_ERR_INVALID_ARG;
     if (!aligned16(q) || !fits(X, dtype) || !fits(Y, dtype) || !fits(scales, stype) || !fits(ends, EMU_F32))
         return EMU_ERR_MISALIGNED;
     if (rows > 65535 * 2) return EMU_ERR_UNSUPPORTED;           // items of two rows and more on the grid's y dimension
-    if (!w4_direct(dtype == EMU_F32, X, ldx)) {
-        s = check_ws(ws, ws_bytes, emu_w4_workspace_bytes(dtype, rows, K));
+    const bool direct = w4_direct(dtype == EMU_F32, X, ldx);
+    if (!direct || ws) {
+        s = check_ws(ws, ws_bytes, direct ? kWsHeaderBytes : emu_w4_workspace_bytes(dtype, rows, K));
         if (s != EMU_OK) return s;
     }
     return cuda_status(launch_w4_matvec(dtype == EMU_F32, G, rows, N, K, (int)group, X, ldx, q, scales,
-                                        stype == EMU_F32, zeros, ends, Y, ldy, static_cast<uint16_t *>(ws), st));
+                                        stype == EMU_F32, zeros, ends, Y, ldy,
+                                        direct ? nullptr : reinterpret_cast<uint16_t *>(static_cast<char *>(ws) + kWsHeaderBytes),
+                                        ws ? &static_cast<WsHeader *>(ws)->flags : nullptr, st));
 }
 
 size_t emu_route_workspace_bytes(int64_t T, int64_t E, int64_t k)

@@ -100,3 +100,13 @@ def test_a_training_steps_workspace_is_enough_for_every_call():
                 X = torch.zeros(60, K, dtype=dt)
                 assert emu.grouped_workspace(X, W, ends, op, train=True).numel() >= need
                 assert emu.grouped_workspace(X, W, ends, op).numel() >= emu.emu_grouped_gemm_workspace_bytes(code, 3, 60, N, K)
+
+
+def test_4_bit_workspaces():
+    P, w = 16, emu.emu_w4_matvec
+    need = emu.emu_w4_workspace_bytes(emu.F32, 2, 64)
+    assert need >= emu.emu_split_workspace_bytes(32) + 2 * 64 * 6
+    assert w(0, 1, 2, 8, 64, 32, P, 64, P, P, 0, None, None, P, 8, P, need - 1, None) == 3
+    assert w(0, 1, 2, 8, 64, 32, P, 64, P, P, 0, None, None, P, 8, P + 8, need, None) == 2
+    assert w(1, 1, 2, 8, 64, 32, P, 64, P, P, 1, None, None, P, 8, P, 511, None) == 3            # no room for the flags
+    assert w(1, 1, 2, 8, 64, 32, P + 2, 64, P, P, 1, None, None, P, 8, P, 512, None) == 3        # rows that need slices
