@@ -36,8 +36,10 @@ extern "C" {
  *
  * Operands are plane sets of nslices BF16 planes: 3 for FP32 operands (the
  * split of Eq. (fp32split); products are Eq. (fp32six), FP32 accumulation), 1
- * for BF16 operands (exact products, FP32 accumulation, one rounding to the
- * result's type).  BF16 token rows and weights whose base is 16-byte aligned
+ * for BF16 operands (exact products, one rounding to the result's type).  Sums are
+ * in FP32: for FP32 results rounded every 256 terms, for BF16 results in one
+ * accumulator, to which the tensor cores add with truncation (1.6e-4 of a result
+ * over 32768 terms of one sign, before the rounding to BF16's 8 bits).  BF16 token rows and weights whose base is 16-byte aligned
  * and whose row pitch and matrix distance are multiples of 8 elements are such
  * a plane as they stand.
  * ------------------------------------------------------------------------- */

@@ -16,11 +16,21 @@
 // operands, before it passes the stage on to the MMAs (a zero times an infinity
 // would not be zero).
 //
+// BF16 results take one accumulator over the whole contraction: the tensor cores
+// truncate when they add to it, 9e-6 of a result over 8192 terms of either sign and
+// 1.6e-4 over 32768 of one sign (2-norm), below the rounding to 8 bits (1.7e-3).  FP32
+// results (SUM) read it every 256 terms, from two accumulators in turn while the MMAs
+// go on in the other, and add in FP32 with rounding in registers: 2.3e-7 to 3.4e-7 for
+// 512 to 32768 terms.  64 groups of 512 rows, 2048 x 4096: 418 us (368 without the sums,
+// 333 for BF16 results).
+//
 // Bound by the copies from L2 into the SMs (41-45 bytes per clock and SM) where
 // groups have hundreds of rows: 64 uneven groups of 512 rows on average, 2048 x 4096:
 // 411 us (1.34 PFLOP/s), the rows' gradient 392, the weights' 455 (1.21; only 8
 // K-blocks between two epilogues); by reading the weights with few: 32 groups
 // of 4 to 64 rows 81-87 us (6.6-6.1 TB/s), one row of 4 groups 14 us.
+#include <type_traits>
+
 #include "grouped_tile.cuh"
 
 namespace emu {
@@ -105,13 +115,15 @@ __device__ __forceinline__ void zero_rows_of(uint32_t at, int blocks, int from, 
 }
 
 // LMN / CMN: the feature / column operand is stored with its MN dimension
-// contiguous (else with the contraction contiguous).  CMN is the gradient.
-template <int BC, bool PAIR, bool LMN, bool CMN>
+// contiguous (else with the contraction contiguous).  CMN is the gradient.  SUM:
+// FP32 results, tiles of one half; else BF16.
+template <int BC, bool PAIR, bool LMN, bool CMN, bool SUM>
 __global__ void __launch_bounds__(Bf16Cfg<BC, PAIR>::THREADS + (CMN ? 32 : 0), 1)
 grouped_bf16_kernel(const __grid_constant__ CUtensorMap tmL, const __grid_constant__ CUtensorMap tmC,
                     const __grid_constant__ CUtensorMap tmS, const GroupedArgs a)
 {
     using Cfg = Bf16Cfg<BC, PAIR>;
+    static_assert(!SUM || Cfg::HALVES == 1, "FP32 sums are held for one half");
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t base = (raw + 1023u) & ~1023u;
@@ -266,6 +278,28 @@ grouped_bf16_kernel(const __grid_constant__ CUtensorMap tmL, const __grid_consta
             const uint32_t n0 = (uint32_t)uniform(x.n[0]), n1 = Cfg::HALVES == 2 ? (uint32_t)uniform(x.n[1]) : 0u;
             constexpr uint32_t id0 = make_idesc_bf16(kLRows * Cfg::CTAS, 0) | (LMN ? 1u << 15 : 0u) | (CMN ? 1u << 16 : 0u);
             const uint32_t i0 = id0 | n0 >> 3 << 17, i1 = id0 | n1 >> 3 << 17;
+            if constexpr (SUM) {
+                for (int kb = 0; kb < nkb; ++kb) {
+                    const uint32_t b = uses & 1u;
+                    const int kc = kb % kChunkBlocks, left = nk - kb * kKB;
+                    if (kc == 0) {                    // this accumulator's last sum has been read
+                        if (!(ok = warp_wait(tempty0 + 8u * b, ((uses >> 1) & 1u) ^ 1u, flags))) break;
+                        tc_fence_after();
+                    }
+                    if (!(ok = warp_wait(full0 + 8u * s, ph, flags))) break;
+                    tc_fence_after();
+                    const uint32_t st = (base + s * (uint32_t)Cfg::STAGE) >> 4;
+#pragma unroll
+                    for (int kk = 0; kk < kKB / 16; ++kk)
+                        if (16 * kk < left)
+                            mma_elected<PAIR>(elected, tmem + b * 256u, descL + (st + (uint32_t)((kk * kstepL) >> 4)),
+                                              descC + (st + (uint32_t)((Cfg::L_TILE + kk * kstepC) >> 4)), i0, (kc | kk) != 0);
+                    commit_elected<PAIR>(elected, empty0 + 8u * s);
+                    if (kc == kChunkBlocks - 1 || kb == nkb - 1) { commit_elected<PAIR>(elected, tfull0 + 8u * b); ++uses; }
+                    if (++s == Cfg::STAGES) { s = 0; ph ^= 1u; }
+                }
+                continue;
+            }
             const uint32_t b0 = uses & 1u, b1 = b0 ^ 1u, d0 = tmem + b0 * 256u, d1 = tmem + b1 * 256u;
             const uint32_t p0 = ((uses >> 1) & 1u) ^ 1u, p1 = (((uses + 1u) >> 1) & 1u) ^ 1u;
             if (!(ok = warp_wait(tempty0 + 8u * b0, p0, flags))) break;
@@ -342,48 +376,86 @@ grouped_bf16_kernel(const __grid_constant__ CUtensorMap tmL, const __grid_consta
         // ---------------- epilogue: this CTA's 128 features of each half; a warp
         // has a quarter of the lanes and WCOLS of the columns
         const int quarter = warp & 3, h0 = ((warp - 2) >> 2) * Cfg::WCOLS;
-        const int esize = a.out_f32 ? 4 : 2;
+        constexpr int esize = SUM ? 4 : 2;
         const bool pairs_ok = (a.ldo & 1) == 0 && (a.strideo & 1) == 0 && (reinterpret_cast<uintptr_t>(a.out) & 3u) == 0;
         const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)h0;
         if constexpr (!CMN) zero_rest(a, starts, (int)threadIdx.x - 64, 32 * Cfg::EPI_WARPS);
+        auto release = [&](uint32_t bar) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                if constexpr (PAIR) mbar_arrive_peer(peer_addr(bar, 0));
+                else mbar_arrive(bar);
+            }
+        };
         uint32_t uses = 0;
         bool ok = true;
         for (int t = first; t < total && ok; t += step) {
             const HalfTile x = tile(t);
             const int l = x.l0 + quarter * 32;
-#pragma unroll 1
-            for (int h = 0; h < (x.n[1] ? 2 : 1); ++h) {
-                const int c0 = (h ? x.n[0] : 0) + h0;                     // this warp's first column of the tile
-                const int cols = min(h ? x.cols - x.n[0] : x.n[0], x.cols) - h0;
-                const int64_t row0 = (CMN ? 0 : (int64_t)starts[x.g]) + x.c0 + c0;
-                char *o = static_cast<char *>(a.out) + (row0 * a.ldo + (CMN ? x.g * a.strideo : 0)) * esize;
-                const uint32_t b = uses & 1u;
-                // tcgen05.ld needs the whole warp, so a timeout in any lane ends the warp's work
-                if (x.nk > 0) {
+            if constexpr (SUM) {
+                const int cols = x.cols - h0;             // columns from this warp's first on
+                float acc[Cfg::WCOLS];
+#pragma unroll
+                for (int j = 0; j < Cfg::WCOLS; ++j) acc[j] = 0.0f;
+                const int nch = (x.nk + kKChunk - 1) / kKChunk;
+                for (int c = 0; c < nch; ++c, ++uses) {
+                    const uint32_t b = uses & 1u;
                     if (!(ok = warp_wait(tfull0 + 8u * b, (uses >> 1) & 1u, flags))) break;
                     tc_fence_after();
-                }
-#pragma unroll 1
-                for (int c = 0; c < Cfg::WCOLS; c += 32) {
-                    if (c >= cols) break;
-                    uint32_t v[32];
-                    if (x.nk > 0) {
-                        tmem_ld32(lanes + b * 256u + (uint32_t)c, v);
-                        tmem_ld_wait();
-                    } else {
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] = 0u;
+                    for (int h = 0; h < Cfg::WCOLS; h += 16) {
+                        if (h < cols) {
+                            uint32_t v[16];
+                            tmem_load16(lanes + b * 256u + (uint32_t)h, v);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) acc[h + j] = __fadd_rn(acc[h + j], __uint_as_float(v[j]));
+                        }
                     }
-                    if (l < a.L)
-                        store_columns(v, cols - c, o + (int64_t)c * a.ldo * esize, a.ldo, l, a.L, a.out_f32 != 0, pairs_ok);
+                    release(tempty0 + 8u * b);
                 }
-                if (x.nk == 0) continue;
-                ++uses;
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) {
-                    if constexpr (PAIR) mbar_arrive_peer(peer_addr(tempty0 + 8u * b, 0));
-                    else mbar_arrive(tempty0 + 8u * b);
+                const int64_t row0 = (CMN ? 0 : (int64_t)starts[x.g]) + x.c0 + h0;
+                float *o = static_cast<float *>(a.out) + row0 * a.ldo + (CMN ? x.g * a.strideo : 0);
+                if (ok && l < a.L) {
+#pragma unroll
+                    for (int h = 0; h < Cfg::WCOLS; h += 32) {
+                        float v[32];
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] = acc[h + j];
+                        if (h < cols) store_columns(v, cols - h, o + (int64_t)h * a.ldo, a.ldo, l, a.L, true, false);
+                    }
+                }
+            } else {
+#pragma unroll 1
+                for (int h = 0; h < (x.n[1] ? 2 : 1); ++h) {
+                    const int c0 = (h ? x.n[0] : 0) + h0;                     // this warp's first column of the tile
+                    const int cols = min(h ? x.cols - x.n[0] : x.n[0], x.cols) - h0;
+                    const int64_t row0 = (CMN ? 0 : (int64_t)starts[x.g]) + x.c0 + c0;
+                    char *o = static_cast<char *>(a.out) + (row0 * a.ldo + (CMN ? x.g * a.strideo : 0)) * esize;
+                    const uint32_t b = uses & 1u;
+                    // tcgen05.ld needs the whole warp, so a timeout in any lane ends the warp's work
+                    if (x.nk > 0) {
+                        if (!(ok = warp_wait(tfull0 + 8u * b, (uses >> 1) & 1u, flags))) break;
+                        tc_fence_after();
+                    }
+#pragma unroll 1
+                    for (int c = 0; c < Cfg::WCOLS; c += 32) {
+                        if (c >= cols) break;
+                        uint32_t v[32];
+                        if (x.nk > 0) {
+                            tmem_ld32(lanes + b * 256u + (uint32_t)c, v);
+                            tmem_ld_wait();
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) v[j] = 0u;
+                        }
+                        if (l < a.L)
+                            store_columns(v, cols - c, o + (int64_t)c * a.ldo * esize, a.ldo, l, a.L, false, pairs_ok);
+                    }
+                    if (x.nk == 0) continue;
+                    ++uses;
+                    release(tempty0 + 8u * b);
                 }
             }
         }
@@ -400,12 +472,12 @@ grouped_bf16_kernel(const __grid_constant__ CUtensorMap tmL, const __grid_consta
     }
 }
 
-template <int BC, bool PAIR, bool LMN, bool CMN>
+template <int BC, bool PAIR, bool LMN, bool CMN, bool SUM>
 cudaError_t run_bf16(const CUtensorMap &tl, const CUtensorMap &tc, const CUtensorMap &ts, const GroupedArgs &a, int64_t tiles,
                      cudaStream_t st)
 {
     using Cfg = Bf16Cfg<BC, PAIR>;
-    return launch_persistent<grouped_bf16_kernel<BC, PAIR, LMN, CMN>>(Cfg::SMEM, Cfg::THREADS + (CMN ? 32 : 0), Cfg::CTAS,
+    return launch_persistent<grouped_bf16_kernel<BC, PAIR, LMN, CMN, SUM>>(Cfg::SMEM, Cfg::THREADS + (CMN ? 32 : 0), Cfg::CTAS,
                                                                       tiles, st, tl, tc, ts, a);
 }
 
@@ -434,11 +506,14 @@ cudaError_t product(const GroupedOperand &X, const GroupedOperand &W, GroupedArg
         !make_group_map(&ts, X.planes, a.K, X.rows, 1, 1, X.ld, 0, X.plane, 16))
         return cudaErrorInvalidValue;
     const int bc = columns_for((a.rows + a.G - 1) / a.G, a.L, a.G);
-    if (bc == 512)
-        return run_bf16<512, true, LMN, false>(tl, tc, ts, a, max_tiles(a.rows, a.G, a.L, 512, 2), st);
-    if (bc == 256)
-        return run_bf16<256, true, LMN, false>(tl, tc, ts, a, max_tiles(a.rows, a.G, a.L, 256, 2), st);
-    return run_bf16<64, false, LMN, false>(tl, tc, ts, a, max_tiles(a.rows, a.G, a.L, 64, 1), st);
+    auto run = [&](auto sum) {
+        constexpr bool SUM = decltype(sum)::value;
+        if constexpr (!SUM)
+            if (bc == 512) return run_bf16<512, true, LMN, false, false>(tl, tc, ts, a, max_tiles(a.rows, a.G, a.L, 512, 2), st);
+        if (bc >= 256) return run_bf16<256, true, LMN, false, SUM>(tl, tc, ts, a, max_tiles(a.rows, a.G, a.L, 256, 2), st);
+        return run_bf16<64, false, LMN, false, SUM>(tl, tc, ts, a, max_tiles(a.rows, a.G, a.L, 64, 1), st);
+    };
+    return a.out_f32 ? run(std::true_type{}) : run(std::false_type{});
 }
 
 }  // namespace
@@ -458,7 +533,9 @@ cudaError_t launch_bf16_gradient(const GroupedOperand &A, const GroupedOperand &
     a.padded = A.padded;
     // (512 columns: 547 us for 64 groups of 512 rows, 2048 x 4096, against 495; a
     // short contraction does not hide the reading of two halves)
-    return run_bf16<256, true, true, true>(tl, tc, tc, a, (int64_t)a.G * ((a.L + 255) / 256) * ((a.C + 255) / 256), st);
+    const int64_t tiles = (int64_t)a.G * ((a.L + 255) / 256) * ((a.C + 255) / 256);
+    return a.out_f32 ? run_bf16<256, true, true, true, true>(tl, tc, tc, a, tiles, st)
+                     : run_bf16<256, true, true, true, false>(tl, tc, tc, a, tiles, st);
 }
 
 }  // namespace emu
