@@ -1,4 +1,4 @@
-// C-ABI of the products grouped by expert (declared in include/emu.h):
+// C-ABI of the expert layers (declared in include/emu_experts.h):
 // argument checks, workspace layout and launch sequences.
 #include "grouped_common.cuh"
 #include "expert_launchers.cuh"

@@ -12,7 +12,8 @@
 // FP32 accumulators): the codes q - z are integers of at most 15 and exact in
 // BF16, 16 features are its rows, and its 8 columns are BF16 rows of X, or the
 // three BF16 slices (Eq. (fp32split)) of FP32 rows, whose products are exact as
-// well.  tcgen05 would need the decoded weights back in shared memory.  A code
+// well.  (tcgen05 could take decoded weights as its A operand from tensor memory,
+// written there by the decoding warps; that form has not been built.)  A code
 // pair becomes BF16 by one or-with-mask (128 + q) and one multiply-add that
 // takes 128 + z off; since a dot product may take its k in any order, the pairs are the
 // nibbles i and i + 4 of a word, and X is staged in that order.  Sums of one
@@ -31,9 +32,9 @@
 // registers allow (more warps spill and are slower; 16 features per CTA: 29 us
 // for the 16 rows; K split over a cluster with X staged for 256 features: 28 us
 // and 53 us for 7 FP32 rows).
-// Measured (GPU time, weights from HBM): 1 row x 4096 x 4096 5.8 us; 1 row x 16384 x
-// 16384 47 us (2.8 TB/s of weights); 16 rows over 12 experts of 2048 x 4096 25 us;
-// 7 FP32 rows x 16384 x 8192 41 us with the slices' kernel.
+// Measured (GPU time, weights from HBM): 1 row x 4096 x 4096 5.9 us; 1 row x 16384 x
+// 16384 44-47 us (2.8-3.1 TB/s of weights); 16 rows over 12 experts of 2048 x 4096 25 us;
+// 7 FP32 rows x 16384 x 8192 42 us with the slices' and the flags' kernels.
 #include "grouped_common.cuh"
 #include "expert_launchers.cuh"
 #include "split_f32_pair.cuh"
