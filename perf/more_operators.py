@@ -160,10 +160,12 @@ def prepare(case, seed):
             s["ends"] = torch.tensor(ends, dtype=torch.int32, device="cuda")
     else:
         T, E, k = c["tokens"], c["experts"], c["k"]
-        s["logits"] = _normal(g, (T, E), dt, 1.5)
+        # some experts are liked better than others; the gradient to add is of the loss's own size, so
+        # that neither hides the other's errors
+        s["logits"] = _normal(g, (T, E), dt, 1.5) + _normal(g, (1, E), dt, 0.5)
         s["experts"] = torch.topk(s["logits"].float(), k, dim=1).indices.to(torch.int32).contiguous()
         s["mask"] = torch.rand(T, generator=g, device="cuda") < 0.67 if c["masked"] else None
-        s["add"] = _normal(g, (T, E), dt, 0.5 / max(1, T)) if c["add"] else None
+        s["add"] = _normal(g, (T, E), dt, 1e-4 / max(1, T)) if c["add"] else None
         s["dloss"] = torch.rand((), generator=g, device="cuda") + 0.5
         s["coef"] = 0.01
     return s
