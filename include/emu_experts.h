@@ -17,6 +17,7 @@ extern "C" {
 /* Element types of the expert-layer entry points. */
 #define EMU_F32  0
 #define EMU_BF16 1
+#define EMU_I32  2   /* results of emu_i8_gemm alone */
 
 /* Added to the first argument (type or slices) of emu_grouped_split,
  * emu_grouped_split_rows, emu_grouped_prodsum and emu_grouped_prodsum_wgrad: the
@@ -173,6 +174,63 @@ emu_status emu_rows_combine_backward_full(int dtype, int64_t T, int64_t k, int64
                                           const void *Y, int64_t yrows, int64_t ldy, const int32_t *slots,
                                           const float *weights, void *dY, int64_t lddy, float *dweights, void *ws,
                                           size_t ws_bytes, emu_stream_t stream);
+
+/* Balance loss of a routing: with the n tokens t whose mask[t] is not 0 (mask: device
+ * uint8[T]; NULL: all), p_t the softmax of token t's logits over all experts, counts[e]
+ * their assignments to expert e (experts [T][k], as emu_route gives them), P_e the mean of p_te:
+ *   loss = coef E / (n k) sum_e counts[e] P_e, 0 for n = 0
+ * (device float; 1 x coef for a perfectly even routing).  counts: device int32[E + 1],
+ * the last entry is n.  NaN counts as a logit of minus infinity; a token whose
+ * logits all are has p = 0.  An entry of experts outside 0 .. E-1 is not counted.
+ * 1 <= k <= 32, k <= E <= 1024, T k < 2^31 - 65536.  Sums in FP32, in an order that depends
+ * on the sizes alone: same inputs, same bits.  ws: at least
+ * emu_route_balance_workspace_bytes, not shared by calls in flight at once.
+ * Flags: EMU_FLAG_NONFINITE (a counted token's logit is NaN or plus infinity),
+ * EMU_FLAG_INDEX. */
+size_t emu_route_balance_workspace_bytes(int64_t E);
+emu_status emu_route_balance(int dtype, int64_t T, int64_t E, int64_t k, const void *logits, int64_t ldl,
+                             const int32_t *experts, const uint8_t *mask, float coef, float *loss, int32_t *counts,
+                             void *ws, size_t ws_bytes, emu_stream_t stream);
+
+/* Its gradient, counts being constants:
+ *   dlogits[t, e] = add[t, e] + dloss / n p_te (f_e - sum_e' f_e' p_te'), f_e = coef E / (n k) counts[e],
+ * without the second term where mask[t] is 0.  counts: those of emu_route_balance for the same
+ * logits and mask.  dloss: device float, NULL for 1.  add: T x E of dtype (a gradient
+ * of the same logits; may be dlogits itself, then with the same pitch), or NULL for 0; it
+ * may not overlap dlogits otherwise.  One rounding to dtype; all of dlogits is written. */
+emu_status emu_route_balance_backward(int dtype, int64_t T, int64_t E, int64_t k, const void *logits, int64_t ldl,
+                                      const int32_t *counts, const uint8_t *mask, float coef, const float *dloss,
+                                      const void *add, int64_t lda, void *dlogits, int64_t lddl, emu_stream_t stream);
+
+/* Rows to 8-bit integers: scales[g, r] = max_k |X[g, r, k]| / 127 in FP32 and
+ * codes[g, r, k] = X / scale rounded to the nearest integer, ties to even, exactly, clamped to
+ * -127 .. 127 (which only subnormal scales need).  A row whose scale is 0 has zero codes; one with a NaN or
+ * infinity has zero codes and a NaN for its scale.  X: G matrices of rows x cols of dtype, row
+ * pitch ldx, stridex apart, any alignment; codes likewise int8; scales FP32 [G][rows].  Rows of the
+ * result may not overlap.  ws: for the flags (emu_split_workspace_bytes(32)), or NULL, which reports none.
+ * Flags: EMU_FLAG_NONFINITE. */
+emu_status emu_i8_quantize(int dtype, int64_t G, int64_t rows, int64_t cols, const void *X, int64_t ldx, int64_t stridex,
+                           int8_t *codes, int64_t ldq, int64_t strideq, float *scales, void *ws, size_t ws_bytes,
+                           emu_stream_t stream);
+
+/* Products in 8-bit integers with a scale for each token and each channel, dense or
+ * grouped by expert:
+ *   Y[r, n] = (sum_k X[src[r], k] W[g, n, k]) wscales[g, n] xscales[src[r]]
+ * for the rows r of group g (ends as above; NULL with G = 1: one matrix for all rows;
+ * src NULL: row r itself, xrows >= rows).  The sum is exact: codes are -128 .. 127 and
+ * K <= 131071.  It is rounded to FP32, multiplied by the channel's and then by the token's
+ * scale (NULL: 1) and rounded to ytype (EMU_F32, EMU_BF16); EMU_I32 gives the sums themselves and
+ * takes no scales.  X: xrows x K, W: G matrices N x K, stridew apart, int8 of any alignment,
+ * those whose base, row pitch and distance are multiples of 16 bytes are read as they stand, others
+ * of W may be copied first.  xscales [xrows], wscales [G][N] FP32.  Rows of no group, and rows whose src is
+ * outside 0 .. xrows-1, are zero.  aligned: whether W's base, pitch and distance are
+ * multiples of 16.  ws: at least emu_i8_gemm_workspace_bytes, 16-byte aligned, not shared by calls
+ * in flight at once.  Flags: EMU_FLAG_INDEX, EMU_FLAG_TIMEOUT. */
+size_t emu_i8_gemm_workspace_bytes(int64_t G, int64_t rows, int64_t N, int64_t K, int aligned);
+emu_status emu_i8_gemm(int64_t G, int64_t rows, int64_t N, int64_t K, const int8_t *X, int64_t xrows, int64_t ldx,
+                       const float *xscales, const int32_t *src, const int8_t *W, int64_t ldw, int64_t stridew,
+                       const float *wscales, const int32_t *ends, void *Y, int ytype, int64_t ldy, void *ws,
+                       size_t ws_bytes, emu_stream_t stream);
 
 #ifdef __cplusplus
 }

@@ -26,7 +26,7 @@ STATUS = {0: "ok", 1: "invalid argument", 2: "misaligned", 3: "workspace too sma
           5: "unsupported size"}
 FLAG_NONFINITE, FLAG_RANGE, FLAG_SLICE, FLAG_TIMEOUT, FLAG_INDEX = 0x1, 0x2, 0x4, 0x8, 0x10
 OP_N, OP_T = 0, 1
-F32, BF16 = 0, 1
+F32, BF16, I32 = 0, 1, 2
 KEEP_FLAGS = 0x100
 ZERO_LEVEL = -(2 ** 31)
 
@@ -86,6 +86,13 @@ _SIGS = {
     "emu_rows_combine_workspace_bytes": ("size", ["l"]),
     "emu_rows_combine_backward_full": ("i", ["i", "l", "l", "l", "p", "l", "p", "l", "l", "p", "p", "p", "l", "p", "p",
                                              "size", "p"]),
+    "emu_route_balance_workspace_bytes": ("size", ["l"]),
+    "emu_route_balance": ("i", ["i", "l", "l", "l", "p", "l", "p", "p", "f", "p", "p", "p", "size", "p"]),
+    "emu_route_balance_backward": ("i", ["i", "l", "l", "l", "p", "l", "p", "p", "f", "p", "p", "l", "p", "l", "p"]),
+    "emu_i8_quantize": ("i", ["i", "l", "l", "l", "p", "l", "l", "p", "l", "l", "p", "p", "size", "p"]),
+    "emu_i8_gemm_workspace_bytes": ("size", ["l", "l", "l", "l", "i"]),
+    "emu_i8_gemm": ("i", ["l", "l", "l", "l", "p", "l", "l", "p", "p", "p", "l", "l", "p", "p", "p", "i", "l", "p", "size",
+                          "p"]),
     "emu_read_flags": ("i", ["p", "p", "p"]),
     "emu_selftest_timeout": ("i", ["p", "size", "u32", "p"]),
     "emu_status_string": ("str", ["i"]),
@@ -177,6 +184,12 @@ emu_rows_combine = _mk("emu_rows_combine")
 emu_rows_combine_backward = _mk("emu_rows_combine_backward")
 emu_rows_combine_workspace_bytes = _mk("emu_rows_combine_workspace_bytes")
 emu_rows_combine_backward_full = _mk("emu_rows_combine_backward_full")
+emu_route_balance_workspace_bytes = _mk("emu_route_balance_workspace_bytes")
+emu_route_balance = _mk("emu_route_balance")
+emu_route_balance_backward = _mk("emu_route_balance_backward")
+emu_i8_quantize = _mk("emu_i8_quantize")
+emu_i8_gemm_workspace_bytes = _mk("emu_i8_gemm_workspace_bytes")
+emu_i8_gemm = _mk("emu_i8_gemm")
 emu_read_flags = _mk("emu_read_flags")
 emu_selftest_timeout = _mk("emu_selftest_timeout")
 emu_status_string = _mk("emu_status_string")
@@ -805,3 +818,155 @@ def rows_combine_backward(dO, Y, slots, weights=None, dY=None, stream=None):
     if r:
         _check(r, "emu_rows_combine_backward")
     return dY, dw
+
+
+Balance = collections.namedtuple("Balance", "loss counts tokens k")
+
+
+def _mask(mask, T, device, where):
+    """Address of a contiguous bool or uint8 tensor [T] (None: none)."""
+    if mask is None:
+        return None
+    if mask.shape != (T,) or mask.dtype not in (_torch().bool, _torch().uint8) or mask.device != device or \
+            not mask.is_contiguous():
+        _bad(where, f"a contiguous bool or uint8 tensor ({T},) on {device} is needed")
+    return mask.data_ptr()
+
+
+def route_balance(logits, experts, coef: float = 1.0, mask=None, ws=None, stream=None):
+    """emu_route_balance: the balance loss of a routing, coef E / (n k) sum_e
+    counts_e P_e over the n tokens with a mask (bool or uint8 [T]; None: all).
+    experts: route's, int32 [T, k].  Returns (Balance(loss, a float32 scalar on
+    the GPU, counts int32 [E], tokens int32 scalar, k), ws)."""
+    torch, where = _torch(), "route_balance"
+    dt, ldl, (T, E), dev = _dtype(logits, where), _pitch(logits, where), logits.shape, logits.device
+    if len(experts.shape) != 2 or experts.shape[0] != T:
+        _bad(where, f"experts have to be [{T}, k], got {tuple(experts.shape)}")
+    k = experts.shape[1]
+    pe, pm = _ints(experts, T * k, dev, "route_balance: experts"), _mask(mask, T, dev, "route_balance: mask")
+    if ws is None:
+        ws = _empty(_lib.emu_route_balance_workspace_bytes(E), torch.uint8, dev, stream)
+    loss, counts = _empty((), torch.float32, dev, stream), _empty(E + 1, torch.int32, dev, stream)
+    r = _lib.emu_route_balance(dt, T, E, k, logits.data_ptr(), ldl, pe, pm, coef, loss.data_ptr(), counts.data_ptr(),
+                               ws.data_ptr(), ws.numel(), _raw_stream(stream, dev))
+    if r:
+        _check(r, "emu_route_balance")
+    return Balance(loss, counts[:E], counts[E], k), ws
+
+
+def route_balance_backward(logits, balance, dloss=None, coef: float = 1.0, mask=None, add=None, dlogits=None,
+                           stream=None):
+    """emu_route_balance_backward: the logits' gradient of route_balance(logits,
+    .., coef, mask), which gave `balance`; dloss: float32 scalar on the GPU
+    (None: 1).  add: a gradient of the same logits (of route_backward, say) that
+    this one is added to, before the one rounding; dlogits may be the same tensor."""
+    where = "route_balance_backward"
+    dt, ldl, (T, E), dev = _dtype(logits, where), _pitch(logits, where), logits.shape, logits.device
+    counts = balance.counts
+    if counts.shape != (E,) or balance.tokens.data_ptr() != counts.data_ptr() + 4 * E:
+        _bad(where, "the result of route_balance for the same logits is needed")
+    if dlogits is None:
+        dlogits = _empty((T, E), logits.dtype, dev, stream)
+    elif dlogits.shape != logits.shape or dlogits.dtype is not logits.dtype:
+        _bad(where, "dlogits differ from logits")
+    pa, lda = None, 0
+    if add is not None:
+        if add.shape != logits.shape or add.dtype is not logits.dtype:
+            _bad(where, "add differs from logits")
+        pa, lda = add.data_ptr(), _pitch(add, "route_balance_backward: add", dev)
+    r = _lib.emu_route_balance_backward(dt, T, E, balance.k, logits.data_ptr(), ldl,
+                                        _ints(counts, E, dev, "route_balance_backward: counts"),
+                                        _mask(mask, T, dev, "route_balance_backward: mask"), coef,
+                                        _float_pairs(dloss, (), dev, "route_balance_backward: dloss"), pa, lda,
+                                        dlogits.data_ptr(), _pitch(dlogits, where, dev), _raw_stream(stream, dev))
+    if r:
+        _check(r, "emu_route_balance_backward")
+    return dlogits
+
+
+Int8 = collections.namedtuple("Int8", "codes scales")
+
+
+def _codes8(t, where, device=None):
+    """Row pitch of a CUDA tensor of codes."""
+    if t.dtype is not _torch().int8:
+        _bad(where, f"int8 codes are needed, got {t.dtype}")
+    return _pitch(t, where, device)
+
+
+def i8_quantize(X, codes=None, scales=None, ws=None, stream=None):
+    """emu_i8_quantize: rows of X (FP32 or BF16, [rows, cols] or [G, rows, cols]) as
+    8-bit codes with a scale for each row: its largest magnitude / 127, codes the
+    nearest integers of X / scale (ties to even).  Rows of a result made here start
+    on 16 bytes.  A row with a NaN or infinity gets a NaN scale; the call's flags are
+    in a given ws.  Returns Int8(codes, scales), an operand of i8_gemm: tokens with
+    a scale for each, weights [N, K] or [G, N, K] with one for each channel."""
+    torch, where = _torch(), "i8_quantize"
+    dt, ldx, dev, shape = _dtype(X, "i8_quantize: X"), _pitch(X, "i8_quantize: X"), X.device, X.shape
+    if len(shape) not in (2, 3):
+        _bad(where, f"X has to be [rows, cols] or [G, rows, cols], got {tuple(shape)}")
+    G, rows, cols = (1, *shape) if len(shape) == 2 else shape
+    if codes is None:
+        ld = (cols + 15) // 16 * 16 or 16
+        codes = _empty((*shape[:-1], ld), torch.int8, dev, stream)
+        if ld != cols:
+            codes = codes[..., :cols]
+        ldq, strideq = ld, rows * ld
+    else:
+        ldq, strideq = _codes8(codes, "i8_quantize: codes", dev), codes.stride(0) if len(shape) == 3 else 0
+        if codes.shape != shape:
+            _bad(where, "codes have another shape")
+    if scales is None:
+        scales = _empty(shape[:-1], torch.float32, dev, stream)
+    if G:
+        r = _lib.emu_i8_quantize(dt, G, rows, cols, X.data_ptr(), ldx, X.stride(0) if G > 1 else 0, codes.data_ptr(), ldq,
+                                 strideq, _float_pairs(scales, shape[:-1], dev, "i8_quantize: scales"),
+                                 ws.data_ptr() if ws is not None else None, ws.numel() if ws is not None else 0,
+                                 _raw_stream(stream, dev))
+        if r:
+            _check(r, "emu_i8_quantize")
+    return Int8(codes, scales)
+
+
+def i8_gemm(X, W, ends=None, src=None, Y=None, dtype=None, ws=None, stream=None):
+    """emu_i8_gemm: Y[r] = (codes of X[src[r]] times those of W_g), exactly, times the
+    channels' and the token's scale, for the rows r of group g (ends None: one
+    matrix W [N, K] for all rows, else [G, N, K]; src None: X[r]).  X and W:
+    pairs (int8 codes, FP32 scales) as i8_quantize makes them.  Y: BF16, FP32 or
+    int32 (dtype, or a given Y's; BF16 otherwise); int32 results are the sums
+    themselves, without scales.  ws: emu_i8_gemm_workspace_bytes bytes that a
+    caller may keep (one for all calls of a stream).  Returns (Y, ws)."""
+    torch, where = _torch(), "i8_gemm"
+    (x, xs), (w, wscales) = X, W
+    dev = x.device
+    ldx, ldw = _codes8(x, "i8_gemm: X"), _codes8(w, "i8_gemm: W", dev)
+    shape = w.shape
+    G = 1 if ends is None else ends.numel()
+    if len(x.shape) != 2 or len(shape) != (2 if ends is None else 3) or (ends is not None and shape[0] != G):
+        _bad(where, f"X {tuple(x.shape)}, weights {tuple(shape)} for {G} group(s)")
+    (xrows, K), N = x.shape, shape[-2]
+    if shape[-1] != K:
+        _bad(where, f"X has {K} columns, the weights {shape[-1]}")
+    rows = src.numel() if src is not None else xrows
+    if Y is None:
+        Y = _empty((rows, N), torch.bfloat16 if dtype is None else dtype, dev, stream)
+    elif Y.shape != (rows, N) or (dtype is not None and Y.dtype is not dtype):
+        _bad(where, "Y has another shape or type")
+    yt = I32 if Y.dtype is torch.int32 else _dtype(Y, "i8_gemm: Y")
+    if yt == I32:
+        load()
+        px = pw = None
+    else:
+        px = _float_pairs(xs, (xrows,), dev, "i8_gemm: scales of X")
+        pw = _float_pairs(wscales, shape[:-1], dev, "i8_gemm: scales of W")
+    pw8, stride = w.data_ptr(), w.stride(0) if G > 1 else 0
+    if ws is None:
+        ws = _empty(_lib.emu_i8_gemm_workspace_bytes(G, rows, N, K, int((pw8 | ldw | stride) % 16 == 0)), torch.uint8, dev,
+                    stream)
+    r = _lib.emu_i8_gemm(G, rows, N, K, x.data_ptr(), xrows, ldx, px,
+                         _ints(src, None, dev, "i8_gemm: src") if src is not None else None, pw8, ldw, stride, pw,
+                         _ints(ends, G, dev, "i8_gemm: ends") if ends is not None else None, Y.data_ptr(), yt,
+                         _pitch(Y, "i8_gemm: Y", dev), ws.data_ptr(), ws.numel(), _raw_stream(stream, dev))
+    if r:
+        _check(r, "emu_i8_gemm")
+    return Y, ws

@@ -61,4 +61,27 @@ cudaError_t launch_combine_backward(bool f32, int64_t T, int k, int64_t cols, co
                                     const float *weights, void *dY, int64_t lddy, float *dw, int32_t *owner,
                                     cudaStream_t st);       // owner: [yrows], or NULL: unnamed rows of dY are left
 
+// Balance loss of the routing (balance.cu).
+size_t balance_scratch_bytes(int64_t E);
+cudaError_t launch_balance(int64_t T, int64_t E, int k, const void *logits, bool f32, int64_t ldl, const int32_t *experts,
+                           const uint8_t *mask, float coef, float *loss, int32_t *counts, void *scratch, uint32_t *flags,
+                           cudaStream_t st);
+cudaError_t launch_balance_backward(int64_t T, int64_t E, int k, const void *logits, bool f32, int64_t ldl,
+                                    const int32_t *counts, const uint8_t *mask, float coef, const float *dloss,
+                                    const void *add, int64_t lda, void *dlogits, int64_t ldd, cudaStream_t st);
+
+// 8-bit integers (i8_*.cu): rows to codes, and products of codes.
+cudaError_t launch_i8_quantize(bool f32, int64_t G, int64_t rows, int64_t cols, const void *X, int64_t ldx, int64_t stridex,
+                               int8_t *q, int64_t ldq, int64_t strideq, float *scales, uint32_t *flags, cudaStream_t st);
+struct I8Product {
+    const int8_t *X, *W;
+    const float *xscales, *wscales;        // or NULL: 1
+    const int32_t *src, *ends;             // or NULL: row r is X's, one group
+    int64_t xrows, ldx, ldw, stridew, ldy;
+    void *Y;
+    int ytype, G, rows, N, K;
+    uint32_t *flags;
+};
+cudaError_t launch_i8_rows(const I8Product &p, cudaStream_t st);
+
 }  // namespace emu

@@ -2,6 +2,7 @@
 // argument checks, workspace layout and launch sequences.
 #include "grouped_common.cuh"
 #include "expert_launchers.cuh"
+#include "i8_common.cuh"
 
 using namespace emu;
 
@@ -107,6 +108,16 @@ emu_status check_combine_backward(int dtype, int64_t T, int64_t k, int64_t cols,
         return EMU_ERR_MISALIGNED;
     return EMU_OK;
 }
+
+emu_status check_balance(int dtype, int64_t T, int64_t E, int64_t k, const void *logits, int64_t ldl, const int32_t *counts)
+{
+    if (!known(dtype) || T < 0 || E < 1 || k < 1 || k > E || ldl < E || !counts) return EMU_ERR_INVALID_ARG;
+    if (E > kMaxGroups || k > 32 || T >= kMaxWalk / k) return EMU_ERR_UNSUPPORTED;
+    if (T > 0 && !logits) return EMU_ERR_INVALID_ARG;
+    return fits(logits, dtype) && fits(counts, EMU_F32) ? EMU_OK : EMU_ERR_MISALIGNED;
+}
+
+constexpr int64_t kMaxI8K = 131071;      // 128 * 128 * K stays below 2^31
 
 }  // namespace
 
@@ -417,6 +428,100 @@ emu_status emu_rows_combine_backward_full(int dtype, int64_t T, int64_t k, int64
                                                weights, dY, lddy, dweights,
                                                yrows > 0 && cols > 0 ? static_cast<int32_t *>(ws) : nullptr,
                                                reinterpret_cast<cudaStream_t>(stream)));
+}
+
+size_t emu_route_balance_workspace_bytes(int64_t E)
+{
+    return E < 1 ? 0 : kWsHeaderBytes + balance_scratch_bytes(E);
+}
+
+emu_status emu_route_balance(int dtype, int64_t T, int64_t E, int64_t k, const void *logits, int64_t ldl,
+                             const int32_t *experts, const uint8_t *mask, float coef, float *loss, int32_t *counts,
+                             void *ws, size_t ws_bytes, emu_stream_t stream)
+{
+    emu_status s = check_balance(dtype, T, E, k, logits, ldl, counts);
+    if (s != EMU_OK) return s;
+    if (!loss || (T > 0 && !experts)) return EMU_ERR_INVALID_ARG;
+    if (!fits(loss, EMU_F32) || !fits(experts, EMU_F32)) return EMU_ERR_MISALIGNED;
+    s = check_ws(ws, ws_bytes, emu_route_balance_workspace_bytes(E));
+    if (s != EMU_OK) return s;
+    return cuda_status(launch_balance(T, E, (int)k, logits, dtype == EMU_F32, ldl, experts, mask, coef, loss, counts,
+                                      static_cast<char *>(ws) + kWsHeaderBytes, &static_cast<WsHeader *>(ws)->flags,
+                                      reinterpret_cast<cudaStream_t>(stream)));
+}
+
+emu_status emu_route_balance_backward(int dtype, int64_t T, int64_t E, int64_t k, const void *logits, int64_t ldl,
+                                      const int32_t *counts, const uint8_t *mask, float coef, const float *dloss,
+                                      const void *add, int64_t lda, void *dlogits, int64_t lddl, emu_stream_t stream)
+{
+    const emu_status s = check_balance(dtype, T, E, k, logits, ldl, counts);
+    if (s != EMU_OK) return s;
+    if (lddl < E || (add && lda < E) || (add && add == dlogits && lda != lddl)) return EMU_ERR_INVALID_ARG;
+    if (T == 0) return EMU_OK;
+    if (!dlogits) return EMU_ERR_INVALID_ARG;
+    if (!fits(dlogits, dtype) || !fits(add, dtype) || !fits(dloss, EMU_F32)) return EMU_ERR_MISALIGNED;
+    return cuda_status(launch_balance_backward(T, E, (int)k, logits, dtype == EMU_F32, ldl, counts, mask, coef, dloss, add,
+                                               lda, dlogits, lddl, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+emu_status emu_i8_quantize(int dtype, int64_t G, int64_t rows, int64_t cols, const void *X, int64_t ldx, int64_t stridex,
+                           int8_t *codes, int64_t ldq, int64_t strideq, float *scales, void *ws, size_t ws_bytes,
+                           emu_stream_t stream)
+{
+    if (!known(dtype) || G < 1 || rows < 0 || cols < 0 || ldx < cols || ldq < cols ||
+        (G > 1 && (stridex < 0 || strideq < rows * ldq)))
+        return EMU_ERR_INVALID_ARG;
+    if (rows >= kMaxDim || cols >= kMaxWalk || G >= kMaxDim || (rows > 0 && G >= kMaxDim / rows)) return EMU_ERR_UNSUPPORTED;
+    if (G * rows > 0) {
+        if (!scales || (cols > 0 && (!X || !codes))) return EMU_ERR_INVALID_ARG;
+        if (!fits(X, dtype) || !fits(scales, EMU_F32)) return EMU_ERR_MISALIGNED;
+    }
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    if (ws) {
+        const emu_status s = check_ws(ws, ws_bytes, kWsHeaderBytes);
+        if (s != EMU_OK) return s;
+        if (clear_flags(ws, st) != cudaSuccess) return EMU_ERR_CUDA;
+    }
+    return cuda_status(launch_i8_quantize(dtype == EMU_F32, G, rows, cols, X, ldx, stridex, codes, ldq, strideq, scales,
+                                          ws ? &static_cast<WsHeader *>(ws)->flags : nullptr, st));
+}
+
+size_t emu_i8_gemm_workspace_bytes(int64_t G, int64_t rows, int64_t N, int64_t K, int aligned)
+{
+    (void)aligned;
+    return G < 1 || rows < 0 || N < 0 || K < 0 ? 0 : kWsHeaderBytes;
+}
+
+emu_status emu_i8_gemm(int64_t G, int64_t rows, int64_t N, int64_t K, const int8_t *X, int64_t xrows, int64_t ldx,
+                       const float *xscales, const int32_t *src, const int8_t *W, int64_t ldw, int64_t stridew,
+                       const float *wscales, const int32_t *ends, void *Y, int ytype, int64_t ldy, void *ws,
+                       size_t ws_bytes, emu_stream_t stream)
+{
+    if ((ytype != EMU_F32 && ytype != EMU_BF16 && ytype != EMU_I32) || xrows < 0 || ldx < K || ldw < K || ldy < N ||
+        (G > 1 && stridew < 0) || (!ends && G != 1) || (!src && xrows < rows) ||
+        (ytype == EMU_I32 && (xscales || wscales)))
+        return EMU_ERR_INVALID_ARG;
+    emu_status s = check_sizes(G, rows, N, K);
+    if (s != EMU_OK) return s;
+    if (K > kMaxI8K || xrows >= kMaxDim) return EMU_ERR_UNSUPPORTED;
+    const int esize = ytype == EMU_BF16 ? 2 : 4, etype = ytype == EMU_BF16 ? EMU_BF16 : EMU_F32;
+    if (rows > 0 && N > 0) {
+        if (!Y || (K > 0 && (!W || (xrows > 0 && !X)))) return EMU_ERR_INVALID_ARG;
+        if (!fits(Y, etype) || !fits(xscales, EMU_F32) || !fits(wscales, EMU_F32) || !fits(src, EMU_F32) || !fits(ends, EMU_F32))
+            return EMU_ERR_MISALIGNED;
+    }
+    s = check_ws(ws, ws_bytes, emu_i8_gemm_workspace_bytes(G, rows, N, K, aligned_codes(W, ldw, G > 1 ? stridew : 0)));
+    if (s != EMU_OK) return s;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    if (rows == 0 || N == 0 || K == 0) {
+        if (clear_flags(ws, st) != cudaSuccess) return EMU_ERR_CUDA;
+        return cuda_status(zero_rows(Y, rows, N, ldy, esize, st));
+    }
+    I8Product p = {};
+    p.X = X; p.W = W; p.xscales = xscales; p.wscales = wscales; p.src = src; p.ends = ends; p.xrows = xrows; p.ldx = ldx;
+    p.ldw = ldw; p.stridew = G > 1 ? stridew : 0; p.ldy = ldy; p.Y = Y; p.ytype = ytype; p.G = (int)G; p.rows = (int)rows;
+    p.N = (int)N; p.K = (int)K; p.flags = &static_cast<WsHeader *>(ws)->flags;
+    return cuda_status(launch_i8_rows(p, st));
 }
 
 }  // extern "C"
