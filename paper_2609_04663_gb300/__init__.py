@@ -961,8 +961,8 @@ def i8_gemm(X, W, ends=None, src=None, Y=None, dtype=None, ws=None, stream=None)
         pw = _float_pairs(wscales, shape[:-1], dev, "i8_gemm: scales of W")
     pw8, stride = w.data_ptr(), w.stride(0) if G > 1 else 0
     if ws is None:
-        ws = _empty(_lib.emu_i8_gemm_workspace_bytes(G, rows, N, K, int((pw8 | ldw | stride) % 16 == 0)), torch.uint8, dev,
-                    stream)
+        whole = (pw8 | ldw | stride) % 16 == 0 and (G <= 1 or stride >= N * ldw)
+        ws = _empty(_lib.emu_i8_gemm_workspace_bytes(G, rows, N, K, int(whole)), torch.uint8, dev, stream)
     r = _lib.emu_i8_gemm(G, rows, N, K, x.data_ptr(), xrows, ldx, px,
                          _ints(src, None, dev, "i8_gemm: src") if src is not None else None, pw8, ldw, stride, pw,
                          _ints(ends, G, dev, "i8_gemm: ends") if ends is not None else None, Y.data_ptr(), yt,

@@ -51,4 +51,10 @@ inline bool aligned_codes(const void *q, int64_t ld, int64_t stride)
     return ((reinterpret_cast<uintptr_t>(q) | (uintptr_t)ld | (uintptr_t)stride) & 15u) == 0;
 }
 
+// Whether the tensor memory accelerator can read weights as they stand.
+inline bool i8_tma_reads(const void *W, int64_t G, int64_t N, int64_t ldw, int64_t stridew)
+{
+    return G <= 1 ? aligned_codes(W, ldw, 0) : aligned_codes(W, ldw, stridew) && stridew >= N * ldw;
+}
+
 }  // namespace emu

@@ -157,6 +157,8 @@ cudaError_t by_alignment(const RowsArgs &a, cudaStream_t st)
 
 }  // namespace
 
+bool i8_few_rows(int64_t G, int64_t rows) { return rows <= (G > 1 ? 4 * G : 8); }
+
 cudaError_t launch_i8_rows(const I8Product &p, cudaStream_t st)
 {
     RowsArgs a = {};
