@@ -5,7 +5,8 @@
 //
 // A quotient's nearest integer comes from x times the reciprocal (off by less than
 // 2e-5), and where that lies within 1e-4 of the border between two integers, from the sign of
-// x - (n +- 1/2) s, which one fused multiply-add gives exactly.
+// x - (n +- 1/2) s, which one fused multiply-add gives exactly.  That is not rare: half of
+// a row's largest value is at 63.5, and of BF16 values every three-hundredth or so is that.
 //
 // A group of R threads (32, 128 or 512) has a row, four pieces of 16 bytes a thread in
 // registers: each element is read once while rows have up to 4 R pieces, longer rows are read
@@ -50,50 +51,95 @@ __device__ __forceinline__ uint4 load_values16(const char *row, int c, int cols)
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+// The values of a piece as pairs of FP32 numbers.
 template <bool F32>
-__device__ __forceinline__ void as_floats(uint4 v, float (&x)[F32 ? 4 : 8])
+__device__ __forceinline__ void as_pairs(uint4 v, uint64_t (&x)[F32 ? 2 : 4])
 {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    if constexpr (F32) {
+        x[0] = (uint64_t)w[1] << 32 | w[0];
+        x[1] = (uint64_t)w[3] << 32 | w[2];
+    } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if constexpr (F32) {
-            x[i] = __uint_as_float(w[i]);
-        } else {
-            x[2 * i] = __uint_as_float(w[i] << 16);
-            x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-        }
+        for (int i = 0; i < 4; ++i) x[i] = (uint64_t)(w[i] & 0xFFFF0000u) << 32 | (w[i] << 16);
     }
 }
 
-// Bits of the largest magnitude: magnitudes order like their bits, NaN above infinity.
+// Largest magnitudes: bits of one FP32 magnitude, or of two BF16 ones (halves).  Magnitudes
+// order like their bits, NaN above infinity.
 template <bool F32>
 __device__ __forceinline__ uint32_t largest(uint4 v, uint32_t top)
 {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        if constexpr (F32) {
-            top = max(top, w[i] & 0x7FFFFFFFu);
-        } else {
-            top = max(top, w[i] << 16 & 0x7FFFFFFFu);
-            top = max(top, w[i] & 0x7FFF0000u);
-        }
+        if constexpr (F32) top = max(top, w[i] & 0x7FFFFFFFu);
+        else asm("max.u16x2 %0, %1, %2;" : "=r"(top) : "r"(top), "r"(w[i] & 0x7FFF7FFFu));
     }
     return top;
 }
 
-// The nearest integer to x / s (ties to even), for s well inside the normal range.
-__device__ __noinline__ int nearest_exact(float x, float s, float inv)
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
 {
-    float n = rintf(x * inv);
-    const float up = fmaf(-(n + 0.5f), s, x), down = fmaf(-(n - 0.5f), s, x);     // signs are exact
-    const bool odd = ((int)n & 1) != 0;
-    if (up > 0.0f || (up == 0.0f && odd)) n += 1.0f;
-    else if (down < 0.0f || (down == 0.0f && odd)) n -= 1.0f;
-    return (int)fminf(fmaxf(n, -127.0f), 127.0f);
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
+{
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ uint64_t both(float x) { return (uint64_t)__float_as_uint(x) << 32 | __float_as_uint(x); }
+__device__ __forceinline__ float first_of(uint64_t x) { return __uint_as_float((uint32_t)x); }
+__device__ __forceinline__ float second_of(uint64_t x) { return __uint_as_float((uint32_t)(x >> 32)); }
+
+// Codes of a piece: the low bytes of m.
+template <bool F32>
+__device__ __forceinline__ uint2 pack(const uint32_t (&m)[F32 ? 4 : 8])
+{
+    uint2 o = make_uint2(0u, 0u);
+    o.x = __byte_perm(__byte_perm(m[0], m[1], 0x0040), __byte_perm(m[2], m[3], 0x0040), 0x5410);
+    if constexpr (!F32) o.y = __byte_perm(__byte_perm(m[4], m[5], 0x0040), __byte_perm(m[6], m[7], 0x0040), 0x5410);
+    return o;
 }
 
-template <bool F32, bool VEC, int R>
+// The nearest integers to x lift / s (ties to even), s well inside the normal range: the
+// signs of x - (n +- 1/2) s are exact.
+template <bool F32>
+__device__ __noinline__ uint2 codes_exact(uint4 v, float lift, float s, float inv)
+{
+    constexpr int N = F32 ? 4 : 8;
+    uint64_t x[N / 2];
+    as_pairs<F32>(v, x);
+    uint32_t m[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+        const float y = (e & 1 ? second_of(x[e / 2]) : first_of(x[e / 2])) * lift;
+        float n = rintf(y * inv);
+        const float up = fmaf(-(n + 0.5f), s, y), down = fmaf(-(n - 0.5f), s, y);
+        const bool odd = ((int)n & 1) != 0;
+        if (up > 0.0f || (up == 0.0f && odd)) n += 1.0f;
+        else if (down < 0.0f || (down == 0.0f && odd)) n -= 1.0f;
+        m[e] = (uint32_t)(int)fminf(fmaxf(n, -127.0f), 127.0f);
+    }
+    return pack<F32>(m);
+}
+
+// What n, an integer next to x / s and d to its one or other side of it, is off by: 1 or -1
+// where x / s lies past the border n +- 1/2, or on it and n (of whose bits m has the last) is odd.
+// The sign of x - (n +- 1/2) s is exact.
+__device__ __forceinline__ uint32_t beyond_border(float x, float s, float n, float d, uint32_t m)
+{
+    const float t = fmaf(-(n + copysignf(0.5f, d)), s, x);
+    const float past = d < 0.0f ? -t : t;
+    const bool off = past > 0.0f || (past == 0.0f && (m & 1u));
+    return off ? (d < 0.0f ? 0xFFFFFFFFu : 1u) : 0u;
+}
+
+// VEC: rows are read 16 bytes at a time; R threads a row; ONE: one matrix.
+template <bool F32, bool VEC, int R, bool ONE>
 __global__ void __launch_bounds__(R < 256 ? 256 : R) quantize_kernel(const QuantArgs a)
 {
     constexpr int N = F32 ? 4 : 8, NT = R < 256 ? 256 : R, ROWS = NT / R, W = R / 32;
@@ -101,7 +147,7 @@ __global__ void __launch_bounds__(R < 256 ? 256 : R) quantize_kernel(const Quant
     const int sub = (int)threadIdx.x / R, tid = (int)threadIdx.x % R;
     const int64_t r = (int64_t)blockIdx.x * ROWS + sub;
     const bool here = r < a.rows;
-    const int64_t g = here ? r / a.per : 0, i = here ? r - g * a.per : 0;
+    const int64_t g = ONE || !here ? 0 : r / a.per, i = here ? r - g * a.per : 0;
     const char *row = static_cast<const char *>(a.X) + (g * a.stridex + i * a.ldx) * (F32 ? 4 : 2);
     const int cols = here ? a.cols : 0;
     uint4 v[kPieces];
@@ -116,6 +162,7 @@ __global__ void __launch_bounds__(R < 256 ? 256 : R) quantize_kernel(const Quant
     for (int p = 0; p < kPieces; ++p) top = largest<F32>(v[p], top);
     for (int64_t c = (int64_t)(kPieces * R + tid) * N; c < cols; c += R * N)
         top = largest<F32>(load_values16<F32, VEC>(row, (int)c, cols), top);
+    if constexpr (!F32) top = max(top & 0xFFFFu, top >> 16) << 16;
     top = __reduce_max_sync(0xFFFFFFFFu, top);
     if constexpr (W > 1) {
         if (lane_id() == 0) part[threadIdx.x >> 5] = top;
@@ -131,41 +178,43 @@ __global__ void __launch_bounds__(R < 256 ? 256 : R) quantize_kernel(const Quant
         a.scales[r] = finite ? s : __uint_as_float(0x7FFFFFFFu);
         if (!finite && a.flags) atomicOr(a.flags, (uint32_t)EMU_FLAG_NONFINITE);
     }
-    // tiny rows: scaled up by a power of two, away from the subnormal range, where differences
-    // lose their sign (a scale that is itself rounded there can give codes above 127: nearest_exact clamps)
+    // tiny rows are lifted by a power of two, away from the subnormal range, where differences
+    // lose their sign (a scale that is itself rounded there can give codes above 127: codes_exact clamps)
     const bool tiny = amax < 0x1p-60f;
     const float lift = tiny ? 0x1p80f : 1.0f;
     s *= lift;
-    const bool some = finite && s > 0.0f;
-    const float inv = some ? __frcp_rn(s) : 0.0f;
+    const bool none = !finite || !(s > 0.0f);         // such rows have zero codes
+    const float inv = none ? 0.0f : __frcp_rn(s);
+    const uint64_t inv2 = both(inv);
     int8_t *q = a.q + g * a.strideq + i * a.ldq;
+    const bool words = ((reinterpret_cast<uintptr_t>(q)) & (N - 1u)) == 0;
     auto piece = [&](uint4 w, int c) {
-        float x[N];
-        as_floats<F32>(w, x);
+        uint64_t x[N / 2];
+        as_pairs<F32>(w, x);
         uint32_t m[N];
-        bool close = tiny;
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-            const float y = some ? x[e] * inv : 0.0f, b = y + 12582912.0f;     // 1.5 * 2^23: the low bits are the integer
-            m[e] = __float_as_uint(b);
-            close |= fabsf(y - (b - 12582912.0f)) > 0.4999f;
+        for (int e = 0; e < N / 2; ++e) {
+            // 1.5 * 2^23 has the units at its last bit: the low byte of the sum is the integer
+            const uint64_t b = fma2(x[e], inv2, both(12582912.0f));
+            const uint64_t n = add2(b, both(-12582912.0f)), d = fma2(x[e], inv2, n ^ 0x8000000080000000ull);
+            m[2 * e] = (uint32_t)b;
+            m[2 * e + 1] = (uint32_t)(b >> 32);
+            const float d0 = first_of(d), d1 = second_of(d);
+            if (fmaxf(fabsf(d0), fabsf(d1)) > 0.4999f) {
+                m[2 * e] += beyond_border(first_of(x[e]), s, first_of(n), d0, m[2 * e]);
+                m[2 * e + 1] += beyond_border(second_of(x[e]), s, second_of(n), d1, m[2 * e + 1]);
+            }
         }
-        if (close) {
-#pragma unroll
-            for (int e = 0; e < N; ++e) m[e] = some ? (uint32_t)nearest_exact(x[e] * lift, s, inv) : 0u;
-        }
-        uint32_t o[N / 4];
-#pragma unroll
-        for (int j = 0; j < N / 4; ++j)
-            o[j] = __byte_perm(__byte_perm(m[4 * j], m[4 * j + 1], 0x0040), __byte_perm(m[4 * j + 2], m[4 * j + 3], 0x0040), 0x5410);
+        uint2 o = tiny ? codes_exact<F32>(w, lift, s, inv) : pack<F32>(m);
+        if (none) o = make_uint2(0u, 0u);
         int8_t *to = q + c;
-        if (c + N <= cols && (reinterpret_cast<uintptr_t>(to) & (N - 1u)) == 0) {
-            if constexpr (F32) *reinterpret_cast<uint32_t *>(to) = o[0];
-            else *reinterpret_cast<uint2 *>(to) = make_uint2(o[0], o[1]);
+        if (words && c + N <= cols) {
+            if constexpr (F32) *reinterpret_cast<uint32_t *>(to) = o.x;
+            else *reinterpret_cast<uint2 *>(to) = o;
         } else {
 #pragma unroll
             for (int e = 0; e < N; ++e)
-                if (c + e < cols) to[e] = (int8_t)(m[e] & 0xFFu);
+                if (c + e < cols) to[e] = (int8_t)((e < 4 ? o.x : o.y) >> (8 * (e & 3)) & 0xFFu);
         }
     };
 #pragma unroll
@@ -180,7 +229,9 @@ template <bool F32, bool VEC, int R>
 cudaError_t run(const QuantArgs &a, cudaStream_t st)
 {
     constexpr int NT = R < 256 ? 256 : R, ROWS = NT / R;
-    quantize_kernel<F32, VEC, R><<<(unsigned)((a.rows + ROWS - 1) / ROWS), NT, 0, st>>>(a);
+    const unsigned grid = (unsigned)((a.rows + ROWS - 1) / ROWS);
+    if (a.per == a.rows) quantize_kernel<F32, VEC, R, true><<<grid, NT, 0, st>>>(a);
+    else quantize_kernel<F32, VEC, R, false><<<grid, NT, 0, st>>>(a);
     return cudaGetLastError();
 }
 
