@@ -179,8 +179,8 @@ emu_status emu_rows_combine_backward_full(int dtype, int64_t T, int64_t k, int64
  * uint8[T]; NULL: all), p_t the softmax of token t's logits over all experts, counts[e]
  * their assignments to expert e (experts [T][k], as emu_route gives them), P_e the mean of p_te:
  *   loss = coef E / (n k) sum_e counts[e] P_e, 0 for n = 0
- * (device float; 1 x coef for a perfectly even routing).  counts: device int32[E + 1],
- * the last entry is n.  NaN counts as a logit of minus infinity; a token whose
+ * (device float; 1 x coef for a perfectly even routing).  counts: device int32[E],
+ * tokens: device int32, n.  NaN counts as a logit of minus infinity; a token whose
  * logits all are has p = 0.  An entry of experts outside 0 .. E-1 is not counted.
  * 1 <= k <= 32, k <= E <= 1024, T k < 2^31 - 65536.  Sums in FP32, in an order that depends
  * on the sizes alone: same inputs, same bits.  ws: at least
@@ -190,17 +190,17 @@ emu_status emu_rows_combine_backward_full(int dtype, int64_t T, int64_t k, int64
 size_t emu_route_balance_workspace_bytes(int64_t E);
 emu_status emu_route_balance(int dtype, int64_t T, int64_t E, int64_t k, const void *logits, int64_t ldl,
                              const int32_t *experts, const uint8_t *mask, float coef, float *loss, int32_t *counts,
-                             void *ws, size_t ws_bytes, emu_stream_t stream);
+                             int32_t *tokens, void *ws, size_t ws_bytes, emu_stream_t stream);
 
 /* Its gradient, counts being constants:
  *   dlogits[t, e] = add[t, e] + dloss / n p_te (f_e - sum_e' f_e' p_te'), f_e = coef E / (n k) counts[e],
- * without the second term where mask[t] is 0.  counts: those of emu_route_balance for the same
+ * without the second term where mask[t] is 0.  counts, tokens: those of emu_route_balance for the same
  * logits and mask.  dloss: device float, NULL for 1.  add: T x E of dtype (a gradient
  * of the same logits; may be dlogits itself, then with the same pitch), or NULL for 0; it
  * may not overlap dlogits otherwise.  One rounding to dtype; all of dlogits is written. */
 emu_status emu_route_balance_backward(int dtype, int64_t T, int64_t E, int64_t k, const void *logits, int64_t ldl,
-                                      const int32_t *counts, const uint8_t *mask, float coef, const float *dloss,
-                                      const void *add, int64_t lda, void *dlogits, int64_t lddl, emu_stream_t stream);
+                                      const int32_t *counts, const int32_t *tokens, const uint8_t *mask, float coef,
+                                      const float *dloss, const void *add, int64_t lda, void *dlogits, int64_t lddl, emu_stream_t stream);
 
 /* Rows to 8-bit integers: scales[g, r] = max_k |X[g, r, k]| / 127 in FP32 and
  * codes[g, r, k] = X / scale rounded to the nearest integer, ties to even, exactly, clamped to

@@ -87,8 +87,8 @@ _SIGS = {
     "emu_rows_combine_backward_full": ("i", ["i", "l", "l", "l", "p", "l", "p", "l", "l", "p", "p", "p", "l", "p", "p",
                                              "size", "p"]),
     "emu_route_balance_workspace_bytes": ("size", ["l"]),
-    "emu_route_balance": ("i", ["i", "l", "l", "l", "p", "l", "p", "p", "f", "p", "p", "p", "size", "p"]),
-    "emu_route_balance_backward": ("i", ["i", "l", "l", "l", "p", "l", "p", "p", "f", "p", "p", "l", "p", "l", "p"]),
+    "emu_route_balance": ("i", ["i", "l", "l", "l", "p", "l", "p", "p", "f", "p", "p", "p", "p", "size", "p"]),
+    "emu_route_balance_backward": ("i", ["i", "l", "l", "l", "p", "l", "p", "p", "p", "f", "p", "p", "l", "p", "l", "p"]),
     "emu_i8_quantize": ("i", ["i", "l", "l", "l", "p", "l", "l", "p", "l", "l", "p", "p", "size", "p"]),
     "emu_i8_gemm_workspace_bytes": ("size", ["l", "l", "l", "l", "i"]),
     "emu_i8_gemm": ("i", ["l", "l", "l", "l", "p", "l", "l", "p", "p", "p", "l", "l", "p", "p", "p", "i", "l", "p", "size",
@@ -846,12 +846,13 @@ def route_balance(logits, experts, coef: float = 1.0, mask=None, ws=None, stream
     pe, pm = _ints(experts, T * k, dev, "route_balance: experts"), _mask(mask, T, dev, "route_balance: mask")
     if ws is None:
         ws = _empty(_lib.emu_route_balance_workspace_bytes(E), torch.uint8, dev, stream)
-    loss, counts = _empty((), torch.float32, dev, stream), _empty(E + 1, torch.int32, dev, stream)
-    r = _lib.emu_route_balance(dt, T, E, k, logits.data_ptr(), ldl, pe, pm, coef, loss.data_ptr(), counts.data_ptr(),
-                               ws.data_ptr(), ws.numel(), _raw_stream(stream, dev))
+    b = Balance(_empty((), torch.float32, dev, stream), _empty((E,), torch.int32, dev, stream),
+                _empty((), torch.int32, dev, stream), k)
+    r = _lib.emu_route_balance(dt, T, E, k, logits.data_ptr(), ldl, pe, pm, coef, b[0].data_ptr(), b[1].data_ptr(),
+                               b[2].data_ptr(), ws.data_ptr(), ws.numel(), _raw_stream(stream, dev))
     if r:
         _check(r, "emu_route_balance")
-    return Balance(loss, counts[:E], counts[E], k), ws
+    return b, ws
 
 
 def route_balance_backward(logits, balance, dloss=None, coef: float = 1.0, mask=None, add=None, dlogits=None,
@@ -862,9 +863,7 @@ def route_balance_backward(logits, balance, dloss=None, coef: float = 1.0, mask=
     this one is added to, before the one rounding; dlogits may be the same tensor."""
     where = "route_balance_backward"
     dt, ldl, (T, E), dev = _dtype(logits, where), _pitch(logits, where), logits.shape, logits.device
-    counts = balance.counts
-    if counts.shape != (E,) or balance.tokens.data_ptr() != counts.data_ptr() + 4 * E:
-        _bad(where, "the result of route_balance for the same logits is needed")
+    _, counts, tokens, k = balance
     if dlogits is None:
         dlogits = _empty((T, E), logits.dtype, dev, stream)
     elif dlogits.shape != logits.shape or dlogits.dtype is not logits.dtype:
@@ -874,8 +873,9 @@ def route_balance_backward(logits, balance, dloss=None, coef: float = 1.0, mask=
         if add.shape != logits.shape or add.dtype is not logits.dtype:
             _bad(where, "add differs from logits")
         pa, lda = add.data_ptr(), _pitch(add, "route_balance_backward: add", dev)
-    r = _lib.emu_route_balance_backward(dt, T, E, balance.k, logits.data_ptr(), ldl,
+    r = _lib.emu_route_balance_backward(dt, T, E, k, logits.data_ptr(), ldl,
                                         _ints(counts, E, dev, "route_balance_backward: counts"),
+                                        _ints(tokens, 1, dev, "route_balance_backward: tokens"),
                                         _mask(mask, T, dev, "route_balance_backward: mask"), coef,
                                         _float_pairs(dloss, (), dev, "route_balance_backward: dloss"), pa, lda,
                                         dlogits.data_ptr(), _pitch(dlogits, where, dev), _raw_stream(stream, dev))

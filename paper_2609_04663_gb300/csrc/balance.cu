@@ -11,6 +11,7 @@
 // time.  With few tokens the first launch is one block and does both.
 #include "grouped_common.cuh"
 #include "expert_launchers.cuh"
+#include "pair_common.cuh"
 #include "split_f32_pair.cuh"
 
 namespace emu {
@@ -27,7 +28,8 @@ struct BalanceArgs {
     const float *dloss;
     void *dlogits;
     float *loss;
-    int32_t *counts;              // [E + 1]: assignments of each expert, tokens that count
+    int32_t *counts;              // [E] assignments of each expert
+    int32_t *tokens;              // tokens that count
     float *sums;                  // [blocks][E] sums of p
     int32_t *parts;               // [blocks][E + 2]: counts, tokens, flags
     uint32_t *flags;
@@ -35,47 +37,46 @@ struct BalanceArgs {
     int T, E, k, blocks;
 };
 
-// V values of a row for one of L lanes: consecutive ones (VEC: rows start on whole
-// lanes, and E is a multiple of 4), or every L-th.  NaN and places past the end as minus
-// infinity.
-template <int V, int L, bool VEC>
-__device__ __forceinline__ int expert_of(int lane, int i) { return VEC ? lane * V + i : i * L + lane; }
+// The expert of value i of a lane, of L lanes with V values each: C neighbouring ones at a
+// time (one load: E and the row pitch are multiples of C then), the lanes side by side.
+template <int L, int C>
+__device__ __forceinline__ int expert_of(int lane, int i) { return i / C * (C * L) + lane * C + i % C; }
 
-template <int V, int L, bool F32, bool VEC, bool KEPT = true>     // KEPT: nothing writes there during the launch
+// A lane's values of a row, `none` past the last expert.  KEPT: nothing writes there during the launch.
+template <int V, int L, bool F32, int C, bool KEPT = true>
 __device__ __forceinline__ void load_values(const void *base, int64_t at, int lane, int E, float (&x)[V], float none)
 {
-    if constexpr (VEC) {
 #pragma unroll
-        for (int i = 0; i < V; i += 4) {
-            const int e = lane * V + i;
-            if (e < E) {
-                if constexpr (F32) {
-                    const float4 *p = reinterpret_cast<const float4 *>(static_cast<const float *>(base) + at + e);
-                    const float4 v = KEPT ? __ldg(p) : *p;
-                    x[i] = v.x; x[i + 1] = v.y; x[i + 2] = v.z; x[i + 3] = v.w;
-                } else {
-                    const uint2 *p = reinterpret_cast<const uint2 *>(static_cast<const uint16_t *>(base) + at + e);
-                    const uint2 v = KEPT ? __ldg(p) : *p;
-                    x[i] = __uint_as_float(v.x << 16); x[i + 1] = __uint_as_float(v.x & 0xFFFF0000u);
-                    x[i + 2] = __uint_as_float(v.y << 16); x[i + 3] = __uint_as_float(v.y & 0xFFFF0000u);
-                }
+    for (int i = 0; i < V; i += C) {
+        const int e = expert_of<L, C>(lane, i);
+#pragma unroll
+        for (int j = 0; j < C; ++j) x[i + j] = none;
+        if (e >= E) continue;
+        if constexpr (F32) {
+            const float *p = static_cast<const float *>(base) + at + e;
+            if constexpr (C == 4) {
+                const float4 *q = reinterpret_cast<const float4 *>(p);
+                const float4 v = KEPT ? __ldg(q) : *q;
+                x[i] = v.x; x[i + 1] = v.y; x[i + 2] = v.z; x[i + 3] = v.w;
             } else {
-                x[i] = x[i + 1] = x[i + 2] = x[i + 3] = none;
-            }
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const int e = i * L + lane;
-            x[i] = none;
-            if (e >= E) continue;
-            if constexpr (F32) {
-                const float *p = static_cast<const float *>(base) + at + e;
                 x[i] = KEPT ? __ldg(p) : *p;
-            } else {
-                const uint16_t *p = static_cast<const uint16_t *>(base) + at + e;
-                x[i] = __uint_as_float((uint32_t)(KEPT ? __ldg(p) : *p) << 16);
             }
+        } else {
+            const uint16_t *p = static_cast<const uint16_t *>(base) + at + e;
+            uint32_t w[4] = {};
+            if constexpr (C == 8) {
+                const uint4 *q = reinterpret_cast<const uint4 *>(p);
+                const uint4 v = KEPT ? __ldg(q) : *q;
+                w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+            } else if constexpr (C == 4) {
+                const uint2 *q = reinterpret_cast<const uint2 *>(p);
+                const uint2 v = KEPT ? __ldg(q) : *q;
+                w[0] = v.x; w[1] = v.y;
+            } else {
+                w[0] = KEPT ? __ldg(p) : *p;
+            }
+#pragma unroll
+            for (int j = 0; j < C; ++j) x[i + j] = __uint_as_float(j & 1 ? w[j / 2] & 0xFFFF0000u : w[j / 2] << 16);
         }
     }
 }
@@ -88,20 +89,42 @@ __device__ __forceinline__ float lanes_sum(float x)
     return x;
 }
 
-// x: logits -> exp(x - max); returns 1 / their sum, or 0 where all are minus infinity.
+// The larger one, NaN if one is.
+__device__ __forceinline__ float max_nan(float a, float b)
+{
+    float m;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(a), "f"(b));
+    return m;
+}
+
+// x: logits -> exp(x - max); returns 1 / their sum, or 0 where all are minus infinity.  NaN
+// counts as minus infinity.  odd: set where a lane's value is NaN or plus infinity.
+// As powers of two: x log2 e - c with one rounding, c = max log2 e rounded, the same for the
+// whole row, which the sum takes out again.  A power of two is off by 2^-22 at most.
 template <int V, int L>
-__device__ __forceinline__ float softmax_parts(float (&x)[V])
+__device__ __forceinline__ float softmax_parts(float (&x)[V], bool &odd)
 {
     float top = x[0];
 #pragma unroll
-    for (int i = 1; i < V; ++i) top = fmaxf(top, x[i]);
+    for (int i = 1; i < V; ++i) top = max_nan(top, x[i]);
+    odd = !(top < INFINITY);
+    if (odd) {
+        top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            x[i] = fmaxf(x[i], -INFINITY);
+            top = fmaxf(top, x[i]);
+        }
+    }
 #pragma unroll
     for (int d = L / 2; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
     const bool some = top > -INFINITY;
+    constexpr float log2e = 1.4426950408889634f;
+    const float c = some ? top * log2e : 0.0f;
     float total = 0.0f;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        x[i] = some ? expf(x[i] - top) : 0.0f;
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(x[i]) : "f"(fmaf(x[i], log2e, -c)));
         total += x[i];
     }
     total = lanes_sum<L>(total);
@@ -114,69 +137,60 @@ __device__ __forceinline__ float count_scale(const BalanceArgs &a, int n)
     return n > 0 ? a.coef * (float)a.E / ((float)n * (float)a.k) : 0.0f;
 }
 
-// One block: counts and the loss from the sums of `blocks` blocks.  sm: NT floats and
-// NT ints at least.
-template <int NT>
-__device__ void finish(const BalanceArgs &a, const float *sums, const int32_t *parts, int blocks, float *sm)
+// Adds `rows` rows of E sums, all threads of a block: W columns at a time with NT / W threads
+// a column, in an order that depends on the sizes alone.  at(row, e): a sum; done(e, sum): column e's, in
+// one thread.
+template <int NT, typename At, typename Done>
+__device__ __forceinline__ void add_columns(int rows, int E, float *red, At at, Done done)
 {
-    __shared__ float warp_part[NT / 32];
-    __shared__ int n_all, bits;
-    const int tid = threadIdx.x;
-    if (tid == 0) { n_all = 0; bits = 0; }
-    __syncthreads();
-    for (int b = tid; b < blocks; b += NT) {
-        const int32_t *p = parts + (int64_t)b * (a.E + 2) + a.E;
-        atomicAdd(&n_all, p[0]);
-        if (p[1]) atomicOr(&bits, p[1]);
-    }
-    __syncthreads();
-    const int n = n_all;
-    const float cs = count_scale(a, n), inv_n = n > 0 ? 1.0f / (float)n : 0.0f;
-    // W columns at a time, `split` threads a column, each every split-th block
     int W = 32;
-    while (W < a.E && W < NT) W *= 2;
-    const int split = NT / W, col = tid % W, part = tid / W;
-    int *si = reinterpret_cast<int *>(sm + NT);
-    float loss = 0.0f;
-    for (int e0 = 0; e0 < a.E; e0 += W) {
+    while (W < E && W < NT) W *= 2;
+    const int tid = (int)threadIdx.x, split = NT / W, col = tid % W, part = tid / W;
+    for (int e0 = 0; e0 < E; e0 += W) {
         const int e = e0 + col;
         float s = 0.0f;
-        int c = 0;
-        if (e < a.E) {
-#pragma unroll 4
-            for (int b = part; b < blocks; b += split) {
-                s += sums[(int64_t)b * a.E + e];
-                c += parts[(int64_t)b * (a.E + 2) + e];
-            }
+        if (e < E) {
+#pragma unroll 8
+            for (int r = part; r < rows; r += split) s += at(r, e);
         }
-        sm[tid] = s;
-        si[tid] = c;
-        __syncthreads();
-        if (part == 0 && e < a.E) {
-            for (int q = 1; q < split; ++q) { s += sm[q * W + col]; c += si[q * W + col]; }
-            a.counts[e] = c;
-            loss = fmaf((float)c * cs, s * inv_n, loss);
+        if (split > 1) {
+            red[tid] = s;
+            __syncthreads();
+            if (part == 0)
+                for (int q = 1; q < split; ++q) s += red[q * W + col];
         }
-        __syncthreads();
-    }
-    loss = lanes_sum<32>(loss);
-    if (lane_id() == 0) warp_part[tid >> 5] = loss;
-    __syncthreads();
-    if (tid == 0) {
-        for (int w = 1; w < NT / 32; ++w) loss += warp_part[w];
-        *a.loss = loss;
-        a.counts[a.E] = n;
-        if (a.flags) *a.flags = (uint32_t)bits;
+        if (part == 0 && e < E) done(e, s);
+        if (split > 1) __syncthreads();
     }
 }
 
-template <int V, int L, bool F32, bool VEC, int NT>
+// The loss from every thread's share of it, and what else there is to say; a whole block.
+template <int NT>
+__device__ __forceinline__ void publish(const BalanceArgs &a, float share, int n, uint32_t bits, float *red)
+{
+    share = lanes_sum<32>(share);
+    __syncthreads();
+    if (lane_id() == 0) red[threadIdx.x >> 5] = share;
+    __syncthreads();
+    if (threadIdx.x < 32) {
+        share = lanes_sum<32>(threadIdx.x < NT / 32 ? red[threadIdx.x] : 0.0f);
+        if (threadIdx.x == 0) {
+            *a.loss = share;
+            *a.tokens = n;
+            *a.flags = bits;
+        }
+    }
+}
+
+template <int V, int L, bool F32, int C, int NT>
 __global__ void __launch_bounds__(NT) balance_kernel(const BalanceArgs a)
 {
-    extern __shared__ float sm[];                 // [warps][E] sums, then [E] counts
+    extern __shared__ float sm[];                 // [warps][E] sums, [E] counts
     constexpr int WARPS = NT / 32, PER = 32 / L;
     int *hist = reinterpret_cast<int *>(sm + (size_t)WARPS * a.E);
+    __shared__ float red[NT];
     __shared__ int tokens, bits;
+    griddep_launch_dependents();
     const int warp = threadIdx.x >> 5, lane = (int)lane_id() % L, sub = (int)lane_id() / L;
     if (threadIdx.x == 0) { tokens = 0; bits = 0; }
     for (int e = threadIdx.x; e < a.E; e += NT) hist[e] = 0;
@@ -192,7 +206,7 @@ __global__ void __launch_bounds__(NT) balance_kernel(const BalanceArgs a)
         float x[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) x[i] = -INFINITY;
-        if (on) load_values<V, L, F32, VEC>(a.logits, t * a.ldl, lane, a.E, x, -INFINITY);
+        if (on) load_values<V, L, F32, C>(a.logits, t * a.ldl, lane, a.E, x, -INFINITY);
         if (on) {
             for (int j = lane; j < a.k; j += L) {
                 const int e = __ldg(a.experts + t * a.k + j);
@@ -201,12 +215,9 @@ __global__ void __launch_bounds__(NT) balance_kernel(const BalanceArgs a)
             }
             n += lane == 0;
         }
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            if (!(x[i] < INFINITY)) odd |= EMU_FLAG_NONFINITE;
-            x[i] = fmaxf(x[i], -INFINITY);                // NaN counts as minus infinity
-        }
-        const float inv = softmax_parts<V, L>(x);
+        bool bad;
+        const float inv = softmax_parts<V, L>(x, bad);
+        if (bad) odd |= EMU_FLAG_NONFINITE;
 #pragma unroll
         for (int i = 0; i < V; ++i) acc[i] = fmaf(x[i], inv, acc[i]);
     }
@@ -217,47 +228,118 @@ __global__ void __launch_bounds__(NT) balance_kernel(const BalanceArgs a)
     if (sub == 0) {
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const int e = expert_of<V, L, VEC>(lane, i);
+            const int e = expert_of<L, C>(lane, i);
             if (e < a.E) sm[(size_t)warp * a.E + e] = acc[i];
         }
     }
-    if (n) atomicAdd(&tokens, n);
-    if (odd) atomicOr(&bits, odd);
+    n = __reduce_add_sync(0xFFFFFFFFu, n);
+    odd = (int)__reduce_or_sync(0xFFFFFFFFu, (unsigned)odd);
+    if (lane_id() == 0) {
+        if (n) atomicAdd(&tokens, n);
+        if (odd) atomicOr(&bits, odd);
+    }
     __syncthreads();
-    float *sums = a.sums + (int64_t)blockIdx.x * a.E;
-    int32_t *parts = a.parts + (int64_t)blockIdx.x * (a.E + 2);
-    for (int e = threadIdx.x; e < a.E; e += NT) {
-        float s = sm[e];
-        for (int w = 1; w < WARPS; ++w) s += sm[(size_t)w * a.E + e];
-        sums[e] = s;
-        parts[e] = hist[e];
-    }
-    if (threadIdx.x == 0) { parts[a.E] = tokens; parts[a.E + 1] = bits; }
+    const int all = tokens;
+    auto at = [&](int w, int e) { return sm[(size_t)w * a.E + e]; };
     if (gridDim.x == 1) {
-        __syncthreads();                              // (global writes too: of this block alone)
-        finish<NT>(a, a.sums, a.parts, 1, sm);
+        const float cs = count_scale(a, all), inv_n = all > 0 ? 1.0f / (float)all : 0.0f;
+        float loss = 0.0f;
+        add_columns<NT>(WARPS, a.E, red, at, [&](int e, float s) {
+            const int c = hist[e];
+            a.counts[e] = c;
+            loss = fmaf((float)c * cs, s * inv_n, loss);
+        });
+        publish<NT>(a, loss, all, (uint32_t)bits, red);
+    } else {
+        float *sums = a.sums + (int64_t)blockIdx.x * a.E;
+        int32_t *parts = a.parts + (int64_t)blockIdx.x * (a.E + 2);
+        add_columns<NT>(WARPS, a.E, red, at, [&](int e, float s) {
+            sums[e] = s;
+            parts[e] = hist[e];
+        });
+        if (threadIdx.x == 0) { parts[a.E] = all; parts[a.E + 1] = bits; }
     }
 }
 
-__global__ void __launch_bounds__(1024) balance_finish_kernel(const BalanceArgs a)
+// The second launch: a cluster of 8 CTAs, each with an eighth of the experts; the first one adds
+// their shares of the loss, through shared memory, in order.
+constexpr int kFinishCtas = 8;
+__global__ void __cluster_dims__(kFinishCtas, 1, 1) __launch_bounds__(512) balance_finish_kernel(const BalanceArgs a)
 {
-    __shared__ float sm[2048];
+    constexpr int NT = 512;
+    __shared__ float red[NT], share;
+    __shared__ int redc[NT], tokens, bits;
+    const int tid = (int)threadIdx.x, rank = (int)cluster_rank();
+    if (tid == 0) { tokens = 0; bits = 0; }
+    __syncthreads();
     griddep_wait();
-    finish<1024>(a, a.sums, a.parts, a.blocks, sm);
+    if (tid < a.blocks) {
+        const int32_t *p = a.parts + (int64_t)tid * (a.E + 2) + a.E;
+        if (p[0]) atomicAdd(&tokens, p[0]);
+        if (p[1]) atomicOr(&bits, p[1]);
+    }
+    static_assert(kBalanceBlocks <= NT, "a thread a block");
+    const int each = (a.E + kFinishCtas - 1) / kFinishCtas, e0 = rank * each;      // at most 128
+    int W = 16;
+    while (W < each) W *= 2;
+    const int split = NT / W, col = tid % W, part = tid / W, e = e0 + col;
+    const bool mine = col < each && e < a.E;
+    float s = 0.0f;
+    int c = 0;
+    if (mine) {
+#pragma unroll 8
+        for (int b = part; b < a.blocks; b += split) {
+            s += a.sums[(int64_t)b * a.E + e];
+            c += a.parts[(int64_t)b * (a.E + 2) + e];
+        }
+    }
+    red[tid] = s;
+    redc[tid] = c;
+    __syncthreads();
+    const int n = tokens;
+    const float cs = count_scale(a, n), inv_n = n > 0 ? 1.0f / (float)n : 0.0f;
+    float loss = 0.0f;
+    if (part == 0 && mine) {
+        for (int q = 1; q < split; ++q) { s += red[q * W + col]; c += redc[q * W + col]; }
+        a.counts[e] = c;
+        loss = (float)c * cs * (s * inv_n);
+    }
+    loss = lanes_sum<32>(loss);
+    __syncthreads();
+    if (lane_id() == 0) red[tid >> 5] = loss;
+    __syncthreads();
+    if (tid == 0) {
+        for (int w = 1; w < NT / 32; ++w) loss += red[w];
+        share = loss;
+    }
+    cluster_sync();
+    if (rank == 0 && tid == 0) {
+        float v[kFinishCtas];
+#pragma unroll
+        for (int r = 0; r < kFinishCtas; ++r)
+            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[r]) : "r"(peer_addr(smem_u32(&share), (uint32_t)r)) : "memory");
+        loss = v[0];
+#pragma unroll
+        for (int r = 1; r < kFinishCtas; ++r) loss += v[r];
+        *a.loss = loss;
+        *a.tokens = n;
+        *a.flags = (uint32_t)bits;
+    }
+    cluster_sync();                                   // shared memory stays until it has been read
 }
 
-template <int V, int L, bool F32, bool VEC>
+template <int V, int L, bool F32, int C>
 __global__ void __launch_bounds__(256) balance_backward_kernel(const BalanceArgs a)
 {
     constexpr int PER = 32 / L;
     const int lane = (int)lane_id() % L, sub = (int)lane_id() / L;
-    const int n = __ldg(a.counts + a.E);
+    const int n = __ldg(a.tokens);
     const float cs = count_scale(a, n);
     const float scale = n > 0 ? (a.dloss ? __ldg(a.dloss) : 1.0f) / (float)n : 0.0f;
     float f[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        const int e = expert_of<V, L, VEC>(lane, i);
+        const int e = expert_of<L, C>(lane, i);
         f[i] = e < a.E ? (float)__ldg(a.counts + e) * cs : 0.0f;
     }
     for (int64_t t0 = ((int64_t)blockIdx.x * 8 + (threadIdx.x >> 5)) * PER; t0 < a.T; t0 += (int64_t)gridDim.x * 8 * PER) {
@@ -266,12 +348,11 @@ __global__ void __launch_bounds__(256) balance_backward_kernel(const BalanceArgs
         float x[V], d[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) { x[i] = -INFINITY; d[i] = 0.0f; }
-        if (on) load_values<V, L, F32, VEC>(a.logits, t * a.ldl, lane, a.E, x, -INFINITY);
+        if (on) load_values<V, L, F32, C>(a.logits, t * a.ldl, lane, a.E, x, -INFINITY);
         // (dlogits may be `add`: each entry is read before the same lane writes it)
-        if (here && a.add) load_values<V, L, F32, VEC, false>(a.add, t * a.lda, lane, a.E, d, 0.0f);
-#pragma unroll
-        for (int i = 0; i < V; ++i) x[i] = fmaxf(x[i], -INFINITY);
-        const float inv = softmax_parts<V, L>(x);
+        if (here && a.add) load_values<V, L, F32, C, false>(a.add, t * a.lda, lane, a.E, d, 0.0f);
+        bool bad;
+        const float inv = softmax_parts<V, L>(x, bad);
         float inner = 0.0f;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
@@ -284,79 +365,90 @@ __global__ void __launch_bounds__(256) balance_backward_kernel(const BalanceArgs
 #pragma unroll
             for (int i = 0; i < V; ++i) d[i] = fmaf(scale * x[i], f[i] - inner, d[i]);
         }
-        if constexpr (VEC) {
 #pragma unroll
-            for (int i = 0; i < V; i += 4) {
-                const int e = lane * V + i;
-                if (e >= a.E) continue;
-                if constexpr (F32)
-                    *reinterpret_cast<float4 *>(static_cast<float *>(a.dlogits) + t * a.ldd + e) = make_float4(d[i], d[i + 1], d[i + 2], d[i + 3]);
+        for (int i = 0; i < V; i += C) {
+            const int e = expert_of<L, C>(lane, i);
+            if (e >= a.E) continue;
+            if constexpr (F32) {
+                float *o = static_cast<float *>(a.dlogits) + t * a.ldd + e;
+                if constexpr (C == 4) *reinterpret_cast<float4 *>(o) = make_float4(d[i], d[i + 1], d[i + 2], d[i + 3]);
+                else *o = d[i];
+            } else {
+                uint16_t *o = static_cast<uint16_t *>(a.dlogits) + t * a.ldd + e;
+                if constexpr (C == 8)
+                    *reinterpret_cast<uint4 *>(o) = make_uint4(bf16x2_rn(d[i], d[i + 1]), bf16x2_rn(d[i + 2], d[i + 3]),
+                                                               bf16x2_rn(d[i + 4], d[i + 5]), bf16x2_rn(d[i + 6], d[i + 7]));
+                else if constexpr (C == 4)
+                    *reinterpret_cast<uint2 *>(o) = make_uint2(bf16x2_rn(d[i], d[i + 1]), bf16x2_rn(d[i + 2], d[i + 3]));
                 else
-                    *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.dlogits) + t * a.ldd + e) =
-                        make_uint2(bf16x2_rn(d[i], d[i + 1]), bf16x2_rn(d[i + 2], d[i + 3]));
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const int e = i * L + lane;
-                if (e >= a.E) continue;
-                if constexpr (F32) static_cast<float *>(a.dlogits)[t * a.ldd + e] = d[i];
-                else static_cast<uint16_t *>(a.dlogits)[t * a.ldd + e] = (uint16_t)bf16x2_rn(d[i], 0.0f);
+                    *o = (uint16_t)bf16x2_rn(d[i], 0.0f);
             }
         }
     }
 }
 
-// Rows that lanes can read 4 values at a time.
-bool whole_lanes(const void *p, int64_t ld, bool f32)
+// Whether rows can be read C values at a time.
+bool whole_lanes(const void *p, int64_t ld, int bytes, int C)
 {
-    return !p || ((reinterpret_cast<uintptr_t>(p) & (f32 ? 15u : 7u)) == 0 && ld % 4 == 0);
+    return !p || ((reinterpret_cast<uintptr_t>(p) & (unsigned)(bytes * C - 1)) == 0 && ld % C == 0);
 }
 
-template <int V, int L, bool F32, bool VEC>
+template <int V, int L, bool F32, int C>
 cudaError_t run_balance(BalanceArgs a, bool backward, cudaStream_t st)
 {
     if (backward) {
         const int64_t blocks = ((int64_t)a.T + 8 * (32 / L) - 1) / (8 * (32 / L));
-        balance_backward_kernel<V, L, F32, VEC><<<(unsigned)(blocks > 152 * 8 ? 152 * 8 : blocks), 256, 0, st>>>(a);
+        balance_backward_kernel<V, L, F32, C><<<(unsigned)(blocks > 152 * 8 ? 152 * 8 : blocks), 256, 0, st>>>(a);
         return cudaGetLastError();
     }
-    constexpr int NT = V >= 16 ? 512 : 1024, PASS = NT / L;
-    const size_t need = ((size_t)(NT / 32) * a.E + a.E) * 4, least = (size_t)NT * 8;
-    const size_t sm = need > least ? need : least;
-    auto kern = balance_kernel<V, L, F32, VEC, NT>;
-    if (sm > 48 * 1024) {
+    constexpr int NT = V >= 32 ? 512 : 1024, PASS = NT / L;
+    const size_t sm = ((size_t)(NT / 32) * a.E + a.E) * 4;
+    auto kern = balance_kernel<V, L, F32, C, NT>;
+    if (sm > 44 * 1024) {
         const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sm);
         if (e != cudaSuccess) return e;
     }
     int64_t blocks = ((int64_t)a.T + PASS - 1) / PASS;
-    if (blocks <= 4) blocks = 1;
+    if (blocks < 1) blocks = 1;
     if (blocks > kBalanceBlocks) blocks = kBalanceBlocks;
     a.blocks = (int)blocks;
     kern<<<(unsigned)blocks, NT, sm, st>>>(a);
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess || blocks == 1) return e;
-    balance_finish_kernel<<<1, 1024, 0, st>>>(a);
-    return cudaGetLastError();
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(kFinishCtas);
+    cfg.blockDim = dim3(512);
+    cfg.stream = st;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    e = cudaLaunchKernelEx(&cfg, balance_finish_kernel, a);
+    return e != cudaSuccess ? e : cudaGetLastError();
 }
 
-template <bool F32, bool VEC>
+// Rows read in pieces of 16 bytes (8 for the fewest experts in BF16), or value by value.
+template <int V, int L, bool F32>
+cudaError_t by_pieces(const BalanceArgs &a, bool backward, cudaStream_t st)
+{
+    constexpr int C = F32 || V < 8 ? 4 : 8, bytes = F32 ? 4 : 2;
+    const bool whole = a.E % C == 0 && whole_lanes(a.logits, a.ldl, bytes, C) &&
+                       (!backward || (whole_lanes(a.add, a.lda, bytes, C) && whole_lanes(a.dlogits, a.ldd, bytes, C)));
+    return whole ? run_balance<V, L, F32, C>(a, backward, st) : run_balance<V, L, F32, 1>(a, backward, st);
+}
+
+template <bool F32>
 cudaError_t by_experts(const BalanceArgs &a, bool backward, cudaStream_t st)
 {
-    if (a.E <= 32) return run_balance<4, 8, F32, VEC>(a, backward, st);
-    if (a.E <= 64) return run_balance<4, 16, F32, VEC>(a, backward, st);
-    if (a.E <= 128) return run_balance<4, 32, F32, VEC>(a, backward, st);
-    if (a.E <= 256) return run_balance<8, 32, F32, VEC>(a, backward, st);
-    if (a.E <= 512) return run_balance<16, 32, F32, VEC>(a, backward, st);
-    return run_balance<32, 32, F32, VEC>(a, backward, st);
+    return a.E <= 32 ? by_pieces<4, 8, F32>(a, backward, st) : a.E <= 64 ? by_pieces<8, 8, F32>(a, backward, st)
+           : a.E <= 128 ? by_pieces<16, 8, F32>(a, backward, st) : a.E <= 256 ? by_pieces<16, 16, F32>(a, backward, st)
+           : a.E <= 512 ? by_pieces<16, 32, F32>(a, backward, st) : by_pieces<32, 32, F32>(a, backward, st);
 }
 
 cudaError_t by_type(const BalanceArgs &a, bool f32, bool backward, cudaStream_t st)
 {
-    const bool vec = a.E % 4 == 0 && whole_lanes(a.logits, a.ldl, f32) &&
-                     (!backward || (whole_lanes(a.add, a.lda, f32) && whole_lanes(a.dlogits, a.ldd, f32)));
-    return f32 ? (vec ? by_experts<true, true>(a, backward, st) : by_experts<true, false>(a, backward, st))
-               : (vec ? by_experts<false, true>(a, backward, st) : by_experts<false, false>(a, backward, st));
+    return f32 ? by_experts<true>(a, backward, st) : by_experts<false>(a, backward, st);
 }
 
 }  // namespace
@@ -364,11 +456,11 @@ cudaError_t by_type(const BalanceArgs &a, bool f32, bool backward, cudaStream_t 
 size_t balance_scratch_bytes(int64_t E) { return (size_t)kBalanceBlocks * (size_t)(2 * E + 2) * 4; }
 
 cudaError_t launch_balance(int64_t T, int64_t E, int k, const void *logits, bool f32, int64_t ldl, const int32_t *experts,
-                           const uint8_t *mask, float coef, float *loss, int32_t *counts, void *scratch, uint32_t *flags,
+                           const uint8_t *mask, float coef, float *loss, int32_t *counts, int32_t *tokens, void *scratch, uint32_t *flags,
                            cudaStream_t st)
 {
     BalanceArgs a = {};
-    a.logits = logits; a.ldl = ldl; a.experts = experts; a.mask = mask; a.coef = coef; a.loss = loss; a.counts = counts;
+    a.logits = logits; a.ldl = ldl; a.experts = experts; a.mask = mask; a.coef = coef; a.loss = loss; a.counts = counts; a.tokens = tokens;
     a.T = (int)T; a.E = (int)E; a.k = k; a.flags = flags;
     a.sums = static_cast<float *>(scratch);
     a.parts = reinterpret_cast<int32_t *>(a.sums + (size_t)kBalanceBlocks * E);
@@ -377,11 +469,12 @@ cudaError_t launch_balance(int64_t T, int64_t E, int k, const void *logits, bool
 }
 
 cudaError_t launch_balance_backward(int64_t T, int64_t E, int k, const void *logits, bool f32, int64_t ldl,
-                                    const int32_t *counts, const uint8_t *mask, float coef, const float *dloss,
+                                    const int32_t *counts, const int32_t *tokens, const uint8_t *mask, float coef, const float *dloss,
                                     const void *add, int64_t lda, void *dlogits, int64_t ldd, cudaStream_t st)
 {
     BalanceArgs a = {};
-    a.logits = logits; a.ldl = ldl; a.counts = const_cast<int32_t *>(counts); a.mask = mask; a.coef = coef;
+    a.logits = logits; a.ldl = ldl; a.counts = const_cast<int32_t *>(counts);
+    a.tokens = const_cast<int32_t *>(tokens); a.mask = mask; a.coef = coef;
     a.dloss = dloss; a.add = add; a.lda = lda; a.dlogits = dlogits; a.ldd = ldd; a.T = (int)T; a.E = (int)E; a.k = k;
     return by_type(a, f32, true, st);
 }

@@ -64,10 +64,10 @@ cudaError_t launch_combine_backward(bool f32, int64_t T, int k, int64_t cols, co
 // Balance loss of the routing (balance.cu).
 size_t balance_scratch_bytes(int64_t E);
 cudaError_t launch_balance(int64_t T, int64_t E, int k, const void *logits, bool f32, int64_t ldl, const int32_t *experts,
-                           const uint8_t *mask, float coef, float *loss, int32_t *counts, void *scratch, uint32_t *flags,
-                           cudaStream_t st);
+                           const uint8_t *mask, float coef, float *loss, int32_t *counts, int32_t *tokens, void *scratch,
+                           uint32_t *flags, cudaStream_t st);
 cudaError_t launch_balance_backward(int64_t T, int64_t E, int k, const void *logits, bool f32, int64_t ldl,
-                                    const int32_t *counts, const uint8_t *mask, float coef, const float *dloss,
+                                    const int32_t *counts, const int32_t *tokens, const uint8_t *mask, float coef, const float *dloss,
                                     const void *add, int64_t lda, void *dlogits, int64_t ldd, cudaStream_t st);
 
 // 8-bit integers (i8_*.cu): rows to codes, and products of codes.

@@ -109,12 +109,13 @@ emu_status check_combine_backward(int dtype, int64_t T, int64_t k, int64_t cols,
     return EMU_OK;
 }
 
-emu_status check_balance(int dtype, int64_t T, int64_t E, int64_t k, const void *logits, int64_t ldl, const int32_t *counts)
+emu_status check_balance(int dtype, int64_t T, int64_t E, int64_t k, const void *logits, int64_t ldl, const int32_t *counts,
+                         const int32_t *tokens)
 {
-    if (!known(dtype) || T < 0 || E < 1 || k < 1 || k > E || ldl < E || !counts) return EMU_ERR_INVALID_ARG;
+    if (!known(dtype) || T < 0 || E < 1 || k < 1 || k > E || ldl < E || !counts || !tokens) return EMU_ERR_INVALID_ARG;
     if (E > kMaxGroups || k > 32 || T >= kMaxWalk / k) return EMU_ERR_UNSUPPORTED;
     if (T > 0 && !logits) return EMU_ERR_INVALID_ARG;
-    return fits(logits, dtype) && fits(counts, EMU_F32) ? EMU_OK : EMU_ERR_MISALIGNED;
+    return fits(logits, dtype) && fits(counts, EMU_F32) && fits(tokens, EMU_F32) ? EMU_OK : EMU_ERR_MISALIGNED;
 }
 
 constexpr int64_t kMaxI8K = 131071;      // 128 * 128 * K stays below 2^31
@@ -437,30 +438,30 @@ size_t emu_route_balance_workspace_bytes(int64_t E)
 
 emu_status emu_route_balance(int dtype, int64_t T, int64_t E, int64_t k, const void *logits, int64_t ldl,
                              const int32_t *experts, const uint8_t *mask, float coef, float *loss, int32_t *counts,
-                             void *ws, size_t ws_bytes, emu_stream_t stream)
+                             int32_t *tokens, void *ws, size_t ws_bytes, emu_stream_t stream)
 {
-    emu_status s = check_balance(dtype, T, E, k, logits, ldl, counts);
+    emu_status s = check_balance(dtype, T, E, k, logits, ldl, counts, tokens);
     if (s != EMU_OK) return s;
     if (!loss || (T > 0 && !experts)) return EMU_ERR_INVALID_ARG;
     if (!fits(loss, EMU_F32) || !fits(experts, EMU_F32)) return EMU_ERR_MISALIGNED;
     s = check_ws(ws, ws_bytes, emu_route_balance_workspace_bytes(E));
     if (s != EMU_OK) return s;
-    return cuda_status(launch_balance(T, E, (int)k, logits, dtype == EMU_F32, ldl, experts, mask, coef, loss, counts,
+    return cuda_status(launch_balance(T, E, (int)k, logits, dtype == EMU_F32, ldl, experts, mask, coef, loss, counts, tokens,
                                       static_cast<char *>(ws) + kWsHeaderBytes, &static_cast<WsHeader *>(ws)->flags,
                                       reinterpret_cast<cudaStream_t>(stream)));
 }
 
 emu_status emu_route_balance_backward(int dtype, int64_t T, int64_t E, int64_t k, const void *logits, int64_t ldl,
-                                      const int32_t *counts, const uint8_t *mask, float coef, const float *dloss,
-                                      const void *add, int64_t lda, void *dlogits, int64_t lddl, emu_stream_t stream)
+                                      const int32_t *counts, const int32_t *tokens, const uint8_t *mask, float coef,
+                                      const float *dloss, const void *add, int64_t lda, void *dlogits, int64_t lddl, emu_stream_t stream)
 {
-    const emu_status s = check_balance(dtype, T, E, k, logits, ldl, counts);
+    const emu_status s = check_balance(dtype, T, E, k, logits, ldl, counts, tokens);
     if (s != EMU_OK) return s;
     if (lddl < E || (add && lda < E) || (add && add == dlogits && lda != lddl)) return EMU_ERR_INVALID_ARG;
     if (T == 0) return EMU_OK;
     if (!dlogits) return EMU_ERR_INVALID_ARG;
     if (!fits(dlogits, dtype) || !fits(add, dtype) || !fits(dloss, EMU_F32)) return EMU_ERR_MISALIGNED;
-    return cuda_status(launch_balance_backward(T, E, (int)k, logits, dtype == EMU_F32, ldl, counts, mask, coef, dloss, add,
+    return cuda_status(launch_balance_backward(T, E, (int)k, logits, dtype == EMU_F32, ldl, counts, tokens, mask, coef, dloss, add,
                                                lda, dlogits, lddl, reinterpret_cast<cudaStream_t>(stream)));
 }
 

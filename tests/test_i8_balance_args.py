@@ -65,28 +65,29 @@ def test_balance_checks(lib):
     b, d = emu.emu_route_balance, emu.emu_route_balance_backward
     need = emu.emu_route_balance_workspace_bytes(8)
     assert emu.emu_route_balance_workspace_bytes(0) == 0
-    #        dt T  E  k  z  ldl ex mask coef loss counts ws bytes stream
-    assert b(2, 4, 8, 2, P, 8, P, None, 1.0, P, P, P, need, None) == 1
-    assert b(0, 4, 8, 9, P, 8, P, None, 1.0, P, P, P, need, None) == 1        # k > E
-    assert b(0, 4, 8, 0, P, 8, P, None, 1.0, P, P, P, need, None) == 1
-    assert b(0, 4, 8, 2, P, 7, P, None, 1.0, P, P, P, need, None) == 1        # ldl < E
-    assert b(0, 4, 8, 2, P, 8, None, None, 1.0, P, P, P, need, None) == 1     # no experts
-    assert b(0, 4, 8, 2, P, 8, P, None, 1.0, None, P, P, need, None) == 1
-    assert b(0, 4, 8, 2, P, 8, P, None, 1.0, P, None, P, need, None) == 1
-    assert b(0, 4, 8, 2, P + 2, 8, P, None, 1.0, P, P, P, need, None) == 2
-    assert b(0, 4, 8, 2, P, 8, P, None, 1.0, P, P + 2, P, need, None) == 2
-    assert b(0, 4, 8, 2, P, 8, P, None, 1.0, P, P, P, need - 1, None) == 3
-    assert b(0, 4, 2000, 2, P, 2000, P, None, 1.0, P, P, P, BIG, None) == 5
-    assert b(0, 4, 64, 33, P, 64, P, None, 1.0, P, P, P, BIG, None) == 5
-    assert b(0, 1 << 30, 8, 2, P, 8, P, None, 1.0, P, P, P, need, None) == 5
-    #        dt T  E  k  z  ldl counts mask coef dloss add lda d ldd stream
-    assert d(0, 4, 8, 2, P, 8, P, None, 1.0, None, None, 0, P, 7, None) == 1
-    assert d(0, 4, 8, 2, P, 8, P, None, 1.0, None, P + 64, 7, P, 8, None) == 1
-    assert d(0, 4, 8, 2, P, 8, P, None, 1.0, None, P, 9, P, 8, None) == 1     # in place with another pitch
-    assert d(0, 4, 8, 2, P, 8, None, None, 1.0, None, None, 0, P, 8, None) == 1
-    assert d(0, 4, 8, 2, P, 8, P, None, 1.0, None, None, 0, None, 8, None) == 1
-    assert d(0, 4, 8, 2, P, 8, P, None, 1.0, P + 1, None, 0, P, 8, None) == 2
-    assert d(0, 0, 8, 2, None, 8, P, None, 1.0, None, None, 0, None, 8, None) == 0
+    #        dt T  E  k  z  ldl ex mask coef loss counts tokens ws bytes stream
+    assert b(2, 4, 8, 2, P, 8, P, None, 1.0, P, P, P, P, need, None) == 1
+    assert b(0, 4, 8, 9, P, 8, P, None, 1.0, P, P, P, P, need, None) == 1        # k > E
+    assert b(0, 4, 8, 0, P, 8, P, None, 1.0, P, P, P, P, need, None) == 1
+    assert b(0, 4, 8, 2, P, 7, P, None, 1.0, P, P, P, P, need, None) == 1        # ldl < E
+    assert b(0, 4, 8, 2, P, 8, None, None, 1.0, P, P, P, P, need, None) == 1     # no experts
+    assert b(0, 4, 8, 2, P, 8, P, None, 1.0, None, P, P, P, need, None) == 1
+    assert b(0, 4, 8, 2, P, 8, P, None, 1.0, P, None, P, P, need, None) == 1
+    assert b(0, 4, 8, 2, P, 8, P, None, 1.0, P, P, None, P, need, None) == 1
+    assert b(0, 4, 8, 2, P + 2, 8, P, None, 1.0, P, P, P, P, need, None) == 2
+    assert b(0, 4, 8, 2, P, 8, P, None, 1.0, P, P + 2, P, P, need, None) == 2
+    assert b(0, 4, 8, 2, P, 8, P, None, 1.0, P, P, P, P, need - 1, None) == 3
+    assert b(0, 4, 2000, 2, P, 2000, P, None, 1.0, P, P, P, P, BIG, None) == 5
+    assert b(0, 4, 64, 33, P, 64, P, None, 1.0, P, P, P, P, BIG, None) == 5
+    assert b(0, 1 << 30, 8, 2, P, 8, P, None, 1.0, P, P, P, P, need, None) == 5
+    #        dt T  E  k  z  ldl counts tokens mask coef dloss add lda d ldd stream
+    assert d(0, 4, 8, 2, P, 8, P, P, None, 1.0, None, None, 0, P, 7, None) == 1
+    assert d(0, 4, 8, 2, P, 8, P, P, None, 1.0, None, P + 64, 7, P, 8, None) == 1
+    assert d(0, 4, 8, 2, P, 8, P, P, None, 1.0, None, P, 9, P, 8, None) == 1     # in place with another pitch
+    assert d(0, 4, 8, 2, P, 8, None, P, None, 1.0, None, None, 0, P, 8, None) == 1
+    assert d(0, 4, 8, 2, P, 8, P, P, None, 1.0, None, None, 0, None, 8, None) == 1
+    assert d(0, 4, 8, 2, P, 8, P, P, None, 1.0, P + 1, None, 0, P, 8, None) == 2
+    assert d(0, 0, 8, 2, None, 8, P, P, None, 1.0, None, None, 0, None, 8, None) == 0
 
 
 def test_tensor_checks_need_no_gpu(lib):
