@@ -321,46 +321,68 @@ i8_tile_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ 
         const int quarter = warp & 3, mine = (warp - Cfg::CONV) >> 2, row = quarter * 32 + lane;
         const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)Cfg::A0;
         const uint32_t from = base + Cfg::W_OFF + (uint32_t)row * kWK;
-        uint32_t s = 0, ph = 0, blocks = 0;           // blocks: K-blocks of the tiles before
+        // one K-block ahead: the next one's bytes are on their way into registers while this one's
+        // FP16 numbers are on theirs to tensor memory
+        struct Place {
+            int t, nkb, kb;                           // tile, its K-blocks, the K-block
+            uint32_t s, ph, i;                        // stage of the bytes; K-blocks before
+        };
+        auto open = [&](Place &p) {                   // the first K-block of tile p.t or of a later one
+            p.nkb = p.t < total ? (uniform(tile(p.t).nk) + kKB - 1) / kKB : 0;
+            p.kb = Cfg::GROUPS == 2 ? mine : 0;
+        };
+        auto stage_done = [&](Place &p) {
+            __syncwarp();
+            if (lane == 0) mbar_arrive(wempty0 + 8u * p.s);
+            if (++p.s == Cfg::NW) { p.s = 0; p.ph ^= 1u; }
+        };
         bool ok = true;
-        for (int t = first; t < total && ok; t += step) {
-            const int nkb = (uniform(tile(t).nk) + kKB - 1) / kKB;
-            for (int kb = 0; kb < nkb && ok; kb += 2) {
-                if (!(ok = warp_wait(wfull0 + 8u * s, ph, flags))) break;
+        // reads the K-block at p into w, false at the end; leaves p behind it
+        auto fetch = [&](Place &p, uint4 (&w)[4], uint32_t &i) {
+            while (p.t < total) {
+                if (p.kb < p.nkb) {
+                    if ((Cfg::GROUPS == 2 || (p.kb & 1) == 0) && !(ok = warp_wait(wfull0 + 8u * p.s, p.ph, flags))) return false;
 #pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    if (Cfg::GROUPS == 2 && b != mine) continue;
-                    const bool there = kb + b < nkb;
-                    uint4 w[4];
-                    if (there) {
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            w[j] = lds_u4(from + s * (uint32_t)Cfg::W_STAGE + (uint32_t)(((b * 4 + j) ^ (row & 7)) << 4));
-                    }
-                    if (b == 1 || Cfg::GROUPS == 2) {
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(wempty0 + 8u * s);
-                    }
-                    if (!there) continue;
-                    const uint32_t i = blocks + (uint32_t)(kb + b), q = i % Cfg::NA;
-                    uint32_t f[16];
-                    half_block(w[0], w[1], f);
-                    if (!(ok = warp_wait(aempty0 + 8u * q, ((i / Cfg::NA) & 1u) ^ 1u, flags))) break;
-                    tc_fence_after();
-                    tmem_store16(lanes + q * 32u, f);
-                    half_block(w[2], w[3], f);
-                    tmem_store16(lanes + q * 32u + 16u, f);
-                    tmem_st_wait();
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) {
-                        if constexpr (PAIR) mbar_arrive_peer(peer_addr(afull0 + 8u * q, 0));
-                        else mbar_arrive(afull0 + 8u * q);
-                    }
+                    for (int j = 0; j < 4; ++j)
+                        w[j] = lds_u4(from + p.s * (uint32_t)Cfg::W_STAGE + (uint32_t)((((p.kb & 1) * 4 + j) ^ (row & 7)) << 4));
+                    i = p.i + (uint32_t)p.kb;
+                    if (Cfg::GROUPS == 2 || (p.kb & 1) || p.kb + 1 == p.nkb) stage_done(p);
+                    p.kb += Cfg::GROUPS;
+                    return true;
                 }
-                if (++s == Cfg::NW) { s = 0; ph ^= 1u; }
+                // (two groups, an odd number of K-blocks: the second group has no part in the last stage)
+                if (Cfg::GROUPS == 2 && mine == 1 && (p.nkb & 1)) {
+                    if (!(ok = warp_wait(wfull0 + 8u * p.s, p.ph, flags))) return false;
+                    stage_done(p);
+                }
+                p.i += (uint32_t)p.nkb;
+                p.t += step;
+                open(p);
             }
-            blocks += (uint32_t)nkb;
+            return false;
+        };
+        Place p = {first, 0, 0, 0, 0, 0};
+        open(p);
+        uint4 w[4];
+        uint32_t i = 0;
+        bool more = fetch(p, w, i);
+        while (more) {
+            const uint32_t q = i % Cfg::NA, par = ((i / Cfg::NA) & 1u) ^ 1u;
+            uint32_t f[16], g[16];
+            half_block(w[0], w[1], f);
+            half_block(w[2], w[3], g);
+            more = fetch(p, w, i);
+            if (!ok || !(ok = warp_wait(aempty0 + 8u * q, par, flags))) break;
+            tc_fence_after();
+            tmem_store16(lanes + q * 32u, f);
+            tmem_store16(lanes + q * 32u + 16u, g);
+            tmem_st_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                if constexpr (PAIR) mbar_arrive_peer(peer_addr(afull0 + 8u * q, 0));
+                else mbar_arrive(afull0 + 8u * q);
+            }
         }
     } else {
         registers_issue<PAIR>();
@@ -499,10 +521,11 @@ struct ExpandArgs {
     float *xs;                        // [rows]
     uint4 *clear;                     // sums and tickets
     int64_t clear_n;
+    int per, chunks;                  // codes of a row that a warp takes at once (512 or 2048), such parts of a row
     int own_flags;                    // block 0 looks at all rows and sets the flag word
 };
 
-// One warp a row, 16 codes a lane.  Bound by HBM and L2: one byte read and two written an element.
+// 16 codes a lane.  Bound by HBM and L2: one byte read and two written an element.
 template <bool WIDE>
 __global__ void __launch_bounds__(256) i8_expand_kernel(const ExpandArgs a)
 {
@@ -525,36 +548,37 @@ __global__ void __launch_bounds__(256) i8_expand_kernel(const ExpandArgs a)
         }
     }
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < a.clear_n; i += (int64_t)gridDim.x * 256) a.clear[i] = make_uint4(0u, 0u, 0u, 0u);
-    for (int64_t r = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); r < p.rows; r += (int64_t)gridDim.x * 8) {
+    const int64_t units = (int64_t)p.rows * a.chunks;
+    for (int64_t i = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); i < units; i += (int64_t)gridDim.x * 8) {
+        const int64_t r = i / a.chunks;
+        const int first = (int)(i - r * a.chunks) * a.per;
         const int64_t t = p.src ? __ldg(p.src + r) : r;
         const bool there = t >= 0 && t < p.xrows;
-        if (lane == 0) {
+        if (lane == 0 && first == 0) {
             a.xs[r] = !there ? 0.0f : p.xscales ? __ldg(p.xscales + t) : 1.0f;
             if (!there && !a.own_flags) atomicOr(p.flags, (uint32_t)EMU_FLAG_INDEX);
         }
         const int8_t *x = p.X + (there ? t : 0) * p.ldx;
         uint16_t *out = a.plane + r * a.ld;
         constexpr int B = 4;                          // pieces loaded before the first is stored
-        for (int64_t k0 = lane * 16; k0 < p.K; k0 += 512 * B) {
-            uint4 v[B];
+        uint4 v[B];
 #pragma unroll
-            for (int b = 0; b < B; ++b) {
-                const int64_t k = k0 + 512 * b;
-                v[b] = make_uint4(0u, 0u, 0u, 0u);
-                if (there && k < p.K) v[b] = load_codes<WIDE>(x + k, (int)(p.K - k));
-            }
+        for (int b = 0; b < B; ++b) {
+            const int k = first + lane * 16 + 512 * b;
+            v[b] = make_uint4(0u, 0u, 0u, 0u);
+            if (there && 512 * b < a.per && k < p.K) v[b] = load_codes<WIDE>(x + k, p.K - k);
+        }
 #pragma unroll
-            for (int b = 0; b < B; ++b) {
-                const int64_t k = k0 + 512 * b;
-                if (k >= p.K) break;
-                uint4 f[2];
-                codes_f16(v[b].x, f[0].x, f[0].y);
-                codes_f16(v[b].y, f[0].z, f[0].w);
-                codes_f16(v[b].z, f[1].x, f[1].y);
-                codes_f16(v[b].w, f[1].z, f[1].w);
-                *reinterpret_cast<uint4 *>(out + k) = f[0];
-                if (k + 8 < a.ld) *reinterpret_cast<uint4 *>(out + k + 8) = f[1];
-            }
+        for (int b = 0; b < B; ++b) {
+            const int k = first + lane * 16 + 512 * b;
+            if (512 * b >= a.per || k >= p.K) break;
+            uint4 f[2];
+            codes_f16(v[b].x, f[0].x, f[0].y);
+            codes_f16(v[b].y, f[0].z, f[0].w);
+            codes_f16(v[b].z, f[1].x, f[1].y);
+            codes_f16(v[b].w, f[1].z, f[1].w);
+            *reinterpret_cast<uint4 *>(out + k) = f[0];
+            if (k + 8 < a.ld) *reinterpret_cast<uint4 *>(out + k + 8) = f[1];
         }
     }
 }
@@ -691,7 +715,11 @@ cudaError_t launch_i8_tile(I8Product p, void *scratch, cudaStream_t st)
         const cudaError_t c = cudaMemsetAsync(p.flags, 0, sizeof(uint32_t), st);
         if (c != cudaSuccess) return c;
     }
-    const int64_t blocks = (p.rows + 7) / 8;
+    // short pieces while there are not warps enough
+    e.per = (int64_t)p.rows * ((p.K + 2047) / 2048) < 152 * 32 ? 512 : 2048;
+    e.chunks = (p.K + e.per - 1) / e.per;
+    int64_t blocks = ((int64_t)p.rows * e.chunks + 7) / 8;
+    if (blocks < e.clear_n / 512) blocks = e.clear_n / 512;
     const unsigned grid = (unsigned)(blocks > 152 * 8 ? 152 * 8 : blocks);
     if (aligned_codes(p.X, p.xrows > 1 ? p.ldx : 0, 0)) i8_expand_kernel<true><<<grid, 256, 0, st>>>(e);
     else i8_expand_kernel<false><<<grid, 256, 0, st>>>(e);
