@@ -31,18 +31,18 @@ struct I8Cfg {
     static constexpr int HALVES = BC > 128 ? 2 : 1, HC = BC / HALVES;     // halves of a tile's columns
     static constexpr int STEP = PAIR ? 32 : 16;
     static constexpr int SLOTS = HALVES == 2 ? 3 : 4;                     // accumulators of HC columns
-    static constexpr int A0 = SLOTS * HC, NA = (512 - A0) / 32;           // A stages: 32 TMEM columns of 64 codes
+    static constexpr int A0 = SLOTS * HC, NA = (512 - A0) / 64;           // A stages: 64 TMEM columns of 128 codes
     static constexpr int C_HALF = HC / CTAS * kKB * 2, C_BLOCK = HALVES * C_HALF;     // rows of one K-block
     static constexpr int C_STAGE = 2 * C_BLOCK, NC = 4;
     static constexpr int W_STAGE = kLRows * kWK, NW = HALVES == 2 ? 4 : 8;
-    static constexpr int GROUPS = HALVES == 2 ? 1 : 2;                    // groups of four converting warps
+    static constexpr int GROUPS = 2;                                      // groups of four converting warps
     static constexpr int CONV = kDrainWarps, TMAW = CONV + 4 * GROUPS, MMA = TMAW + 1, TMAC = TMAW + 2;
     static constexpr int THREADS = 32 * (TMAW + 4);
     static constexpr int WC = HC / 2;                                     // columns of a half that a draining warp reads
     static constexpr int W_OFF = NC * C_STAGE, BAR_OFF = W_OFF + NW * W_STAGE, TAB_OFF = BAR_OFF + 512;
     static constexpr int SMEM = TAB_OFF + 2 * (kMaxGroups + 1) * 4 + 1024;
     static_assert(SMEM <= kSmemMax, "shared memory per CTA");
-    static_assert(NA >= 4 && C_HALF == 8192, "stages");
+    static_assert(NA >= 2 && NC % NA == 0 && C_HALF == 8192, "stages");
 };
 
 struct I8TileArgs {
@@ -154,12 +154,12 @@ __device__ __forceinline__ void half_block(const uint4 &u, const uint4 &v, uint3
 }
 
 template <bool PAIR>
-__device__ __forceinline__ void registers_drain() { if constexpr (PAIR) asm volatile("setmaxnreg.inc.sync.aligned.u32 192;"); }
+__device__ __forceinline__ void registers_drain() { if constexpr (PAIR) asm volatile("setmaxnreg.inc.sync.aligned.u32 168;"); }
 template <bool PAIR>
-__device__ __forceinline__ void registers_convert() { if constexpr (PAIR) asm volatile("setmaxnreg.dec.sync.aligned.u32 80;"); }
+__device__ __forceinline__ void registers_convert() { if constexpr (PAIR) asm volatile("setmaxnreg.dec.sync.aligned.u32 48;"); }
 template <bool PAIR>
 __device__ __forceinline__ void registers_issue() { if constexpr (PAIR) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;"); }
-constexpr int kSplitRegisters = 128 * (192 + 192 + 80 + 40);     // of the 512 threads of a pair's CTA
+constexpr int kSplitRegisters = 128 * (2 * 168 + 2 * 48 + 40);     // of the 640 threads of a pair's CTA
 
 template <int BC, bool PAIR>
 __global__ void __launch_bounds__(I8Cfg<BC, PAIR>::THREADS, 1)
@@ -171,11 +171,10 @@ i8_tile_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ 
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t base = (raw + 1023u) & ~1023u;
     uint8_t *base_ptr = smem_raw + (base - raw);
-    const uint32_t cfull0 = base + Cfg::BAR_OFF, cempty0 = cfull0 + 8u * Cfg::NC;
-    const uint32_t wfull0 = cempty0 + 8u * Cfg::NC, wempty0 = wfull0 + 8u * Cfg::NW;
-    const uint32_t afull0 = wempty0 + 8u * Cfg::NW, aempty0 = afull0 + 8u * Cfg::NA;
-    const uint32_t tfull0 = aempty0 + 8u * Cfg::NA, tempty0 = tfull0 + 8u * Cfg::SLOTS, done_bar = tempty0 + 8u * Cfg::SLOTS;
-    static_assert(8 * (2 * (Cfg::NC + Cfg::NW + Cfg::NA + Cfg::SLOTS) + 1) <= 496, "barriers");
+    const uint32_t cfull0 = base + Cfg::BAR_OFF, used0 = cfull0 + 8u * Cfg::NC;
+    const uint32_t wfull0 = used0 + 8u * Cfg::NC, wempty0 = wfull0 + 8u * Cfg::NW;
+    const uint32_t afull0 = wempty0 + 8u * Cfg::NW, tfull0 = afull0 + 8u * Cfg::NA, tempty0 = tfull0 + 8u * Cfg::SLOTS, done_bar = tempty0 + 8u * Cfg::SLOTS;
+    static_assert(8 * (2 * (Cfg::NC + Cfg::NW + Cfg::SLOTS) + Cfg::NA + 1) <= 496, "barriers");
     volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(base_ptr + Cfg::BAR_OFF + 496);
     int *starts = reinterpret_cast<int *>(base_ptr + Cfg::TAB_OFF), *tpre = starts + a.p.G + 1;
     const int warp = uniform((int)threadIdx.x >> 5), lane = (int)lane_id();
@@ -183,9 +182,9 @@ i8_tile_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ 
     uint32_t *flags = a.p.flags;
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < Cfg::NC; ++s) { mbar_init(cfull0 + 8u * s, 1); mbar_init(cempty0 + 8u * s, 1); }
+        for (int s = 0; s < Cfg::NC; ++s) { mbar_init(cfull0 + 8u * s, 1); mbar_init(used0 + 8u * s, 1); }
         for (int s = 0; s < Cfg::NW; ++s) { mbar_init(wfull0 + 8u * s, 1); mbar_init(wempty0 + 8u * s, 4 * Cfg::GROUPS); }
-        for (int s = 0; s < Cfg::NA; ++s) { mbar_init(afull0 + 8u * s, 4 * Cfg::CTAS); mbar_init(aempty0 + 8u * s, 1); }
+        for (int s = 0; s < Cfg::NA; ++s) mbar_init(afull0 + 8u * s, 4 * Cfg::GROUPS * Cfg::CTAS);
         for (int s = 0; s < Cfg::SLOTS; ++s) { mbar_init(tfull0 + 8u * s, 1); mbar_init(tempty0 + 8u * s, kDrainWarps * Cfg::CTAS); }
         mbar_init(done_bar, 1);
         fence_mbar_init();
@@ -316,72 +315,43 @@ i8_tile_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ 
         }
     } else if (warp < Cfg::TMAW) {
         // ---------------- weights: bytes of shared memory -> FP16 in tensor memory.  Lane: one
-        // feature; group b of four warps (or the one group) takes K-block b of a stage
+        // feature; group b of four warps takes K-block b of a stage
         registers_convert<PAIR>();
         const int quarter = warp & 3, mine = (warp - Cfg::CONV) >> 2, row = quarter * 32 + lane;
         const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)Cfg::A0;
         const uint32_t from = base + Cfg::W_OFF + (uint32_t)row * kWK;
-        // one K-block ahead: the next one's bytes are on their way into registers while this one's
-        // FP16 numbers are on theirs to tensor memory
-        struct Place {
-            int t, nkb, kb;                           // tile, its K-blocks, the K-block
-            uint32_t s, ph, i;                        // stage of the bytes; K-blocks before
-        };
-        auto open = [&](Place &p) {                   // the first K-block of tile p.t or of a later one
-            p.nkb = p.t < total ? (uniform(tile(p.t).nk) + kKB - 1) / kKB : 0;
-            p.kb = Cfg::GROUPS == 2 ? mine : 0;
-        };
-        auto stage_done = [&](Place &p) {
-            __syncwarp();
-            if (lane == 0) mbar_arrive(wempty0 + 8u * p.s);
-            if (++p.s == Cfg::NW) { p.s = 0; p.ph ^= 1u; }
-        };
+        // i: stages before (of 128 codes; the MMAs tell by used0 which of them they are done with)
+        uint32_t s = 0, ph = 0, i = 0;
         bool ok = true;
-        // reads the K-block at p into w, false at the end; leaves p behind it
-        auto fetch = [&](Place &p, uint4 (&w)[4], uint32_t &i) {
-            while (p.t < total) {
-                if (p.kb < p.nkb) {
-                    if ((Cfg::GROUPS == 2 || (p.kb & 1) == 0) && !(ok = warp_wait(wfull0 + 8u * p.s, p.ph, flags))) return false;
+        for (int t = first; t < total && ok; t += step) {
+            const int nk = uniform(tile(t).nk);
+            for (int k = 0; k < nk; k += kWK, ++i) {
+                if (!(ok = warp_wait(wfull0 + 8u * s, ph, flags))) break;
+                const bool there = k + mine * kKB < nk;
+                uint4 w[4];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        w[j] = lds_u4(from + p.s * (uint32_t)Cfg::W_STAGE + (uint32_t)((((p.kb & 1) * 4 + j) ^ (row & 7)) << 4));
-                    i = p.i + (uint32_t)p.kb;
-                    if (Cfg::GROUPS == 2 || (p.kb & 1) || p.kb + 1 == p.nkb) stage_done(p);
-                    p.kb += Cfg::GROUPS;
-                    return true;
+                for (int j = 0; j < 4; ++j)
+                    w[j] = lds_u4(from + s * (uint32_t)Cfg::W_STAGE + (uint32_t)(((mine * 4 + j) ^ (row & 7)) << 4));
+                __syncwarp();
+                if (lane == 0) mbar_arrive(wempty0 + 8u * s);
+                if (++s == Cfg::NW) { s = 0; ph ^= 1u; }
+                const uint32_t to = lanes + i % Cfg::NA * 64u + (uint32_t)mine * 32u, before = i - Cfg::NA;
+                uint32_t f[16];
+                half_block(w[0], w[1], f);
+                if (i >= Cfg::NA && !(ok = warp_wait(used0 + 8u * (before % Cfg::NC), (before / Cfg::NC) & 1u, flags))) break;
+                tc_fence_after();
+                if (there) {
+                    tmem_store16(to, f);
+                    half_block(w[2], w[3], f);
+                    tmem_store16(to + 16u, f);
+                    tmem_st_wait();
                 }
-                // (two groups, an odd number of K-blocks: the second group has no part in the last stage)
-                if (Cfg::GROUPS == 2 && mine == 1 && (p.nkb & 1)) {
-                    if (!(ok = warp_wait(wfull0 + 8u * p.s, p.ph, flags))) return false;
-                    stage_done(p);
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    if constexpr (PAIR) mbar_arrive_peer(peer_addr(afull0 + 8u * (i % Cfg::NA), 0));
+                    else mbar_arrive(afull0 + 8u * (i % Cfg::NA));
                 }
-                p.i += (uint32_t)p.nkb;
-                p.t += step;
-                open(p);
-            }
-            return false;
-        };
-        Place p = {first, 0, 0, 0, 0, 0};
-        open(p);
-        uint4 w[4];
-        uint32_t i = 0;
-        bool more = fetch(p, w, i);
-        while (more) {
-            const uint32_t q = i % Cfg::NA, par = ((i / Cfg::NA) & 1u) ^ 1u;
-            uint32_t f[16], g[16];
-            half_block(w[0], w[1], f);
-            half_block(w[2], w[3], g);
-            more = fetch(p, w, i);
-            if (!ok || !(ok = warp_wait(aempty0 + 8u * q, par, flags))) break;
-            tc_fence_after();
-            tmem_store16(lanes + q * 32u, f);
-            tmem_store16(lanes + q * 32u + 16u, g);
-            tmem_st_wait();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) {
-                if constexpr (PAIR) mbar_arrive_peer(peer_addr(afull0 + 8u * q, 0));
-                else mbar_arrive(afull0 + 8u * q);
             }
         }
     } else {
@@ -421,7 +391,7 @@ i8_tile_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ 
                     bytes += n ? (uint32_t)((big[h] ? 64 : 16) * kKB * 2) : 0u;
                 }
                 for (int k = 0; k < x.nk; k += kWK) {
-                    if (!(ok = mbar_wait(cempty0 + 8u * s, ph ^ 1u, flags))) break;
+                    if (!(ok = mbar_wait(used0 + 8u * s, ph ^ 1u, flags))) break;
                     const uint32_t fb = cfull0 + 8u * s, bar = PAIR ? peer_addr(fb, 0) : fb;
                     const int blocks = k + kKB < x.nk ? 2 : 1;
                     if (rank == 0) mbar_arrive_expect_tx(fb, bytes * Cfg::CTAS * (uint32_t)blocks);
@@ -459,42 +429,39 @@ i8_tile_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ 
             };
             for (int t = first; t < total && ok; t += step) {
                 const I8Tile x = tile(t);
-                const int nkb = (uniform(x.nk) + kKB - 1) / kKB;
+                const int nk = uniform(x.nk);
                 const uint32_t n0 = (uint32_t)uniform(x.n[0]), n1 = Cfg::HALVES == 2 ? (uint32_t)uniform(x.n[1]) : 0u;
                 const uint32_t i0 = idesc_f16(kLRows * Cfg::CTAS) | n0 >> 3 << 17, i1 = idesc_f16(kLRows * Cfg::CTAS) | n1 >> 3 << 17;
-                for (int kb = 0; kb < nkb && ok; kb += 2) {
+                for (int k = 0; k < nk; k += kWK) {
+                    const int kc = k % kI8Chunk;
+                    const bool two = k + kKB < nk;
                     if (!(ok = warp_wait(cfull0 + 8u * cs, cph, flags))) break;
-#pragma unroll
-                    for (int b = 0; b < 2; ++b) {
-                        if (kb + b >= nkb) break;
-                        const int kc = (kb + b) % (kI8Chunk / kKB);
-                        if (!(ok = warp_wait(afull0 + 8u * as, aph, flags))) break;
-                        const uint32_t st = (base + cs * (uint32_t)Cfg::C_STAGE + (uint32_t)(b * Cfg::C_BLOCK)) >> 4;
-                        const uint32_t at = tmem + (uint32_t)Cfg::A0 + as * 32u;
-                        if (kc == 0 && !(ok = warp_wait(tempty0 + 8u * s0, e0, flags))) break;
-                        tc_fence_after();
-                        mma_block<PAIR>(elected, tmem + s0 * (uint32_t)Cfg::HC, at, st, i0, kc != 0);
-                        if (n1) {
-                            if (kc == 0) {
-                                if (!(ok = warp_wait(tempty0 + 8u * s1, e1, flags))) break;
-                                tc_fence_after();
-                            }
-                            mma_block<PAIR>(elected, tmem + s1 * (uint32_t)Cfg::HC, at, st + (uint32_t)(Cfg::C_HALF >> 4), i1, kc != 0);
+                    if (kc == 0 && !(ok = warp_wait(tempty0 + 8u * s0, e0, flags))) break;
+                    if (!(ok = warp_wait(afull0 + 8u * as, aph, flags))) break;
+                    tc_fence_after();
+                    const uint32_t st = (base + cs * (uint32_t)Cfg::C_STAGE) >> 4, at = tmem + (uint32_t)Cfg::A0 + as * 64u;
+                    mma_block<PAIR>(elected, tmem + s0 * (uint32_t)Cfg::HC, at, st, i0, kc != 0);
+                    if (two) mma_block<PAIR>(elected, tmem + s0 * (uint32_t)Cfg::HC, at + 32u, st + (uint32_t)(Cfg::C_BLOCK >> 4), i0, 1);
+                    if (n1) {
+                        if (kc == 0) {
+                            if (!(ok = warp_wait(tempty0 + 8u * s1, e1, flags))) break;
+                            tc_fence_after();
                         }
-                        commit_elected<PAIR>(elected, aempty0 + 8u * as);
-                        if (++as == Cfg::NA) { as = 0; aph ^= 1u; }
-                        if (kc == kI8Chunk / kKB - 1 || kb + b == nkb - 1) {
+                        const uint32_t sh = st + (uint32_t)(Cfg::C_HALF >> 4);
+                        mma_block<PAIR>(elected, tmem + s1 * (uint32_t)Cfg::HC, at, sh, i1, kc != 0);
+                        if (two) mma_block<PAIR>(elected, tmem + s1 * (uint32_t)Cfg::HC, at + 32u, sh + (uint32_t)(Cfg::C_BLOCK >> 4), i1, 1);
+                    }
+                    commit_elected<PAIR>(elected, used0 + 8u * cs);
+                    if (++as == Cfg::NA) { as = 0; aph ^= 1u; }
+                    if (++cs == Cfg::NC) { cs = 0; cph ^= 1u; }
+                    if (kc == kI8Chunk - kWK || k + kWK >= nk) {
+                        commit_elected<PAIR>(elected, tfull0 + 8u * s0);
+                        next();
+                        if (n1) {
                             commit_elected<PAIR>(elected, tfull0 + 8u * s0);
                             next();
-                            if (n1) {
-                                commit_elected<PAIR>(elected, tfull0 + 8u * s0);
-                                next();
-                            }
                         }
                     }
-                    if (!ok) break;
-                    commit_elected<PAIR>(elected, cempty0 + 8u * cs);
-                    if (++cs == Cfg::NC) { cs = 0; cph ^= 1u; }
                 }
             }
             commit_elected<PAIR>(elected, done_bar);
