@@ -839,17 +839,18 @@ def route_balance(logits, experts, coef: float = 1.0, mask=None, ws=None, stream
     experts: route's, int32 [T, k].  Returns (Balance(loss, a float32 scalar on
     the GPU, counts int32 [E], tokens int32 scalar, k), ws)."""
     torch, where = _torch(), "route_balance"
-    dt, ldl, (T, E), dev = _dtype(logits, where), _pitch(logits, where), logits.shape, logits.device
-    if len(experts.shape) != 2 or experts.shape[0] != T:
-        _bad(where, f"experts have to be [{T}, k], got {tuple(experts.shape)}")
-    k = experts.shape[1]
-    pe, pm = _ints(experts, T * k, dev, "route_balance: experts"), _mask(mask, T, dev, "route_balance: mask")
+    dt, ldl, (T, E), dev, shape = _dtype(logits, where), _pitch(logits, where), logits.shape, logits.device, experts.shape
+    if len(shape) != 2 or shape[0] != T:
+        _bad(where, f"experts have to be [{T}, k], got {tuple(shape)}")
+    k, i32 = shape[1], torch.int32
+    pe = _ints(experts, None, dev, "route_balance: experts")
     if ws is None:
         ws = _empty(_lib.emu_route_balance_workspace_bytes(E), torch.uint8, dev, stream)
-    b = Balance(_empty((), torch.float32, dev, stream), _empty((E,), torch.int32, dev, stream),
-                _empty((), torch.int32, dev, stream), k)
-    r = _lib.emu_route_balance(dt, T, E, k, logits.data_ptr(), ldl, pe, pm, coef, b[0].data_ptr(), b[1].data_ptr(),
-                               b[2].data_ptr(), ws.data_ptr(), ws.numel(), _raw_stream(stream, dev))
+    b = Balance(_empty((), torch.float32, dev, stream), _empty(E, i32, dev, stream), _empty((), i32, dev, stream), k)
+    r = _lib.emu_route_balance(dt, T, E, k, logits.data_ptr(), ldl, pe,
+                               None if mask is None else _mask(mask, T, dev, "route_balance: mask"), coef,
+                               b[0].data_ptr(), b[1].data_ptr(), b[2].data_ptr(), ws.data_ptr(), ws.numel(),
+                               _raw_stream(stream, dev))
     if r:
         _check(r, "emu_route_balance")
     return b, ws
@@ -862,23 +863,25 @@ def route_balance_backward(logits, balance, dloss=None, coef: float = 1.0, mask=
     (None: 1).  add: a gradient of the same logits (of route_backward, say) that
     this one is added to, before the one rounding; dlogits may be the same tensor."""
     where = "route_balance_backward"
-    dt, ldl, (T, E), dev = _dtype(logits, where), _pitch(logits, where), logits.shape, logits.device
-    _, counts, tokens, k = balance
+    dt, ldl, shape, dev = _dtype(logits, where), _pitch(logits, where), logits.shape, logits.device
+    (T, E), (_, counts, tokens, k) = shape, balance
     if dlogits is None:
-        dlogits = _empty((T, E), logits.dtype, dev, stream)
-    elif dlogits.shape != logits.shape or dlogits.dtype is not logits.dtype:
+        dlogits, ldd = _empty(shape, logits.dtype, dev, stream), E
+    elif dlogits.shape != shape or dlogits.dtype is not logits.dtype:
         _bad(where, "dlogits differ from logits")
+    else:
+        ldd = _pitch(dlogits, where, dev)
     pa, lda = None, 0
     if add is not None:
-        if add.shape != logits.shape or add.dtype is not logits.dtype:
+        if add.shape != shape or add.dtype is not logits.dtype:
             _bad(where, "add differs from logits")
         pa, lda = add.data_ptr(), _pitch(add, "route_balance_backward: add", dev)
     r = _lib.emu_route_balance_backward(dt, T, E, k, logits.data_ptr(), ldl,
                                         _ints(counts, E, dev, "route_balance_backward: counts"),
                                         _ints(tokens, 1, dev, "route_balance_backward: tokens"),
-                                        _mask(mask, T, dev, "route_balance_backward: mask"), coef,
-                                        _float_pairs(dloss, (), dev, "route_balance_backward: dloss"), pa, lda,
-                                        dlogits.data_ptr(), _pitch(dlogits, where, dev), _raw_stream(stream, dev))
+                                        None if mask is None else _mask(mask, T, dev, "route_balance_backward: mask"),
+                                        coef, _float_pairs(dloss, (), dev, "route_balance_backward: dloss"), pa, lda,
+                                        dlogits.data_ptr(), ldd, _raw_stream(stream, dev))
     if r:
         _check(r, "emu_route_balance_backward")
     return dlogits
@@ -889,7 +892,7 @@ Int8 = collections.namedtuple("Int8", "codes scales")
 
 def _codes8(t, where, device=None):
     """Row pitch of a CUDA tensor of codes."""
-    if t.dtype is not _torch().int8:
+    if t.dtype is not _torch_module.int8:
         _bad(where, f"int8 codes are needed, got {t.dtype}")
     return _pitch(t, where, device)
 
@@ -903,25 +906,31 @@ def i8_quantize(X, codes=None, scales=None, ws=None, stream=None):
     a scale for each, weights [N, K] or [G, N, K] with one for each channel."""
     torch, where = _torch(), "i8_quantize"
     dt, ldx, dev, shape = _dtype(X, "i8_quantize: X"), _pitch(X, "i8_quantize: X"), X.device, X.shape
-    if len(shape) not in (2, 3):
+    if len(shape) == 2:
+        G, (rows, cols) = 1, shape
+    elif len(shape) == 3:
+        G, rows, cols = shape
+    else:
         _bad(where, f"X has to be [rows, cols] or [G, rows, cols], got {tuple(shape)}")
-    G, rows, cols = (1, *shape) if len(shape) == 2 else shape
     if codes is None:
-        ld = (cols + 15) // 16 * 16 or 16
-        codes = _empty((*shape[:-1], ld), torch.int8, dev, stream)
-        if ld != cols:
-            codes = codes[..., :cols]
-        ldq, strideq = ld, rows * ld
+        ldq = (cols + 15) // 16 * 16 or 16
+        strideq = rows * ldq
+        if ldq == cols:
+            codes = _empty(shape, torch.int8, dev, stream)
+        else:
+            codes = _empty((*shape[:-1], ldq), torch.int8, dev, stream)[..., :cols]
     else:
         ldq, strideq = _codes8(codes, "i8_quantize: codes", dev), codes.stride(0) if len(shape) == 3 else 0
         if codes.shape != shape:
             _bad(where, "codes have another shape")
     if scales is None:
         scales = _empty(shape[:-1], torch.float32, dev, stream)
+        ps = scales.data_ptr()
+    else:
+        ps = _float_pairs(scales, shape[:-1], dev, "i8_quantize: scales")
     if G:
         r = _lib.emu_i8_quantize(dt, G, rows, cols, X.data_ptr(), ldx, X.stride(0) if G > 1 else 0, codes.data_ptr(), ldq,
-                                 strideq, _float_pairs(scales, shape[:-1], dev, "i8_quantize: scales"),
-                                 ws.data_ptr() if ws is not None else None, ws.numel() if ws is not None else 0,
+                                 strideq, ps, None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(),
                                  _raw_stream(stream, dev))
         if r:
             _check(r, "emu_i8_quantize")
@@ -935,38 +944,44 @@ def i8_gemm(X, W, ends=None, src=None, Y=None, dtype=None, ws=None, stream=None)
     pairs (int8 codes, FP32 scales) as i8_quantize makes them.  Y: BF16, FP32 or
     int32 (dtype, or a given Y's; BF16 otherwise); int32 results are the sums
     themselves, without scales.  ws: emu_i8_gemm_workspace_bytes bytes that a
-    caller may keep (one for all calls of a stream).  Returns (Y, ws)."""
+    caller may keep for calls of these sizes, one after the other.  Returns (Y, ws)."""
     torch, where = _torch(), "i8_gemm"
     (x, xs), (w, wscales) = X, W
-    dev = x.device
+    dev, xshape, shape = x.device, x.shape, w.shape
     ldx, ldw = _codes8(x, "i8_gemm: X"), _codes8(w, "i8_gemm: W", dev)
-    shape = w.shape
-    G = 1 if ends is None else ends.numel()
-    if len(x.shape) != 2 or len(shape) != (2 if ends is None else 3) or (ends is not None and shape[0] != G):
-        _bad(where, f"X {tuple(x.shape)}, weights {tuple(shape)} for {G} group(s)")
-    (xrows, K), N = x.shape, shape[-2]
+    G, pe, stride = 1, None, 0
+    if ends is not None:
+        G, pe = ends.numel(), _ints(ends, None, dev, "i8_gemm: ends")
+        if G > 1 and len(shape) == 3:
+            stride = w.stride(0)
+    if len(xshape) != 2 or len(shape) != (2 if ends is None else 3) or (ends is not None and shape[0] != G):
+        _bad(where, f"X {tuple(xshape)}, weights {tuple(shape)} for {G} group(s)")
+    (xrows, K), N = xshape, shape[-2]
     if shape[-1] != K:
         _bad(where, f"X has {K} columns, the weights {shape[-1]}")
-    rows = src.numel() if src is not None else xrows
+    rows, ps = xrows, None
+    if src is not None:
+        rows, ps = src.numel(), _ints(src, None, dev, "i8_gemm: src")
     if Y is None:
-        Y = _empty((rows, N), torch.bfloat16 if dtype is None else dtype, dev, stream)
+        Y, ldy = _empty((rows, N), torch.bfloat16 if dtype is None else dtype, dev, stream), N
     elif Y.shape != (rows, N) or (dtype is not None and Y.dtype is not dtype):
         _bad(where, "Y has another shape or type")
-    yt = I32 if Y.dtype is torch.int32 else _dtype(Y, "i8_gemm: Y")
-    if yt == I32:
-        load()
-        px = pw = None
     else:
+        ldy = _pitch(Y, "i8_gemm: Y", dev)
+    px = pw = None
+    if Y.dtype is torch.int32:
+        yt = I32
+        load()
+    else:
+        yt = _dtype(Y, "i8_gemm: Y")
         px = _float_pairs(xs, (xrows,), dev, "i8_gemm: scales of X")
         pw = _float_pairs(wscales, shape[:-1], dev, "i8_gemm: scales of W")
-    pw8, stride = w.data_ptr(), w.stride(0) if G > 1 else 0
+    pc = w.data_ptr()
     if ws is None:
-        whole = (pw8 | ldw | stride) % 16 == 0 and (G <= 1 or stride >= N * ldw)
-        ws = _empty(_lib.emu_i8_gemm_workspace_bytes(G, rows, N, K, int(whole)), torch.uint8, dev, stream)
-    r = _lib.emu_i8_gemm(G, rows, N, K, x.data_ptr(), xrows, ldx, px,
-                         _ints(src, None, dev, "i8_gemm: src") if src is not None else None, pw8, ldw, stride, pw,
-                         _ints(ends, G, dev, "i8_gemm: ends") if ends is not None else None, Y.data_ptr(), yt,
-                         _pitch(Y, "i8_gemm: Y", dev), ws.data_ptr(), ws.numel(), _raw_stream(stream, dev))
+        whole = (pc | ldw | stride) % 16 == 0 and (G <= 1 or stride >= N * ldw)
+        ws = _empty(_lib.emu_i8_gemm_workspace_bytes(G, rows, N, K, whole), torch.uint8, dev, stream)
+    r = _lib.emu_i8_gemm(G, rows, N, K, x.data_ptr(), xrows, ldx, px, ps, pc, ldw, stride, pw, pe, Y.data_ptr(), yt, ldy or 1,
+                         ws.data_ptr(), ws.numel(), _raw_stream(stream, dev))
     if r:
         _check(r, "emu_i8_gemm")
     return Y, ws
