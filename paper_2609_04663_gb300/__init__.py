@@ -917,6 +917,8 @@ def i8_quantize(X, codes=None, scales=None, ws=None, stream=None):
         strideq = rows * ldq
         if ldq == cols:
             codes = _empty(shape, torch.int8, dev, stream)
+        elif stream is None:
+            codes = torch.empty_strided(shape, (strideq, ldq, 1)[-len(shape):], dtype=torch.int8, device=dev)
         else:
             codes = _empty((*shape[:-1], ldq), torch.int8, dev, stream)[..., :cols]
     else:
