@@ -442,7 +442,10 @@ i8_tile_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ 
                     const uint32_t st = (base + cs * (uint32_t)Cfg::C_STAGE) >> 4, at = tmem + (uint32_t)Cfg::A0 + as * 64u;
                     mma_block<PAIR>(elected, tmem + s0 * (uint32_t)Cfg::HC, at, st, i0, kc != 0);
                     if (two) mma_block<PAIR>(elected, tmem + s0 * (uint32_t)Cfg::HC, at + 32u, st + (uint32_t)(Cfg::C_BLOCK >> 4), i0, 1);
+                    // a sum's last stage: the first half is read while the second one is still multiplied
+                    const bool whole = kc == kI8Chunk - kWK || k + kWK >= nk;
                     if (n1) {
+                        if (whole) commit_elected<PAIR>(elected, tfull0 + 8u * s0);
                         if (kc == 0) {
                             if (!(ok = warp_wait(tempty0 + 8u * s1, e1, flags))) break;
                             tc_fence_after();
@@ -454,13 +457,10 @@ i8_tile_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ 
                     commit_elected<PAIR>(elected, used0 + 8u * cs);
                     if (++as == Cfg::NA) { as = 0; aph ^= 1u; }
                     if (++cs == Cfg::NC) { cs = 0; cph ^= 1u; }
-                    if (kc == kI8Chunk - kWK || k + kWK >= nk) {
+                    if (whole) {
+                        if (n1) next();
                         commit_elected<PAIR>(elected, tfull0 + 8u * s0);
                         next();
-                        if (n1) {
-                            commit_elected<PAIR>(elected, tfull0 + 8u * s0);
-                            next();
-                        }
                     }
                 }
             }
