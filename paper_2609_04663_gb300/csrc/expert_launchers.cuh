@@ -83,7 +83,7 @@ struct I8Product {
     uint32_t *flags;
 };
 cudaError_t launch_i8_rows(const I8Product &p, cudaStream_t st);
-bool i8_few_rows(int64_t G, int64_t rows);      // launch_i8_rows is the faster way
+bool i8_few_rows(int64_t G, int64_t rows, int64_t N, int64_t K);      // launch_i8_rows is the faster way
 // On the tensor cores; scratch: i8_tile_scratch_bytes (aligned: W's rows can be read 16 bytes at a time).
 size_t i8_tile_scratch_bytes(int64_t G, int64_t rows, int64_t N, int64_t K, bool aligned);
 cudaError_t launch_i8_tile(I8Product p, void *scratch, cudaStream_t st);

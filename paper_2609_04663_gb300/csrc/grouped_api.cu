@@ -490,7 +490,7 @@ emu_status emu_i8_quantize(int dtype, int64_t G, int64_t rows, int64_t cols, con
 size_t emu_i8_gemm_workspace_bytes(int64_t G, int64_t rows, int64_t N, int64_t K, int aligned)
 {
     if (G < 1 || rows < 0 || N < 0 || K < 0) return 0;
-    if (rows == 0 || N == 0 || K == 0 || i8_few_rows(G, rows)) return kWsHeaderBytes;
+    if (rows == 0 || N == 0 || K == 0 || i8_few_rows(G, rows, N, K)) return kWsHeaderBytes;
     return kWsHeaderBytes + i8_tile_scratch_bytes(G, rows, N, K, aligned != 0);
 }
 
@@ -523,7 +523,7 @@ emu_status emu_i8_gemm(int64_t G, int64_t rows, int64_t N, int64_t K, const int8
     p.X = X; p.W = W; p.xscales = xscales; p.wscales = wscales; p.src = src; p.ends = ends; p.xrows = xrows; p.ldx = ldx;
     p.ldw = ldw; p.stridew = G > 1 ? stridew : 0; p.ldy = ldy; p.Y = Y; p.ytype = ytype; p.G = (int)G; p.rows = (int)rows;
     p.N = (int)N; p.K = (int)K; p.flags = &static_cast<WsHeader *>(ws)->flags;
-    return cuda_status(i8_few_rows(G, rows) ? launch_i8_rows(p, st)
+    return cuda_status(i8_few_rows(G, rows, N, K) ? launch_i8_rows(p, st)
                                             : launch_i8_tile(p, static_cast<char *>(ws) + kWsHeaderBytes, st));
 }
 

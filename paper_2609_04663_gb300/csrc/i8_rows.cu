@@ -252,14 +252,22 @@ cudaError_t by_alignment(const RowsArgs &a, cudaStream_t st)
 
 }  // namespace
 
-bool i8_few_rows(int64_t G, int64_t rows) { return rows <= (G > 1 ? 4 * G : 8); }
+// Up to where the tensor cores' kernel, which needs 9.5 us for the smallest product, is slower:
+// 8 rows x 4096 x 4096 10.5 us here and 11.6 there, x 8192 x 8192 32 and 22; 3 rows x 8192 x 8192 20 and 22, x 16384 x
+// 16384 63 and 52; 1 and 2 rows always; 2 rows of each of 32 experts of 2048 x 4096 54.6 and 53.0, 4 rows 62.0 and 53.6.
+bool i8_few_rows(int64_t G, int64_t rows, int64_t N, int64_t K)
+{
+    const int64_t weights = N * K;
+    return G > 1 ? rows <= 2 * G : rows <= 2 || (rows <= 4 && weights < (int64_t)1 << 27) || (rows <= 8 && weights <= (int64_t)1 << 24);
+}
 
 cudaError_t launch_i8_rows(const I8Product &p, cudaStream_t st)
 {
     RowsArgs a = {};
     a.p = p;
     return p.rows == 1 ? by_alignment<1>(a, st) : p.rows <= 2 ? by_alignment<2>(a, st)
-           : p.rows <= 4 || p.G > 1 ? by_alignment<4>(a, st) : by_alignment<8>(a, st);
+           : p.G > 1 && p.rows <= p.G ? by_alignment<2>(a, st) : p.rows <= 4 || p.G > 1 ? by_alignment<4>(a, st)
+           : by_alignment<8>(a, st);
 }
 
 }  // namespace emu

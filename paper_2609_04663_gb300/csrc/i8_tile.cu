@@ -575,7 +575,10 @@ bool make_code_map(CUtensorMap *map, const int8_t *W, int64_t K, int64_t N, int6
 
 int64_t up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
 
-// Which tiles: 256 columns on a pair of SMs, or 64 on one with K in parts while SMs are free.
+// Which tiles: 256 columns on a pair of SMs, or 64 on one with K in parts while SMs are free; by
+// waves times the nanoseconds of 64 codes (measured, weights from HBM: a pair's 290 up to 128 columns and 410
+// up to 256, one SM's 240).  32 experts of 2048 x 4096: 1024 rows 63 us with 64 columns and 66 with pairs, 4096 rows 118
+// and 88; 512 rows x 4096 x 4096 30 and 32, 1024 rows 55 and 34.
 struct Plan {
     bool pair;
     int parts;
@@ -584,15 +587,13 @@ struct Plan {
 Plan plan(int64_t G, int64_t rows, int64_t N, int64_t K)
 {
     auto waves = [](int64_t tiles, int64_t units) { return (tiles + units - 1) / units; };
-    const int64_t sms = 152, n = (rows + G - 1) / G;
-    const int64_t t256 = waves(G * ((n + 255) / 256) * ((N + 255) / 256), sms / 2) * 560;
-    const int64_t t64 = waves(G * ((n + 63) / 64) * ((N + 127) / 128), sms) * 350;
+    const int64_t sms = 152, n = (rows + G - 1) / G, least = G * ((n + 63) / 64) * ((N + 127) / 128);
+    const int64_t t256 = waves(G * ((n + 255) / 256) * ((N + 255) / 256), sms / 2) * (n <= 128 ? 290 : 410);
     Plan x;
-    x.pair = t256 < t64;
+    x.pair = t256 < waves(least, sms) * 240;
     x.tiles = max_tiles(rows, G, N, x.pair ? 256 : 64, x.pair ? 2 : 1);
     x.parts = 1;
     if (!x.pair) {
-        const int64_t least = G * ((n + 63) / 64) * ((N + 127) / 128);
         int64_t parts = sms / least;
         if (parts > K / 512) parts = K / 512;
         if (parts > 1) x.parts = (int)(parts > 16 ? 16 : parts);
