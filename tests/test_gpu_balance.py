@@ -167,6 +167,22 @@ def test_pitches_and_alignments(dev, dtype):
         assert bool((out == 9.0).all())
 
 
+def test_past_two_to_the_31(dev):
+    T, E, k = 2_200_000, 1024, 2
+    z = torch.empty(T, E, dtype=torch.bfloat16, device=dev).normal_(generator=torch.Generator(device=dev).manual_seed(1))
+    experts = torch.stack((torch.arange(T, device=dev) % E, (torch.arange(T, device=dev) * 7 + 1) % E), 1).int()
+    b, ws = emu.route_balance(z, experts)
+    assert emu.read_flags(ws) == 0 and int(b.tokens) == T
+    assert torch.equal(b.counts.long(), torch.bincount(experts.reshape(-1).long(), minlength=E))
+    d = emu.route_balance_backward(z, b)
+    f = b.counts.double() * (E / (T * k))
+    at = torch.tensor([0, 1, 2 ** 21 - 1, 2 ** 21, 2 ** 21 + 1, T - 1], device=dev)
+    p = torch.softmax(z[at].double(), 1)
+    S = (p * f).sum(1, keepdim=True)
+    want, room = p * (f - S) / T, p * (f + S) / T * (2 * 12 + 200) * U
+    assert bool(((d[at].double() - want).abs() <= room * (1 + 2 ** -8) + want.abs() * 2 ** -8).all())
+
+
 def test_gradient_against_differences(dev):
     z, experts, mask, _ = case(dev, 60, 24, 3, torch.float32, True)
     coef = 0.7

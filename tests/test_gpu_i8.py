@@ -178,6 +178,12 @@ def test_one_matrix(dev, rows, N, K):
     check(*make(dev, rows, N, K))
 
 
+@pytest.mark.parametrize("K", [1, 2, 15, 17, 63, 127, 129])
+@pytest.mark.parametrize("rows,N", [(1, 1), (9, 1), (40, 127), (300, 2), (700, 257)])
+def test_short_contractions_and_narrow_results(dev, rows, N, K):
+    check(*make(dev, rows, N, K))
+
+
 @pytest.mark.parametrize("rows,N,K", [(1, 40, 333), (6, 40, 333), (20, 200, 333), (300, 300, 1029)])
 def test_rows_on_16_bytes_within_a_wider_pitch(dev, rows, N, K):
     check(*make(dev, rows, N, K, pad=-K % 16))
@@ -210,6 +216,59 @@ def test_bad_rows_and_ends_are_flagged(dev, rows):
     check(X, W, ends=[2, rows // 2, rows], src=bad, flags=emu.FLAG_INDEX)
     check(X, W, ends=[rows // 2, 2, rows], src=src, flags=emu.FLAG_INDEX)
     check(X, W, ends=[-5, 4, rows + 9], src=src, flags=emu.FLAG_INDEX)
+
+
+@pytest.mark.parametrize("rows", [3, 200])
+def test_no_rows_to_take_and_nothing_to_multiply(dev, rows):
+    X, W = make(dev, 5, 40, 64)
+    none = (X[0][:0], X[1][:0])
+    src = torch.arange(rows, dtype=torch.int32, device=dev)
+    Y, ws = emu.i8_gemm(none, W, src=src, dtype=torch.float32)
+    assert emu.read_flags(ws) == emu.FLAG_INDEX and Y.shape == (rows, 40) and not Y.any()
+    Y, ws = emu.i8_gemm(none, W)
+    assert Y.shape == (0, 40) and emu.read_flags(ws) == 0
+    Y, _ = emu.i8_gemm((X[0][:, :0], X[1]), (W[0][:, :0], W[1]))
+    assert Y.shape == (5, 40) and not Y.any()
+    Y, _ = emu.i8_gemm(X, (W[0][:0], W[1][:0]))
+    assert Y.shape == (5, 0)
+
+
+@pytest.mark.parametrize("rows", [2, 60, 600])
+def test_scales_left_out(dev, rows):
+    (x, xs), (w, v) = make(dev, rows, 80, 192)
+    S = sums(x, w)
+    for X, W, want in (((x, None), (w, v), S * v.double()), ((x, xs), (w, None), S * xs.double()[:, None]), ((x, None), (w, None), S)):
+        Y, _ = emu.i8_gemm(X, W, dtype=torch.float32)
+        assert bool(((Y.double() - want).abs() <= F32_TOL * want.abs()).all())
+
+
+def test_past_two_to_the_31(dev):
+    # weights of 4.9 GB: the last group's lie past 2^32 bytes
+    G, N, K = 5, 8192, 119984
+    W = torch.empty(G, N, K, dtype=torch.int8, device=dev).random_(-128, 128, generator=gen(dev, 1))
+    v = torch.rand(G, N, device=dev)
+    some = torch.randint(0, N, (50,), device=dev)
+    for rows in (2, 20):
+        X = torch.empty(rows, K, dtype=torch.int8, device=dev).random_(-128, 128, generator=gen(dev, rows))
+        xs = torch.rand(rows, device=dev)
+        ends = torch.tensor([0, 0, 0, 0, rows], dtype=torch.int32, device=dev)
+        Y, ws = emu.i8_gemm((X, xs), (W, v), ends=ends, dtype=torch.int32)
+        assert torch.equal(Y[:, some].double(), X.double() @ W[4][some].double().T) and emu.read_flags(ws) == 0
+    del W
+    # and an answer of 4.6 GB
+    X, W = make(dev, 70001, 32768, 64)
+    Y, ws = emu.i8_gemm(X, W)
+    at = torch.tensor([0, 1, 65535, 65536, 70000], device=dev)
+    want = scaled(sums(X[0][at], W[0]), X[1][at], W[1])
+    assert bool(((Y[at].double() - want).abs() <= BF16_TOL * want.abs()).all()) and emu.read_flags(ws) == 0
+
+
+def test_quantise_past_two_to_the_31(dev):
+    X = torch.empty(40000, 65536, dtype=torch.bfloat16, device=dev).normal_(generator=gen(dev, 2))
+    q = emu.i8_quantize(X)
+    at = torch.tensor([0, 17, 32767, 32768, 39999], device=dev)
+    codes, scales = quantized(X[at])
+    assert torch.equal(q.codes[at], codes) and torch.equal(q.scales[at], scales)
 
 
 def test_many_groups(dev):
