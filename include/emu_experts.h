@@ -184,10 +184,11 @@ emu_status emu_rows_combine_backward_full(int dtype, int64_t T, int64_t k, int64
  * logits all are has p = 0.  An entry of experts outside 0 .. E-1 is not counted.
  * 1 <= k <= 32, k <= E <= 1024, T k < 2^31 - 65536.  Sums in FP32, in an order that depends
  * on the sizes alone: same inputs, same bits.  ws: at least
- * emu_route_balance_workspace_bytes, not shared by calls in flight at once.
+ * emu_route_balance_workspace_bytes, 16-byte aligned, not shared by calls in flight at once; where
+ * that is 0, emu_split_workspace_bytes(32) for the flags, or NULL, which reports none.
  * Flags: EMU_FLAG_NONFINITE (a counted token's logit is NaN or plus infinity),
  * EMU_FLAG_INDEX. */
-size_t emu_route_balance_workspace_bytes(int64_t E);
+size_t emu_route_balance_workspace_bytes(int64_t T, int64_t E);
 emu_status emu_route_balance(int dtype, int64_t T, int64_t E, int64_t k, const void *logits, int64_t ldl,
                              const int32_t *experts, const uint8_t *mask, float coef, float *loss, int32_t *counts,
                              int32_t *tokens, void *ws, size_t ws_bytes, emu_stream_t stream);
@@ -225,7 +226,8 @@ emu_status emu_i8_quantize(int dtype, int64_t G, int64_t rows, int64_t cols, con
  * not overlap, and copied first otherwise where many rows meet it.  xscales [xrows], wscales [G][N] FP32.  Rows of no group, and rows whose src is
  * outside 0 .. xrows-1, are zero.  aligned: whether W is
  * such a one (0 is enough for any).  ws: at least emu_i8_gemm_workspace_bytes, 16-byte aligned, not shared by calls
- * in flight at once.  Flags: EMU_FLAG_INDEX, EMU_FLAG_TIMEOUT. */
+ * in flight at once; where that is 0 (a few rows), emu_split_workspace_bytes(32) for the flags, or NULL,
+ * which reports none.  Flags: EMU_FLAG_INDEX, EMU_FLAG_TIMEOUT. */
 size_t emu_i8_gemm_workspace_bytes(int64_t G, int64_t rows, int64_t N, int64_t K, int aligned);
 emu_status emu_i8_gemm(int64_t G, int64_t rows, int64_t N, int64_t K, const int8_t *X, int64_t xrows, int64_t ldx,
                        const float *xscales, const int32_t *src, const int8_t *W, int64_t ldw, int64_t stridew,

@@ -86,7 +86,7 @@ _SIGS = {
     "emu_rows_combine_workspace_bytes": ("size", ["l"]),
     "emu_rows_combine_backward_full": ("i", ["i", "l", "l", "l", "p", "l", "p", "l", "l", "p", "p", "p", "l", "p", "p",
                                              "size", "p"]),
-    "emu_route_balance_workspace_bytes": ("size", ["l"]),
+    "emu_route_balance_workspace_bytes": ("size", ["l", "l"]),
     "emu_route_balance": ("i", ["i", "l", "l", "l", "p", "l", "p", "p", "f", "p", "p", "p", "p", "size", "p"]),
     "emu_route_balance_backward": ("i", ["i", "l", "l", "l", "p", "l", "p", "p", "p", "f", "p", "p", "l", "p", "l", "p"]),
     "emu_i8_quantize": ("i", ["i", "l", "l", "l", "p", "l", "l", "p", "l", "l", "p", "p", "size", "p"]),
@@ -836,8 +836,10 @@ def _mask(mask, T, device, where):
 def route_balance(logits, experts, coef: float = 1.0, mask=None, ws=None, stream=None):
     """emu_route_balance: the balance loss of a routing, coef E / (n k) sum_e
     counts_e P_e over the n tokens with a mask (bool or uint8 [T]; None: all).
-    experts: route's, int32 [T, k].  Returns (Balance(loss, a float32 scalar on
-    the GPU, counts int32 [E], tokens int32 scalar, k), ws)."""
+    experts: route's, int32 [T, k].  ws: emu_route_balance_workspace_bytes bytes
+    that a caller may keep (made here where they are needed); the call's flags are
+    in it.  Returns (Balance(loss, a float32 scalar on the GPU, counts int32 [E],
+    tokens int32 scalar, k), ws); ws is None where none was given or needed."""
     torch, where = _torch(), "route_balance"
     dt, ldl, (T, E), dev, shape = _dtype(logits, where), _pitch(logits, where), logits.shape, logits.device, experts.shape
     if len(shape) != 2 or shape[0] != T:
@@ -845,12 +847,14 @@ def route_balance(logits, experts, coef: float = 1.0, mask=None, ws=None, stream
     k, i32 = shape[1], torch.int32
     pe = _ints(experts, None, dev, "route_balance: experts")
     if ws is None:
-        ws = _empty(_lib.emu_route_balance_workspace_bytes(E), torch.uint8, dev, stream)
+        need = _lib.emu_route_balance_workspace_bytes(T, E)
+        if need:
+            ws = _empty(need, torch.uint8, dev, stream)
     b = Balance(_empty((), torch.float32, dev, stream), _empty(E, i32, dev, stream), _empty((), i32, dev, stream), k)
     r = _lib.emu_route_balance(dt, T, E, k, logits.data_ptr(), ldl, pe,
                                None if mask is None else _mask(mask, T, dev, "route_balance: mask"), coef,
-                               b[0].data_ptr(), b[1].data_ptr(), b[2].data_ptr(), ws.data_ptr(), ws.numel(),
-                               _raw_stream(stream, dev))
+                               b[0].data_ptr(), b[1].data_ptr(), b[2].data_ptr(), None if ws is None else ws.data_ptr(),
+                               0 if ws is None else ws.numel(), _raw_stream(stream, dev))
     if r:
         _check(r, "emu_route_balance")
     return b, ws
@@ -945,8 +949,10 @@ def i8_gemm(X, W, ends=None, src=None, Y=None, dtype=None, ws=None, stream=None)
     matrix W [N, K] for all rows, else [G, N, K]; src None: X[r]).  X and W:
     pairs (int8 codes, FP32 scales) as i8_quantize makes them.  Y: BF16, FP32 or
     int32 (dtype, or a given Y's; BF16 otherwise); int32 results are the sums
-    themselves, without scales.  ws: emu_i8_gemm_workspace_bytes bytes that a
-    caller may keep for calls of these sizes, one after the other.  Returns (Y, ws)."""
+    themselves, without scales (None in place of scales: 1).  ws:
+    emu_i8_gemm_workspace_bytes bytes that a caller may keep for calls of these
+    sizes, one after the other (made here where they are needed); the call's flags
+    are in it.  Returns (Y, ws); ws is None where none was given or needed."""
     torch, where = _torch(), "i8_gemm"
     (x, xs), (w, wscales) = X, W
     dev, xshape, shape = x.device, x.shape, w.shape
@@ -980,10 +986,11 @@ def i8_gemm(X, W, ends=None, src=None, Y=None, dtype=None, ws=None, stream=None)
         pw = _float_pairs(wscales, shape[:-1], dev, "i8_gemm: scales of W")
     pc = w.data_ptr()
     if ws is None:
-        whole = (pc | ldw | stride) % 16 == 0 and (G <= 1 or stride >= N * ldw)
-        ws = _empty(_lib.emu_i8_gemm_workspace_bytes(G, rows, N, K, whole), torch.uint8, dev, stream)
+        need = _lib.emu_i8_gemm_workspace_bytes(G, rows, N, K, (pc | ldw | stride) % 16 == 0 and (G <= 1 or stride >= N * ldw))
+        if need:
+            ws = _empty(need, torch.uint8, dev, stream)
     r = _lib.emu_i8_gemm(G, rows, N, K, x.data_ptr(), xrows, ldx, px, ps, pc, ldw, stride, pw, pe, Y.data_ptr(), yt, ldy or 1,
-                         ws.data_ptr(), ws.numel(), _raw_stream(stream, dev))
+                         None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), _raw_stream(stream, dev))
     if r:
         _check(r, "emu_i8_gemm")
     return Y, ws

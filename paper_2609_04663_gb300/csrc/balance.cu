@@ -8,7 +8,8 @@
 // row with V values each) has a token; lanes keep their experts' sums of p in FP32 over
 // all their tokens, a block adds its warps' in a fixed order, and one block of a second
 // launch adds the blocks' in a fixed order: no floating-point atomics, the same bits every
-// time.  With few tokens the first launch is one block and does both.
+// time.  With few tokens the first launch is one cluster, whose first block does that through shared
+// memory.
 #include "grouped_common.cuh"
 #include "expert_launchers.cuh"
 #include "pair_common.cuh"
@@ -35,6 +36,7 @@ struct BalanceArgs {
     uint32_t *flags;
     float coef;
     int T, E, k, blocks;
+    int cluster;                  // the blocks are one cluster
 };
 
 // The expert of value i of a lane, of L lanes with V values each: C neighbouring ones at a
@@ -177,7 +179,7 @@ __device__ __forceinline__ void publish(const BalanceArgs &a, float share, int n
         if (threadIdx.x == 0) {
             *a.loss = share;
             *a.tokens = n;
-            *a.flags = bits;
+            if (a.flags) *a.flags = bits;
         }
     }
 }
@@ -241,15 +243,35 @@ __global__ void __launch_bounds__(NT) balance_kernel(const BalanceArgs a)
     __syncthreads();
     const int all = tokens;
     auto at = [&](int w, int e) { return sm[(size_t)w * a.E + e]; };
-    if (gridDim.x == 1) {
-        const float cs = count_scale(a, all), inv_n = all > 0 ? 1.0f / (float)all : 0.0f;
-        float loss = 0.0f;
-        add_columns<NT>(WARPS, a.E, red, at, [&](int e, float s) {
-            const int c = hist[e];
-            a.counts[e] = c;
-            loss = fmaf((float)c * cs, s * inv_n, loss);
-        });
-        publish<NT>(a, loss, all, (uint32_t)bits, red);
+    if (a.cluster) {
+        // the block's sums end up in its first warp's row
+        add_columns<NT>(WARPS, a.E, red, at, [&](int e, float s) { sm[e] = s; });
+        if (a.blocks > 1) cluster_sync();
+        else __syncthreads();
+        if (blockIdx.x == 0) {
+            auto other = [&](const void *p, int r) {
+                uint32_t v;
+                asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(v) : "r"(peer_addr(smem_u32(p), (uint32_t)r)) : "memory");
+                return v;
+            };
+            int n_all = 0;
+            uint32_t some = 0;
+            for (int r = 0; r < a.blocks; ++r) { n_all += (int)other(&tokens, r); some |= other(&bits, r); }
+            const float cs = count_scale(a, n_all), inv_n = n_all > 0 ? 1.0f / (float)n_all : 0.0f;
+            float loss = 0.0f;
+            for (int e = threadIdx.x; e < a.E; e += NT) {
+                float s = 0.0f;
+                int c = 0;
+                for (int r = 0; r < a.blocks; ++r) {
+                    s += __uint_as_float(other(sm + e, r));
+                    c += (int)other(hist + e, r);
+                }
+                a.counts[e] = c;
+                loss = fmaf((float)c * cs, s * inv_n, loss);
+            }
+            publish<NT>(a, loss, n_all, some, red);
+        }
+        if (a.blocks > 1) cluster_sync();             // shared memory stays until it has been read
     } else {
         float *sums = a.sums + (int64_t)blockIdx.x * a.E;
         int32_t *parts = a.parts + (int64_t)blockIdx.x * (a.E + 2);
@@ -323,7 +345,7 @@ __global__ void __cluster_dims__(kFinishCtas, 1, 1) __launch_bounds__(512) balan
         for (int r = 1; r < kFinishCtas; ++r) loss += v[r];
         *a.loss = loss;
         *a.tokens = n;
-        *a.flags = (uint32_t)bits;
+        if (a.flags) *a.flags = (uint32_t)bits;
     }
     cluster_sync();                                   // shared memory stays until it has been read
 }
@@ -387,6 +409,12 @@ __global__ void __launch_bounds__(256) balance_backward_kernel(const BalanceArgs
     }
 }
 
+// Lanes a token.
+int lanes_of(int E) { return E <= 128 ? 8 : E <= 256 ? 16 : 32; }
+
+// Few tokens: at most four passes over them by a cluster of 8.
+bool one_cluster(int64_t T, int64_t E) { return T * lanes_of((int)E) <= 4 * 8 * (E > 512 ? 512 : 1024); }
+
 // Whether rows can be read C values at a time.
 bool whole_lanes(const void *p, int64_t ld, int bytes, int C)
 {
@@ -401,28 +429,37 @@ cudaError_t run_balance(BalanceArgs a, bool backward, cudaStream_t st)
         balance_backward_kernel<V, L, F32, C><<<(unsigned)(blocks > 152 * 8 ? 152 * 8 : blocks), 256, 0, st>>>(a);
         return cudaGetLastError();
     }
-    constexpr int NT = V >= 32 ? 512 : 1024, PASS = NT / L;
+    constexpr int NT = V >= 32 ? 512 : 1024, PASS = NT / L;      // (as one_cluster has it)
     const size_t sm = ((size_t)(NT / 32) * a.E + a.E) * 4;
     auto kern = balance_kernel<V, L, F32, C, NT>;
     if (sm > 44 * 1024) {
         const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sm);
         if (e != cudaSuccess) return e;
     }
-    int64_t blocks = ((int64_t)a.T + PASS - 1) / PASS;
-    if (blocks < 1) blocks = 1;
-    if (blocks > kBalanceBlocks) blocks = kBalanceBlocks;
-    a.blocks = (int)blocks;
-    kern<<<(unsigned)blocks, NT, sm, st>>>(a);
-    cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess || blocks == 1) return e;
+    const int64_t passes = ((int64_t)a.T + PASS - 1) / PASS;
     cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr;
+    cfg.blockDim = dim3(NT);
+    cfg.dynamicSmemBytes = sm;
+    cfg.stream = st;
+    cfg.attrs = &attr;
+    a.cluster = one_cluster(a.T, a.E) ? 1 : 0;
+    a.blocks = passes > kBalanceBlocks ? kBalanceBlocks : (int)passes;
+    if (a.cluster) a.blocks = passes <= 1 ? 1 : passes <= 2 ? 2 : passes <= 4 ? 4 : 8;
+    cfg.gridDim = dim3((unsigned)a.blocks);
+    if (a.cluster && a.blocks > 1) {
+        attr.id = cudaLaunchAttributeClusterDimension;
+        attr.val.clusterDim.x = (unsigned)a.blocks;
+        attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+        cfg.numAttrs = 1;
+    }
+    cudaError_t e = cudaLaunchKernelEx(&cfg, kern, a);
+    if (e != cudaSuccess || a.cluster) return e != cudaSuccess ? e : cudaGetLastError();
     cfg.gridDim = dim3(kFinishCtas);
     cfg.blockDim = dim3(512);
-    cfg.stream = st;
-    cudaLaunchAttribute attr;
+    cfg.dynamicSmemBytes = 0;
     attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr.val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = &attr;
     cfg.numAttrs = 1;
     e = cudaLaunchKernelEx(&cfg, balance_finish_kernel, a);
     return e != cudaSuccess ? e : cudaGetLastError();
@@ -453,7 +490,10 @@ cudaError_t by_type(const BalanceArgs &a, bool f32, bool backward, cudaStream_t 
 
 }  // namespace
 
-size_t balance_scratch_bytes(int64_t E) { return (size_t)kBalanceBlocks * (size_t)(2 * E + 2) * 4; }
+size_t balance_scratch_bytes(int64_t T, int64_t E)
+{
+    return one_cluster(T, E) ? 0 : (size_t)kBalanceBlocks * (size_t)(2 * E + 2) * 4;
+}
 
 cudaError_t launch_balance(int64_t T, int64_t E, int k, const void *logits, bool f32, int64_t ldl, const int32_t *experts,
                            const uint8_t *mask, float coef, float *loss, int32_t *counts, int32_t *tokens, void *scratch, uint32_t *flags,

@@ -62,7 +62,7 @@ cudaError_t launch_combine_backward(bool f32, int64_t T, int k, int64_t cols, co
                                     cudaStream_t st);       // owner: [yrows], or NULL: unnamed rows of dY are left
 
 // Balance loss of the routing (balance.cu).
-size_t balance_scratch_bytes(int64_t E);
+size_t balance_scratch_bytes(int64_t T, int64_t E);      // 0: none
 cudaError_t launch_balance(int64_t T, int64_t E, int k, const void *logits, bool f32, int64_t ldl, const int32_t *experts,
                            const uint8_t *mask, float coef, float *loss, int32_t *counts, int32_t *tokens, void *scratch,
                            uint32_t *flags, cudaStream_t st);
@@ -80,7 +80,7 @@ struct I8Product {
     int64_t xrows, ldx, ldw, stridew, ldy;
     void *Y;
     int ytype, G, rows, N, K;
-    uint32_t *flags;
+    uint32_t *flags;                       // (NULL for launch_i8_rows: none are reported)
 };
 cudaError_t launch_i8_rows(const I8Product &p, cudaStream_t st);
 bool i8_few_rows(int64_t G, int64_t rows, int64_t N, int64_t K);      // launch_i8_rows is the faster way

@@ -28,6 +28,12 @@ emu_status check_ws(void *ws, size_t ws_bytes, size_t need)
     return aligned16(ws) ? EMU_OK : EMU_ERR_MISALIGNED;
 }
 
+// A workspace that calls which need none (need = 0) may be given for their flags.
+emu_status check_optional_ws(void *ws, size_t ws_bytes, size_t need)
+{
+    return !ws && need == 0 ? EMU_OK : check_ws(ws, ws_bytes, need ? need : kWsHeaderBytes);
+}
+
 cudaError_t clear_flags(void *ws, cudaStream_t st)
 {
     return cudaMemsetAsync(&static_cast<WsHeader *>(ws)->flags, 0, sizeof(uint32_t), st);
@@ -431,9 +437,11 @@ emu_status emu_rows_combine_backward_full(int dtype, int64_t T, int64_t k, int64
                                                reinterpret_cast<cudaStream_t>(stream)));
 }
 
-size_t emu_route_balance_workspace_bytes(int64_t E)
+// The flag word and, where that is needed, scratch; 0: none needed.
+size_t emu_route_balance_workspace_bytes(int64_t T, int64_t E)
 {
-    return E < 1 ? 0 : kWsHeaderBytes + balance_scratch_bytes(E);
+    const size_t scratch = T < 0 || E < 1 ? 0 : balance_scratch_bytes(T, E);
+    return scratch ? kWsHeaderBytes + scratch : 0;
 }
 
 emu_status emu_route_balance(int dtype, int64_t T, int64_t E, int64_t k, const void *logits, int64_t ldl,
@@ -444,10 +452,11 @@ emu_status emu_route_balance(int dtype, int64_t T, int64_t E, int64_t k, const v
     if (s != EMU_OK) return s;
     if (!loss || (T > 0 && !experts)) return EMU_ERR_INVALID_ARG;
     if (!fits(loss, EMU_F32) || !fits(experts, EMU_F32)) return EMU_ERR_MISALIGNED;
-    s = check_ws(ws, ws_bytes, emu_route_balance_workspace_bytes(E));
+    s = check_optional_ws(ws, ws_bytes, emu_route_balance_workspace_bytes(T, E));
     if (s != EMU_OK) return s;
     return cuda_status(launch_balance(T, E, (int)k, logits, dtype == EMU_F32, ldl, experts, mask, coef, loss, counts, tokens,
-                                      static_cast<char *>(ws) + kWsHeaderBytes, &static_cast<WsHeader *>(ws)->flags,
+                                      ws ? static_cast<char *>(ws) + kWsHeaderBytes : nullptr,
+                                      ws ? &static_cast<WsHeader *>(ws)->flags : nullptr,
                                       reinterpret_cast<cudaStream_t>(stream)));
 }
 
@@ -489,8 +498,7 @@ emu_status emu_i8_quantize(int dtype, int64_t G, int64_t rows, int64_t cols, con
 
 size_t emu_i8_gemm_workspace_bytes(int64_t G, int64_t rows, int64_t N, int64_t K, int aligned)
 {
-    if (G < 1 || rows < 0 || N < 0 || K < 0) return 0;
-    if (rows == 0 || N == 0 || K == 0 || i8_few_rows(G, rows, N, K)) return kWsHeaderBytes;
+    if (G < 1 || rows <= 0 || N <= 0 || K <= 0 || i8_few_rows(G, rows, N, K)) return 0;
     return kWsHeaderBytes + i8_tile_scratch_bytes(G, rows, N, K, aligned != 0);
 }
 
@@ -512,17 +520,17 @@ emu_status emu_i8_gemm(int64_t G, int64_t rows, int64_t N, int64_t K, const int8
         if (!fits(Y, etype) || !fits(xscales, EMU_F32) || !fits(wscales, EMU_F32) || !fits(src, EMU_F32) || !fits(ends, EMU_F32))
             return EMU_ERR_MISALIGNED;
     }
-    s = check_ws(ws, ws_bytes, emu_i8_gemm_workspace_bytes(G, rows, N, K, i8_tma_reads(W, G, N, ldw, stridew)));
+    s = check_optional_ws(ws, ws_bytes, emu_i8_gemm_workspace_bytes(G, rows, N, K, i8_tma_reads(W, G, N, ldw, stridew)));
     if (s != EMU_OK) return s;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     if (rows == 0 || N == 0 || K == 0) {
-        if (clear_flags(ws, st) != cudaSuccess) return EMU_ERR_CUDA;
+        if (ws && clear_flags(ws, st) != cudaSuccess) return EMU_ERR_CUDA;
         return cuda_status(zero_rows(Y, rows, N, ldy, esize, st));
     }
     I8Product p = {};
     p.X = X; p.W = W; p.xscales = xscales; p.wscales = wscales; p.src = src; p.ends = ends; p.xrows = xrows; p.ldx = ldx;
     p.ldw = ldw; p.stridew = G > 1 ? stridew : 0; p.ldy = ldy; p.Y = Y; p.ytype = ytype; p.G = (int)G; p.rows = (int)rows;
-    p.N = (int)N; p.K = (int)K; p.flags = &static_cast<WsHeader *>(ws)->flags;
+    p.N = (int)N; p.K = (int)K; p.flags = ws ? &static_cast<WsHeader *>(ws)->flags : nullptr;
     return cuda_status(i8_few_rows(G, rows, N, K) ? launch_i8_rows(p, st)
                                             : launch_i8_tile(p, static_cast<char *>(ws) + kWsHeaderBytes, st));
 }

@@ -47,7 +47,7 @@ __global__ void __launch_bounds__(32 * kWarps, 2) i8_rows_kernel(const RowsArgs 
     const int warp = (int)threadIdx.x >> 5, lane = (int)lane_id();
     bool bad = false;
     if (p.ends) bad = load_groups(p.ends, p.G, p.rows, starts);
-    if (blockIdx.x == 0) {                            // the flag word is this kernel's alone: one CTA sets it
+    if (blockIdx.x == 0 && p.flags) {                 // the flag word is this kernel's alone: one CTA sets it
         if (p.src)
             for (int r = threadIdx.x; r < p.rows; r += 32 * kWarps) {
                 const int t = __ldg(p.src + r);

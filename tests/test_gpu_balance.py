@@ -49,12 +49,18 @@ def formula(z, experts, mask, coef):
     return (f * p.sum(0)).sum() / max(n, 1), counts, n, p, f
 
 
+def space(T, E, dev):
+    return emu.workspace(max(emu.emu_route_balance_workspace_bytes(T, E), emu.emu_split_workspace_bytes(32)), dev)
+
+
 def check(z, experts, mask, add, coef=0.01, dloss=None, flags=0):
     loss, counts, n, p, f = formula(z, experts, mask, coef)
     finite = z[z.isfinite()].double()
     R = float(finite.max() - finite.min()) if finite.numel() else 0.0
-    b, ws = emu.route_balance(z, experts, coef=coef, mask=mask)
+    ws = space(*z.shape, z.device)
+    b, _ = emu.route_balance(z, experts, coef=coef, mask=mask, ws=ws)
     assert emu.read_flags(ws) == flags
+    assert torch.equal(b.loss, emu.route_balance(z, experts, coef=coef, mask=mask)[0].loss)
     assert torch.equal(b.counts.long(), counts) and int(b.tokens) == n
     assert abs(float(b.loss) - float(loss)) <= (R + z.shape[0] / 32 + 300) * U * float(loss)
     scale = (1.0 if dloss is None else float(dloss)) / max(n, 1)
@@ -76,7 +82,7 @@ def check(z, experts, mask, add, coef=0.01, dloss=None, flags=0):
 
 
 SIZES = [(1, 1, 1), (1, 8, 2), (2, 4, 4), (5, 7, 3), (64, 64, 4), (100, 33, 5), (129, 60, 6), (1000, 128, 8), (700, 130, 2),
-         (333, 256, 8), (300, 500, 16), (200, 1024, 32), (65, 1023, 9), (5003, 60, 6), (20000, 16, 2), (3000, 512, 1)]
+         (333, 256, 8), (300, 500, 16), (200, 1024, 32), (65, 1023, 9), (4096, 128, 8), (4097, 128, 8), (2049, 200, 3), (600, 700, 4), (5003, 60, 6), (20000, 16, 2), (3000, 512, 1)]
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
@@ -124,14 +130,15 @@ def test_logits_that_are_not_finite(dev):
     z[7], z[6, 5] = nan, inf
     zc = z.clone()
     zc[6:8] = 0
-    a, ws = emu.route_balance(z, experts, mask=mask)
+    ws = space(*z.shape, dev)
+    a, _ = emu.route_balance(z, experts, mask=mask, ws=ws)
     assert emu.read_flags(ws) == 0
     c, _ = emu.route_balance(zc, experts, mask=mask)
     assert torch.equal(a.loss, c.loss)
     assert torch.equal(emu.route_balance_backward(z, a, mask=mask, add=add), emu.route_balance_backward(zc, c, mask=mask, add=add))
     # plus infinity in one that does: flagged, its own row alone is lost in the gradient
     z[7], z[6], z[9, 1] = 0, 0, inf
-    a, ws = emu.route_balance(z, experts)
+    a, _ = emu.route_balance(z, experts, ws=ws)
     assert emu.read_flags(ws) == emu.FLAG_NONFINITE
     d = emu.route_balance_backward(z, a)
     assert bool(d[9].isnan().any()) and bool(d[[i for i in range(50) if i != 9]].isfinite().all())

@@ -154,16 +154,25 @@ def scaled(S, xs, ws, ends=None, src=None):
     return Y
 
 
+def space(X, W, ends=None, src=None):
+    """A workspace that is enough for the call however W lies, or for its flags."""
+    rows, G = src.numel() if src is not None else X[0].shape[0], 1 if ends is None else len(ends)
+    need = emu.emu_i8_gemm_workspace_bytes(G, rows, W[0].shape[-2], W[0].shape[-1], 0)
+    return emu.workspace(max(need, emu.emu_split_workspace_bytes(32)), X[0].device)
+
+
 def check(X, W, ends=None, src=None, flags=0):
     e = None if ends is None else torch.tensor(ends, dtype=torch.int32, device=X[0].device)
     S = sums(X[0], W[0], ends, src)
-    Y, ws = emu.i8_gemm(X, W, ends=e, src=src, dtype=torch.int32)
+    ws = space(X, W, ends, src)
+    Y, _ = emu.i8_gemm(X, W, ends=e, src=src, dtype=torch.int32, ws=ws)
     assert emu.read_flags(ws) == flags
     assert torch.equal(Y.double(), S), float((Y.double() - S).abs().max())
     want = scaled(S, X[1], W[1], ends, src)
     for dtype, tol in ((torch.float32, F32_TOL), (torch.bfloat16, BF16_TOL)):
-        Y, ws = emu.i8_gemm(X, W, ends=e, src=src, dtype=dtype, ws=ws)
+        Y, _ = emu.i8_gemm(X, W, ends=e, src=src, dtype=dtype, ws=ws)
         assert emu.read_flags(ws) == flags and Y.dtype is dtype
+        assert torch.equal(Y, emu.i8_gemm(X, W, ends=e, src=src, dtype=dtype)[0])      # in a workspace of its own, or none
         assert bool(((Y.double() - want).abs() <= tol * want.abs()).all())
 
 
@@ -223,9 +232,10 @@ def test_no_rows_to_take_and_nothing_to_multiply(dev, rows):
     X, W = make(dev, 5, 40, 64)
     none = (X[0][:0], X[1][:0])
     src = torch.arange(rows, dtype=torch.int32, device=dev)
-    Y, ws = emu.i8_gemm(none, W, src=src, dtype=torch.float32)
+    ws = space(none, W, src=src)
+    Y, _ = emu.i8_gemm(none, W, src=src, dtype=torch.float32, ws=ws)
     assert emu.read_flags(ws) == emu.FLAG_INDEX and Y.shape == (rows, 40) and not Y.any()
-    Y, ws = emu.i8_gemm(none, W)
+    Y, _ = emu.i8_gemm(none, W, ws=ws)
     assert Y.shape == (0, 40) and emu.read_flags(ws) == 0
     Y, _ = emu.i8_gemm((X[0][:, :0], X[1]), (W[0][:, :0], W[1]))
     assert Y.shape == (5, 40) and not Y.any()
@@ -252,7 +262,8 @@ def test_past_two_to_the_31(dev):
         X = torch.empty(rows, K, dtype=torch.int8, device=dev).random_(-128, 128, generator=gen(dev, rows))
         xs = torch.rand(rows, device=dev)
         ends = torch.tensor([0, 0, 0, 0, rows], dtype=torch.int32, device=dev)
-        Y, ws = emu.i8_gemm((X, xs), (W, v), ends=ends, dtype=torch.int32)
+        ws = space((X, xs), (W, v), ends)
+        Y, _ = emu.i8_gemm((X, xs), (W, v), ends=ends, dtype=torch.int32, ws=ws)
         assert torch.equal(Y[:, some].double(), X.double() @ W[4][some].double().T) and emu.read_flags(ws) == 0
     del W
     # and an answer of 4.6 GB
@@ -285,7 +296,8 @@ def test_largest_sums(dev, rows):
     X = torch.full((rows, K), -128, dtype=torch.int8, device=dev)
     W = torch.full((130, K), -128, dtype=torch.int8, device=dev)
     W[1::2] = 127
-    Y, ws = emu.i8_gemm((X, None), (W, None), dtype=torch.int32)
+    ws = space((X, None), (W, None))
+    Y, _ = emu.i8_gemm((X, None), (W, None), dtype=torch.int32, ws=ws)
     assert emu.read_flags(ws) == 0
     assert bool((Y[:, 0::2] == 128 * 128 * K).all()) and bool((Y[:, 1::2] == -128 * 127 * K).all())
 
@@ -340,7 +352,8 @@ def test_other_streams_graphs_and_two_calls_at_once(dev, rows, N, K, G):
         assert torch.equal(y, want[i % 2])
     # captured and replayed, two graphs with one workspace, other inputs in the same place
     (x, xs), W = a
-    Y1, ws = emu.i8_gemm((x, xs), W, ends=ends)
+    ws = space((x, xs), W, ends)
+    Y1, _ = emu.i8_gemm((x, xs), W, ends=ends, ws=ws)
     Y2 = torch.empty_like(Y1)
     graphs = []
     torch.cuda.synchronize()

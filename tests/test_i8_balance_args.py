@@ -51,20 +51,21 @@ def test_product_checks(lib):
     assert g(1, 4, 8, 16, P, 4, 16, P + 2, None, P, 16, 0, P, None, P, 0, 8, P, BIG, None) == 2
     assert g(1, 4, 8, 16, P, 4, 16, P, P + 1, P, 16, 0, P, None, P, 0, 8, P, BIG, None) == 2
     assert g(1, 4, 8, 16, P, 4, 16, P, None, P, 16, 0, P, None, P + 2, 0, 8, P, BIG, None) == 2
-    assert g(1, 4, 8, 16, P, 4, 16, P, None, P, 16, 0, P, None, P, 0, 8, None, 0, None) == 1
-    assert g(1, 4, 8, 16, P, 4, 16, P, None, P, 16, 0, P, None, P, 0, 8, P, 511, None) == 3
+    assert g(1, 40, 8, 16, P, 40, 16, P, None, P, 16, 0, P, None, P, 0, 8, None, 0, None) == 1    # more than a few rows
+    assert g(1, 40, 8, 16, P, 40, 16, P, None, P, 16, 0, P, None, P, 0, 8, P, 512, None) == 3
+    assert g(1, 4, 8, 16, P, 4, 16, P, None, P, 16, 0, P, None, P, 0, 8, P, 511, None) == 3       # a few: for the flags
     assert g(1, 4, 8, 16, P, 4, 16, P, None, P, 16, 0, P, None, P, 0, 8, P + 8, BIG, None) == 2
     assert g(1, 4, 8, 131072, P, 4, 131072, P, None, P, 131072, 0, P, None, P, 0, 8, P, BIG, None) == 5    # sums past 32 bits
     assert g(1025, 4, 8, 16, P, 4, 16, P, None, P, 16, 128, P, P, P, 0, 8, P, BIG, None) == 5
     assert g(1, 1 << 31, 8, 16, P, 1 << 31, 16, P, None, P, 16, 0, P, None, P, 0, 8, P, BIG, None) == 5
     assert emu.emu_i8_gemm_workspace_bytes(0, 4, 8, 16, 1) == 0
-    assert emu.emu_i8_gemm_workspace_bytes(2, 1, 8, 16, 1) >= 512
+    assert emu.emu_i8_gemm_workspace_bytes(2, 1, 8, 16, 1) == 0 and emu.emu_i8_gemm_workspace_bytes(2, 100, 8, 16, 1) >= 512
 
 
 def test_balance_checks(lib):
     b, d = emu.emu_route_balance, emu.emu_route_balance_backward
-    need = emu.emu_route_balance_workspace_bytes(8)
-    assert emu.emu_route_balance_workspace_bytes(0) == 0
+    need = emu.emu_route_balance_workspace_bytes(1 << 20, 8)
+    assert emu.emu_route_balance_workspace_bytes(4, 0) == 0 and emu.emu_route_balance_workspace_bytes(4, 8) == 0 and need > 512
     #        dt T  E  k  z  ldl ex mask coef loss counts tokens ws bytes stream
     assert b(2, 4, 8, 2, P, 8, P, None, 1.0, P, P, P, P, need, None) == 1
     assert b(0, 4, 8, 9, P, 8, P, None, 1.0, P, P, P, P, need, None) == 1        # k > E
@@ -76,7 +77,10 @@ def test_balance_checks(lib):
     assert b(0, 4, 8, 2, P, 8, P, None, 1.0, P, P, None, P, need, None) == 1
     assert b(0, 4, 8, 2, P + 2, 8, P, None, 1.0, P, P, P, P, need, None) == 2
     assert b(0, 4, 8, 2, P, 8, P, None, 1.0, P, P + 2, P, P, need, None) == 2
-    assert b(0, 4, 8, 2, P, 8, P, None, 1.0, P, P, P, P, need - 1, None) == 3
+    assert b(0, 1 << 20, 8, 2, P, 8, P, None, 1.0, P, P, P, P, need - 1, None) == 3
+    assert b(0, 1 << 20, 8, 2, P, 8, P, None, 1.0, P, P, P, None, 0, None) == 1
+    assert b(0, 4, 8, 2, P, 8, P, None, 1.0, P, P, P, P, 511, None) == 3
+    assert b(0, 4, 8, 2, P, 8, P, None, 1.0, P, P, P, P + 8, need, None) == 2
     assert b(0, 4, 2000, 2, P, 2000, P, None, 1.0, P, P, P, P, BIG, None) == 5
     assert b(0, 4, 64, 33, P, 64, P, None, 1.0, P, P, P, P, BIG, None) == 5
     assert b(0, 1 << 30, 8, 2, P, 8, P, None, 1.0, P, P, P, P, need, None) == 5
