@@ -986,7 +986,8 @@ def i8_gemm(X, W, ends=None, src=None, Y=None, dtype=None, ws=None, stream=None)
         pw = _float_pairs(wscales, shape[:-1], dev, "i8_gemm: scales of W")
     pc = w.data_ptr()
     if ws is None:
-        need = _lib.emu_i8_gemm_workspace_bytes(G, rows, N, K, (pc | ldw | stride) % 16 == 0 and (G <= 1 or stride >= N * ldw))
+        whole = (pc | ldw | stride | x.data_ptr() | ldx) % 16 == 0 and (G <= 1 or stride >= N * ldw)
+        need = _lib.emu_i8_gemm_workspace_bytes(G, rows, N, K, whole)
         if need:
             ws = _empty(need, torch.uint8, dev, stream)
     r = _lib.emu_i8_gemm(G, rows, N, K, x.data_ptr(), xrows, ldx, px, ps, pc, ldw, stride, pw, pe, Y.data_ptr(), yt, ldy or 1,

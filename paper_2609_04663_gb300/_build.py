@@ -18,7 +18,7 @@ INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 SO = os.path.join(HERE, "_emu.so")
 SOURCES = ["emu_api.cu", "split_f32.cu", "split_f64.cu", "split_fix.cu", "split_rc.cu", "prodsum_f32.cu", "gemm_f32_fused.cu", "prodsum_f64.cu", "prodsum_f64w.cu", "prodsum_tail.cu", "noalloc.cu", "host_api.cu", "epilogue.cu",
            "grouped.cu", "grouped_split.cu", "grouped_api.cu", "grouped_fused.cu", "grouped_bf16.cu", "w4.cu", "route.cu",
-           "balance.cu", "i8_quantize.cu", "i8_rows.cu", "i8_tile.cu"]
+           "balance.cu", "i8_quantize.cu", "i8_rows.cu", "i8_tile.cu", "i8_batch.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-ftz=false", "-prec-div=true",
          "-prec-sqrt=true", "-fmad=true"]

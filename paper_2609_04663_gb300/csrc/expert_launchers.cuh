@@ -84,8 +84,11 @@ struct I8Product {
 };
 cudaError_t launch_i8_rows(const I8Product &p, cudaStream_t st);
 bool i8_few_rows(int64_t G, int64_t rows, int64_t N, int64_t K);      // launch_i8_rows is the faster way
-// On the tensor cores; scratch: i8_tile_scratch_bytes (aligned: W's rows can be read 16 bytes at a time).
+// On the tensor cores, many rows (i8_tile.cu), or some in one launch with K in `parts` (i8_batch.cu); scratch: the
+// bytes below (aligned: X's and W's rows can be read 16 bytes at a time).
 size_t i8_tile_scratch_bytes(int64_t G, int64_t rows, int64_t N, int64_t K, bool aligned);
 cudaError_t launch_i8_tile(I8Product p, void *scratch, cudaStream_t st);
+size_t i8_batch_scratch_bytes(int64_t G, int64_t rows, int64_t N, int64_t K, bool aligned);
+cudaError_t launch_i8_batch(I8Product p, int parts, void *scratch, cudaStream_t st);
 
 }  // namespace emu

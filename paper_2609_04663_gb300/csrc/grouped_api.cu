@@ -126,6 +126,21 @@ emu_status check_balance(int dtype, int64_t T, int64_t E, int64_t k, const void 
 
 constexpr int64_t kMaxI8K = 131071;      // 128 * 128 * K stays below 2^31
 
+// Which tensor-core kernel multiplies: 0, pairs of SMs with 256 columns (i8_tile.cu); else 64 columns on one
+// (i8_batch.cu), in so many parts of K while SMs are free.  By waves times the nanoseconds of 64 codes (measured,
+// weights from HBM: a pair's 280 up to 128 columns and 390 up to 256, one SM's 240 up to 16, 265 below 32 and 310 up to 64).
+// 32 experts of 2048 x 4096: 1024 rows 72 us on single SMs and 66 on pairs, 128 rows 56 and 63; 256 rows x 4096 x 4096 20
+// and 31.
+int i8_batch_parts(int64_t G, int64_t rows, int64_t N, int64_t K)
+{
+    auto waves = [](int64_t tiles, int64_t units) { return (tiles + units - 1) / units; };
+    const int64_t sms = 152, n = (rows + G - 1) / G, tiles = G * ((n + 63) / 64) * ((N + 127) / 128);
+    int parts = 1;
+    while (parts < 8 && 2 * parts * tiles <= sms && K >= 1024 * parts) parts *= 2;
+    const int64_t pairs = waves(G * ((n + 255) / 256) * ((N + 255) / 256), sms / 2) * (n <= 128 ? 280 : 390);
+    return pairs * parts < waves(tiles, sms) * (n <= 16 ? 240 : n < 32 ? 265 : 310) ? 0 : parts;
+}
+
 }  // namespace
 
 extern "C" {
@@ -499,7 +514,9 @@ emu_status emu_i8_quantize(int dtype, int64_t G, int64_t rows, int64_t cols, con
 size_t emu_i8_gemm_workspace_bytes(int64_t G, int64_t rows, int64_t N, int64_t K, int aligned)
 {
     if (G < 1 || rows <= 0 || N <= 0 || K <= 0 || i8_few_rows(G, rows, N, K)) return 0;
-    return kWsHeaderBytes + i8_tile_scratch_bytes(G, rows, N, K, aligned != 0);
+    const size_t scratch = i8_batch_parts(G, rows, N, K) ? i8_batch_scratch_bytes(G, rows, N, K, aligned != 0)
+                                                         : i8_tile_scratch_bytes(G, rows, N, K, aligned != 0);
+    return scratch ? kWsHeaderBytes + scratch : 0;
 }
 
 emu_status emu_i8_gemm(int64_t G, int64_t rows, int64_t N, int64_t K, const int8_t *X, int64_t xrows, int64_t ldx,
@@ -520,7 +537,8 @@ emu_status emu_i8_gemm(int64_t G, int64_t rows, int64_t N, int64_t K, const int8
         if (!fits(Y, etype) || !fits(xscales, EMU_F32) || !fits(wscales, EMU_F32) || !fits(src, EMU_F32) || !fits(ends, EMU_F32))
             return EMU_ERR_MISALIGNED;
     }
-    s = check_optional_ws(ws, ws_bytes, emu_i8_gemm_workspace_bytes(G, rows, N, K, i8_tma_reads(W, G, N, ldw, stridew)));
+    s = check_optional_ws(ws, ws_bytes, emu_i8_gemm_workspace_bytes(
+                                             G, rows, N, K, i8_tma_reads(W, G, N, ldw, stridew) && aligned_codes(X, xrows > 1 ? ldx : 0, 0)));
     if (s != EMU_OK) return s;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     if (rows == 0 || N == 0 || K == 0) {
@@ -531,8 +549,10 @@ emu_status emu_i8_gemm(int64_t G, int64_t rows, int64_t N, int64_t K, const int8
     p.X = X; p.W = W; p.xscales = xscales; p.wscales = wscales; p.src = src; p.ends = ends; p.xrows = xrows; p.ldx = ldx;
     p.ldw = ldw; p.stridew = G > 1 ? stridew : 0; p.ldy = ldy; p.Y = Y; p.ytype = ytype; p.G = (int)G; p.rows = (int)rows;
     p.N = (int)N; p.K = (int)K; p.flags = ws ? &static_cast<WsHeader *>(ws)->flags : nullptr;
-    return cuda_status(i8_few_rows(G, rows, N, K) ? launch_i8_rows(p, st)
-                                            : launch_i8_tile(p, static_cast<char *>(ws) + kWsHeaderBytes, st));
+    if (i8_few_rows(G, rows, N, K)) return cuda_status(launch_i8_rows(p, st));
+    void *scratch = ws ? static_cast<char *>(ws) + kWsHeaderBytes : nullptr;
+    const int parts = i8_batch_parts(G, rows, N, K);
+    return cuda_status(parts ? launch_i8_batch(p, parts, scratch, st) : launch_i8_tile(p, scratch, st));
 }
 
 }  // extern "C"

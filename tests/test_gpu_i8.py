@@ -381,7 +381,7 @@ def test_quantise_multiply_twice(dev):
     ends = torch.tensor([10, 10, 33, 40], dtype=torch.int32, device=dev)
     src = torch.randperm(40, generator=g, device=dev).int()
     q1, q2 = emu.i8_quantize(W1), emu.i8_quantize(W2)
-    ws = emu.workspace(max(emu.emu_i8_gemm_workspace_bytes(4, 40, 512, 256, 1), emu.emu_i8_gemm_workspace_bytes(4, 40, 256, 512, 1)), dev)
+    ws = emu.workspace(max(emu.emu_i8_gemm_workspace_bytes(4, 40, 512, 256, 0), emu.emu_i8_gemm_workspace_bytes(4, 40, 256, 512, 0)), dev)
     h, _ = emu.i8_gemm(emu.i8_quantize(x), q1, ends=ends, src=src, ws=ws)
     y, _ = emu.i8_gemm(emu.i8_quantize(h), q2, ends=ends, ws=ws)
     # (the sums as integers first: those of scaled codes would leave 2^-53 of their terms where the sum is 0)

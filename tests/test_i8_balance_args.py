@@ -51,15 +51,18 @@ def test_product_checks(lib):
     assert g(1, 4, 8, 16, P, 4, 16, P + 2, None, P, 16, 0, P, None, P, 0, 8, P, BIG, None) == 2
     assert g(1, 4, 8, 16, P, 4, 16, P, P + 1, P, 16, 0, P, None, P, 0, 8, P, BIG, None) == 2
     assert g(1, 4, 8, 16, P, 4, 16, P, None, P, 16, 0, P, None, P + 2, 0, 8, P, BIG, None) == 2
-    assert g(1, 40, 8, 16, P, 40, 16, P, None, P, 16, 0, P, None, P, 0, 8, None, 0, None) == 1    # more than a few rows
-    assert g(1, 40, 8, 16, P, 40, 16, P, None, P, 16, 0, P, None, P, 0, 8, P, 512, None) == 3
+    assert g(1, 40, 8, 16, P, 40, 16, P, None, P + 8, 16, 0, P, None, P, 0, 8, None, 0, None) == 1    # weights are copied
+    assert g(1, 40, 8, 16, P, 40, 16, P, None, P + 8, 16, 0, P, None, P, 0, 8, P, 512, None) == 3
+    assert g(1, 40, 8, 16, P + 8, 40, 16, P, None, P, 16, 0, P, None, P, 0, 8, None, 0, None) == 1    # rows are copied
+    assert g(1, 4000, 4000, 16, P, 4000, 16, P, None, P, 16, 0, P, None, P, 0, 4000, None, 0, None) == 1    # rows as FP16
     assert g(1, 4, 8, 16, P, 4, 16, P, None, P, 16, 0, P, None, P, 0, 8, P, 511, None) == 3       # a few: for the flags
     assert g(1, 4, 8, 16, P, 4, 16, P, None, P, 16, 0, P, None, P, 0, 8, P + 8, BIG, None) == 2
     assert g(1, 4, 8, 131072, P, 4, 131072, P, None, P, 131072, 0, P, None, P, 0, 8, P, BIG, None) == 5    # sums past 32 bits
     assert g(1025, 4, 8, 16, P, 4, 16, P, None, P, 16, 128, P, P, P, 0, 8, P, BIG, None) == 5
     assert g(1, 1 << 31, 8, 16, P, 1 << 31, 16, P, None, P, 16, 0, P, None, P, 0, 8, P, BIG, None) == 5
     assert emu.emu_i8_gemm_workspace_bytes(0, 4, 8, 16, 1) == 0
-    assert emu.emu_i8_gemm_workspace_bytes(2, 1, 8, 16, 1) == 0 and emu.emu_i8_gemm_workspace_bytes(2, 100, 8, 16, 1) >= 512
+    assert emu.emu_i8_gemm_workspace_bytes(2, 1, 8, 16, 1) == 0 and emu.emu_i8_gemm_workspace_bytes(2, 100, 8, 16, 0) >= 512
+    assert emu.emu_i8_gemm_workspace_bytes(2, 100, 8, 16, 1) == 0 and emu.emu_i8_gemm_workspace_bytes(1, 4000, 4000, 16, 1) >= 512
 
 
 def test_balance_checks(lib):
