@@ -100,16 +100,17 @@ __device__ __forceinline__ void half_block(const uint4 &u, const uint4 &v, uint3
 
 
 // A converting warp's part of a stage: 64 codes of its lane's feature in shared memory at `from`
-// -> FP16 in tensor memory at `to`.  Between reading and writing, `wait` waits until the MMAs have used
-// what was there; false when it gave up.
+// -> FP16 in tensor memory at `to`.  In between, `wait` waits until the MMAs have used what was there; false
+// when it gave up.  was_read gives the stage of bytes back to TMA: after the stores to tensor
+// memory, which cannot be issued before all that was loaded has arrived.  (Right after the loads it came too
+// early: an arrival does not wait for them, and where a box lies past the end of the rows TMA writes its zeros at
+// once.  Last codes of a stage came out as zero in one of a hundred products of 1030 rows x 2064 x 700.)
 template <typename Read, typename Wait>
 __device__ __forceinline__ bool convert_weights(uint32_t from, int first, int row, uint32_t to, bool there, Read &&was_read, Wait &&wait)
 {
     uint4 w[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) w[j] = lds_u4(from + (uint32_t)(((first + j) ^ (row & 7)) << 4));
-    __syncwarp();
-    was_read();
     uint32_t f[16];
     half_block(w[0], w[1], f);
     if (!wait()) return false;
@@ -118,7 +119,10 @@ __device__ __forceinline__ bool convert_weights(uint32_t from, int first, int ro
         tmem_store16(to, f);
         half_block(w[2], w[3], f);
         tmem_store16(to + 16u, f);
+        was_read();
         tmem_st_wait();
+    } else {
+        was_read();                                   // (what was loaded is not used)
     }
     tc_fence_before();
     __syncwarp();

@@ -282,6 +282,17 @@ def test_quantise_past_two_to_the_31(dev):
     assert torch.equal(q.codes[at], codes) and torch.equal(q.scales[at], scales)
 
 
+@pytest.mark.parametrize("rows,N,K", [(1030, 700, 2064), (4000, 1000, 1040), (20, 4096, 5136), (6, 900, 2064)])
+def test_the_same_sums_every_time(dev, rows, N, K):
+    # a stage's last bytes must not be given up before they are read: K that ends inside of one, many times
+    X, W = make(dev, rows, N, K)
+    S = sums(X[0], W[0]).int()
+    off = torch.zeros((), dtype=torch.int64, device=dev)
+    for _ in range(500):
+        off += (emu.i8_gemm(X, W, dtype=torch.int32)[0] != S).sum()
+    assert int(off) == 0
+
+
 def test_many_groups(dev):
     rng = np.random.default_rng(0)
     for per in (1, 40):
