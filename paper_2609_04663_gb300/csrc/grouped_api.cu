@@ -2,6 +2,7 @@
 // argument checks, workspace layout and launch sequences.
 #include "grouped_common.cuh"
 #include "expert_launchers.cuh"
+#include <algorithm>
 #include "i8_common.cuh"
 
 using namespace emu;
@@ -127,18 +128,21 @@ emu_status check_balance(int dtype, int64_t T, int64_t E, int64_t k, const void 
 constexpr int64_t kMaxI8K = 131071;      // 128 * 128 * K stays below 2^31
 
 // Which tensor-core kernel multiplies: 0, pairs of SMs with 256 columns (i8_tile.cu); else 64 columns on one
-// (i8_batch.cu), in so many parts of K while SMs are free.  By waves times the nanoseconds of 64 codes (measured,
-// weights from HBM: a pair's 280 up to 128 columns and 390 up to 256, one SM's 240 up to 16, 265 below 32 and 310 up to 64).
-// 32 experts of 2048 x 4096: 1024 rows 72 us on single SMs and 66 on pairs, 128 rows 56 and 63; 256 rows x 4096 x 4096 20
-// and 31.
+// (i8_batch.cu), in so many parts of K while SMs are free.  By times in ns as they were measured: what a launch takes
+// besides, waves of tiles, and in each 64 codes at a time, but no less than a tile's start and end.
+// 32 experts of 2048 x 4096: 1024 rows 70 us on single SMs and 62 on pairs, 128 rows 56 and 59; 256 rows x 4096 x 4096 20
+// and 29; 16 rows x 16384 x 16384 66 and 60; 64 rows x 512 x 4096 7.2 and 8.9.
+// Parts cost some 2 us: 16 rows x 1024 x 4096 7.4 us in one and 8.4 in two, 64 rows x 2048 x 4096 13 in one and 11.6 in four.
 int i8_batch_parts(int64_t G, int64_t rows, int64_t N, int64_t K)
 {
     auto waves = [](int64_t tiles, int64_t units) { return (tiles + units - 1) / units; };
-    const int64_t sms = 152, n = (rows + G - 1) / G, tiles = G * ((n + 63) / 64) * ((N + 127) / 128);
+    const int64_t sms = 152, n = (rows + G - 1) / G, tiles = G * ((n + 63) / 64) * ((N + 127) / 128), steps = (K + 63) / 64;
     int parts = 1;
-    while (parts < 8 && 2 * parts * tiles <= sms && K >= 1024 * parts) parts *= 2;
-    const int64_t pairs = waves(G * ((n + 255) / 256) * ((N + 255) / 256), sms / 2) * (n <= 128 ? 280 : 390);
-    return pairs * parts < waves(tiles, sms) * (n <= 16 ? 240 : n < 32 ? 265 : 310) ? 0 : parts;
+    while (parts < 8 && 2 * parts * tiles <= sms && K >= 1024 * std::max(parts, 2)) parts *= 2;
+    const int64_t pair = std::max<int64_t>(steps * (n <= 128 ? 222 : 330), 3000);
+    const int64_t single = std::max<int64_t>(steps * (n <= 16 ? 235 : n < 32 ? 253 : 288) / parts, 2800);
+    return 6500 + waves(G * ((n + 255) / 256) * ((N + 255) / 256), sms / 2) * pair <
+                   (parts > 1 ? 7000 : 3500) + waves(tiles, sms) * single ? 0 : parts;
 }
 
 }  // namespace

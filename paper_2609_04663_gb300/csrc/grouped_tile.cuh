@@ -213,29 +213,29 @@ __device__ __forceinline__ float as_float(uint32_t x) { return __uint_as_float(x
 // of one row.  The usual case (32 whole columns, 32 features, pairs that can be
 // stored as words) has no test per element: these instructions, not the
 // stores' bandwidth, are what the epilogue takes.
-template <typename T>
-__device__ __forceinline__ void store_columns(const T (&v)[32], int cols, void *out, int64_t ldo, int l, int L,
+template <typename T, int C>
+__device__ __forceinline__ void store_columns(const T (&v)[C], int cols, void *out, int64_t ldo, int l, int L,
                                               bool out_f32, bool pairs_ok)
 {
     const int lane = (int)lane_id();
-    const bool whole = cols >= 32 && l + 32 <= L;
+    const bool whole = cols >= C && l + 32 <= L;
     if (out_f32) {
         float *o = static_cast<float *>(out) + l + lane;
         if (whole) {
 #pragma unroll
-            for (int j = 0; j < 32; ++j, o += ldo) *o = as_float(v[j]);
+            for (int j = 0; j < C; ++j, o += ldo) *o = as_float(v[j]);
         } else {
 #pragma unroll
-            for (int j = 0; j < 32; ++j)
+            for (int j = 0; j < C; ++j)
                 if (l + lane < L && j < cols) o[(int64_t)j * ldo] = as_float(v[j]);
         }
     } else {
         const bool odd = lane & 1;
         const int i = lane & ~1;
         uint16_t *o = static_cast<uint16_t *>(out) + (odd ? ldo : 0) + l + i;
-        uint32_t w[16];                               // features i (low half) and i + 1 of row 2 j + odd
+        uint32_t w[C / 2];                              // features i (low half) and i + 1 of row 2 j + odd
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
+        for (int j = 0; j < C / 2; ++j) {
             const float keep = as_float(odd ? v[2 * j + 1] : v[2 * j]);
             const float got = __shfl_xor_sync(0xFFFFFFFFu, as_float(odd ? v[2 * j] : v[2 * j + 1]), 1);
             asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[j]) : "f"(odd ? keep : got), "f"(odd ? got : keep));
@@ -244,10 +244,10 @@ __device__ __forceinline__ void store_columns(const T (&v)[32], int cols, void *
             char *p = reinterpret_cast<char *>(o);
             const int64_t two = 4 * ldo;
 #pragma unroll
-            for (int j = 0; j < 16; ++j, p += two) *reinterpret_cast<uint32_t *>(p) = w[j];
+            for (int j = 0; j < C / 2; ++j, p += two) *reinterpret_cast<uint32_t *>(p) = w[j];
         } else {
 #pragma unroll
-            for (int j = 0; j < 16; ++j) {
+            for (int j = 0; j < C / 2; ++j) {
                 if (2 * j + (odd ? 1 : 0) >= cols) continue;
                 uint16_t *p = o + (int64_t)(2 * j) * ldo;
                 if (l + i < L) p[0] = (uint16_t)w[j];

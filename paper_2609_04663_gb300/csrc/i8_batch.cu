@@ -7,10 +7,14 @@
 // thread's loads in flight: those were asked for three stages before.)  Warps 12-19 convert weights, 20 brings
 // them by TMA and looks for bad indexes, 21 issues the MMAs.
 //
-// While there are SMs left, K is split between the CTAs of a cluster; the first one reads the
-// others' sums from their shared memory.
+// While there are SMs left, K is split between the CTAs of a cluster; each adds and stores a share of the columns,
+// whose other sums it reads from their shared memory.
 //
-// (figures)
+// 48 rows x 5120 x 8192 take 20.4 us (HBM alone would 6.5), 64 x 4096 x 4096 13.2, 256 rows over 32 experts of
+// 2048 x 4096 58 (4.7 TB/s): bound by a stage's way through the warps, 235-290 ns for 64 codes, and by start and end
+// of the launch, 4 us, with parts 6.  Tried: all eight row warps on each stage instead of two groups in turn, with the bytes
+// brought to L1 ahead, 64 us for the 256 rows, with loads behind the fence 72; the first CTA of a cluster adding and storing
+// all columns 16 us for the 64 rows.
 #include "i8_tile.cuh"
 
 namespace emu {
@@ -85,6 +89,8 @@ __device__ __forceinline__ void arrive_cluster(uint32_t bar, int rank)
 {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(peer_addr(bar, (uint32_t)rank)) : "memory");
 }
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ void fence_cluster() { asm volatile("fence.acq_rel.cluster;" ::: "memory"); }
 
 __global__ void __launch_bounds__(BatchCfg::THREADS, 1)
@@ -114,7 +120,7 @@ i8_batch_kernel(const __grid_constant__ CUtensorMap tmW, const BatchArgs a)
         }
         for (int s = 0; s < Cfg::NW; ++s) { mbar_init(wfull0 + 8u * s, 1); mbar_init(wempty0 + 8u * s, kConvertWarps); }
         for (int s = 0; s < Cfg::SLOTS; ++s) { mbar_init(tfull0 + 8u * s, 1); mbar_init(tempty0 + 8u * s, kReadWarps); }
-        for (int w = 0; w < kReadWarps; ++w) { mbar_init(sfull0 + 8u * w, a.parts > 1 ? (uint32_t)a.parts - 1u : 1u); mbar_init(sempty0 + 8u * w, 1); }
+        for (int w = 0; w < kReadWarps; ++w) { mbar_init(sfull0 + 8u * w, a.parts > 1 ? (uint32_t)a.parts - 1u : 1u); mbar_init(sempty0 + 8u * w, a.parts > 1 ? (uint32_t)a.parts - 1u : 1u); }
         mbar_init(done_bar, 1);
         fence_mbar_init();
         tma_prefetch_desc(&tmW);
@@ -133,7 +139,7 @@ i8_batch_kernel(const __grid_constant__ CUtensorMap tmW, const BatchArgs a)
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (a.parts > 1) cluster_sync();                  // the other CTAs' barriers are initialised
+    if (a.parts > 1) cluster_arrive();                // this CTA's barriers are initialised
     const int total = uniform(tpre[a.p.G]);
     const uint32_t tmem = (uint32_t)uniform((int)*tmem_slot);
     const int first = (int)blockIdx.x >> a.shift, step = (int)gridDim.x >> a.shift;
@@ -148,6 +154,7 @@ i8_batch_kernel(const __grid_constant__ CUtensorMap tmW, const BatchArgs a)
         const bool pairs_ok = (a.p.ldy & 1) == 0 && (reinterpret_cast<uintptr_t>(a.p.Y) & 3u) == 0;
         for (int64_t r = (int64_t)starts[a.p.G] + blockIdx.x; r < a.p.rows; r += gridDim.x)      // rows of no group are zero
             for (int l = (int)threadIdx.x; l < a.p.N; l += 32 * kReadWarps) store_value(a.p, r, l, 0.0f, 0);
+        if (a.parts > 1) cluster_wait();              // the other CTAs' barriers are initialised
         uint32_t u = 0, par = 0;                      // accumulator; parity of the tiles before
         bool ok = true;
         for (int t = first; t < total && ok; t += step, par ^= 1u) {
@@ -156,15 +163,13 @@ i8_batch_kernel(const __grid_constant__ CUtensorMap tmW, const BatchArgs a)
             const int64_t row0 = (int64_t)starts[x.g] + x.c0;
             // scales, while the products are under way (a row without a source has zero sums)
             float ws = 1.0f, xs[2] = {};
-            if (rank == 0) {
-                if (a.p.wscales && l + lane < a.p.N) ws = __ldg(a.p.wscales + (int64_t)x.g * a.p.N + l + lane);
+            if (a.p.wscales && l + lane < a.p.N) ws = __ldg(a.p.wscales + (int64_t)x.g * a.p.N + l + lane);
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
-                    if (32 * h + lane < x.cols) {
-                        const int64_t from = a.p.src ? __ldg(a.p.src + row0 + 32 * h + lane) : row0 + 32 * h + lane;
-                        if (from >= 0 && from < a.p.xrows) xs[h] = a.p.xscales ? __ldg(a.p.xscales + from) : 1.0f;
-                    }
-            }
+            for (int h = 0; h < 2; ++h)
+                if (32 * h + lane < x.cols) {
+                    const int64_t from = a.p.src ? __ldg(a.p.src + row0 + 32 * h + lane) : row0 + 32 * h + lane;
+                    if (from >= 0 && from < a.p.xrows) xs[h] = a.p.xscales ? __ldg(a.p.xscales + from) : 1.0f;
+                }
             int acc[Cfg::COLS];
 #pragma unroll
             for (int j = 0; j < Cfg::COLS; ++j) acc[j] = 0;
@@ -188,34 +193,42 @@ i8_batch_kernel(const __grid_constant__ CUtensorMap tmW, const BatchArgs a)
             }
             if (!ok) break;
             if (a.parts > 1) {
+                // sums of this part of K to shared memory; then each CTA of the cluster adds and stores a share of
+                // the columns, in blocks of eight
                 const uint32_t mine = base + (uint32_t)(Cfg::SUM_OFF + warp * Cfg::COLS * 128 + lane * 4);
-                if (rank != 0) {
-                    if (!(ok = warp_wait(sempty0 + 8u * warp, par ^ 1u, flags))) break;
+                if (!(ok = warp_wait(sempty0 + 8u * warp, par ^ 1u, flags))) break;
 #pragma unroll
-                    for (int j = 0; j < Cfg::COLS; ++j)
-                        if (j < x.cols) asm volatile("st.shared.b32 [%0], %1;" ::"r"(mine + (uint32_t)(j * 128)), "r"(acc[j]) : "memory");
-                    __syncwarp();
-                    if (lane == 0) arrive_cluster(sfull0 + 8u * warp, 0);
-                    continue;
-                }
+                for (int j = 0; j < Cfg::COLS; ++j)
+                    if (j < x.cols) asm volatile("st.shared.b32 [%0], %1;" ::"r"(mine + (uint32_t)(j * 128)), "r"(acc[j]) : "memory");
+                __syncwarp();
+                if (lane < a.parts && lane != rank) arrive_cluster(sfull0 + 8u * warp, lane);
                 if (!(ok = warp_wait(sfull0 + 8u * warp, par, flags))) break;
                 fence_cluster();
-                for (int r = 1; r < a.parts; ++r) {
-                    const uint32_t from = peer_addr(mine, (uint32_t)r);
+                for (int c = 8 * rank; c < x.cols; c += 8 * a.parts) {
+                    const uint32_t at = mine + (uint32_t)(c * 128);
+                    int sum[8];                       // (columns past the tile's hold anything, and are not stored)
 #pragma unroll
-                    for (int q = 0; q < Cfg::COLS; q += 16) {
-                        if (q < x.cols) {             // (columns past the tile's hold anything, and are not stored)
-                            uint32_t v[16];
+                    for (int j = 0; j < 8; ++j) sum[j] = 0;
+#pragma unroll 2
+                    for (int r = 0; r < a.parts; ++r) {
+                        const uint32_t from = peer_addr(at, (uint32_t)(rank ^ r));
+                        uint32_t v[8];
 #pragma unroll
-                            for (int j = 0; j < 16; ++j) v[j] = ld_cluster(from + (uint32_t)((q + j) * 128));
+                        for (int j = 0; j < 8; ++j) v[j] = ld_cluster(from + (uint32_t)(j * 128));
 #pragma unroll
-                            for (int j = 0; j < 16; ++j) acc[q + j] += (int)v[j];
-                        }
+                        for (int j = 0; j < 8; ++j) sum[j] += (int)v[j];
                     }
+                    float v[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        v[j] = a.p.ytype == EMU_I32 ? __int_as_float(sum[j])
+                                                    : scaled_sum(sum[j], ws, __shfl_sync(0xFFFFFFFFu, c < 32 ? xs[0] : xs[1], (c & 31) + j));
+                    if (l < a.p.N)
+                        store_columns(v, x.cols - c, static_cast<char *>(a.p.Y) + (row0 + c) * a.p.ldy * esize, a.p.ldy, l, a.p.N, f32, pairs_ok);
                 }
                 __syncwarp();
-                if (lane == 0)
-                    for (int r = 1; r < a.parts; ++r) arrive_cluster(sempty0 + 8u * warp, r);
+                if (lane < a.parts && lane != rank) arrive_cluster(sempty0 + 8u * warp, lane);
+                continue;
             }
             if (l >= a.p.N) continue;
 #pragma unroll
@@ -419,7 +432,8 @@ i8_batch_kernel(const __grid_constant__ CUtensorMap tmW, const BatchArgs a)
     __syncwarp();
     tc_fence_before();
     __syncthreads();
-    if (a.parts > 1) cluster_sync();                  // the first CTA has read the others' sums
+    if (a.parts > 1 && warp >= kReadWarps) cluster_wait();
+    if (a.parts > 1) cluster_sync();                  // the others have read this CTA's sums
     if (warp == Cfg::MMA) {
         __syncwarp();
         tc_fence_after();

