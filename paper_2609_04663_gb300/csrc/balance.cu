@@ -124,6 +124,11 @@ __device__ __forceinline__ float softmax_parts(float (&x)[V], bool &odd)
 #pragma unroll
     for (int d = L / 2; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
     const bool some = top > -INFINITY;
+    if (some && fabsf(top) > 1e38f) {                 // (a mask of the type's lowest value in a whole row: top log2 e would overflow)
+#pragma unroll
+        for (int i = 0; i < V; ++i) x[i] -= top;
+        top = 0.0f;
+    }
     constexpr float log2e = 1.4426950408889634f;
     const float c = some ? top * log2e : 0.0f;
     float total = 0.0f;

@@ -144,6 +144,26 @@ def test_logits_that_are_not_finite(dev):
     assert bool(d[9].isnan().any()) and bool(d[[i for i in range(50) if i != 9]].isfinite().all())
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_logits_of_the_largest_magnitudes(dev, dtype):
+    # masks of the type's lowest value: as minus infinity beside others, and an even row where there are no others
+    lowest, largest = torch.finfo(dtype).min, torch.finfo(dtype).max
+    z, experts, _, add = case(dev, 5000, 20, 2, dtype, False)
+    same = z.clone()
+    z[3, :19], same[3, :19] = lowest, -float("inf")
+    z[4], same[4] = lowest, 0
+    z[5, 2:9], same[5, 2:9] = lowest, -float("inf")
+    z[6, 4], same[6], same[6, 4] = largest, -float("inf"), 0
+    z[7], same[7] = largest, 0
+    z[8], same[8], same[8, :3] = lowest, -float("inf"), 0
+    z[8, :3] = largest
+    for T in (50, 5000):
+        a, _ = emu.route_balance(z[:T], experts[:T])
+        b, _ = emu.route_balance(same[:T], experts[:T])
+        assert bool(b.loss.isfinite()) and torch.equal(a.loss, b.loss) and torch.equal(a.counts, b.counts)
+        assert torch.equal(emu.route_balance_backward(z[:T], a, add=add[:T]), emu.route_balance_backward(same[:T], b, add=add[:T]))
+
+
 @pytest.mark.parametrize("T", [30, 6000])
 def test_entries_outside_are_not_counted(dev, T):
     z, experts, mask, add = case(dev, T, 24, 4, torch.float32, True)
