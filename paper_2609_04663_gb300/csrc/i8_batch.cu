@@ -441,6 +441,12 @@ i8_batch_kernel(const __grid_constant__ CUtensorMap tmW, const BatchArgs a)
     }
 }
 
+__global__ void __launch_bounds__(256) i8_copy_kernel(const I8Product p, const CopyArgs a)
+{
+    for (int64_t i = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); i < a.wrows + a.trows; i += (int64_t)gridDim.x * 8)
+        copy_row(p, a, i, (int)lane_id());
+}
+
 // Token rows and weights that cannot be read as they stand are copied to the scratch.
 bool rows_direct(const I8Product &p) { return aligned_codes(p.X, p.xrows > 1 ? p.ldx : 0, 0); }
 
@@ -471,12 +477,14 @@ cudaError_t launch_i8_batch(I8Product p, int parts, void *scratch, cudaStream_t 
     a.ldr = p.ldx;
     if (weights || tokens) {
         CopyArgs c = {};
-        c.p = p; c.ld = ld;
+        c.ld = ld;
         c.t = static_cast<int8_t *>(scratch);
         c.w = c.t + up(p.rows * ld, 256);
         c.wrows = weights ? (int64_t)p.G * p.N : 0;
         c.trows = tokens ? p.rows : 0;
-        const cudaError_t e = copy_rows(c, st);
+        const int64_t blocks = (c.wrows + c.trows + 7) / 8;
+        i8_copy_kernel<<<(unsigned)(blocks > 152 * 16 ? 152 * 16 : blocks), 256, 0, st>>>(p, c);
+        const cudaError_t e = cudaGetLastError();
         if (e != cudaSuccess) return e;
         if (weights) { p.W = c.w; p.ldw = ld; p.stridew = p.N * ld; }
         if (tokens) { a.rows = c.t; a.ldr = ld; a.copied = 1; }

@@ -39,6 +39,7 @@ struct PairCfg {
 struct PairArgs {
     I8Product p;
     const float *xs;                  // [rows] the rows' scales in group order (0: no such row)
+    int copied;                       // the launch before also writes the weights that are read
 };
 
 __device__ __forceinline__ I8Tile pair_tile(int t, const I8Product &p, const int *starts, const int *tpre, int rank)
@@ -214,6 +215,7 @@ i8_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ 
         asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
         if (warp == Cfg::TMAW && lane == 0) {
             // ---------------- TMA: the weights' bytes
+            if (a.copied) griddep_wait();
             long issued = 0;
             uint32_t s = 0, ph = 0;
             bool ok = true;
@@ -343,6 +345,7 @@ struct ExpandArgs {
     float *xs;                        // [rows]
     int per, chunks;                  // codes of a row that a warp takes at once (512 or 2048), such parts of a row
     int own_flags;                    // block 0 looks at all rows and sets the flag word
+    CopyArgs copy;                    // of weights, or none
 };
 
 // 16 codes a lane.  Bound by HBM and L2: one byte read and two written an element.
@@ -368,7 +371,11 @@ __global__ void __launch_bounds__(256) i8_expand_kernel(const ExpandArgs a)
         }
     }
     const int64_t units = (int64_t)p.rows * a.chunks;
-    for (int64_t i = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); i < units; i += (int64_t)gridDim.x * 8) {
+    for (int64_t i = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); i < units + a.copy.wrows; i += (int64_t)gridDim.x * 8) {
+        if (i >= units) {
+            copy_row(p, a.copy, i - units, lane);
+            continue;
+        }
         const int64_t r = i / a.chunks;
         const int first = (int)(i - r * a.chunks) * a.per;
         const int64_t t = p.src ? __ldg(p.src + r) : r;
@@ -439,16 +446,16 @@ cudaError_t launch_i8_tile(I8Product p, void *scratch, cudaStream_t st)
         fit.store(at.numRegs * PairCfg::THREADS >= kSplitRegisters ? 1 : -1, std::memory_order_relaxed);
     }
     if (fit.load(std::memory_order_relaxed) < 0) return cudaErrorLaunchOutOfResources;
+    ExpandArgs e = {};
+    e.p = p;
+    PairArgs a = {};
     if (!aligned) {
-        CopyArgs c = {};
-        c.p = p; c.wrows = (int64_t)p.G * p.N; c.w = reinterpret_cast<int8_t *>(s + y.copy); c.ld = y.ldcopy;
-        const cudaError_t e = copy_rows(c, st);
-        if (e != cudaSuccess) return e;
-        p.W = c.w;
+        e.copy.wrows = (int64_t)p.G * p.N; e.copy.w = reinterpret_cast<int8_t *>(s + y.copy); e.copy.ld = y.ldcopy;
+        p.W = e.copy.w;
         p.ldw = y.ldcopy;
         p.stridew = p.N * y.ldcopy;
+        a.copied = 1;
     }
-    PairArgs a = {};
     a.p = p;
     a.xs = reinterpret_cast<float *>(s + y.xs);
     uint16_t *plane = reinterpret_cast<uint16_t *>(s);
@@ -456,8 +463,7 @@ cudaError_t launch_i8_tile(I8Product p, void *scratch, cudaStream_t st)
     if (!make_code_map(&tw, p.W, p.K, p.N, p.G, p.ldw, p.stridew) ||
         !make_group_map(&tc, plane, p.K, p.rows, 1, 1, y.ld, 0, 0, 64) || !make_group_map(&ts, plane, p.K, p.rows, 1, 1, y.ld, 0, 0, 16))
         return cudaErrorInvalidValue;
-    ExpandArgs e = {};
-    e.p = p; e.plane = plane; e.ld = y.ld; e.xs = reinterpret_cast<float *>(s + y.xs);
+    e.plane = plane; e.ld = y.ld; e.xs = reinterpret_cast<float *>(s + y.xs);
     e.own_flags = p.rows <= 4096;
     if (!e.own_flags) {
         const cudaError_t c = cudaMemsetAsync(p.flags, 0, sizeof(uint32_t), st);
@@ -466,7 +472,7 @@ cudaError_t launch_i8_tile(I8Product p, void *scratch, cudaStream_t st)
     // short pieces while there are not warps enough
     e.per = (int64_t)p.rows * ((p.K + 2047) / 2048) < 152 * 32 ? 512 : 2048;
     e.chunks = (p.K + e.per - 1) / e.per;
-    const int64_t blocks = ((int64_t)p.rows * e.chunks + 7) / 8;
+    const int64_t blocks = ((int64_t)p.rows * e.chunks + e.copy.wrows + 7) / 8;
     const unsigned grid = (unsigned)(blocks > 152 * 8 ? 152 * 8 : blocks);
     if (aligned_codes(p.X, p.xrows > 1 ? p.ldx : 0, 0)) i8_expand_kernel<true><<<grid, 256, 0, st>>>(e);
     else i8_expand_kernel<false><<<grid, 256, 0, st>>>(e);

@@ -132,35 +132,25 @@ __device__ __forceinline__ bool convert_weights(uint32_t from, int first, int ro
 // Rows of weights that TMA cannot read, and token rows that cannot be read 16 codes at a time, in
 // group order: copies with rows on 16 bytes (the bytes between are not read).
 struct CopyArgs {
-    I8Product p;
     int64_t wrows, trows;             // rows of weights (of all groups) and of tokens to copy
     int8_t *w, *t;
     int64_t ld;
 };
-__global__ void __launch_bounds__(256) i8_copy_kernel(const CopyArgs a)
+// Row i of the copies, by a warp.
+__device__ __forceinline__ void copy_row(const I8Product &p, const CopyArgs &a, int64_t i, int lane)
 {
-    const I8Product &p = a.p;
-    const int lane = (int)lane_id();
-    for (int64_t i = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); i < a.wrows + a.trows; i += (int64_t)gridDim.x * 8) {
-        const int8_t *from = nullptr;
-        int8_t *to = a.w + i * a.ld;
-        if (i < a.wrows) {
-            const int64_t g = i / p.N;
-            from = p.W + g * p.stridew + (i - g * p.N) * p.ldw;
-        } else {
-            const int64_t r = i - a.wrows, t = p.src ? __ldg(p.src + r) : r;
-            if (t >= 0 && t < p.xrows) from = p.X + t * p.ldx;
-            to = a.t + r * a.ld;
-        }
-        for (int k = lane * 16; k < p.K; k += 512)
-            *reinterpret_cast<uint4 *>(to + k) = from ? load_codes<false>(from + k, p.K - k) : make_uint4(0u, 0u, 0u, 0u);
+    const int8_t *from = nullptr;
+    int8_t *to = a.w + i * a.ld;
+    if (i < a.wrows) {
+        const int64_t g = i / p.N;
+        from = p.W + g * p.stridew + (i - g * p.N) * p.ldw;
+    } else {
+        const int64_t r = i - a.wrows, t = p.src ? __ldg(p.src + r) : r;
+        if (t >= 0 && t < p.xrows) from = p.X + t * p.ldx;
+        to = a.t + r * a.ld;
     }
-}
-cudaError_t copy_rows(const CopyArgs &a, cudaStream_t st)
-{
-    const int64_t blocks = (a.wrows + a.trows + 7) / 8;
-    i8_copy_kernel<<<(unsigned)(blocks > 152 * 16 ? 152 * 16 : blocks), 256, 0, st>>>(a);
-    return cudaGetLastError();
+    for (int k = lane * 16; k < p.K; k += 512)
+        *reinterpret_cast<uint4 *>(to + k) = from ? load_codes<false>(from + k, p.K - k) : make_uint4(0u, 0u, 0u, 0u);
 }
 
 // Tensor map over G matrices of N rows of K codes, boxes of 128 x 128 bytes.

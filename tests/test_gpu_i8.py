@@ -293,6 +293,19 @@ def test_the_same_sums_every_time(dev, rows, N, K):
     assert int(off) == 0
 
 
+@pytest.mark.parametrize("N,K", [(1300, 333), (1301, 1100), (1024, 17), (1500, 129), (1100, 2064)])
+@pytest.mark.parametrize("ends", [None, [4000, 4000, 4001, 5300, 5990], [1, 300, 2300, 4444, 6000]])
+def test_many_rows(dev, ends, N, K):
+    # sizes that pairs of SMs get, of any alignment, gathered
+    G = len(ends) if ends else 0
+    assert emu.emu_i8_gemm_workspace_bytes(max(G, 1), 6000, N, K, 1) > 0
+    X, W = make(dev, 6000 if not ends else 777, N, K, G=G)
+    if not ends:
+        return check(X, W)
+    src = torch.randint(0, 777, (6000,), generator=gen(dev, N), device=dev, dtype=torch.int32)
+    check(X, W, ends=ends, src=src)
+
+
 def test_many_groups(dev):
     rng = np.random.default_rng(0)
     for per in (1, 40):
