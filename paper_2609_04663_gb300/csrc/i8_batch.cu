@@ -22,6 +22,7 @@ namespace emu {
 namespace {
 
 constexpr int kReadWarps = 4, kRowWarps = 8;
+constexpr int kRowGroups = 4, kGroupWarps = kRowWarps / kRowGroups, kStepRows = 4 * kGroupWarps, kRuns = 64 / kStepRows;
 
 struct BatchCfg {
     static constexpr int COLS = 64, STEP = 16;
@@ -114,7 +115,7 @@ i8_batch_kernel(const __grid_constant__ CUtensorMap tmW, const BatchArgs a)
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < Cfg::NS; ++s) {
-            mbar_init(cfull0 + 8u * s, kRowWarps / 2);
+            mbar_init(cfull0 + 8u * s, kGroupWarps);
             mbar_init(afull0 + 8u * s, kConvertWarps);
             mbar_init(used0 + 8u * s, 1);
         }
@@ -245,15 +246,14 @@ i8_batch_kernel(const __grid_constant__ CUtensorMap tmW, const BatchArgs a)
         }
     } else if (warp < Cfg::CONV) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 88;");
-        const int group = (warp - Cfg::ROWS) >> 2;
+        const int group = (warp - Cfg::ROWS) / kGroupWarps;
         // ---- rows: this group's next stage (tile, K), its runs of 16 codes on their way
-        const int gt = (int)threadIdx.x & 127, chunk = gt & 7, xrow = gt >> 3;       // rows xrow + 16 j
+        const int gt = (int)threadIdx.x % (32 * kGroupWarps), chunk = gt & 7, xrow = gt >> 3;        // rows xrow + 8 j
         const uint32_t xput = base + (uint32_t)((chunk >> 2) * Cfg::C_BLOCK + xrow * 128 + ((((chunk & 3) * 2) ^ (xrow & 7)) << 4));
         int lt = first, lk = -kWK, lnk = 0, lk0 = 0, ln = 0;
-        const int8_t *source[4] = {};                 // this thread's runs in the rows (none: NULL)
+        const int8_t *source[kRuns] = {};               // this thread's runs in the rows (none: NULL)
         uint32_t li = 0xFFFFFFFFu;                    // stage that was asked for last
-        uint4 v[2][4];
-        int rows_of[2] = {};                          // rows of the tiles that v's stages are of
+        uint4 v[kRuns];
         // to the group's next stage; false behind the last
         auto advance = [&]() {
             do {
@@ -268,8 +268,8 @@ i8_batch_kernel(const __grid_constant__ CUtensorMap tmW, const BatchArgs a)
                 lk0 = x.k0 + chunk * 16;
                 ln = x.n[0];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int c = xrow + 16 * j;
+                for (int j = 0; j < kRuns; ++j) {
+                    const int c = xrow + kStepRows * j;
                     source[j] = nullptr;
                     if (c < x.cols) {
                         const int64_t at = (int64_t)starts[x.g] + x.c0 + c;
@@ -277,59 +277,47 @@ i8_batch_kernel(const __grid_constant__ CUtensorMap tmW, const BatchArgs a)
                         if (a.copied || (r >= 0 && r < a.p.xrows)) source[j] = a.rows + r * a.ldr + lk0;
                     }
                 }
-            } while ((li & 1u) != (uint32_t)group);
+            } while (li % kRowGroups != (uint32_t)group);
             return true;
         };
         // the loads stand next to each other, so that all are on their way before the first is waited for
-        auto ask = [&](uint4 (&v)[4]) {
+        auto ask = [&]() {
             const int n = a.p.K - lk0 - lk;
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+            for (int j = 0; j < kRuns; ++j)
                 asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %5, 0;\n\tmov.b32 %0, 0;\n\tmov.b32 %1, 0;\n\tmov.b32 %2, 0;\n\tmov.b32 %3, 0;\n\t"
                              "@p ld.global.nc.v4.b32 {%0, %1, %2, %3}, [%4];\n\t}"
                              : "=&r"(v[j].x), "=&r"(v[j].y), "=&r"(v[j].z), "=&r"(v[j].w)
                              : "l"(source[j] + lk), "r"((uint32_t)(source[j] != nullptr && n >= 16)));
             if (n > 0 && n < 16) {                    // the last run of a row
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
+                for (int j = 0; j < kRuns; ++j)
                     if (source[j]) v[j] = load_tail(source[j] + lk, n);
             }
         };
-        bool have[2];
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            have[b] = (b == 0 || have[0]) && advance();
-            rows_of[b] = ln;
-            if (have[b]) ask(v[b]);
-        }
         uint32_t i = (uint32_t)group;                 // the group's next stage
-        bool ok = true;
-        while ((have[0] || have[1]) && ok) {
+        bool have = advance();
+        if (have) ask();
+        while (have) {
+            const uint32_t s = i % Cfg::NS;
+            if (!warp_wait(used0 + 8u * s, ((i / Cfg::NS) & 1u) ^ 1u, flags)) break;
+            const uint32_t to = xput + s * (uint32_t)Cfg::C_STAGE;
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                if (!have[b] || !ok) continue;
-                const uint32_t s = i % Cfg::NS;
-                if (!(ok = warp_wait(used0 + 8u * s, ((i / Cfg::NS) & 1u) ^ 1u, flags))) continue;
-                const uint32_t to = xput + s * (uint32_t)Cfg::C_STAGE;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if (16 * j >= rows_of[b]) break;
-                    uint32_t lo[4], hi[4];
-                    codes_f16(v[b][j].x, lo[0], lo[1]);
-                    codes_f16(v[b][j].y, lo[2], lo[3]);
-                    codes_f16(v[b][j].z, hi[0], hi[1]);
-                    codes_f16(v[b][j].w, hi[2], hi[3]);
-                    st_shared_v4(to + (uint32_t)(j * 16 * 128), lo[0], lo[1], lo[2], lo[3]);
-                    st_shared_v4((to + (uint32_t)(j * 16 * 128)) ^ 16u, hi[0], hi[1], hi[2], hi[3]);
-                }
-                fence_proxy_async_smem();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(cfull0 + 8u * s);
-                i += 2u;
-                have[b] = advance();
-                rows_of[b] = ln;
-                if (have[b]) ask(v[b]);
+            for (int j = 0; j < kRuns; ++j) {
+                if (kStepRows * j >= ln) break;
+                uint32_t lo[4], hi[4];
+                codes_f16(v[j].x, lo[0], lo[1]);
+                codes_f16(v[j].y, lo[2], lo[3]);
+                codes_f16(v[j].z, hi[0], hi[1]);
+                codes_f16(v[j].w, hi[2], hi[3]);
+                st_shared_v4(to + (uint32_t)(j * kStepRows * 128), lo[0], lo[1], lo[2], lo[3]);
+                st_shared_v4((to + (uint32_t)(j * kStepRows * 128)) ^ 16u, hi[0], hi[1], hi[2], hi[3]);
             }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(cfull0 + 8u * s);
+            i += kRowGroups;
+            if ((have = advance())) ask();
         }
     } else if (warp < Cfg::TMAW) {
         // ---------------- weights: bytes of shared memory -> FP16 in tensor memory.  Lane: one
