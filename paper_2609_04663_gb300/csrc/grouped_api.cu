@@ -130,8 +130,8 @@ constexpr int64_t kMaxI8K = 131071;      // 128 * 128 * K stays below 2^31
 // Which tensor-core kernel multiplies: 0, pairs of SMs with 256 columns (i8_tile.cu); else 64 columns on one
 // (i8_batch.cu), in so many parts of K while SMs are free.  By times in ns as they were measured: what a launch takes
 // besides, waves of tiles, and in each 64 codes at a time, but no less than a tile's start and end.
-// 32 experts of 2048 x 4096: 1024 rows 70 us on single SMs and 62 on pairs, 128 rows 56 and 59; 256 rows x 4096 x 4096 20
-// and 29; 16 rows x 16384 x 16384 66 and 60; 64 rows x 512 x 4096 7.2 and 8.9.
+// 32 experts of 2048 x 4096: 2048 rows 85 us on single SMs and 67 on pairs, 128 rows 50 and 59; 256 rows x 4096 x 4096 19
+// and 29; 64 rows x 16384 x 16384 65 and 63, 16 rows 51 and 60; 64 rows x 512 x 4096 7.2 and 8.9.
 // Parts cost some 2 us: 16 rows x 1024 x 4096 7.4 us in one and 8.4 in two, 64 rows x 2048 x 4096 13 in one and 11.6 in four.
 int i8_batch_parts(int64_t G, int64_t rows, int64_t N, int64_t K)
 {
@@ -140,7 +140,7 @@ int i8_batch_parts(int64_t G, int64_t rows, int64_t N, int64_t K)
     int parts = 1;
     while (parts < 8 && 2 * parts * tiles <= sms && K >= 1024 * std::max(parts, 2)) parts *= 2;
     const int64_t pair = std::max<int64_t>(steps * (n <= 128 ? 222 : 330), 3000);
-    const int64_t single = std::max<int64_t>(steps * (n <= 16 ? 235 : n < 32 ? 253 : 288) / parts, 2800);
+    const int64_t single = std::max<int64_t>(steps * (n <= 16 ? 195 : n < 32 ? 210 : n <= 48 ? 225 : 245) / parts, 2800);
     return 6500 + waves(G * ((n + 255) / 256) * ((N + 255) / 256), sms / 2) * pair <
                    (parts > 1 ? 7000 : 3500) + waves(tiles, sms) * single ? 0 : parts;
 }

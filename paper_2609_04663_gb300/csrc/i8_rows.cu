@@ -259,13 +259,15 @@ cudaError_t by_alignment(const RowsArgs &a, cudaStream_t st)
 
 }  // namespace
 
-// Up to where the tensor cores' kernel is slower:
-// 8 rows x 4096 x 4096 10.5 us here and 10.7 there, x 8192 x 8192 32 and 22; 4 rows x 8192 x 8192 19 and 22, x 16384 x
-// 16384 55 and 60; 2 rows of each of 32 experts of 2048 x 4096 55.0 and 53.8, 4 rows 62.1 and 56.0.
+// Up to where the tensor cores' kernel is slower: 8 rows x 2048 x 2048 5.7 us here and 8.5 there, x 4096 x 4096 10.5
+// and 10.6, x 8192 x 8192 32 and 20; 4 rows x 8192 x 8192 19 and 20, x 16384 x 16384 55 and 50; 2 rows there 46 and 50.
+// One row of each of 32 experts of 1024 x 1024 12.6 and 13.1, two 14.7 and 13.3; two of each of 8 of 4096 x 4096 27 and
+// 31, four 32 and 31.
 bool i8_few_rows(int64_t G, int64_t rows, int64_t N, int64_t K)
 {
     const int64_t weights = N * K;
-    return G > 1 ? rows <= 2 * G : rows <= 4 || (rows <= 8 && weights <= (int64_t)1 << 24);
+    if (G > 1) return rows <= (G <= 8 ? 2 * G : G);
+    return rows <= 2 || (rows <= 4 && weights <= (int64_t)1 << 26) || (rows <= 8 && weights <= (int64_t)1 << 24);
 }
 
 cudaError_t launch_i8_rows(const I8Product &p, cudaStream_t st)
