@@ -2,19 +2,20 @@
 // up to 64 columns on one SM (i8_tile.cuh has the arithmetic).
 //
 // Warps 0-3 read the accumulators and store.  Warps 4-11 turn the token rows into FP16 in swizzled shared
-// memory, gathered, four warps a stage of 128 codes in turn: a thread has its runs of 16 codes of its group's
-// next two stages on their way into registers.  (The fence that shows a stage to the tensor cores waits for a
-// thread's loads in flight: those were asked for three stages before.)  Warps 12-19 convert weights, 20 brings
-// them by TMA and looks for bad indexes, 21 issues the MMAs.
+// memory, gathered, two warps a stage of 128 codes in turn: a thread asks for its runs of 16 codes of its group's
+// next stage once it has handed over the one before.  (An arrival, like the fence that shows a stage to the tensor
+// cores, waits for all loads that its thread has in flight: two stages ahead in two groups were none, 58.6 us for 256 rows over
+// 32 experts of 2048 x 4096 against 51.)  Warps 12-19 convert weights, 20 brings them by TMA and looks for
+// bad indexes, 21 issues the MMAs.
 //
 // While there are SMs left, K is split between the CTAs of a cluster; each adds and stores a share of the columns,
 // whose other sums it reads from their shared memory.
 //
-// 48 rows x 5120 x 8192 take 20.4 us (HBM alone would 6.5), 64 x 4096 x 4096 13.2, 256 rows over 32 experts of
-// 2048 x 4096 58 (4.7 TB/s): bound by a stage's way through the warps, 235-290 ns for 64 codes, and by start and end
-// of the launch, 4 us, with parts 6.  Tried: all eight row warps on each stage instead of two groups in turn, with the bytes
-// brought to L1 ahead, 64 us for the 256 rows, with loads behind the fence 72; the first CTA of a cluster adding and storing
-// all columns 16 us for the 64 rows.
+// 48 rows x 5120 x 8192 take 18.1 us (HBM alone would 6.5), 64 x 4096 x 4096 13.2, 256 rows over 32 experts of
+// 2048 x 4096 51 (5.3 TB/s): bound by a stage's way through the warps, 185-245 ns for 64 codes (without loads of rows 16.9
+// and 49 us, without converting weights as well 15.5 and 47), and by start and end of the launch, 4 us, with parts 6.
+// Tried: all eight row warps on each stage, with the bytes brought to L1 ahead, 64 us for the 256 rows; a third group of
+// converting warps 60 against 58.6; the first CTA of a cluster adding and storing all columns 16 us for the 64 rows.
 #include "i8_tile.cuh"
 
 namespace emu {
