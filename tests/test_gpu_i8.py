@@ -306,6 +306,18 @@ def test_many_rows(dev, ends, N, K):
     check(X, W, ends=ends, src=src)
 
 
+@pytest.mark.parametrize("K", [2064, 2050, 4112])
+@pytest.mark.parametrize("per", [65, 49, 17])
+def test_parts_of_the_contraction_and_several_tiles_each(dev, per, K):
+    # more tiles than clusters that share a contraction: sums are handed over again and again
+    G, N = 7, 600
+    ends = [per * (g + 1) for g in range(6)] + [448]
+    X, W = make(dev, 448, N, K, G=G)
+    check(X, W, ends=ends)
+    src = torch.randint(0, 448, (448,), generator=gen(dev, K), device=dev, dtype=torch.int32)
+    check(X, W, ends=ends, src=src)
+
+
 def test_many_groups(dev):
     rng = np.random.default_rng(0)
     for per in (1, 40):
