@@ -7,8 +7,8 @@
 // In a pair's CTA warps 0-7 read accumulators and store, 8-15 convert weights, 16 brings weights by TMA, 17
 // (of the first CTA) issues the MMAs, 18 brings the rows.
 //
-// 16384 x 8192 x 4096 takes 644 us, 1.71 PFLOP/s, 75 of them before the products (bytes in, FP16 out, by HBM); the
-// tensor pipe is 84 % active there at 8192 rows.  8192 rows over 32 experts, 2048 -> 4096: 123 us, tensor pipe 59 %
+// 16384 x 8192 x 4096 takes 630 us, 1.75 PFLOP/s, 61 of them before the products (bytes in, FP16 out, by HBM); the
+// tensor pipe is 84 % active there at 8192 rows.  8192 rows over 32 experts, 2048 -> 4096: 120 us, tensor pipe 59 %
 // active: groups' last tiles are not full, and each tile has only 16 stages between two read-outs.
 // Tried: rows turned into FP16 by these CTAs (599 ns for 64 codes of 256 columns, 404-448 from FP16), two accumulators
 // instead of three (742 us against 682), one converting group of four warps (353 ns against 253 with 16 columns).
@@ -343,14 +343,15 @@ struct ExpandArgs {
     uint16_t *plane;                  // [rows][ld], in group order
     int64_t ld;
     float *xs;                        // [rows]
-    int per, chunks;                  // codes of a row that a warp takes at once (512 or 2048), such parts of a row
+    int chunks;                       // parts of a row, of 512 codes
     int own_flags;                    // block 0 looks at all rows and sets the flag word
     CopyArgs copy;                    // of weights, or none
 };
 
-// 16 codes a lane.  Bound by HBM and L2: one byte read and two written an element.
+// 16 codes a lane, 512 of a row a warp, most warps once.  Bound by HBM and L2: one byte read and two written an
+// element (16384 x 8192 61 us, 6.6 TB/s; four such parts a warp, in 8 blocks an SM, took 75).
 template <bool WIDE>
-__global__ void __launch_bounds__(256) i8_expand_kernel(const ExpandArgs a)
+__global__ void __launch_bounds__(256, 8) i8_expand_kernel(const ExpandArgs a)
 {
     griddep_launch_dependents();
     const I8Product &p = a.p;
@@ -377,7 +378,7 @@ __global__ void __launch_bounds__(256) i8_expand_kernel(const ExpandArgs a)
             continue;
         }
         const int64_t r = i / a.chunks;
-        const int first = (int)(i - r * a.chunks) * a.per;
+        const int first = (int)(i - r * a.chunks) * 512, k = first + lane * 16;
         const int64_t t = p.src ? __ldg(p.src + r) : r;
         const bool there = t >= 0 && t < p.xrows;
         if (lane == 0 && first == 0) {
@@ -386,26 +387,15 @@ __global__ void __launch_bounds__(256) i8_expand_kernel(const ExpandArgs a)
         }
         const int8_t *x = p.X + (there ? t : 0) * p.ldx;
         uint16_t *out = a.plane + r * a.ld;
-        constexpr int B = 4;                          // pieces loaded before the first is stored
-        uint4 v[B];
-#pragma unroll
-        for (int b = 0; b < B; ++b) {
-            const int k = first + lane * 16 + 512 * b;
-            v[b] = make_uint4(0u, 0u, 0u, 0u);
-            if (there && 512 * b < a.per && k < p.K) v[b] = load_codes<WIDE>(x + k, p.K - k);
-        }
-#pragma unroll
-        for (int b = 0; b < B; ++b) {
-            const int k = first + lane * 16 + 512 * b;
-            if (512 * b >= a.per || k >= p.K) break;
-            uint4 f[2];
-            codes_f16(v[b].x, f[0].x, f[0].y);
-            codes_f16(v[b].y, f[0].z, f[0].w);
-            codes_f16(v[b].z, f[1].x, f[1].y);
-            codes_f16(v[b].w, f[1].z, f[1].w);
-            *reinterpret_cast<uint4 *>(out + k) = f[0];
-            if (k + 8 < a.ld) *reinterpret_cast<uint4 *>(out + k + 8) = f[1];
-        }
+        if (k >= p.K) continue;
+        const uint4 v = there ? load_codes<WIDE>(x + k, p.K - k) : make_uint4(0u, 0u, 0u, 0u);
+        uint4 f[2];
+        codes_f16(v.x, f[0].x, f[0].y);
+        codes_f16(v.y, f[0].z, f[0].w);
+        codes_f16(v.z, f[1].x, f[1].y);
+        codes_f16(v.w, f[1].z, f[1].w);
+        *reinterpret_cast<uint4 *>(out + k) = f[0];
+        if (k + 8 < a.ld) *reinterpret_cast<uint4 *>(out + k + 8) = f[1];
     }
 }
 
@@ -469,11 +459,9 @@ cudaError_t launch_i8_tile(I8Product p, void *scratch, cudaStream_t st)
         const cudaError_t c = cudaMemsetAsync(p.flags, 0, sizeof(uint32_t), st);
         if (c != cudaSuccess) return c;
     }
-    // short pieces while there are not warps enough
-    e.per = (int64_t)p.rows * ((p.K + 2047) / 2048) < 152 * 32 ? 512 : 2048;
-    e.chunks = (p.K + e.per - 1) / e.per;
+    e.chunks = (p.K + 511) / 512;
     const int64_t blocks = ((int64_t)p.rows * e.chunks + e.copy.wrows + 7) / 8;
-    const unsigned grid = (unsigned)(blocks > 152 * 8 ? 152 * 8 : blocks);
+    const unsigned grid = (unsigned)(blocks > 152 * 1024 ? 152 * 1024 : blocks);
     if (aligned_codes(p.X, p.xrows > 1 ? p.ldx : 0, 0)) i8_expand_kernel<true><<<grid, 256, 0, st>>>(e);
     else i8_expand_kernel<false><<<grid, 256, 0, st>>>(e);
     const cudaError_t c = cudaGetLastError();
