@@ -207,10 +207,10 @@ __device__ __forceinline__ Tile tile_at(int t, const GroupedArgs &a, const int *
 __device__ __forceinline__ float as_float(float x) { return x; }
 __device__ __forceinline__ float as_float(uint32_t x) { return __uint_as_float(x); }
 
-// 32 accumulator columns of this warp's lanes -> rows 0 .. cols - 1 of out:
+// C accumulator columns of this warp's lanes -> rows 0 .. cols - 1 of out:
 // column j is output row j, lane i feature l + i.  BF16: two columns at a
 // time, neighbouring lanes exchange values so that each stores two features
-// of one row.  The usual case (32 whole columns, 32 features, pairs that can be
+// of one row.  The usual case (C whole columns, 32 features, pairs that can be
 // stored as words) has no test per element: these instructions, not the
 // stores' bandwidth, are what the epilogue takes.
 template <typename T, int C>
