@@ -104,8 +104,11 @@ __device__ __forceinline__ float max_nan(float a, float b)
 
 // x: logits -> exp(x - max); returns 1 / their sum, or 0 where all are minus infinity.  NaN
 // counts as minus infinity.  odd: set where a lane's value is NaN or plus infinity.
-// As powers of two: x log2 e - c with one rounding, c = max log2 e rounded, the same for the
-// whole row, which the sum takes out again.  A power of two is off by 2^-22 at most.
+// As powers of two: x log2 e - c with one rounding, c = max log2 e rounded.  What c is off by is a
+// factor that the whole row has and the sum takes out again, while it is
+// small: below 2^(1/16) for |max| <= 2^20, 2^128 at worst from 2^31 on.  Larger ones are subtracted first, which is
+// exact for values whose exponentials are not 0 (within 104 of the largest; always subtracting would put a
+// second rounding into ordinary rows).  A power of two is off by 2^-22 at most.
 template <int V, int L>
 __device__ __forceinline__ float softmax_parts(float (&x)[V], bool &odd)
 {
@@ -124,7 +127,7 @@ __device__ __forceinline__ float softmax_parts(float (&x)[V], bool &odd)
 #pragma unroll
     for (int d = L / 2; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
     const bool some = top > -INFINITY;
-    if (some && fabsf(top) > 1e38f) {                 // (a mask of the type's lowest value in a whole row: top log2 e would overflow)
+    if (some && fabsf(top) > 0x1p20f) {               // (a row of a mask's -1e9, or of the type's lowest value)
 #pragma unroll
         for (int i = 0; i < V; ++i) x[i] -= top;
         top = 0.0f;
