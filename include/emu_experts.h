@@ -224,8 +224,8 @@ emu_status emu_i8_quantize(int dtype, int64_t G, int64_t rows, int64_t cols, con
  * takes no scales.  X: xrows x K, W: G matrices N x K, stridew apart, int8 of any alignment:
  * read as they stand where base, row pitch and distance are multiples of 16 bytes and W's matrices do
  * not overlap, and copied first otherwise where more than a few rows meet.  xscales [xrows], wscales
- * [G][N] FP32.  Rows of no group, and rows whose src is outside 0 .. xrows-1, are zero.  aligned: whether
- * both X and W are such (0 is enough for any).  ws: at least emu_i8_gemm_workspace_bytes, 16-byte
+ * [G][N] FP32.  Rows of no group, and rows whose src is outside 0 .. xrows-1, are zero whatever the
+ * scales are.  aligned: whether both X and W are such (0 is enough for any).  ws: at least emu_i8_gemm_workspace_bytes, 16-byte
  * aligned, not shared by calls in flight at once; where that is 0, emu_split_workspace_bytes(32) for the
  * flags, or NULL, which reports none.  Flags: EMU_FLAG_INDEX, EMU_FLAG_TIMEOUT. */
 size_t emu_i8_gemm_workspace_bytes(int64_t G, int64_t rows, int64_t N, int64_t K, int aligned);

@@ -163,15 +163,20 @@ i8_batch_kernel(const __grid_constant__ CUtensorMap tmW, const BatchArgs a)
             const I8Tile x = tile(t);
             const int l = x.l0 + warp * 32;
             const int64_t row0 = (int64_t)starts[x.g] + x.c0;
-            // scales, while the products are under way (a row without a source has zero sums)
+            // scales, while the products are under way
             float ws = 1.0f, xs[2] = {};
+            uint32_t gone[2];                         // columns without a source
             if (a.p.wscales && l + lane < a.p.N) ws = __ldg(a.p.wscales + (int64_t)x.g * a.p.N + l + lane);
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+            for (int h = 0; h < 2; ++h) {
+                bool none = false;
                 if (32 * h + lane < x.cols) {
                     const int64_t from = a.p.src ? __ldg(a.p.src + row0 + 32 * h + lane) : row0 + 32 * h + lane;
-                    if (from >= 0 && from < a.p.xrows) xs[h] = a.p.xscales ? __ldg(a.p.xscales + from) : 1.0f;
+                    none = from < 0 || from >= a.p.xrows;
+                    if (!none) xs[h] = a.p.xscales ? __ldg(a.p.xscales + from) : 1.0f;
                 }
+                gone[h] = __ballot_sync(0xFFFFFFFFu, none);
+            }
             int acc[Cfg::COLS];
 #pragma unroll
             for (int j = 0; j < Cfg::COLS; ++j) acc[j] = 0;
@@ -225,8 +230,10 @@ i8_batch_kernel(const __grid_constant__ CUtensorMap tmW, const BatchArgs a)
                     for (int j = 0; j < 8; ++j)
                         v[j] = a.p.ytype == EMU_I32 ? __int_as_float(sum[j])
                                                     : scaled_sum(sum[j], ws, __shfl_sync(0xFFFFFFFFu, c < 32 ? xs[0] : xs[1], (c & 31) + j));
-                    if (l < a.p.N)
+                    if (l < a.p.N) {
                         store_columns(v, x.cols - c, static_cast<char *>(a.p.Y) + (row0 + c) * a.p.ldy * esize, a.p.ldy, l, a.p.N, f32, pairs_ok);
+                        clear_rows(a.p, row0 + c, (c < 32 ? gone[0] : gone[1]) >> (c & 31) & 0xFFu, l + lane);
+                    }
                 }
                 __syncwarp();
                 if (lane < a.parts && lane != rank) arrive_cluster(sempty0 + 8u * warp, lane);
@@ -243,6 +250,7 @@ i8_batch_kernel(const __grid_constant__ CUtensorMap tmW, const BatchArgs a)
                     v[j] = a.p.ytype == EMU_I32 ? __int_as_float(acc[32 * h + j])
                                                 : scaled_sum(acc[32 * h + j], ws, __shfl_sync(0xFFFFFFFFu, xs[h], j));
                 store_columns(v, cols, static_cast<char *>(a.p.Y) + (row0 + 32 * h) * a.p.ldy * esize, a.p.ldy, l, a.p.N, f32, pairs_ok);
+                clear_rows(a.p, row0 + 32 * h, gone[h], l + lane);
             }
         }
     } else if (warp < Cfg::CONV) {

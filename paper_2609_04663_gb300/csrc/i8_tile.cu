@@ -36,9 +36,11 @@ struct PairCfg {
     static_assert(NA >= 2 && NA <= NC && C_HALF == 8192, "stages");
 };
 
+constexpr uint32_t kNoRow = 0xFFFFFFFFu;              // a NaN that no scale is handed over as
+
 struct PairArgs {
     I8Product p;
-    const float *xs;                  // [rows] the rows' scales in group order (0: no such row)
+    const float *xs;                  // [rows] the rows' scales in group order (the bits kNoRow: no such row)
     int copied;                       // the launch before also writes the weights that are read
 };
 
@@ -169,6 +171,8 @@ i8_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ 
             const int64_t row0 = (int64_t)starts[x.g] + x.c0;
             if (l >= a.p.N) continue;
             const float ws = a.p.wscales && l + lane < a.p.N ? __ldg(a.p.wscales + (int64_t)x.g * a.p.N + l + lane) : 1.0f;
+            uint32_t nowhere = 0;                     // this lane's columns (of four blocks of 32) without a source
+            static_assert(Cfg::WC == 64, "two blocks of 32 columns a half");
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
 #pragma unroll
@@ -184,6 +188,14 @@ i8_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ 
                         v[j] = a.p.ytype == EMU_I32 ? __int_as_float(s) : scaled_sum(s, ws, __shfl_sync(0xFFFFFFFFu, xs, j));
                     }
                     store_columns(v, cols, static_cast<char *>(a.p.Y) + r * a.p.ldy * esize, a.p.ldy, l, a.p.N, f32, pairs_ok);
+                    nowhere |= (uint32_t)(__float_as_uint(xs) == kNoRow) << (h * 2 + q / 32);
+                }
+            }
+            if (__any_sync(0xFFFFFFFFu, nowhere != 0)) {
+#pragma unroll 1
+                for (int i = 0; i < 4; ++i) {
+                    const int h = i >> 1, q = (i & 1) * 32;
+                    clear_rows(a.p, row0 + (h ? x.n[0] : 0) + w0 + q, __ballot_sync(0xFFFFFFFFu, nowhere >> i & 1u), l + lane);
                 }
             }
         }
@@ -381,10 +393,9 @@ __global__ void __launch_bounds__(256, 8) i8_expand_kernel(const ExpandArgs a)
         const int first = (int)(i - r * a.chunks) * 512, k = first + lane * 16;
         const int64_t t = p.src ? __ldg(p.src + r) : r;
         const bool there = t >= 0 && t < p.xrows;
-        if (lane == 0 && first == 0) {
-            a.xs[r] = !there ? 0.0f : p.xscales ? __ldg(p.xscales + t) : 1.0f;
-            if (!there && !a.own_flags) atomicOr(p.flags, (uint32_t)EMU_FLAG_INDEX);
-        }
+        const bool start = lane == 0 && first == 0;
+        float xs = 1.0f;                              // (looked at behind the row's loads: nothing waits for it before)
+        if (start && there && p.xscales) xs = __ldg(p.xscales + t);
         const int8_t *x = p.X + (there ? t : 0) * p.ldx;
         uint16_t *out = a.plane + r * a.ld;
         if (k >= p.K) continue;
@@ -396,6 +407,10 @@ __global__ void __launch_bounds__(256, 8) i8_expand_kernel(const ExpandArgs a)
         codes_f16(v.w, f[1].z, f[1].w);
         *reinterpret_cast<uint4 *>(out + k) = f[0];
         if (k + 8 < a.ld) *reinterpret_cast<uint4 *>(out + k + 8) = f[1];
+        if (start) {                                  // (K > 0: this lane has codes)
+            a.xs[r] = __uint_as_float(!there ? kNoRow : isnan(xs) ? 0x7FFFFFFFu : __float_as_uint(xs));
+            if (!there && !a.own_flags) atomicOr(p.flags, (uint32_t)EMU_FLAG_INDEX);
+        }
     }
 }
 
