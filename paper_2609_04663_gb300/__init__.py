@@ -934,12 +934,12 @@ def i8_quantize(X, codes=None, scales=None, ws=None, stream=None):
         ps = scales.data_ptr()
     else:
         ps = _float_pairs(scales, shape[:-1], dev, "i8_quantize: scales")
-    if G:
-        r = _lib.emu_i8_quantize(dt, G, rows, cols, X.data_ptr(), ldx, X.stride(0) if G > 1 else 0, codes.data_ptr(), ldq,
-                                 strideq, ps, None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(),
-                                 _raw_stream(stream, dev))
-        if r:
-            _check(r, "emu_i8_quantize")
+    # (no matrices: one without rows, which clears the flags)
+    r = _lib.emu_i8_quantize(dt, G or 1, rows if G else 0, cols, X.data_ptr(), ldx, X.stride(0) if G > 1 else 0,
+                             codes.data_ptr(), ldq, strideq, ps, None if ws is None else ws.data_ptr(),
+                             0 if ws is None else ws.numel(), _raw_stream(stream, dev))
+    if r:
+        _check(r, "emu_i8_quantize")
     return Int8(codes, scales)
 
 
