@@ -234,6 +234,14 @@ emu_status emu_i8_gemm(int64_t G, int64_t rows, int64_t N, int64_t K, const int8
                        const float *wscales, const int32_t *ends, void *Y, int ytype, int64_t ldy, void *ws,
                        size_t ws_bytes, emu_stream_t stream);
 
+/* Watchdog self-test of emu_i8_gemm (with a workspace, at sizes whose products are one launch on single
+ * SMs; others are unsupported): nothing is multiplied, a wait runs out after timeout_us microseconds (1 .. 10^6) and sets
+ * EMU_FLAG_TIMEOUT beside the call's other flags; rows of groups keep what they hold. */
+emu_status emu_selftest_i8_timeout(uint32_t timeout_us, int64_t G, int64_t rows, int64_t N, int64_t K, const int8_t *X,
+                                   int64_t xrows, int64_t ldx, const float *xscales, const int32_t *src, const int8_t *W,
+                                   int64_t ldw, int64_t stridew, const float *wscales, const int32_t *ends, void *Y,
+                                   int ytype, int64_t ldy, void *ws, size_t ws_bytes, emu_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -93,6 +93,8 @@ _SIGS = {
     "emu_i8_gemm_workspace_bytes": ("size", ["l", "l", "l", "l", "i"]),
     "emu_i8_gemm": ("i", ["l", "l", "l", "l", "p", "l", "l", "p", "p", "p", "l", "l", "p", "p", "p", "i", "l", "p", "size",
                           "p"]),
+    "emu_selftest_i8_timeout": ("i", ["u32", "l", "l", "l", "l", "p", "l", "l", "p", "p", "p", "l", "l", "p", "p", "p", "i",
+                                      "l", "p", "size", "p"]),
     "emu_read_flags": ("i", ["p", "p", "p"]),
     "emu_selftest_timeout": ("i", ["p", "size", "u32", "p"]),
     "emu_status_string": ("str", ["i"]),
@@ -190,6 +192,7 @@ emu_route_balance_backward = _mk("emu_route_balance_backward")
 emu_i8_quantize = _mk("emu_i8_quantize")
 emu_i8_gemm_workspace_bytes = _mk("emu_i8_gemm_workspace_bytes")
 emu_i8_gemm = _mk("emu_i8_gemm")
+emu_selftest_i8_timeout = _mk("emu_selftest_i8_timeout")
 emu_read_flags = _mk("emu_read_flags")
 emu_selftest_timeout = _mk("emu_selftest_timeout")
 emu_status_string = _mk("emu_status_string")

@@ -89,6 +89,7 @@ bool i8_few_rows(int64_t G, int64_t rows, int64_t N, int64_t K);      // launch_
 size_t i8_tile_scratch_bytes(int64_t G, int64_t rows, int64_t N, int64_t K, bool aligned);
 cudaError_t launch_i8_tile(I8Product p, void *scratch, cudaStream_t st);
 size_t i8_batch_scratch_bytes(int64_t G, int64_t rows, int64_t N, int64_t K, bool aligned);
-cudaError_t launch_i8_batch(I8Product p, int parts, void *scratch, cudaStream_t st);
+cudaError_t launch_i8_batch(I8Product p, int parts, void *scratch, cudaStream_t st,
+                            unsigned long long selftest_ns = 0);      // not 0: no products, a wait that runs out
 
 }  // namespace emu

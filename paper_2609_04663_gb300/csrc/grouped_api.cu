@@ -523,10 +523,11 @@ size_t emu_i8_gemm_workspace_bytes(int64_t G, int64_t rows, int64_t N, int64_t K
     return scratch ? kWsHeaderBytes + scratch : 0;
 }
 
-emu_status emu_i8_gemm(int64_t G, int64_t rows, int64_t N, int64_t K, const int8_t *X, int64_t xrows, int64_t ldx,
-                       const float *xscales, const int32_t *src, const int8_t *W, int64_t ldw, int64_t stridew,
-                       const float *wscales, const int32_t *ends, void *Y, int ytype, int64_t ldy, void *ws,
-                       size_t ws_bytes, emu_stream_t stream)
+// selftest_ns: launch_i8_batch's, 0 for a product.
+static emu_status i8_gemm(int64_t G, int64_t rows, int64_t N, int64_t K, const int8_t *X, int64_t xrows, int64_t ldx,
+                          const float *xscales, const int32_t *src, const int8_t *W, int64_t ldw, int64_t stridew,
+                          const float *wscales, const int32_t *ends, void *Y, int ytype, int64_t ldy, void *ws,
+                          size_t ws_bytes, emu_stream_t stream, unsigned long long selftest_ns)
 {
     if ((ytype != EMU_F32 && ytype != EMU_BF16 && ytype != EMU_I32) || xrows < 0 || ldx < K || ldw < K || ldy < N ||
         (G > 1 && stridew < 0) || (!ends && G != 1) || (!src && xrows < rows) ||
@@ -553,10 +554,31 @@ emu_status emu_i8_gemm(int64_t G, int64_t rows, int64_t N, int64_t K, const int8
     p.X = X; p.W = W; p.xscales = xscales; p.wscales = wscales; p.src = src; p.ends = ends; p.xrows = xrows; p.ldx = ldx;
     p.ldw = ldw; p.stridew = G > 1 ? stridew : 0; p.ldy = ldy; p.Y = Y; p.ytype = ytype; p.G = (int)G; p.rows = (int)rows;
     p.N = (int)N; p.K = (int)K; p.flags = ws ? &static_cast<WsHeader *>(ws)->flags : nullptr;
-    if (i8_few_rows(G, rows, N, K)) return cuda_status(launch_i8_rows(p, st));
+    const bool few = i8_few_rows(G, rows, N, K);
+    const int parts = few ? 0 : i8_batch_parts(G, rows, N, K);
+    if (selftest_ns && !parts) return EMU_ERR_UNSUPPORTED;
+    if (few) return cuda_status(launch_i8_rows(p, st));
     void *scratch = ws ? static_cast<char *>(ws) + kWsHeaderBytes : nullptr;
-    const int parts = i8_batch_parts(G, rows, N, K);
-    return cuda_status(parts ? launch_i8_batch(p, parts, scratch, st) : launch_i8_tile(p, scratch, st));
+    return cuda_status(parts ? launch_i8_batch(p, parts, scratch, st, selftest_ns) : launch_i8_tile(p, scratch, st));
+}
+
+emu_status emu_i8_gemm(int64_t G, int64_t rows, int64_t N, int64_t K, const int8_t *X, int64_t xrows, int64_t ldx,
+                       const float *xscales, const int32_t *src, const int8_t *W, int64_t ldw, int64_t stridew,
+                       const float *wscales, const int32_t *ends, void *Y, int ytype, int64_t ldy, void *ws,
+                       size_t ws_bytes, emu_stream_t stream)
+{
+    return i8_gemm(G, rows, N, K, X, xrows, ldx, xscales, src, W, ldw, stridew, wscales, ends, Y, ytype, ldy, ws, ws_bytes,
+                   stream, 0);
+}
+
+emu_status emu_selftest_i8_timeout(uint32_t timeout_us, int64_t G, int64_t rows, int64_t N, int64_t K, const int8_t *X,
+                                   int64_t xrows, int64_t ldx, const float *xscales, const int32_t *src, const int8_t *W,
+                                   int64_t ldw, int64_t stridew, const float *wscales, const int32_t *ends, void *Y,
+                                   int ytype, int64_t ldy, void *ws, size_t ws_bytes, emu_stream_t stream)
+{
+    if (timeout_us < 1 || timeout_us > 1000000 || !ws || rows < 1 || N < 1 || K < 1) return EMU_ERR_INVALID_ARG;
+    return i8_gemm(G, rows, N, K, X, xrows, ldx, xscales, src, W, ldw, stridew, wscales, ends, Y, ytype, ldy, ws, ws_bytes,
+                   stream, 1000ull * timeout_us);
 }
 
 }  // extern "C"

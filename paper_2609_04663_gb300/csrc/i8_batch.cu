@@ -48,7 +48,8 @@ struct BatchArgs {
     int64_t ldr;
     int copied;
     int parts, shift;                 // CTAs of a cluster, each with a part of K; the number's logarithm
-    int own_flags;                    // one warp looks at all rows and sets the flag word; else it is zero, and all CTAs look
+    int own_flags;                    // the first CTA clears the flag word and looks at all rows; else it is clear, and all CTAs look
+    unsigned long long selftest_ns;   // not 0: nothing is multiplied, and a wait for weights runs out after so long
 };
 
 __device__ uint32_t unread_flags;     // of calls without a workspace
@@ -130,6 +131,8 @@ i8_batch_kernel(const __grid_constant__ CUtensorMap tmW, const BatchArgs a)
     if (warp == Cfg::MMA) { tmem_alloc(smem_u32((const void *)tmem_slot), 512); tmem_relinquish(); }
     // the set-up above overlaps the end of the kernel before this one where that allows it
     griddep_wait();
+    // before any wait of this CTA can give up (those of others take seconds): flags are only added from here on
+    if (threadIdx.x == 0 && blockIdx.x == 0 && a.own_flags && a.p.flags) *a.p.flags = 0u;
     if (a.p.ends) {
         (void)load_groups(a.p.ends, a.p.G, a.p.rows, starts);
     } else if (threadIdx.x == 0) {
@@ -142,7 +145,7 @@ i8_batch_kernel(const __grid_constant__ CUtensorMap tmW, const BatchArgs a)
     __syncthreads();
     tc_fence_after();
     if (a.parts > 1) cluster_arrive();                // this CTA's barriers are initialised
-    const int total = uniform(tpre[a.p.G]);
+    const int total = a.selftest_ns ? 0 : uniform(tpre[a.p.G]);
     const uint32_t tmem = (uint32_t)uniform((int)*tmem_slot);
     const int first = (int)blockIdx.x >> a.shift, step = (int)gridDim.x >> a.shift;
     auto tile = [&](int t) { return batch_tile(t, a, starts, tpre, rank); };
@@ -368,6 +371,7 @@ i8_batch_kernel(const __grid_constant__ CUtensorMap tmW, const BatchArgs a)
                         if (++s == Cfg::NW) { s = 0; ph ^= 1u; }
                     }
                 }
+                if (a.selftest_ns) (void)mbar_wait(wfull0, 0, flags, a.selftest_ns);
                 if (!ok) drain_inflight(wfull0, Cfg::NW, issued, flags);
             }
             __syncwarp();
@@ -388,11 +392,7 @@ i8_batch_kernel(const __grid_constant__ CUtensorMap tmW, const BatchArgs a)
                     }
                 }
                 bad = __any_sync(0xFFFFFFFFu, bad);
-                if (lane == 0) {
-                    // (the only other flag, a wait that gave up, comes seconds later)
-                    if (a.own_flags) *flags = bad ? (uint32_t)EMU_FLAG_INDEX : 0u;
-                    else if (bad) atomicOr(flags, (uint32_t)EMU_FLAG_INDEX);
-                }
+                if (lane == 0 && bad) atomicOr(flags, (uint32_t)EMU_FLAG_INDEX);
             }
         } else if (warp == Cfg::MMA) {
             // ---------------- MMA issuer.  Contraction elements past K are zero in both operands, so
@@ -456,7 +456,7 @@ size_t i8_batch_scratch_bytes(int64_t G, int64_t rows, int64_t N, int64_t K, boo
 }
 
 // scratch: i8_batch_scratch_bytes, 16-byte aligned; NULL where X and W can be read as they stand.
-cudaError_t launch_i8_batch(I8Product p, int parts, void *scratch, cudaStream_t st)
+cudaError_t launch_i8_batch(I8Product p, int parts, void *scratch, cudaStream_t st, unsigned long long selftest_ns)
 {
     // the warps' shares of the registers have to fit what the launch has, or they would be waited for without end
     static std::atomic<int> fit{0};
@@ -489,6 +489,7 @@ cudaError_t launch_i8_batch(I8Product p, int parts, void *scratch, cudaStream_t 
     a.p = p;
     a.parts = parts;
     while (1 << a.shift < parts) ++a.shift;
+    a.selftest_ns = selftest_ns;
     a.own_flags = p.rows <= 4096;
     if (p.flags && !a.own_flags) {
         const cudaError_t e = cudaMemsetAsync(p.flags, 0, sizeof(uint32_t), st);
