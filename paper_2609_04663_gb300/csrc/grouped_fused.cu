@@ -3,9 +3,9 @@
 // to the tensor cores, instead of being written and read again as planes (10
 // bytes of traffic per element more than the 4 that are needed).  Bound by the
 // way of a K-block through the split (HBM latency, 16 warps' splitting, MMAs) and
-// by HBM's rate behind it.  16 matrices of 1024 x 2048 with the rows' split: 37 us
-// for one row each, 38 for 16, 44 for 64, 115 for 256; 8 of 4096 x 4096 with 8 rows
-// each: 125 us (4.3 TB/s).
+// by HBM's rate behind it.  16 matrices of 1024 x 2048 with the rows' split: 39 us
+// for one row each, 40 for 16, 44 for 64, 114 for 256; 8 of 4096 x 4096 with 8 rows
+// each: 126 us (4.3 TB/s).
 //
 // Tiles and products are those of grouped.cu with one CTA per tile (128
 // features x up to 64 rows).  The leading products A0B0 of every 256 elements
@@ -35,6 +35,16 @@ __device__ __forceinline__ float4 lds_f4(uint32_t a)
     float4 v;
     asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a));
     return v;
+}
+
+// Gives a stage of weights back to TMA, by lane 0, once the loads from it have arrived in all lanes: an arrival does not
+// wait for a thread's loads from shared memory, and where a box lies past the end of a matrix TMA writes its zeros at once.
+// top: the largest magnitude's bits of what was loaded, below 2^31; never: a larger number that the
+// compiler does not know.  The arrival is made where no lane's top is that, which needs all of them.
+// (Arriving behind the stores of the slices instead: 45 us against 41 for 256 rows over 16 matrices of 1024 x 2048, unevenly.)
+__device__ __forceinline__ void arrive_behind_loads(uint32_t bar, int lane, uint32_t top, uint32_t never)
+{
+    if (__all_sync(0xFFFFFFFFu, top != never) && lane == 0) mbar_arrive(bar);
 }
 
 constexpr int kCols = 64;                             // rows of X per tile at most
@@ -113,15 +123,17 @@ grouped_fused_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_const
             ok = __all_sync(0xFFFFFFFFu, mbar_wait(wfull0 + 8u * ws, wph, flags));
             if (!ok) break;
             float4 w[kRuns][2];
+            uint32_t top = 0;
 #pragma unroll
             for (int r = 0; r < kRuns; ++r) {
                 const uint32_t at = from + ws * Cfg::W_TILE + (uint32_t)(r * RSTEP * (LMN ? 512 : 256));
                 const float4 u = lds_f4(at + (swap ? 16u : 0u)), v = lds_f4(at + (swap ? 0u : 16u));
                 w[r][0] = swap ? v : u;
                 w[r][1] = swap ? u : v;
+                top = max(top, max(abs_bits_max(abs_bits_max(0u, u.x, u.y), u.z, u.w), abs_bits_max(abs_bits_max(0u, v.x, v.y), v.z, v.w)));
             }
-            __syncwarp();
-            if (lane == 0) mbar_arrive(wempty0 + 8u * ws);
+            arrive_behind_loads(wempty0 + 8u * ws, lane, top, a.never);
+            amax = max(amax, top);
             if (++ws == Cfg::W_STAGES) { ws = 0; wph ^= 1u; }
             // split before the stage is waited for: between its release and the
             // next MMAs only the stores are left
@@ -129,7 +141,6 @@ grouped_fused_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_const
 #pragma unroll
             for (int r = 0; r < kRuns; ++r) {
                 const float4 u = w[r][0], v = w[r][1];
-                amax = abs_bits_max(abs_bits_max(abs_bits_max(abs_bits_max(amax, u.x, u.y), u.z, u.w), v.x, v.y), v.z, v.w);
                 split_pair(u.x, u.y, p[r][0].x, p[r][1].x, p[r][2].x);
                 split_pair(u.z, u.w, p[r][0].y, p[r][1].y, p[r][2].y);
                 split_pair(v.x, v.y, p[r][0].z, p[r][1].z, p[r][2].z);
@@ -326,6 +337,7 @@ cudaError_t launch_grouped_fused(bool trans, int64_t G, int64_t rows, int64_t N,
 {
     GroupedArgs a = {};
     a.ends = ends; a.G = (int)G; a.rows = (int)rows; a.L = (int)N; a.K = (int)K;
+    a.never = 0xFFFFFFFFu;
     a.padded = X.padded ? 1 : 0; a.out = Y; a.ldo = ldy; a.out_f32 = 1; a.flags = flags;
     CUtensorMap tw, tc, ts;
     const bool ok = trans ? make_weight_map(&tw, W, K, N, G, ldw, stridew, kKB, kLRows)

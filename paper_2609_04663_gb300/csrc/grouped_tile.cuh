@@ -27,6 +27,7 @@ struct GroupedArgs {
     int lwide, cwide;      // the MN-major operand's tensor map loads two blocks of 64 at once
     uint32_t *flags;
     int own_flags;         // the flag word is this kernel's alone: it is set, not added to
+    uint32_t never;        // grouped_fused.cu: 2^32 - 1, as a number that the compiler does not know
 };
 
 // BF16 operands (grouped_bf16.cu).
