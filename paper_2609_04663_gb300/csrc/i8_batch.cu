@@ -3,17 +3,21 @@
 //
 // Warps 0-3 read the accumulators and store.  Warps 4-11 turn the token rows into FP16 in swizzled shared
 // memory, gathered, two warps a stage of 128 codes in turn: a thread asks for its runs of 16 codes of its group's
-// next stage once it has handed over the one before.  (An arrival, like the fence that shows a stage to the tensor
-// cores, waits for all loads that its thread has in flight: two stages ahead in two groups were none, 58.6 us for 256 rows over
+// next stage once it has handed over the one before.  (The fence that shows a stage to the tensor cores, and the arrival
+// behind it, wait for all loads from global memory that a thread has in flight, as measured; not for those from shared
+// memory, see convert_weights: two stages ahead in two groups were none, 58.6 us for 256 rows over
 // 32 experts of 2048 x 4096 against 51.)  Warps 12-19 convert weights, 20 brings them by TMA and looks for
 // bad indexes, 21 issues the MMAs.
 //
 // While there are SMs left, K is split between the CTAs of a cluster; each adds and stores a share of the columns,
 // whose other sums it reads from their shared memory.
 //
-// 48 rows x 5120 x 8192 take 18.1 us (HBM alone would 6.5), 64 x 4096 x 4096 13.2, 256 rows over 32 experts of
-// 2048 x 4096 51 (5.3 TB/s): bound by a stage's way through the warps, 185-245 ns for 64 codes (without loads of rows 16.9
-// and 49 us, without converting weights as well 15.5 and 47), and by start and end of the launch, 4 us, with parts 6.
+// 48 rows x 5120 x 8192 take 18.2 us (HBM alone would 6.5): 1.2 us until all is set up, 3.5 until the first stage's rows and
+// weights are there, 2.5 for the next four stages, 6.4 for the other 16 (0.39 each), 4 from the last
+// accumulator until the two parts' sums have been handed over, added and stored, 0.6 to the end (a clock read by a CTA at
+// each).  64 x 4096 x 4096 13.4, of which handing over to storing takes 3.9.  16 x 16384 x 16384, without parts, 52: 0.4 for each
+// of 128 stages and 0.7 for storing.  256 rows over 32 experts of 2048 x 4096 51 (5.3 TB/s).  (Without loads of rows 16.9 and
+// 49 us for the first and the last, without converting weights as well 15.5 and 47.)
 // Tried: all eight row warps on each stage, with the bytes brought to L1 ahead, 64 us for the 256 rows; a third group of
 // converting warps 60 against 58.6; the first CTA of a cluster adding and storing all columns 16 us for the 64 rows.
 #include "i8_tile.cuh"

@@ -10,7 +10,7 @@
 // Output features lie on the MMA's rows, token rows on its columns (as in grouped.cu).  The
 // weights cross HBM and L2 as bytes; eight warps turn them into FP16 and write them to tensor memory, from
 // which the MMA takes its first operand: the byte u = code + 128 in the mantissa of
-// 1024 + u, less 1152 (five instructions for four codes).
+// 1024 + u, less 1152 (five instructions for four codes; a published method, the constants follow from FP16's layout).
 #pragma once
 #include "grouped_tile.cuh"
 #include "i8_common.cuh"
@@ -115,7 +115,7 @@ __device__ __forceinline__ void clear_rows(const I8Product &p, int64_t row, uint
 // -> FP16 in tensor memory at `to`.  In between, `wait` waits until the MMAs have used what was there; false
 // when it gave up.  was_read gives the stage of bytes back to TMA: after the stores to tensor
 // memory, which cannot be issued before all that was loaded has arrived.  (Right after the loads it came too
-// early: an arrival does not wait for them, and where a box lies past the end of the rows TMA writes its zeros at
+// early: an arrival does not wait for loads from shared memory, and where a box lies past the end of the rows TMA writes its zeros at
 // once.  Last codes of a stage came out as zero in one of a hundred products of 1030 rows x 2064 x 700.)
 template <typename Read, typename Wait>
 __device__ __forceinline__ bool convert_weights(uint32_t from, int first, int row, uint32_t to, bool there, Read &&was_read, Wait &&wait)
